@@ -268,3 +268,9 @@ def clsa_version() -> int:
 def raw():
     """The ctypes library handle (status codes returned, nothing raised) for tests of the error paths."""
     return _lib
+
+
+# The 8-bit cache calls (include/clsa_cache8.h).
+from .cache8 import (CLSA_DEV_BAD_SCALE_BLOCK, EXPORTS_CACHE8, clsa_cache8, clsa_cache8_append,  # noqa: E402
+                     clsa_cache8_workspace_bytes, clsa_heads, clsa_index_scores8, clsa_norm_rope, clsa_norm_rope_spec,
+                     clsa_sparse_attn8, make_cache8, make_norm_rope)

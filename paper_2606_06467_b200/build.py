@@ -9,7 +9,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libclsa.so")
-SOURCES = ["api.cu", "index_scores.cu", "index_gemm.cu", "index_topk.cu", "topk.cu", "topk_filter.cu", "sparse_attn.cu", "sparse_attn_sk.cu", "project_append.cu"]
+SOURCES = ["api.cu", "index_scores.cu", "index_gemm.cu", "index_topk.cu", "topk.cu", "topk_filter.cu", "sparse_attn.cu", "sparse_attn_sk.cu", "project_append.cu",
+           "api_cache8.cu", "norm_rope.cu", "cache8_append.cu", "index_scores8.cu", "sparse_attn8.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
@@ -33,7 +34,7 @@ def _stale(target: str, deps) -> bool:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
-    headers.append(os.path.join(ROOT, "include", "clsa.h"))
+    headers += [os.path.join(ROOT, "include", f) for f in ("clsa.h", "clsa_cache8.h")]
     objdir = os.path.join(PKG, "build")
     os.makedirs(objdir, exist_ok=True)
     objs, procs = [], []

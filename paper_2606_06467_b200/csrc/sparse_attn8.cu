@@ -1,0 +1,623 @@
+// GQA sparse attention over the selected rows of an 8-bit K and V cache (Eq. 4), one launch per layer, T >= 1.
+//
+//   x_s = sm_scale * (q . code_K[s]) * 2^ek,   O = sum_s exp(x_s) 2^ev code_V[s] / sum_s exp(x_s)
+// with ek, ev the exponents of the scale blocks that row s lies in. In the log2 domain a query head keeps two running
+// references: m near the largest x_s + ev for the numerators, whose weights 2^(x_s + ev - m) go to the matrix instructions as
+// f16, and mx near the largest x_s for the denominators 2^(x_s - mx), so that neither underflows however far apart the blocks'
+// scales lie; the difference of the two is applied to the finished quotient. References move only when a weight would
+// exceed 2^8 (one vote per stage): a stage that moves none needs no reduction over its tokens.
+//
+// The work is a flat list of 16-token stages, unit = (KV head, query row), heads outermost, so that a prefill chunk's launch
+// goes over one head's part of the cache (which fits in L2) before the next. Warp w of W takes a contiguous span of the list
+// (unit-aligned where that splits evenly); a warp streams its span through a private ring of cp.async stages of 16 tokens,
+// 128 bytes of K and of V each. e4m3 codes convert to f16 exactly, so the products are those of the stored values, and sums are
+// fp32. A warp-level instruction takes 16 tokens (along M) against up to 8 query heads of the GQA group (along N):
+//   S^T[16 x 8] = K[16 x 128] Q^T: four lanes share a token; a lane takes 16-byte chunks j and j + 4 of its row, whose words
+//     are its share of the eight steps (the contraction index is a dummy, q is laid out to match);
+//   O^T[128 x 8] += V^T[128 x 16] P^T: a transposing matrix load hands a lane the byte pairs (d, d + 1) of two tokens; one
+//     byte permutation makes them (token, token + 1) pairs of d and of d + 1, which go to rows g and g + 8 of the instruction.
+// Units that several warps share are merged by log-sum-exp: partial results meet in shared memory, those of units that straddle
+// blocks in global slots (two per block) with an arrival counter; the block that arrives last reads them in block order, so
+// results do not depend on timing, and puts the counter back to zero.
+#include "attn_common.cuh"
+#include "cache8.cuh"
+
+namespace clsa {
+namespace {
+
+constexpr int kTok = 16;                  // tokens per stage
+constexpr int kStage8Bytes = kTok * 256;  // K rows, then V rows, 128 bytes each
+constexpr int kMaxGroup = 16;
+constexpr int kMinStages8 = 2;            // shorter spans cost more in partials than they return in parallelism
+constexpr float kLazy = 8.f;              // a weight may exceed the reference by 2^8 before the reference moves
+
+struct Attn8Args {
+  const uint16_t* q;
+  const uint8_t* kc;
+  const uint8_t* vc;
+  const uint8_t* ks;
+  const uint8_t* vs;
+  int64_t head_stride, scale_head;
+  uint32_t stride16;  // token stride in 16-byte units
+  int scale_shift;
+  int64_t num_rows;
+  const int64_t* seq_start;
+  const int32_t* seq_len;
+  const int32_t* idx;
+  const int32_t* count;
+  const int32_t* block_table;
+  int block_shift, max_blocks;
+  uint16_t* out;
+  float* lse;
+  uint32_t* status;
+  int rows, q_per_seq, num_q_heads, num_kv_heads, group, top_k, max_seq_len;
+  int reverse, early, keep, pin;
+  int unit_stages, total_stages;
+  int aligned, span_q, span_rem, workers, wpb;
+  float* part;       // records of [group][kPartialStride] floats: W of the workers, then 2 per block
+  uint32_t* arrive;  // [blocks][group] arrival counters of the unit that leaves block b to the right, zero between launches
+  float scale_log2;
+};
+
+// First stage of worker w's span (aligned: unit u has span_q workers, the first span_rem units one more, its stages cut evenly
+// over them; flat: the first span_rem workers take span_q + 1 consecutive stages, the others span_q).
+__device__ __forceinline__ int span_begin(int w, const Attn8Args& a) {
+  if (!a.aligned) return w * a.span_q + min(w, a.span_rem);
+  const int big = a.span_rem * (a.span_q + 1);
+  int u, j, n;
+  if (w < big) { n = a.span_q + 1; u = w / n; j = w - u * n; }
+  else { n = a.span_q; const int w2 = w - big; u = w2 / n; j = w2 - u * n; u += a.span_rem; }
+  return u * a.unit_stages + (int)((int64_t)j * a.unit_stages / n);
+}
+__device__ __forceinline__ void unit_workers(int u, const Attn8Args& a, int& first, int& last) {
+  if (a.aligned) {
+    first = u * a.span_q + min(u, a.span_rem);
+    last = first + a.span_q + (u < a.span_rem ? 1 : 0) - 1;
+  } else {
+    const int big = a.span_rem * (a.span_q + 1);
+    auto owner = [&](int s) { return s < big ? s / (a.span_q + 1) : a.span_rem + (s - big) / a.span_q; };
+    first = owner(u * a.unit_stages);
+    last = owner(u * a.unit_stages + a.unit_stages - 1);
+  }
+}
+
+// Where chunk c (16 bytes) of token j of a stage lies: lanes (two rows, four chunks) of a 16-byte read, and eight rows of one
+// chunk of a transposing matrix load, fall into different banks.
+__device__ __forceinline__ uint32_t chunk_at(int j, int c) {
+  const int f = ((j & 1) << 2) | (j & 2) | ((j & 4) >> 2);
+  return (uint32_t)(j * 128 + ((c ^ f) << 4));
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+
+template <int NT, int WARPS, int STAGES>
+struct Shape {
+  static constexpr int kRing = STAGES * kStage8Bytes;
+  static constexpr int kScale = STAGES * kTok * 8;  // per token: 2^ek, ev
+  static constexpr size_t kSmem = (size_t)WARPS * (kRing + kScale + STAGES * 4) + WARPS * sizeof(int2);
+};
+
+template <int NT, int WARPS, int STAGES, bool PAGED>
+__global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __grid_constant__ Attn8Args a) {
+  using S = Shape<NT, WARPS, STAGES>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rowq = lane >> 2, j4 = lane & 3, hcol = 2 * j4;
+  const int G = a.group, NS = a.unit_stages, W = a.workers;
+  const int w = (int)blockIdx.x * a.wpb + warp;
+  const bool has_work = warp < a.wpb && w < W;
+  const int s_begin = has_work ? span_begin(w, a) : 0;
+  const int s_end = has_work ? (w + 1 < W ? span_begin(w + 1, a) : a.total_stages) : 0;
+  unsigned char* ring = smem + warp * S::kRing;
+  const uint32_t ring_u32 = smem_u32(ring);
+  float2* scales = reinterpret_cast<float2*>(smem + WARPS * S::kRing + warp * S::kScale);
+  uint32_t* stage_mask = reinterpret_cast<uint32_t*>(smem + WARPS * (S::kRing + S::kScale)) + warp * STAGES;
+  int2* span_tab = reinterpret_cast<int2*>(smem + WARPS * (S::kRing + S::kScale + STAGES * 4));
+  if (lane == 0) span_tab[warp] = make_int2(s_begin, s_end);
+
+  // Programmatic dependent launch, as in the bf16 kernels: dependents are released only behind this grid's own wait.
+  bool waited = false;
+  auto wait_now = [&]() {
+    if (!waited) {
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+      waited = true;
+    }
+  };
+  if (!a.early) wait_now();
+
+  const uint64_t pol_keep = a.keep ? l2_policy_evict_last() : l2_policy_evict_normal();
+  const uint64_t pol_last = l2_policy_evict_last(), pol_first = l2_policy_evict_first();
+  uint32_t dst[4];  // this lane's 16-byte chunk of token 4 * it + lane / 8
+#pragma unroll
+  for (int it = 0; it < 4; ++it) dst[it] = chunk_at(4 * it + (lane >> 3), lane & 7);
+
+  int cur = a.reverse ? s_end : s_begin;
+  while (a.reverse ? cur > s_begin : cur < s_end) {
+    // ---- the next segment of this worker's span: stages [seg_lo, seg_hi) of unit u --------------------------------
+    const int u = (a.reverse ? cur - 1 : cur) / NS;
+    const int seg_lo = max(s_begin, u * NS), seg_hi = min(s_end, (u + 1) * NS);
+    cur = a.reverse ? seg_lo : seg_hi;
+    const int g = u / a.rows, r = u - g * a.rows;
+    const int h0 = g * G, b = r / a.q_per_seq;
+    const int slot_lo = (seg_lo - u * NS) * kTok;
+    const int slot_hi = min(a.top_k, (seg_hi - u * NS) * kTok);
+    const int32_t* row_idx = a.idx + (int64_t)r * a.top_k;
+    int cnt = a.count[r];
+    const int n_raw = a.seq_len[b];
+    const bool n_ok = n_raw >= a.q_per_seq && n_raw <= a.max_seq_len;
+    const int n = n_ok ? n_raw : 0;  // a sequence with a bad length is never read: no position passes the range check
+    const int64_t start = PAGED ? 0 : a.seq_start[b];
+    const int32_t* table = PAGED ? a.block_table + (int64_t)b * a.max_blocks : nullptr;
+    const bool first_of_row = slot_lo == 0 && g == 0;
+    if (cnt < 0 || cnt > a.top_k) {
+      if (lane == 0 && first_of_row) flag_status(a.status, CLSA_DEV_BAD_COUNT);
+      cnt = cnt < 0 ? 0 : a.top_k;
+    }
+    const int t_lo = min(cnt, slot_lo), t_hi = min(cnt, slot_hi);
+    const int nstages = (t_hi - t_lo + kTok - 1) / kTok;
+
+    float o[NT][8][4];
+    float m[NT][2], mx[NT][2], l[NT][2];  // references and this lane's share of the denominators, heads hcol and hcol + 1
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = mx[nt][0] = mx[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) { o[nt][c][0] = 0.f; o[nt][c][1] = 0.f; o[nt][c][2] = 0.f; o[nt][c][3] = 0.f; }
+    }
+
+    if (nstages > 0) {
+      const uint8_t* kbase = a.kc + g * a.head_stride + (lane & 7) * 16;
+      const uint8_t* vbase = a.vc + g * a.head_stride + (lane & 7) * 16;
+      const uint8_t* sbase = (lane < kTok ? a.ks : a.vs) + g * a.scale_head;  // lanes 0..15: K's scales, 16..31: V's
+      auto stage_t0 = [&](int i) { return t_lo + (a.reverse ? nstages - 1 - i : i) * kTok; };
+      auto load_raw = [&](int i) -> int {  // lanes k and k + 16: position of token k of step i (-1 past the end)
+        const int tt = stage_t0(i) + (lane & 15);
+        return i < nstages && tt < t_hi ? row_idx[tt] : -1;
+      };
+      auto load_blk = [&](int raw) -> int { return PAGED && raw >= 0 && raw < n ? __ldg(table + (raw >> a.block_shift)) : 0; };
+      auto settle = [&](int i, int byte) {  // the scale bytes of stage i into shared memory
+        if (i < nstages) {
+          const int e = scale_exponent(byte);
+          float* dstf = reinterpret_cast<float*>(scales + (i % STAGES) * kTok + (lane & 15));
+          dstf[lane >> 4] = lane < kTok ? exp2_int(e) : (float)e;
+        }
+      };
+      auto issue = [&](int i, int raw, int blk) -> int {  // the copies of stage i; returns its scale bytes, still in flight
+        int byte = 127;
+        if (i < nstages) {
+          const int buf = i % STAGES;
+          const uint32_t kdst = ring_u32 + buf * kStage8Bytes, vdst = kdst + kStage8Bytes / 2;
+          const uint64_t pol = a.pin < 0 ? pol_keep : (pin_rank((stage_t0(i) >> 4) & 7) < a.pin ? pol_last : pol_first);
+          const int64_t row = PAGED ? ((int64_t)blk << a.block_shift) + (raw & ((1 << a.block_shift) - 1)) : start + raw;
+          const bool ok = raw >= 0 && raw < n && row >= 0 && row < a.num_rows;
+          const uint32_t okmask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
+          if (!ok && n_ok && lane < kTok && stage_t0(i) + lane < t_hi) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+          if (lane == 0) stage_mask[buf] = okmask;
+          if (ok) byte = sbase[row >> a.scale_shift];
+          const uint32_t my16 = ok ? (uint32_t)row * a.stride16 : 0u;  // 16-byte units: the caches span less than 2^32 of them
+          if (okmask == 0xffffu) {
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+              const uint32_t off = __shfl_sync(0xffffffffu, my16, 4 * it + (lane >> 3));
+              cp_async16_full(kdst + dst[it], kbase + (uint64_t)off * 16u, pol);
+              cp_async16_full(vdst + dst[it], vbase + (uint64_t)off * 16u, pol);
+            }
+          } else {
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+              const int jt = 4 * it + (lane >> 3);
+              const uint32_t off = __shfl_sync(0xffffffffu, my16, jt);
+              const bool okj = (okmask >> jt) & 1u;
+              cp_async16(kdst + dst[it], kbase + (uint64_t)off * 16u, okj, pol);
+              cp_async16(vdst + dst[it], vbase + (uint64_t)off * 16u, okj, pol);
+            }
+          }
+        }
+        cp_async_commit();
+        return byte;
+      };
+
+      // Prologue: the ring filled, the positions of the two stages behind it and the page numbers of the first in registers.
+      int raw_p[STAGES], blk_p[STAGES];
+#pragma unroll
+      for (int i = 0; i < STAGES; ++i) raw_p[i] = load_raw(i);
+      int rawX = load_raw(STAGES), rawY = load_raw(STAGES + 1);
+#pragma unroll
+      for (int i = 0; i < STAGES; ++i) blk_p[i] = load_blk(raw_p[i]);
+#pragma unroll
+      for (int i = 0; i < STAGES; ++i) raw_p[i] = issue(i, raw_p[i], blk_p[i]);
+      int blkX = load_blk(rawX);
+      wait_now();  // with only q pending, everything read so far was complete before this launch; q is read behind the wait
+
+      // q as f16: column = head, the lane's words of step (half, w) hold dimensions 16 (j4 + 4 half) + 4 w .. + 3. Scaled by a
+      // power of two so that the head's largest magnitude lies in [2^13, 2^14).
+      uint32_t qb[NT][8][2];
+      float qf[NT][2];
+      const uint16_t* qbase = a.q + ((int64_t)r * a.num_q_heads + h0) * 128;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int head = nt * 8 + rowq;
+        float amax = 0.f;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+          if (head < G) {
+            const uint4* src = reinterpret_cast<const uint4*>(qbase + head * 128 + 16 * (j4 + 4 * hf));
+            v[0] = src[0];
+            v[1] = src[1];
+          }
+          const uint32_t raw8[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            qb[nt][hf * 4 + i / 2][i & 1] = raw8[i];
+            const float lo = fabsf(bf16_lo(raw8[i])), hi = fabsf(bf16_hi(raw8[i]));
+            if (lo <= 3.4028234663852886e38f) amax = fmaxf(amax, lo);  // finite
+            if (hi <= 3.4028234663852886e38f) amax = fmaxf(amax, hi);
+          }
+        }
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        const int shift = min(13 + 127 - (int)(__float_as_uint(amax) >> 23), 120);
+        const float up = exp2_int(shift), down = exp2_int(-shift);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) qb[nt][i][k] = pack_f16x2(bf16_lo(qb[nt][i][k]) * up, bf16_hi(qb[nt][i][k]) * up);
+        qf[nt][0] = __shfl_sync(0xffffffffu, down, 4 * hcol) * a.scale_log2;
+        qf[nt][1] = __shfl_sync(0xffffffffu, down, 4 * hcol + 4) * a.scale_log2;
+      }
+
+#pragma unroll
+      for (int i = 0; i + 1 < STAGES; ++i) settle(i, raw_p[i]);
+      int pend = raw_p[STAGES - 1];  // settled one iteration after its stage was issued
+#pragma unroll 1
+      for (int i = 0; i < nstages; ++i) {
+        const int raw_new = load_raw(i + STAGES + 2);
+        const int blk_new = load_blk(rawY);
+        cp_async_wait<STAGES - 1>();
+        __syncwarp();
+        const int buf = i % STAGES;
+        const uint32_t kbuf = ring_u32 + buf * kStage8Bytes, vbuf = kbuf + kStage8Bytes / 2;
+        const uint32_t okmask = stage_mask[buf];
+        const float2 sc_lo = scales[buf * kTok + rowq], sc_hi = scales[buf * kTok + rowq + 8];  // tokens rowq, rowq + 8
+        float s[NT][2][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) { s[nt][k][0] = 0.f; s[nt][k][1] = 0.f; s[nt][k][2] = 0.f; s[nt][k][3] = 0.f; }
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const uint4 lo = lds128(kbuf + chunk_at(rowq, j4 + 4 * hf)), hi = lds128(kbuf + chunk_at(rowq + 8, j4 + 4 * hf));
+          const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t a0 = e4m3x2_to_f16x2(wl[k]), a2 = e4m3x2_hi_to_f16x2(wl[k]);
+            const uint32_t a1 = e4m3x2_to_f16x2(wh[k]), a3 = e4m3x2_hi_to_f16x2(wh[k]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt][k & 1], a0, a1, a2, a3, qb[nt][hf * 4 + k][0], qb[nt][hf * 4 + k][1]);
+          }
+        }
+        // x of the lane's two tokens and two heads
+        float x[NT][4];
+        bool move = false;
+        const bool ok_lo = (okmask >> rowq) & 1u, ok_hi = (okmask >> (rowq + 8)) & 1u;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const float2& sc = i4 < 2 ? sc_lo : sc_hi;
+            const float v = (s[nt][0][i4] + s[nt][1][i4]) * sc.x * qf[nt][i4 & 1];
+            x[nt][i4] = (i4 < 2 ? ok_lo : ok_hi) ? v : -INFINITY;
+            move = move || x[nt][i4] > mx[nt][i4 & 1] + kLazy || x[nt][i4] + sc.y > m[nt][i4 & 1] + kLazy;
+          }
+        }
+        if (__any_sync(0xffffffffu, move)) {  // some head's references have to move: to the largest seen so far
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float top = fmaxf(x[nt][k], x[nt][k + 2]), tope = fmaxf(x[nt][k] + sc_lo.y, x[nt][k + 2] + sc_hi.y);
+#pragma unroll
+              for (int d = 4; d <= 16; d <<= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                tope = fmaxf(tope, __shfl_xor_sync(0xffffffffu, tope, d));
+              }
+              top = fmaxf(mx[nt][k], top);
+              tope = fmaxf(m[nt][k], tope);
+              l[nt][k] *= top == -INFINITY ? 1.f : fast_exp2(mx[nt][k] - top);
+              const float alpha = tope == -INFINITY ? 1.f : fast_exp2(m[nt][k] - tope);
+              mx[nt][k] = top;
+              m[nt][k] = tope;
+#pragma unroll
+              for (int c = 0; c < 8; ++c) { o[nt][c][k] *= alpha; o[nt][c][k + 2] *= alpha; }
+            }
+        }
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float pv[4];
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const float2& sc = i4 < 2 ? sc_lo : sc_hi;
+            const bool none = m[nt][i4 & 1] == -INFINITY;  // every token so far masked
+            l[nt][i4 & 1] += none ? 0.f : fast_exp2(x[nt][i4] - mx[nt][i4 & 1]);
+            pv[i4] = none ? 0.f : fast_exp2(x[nt][i4] + sc.y - m[nt][i4 & 1]);
+          }
+          // held [token][head]; the second product wants [head][token]
+          pb[nt][0] = movmatrix_trans(pack_f16x2(pv[0], pv[1]));
+          pb[nt][1] = movmatrix_trans(pack_f16x2(pv[2], pv[3]));
+        }
+#pragma unroll
+        for (int c = 0; c < 8; c += 2) {
+          const int mi = lane >> 3;
+          uint32_t v[4];  // (chunk c, tokens 0-7), (c, 8-15), (c + 1, 0-7), (c + 1, 8-15)
+          ldmatrix_x4_trans(v, vbuf + chunk_at((mi & 1) * 8 + (lane & 7), c + (mi >> 1)));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = __byte_perm(v[k], 0u, 0x3120);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t a0 = e4m3x2_to_f16x2(v[2 * k]), a1 = e4m3x2_hi_to_f16x2(v[2 * k]);
+            const uint32_t a2 = e4m3x2_to_f16x2(v[2 * k + 1]), a3 = e4m3x2_hi_to_f16x2(v[2 * k + 1]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][c + k], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+          }
+        }
+        __syncwarp();  // everyone is done with this buffer before it is refilled
+        settle(i + STAGES - 1, pend);
+        pend = issue(i + STAGES, rawX, blkX);
+        rawX = rawY;
+        blkX = blk_new;
+        rawY = raw_new;
+      }
+      cp_async_wait<0>();
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int d = 4; d <= 16; d <<= 1) l[nt][k] += __shfl_xor_sync(0xffffffffu, l[nt][k], d);
+    }
+    wait_now();  // a segment without tokens has read nothing yet; what follows writes global memory
+    if (!n_ok && lane == 0 && first_of_row) flag_status(a.status, CLSA_DEV_BAD_SEQLEN);
+
+    // ---- what becomes of this segment's result (staged through the warp's ring, idle between segments) -------------
+    float* mypart = reinterpret_cast<float*>(ring);
+    const bool whole = seg_lo == u * NS && seg_hi == (u + 1) * NS;
+    __syncwarp();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int head = nt * 8 + hcol + k;
+        if (head < G) {
+          const float inv = whole ? (l[nt][k] != 0.f ? 1.f / l[nt][k] : 0.f) : 1.f;
+          const float half = whole ? fast_exp2(0.5f * (m[nt][k] - mx[nt][k])) : 1.f;  // applied twice: its square may not be a float
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+            *reinterpret_cast<float2*>(mypart + head * kPartialStride + 16 * c + 2 * rowq) = inv == 0.f ? make_float2(0.f, 0.f) : make_float2(o[nt][c][k] * inv * half * half, o[nt][c][k + 2] * inv * half * half);
+          if (rowq == 0) *reinterpret_cast<float4*>(mypart + head * kPartialStride + 128) = make_float4(mx[nt][k], l[nt][k], m[nt][k], 0.f);
+        }
+      }
+    __syncwarp();
+    if (whole) {
+      for (int hh = 0; hh < G; ++hh) {
+        const float4 v = *reinterpret_cast<const float4*>(mypart + hh * kPartialStride + lane * 4);
+        const float2 ml = *reinterpret_cast<const float2*>(mypart + hh * kPartialStride + 128);
+        const int64_t item = (int64_t)r * a.num_q_heads + h0 + hh;
+        *reinterpret_cast<uint2*>(a.out + item * 128 + lane * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+        if (a.lse != nullptr && lane == 0) a.lse[item] = ml.y != 0.f ? (ml.x + log2f(ml.y)) * kLn2 : -INFINITY;
+      }
+      __syncwarp();
+    } else if (a.reverse ? cur > s_begin : cur < s_end) {
+      // more segments follow and will reuse the ring: this partial waits in the worker's global slot
+      const int rec4 = G * (kPartialStride / 4);
+      float4* slot = reinterpret_cast<float4*>(a.part) + (int64_t)w * rec4;
+      const float4* src = reinterpret_cast<const float4*>(mypart);
+      for (int i = lane; i < rec4; i += 32) __stcg(slot + i, src[i]);
+      __syncwarp();
+    }
+  }
+  wait_now();
+  __syncthreads();
+
+  // ---- block-level merge: (unit, query head) jobs dealt over the warps ----------------------------------------------
+  const int w0 = (int)blockIdx.x * a.wpb;
+  if (w0 >= W) return;
+  const int nw = min(W - w0, a.wpb);
+  const int b_lo = span_tab[0].x, b_hi = span_tab[nw - 1].y;
+  const int u_first = b_lo / NS, u_last = (b_hi - 1) / NS;
+  const int rec4 = G * (kPartialStride / 4);
+  const float4* early = reinterpret_cast<const float4*>(a.part);
+  float4* bpart = reinterpret_cast<float4*>(a.part) + (int64_t)W * rec4;  // 2 records per block: its first unit, its last
+  // only units that no warp had whole: at most a unit per pair of neighbouring warps, and the block's first and last
+  const int njobs = (u_last - u_first + 1) * G;
+  for (int job = warp; job < njobs; job += WARPS) {
+    const int u = u_first + job / G, hh = job % G;
+    const int us = u * NS, ue = us + NS;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float L = 0.f, MX = -INFINITY, M = -INFINITY;
+    auto fold = [&](float4 ml, float4 v) {  // ml: mx, l, m
+      const float Mn = fmaxf(M, ml.z), Xn = fmaxf(MX, ml.x);
+      const float mu = Mn == -INFINITY ? 0.f : Mn, xu = Xn == -INFINITY ? 0.f : Xn;
+      const float so = fast_exp2(M - mu), sn = fast_exp2(ml.z - mu);
+      acc.x = fmaf(sn, v.x, acc.x * so); acc.y = fmaf(sn, v.y, acc.y * so);
+      acc.z = fmaf(sn, v.z, acc.z * so); acc.w = fmaf(sn, v.w, acc.w * so);
+      L = fmaf(fast_exp2(ml.x - xu), ml.y, L * fast_exp2(MX - xu));
+      M = Mn;
+      MX = Xn;
+    };
+    bool done = false;
+    for (int lw = 0; lw < nw; ++lw) {
+      const int2 sp = span_tab[lw];
+      if (sp.x >= ue || sp.y <= us) continue;
+      if (sp.x <= us && sp.y >= ue) { done = true; break; }
+      const int last_stage = a.reverse ? sp.x : sp.y - 1;
+      float4 ml, v;
+      if (last_stage >= us && last_stage < ue) {
+        const float* pr = reinterpret_cast<const float*>(smem + lw * S::kRing) + hh * kPartialStride;
+        ml = *reinterpret_cast<const float4*>(pr + 128);
+        v = *reinterpret_cast<const float4*>(pr + lane * 4);
+      } else {
+        const float4* pr = early + (int64_t)(w0 + lw) * rec4 + hh * (kPartialStride / 4);
+        ml = __ldcg(pr + 32);
+        v = __ldcg(pr + lane);
+      }
+      fold(ml, v);
+    }
+    if (done) continue;
+    const int g = u / a.rows, r = u - g * a.rows;
+    const int64_t item = (int64_t)r * a.num_q_heads + g * G + hh;
+    if (!(b_lo <= us && b_hi >= ue)) {
+      // the unit straddles blocks: leave this block's partial, arrive, and finish the pair if this completes it
+      float4* slot = bpart + (int64_t)(2 * blockIdx.x + (b_lo < us ? 1 : 0)) * rec4 + hh * (kPartialStride / 4);
+      __stcg(slot + lane, acc);
+      if (lane == 0) __stcg(slot + 32, make_float4(MX, L, M, 0.f));
+      asm volatile("fence.acq_rel.gpu;" ::: "memory");
+      __syncwarp();
+      int wf, wl;
+      unit_workers(u, a, wf, wl);
+      const int blk_first = wf / a.wpb, blk_last = wl / a.wpb;
+      const int lo_first = span_begin(blk_first * a.wpb, a);
+      uint32_t* counter = a.arrive + blk_first * kMaxGroup + hh;  // one unit at most leaves a block to the right
+      unsigned prev = 0;
+      if (lane == 0) prev = atomicAdd(counter, 1u);
+      prev = __shfl_sync(0xffffffffu, prev, 0);
+      if (prev + 1u != (unsigned)(blk_last - blk_first + 1)) continue;
+      asm volatile("fence.acq_rel.gpu;" ::: "memory");
+      if (lane == 0) *counter = 0u;
+      acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      L = 0.f;
+      MX = M = -INFINITY;
+      for (int b2 = blk_first; b2 <= blk_last; ++b2) {
+        const int kind = b2 == blk_first && lo_first < us ? 1 : 0;
+        const float4* pr = bpart + (int64_t)(2 * b2 + kind) * rec4 + hh * (kPartialStride / 4);
+        fold(__ldcg(pr + 32), __ldcg(pr + lane));
+      }
+    }
+    if (L != 0.f) {
+      const float inv = 1.f / L, half = fast_exp2(0.5f * (M - MX));
+      acc.x = acc.x * inv * half * half; acc.y = acc.y * inv * half * half;
+      acc.z = acc.z * inv * half * half; acc.w = acc.w * inv * half * half;
+    }
+    *reinterpret_cast<uint2*>(a.out + item * 128 + lane * 4) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+    if (a.lse != nullptr && lane == 0) a.lse[item] = L != 0.f ? (MX + log2f(L)) * kLn2 : -INFINITY;
+  }
+}
+
+constexpr int kWarpsNarrow = 16, kStagesNarrow = 3;  // groups of up to 8 query heads
+constexpr int kWarpsWide = 8, kStagesWide = 4;       // wider groups: twice the accumulators per thread
+
+}  // namespace
+
+Attn8Plan make_attn8_plan(const clsa_params& p, const DeviceInfo& dev) {
+  Attn8Plan plan;
+  const bool wide = p.num_q_heads / p.num_kv_heads > 8;
+  plan.warps = wide ? kWarpsWide : kWarpsNarrow;
+  plan.stages = wide ? kStagesWide : kStagesNarrow;
+  plan.smem_bytes = wide ? Shape<2, kWarpsWide, kStagesWide>::kSmem : Shape<1, kWarpsNarrow, kStagesNarrow>::kSmem;
+  plan.units = (int64_t)p.num_seqs * p.q_per_seq * p.num_kv_heads;
+  plan.unit_stages = (p.top_k + kTok - 1) / kTok;
+  plan.total_stages = plan.units * plan.unit_stages;
+  int64_t blocks = dev.sm_count;
+  int64_t workers = plan.total_stages / kMinStages8;
+  if (workers < 1) workers = 1;
+  if (workers > blocks * plan.warps) workers = blocks * plan.warps;
+  if (blocks > workers) blocks = workers;
+  plan.wpb = (int)((workers + blocks - 1) / blocks);
+  plan.blocks = (int)((workers + plan.wpb - 1) / plan.wpb);
+  plan.workers = (int)workers;
+  // Unit-aligned split when every unit can have workers of its own and the longest span that results stays within 15 % of the
+  // even share.
+  plan.aligned = 0;
+  if (workers >= plan.units) {
+    const int64_t longest = (plan.unit_stages + workers / plan.units - 1) / (workers / plan.units);
+    if (longest * workers * 100 <= plan.total_stages * 115) plan.aligned = 1;
+  }
+  return plan;
+}
+
+size_t attn8_counter_bytes(const DeviceInfo& dev) { return ((size_t)dev.sm_count * kMaxGroup * sizeof(uint32_t) + 255) / 256 * 256; }
+
+size_t attn8_partial_bytes(const clsa_params& p, const Attn8Plan& plan) {
+  const size_t group = (size_t)(p.num_q_heads / p.num_kv_heads);
+  return (((size_t)plan.workers + 2 * plan.blocks) * group * kPartialStride * sizeof(float) + 255) / 256 * 256;
+}
+
+cudaError_t launch_sparse_attn8(const clsa_params& p, const clsa_cache8& c, const Attn8Plan& plan, const void* q,
+                                const int32_t* idx, const int32_t* count, void* out, float* lse, const clsa_attn_hints& hints,
+                                uint32_t* status, uint32_t* arrive, float* part, const DeviceInfo& dev, cudaStream_t stream) {
+  Attn8Args a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.kc = static_cast<const uint8_t*>(c.k);
+  a.vc = static_cast<const uint8_t*>(c.v);
+  a.ks = static_cast<const uint8_t*>(c.k_scale);
+  a.vs = static_cast<const uint8_t*>(c.v_scale);
+  a.head_stride = c.kv_head_stride;
+  a.scale_head = c.scale_head_stride;
+  a.stride16 = (uint32_t)(c.kv_token_stride / 16);
+  while ((1 << a.scale_shift) < c.scale_block) ++a.scale_shift;
+  a.num_rows = p.num_cache_rows;
+  a.seq_start = p.seq_start;
+  a.seq_len = p.seq_len;
+  a.idx = idx;
+  a.count = count;
+  a.block_table = p.block_table;
+  while (p.block_table != nullptr && (1 << a.block_shift) < p.block_size) ++a.block_shift;
+  a.max_blocks = p.max_blocks_per_seq;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.status = status;
+  a.rows = p.num_seqs * p.q_per_seq;
+  a.q_per_seq = p.q_per_seq;
+  a.num_q_heads = p.num_q_heads;
+  a.num_kv_heads = p.num_kv_heads;
+  a.group = p.num_q_heads / p.num_kv_heads;
+  a.top_k = p.top_k;
+  a.max_seq_len = p.max_seq_len;
+  a.reverse = hints.reverse;
+  a.early = hints.only_q_pending;
+  a.keep = hints.keep_rows;
+  // keep_rows: all of the selected set evict_last where half of L2 holds it, else the share of every 8 stages that fits
+  a.pin = -1;
+  if (hints.keep_rows) {
+    const double k_eff = (double)(p.top_k < p.max_seq_len ? p.top_k : p.max_seq_len);
+    const double gathered = (double)a.rows * k_eff * p.num_kv_heads * p.head_dim * 2.0;
+    const int pin = (int)(8.0 * 0.5 * (double)dev.l2_bytes / gathered + 0.5);
+    a.pin = pin >= 8 ? -1 : (pin < 1 ? 1 : pin);
+  }
+  a.unit_stages = plan.unit_stages;
+  a.total_stages = (int)plan.total_stages;  // < 2^31, checked by the entry point
+  a.aligned = plan.aligned;
+  a.span_q = plan.aligned ? (int)(plan.workers / plan.units) : (int)(plan.total_stages / plan.workers);
+  a.span_rem = plan.aligned ? (int)(plan.workers % plan.units) : (int)(plan.total_stages % plan.workers);
+  a.workers = plan.workers;
+  a.wpb = plan.wpb;
+  a.arrive = arrive;
+  a.part = part;
+  a.scale_log2 = p.sm_scale * kLog2e;
+  const bool paged = p.block_table != nullptr, wide = a.group > 8;
+  void (*kernel)(const Attn8Args) =
+      wide ? (paged ? sparse_attn8_kernel<2, kWarpsWide, kStagesWide, true> : sparse_attn8_kernel<2, kWarpsWide, kStagesWide, false>)
+           : (paged ? sparse_attn8_kernel<1, kWarpsNarrow, kStagesNarrow, true> : sparse_attn8_kernel<1, kWarpsNarrow, kStagesNarrow, false>);
+  cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem_bytes);
+  if (err != cudaSuccess) return err;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)plan.blocks, 1, 1);
+  cfg.blockDim = dim3((unsigned)plan.warps * 32, 1, 1);
+  cfg.dynamicSmemBytes = plan.smem_bytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+}  // namespace clsa
