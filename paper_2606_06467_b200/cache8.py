@@ -4,8 +4,9 @@ pointers. Checks of dtypes, shapes, strides and devices that C cannot make happe
 from __future__ import annotations
 
 import ctypes
+import struct
 
-from . import (_H, _P, _check, _i64, _lib, _nbytes, _ptr, _stream, _sz, _vp, clsa_params)
+from . import _H, _P, _check, _i64, _lib, _nbytes, _ptr, _stream, _sz, _vp, clsa_params
 
 CLSA_DEV_BAD_SCALE_BLOCK = 64
 
@@ -37,7 +38,7 @@ class clsa_cache8(ctypes.Structure):
 
 _C = ctypes.POINTER(clsa_cache8)
 _N = ctypes.POINTER(clsa_norm_rope_spec)
-_D = ctypes.POINTER(clsa_heads)
+_D = _vp  # clsa_heads by its bytes (or a reference)
 _lib.clsa_norm_rope.argtypes = [_N, ctypes.c_int32, _vp, _D, _D, _D, _D, _vp]
 _lib.clsa_cache8_workspace_bytes.argtypes = [_P, _C, ctypes.POINTER(_sz)]
 _lib.clsa_cache8_append.argtypes = [_P, _C, _N, _D, _D, _D, _vp, _sz, _vp]
@@ -47,29 +48,32 @@ for _name in EXPORTS_CACHE8:
     getattr(_lib, _name).restype = ctypes.c_int
 
 
+_pack_heads = struct.Struct("@Piqq").pack  # clsa_heads
+
+
 def _want(ok, message):
     if not ok:
         raise ValueError(message)
 
 
-def _here(t, what, dtype=None):
-    """A tensor of the current CUDA device (where the call's kernels run) and of the dtype, if one is asked for. Device
-    addresses pass as they are."""
-    if not isinstance(t, int):
+def _dense(t, what, dtype, device, rows=False):
+    """Address of a buffer that is addressed as one dense array of `dtype` (None and device addresses pass). device: where it
+    has to lie, or None for anywhere the device can write (outputs may be pinned host memory). rows: its rows alone are dense."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype != dtype or not (t.is_contiguous() or (rows and t.stride(-1) == 1)) or (device is not None and t.get_device() != device):
+        raise ValueError(f"{what}: contiguous values of {dtype}" + (" on the current CUDA device" if device is not None else "")
+                         + f" are wanted, got {t.dtype} on {t.device}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _stream8(stream, device):
+    """The stream to launch on: the current one's handle without the object around it, or the caller's."""
+    if stream is None and device is not None:
         import torch
 
-        _want(t.is_cuda and t.get_device() == torch.cuda.current_device(), f"{what}: a tensor of the current CUDA device is wanted")
-        _want(dtype is None or t.dtype == dtype, f"{what}: dtype {dtype} is wanted, got {t.dtype}")
-    return t
-
-
-def _dense(t, what, dtype, where=_here):
-    """The same for a buffer that is addressed as one dense array (None passes)."""
-    if t is None or isinstance(t, int):
-        return
-    if where is not None:
-        where(t, what, dtype)
-    _want(t.dtype == dtype and t.is_contiguous(), f"{what}: contiguous values of {dtype} are wanted")
+        return torch._C._cuda_getCurrentRawStream(device)
+    return _stream(stream)
 
 
 def _bytes_like(t, what, names):
@@ -122,27 +126,27 @@ def make_cache8(*, k=None, v=None, k_scale=None, v_scale=None, idx_k=None, idx_k
     return c
 
 
-def _heads(t, what, tokens=None, flat=None):
-    """clsa_heads of a bf16 tensor [tokens, heads, D] or [B, T, heads, D] (or [.., D] with flat=1: one head)."""
-    import torch
-
-    _here(t, what, torch.bfloat16)
+def _heads(t, what, device, bf16, tokens, heads, dim, flat=False):
+    """The clsa_heads bytes of a bf16 tensor [tokens, heads, dim] or [B, T, heads, dim] ([.., dim] with flat: one head) and its
+    number of tokens. tokens, heads: what they have to be, or None."""
+    shape, stride = t.shape, t.stride()
     if flat:
-        t = t.unsqueeze(-2)
-    _want(t.dim() in (3, 4) and t.stride(-1) == 1, f"{what}: [tokens, heads, dim] or [B, T, heads, dim] with dense heads is wanted")
-    if t.dim() == 4:
-        B, T = t.shape[0], t.shape[1]
-        token = t.stride(0) if T == 1 else t.stride(1)
-        _want(T == 1 or B == 1 or t.stride(0) == T * t.stride(1), f"{what}: the tokens of all sequences must be evenly spaced")
-        n = B * T
+        shape, stride = (*shape[:-1], 1, shape[-1]), (*stride[:-1], dim, stride[-1])
+    if len(shape) == 4:
+        T = shape[1]
+        n, token = shape[0] * T, stride[0] if T == 1 else stride[1]
+        even = T == 1 or shape[0] == 1 or stride[0] == T * stride[1]
+    elif len(shape) == 3:
+        n, token, even = shape[0], stride[0], True
     else:
-        n, token = t.shape[0], t.stride(0)
-    _want(tokens is None or n == tokens, f"{what}: {tokens} tokens are wanted, got {n}")
-    return clsa_heads(t.data_ptr(), t.shape[-2], token, t.stride(-2) if t.shape[-2] > 1 else max(t.stride(-2), t.shape[-1])), t
-
-
-def _ref(x):
-    return None if x is None else ctypes.byref(x)
+        even = False
+    if not even or shape[-1] != dim or stride[-1] != 1 or t.dtype != bf16 or t.get_device() != device:
+        raise ValueError(f"{what}: a bf16 tensor [tokens, heads, {dim}] or [B, T, heads, {dim}] on the current CUDA device, with dense heads and "
+                         f"evenly spaced tokens, is wanted; got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+    if (tokens is not None and n != tokens) or (heads is not None and shape[-2] != heads):
+        raise ValueError(f"{what}: {tokens} tokens of {heads} heads are wanted, got {tuple(t.shape)}")
+    h = shape[-2]
+    return _pack_heads(t.data_ptr(), h, token, stride[-2] if h > 1 else dim), n
 
 
 def clsa_norm_rope(spec, positions, q, q_out, k=None, k_out=None, stream=None) -> None:
@@ -150,21 +154,20 @@ def clsa_norm_rope(spec, positions, q, q_out, k=None, k_out=None, stream=None) -
     into q_out and k_out, which may be q and k themselves. positions: int32, one per token (negative: skipped), or None."""
     import torch
 
-    _want((q is None) == (q_out is None) and (k is None) == (k_out is None) and (q is not None or k is not None),
-          "q with q_out, k with k_out, or both are wanted")
-    _dense(positions, "positions", torch.int32)
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
+        raise ValueError("q with q_out, k with k_out, or both are wanted")
+    dev, bf16, dim = torch.cuda.current_device() if torch.cuda.is_initialized() else None, torch.bfloat16, spec.head_dim
     n = None if positions is None else positions.numel()
-    made = []
-    for t, o, what in ((q, q_out, "q"), (k, k_out, "k")):
-        if t is None:
-            made += [None, None]
-            continue
-        a, ta = _heads(t, what, n)
-        n = ta.shape[0] if ta.dim() == 3 else ta.shape[0] * ta.shape[1]
-        b, tb = _heads(o, what + "_out", n)
-        _want(ta.shape[-2:] == tb.shape[-2:] and ta.shape[-1] == spec.head_dim, f"{what}: heads of head_dim, as many in as out, are wanted")
-        made += [a, b]
-    _check(_lib.clsa_norm_rope(ctypes.byref(spec), n, _ptr(positions), *map(_ref, made), _stream(stream)), "clsa_norm_rope")
+    a = b = c = d = None
+    if q is not None:
+        a, n = _heads(q, "q", dev, bf16, n, None, dim)
+        b, _ = _heads(q_out, "q_out", dev, bf16, n, q.shape[-2], dim)
+    if k is not None:
+        c, n = _heads(k, "k", dev, bf16, n, None, dim)
+        d, _ = _heads(k_out, "k_out", dev, bf16, n, k.shape[-2], dim)
+    status = _lib.clsa_norm_rope(ctypes.byref(spec), n, _dense(positions, "positions", torch.int32, dev), a, b, c, d, _stream8(stream, dev))
+    if status:
+        _check(status, "clsa_norm_rope")
 
 
 def clsa_cache8_workspace_bytes(p: clsa_params, c: clsa_cache8) -> int:
@@ -176,38 +179,43 @@ def clsa_cache8_workspace_bytes(p: clsa_params, c: clsa_cache8) -> int:
 def clsa_cache8_append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace_bytes=None, stream=None) -> None:
     """The newest T tokens of every sequence into the 8-bit caches: k_new, v_new [B, T, Hkv, D], idx_k_new [B, T, d_idx]
     (bf16; None leaves K and V, or K_idx, out). spec: the norm and rotation of K's rows (or None)."""
-    n = p.num_seqs * p.q_per_seq
+    import torch
+
+    if (k_new is None) != (v_new is None) or (k_new is None and idx_k_new is None):
+        raise ValueError("k_new with v_new, idx_k_new, or all three are wanted")
+    dev, bf16, n = torch.cuda.current_device() if torch.cuda.is_initialized() else None, torch.bfloat16, p.num_seqs * p.q_per_seq
     k = v = i = None
-    if k_new is not None or v_new is not None:
-        _want(k_new is not None and v_new is not None, "k_new and v_new: both or neither are wanted")
-        (k, tk), (v, tv) = _heads(k_new, "k_new", n), _heads(v_new, "v_new", n)
-        _want(tk.shape[-2:] == tv.shape[-2:] == (p.num_kv_heads, p.head_dim), "k_new, v_new: [num_kv_heads, head_dim] per token is wanted")
+    if k_new is not None:
+        k, _ = _heads(k_new, "k_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
+        v, _ = _heads(v_new, "v_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
     if idx_k_new is not None:
-        i, ti = _heads(idx_k_new, "idx_k_new", n, flat=1)
-        _want(ti.shape[-1] == p.idx_dim, "idx_k_new: idx_dim elements per token are wanted")
-    _check(_lib.clsa_cache8_append(ctypes.byref(p), ctypes.byref(c), _ref(spec), _ref(k), _ref(v), _ref(i), _ptr(workspace),
-                                   _nbytes(workspace, workspace_bytes), _stream(stream)), "clsa_cache8_append")
+        i, _ = _heads(idx_k_new, "idx_k_new", dev, bf16, n, 1, p.idx_dim, True)
+    status = _lib.clsa_cache8_append(ctypes.byref(p), ctypes.byref(c), None if spec is None else ctypes.byref(spec), k, v, i, _ptr(workspace),
+                                     _nbytes(workspace, workspace_bytes), _stream8(stream, dev))
+    if status:
+        _check(status, "clsa_cache8_append")
 
 
 def clsa_index_scores8(p, c, q_idx, scores, score_stride, workspace, workspace_bytes=None, stream=None) -> None:
     """clsa_index_scores over an 8-bit indexer-key cache."""
     import torch
 
-    _dense(q_idx, "q_idx", torch.bfloat16)
-    _here(scores, "scores", torch.float32)
-    _check(_lib.clsa_index_scores8(ctypes.byref(p), ctypes.byref(c), _ptr(q_idx), _ptr(scores), score_stride, _ptr(workspace),
-                                   _nbytes(workspace, workspace_bytes), _stream(stream)), "clsa_index_scores8")
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+    status = _lib.clsa_index_scores8(ctypes.byref(p), ctypes.byref(c), _dense(q_idx, "q_idx", torch.bfloat16, dev),
+                                     _dense(scores, "scores", torch.float32, dev, True), score_stride, _ptr(workspace),
+                                     _nbytes(workspace, workspace_bytes), _stream8(stream, dev))
+    if status:
+        _check(status, "clsa_index_scores8")
 
 
 def clsa_sparse_attn8(p, c, q, idx, count, out, lse, hints, workspace, workspace_bytes=None, stream=None) -> None:
     """clsa_sparse_attn_hinted over an 8-bit K and V cache (hints: None or a clsa_attn_hints with shared_gpu 0)."""
     import torch
 
-    _dense(q, "q", torch.bfloat16)
-    _dense(idx, "idx", torch.int32)
-    _dense(count, "count", torch.int32)
-    _dense(out, "out", torch.bfloat16, None)  # outputs may lie in pinned host memory
-    _dense(lse, "lse", torch.float32, None)
-    _check(_lib.clsa_sparse_attn8(ctypes.byref(p), ctypes.byref(c), _ptr(q), _ptr(idx), _ptr(count), _ptr(out), _ptr(lse),
-                                  _ref(hints), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)),
-           "clsa_sparse_attn8")
+    dev, i32 = torch.cuda.current_device() if torch.cuda.is_initialized() else None, torch.int32
+    status = _lib.clsa_sparse_attn8(ctypes.byref(p), ctypes.byref(c), _dense(q, "q", torch.bfloat16, dev), _dense(idx, "idx", i32, dev),
+                                    _dense(count, "count", i32, dev), _dense(out, "out", torch.bfloat16, None),
+                                    _dense(lse, "lse", torch.float32, None), None if hints is None else ctypes.byref(hints),
+                                    _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream8(stream, dev))
+    if status:
+        _check(status, "clsa_sparse_attn8")

@@ -34,11 +34,11 @@ cudaError_t launch_index_expand8(const clsa_params& p, const clsa_cache8& c, voi
 
 // Launch shape of the 8-bit attention kernel.
 struct Attn8Plan {
-  int warps, stages;    // warps per block, ring depth
+  int warps;            // warps per block
   int blocks, wpb;      // grid, workers per block
   int workers;          // warps that get a span of the stage list
   int aligned;          // 1: every unit has workers of its own
-  int unit_stages;      // 16-token stages per (query row, KV head) unit
+  int unit_stages;      // 32-token stages per (query row, KV head) unit
   int64_t units, total_stages;
   size_t smem_bytes;
 };

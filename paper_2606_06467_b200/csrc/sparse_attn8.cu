@@ -1,35 +1,40 @@
 // GQA sparse attention over the selected rows of an 8-bit K and V cache (Eq. 4), one launch per layer, T >= 1.
 //
 //   x_s = sm_scale * (q . code_K[s]) * 2^ek,   O = sum_s exp(x_s) 2^ev code_V[s] / sum_s exp(x_s)
-// with ek, ev the exponents of the scale blocks that row s lies in. In the log2 domain a query head keeps two running
-// references: m near the largest x_s + ev for the numerators, whose weights 2^(x_s + ev - m) go to the matrix instructions as
-// f16, and mx near the largest x_s for the denominators 2^(x_s - mx), so that neither underflows however far apart the blocks'
-// scales lie; the difference of the two is applied to the finished quotient. References move only when a weight would
-// exceed 2^8 (one vote per stage): a stage that moves none needs no reduction over its tokens.
+// with ek, ev the exponents of the scale blocks that row s lies in.
 //
-// The work is a flat list of 16-token stages, unit = (KV head, query row), heads outermost, so that a prefill chunk's launch
+// e4m3 codes convert to f16 exactly, a query row scaled by a power of two so that its largest magnitude lies in [2^13, 2^14) is
+// exact in f16 down to 2^-31 of it, weights are rounded to f16, sums are fp32. (There is no faster 8-bit form to be had: the
+// warp-level e4m3 instruction is carried out as these conversions and f16 products anyway.) A warp-level instruction has up to 8
+// query heads of the GQA group in its columns (NT tiles cover the group) and 16 tokens or 16 dimensions along M:
+//   S^T[16 tokens x 8 heads] = K[16 x 128] Q^T,   O^T[128 x 8 heads] += V^T[128 x 32 tokens] P^T
+// K's fragments are plain matrix loads: a lane's word holds 4 dimensions of a token, its halves are the lane's two shares of a
+// step (the contraction index is a dummy, q is laid out to match). V's are the transposing 8-bit loads: a word holds 4
+// consecutive tokens of one dimension. K's rows are addressed in the order in which the weights, transposed in registers, then
+// meet those tokens.
+//
+// In the log2 domain a query head keeps two running references: m near the largest x_s + ev for the numerators' weights
+// 2^(x_s + ev - m), and mx near the largest x_s for the denominators 2^(x_s - mx), so that neither underflows however far apart
+// the blocks' scales lie; the difference of the two is applied to the finished quotient. References move only when a
+// weight would leave its range (one vote per stage): a stage that moves none needs no reduction over its tokens.
+//
+// The work is a flat list of 32-token stages, unit = (KV head, query row), heads outermost, so that a prefill chunk's launch
 // goes over one head's part of the cache (which fits in L2) before the next. Warp w of W takes a contiguous span of the list
-// (unit-aligned where that splits evenly); a warp streams its span through a private ring of cp.async stages of 16 tokens,
-// 128 bytes of K and of V each. e4m3 codes convert to f16 exactly, so the products are those of the stored values, and sums are
-// fp32. A warp-level instruction takes 16 tokens (along M) against up to 8 query heads of the GQA group (along N):
-//   S^T[16 x 8] = K[16 x 128] Q^T: four lanes share a token; a lane takes 16-byte chunks j and j + 4 of its row, whose words
-//     are its share of the eight steps (the contraction index is a dummy, q is laid out to match);
-//   O^T[128 x 8] += V^T[128 x 16] P^T: a transposing matrix load hands a lane the byte pairs (d, d + 1) of two tokens; one
-//     byte permutation makes them (token, token + 1) pairs of d and of d + 1, which go to rows g and g + 8 of the instruction.
-// Units that several warps share are merged by log-sum-exp: partial results meet in shared memory, those of units that straddle
-// blocks in global slots (two per block) with an arrival counter; the block that arrives last reads them in block order, so
-// results do not depend on timing, and puts the counter back to zero.
+// (unit-aligned where that splits evenly); a warp streams its span through a private ring of cp.async stages, 128 bytes of K
+// and of V per token. Units that several warps share are merged by log-sum-exp: partial results meet in shared memory, those of
+// units that straddle blocks in global slots (two per block) with an arrival counter; the block that arrives last reads them in
+// block order, so results do not depend on timing, and puts the counter back to zero.
 #include "attn_common.cuh"
 #include "cache8.cuh"
 
 namespace clsa {
 namespace {
 
-constexpr int kTok = 16;                  // tokens per stage
+constexpr int kTok = 32;                  // tokens per stage
 constexpr int kStage8Bytes = kTok * 256;  // K rows, then V rows, 128 bytes each
 constexpr int kMaxGroup = 16;
-constexpr int kMinStages8 = 2;            // shorter spans cost more in partials than they return in parallelism
-constexpr float kLazy = 8.f;              // a weight may exceed the reference by 2^8 before the reference moves
+constexpr float kLazy = 8.f;              // a weight may exceed its reference by 2^8 before the reference moves
+constexpr float kNone = -1e30f;           // a reference before the first token: 2^(x - kNone) of a masked x = -inf is 0, not NaN
 
 struct Attn8Args {
   const uint16_t* q;
@@ -47,6 +52,7 @@ struct Attn8Args {
   const int32_t* count;
   const int32_t* block_table;
   int block_shift, max_blocks;
+  uint32_t page_limit;  // pages of the row space (the last one may be cut short)
   uint16_t* out;
   float* lse;
   uint32_t* status;
@@ -81,20 +87,20 @@ __device__ __forceinline__ void unit_workers(int u, const Attn8Args& a, int& fir
   }
 }
 
-// Where chunk c (16 bytes) of token j of a stage lies: lanes (two rows, four chunks) of a 16-byte read, and eight rows of one
-// chunk of a transposing matrix load, fall into different banks.
-__device__ __forceinline__ uint32_t chunk_at(int j, int c) {
-  const int f = ((j & 1) << 2) | (j & 2) | ((j & 4) >> 2);
-  return (uint32_t)(j * 128 + ((c ^ f) << 4));
+// Token of row r of a 16-token tile of the first product: after the transpose of the weights a lane has rows 2 j and 2 j + 1 of
+// the tile's first eight and of its last eight, which have to be tokens 4 j .. 4 j + 3.
+__device__ __forceinline__ int k_token(int r) { return 4 * ((r >> 1) & 3) + (r & 1) + ((r >> 2) & 2); }
+// Where chunk c (16 bytes) of token t of a stage lies: the eight rows that a matrix load reads together (k_token of eight
+// consecutive r; eight consecutive tokens for V) fall into different banks.
+__device__ __forceinline__ uint32_t k_chunk(int t, int c) { return (uint32_t)(t * 128 + ((c ^ ((t & 1) | ((t >> 1) & 6))) << 4)); }
+__device__ __forceinline__ uint32_t v_chunk(int t, int c) { return (uint32_t)(t * 128 + ((c ^ (t & 7)) << 4)); }
+
+__device__ __forceinline__ void ldmatrix_b8_x2_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 
-__device__ __forceinline__ uint4 lds128(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
-  return v;
-}
-
-template <int NT, int WARPS, int STAGES>
+template <int WARPS, int STAGES>
 struct Shape {
   static constexpr int kRing = STAGES * kStage8Bytes;
   static constexpr int kScale = STAGES * kTok * 8;  // per token: 2^ek, ev
@@ -103,10 +109,10 @@ struct Shape {
 
 template <int NT, int WARPS, int STAGES, bool PAGED>
 __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __grid_constant__ Attn8Args a) {
-  using S = Shape<NT, WARPS, STAGES>;
+  using S = Shape<WARPS, STAGES>;
   extern __shared__ __align__(128) unsigned char smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rowq = lane >> 2, j4 = lane & 3, hcol = 2 * j4;
+  const int rowq = lane >> 2, hcol = 2 * (lane & 3);
   const int G = a.group, NS = a.unit_stages, W = a.workers;
   const int w = (int)blockIdx.x * a.wpb + warp;
   const bool has_work = warp < a.wpb && w < W;
@@ -132,9 +138,17 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 
   const uint64_t pol_keep = a.keep ? l2_policy_evict_last() : l2_policy_evict_normal();
   const uint64_t pol_last = l2_policy_evict_last(), pol_first = l2_policy_evict_first();
-  uint32_t dst[4];  // this lane's 16-byte chunk of token 4 * it + lane / 8
+  // Places inside a stage, from the ring's start. This lane copies chunk lane & 7 of tokens 4 it + lane / 8: k_copy[it & 3] and
+  // v_copy[it & 1] plus 512 it; it addresses row k_frag of K's fragment loads (plus 2048 for tokens 16 ..), where the chunk
+  // pair 2 st is reached by an exclusive or with st << 5, and row v_frag of V's, where chunk c is with c << 4.
+  uint32_t k_copy[4], v_copy[2];
 #pragma unroll
-  for (int it = 0; it < 4; ++it) dst[it] = chunk_at(4 * it + (lane >> 3), lane & 7);
+  for (int i = 0; i < 4; ++i) k_copy[i] = ring_u32 + k_chunk(4 * i + (lane >> 3), lane & 7) - 512u * i;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) v_copy[i] = ring_u32 + kStage8Bytes / 2 + v_chunk(4 * i + (lane >> 3), lane & 7) - 512u * i;
+  const uint32_t k_frag = ring_u32 + k_chunk(k_token(lane & 15), lane >> 4);
+  const uint32_t v_frag = ring_u32 + kStage8Bytes / 2 + v_chunk(lane, 0);
+  const int my_tok = k_token(rowq);  // this lane's tokens of a stage: my_tok + {0, 2, 16, 18}
 
   int cur = a.reverse ? s_end : s_begin;
   while (a.reverse ? cur > s_begin : cur < s_end) {
@@ -147,6 +161,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
     const int slot_lo = (seg_lo - u * NS) * kTok;
     const int slot_hi = min(a.top_k, (seg_hi - u * NS) * kTok);
     const int32_t* row_idx = a.idx + (int64_t)r * a.top_k;
+    // the first positions, fetched together with the count (entries past it are not used)
+    int spec[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) spec[i] = !a.reverse && slot_lo + i * kTok + lane < slot_hi ? row_idx[slot_lo + i * kTok + lane] : -1;
     int cnt = a.count[r];
     const int n_raw = a.seq_len[b];
     const bool n_ok = n_raw >= a.q_per_seq && n_raw <= a.max_seq_len;
@@ -161,11 +179,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
     const int t_lo = min(cnt, slot_lo), t_hi = min(cnt, slot_hi);
     const int nstages = (t_hi - t_lo + kTok - 1) / kTok;
 
-    float o[NT][8][4];
-    float m[NT][2], mx[NT][2], l[NT][2];  // references and this lane's share of the denominators, heads hcol and hcol + 1
+    float o[NT][8][4];                     // O^T: [head tile][16 dimensions]: dimensions rowq, rowq + 8; heads hcol, hcol + 1
+    float m[NT][2], mx[NT][2], l[NT][2];   // references and this lane's share of the denominators of the two heads
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = mx[nt][0] = mx[nt][1] = -INFINITY;
+      m[nt][0] = m[nt][1] = mx[nt][0] = mx[nt][1] = kNone;
       l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
       for (int c = 0; c < 8; ++c) { o[nt][c][0] = 0.f; o[nt][c][1] = 0.f; o[nt][c][2] = 0.f; o[nt][c][3] = 0.f; }
@@ -174,69 +192,81 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
     if (nstages > 0) {
       const uint8_t* kbase = a.kc + g * a.head_stride + (lane & 7) * 16;
       const uint8_t* vbase = a.vc + g * a.head_stride + (lane & 7) * 16;
-      const uint8_t* sbase = (lane < kTok ? a.ks : a.vs) + g * a.scale_head;  // lanes 0..15: K's scales, 16..31: V's
-      auto stage_t0 = [&](int i) { return t_lo + (a.reverse ? nstages - 1 - i : i) * kTok; };
-      auto load_raw = [&](int i) -> int {  // lanes k and k + 16: position of token k of step i (-1 past the end)
-        const int tt = stage_t0(i) + (lane & 15);
-        return i < nstages && tt < t_hi ? row_idx[tt] : -1;
+      const uint8_t* ksb = a.ks + g * a.scale_head;
+      const uint8_t* vsb = a.vs + g * a.scale_head;
+      // stage i begins at entry t_lo + 32 i of the row's index, or, walking from the end, nstages - 1 - i in the place of i
+      const int32_t* my_idx = row_idx + t_lo + lane + (a.reverse ? (nstages - 1) * kTok : 0);
+      const int step = a.reverse ? -kTok : kTok;
+      const int full = (t_hi - t_lo) % kTok;  // tokens of the last stage if it is cut short (0: it is not)
+      auto live = [&](int i) { return i < nstages && (full == 0 || i != (a.reverse ? 0 : nstages - 1) || lane < full); };
+      auto load_raw = [&](int i) -> int { return live(i) ? my_idx[i * step] : -1; };  // position of token `lane` of step i
+      // Positions whose rows may be read: inside the sequence and, without pages, inside the row space too.
+      const int pos_lo = PAGED || start >= 0 ? 0 : (int)min((int64_t)n, -start);
+      const int pos_hi = PAGED ? n : (int)max((int64_t)pos_lo, min((int64_t)n, a.num_rows - start));
+      const uint32_t pos_span = (uint32_t)(pos_hi - pos_lo);
+      auto load_blk = [&](int raw) -> int { return PAGED && (uint32_t)raw < (uint32_t)n ? __ldg(table + (raw >> a.block_shift)) : -1; };
+      auto settle = [&](int i, int kb, int vb) {  // the scale bytes of stage i into shared memory
+        if (i < nstages) scales[(i % STAGES) * kTok + lane] = make_float2(exp2_int(scale_exponent(kb)), (float)scale_exponent(vb));
       };
-      auto load_blk = [&](int raw) -> int { return PAGED && raw >= 0 && raw < n ? __ldg(table + (raw >> a.block_shift)) : 0; };
-      auto settle = [&](int i, int byte) {  // the scale bytes of stage i into shared memory
-        if (i < nstages) {
-          const int e = scale_exponent(byte);
-          float* dstf = reinterpret_cast<float*>(scales + (i % STAGES) * kTok + (lane & 15));
-          dstf[lane >> 4] = lane < kTok ? exp2_int(e) : (float)e;
-        }
-      };
-      auto issue = [&](int i, int raw, int blk) -> int {  // the copies of stage i; returns its scale bytes, still in flight
-        int byte = 127;
+      auto issue = [&](int i, int raw, int blk, int& kb, int& vb) {  // the copies of stage i; its scale bytes stay in flight
         if (i < nstages) {
           const int buf = i % STAGES;
-          const uint32_t kdst = ring_u32 + buf * kStage8Bytes, vdst = kdst + kStage8Bytes / 2;
-          const uint64_t pol = a.pin < 0 ? pol_keep : (pin_rank((stage_t0(i) >> 4) & 7) < a.pin ? pol_last : pol_first);
-          const int64_t row = PAGED ? ((int64_t)blk << a.block_shift) + (raw & ((1 << a.block_shift) - 1)) : start + raw;
-          const bool ok = raw >= 0 && raw < n && row >= 0 && row < a.num_rows;
-          const uint32_t okmask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
-          if (!ok && n_ok && lane < kTok && stage_t0(i) + lane < t_hi) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+          const uint64_t pol = a.pin < 0 ? pol_keep : (pin_rank((t_lo / kTok + (a.reverse ? nstages - 1 - i : i)) & 7) < a.pin ? pol_last : pol_first);
+          uint32_t row;
+          bool ok;
+          if (PAGED) {
+            ok = (uint32_t)blk < a.page_limit;  // (-1 where the position is out of range)
+            row = ((uint32_t)blk << a.block_shift) + ((uint32_t)raw & ((1u << a.block_shift) - 1u));
+            ok = ok && row < (uint32_t)a.num_rows;
+          } else {
+            ok = (uint32_t)(raw - pos_lo) < pos_span;
+            row = (uint32_t)start + (uint32_t)raw;
+          }
+          const uint32_t okmask = __ballot_sync(0xffffffffu, ok);
           if (lane == 0) stage_mask[buf] = okmask;
-          if (ok) byte = sbase[row >> a.scale_shift];
-          const uint32_t my16 = ok ? (uint32_t)row * a.stride16 : 0u;  // 16-byte units: the caches span less than 2^32 of them
-          if (okmask == 0xffffu) {
+          kb = vb = 127;
+          if (ok) {
+            kb = ksb[row >> a.scale_shift];
+            vb = vsb[row >> a.scale_shift];
+          }
+          const uint32_t my16 = ok ? row * a.stride16 : 0u;  // 16-byte units: the caches span less than 2^32 of them
+          const uint32_t at = (uint32_t)(buf * kStage8Bytes);
+          if (okmask == 0xffffffffu) {
 #pragma unroll
-            for (int it = 0; it < 4; ++it) {
-              const uint32_t off = __shfl_sync(0xffffffffu, my16, 4 * it + (lane >> 3));
-              cp_async16_full(kdst + dst[it], kbase + (uint64_t)off * 16u, pol);
-              cp_async16_full(vdst + dst[it], vbase + (uint64_t)off * 16u, pol);
+            for (int it = 0; it < 8; ++it) {
+              const uint64_t off = (uint64_t)__shfl_sync(0xffffffffu, my16, 4 * it + (lane >> 3)) * 16u;
+              cp_async16_full(k_copy[it & 3] + at + 512 * it, kbase + off, pol);
+              cp_async16_full(v_copy[it & 1] + at + 512 * it, vbase + off, pol);
             }
           } else {
+            if (!ok && n_ok && live(i)) flag_status(a.status, CLSA_DEV_BAD_INDEX);
 #pragma unroll
-            for (int it = 0; it < 4; ++it) {
-              const int jt = 4 * it + (lane >> 3);
-              const uint32_t off = __shfl_sync(0xffffffffu, my16, jt);
-              const bool okj = (okmask >> jt) & 1u;
-              cp_async16(kdst + dst[it], kbase + (uint64_t)off * 16u, okj, pol);
-              cp_async16(vdst + dst[it], vbase + (uint64_t)off * 16u, okj, pol);
+            for (int it = 0; it < 8; ++it) {
+              const int t = 4 * it + (lane >> 3);
+              const uint64_t off = (uint64_t)__shfl_sync(0xffffffffu, my16, t) * 16u;
+              const bool okt = (okmask >> t) & 1u;
+              cp_async16(k_copy[it & 3] + at + 512 * it, kbase + off, okt, pol);
+              cp_async16(v_copy[it & 1] + at + 512 * it, vbase + off, okt, pol);
             }
           }
         }
         cp_async_commit();
-        return byte;
       };
 
       // Prologue: the ring filled, the positions of the two stages behind it and the page numbers of the first in registers.
       int raw_p[STAGES], blk_p[STAGES];
 #pragma unroll
-      for (int i = 0; i < STAGES; ++i) raw_p[i] = load_raw(i);
+      for (int i = 0; i < STAGES; ++i)
+        raw_p[i] = a.reverse || i >= 2 ? load_raw(i) : (live(i) ? spec[i] : -1);
       int rawX = load_raw(STAGES), rawY = load_raw(STAGES + 1);
 #pragma unroll
       for (int i = 0; i < STAGES; ++i) blk_p[i] = load_blk(raw_p[i]);
 #pragma unroll
-      for (int i = 0; i < STAGES; ++i) raw_p[i] = issue(i, raw_p[i], blk_p[i]);
+      for (int i = 0; i < STAGES; ++i) issue(i, raw_p[i], blk_p[i], raw_p[i], blk_p[i]);  // (now the scale bytes)
       int blkX = load_blk(rawX);
       wait_now();  // with only q pending, everything read so far was complete before this launch; q is read behind the wait
 
-      // q as f16: column = head, the lane's words of step (half, w) hold dimensions 16 (j4 + 4 half) + 4 w .. + 3. Scaled by a
-      // power of two so that the head's largest magnitude lies in [2^13, 2^14).
+      // q as f16: column rowq = head, step st: dimensions 16 st + 4 (lane & 3) .. + 3.
       uint32_t qb[NT][8][2];
       float qf[NT][2];
       const uint16_t* qbase = a.q + ((int64_t)r * a.num_q_heads + h0) * 128;
@@ -245,18 +275,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
         const int head = nt * 8 + rowq;
         float amax = 0.f;
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-          if (head < G) {
-            const uint4* src = reinterpret_cast<const uint4*>(qbase + head * 128 + 16 * (j4 + 4 * hf));
-            v[0] = src[0];
-            v[1] = src[1];
-          }
-          const uint32_t raw8[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+        for (int st = 0; st < 8; ++st) {
+          const uint2 v = head < G ? *reinterpret_cast<const uint2*>(qbase + head * 128 + 16 * st + 2 * hcol) : make_uint2(0u, 0u);
+          qb[nt][st][0] = v.x;
+          qb[nt][st][1] = v.y;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            qb[nt][hf * 4 + i / 2][i & 1] = raw8[i];
-            const float lo = fabsf(bf16_lo(raw8[i])), hi = fabsf(bf16_hi(raw8[i]));
+          for (int k = 0; k < 2; ++k) {
+            const float lo = fabsf(bf16_lo(qb[nt][st][k])), hi = fabsf(bf16_hi(qb[nt][st][k]));
             if (lo <= 3.4028234663852886e38f) amax = fmaxf(amax, lo);  // finite
             if (hi <= 3.4028234663852886e38f) amax = fmaxf(amax, hi);
           }
@@ -266,16 +291,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
         const int shift = min(13 + 127 - (int)(__float_as_uint(amax) >> 23), 120);
         const float up = exp2_int(shift), down = exp2_int(-shift);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int st = 0; st < 8; ++st)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) qb[nt][i][k] = pack_f16x2(bf16_lo(qb[nt][i][k]) * up, bf16_hi(qb[nt][i][k]) * up);
-        qf[nt][0] = __shfl_sync(0xffffffffu, down, 4 * hcol) * a.scale_log2;
+          for (int k = 0; k < 2; ++k) qb[nt][st][k] = pack_f16x2(bf16_lo(qb[nt][st][k]) * up, bf16_hi(qb[nt][st][k]) * up);
+        qf[nt][0] = __shfl_sync(0xffffffffu, down, 4 * hcol) * a.scale_log2;  // lane 4 h holds head h
         qf[nt][1] = __shfl_sync(0xffffffffu, down, 4 * hcol + 4) * a.scale_log2;
       }
-
 #pragma unroll
-      for (int i = 0; i + 1 < STAGES; ++i) settle(i, raw_p[i]);
-      int pend = raw_p[STAGES - 1];  // settled one iteration after its stage was issued
+      for (int i = 0; i + 1 < STAGES; ++i) settle(i, raw_p[i], blk_p[i]);
+      int pend_k = raw_p[STAGES - 1], pend_v = blk_p[STAGES - 1];  // settled one iteration after their stage was issued
 #pragma unroll 1
       for (int i = 0; i < nstages; ++i) {
         const int raw_new = load_raw(i + STAGES + 2);
@@ -283,94 +307,98 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
         cp_async_wait<STAGES - 1>();
         __syncwarp();
         const int buf = i % STAGES;
-        const uint32_t kbuf = ring_u32 + buf * kStage8Bytes, vbuf = kbuf + kStage8Bytes / 2;
+        const uint32_t at = (uint32_t)(buf * kStage8Bytes);
         const uint32_t okmask = stage_mask[buf];
-        const float2 sc_lo = scales[buf * kTok + rowq], sc_hi = scales[buf * kTok + rowq + 8];  // tokens rowq, rowq + 8
+        float2 sc[4];  // tokens my_tok + 2 (t & 1) + 16 (t / 2)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sc[t] = scales[buf * kTok + my_tok + 2 * (t & 1) + 8 * (t & 2)];
         float s[NT][2][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int k = 0; k < 2; ++k) { s[nt][k][0] = 0.f; s[nt][k][1] = 0.f; s[nt][k][2] = 0.f; s[nt][k][3] = 0.f; }
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const uint4 lo = lds128(kbuf + chunk_at(rowq, j4 + 4 * hf)), hi = lds128(kbuf + chunk_at(rowq + 8, j4 + 4 * hf));
-          const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
+        for (int st = 0; st < 4; ++st)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t a0 = e4m3x2_to_f16x2(wl[k]), a2 = e4m3x2_hi_to_f16x2(wl[k]);
-            const uint32_t a1 = e4m3x2_to_f16x2(wh[k]), a3 = e4m3x2_hi_to_f16x2(wh[k]);
+          for (int mt = 0; mt < 2; ++mt) {
+            uint32_t kf[4];  // chunk 2 st of rows 0-7, 8-15, chunk 2 st + 1 of them
+            ldmatrix_x4(kf, ((k_frag + at) ^ (uint32_t)(st << 5)) + 2048 * mt);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt][k & 1], a0, a1, a2, a3, qb[nt][hf * 4 + k][0], qb[nt][hf * 4 + k][1]);
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t a0 = e4m3x2_to_f16x2(kf[2 * k]), a2 = e4m3x2_hi_to_f16x2(kf[2 * k]);
+              const uint32_t a1 = e4m3x2_to_f16x2(kf[2 * k + 1]), a3 = e4m3x2_hi_to_f16x2(kf[2 * k + 1]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt][mt], a0, a1, a2, a3, qb[nt][2 * st + k][0], qb[nt][2 * st + k][1]);
+            }
           }
-        }
-        // x of the lane's two tokens and two heads
-        float x[NT][4];
+        // x of the lane's four tokens and two heads per tile: x[..][2 t + head]
+        float x[NT][8], top[NT][2], tope[NT][2];
         bool move = false;
-        const bool ok_lo = (okmask >> rowq) & 1u, ok_hi = (okmask >> (rowq + 8)) & 1u;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i4 = 0; i4 < 4; ++i4) {
-            const float2& sc = i4 < 2 ? sc_lo : sc_hi;
-            const float v = (s[nt][0][i4] + s[nt][1][i4]) * sc.x * qf[nt][i4 & 1];
-            x[nt][i4] = (i4 < 2 ? ok_lo : ok_hi) ? v : -INFINITY;
-            move = move || x[nt][i4] > mx[nt][i4 & 1] + kLazy || x[nt][i4] + sc.y > m[nt][i4 & 1] + kLazy;
-          }
+          for (int i = 0; i < 8; ++i) x[nt][i] = s[nt][i >> 2][i & 3] * sc[i >> 1].x * qf[nt][i & 1];
+        if (okmask != 0xffffffffu) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[nt][i] = (okmask >> (my_tok + (i & 2) + 4 * (i & 4))) & 1u ? x[nt][i] : -INFINITY;
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            top[nt][h] = fmaxf(fmaxf(x[nt][h], x[nt][2 + h]), fmaxf(x[nt][4 + h], x[nt][6 + h]));
+            tope[nt][h] = fmaxf(fmaxf(x[nt][h] + sc[0].y, x[nt][2 + h] + sc[1].y), fmaxf(x[nt][4 + h] + sc[2].y, x[nt][6 + h] + sc[3].y));
+            move = move || top[nt][h] > mx[nt][h] + kLazy || tope[nt][h] > m[nt][h] + kLazy;
+          }
         if (__any_sync(0xffffffffu, move)) {  // some head's references have to move: to the largest seen so far
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              float top = fmaxf(x[nt][k], x[nt][k + 2]), tope = fmaxf(x[nt][k] + sc_lo.y, x[nt][k + 2] + sc_hi.y);
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
               for (int d = 4; d <= 16; d <<= 1) {
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                tope = fmaxf(tope, __shfl_xor_sync(0xffffffffu, tope, d));
+                top[nt][h] = fmaxf(top[nt][h], __shfl_xor_sync(0xffffffffu, top[nt][h], d));
+                tope[nt][h] = fmaxf(tope[nt][h], __shfl_xor_sync(0xffffffffu, tope[nt][h], d));
               }
-              top = fmaxf(mx[nt][k], top);
-              tope = fmaxf(m[nt][k], tope);
-              l[nt][k] *= top == -INFINITY ? 1.f : fast_exp2(mx[nt][k] - top);
-              const float alpha = tope == -INFINITY ? 1.f : fast_exp2(m[nt][k] - tope);
-              mx[nt][k] = top;
-              m[nt][k] = tope;
+              const float mxn = fmaxf(mx[nt][h], top[nt][h]), mn = fmaxf(m[nt][h], tope[nt][h]);
+              l[nt][h] *= fast_exp2(mx[nt][h] - mxn);
+              const float alpha = fast_exp2(m[nt][h] - mn);
+              mx[nt][h] = mxn;
+              m[nt][h] = mn;
 #pragma unroll
-              for (int c = 0; c < 8; ++c) { o[nt][c][k] *= alpha; o[nt][c][k + 2] *= alpha; }
+              for (int c = 0; c < 8; ++c) { o[nt][c][h] *= alpha; o[nt][c][h + 2] *= alpha; }
             }
         }
-        uint32_t pb[NT][2];
+        uint32_t pb[NT][4];  // weights as the second product's columns: tokens 4 (lane & 3) + {0, 1}, {2, 3}, then those + 16
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float pv[4];
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i4 = 0; i4 < 4; ++i4) {
-            const float2& sc = i4 < 2 ? sc_lo : sc_hi;
-            const bool none = m[nt][i4 & 1] == -INFINITY;  // every token so far masked
-            l[nt][i4 & 1] += none ? 0.f : fast_exp2(x[nt][i4] - mx[nt][i4 & 1]);
-            pv[i4] = none ? 0.f : fast_exp2(x[nt][i4] + sc.y - m[nt][i4 & 1]);
+          for (int t = 0; t < 4; ++t) {
+            float w[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              l[nt][h] += fast_exp2(x[nt][2 * t + h] - mx[nt][h]);
+              w[h] = fast_exp2(x[nt][2 * t + h] + sc[t].y - m[nt][h]);
+            }
+            pb[nt][t] = movmatrix_trans(pack_f16x2(w[0], w[1]));
           }
-          // held [token][head]; the second product wants [head][token]
-          pb[nt][0] = movmatrix_trans(pack_f16x2(pv[0], pv[1]));
-          pb[nt][1] = movmatrix_trans(pack_f16x2(pv[2], pv[3]));
-        }
 #pragma unroll
-        for (int c = 0; c < 8; c += 2) {
-          const int mi = lane >> 3;
-          uint32_t v[4];  // (chunk c, tokens 0-7), (c, 8-15), (c + 1, 0-7), (c + 1, 8-15)
-          ldmatrix_x4_trans(v, vbuf + chunk_at((mi & 1) * 8 + (lane & 7), c + (mi >> 1)));
-#pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = __byte_perm(v[k], 0u, 0x3120);
+        for (int c = 0; c < 8; ++c) {
+          uint32_t v[4];  // tokens 0-15 of dimensions 16 c + rowq and + 8, then tokens 16-31
+          ldmatrix_b8_x2_trans(v, (v_frag + at) ^ (uint32_t)(c << 4));
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const uint32_t a0 = e4m3x2_to_f16x2(v[2 * k]), a1 = e4m3x2_hi_to_f16x2(v[2 * k]);
-            const uint32_t a2 = e4m3x2_to_f16x2(v[2 * k + 1]), a3 = e4m3x2_hi_to_f16x2(v[2 * k + 1]);
+            const uint32_t a0 = e4m3x2_to_f16x2(v[2 * k]), a2 = e4m3x2_hi_to_f16x2(v[2 * k]);
+            const uint32_t a1 = e4m3x2_to_f16x2(v[2 * k + 1]), a3 = e4m3x2_hi_to_f16x2(v[2 * k + 1]);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][c + k], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+            for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][c], a0, a1, a2, a3, pb[nt][2 * k], pb[nt][2 * k + 1]);
           }
         }
         __syncwarp();  // everyone is done with this buffer before it is refilled
-        settle(i + STAGES - 1, pend);
-        pend = issue(i + STAGES, rawX, blkX);
+        settle(i + STAGES - 1, pend_k, pend_v);
+        issue(i + STAGES, rawX, blkX, pend_k, pend_v);
         rawX = rawY;
         blkX = blk_new;
         rawY = raw_new;
@@ -379,9 +407,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int d = 4; d <= 16; d <<= 1) l[nt][k] += __shfl_xor_sync(0xffffffffu, l[nt][k], d);
+          for (int d = 4; d <= 16; d <<= 1) l[nt][h] += __shfl_xor_sync(0xffffffffu, l[nt][h], d);
     }
     wait_now();  // a segment without tokens has read nothing yet; what follows writes global memory
     if (!n_ok && lane == 0 && first_of_row) flag_status(a.status, CLSA_DEV_BAD_SEQLEN);
@@ -393,15 +421,19 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int head = nt * 8 + hcol + k;
+      for (int h = 0; h < 2; ++h) {
+        const int head = nt * 8 + hcol + h;
         if (head < G) {
-          const float inv = whole ? (l[nt][k] != 0.f ? 1.f / l[nt][k] : 0.f) : 1.f;
-          const float half = whole ? fast_exp2(0.5f * (m[nt][k] - mx[nt][k])) : 1.f;  // applied twice: its square may not be a float
+          // a whole unit is normalised here; the references' difference is applied in two halves: its square may not be a float
+          const float inv = whole ? (l[nt][h] != 0.f ? 1.f / l[nt][h] : 0.f) : 1.f;
+          const float half = whole && l[nt][h] != 0.f ? fast_exp2(0.5f * (m[nt][h] - mx[nt][h])) : 1.f;
+          float* dst = mypart + head * kPartialStride + rowq;
 #pragma unroll
-          for (int c = 0; c < 8; ++c)
-            *reinterpret_cast<float2*>(mypart + head * kPartialStride + 16 * c + 2 * rowq) = inv == 0.f ? make_float2(0.f, 0.f) : make_float2(o[nt][c][k] * inv * half * half, o[nt][c][k + 2] * inv * half * half);
-          if (rowq == 0) *reinterpret_cast<float4*>(mypart + head * kPartialStride + 128) = make_float4(mx[nt][k], l[nt][k], m[nt][k], 0.f);
+          for (int c = 0; c < 8; ++c) {
+            dst[16 * c] = o[nt][c][h] * inv * half * half;
+            dst[16 * c + 8] = o[nt][c][h + 2] * inv * half * half;
+          }
+          if (rowq == 0) *reinterpret_cast<float4*>(mypart + head * kPartialStride + 128) = make_float4(mx[nt][h], l[nt][h], m[nt][h], 0.f);
         }
       }
     __syncwarp();
@@ -431,32 +463,32 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   if (w0 >= W) return;
   const int nw = min(W - w0, a.wpb);
   const int b_lo = span_tab[0].x, b_hi = span_tab[nw - 1].y;
-  const int u_first = b_lo / NS, u_last = (b_hi - 1) / NS;
   const int rec4 = G * (kPartialStride / 4);
   const float4* early = reinterpret_cast<const float4*>(a.part);
   float4* bpart = reinterpret_cast<float4*>(a.part) + (int64_t)W * rec4;  // 2 records per block: its first unit, its last
-  // only units that no warp had whole: at most a unit per pair of neighbouring warps, and the block's first and last
-  const int njobs = (u_last - u_first + 1) * G;
-  for (int job = warp; job < njobs; job += WARPS) {
-    const int u = u_first + job / G, hh = job % G;
+  // Units that no warp of the block had whole, found by the first warp whose span reaches into them: the unit its span starts in,
+  // unless the warp before it reaches into that too, and the unit its span ends in.
+  for (int job = warp; job < 2 * nw * G; job += WARPS) {
+    const int hh = job % G, own = job / G / 2, end = job / G % 2;
+    const int2 my = span_tab[own];
+    const int u = (end ? my.y - 1 : my.x) / NS;
+    if (my.x <= u * NS && my.y >= (u + 1) * NS) continue;                    // whole: written already
+    if (end ? u == my.x / NS : own > 0 && my.x > u * NS) continue;           // found at the span's start, or by an earlier warp
     const int us = u * NS, ue = us + NS;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float L = 0.f, MX = -INFINITY, M = -INFINITY;
+    float L = 0.f, MX = kNone, M = kNone;
     auto fold = [&](float4 ml, float4 v) {  // ml: mx, l, m
       const float Mn = fmaxf(M, ml.z), Xn = fmaxf(MX, ml.x);
-      const float mu = Mn == -INFINITY ? 0.f : Mn, xu = Xn == -INFINITY ? 0.f : Xn;
-      const float so = fast_exp2(M - mu), sn = fast_exp2(ml.z - mu);
+      const float so = fast_exp2(M - Mn), sn = fast_exp2(ml.z - Mn);
       acc.x = fmaf(sn, v.x, acc.x * so); acc.y = fmaf(sn, v.y, acc.y * so);
       acc.z = fmaf(sn, v.z, acc.z * so); acc.w = fmaf(sn, v.w, acc.w * so);
-      L = fmaf(fast_exp2(ml.x - xu), ml.y, L * fast_exp2(MX - xu));
+      L = fmaf(fast_exp2(ml.x - Xn), ml.y, L * fast_exp2(MX - Xn));
       M = Mn;
       MX = Xn;
     };
-    bool done = false;
-    for (int lw = 0; lw < nw; ++lw) {
+    for (int lw = own; lw < nw; ++lw) {
       const int2 sp = span_tab[lw];
-      if (sp.x >= ue || sp.y <= us) continue;
-      if (sp.x <= us && sp.y >= ue) { done = true; break; }
+      if (sp.x >= ue) break;
       const int last_stage = a.reverse ? sp.x : sp.y - 1;
       float4 ml, v;
       if (last_stage >= us && last_stage < ue) {
@@ -470,7 +502,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       }
       fold(ml, v);
     }
-    if (done) continue;
     const int g = u / a.rows, r = u - g * a.rows;
     const int64_t item = (int64_t)r * a.num_q_heads + g * G + hh;
     if (!(b_lo <= us && b_hi >= ue)) {
@@ -493,7 +524,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       if (lane == 0) *counter = 0u;
       acc = make_float4(0.f, 0.f, 0.f, 0.f);
       L = 0.f;
-      MX = M = -INFINITY;
+      MX = M = kNone;
       for (int b2 = blk_first; b2 <= blk_last; ++b2) {
         const int kind = b2 == blk_first && lo_first < us ? 1 : 0;
         const float4* pr = bpart + (int64_t)(2 * b2 + kind) * rec4 + hh * (kPartialStride / 4);
@@ -510,8 +541,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   }
 }
 
-constexpr int kWarpsNarrow = 16, kStagesNarrow = 3;  // groups of up to 8 query heads
-constexpr int kWarpsWide = 8, kStagesWide = 4;       // wider groups: twice the accumulators per thread
+constexpr int kWarpsNarrow = 12, kStagesNarrow = 2;  // groups of up to 8 query heads
+constexpr int kWarpsWide = 8, kStagesWide = 3;       // wider groups: twice the accumulators per thread
 
 }  // namespace
 
@@ -519,14 +550,12 @@ Attn8Plan make_attn8_plan(const clsa_params& p, const DeviceInfo& dev) {
   Attn8Plan plan;
   const bool wide = p.num_q_heads / p.num_kv_heads > 8;
   plan.warps = wide ? kWarpsWide : kWarpsNarrow;
-  plan.stages = wide ? kStagesWide : kStagesNarrow;
-  plan.smem_bytes = wide ? Shape<2, kWarpsWide, kStagesWide>::kSmem : Shape<1, kWarpsNarrow, kStagesNarrow>::kSmem;
+  plan.smem_bytes = wide ? Shape<kWarpsWide, kStagesWide>::kSmem : Shape<kWarpsNarrow, kStagesNarrow>::kSmem;
   plan.units = (int64_t)p.num_seqs * p.q_per_seq * p.num_kv_heads;
   plan.unit_stages = (p.top_k + kTok - 1) / kTok;
   plan.total_stages = plan.units * plan.unit_stages;
   int64_t blocks = dev.sm_count;
-  int64_t workers = plan.total_stages / kMinStages8;
-  if (workers < 1) workers = 1;
+  int64_t workers = plan.total_stages;
   if (workers > blocks * plan.warps) workers = blocks * plan.warps;
   if (blocks > workers) blocks = workers;
   plan.wpb = (int)((workers + blocks - 1) / blocks);
@@ -570,6 +599,7 @@ cudaError_t launch_sparse_attn8(const clsa_params& p, const clsa_cache8& c, cons
   a.block_table = p.block_table;
   while (p.block_table != nullptr && (1 << a.block_shift) < p.block_size) ++a.block_shift;
   a.max_blocks = p.max_blocks_per_seq;
+  a.page_limit = (uint32_t)((p.num_cache_rows + (1 << a.block_shift) - 1) >> a.block_shift);
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
   a.status = status;

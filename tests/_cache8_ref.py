@@ -9,8 +9,10 @@ Tolerances (each rounding counts torch.finfo(t).eps / 2: bf16 2^-8, fp16 2^-11, 
   scores      products are exact, at most 128 fp32 sums, each cut to 2^-23 of the magnitudes: 2^-16 sum |q_j k_j|; and 2^-149, the
               distance of neighbouring fp32 values below 2^-126: a score of smaller magnitude than that has no fp32 form but 0.
   attention   logits as the scores plus three fp32 roundings of numbers up to |x| + 128 in the log2 domain:
-              eps = 2^-16 sm_scale sum |q k| + 2^-21 (|x| + 128). A weight is off by that and by one f16 rounding, the outputs
-              by 2^-8 |o| + (2^-11 + 2^-15 + 2 eps) sum p |v|, the log-sum-exp by eps + 2^-21 (|lse| + 1).
+              eps = 2^-16 sm_scale sum |q k| + 2^-21 (|x| + 128). A weight is off by that and by one f16 rounding, 2^-11 of it, or
+              2^-25 where it is subnormal; the largest weight of a sum is at least 1, so that is 2^-25 of the largest p 2^ev, times
+              the code. Outputs: 2^-8 |o| + (2^-11 + 2^-15 + 2 eps) sum p |v| + 2^-25 max(p 2^ev) sum |code|, the log-sum-exp:
+              eps + 2^-21 (|lse| + 1) (its sum is of unrounded weights).
 """
 from __future__ import annotations
 
@@ -105,20 +107,22 @@ def scores(q, keys):
     return q @ keys.T, np.abs(q) @ np.abs(keys).T
 
 
-def attention(q, k, v, sm_scale):
-    """q [H, D], k, v [c, G, D] of the selected rows: (out [H, D], lse [H], tolerance of out, tolerance of lse)."""
+def attention(q, k, v, f, sm_scale):
+    """q [H, D], k, v [c, G, D] of the selected rows, f [c, G] the scales of v's rows: (out [H, D], lse [H], tolerance of out,
+    tolerance of lse)."""
     H, G = q.shape[0], k.shape[1]
     if k.shape[0] == 0:
         return np.zeros_like(q), np.full(H, -np.inf), np.zeros_like(q), np.zeros(H)
-    k, v = np.repeat(k, H // G, 1), np.repeat(v, H // G, 1)
+    k, v, f = np.repeat(k, H // G, 1), np.repeat(v, H // G, 1), np.repeat(f, H // G, 1)
     x = np.einsum("hd,chd->hc", q, k) * sm_scale
-    mag = np.einsum("hd,chd->hc", np.abs(q), np.abs(k)) * sm_scale
+    mag = 2.0 ** -16 * np.einsum("hd,chd->hc", np.abs(q), np.abs(k)) * sm_scale
     top = x.max(-1, keepdims=True)
     w = np.exp(x - top)
     tot = w.sum(-1, keepdims=True)
     p = w / tot
     lse = (top + np.log(tot))[:, 0]
     out = np.einsum("hc,chd->hd", p, v)
-    eps = (2.0 ** -16 * mag + 2.0 ** -21 * (np.abs(x) + 128)).max(-1)
+    eps = (mag + 2.0 ** -21 * (np.abs(x) + 128)).max(-1)
     tol = 2.0 ** -8 * np.abs(out) + (2.0 ** -11 + 2.0 ** -15 + 2 * eps)[:, None] * np.einsum("hc,chd->hd", p, np.abs(v))
+    tol += 2.0 ** -25 * (p * f.T).max(-1)[:, None] * (np.abs(v) / f[..., None]).sum(0)
     return out, lse, tol, eps + 2.0 ** -21 * (np.abs(lse) + 1)

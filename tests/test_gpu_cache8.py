@@ -404,7 +404,8 @@ def check_attn(c, hq, q, idx, cnt, out, lse, sm_scale=128 ** -0.5, sample=None):
     pairs = [(b, t) for b in range(c.B) for t in range(c.T)]
     for b, t in pairs if sample is None else [pairs[i] for i in np.random.default_rng(0).permutation(len(pairs))[:sample]]:
         rows = c.row(b, ih[b, t, :ch[b, t]])
-        o, l, tol, ltol = ref.attention(f64(q[b, t]), kv[rows], vv[rows], sm_scale)
+        f = 2.0 ** (np.clip(vs[:, np.asarray(rows) // c.block].astype(np.float64), 27, 247).T - 127)
+        o, l, tol, ltol = ref.attention(f64(q[b, t]), kv[rows], vv[rows], f, sm_scale)
         got = f64(out[b, t])
         assert (np.abs(got - o) <= tol).all(), (b, t, float((np.abs(got - o) - tol).max()))
         if lse is not None:
