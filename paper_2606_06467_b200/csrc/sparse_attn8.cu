@@ -104,7 +104,7 @@ template <int WARPS, int STAGES>
 struct Shape {
   static constexpr int kRing = STAGES * kStage8Bytes;
   static constexpr int kScale = STAGES * kTok * 8;  // per token: 2^ek, ev
-  static constexpr size_t kSmem = (size_t)WARPS * (kRing + kScale + STAGES * 4) + WARPS * sizeof(int2);
+  static constexpr size_t kSmem = (size_t)WARPS * (kRing + kScale + STAGES * 4) + WARPS * (sizeof(int2) + sizeof(int2));
 };
 
 template <int NT, int WARPS, int STAGES, bool PAGED>
@@ -123,7 +123,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   float2* scales = reinterpret_cast<float2*>(smem + WARPS * S::kRing + warp * S::kScale);
   uint32_t* stage_mask = reinterpret_cast<uint32_t*>(smem + WARPS * (S::kRing + S::kScale)) + warp * STAGES;
   int2* span_tab = reinterpret_cast<int2*>(smem + WARPS * (S::kRing + S::kScale + STAGES * 4));
-  if (lane == 0) span_tab[warp] = make_int2(s_begin, s_end);
+  int2* split_tab = span_tab + WARPS;
+  if (lane == 0) {
+    // For the merge: the units that this warp does not have whole and that no earlier warp of the block reaches into -- the
+    // one its span starts in, the one it ends in -- or -1.
+    const int uf = s_begin / NS, ul = has_work ? (s_end - 1) / NS : 0;
+    span_tab[warp] = make_int2(s_begin, s_end);
+    split_tab[warp] = make_int2(has_work && (s_begin > uf * NS || s_end < (uf + 1) * NS) && (warp == 0 || s_begin == uf * NS) ? uf : -1,
+                                has_work && ul != uf && s_end < (ul + 1) * NS ? ul : -1);
+  }
 
   // Programmatic dependent launch, as in the bf16 kernels: dependents are released only behind this grid's own wait.
   bool waited = false;
@@ -466,78 +474,92 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   const int rec4 = G * (kPartialStride / 4);
   const float4* early = reinterpret_cast<const float4*>(a.part);
   float4* bpart = reinterpret_cast<float4*>(a.part) + (int64_t)W * rec4;  // 2 records per block: its first unit, its last
-  // Units that no warp of the block had whole, found by the first warp whose span reaches into them: the unit its span starts in,
-  // unless the warp before it reaches into that too, and the unit its span ends in.
-  for (int job = warp; job < 2 * nw * G; job += WARPS) {
-    const int hh = job % G, own = job / G / 2, end = job / G % 2;
-    const int2 my = span_tab[own];
-    const int u = (end ? my.y - 1 : my.x) / NS;
-    if (my.x <= u * NS && my.y >= (u + 1) * NS) continue;                    // whole: written already
-    if (end ? u == my.x / NS : own > 0 && my.x > u * NS) continue;           // found at the span's start, or by an earlier warp
-    const int us = u * NS, ue = us + NS;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float L = 0.f, MX = kNone, M = kNone;
-    auto fold = [&](float4 ml, float4 v) {  // ml: mx, l, m
-      const float Mn = fmaxf(M, ml.z), Xn = fmaxf(MX, ml.x);
-      const float so = fast_exp2(M - Mn), sn = fast_exp2(ml.z - Mn);
-      acc.x = fmaf(sn, v.x, acc.x * so); acc.y = fmaf(sn, v.y, acc.y * so);
-      acc.z = fmaf(sn, v.z, acc.z * so); acc.w = fmaf(sn, v.w, acc.w * so);
-      L = fmaf(fast_exp2(ml.x - Xn), ml.y, L * fast_exp2(MX - Xn));
-      M = Mn;
-      MX = Xn;
-    };
-    for (int lw = own; lw < nw; ++lw) {
-      const int2 sp = span_tab[lw];
-      if (sp.x >= ue) break;
-      const int last_stage = a.reverse ? sp.x : sp.y - 1;
-      float4 ml, v;
-      if (last_stage >= us && last_stage < ue) {
-        const float* pr = reinterpret_cast<const float*>(smem + lw * S::kRing) + hh * kPartialStride;
-        ml = *reinterpret_cast<const float4*>(pr + 128);
-        v = *reinterpret_cast<const float4*>(pr + lane * 4);
-      } else {
-        const float4* pr = early + (int64_t)(w0 + lw) * rec4 + hh * (kPartialStride / 4);
-        ml = __ldcg(pr + 32);
-        v = __ldcg(pr + lane);
-      }
-      fold(ml, v);
+
+  // Up to 32 partials at once, lane i holding the references and sum (mx, l, m) of the i-th and fetch(i) its outputs.
+  float4 acc;
+  float L, MX, M;
+  auto fold = [&](float4 ml, int count, auto fetch) {
+    float mn = fmaxf(M, ml.z), xn = fmaxf(MX, ml.x);
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) {
+      mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
+      xn = fmaxf(xn, __shfl_xor_sync(0xffffffffu, xn, d));
     }
-    const int g = u / a.rows, r = u - g * a.rows;
-    const int64_t item = (int64_t)r * a.num_q_heads + g * G + hh;
-    if (!(b_lo <= us && b_hi >= ue)) {
-      // the unit straddles blocks: leave this block's partial, arrive, and finish the pair if this completes it
-      float4* slot = bpart + (int64_t)(2 * blockIdx.x + (b_lo < us ? 1 : 0)) * rec4 + hh * (kPartialStride / 4);
-      __stcg(slot + lane, acc);
-      if (lane == 0) __stcg(slot + 32, make_float4(MX, L, M, 0.f));
-      asm volatile("fence.acq_rel.gpu;" ::: "memory");
-      __syncwarp();
-      int wf, wl;
-      unit_workers(u, a, wf, wl);
-      const int blk_first = wf / a.wpb, blk_last = wl / a.wpb;
-      const int lo_first = span_begin(blk_first * a.wpb, a);
-      uint32_t* counter = a.arrive + blk_first * kMaxGroup + hh;  // one unit at most leaves a block to the right
-      unsigned prev = 0;
-      if (lane == 0) prev = atomicAdd(counter, 1u);
-      prev = __shfl_sync(0xffffffffu, prev, 0);
-      if (prev + 1u != (unsigned)(blk_last - blk_first + 1)) continue;
-      asm volatile("fence.acq_rel.gpu;" ::: "memory");
-      if (lane == 0) *counter = 0u;
+    const float sn = fast_exp2(ml.z - mn), so = fast_exp2(M - mn);
+    float sum = fast_exp2(ml.x - xn) * ml.y;
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    L = L * fast_exp2(MX - xn) + sum;
+    acc.x *= so; acc.y *= so; acc.z *= so; acc.w *= so;
+#pragma unroll 4
+    for (int i = 0; i < count; ++i) {
+      const float4 v = fetch(i);
+      const float f = __shfl_sync(0xffffffffu, sn, i);
+      acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+    }
+    M = mn;
+    MX = xn;
+  };
+  const float4 nothing = make_float4(kNone, 0.f, kNone, 0.f);
+
+  const int2 my_split = lane < 2 * nw ? split_tab[lane >> 1] : make_int2(-1, -1);
+  const int my_unit = lane & 1 ? my_split.y : my_split.x;
+  const int2 my_span = lane < nw ? span_tab[lane] : make_int2(0, 0);
+  int hh = warp;
+  for (uint32_t todo = __ballot_sync(0xffffffffu, my_unit >= 0); todo != 0u; todo &= todo - 1u, hh -= G) {
+    const int own = (__ffs(todo) - 1) >> 1, u = __shfl_sync(0xffffffffu, my_unit, __ffs(todo) - 1);
+    const int us = u * NS, ue = us + NS;
+    const int nparts = __popc(__ballot_sync(0xffffffffu, lane >= own && lane < nw && my_span.x < ue));  // warps own .. share it
+    for (; hh < G; hh += WARPS) {
       acc = make_float4(0.f, 0.f, 0.f, 0.f);
       L = 0.f;
       MX = M = kNone;
-      for (int b2 = blk_first; b2 <= blk_last; ++b2) {
-        const int kind = b2 == blk_first && lo_first < us ? 1 : 0;
-        const float4* pr = bpart + (int64_t)(2 * b2 + kind) * rec4 + hh * (kPartialStride / 4);
-        fold(__ldcg(pr + 32), __ldcg(pr + lane));
+      auto record = [&](int lw) -> const float4* {  // partial of warp lw: in its ring if the unit was the last of its walk
+        const int2 sp = span_tab[lw];
+        const int last = a.reverse ? sp.x : sp.y - 1;
+        return last >= us && last < ue ? reinterpret_cast<const float4*>(smem + lw * S::kRing) + hh * (kPartialStride / 4)
+                                       : early + (int64_t)(w0 + lw) * rec4 + hh * (kPartialStride / 4);
+      };
+      fold(lane < nparts ? record(own + lane)[32] : nothing, nparts, [&](int i) { return record(own + i)[lane]; });
+      const int g = u / a.rows, r = u - g * a.rows;
+      const int64_t item = (int64_t)r * a.num_q_heads + g * G + hh;
+      if (!(b_lo <= us && b_hi >= ue)) {
+        // the unit straddles blocks: leave this block's partial, arrive, and finish the pair if this completes it
+        float4* slot = bpart + (int64_t)(2 * blockIdx.x + (b_lo < us ? 1 : 0)) * rec4 + hh * (kPartialStride / 4);
+        __stcg(slot + lane, acc);
+        if (lane == 0) __stcg(slot + 32, make_float4(MX, L, M, 0.f));
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");
+        __syncwarp();
+        int wf, wl;
+        unit_workers(u, a, wf, wl);
+        const int blk_first = wf / a.wpb, blk_last = wl / a.wpb;
+        const int lo_first = span_begin(blk_first * a.wpb, a);
+        uint32_t* counter = a.arrive + blk_first * kMaxGroup + hh;  // one unit at most leaves a block to the right
+        unsigned prev = 0;
+        if (lane == 0) prev = atomicAdd(counter, 1u);
+        prev = __shfl_sync(0xffffffffu, prev, 0);
+        if (prev + 1u != (unsigned)(blk_last - blk_first + 1)) continue;
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");
+        if (lane == 0) *counter = 0u;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        L = 0.f;
+        MX = M = kNone;
+        auto block_record = [&](int b2) {
+          const int kind = b2 == blk_first && lo_first < us ? 1 : 0;
+          return bpart + (int64_t)(2 * b2 + kind) * rec4 + hh * (kPartialStride / 4);
+        };
+        for (int b0 = blk_first; b0 <= blk_last; b0 += 32)  // in block order: the result does not depend on who arrived last
+          fold(b0 + lane <= blk_last ? __ldcg(block_record(b0 + lane) + 32) : nothing, min(32, blk_last - b0 + 1),
+               [&](int i) { return __ldcg(block_record(b0 + i) + lane); });
       }
+      if (L != 0.f) {
+        const float inv = 1.f / L, half = fast_exp2(0.5f * (M - MX));
+        acc.x = acc.x * inv * half * half; acc.y = acc.y * inv * half * half;
+        acc.z = acc.z * inv * half * half; acc.w = acc.w * inv * half * half;
+      }
+      *reinterpret_cast<uint2*>(a.out + item * 128 + lane * 4) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+      if (a.lse != nullptr && lane == 0) a.lse[item] = L != 0.f ? (MX + log2f(L)) * kLn2 : -INFINITY;
     }
-    if (L != 0.f) {
-      const float inv = 1.f / L, half = fast_exp2(0.5f * (M - MX));
-      acc.x = acc.x * inv * half * half; acc.y = acc.y * inv * half * half;
-      acc.z = acc.z * inv * half * half; acc.w = acc.w * inv * half * half;
-    }
-    *reinterpret_cast<uint2*>(a.out + item * 128 + lane * 4) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
-    if (a.lse != nullptr && lane == 0) a.lse[item] = L != 0.f ? (MX + log2f(L)) * kLn2 : -INFINITY;
   }
 }
 
@@ -554,20 +576,33 @@ Attn8Plan make_attn8_plan(const clsa_params& p, const DeviceInfo& dev) {
   plan.units = (int64_t)p.num_seqs * p.q_per_seq * p.num_kv_heads;
   plan.unit_stages = (p.top_k + kTok - 1) / kTok;
   plan.total_stages = plan.units * plan.unit_stages;
-  int64_t blocks = dev.sm_count;
-  int64_t workers = plan.total_stages;
-  if (workers > blocks * plan.warps) workers = blocks * plan.warps;
-  if (blocks > workers) blocks = workers;
-  plan.wpb = (int)((workers + blocks - 1) / blocks);
-  plan.blocks = (int)((workers + plan.wpb - 1) / plan.wpb);
-  plan.workers = (int)workers;
-  // Unit-aligned split when every unit can have workers of its own and the longest span that results stays within 15 % of the
-  // even share.
-  plan.aligned = 0;
-  if (workers >= plan.units) {
-    const int64_t longest = (plan.unit_stages + workers / plan.units - 1) / (workers / plan.units);
-    if (longest * workers * 100 <= plan.total_stages * 115) plan.aligned = 1;
+  int64_t blocks, workers;
+  if (plan.units <= dev.sm_count) {
+    // every unit has blocks of its own: one where that fills most of the SMs, else as many as give a warp two stages
+    int64_t per_unit = plan.units * 10 >= dev.sm_count * 6 ? 1 : dev.sm_count / plan.units;
+    const int64_t most = (plan.unit_stages + 2 * plan.warps - 1) / (2 * plan.warps);
+    if (per_unit > most) per_unit = most;
+    plan.wpb = (int)((plan.unit_stages + per_unit - 1) / per_unit);
+    if (plan.wpb > plan.warps) plan.wpb = plan.warps;
+    while (per_unit * plan.wpb > plan.unit_stages) --per_unit;  // no worker without a stage
+    blocks = plan.units * per_unit;
+    workers = blocks * plan.wpb;
+    plan.aligned = 1;
+  } else {
+    blocks = dev.sm_count;
+    workers = plan.total_stages < blocks * plan.warps ? plan.total_stages : blocks * plan.warps;
+    plan.wpb = (int)((workers + blocks - 1) / blocks);
+    blocks = (workers + plan.wpb - 1) / plan.wpb;
+    // Unit-aligned split when every unit can have workers of its own and the longest span that results stays within 15 % of
+    // the even share.
+    plan.aligned = 0;
+    if (workers >= plan.units) {
+      const int64_t longest = (plan.unit_stages + workers / plan.units - 1) / (workers / plan.units);
+      if (longest * workers * 100 <= plan.total_stages * 115) plan.aligned = 1;
+    }
   }
+  plan.blocks = (int)blocks;
+  plan.workers = (int)workers;
   return plan;
 }
 
