@@ -120,7 +120,7 @@ __device__ __forceinline__ void turn_of(int pos, float freq, float scale, float*
   *s *= scale;
 }
 template <int LANES>
-__device__ __forceinline__ void head_norm(float (&x)[8], const float (&w)[8], float eps) {
+__device__ __forceinline__ void head_norm(float (&x)[8], const float (&w)[8], float eps) {  // the lanes' shares of 32 / LANES heads
   float ss = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
@@ -156,6 +156,29 @@ __device__ __forceinline__ void head_rotate(float (&x)[8], const float (&c)[8], 
     }
   }
 }
+// Two fp32 numbers in a register pair: one instruction works on both.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t bf16x2_to_f32x2(uint32_t w) { return pack2(bf16_lo(w), bf16_hi(w)); }
+
 __device__ __forceinline__ void unpack_bf16x8(float (&x)[8], const uint4& w) {
   x[0] = bf16_lo(w.x); x[1] = bf16_hi(w.x); x[2] = bf16_lo(w.y); x[3] = bf16_hi(w.y);
   x[4] = bf16_lo(w.z); x[5] = bf16_hi(w.z); x[6] = bf16_lo(w.w); x[7] = bf16_hi(w.w);

@@ -1,11 +1,14 @@
 // The newest tokens' K, V and K_idx rows into the 8-bit caches: per block of SB cache rows and head, the largest magnitude of
 // the new rows gives the block's power-of-two scale, and each element is rounded once to e4m3.
 //
-// A block of threads takes one scale block of one sequence and one or more heads of the list K heads, V heads, K_idx: 16 (or,
-// for 64-wide indexer keys, 8) lanes per row with 16 bytes each, all rows of a head in registers between the pass that finds
-// the maximum and the pass that writes the codes, so every element is read once. Bound by HBM for long prompts (2 bytes in,
-// 1 out), by one launch and two dependent round trips for a decode step. K's norm and rotation happen on the way in fp32.
-// A scale block that holds older rows is re-coded by the same threads when its exponent grows.
+// Chunks (T > 1): a block of threads takes one scale block of one sequence and K and V of one or more heads (or K_idx), the rows of
+// the next on their way while it works on one: 16 (or, for 64-wide indexer keys, 8) lanes per row with 16 bytes each, all rows of a head in registers between the
+// pass that finds the maximum and the pass that writes the codes, so every element is read once. Bound by HBM for long prompts
+// (2 bytes in, 1 out). K's norm and rotation happen on the way in fp32. The angles of the rows are built by
+// the addition theorem: a row's position is begin + 8 u + v, and cosines and sines of SB / 8 + 8 positions, formed once for all
+// the block's K heads, give those of all SB rows at two instructions a pair of dimensions. A scale block that holds older rows is re-coded by the same threads when its exponent grows.
+// Single tokens (T = 1): half a warp per row, no block barrier; what does not depend on the sequence's length (the row, the
+// weight, the frequencies) is fetched together with it. Bound by a launch and two dependent round trips.
 #include "cache8.cuh"
 
 namespace clsa {
@@ -27,7 +30,8 @@ struct AppendArgs {
   const int32_t* block_table;
   int block_shift, max_blocks;
   int64_t num_rows;
-  int T, max_seq_len, spans, heads_per_block, items;
+  int num_seqs, T, max_seq_len, spans, items;
+  int heads_per_block, head_groups;  // chunks: heads of a block of threads, such groups (K_idx is a group behind them)
   uint32_t* status;
 };
 
@@ -38,92 +42,188 @@ __device__ __forceinline__ int need_exponent(float amax) {
   return min(max(e, kScaleExpMin), kScaleExpMax);
 }
 
-// One head of one scale block: rows `lo` .. `hi` - 1 of the block are new, rows below `lo` older ones of the sequence.
+// Eight codes times a power of two, rounded again.
+__device__ __forceinline__ uint2 recode(uint2 v, float f) {
+  const uint32_t in[4] = {e4m3x2_to_f16x2(v.x), e4m3x2_hi_to_f16x2(v.x), e4m3x2_to_f16x2(v.y), e4m3x2_hi_to_f16x2(v.y)};
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = f32x2_to_e4m3x2(f16_lo(in[i]) * f, f16_hi(in[i]) * f);
+  return make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+}
+
+constexpr float kLargest = 3.4028234663852886e38f;  // what is larger is not finite and does not count for a scale
+
+// A lane's 8 dimensions of a cosine or sine table row, as pairs.
+__device__ __forceinline__ void load_pairs(uint64_t (&p)[4], const float* t, bool inter, int i0) {
+  const float4 a = *reinterpret_cast<const float4*>(t + i0);
+  if (inter) {
+    p[0] = pack2(a.x, a.x); p[1] = pack2(a.y, a.y); p[2] = pack2(a.z, a.z); p[3] = pack2(a.w, a.w);
+  } else {
+    const float4 b = *reinterpret_cast<const float4*>(t + i0 + 4);
+    p[0] = pack2(a.x, a.y); p[1] = pack2(a.z, a.w); p[2] = pack2(b.x, b.y); p[3] = pack2(b.z, b.w);
+  }
+}
+
+// One head of one scale block: rows `lo` .. `hi` - 1 of the block are new, rows below `lo` older ones of the sequence. SPEC: the
+// rows go through K's norm and rotation first (LANES 16); bc, bs: cosines and sines of positions begin + 8 u, then of 0 .. 7.
 template <int SB, int THREADS, int LANES>
-__device__ __forceinline__ void append_head(const uint16_t* src, int64_t src_token, uint8_t* code, int64_t code_token,
-                                            uint8_t* scale, int lo, int hi, bool norm, bool rotate, const AppendArgs& a,
-                                            const float* tc, const float* ts, float* red) {
-  constexpr int kRowsPerPass = THREADS / LANES;
-  constexpr int R = SB / kRowsPerPass;
-  const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
-  float x[R][8];
-  {
-    uint4 raw[R];
+struct Rows {
+  static constexpr int kPerPass = THREADS / LANES;  // a multiple of 8: a lane's rows share their place among 8
+  static constexpr int R = SB / kPerPass;
+  uint4 raw[R];
+  __device__ __forceinline__ void load(const uint16_t* src, int64_t src_token, int lo, int hi) {  // zeros for rows that are not new
+    const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int row = r * kRowsPerPass + sub;
+      const int row = r * kPerPass + sub;
       raw[r] = make_uint4(0, 0, 0, 0);
-      if (row >= lo && row < hi) raw[r] = *reinterpret_cast<const uint4*>(src + (int64_t)(row - lo) * src_token + 8 * l);
+      if (row >= lo && row < hi) raw[r] = *reinterpret_cast<const uint4*>(src + (row - lo) * src_token + 8 * l);
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r) unpack_bf16x8(x[r], raw[r]);
   }
+};
+template <int SB, int THREADS, int LANES, bool SPEC>
+__device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows, uint8_t* code, int64_t code_token,
+                                            uint8_t* scale, int lo, int hi, const AppendArgs& a, const float* bc, const float* bs,
+                                            float* red) {
+  constexpr int kRowsPerPass = THREADS / LANES, R = Rows<SB, THREADS, LANES>::R;
+  const auto& raw = rows.raw;
+  const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
   const int e_old = lo > 0 ? scale_exponent(*scale) : kScaleExpMin;  // every thread reads it before the barrier below
-  if (norm) {
-    float w[8];
-    load_weight8(w, a.k_weight, 8 * l);
-#pragma unroll
-    for (int r = 0; r < R; ++r) head_norm<LANES>(x[r], w, a.spec.eps);
-  }
-  if (rotate) {
-    const int half = a.spec.rot_dim >> 1;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int row = r * kRowsPerPass + sub;
-      float c[8], s[8];
-      load_turns(c, s, tc + row * half, ts + row * half, a.spec.rot_dim, a.spec.interleaved, l);
-      head_rotate<LANES>(x[r], c, s, a.spec.rot_dim, a.spec.interleaved, l);
-    }
-  }
+  uint64_t x[R][4];
   float amax = 0.f;
+  if constexpr (SPEC) {
+    const int rot = a.spec.rot_dim, half = rot >> 1, hl = rot >> 4;
+    const bool turned = 8 * l < rot, inter = a.spec.interleaved;
+    const int partner = l < hl ? l + hl : (l < 2 * hl ? l - hl : l);
+    const int i0 = !turned ? 0 : inter ? 4 * l : (l < hl ? 8 * l : 8 * l - half);
+    // z_i = r (x_i w_i cos + x_partner w'_i sin), w' the partner's weight with the sign of its term
+    uint64_t w[4], wp[4], cv[4], sv[4];
+    {
+      uint4 wr = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);  // ones
+      if (a.spec.norm && a.k_weight != nullptr) wr = *reinterpret_cast<const uint4*>(a.k_weight + 8 * l);
+      const uint32_t w4[4] = {wr.x, wr.y, wr.z, wr.w};
+      const float sg = l < hl ? -1.f : 1.f;
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int row = r * kRowsPerPass + sub;
-    if (row >= lo && row < hi) {  // (table entries of other rows are not set)
+      for (int k = 0; k < 4; ++k) {
+        w[k] = bf16x2_to_f32x2(w4[k]);
+        const uint32_t p = inter ? __byte_perm(w4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, w4[k], partner, LANES);
+        wp[k] = turned ? mul2(bf16x2_to_f32x2(p), inter ? pack2(-1.f, 1.f) : pack2(sg, sg)) : 0ull;
+      }
+      if (rot > 0) {
+        load_pairs(cv, bc + (SB / 8 + (sub & 7)) * half, inter, i0);
+        load_pairs(sv, bs + (SB / 8 + (sub & 7)) * half, inter, i0);
+        if (!turned) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float m = fabsf(x[r][i]);
-        if (m <= 3.4028234663852886e38f) amax = fmaxf(amax, m);  // finite
+          for (int k = 0; k < 4; ++k) { cv[k] = pack2(1.f, 1.f); sv[k] = 0ull; }
+        }
       }
     }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int row = r * kRowsPerPass + sub;
+      const uint32_t in4[4] = {raw[r].x, raw[r].y, raw[r].z, raw[r].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[r][k] = bf16x2_to_f32x2(in4[k]);
+      float root = 1.f;
+      if (a.spec.norm) {
+        const float2 s2 = unpack2(fma2(x[r][3], x[r][3], fma2(x[r][2], x[r][2], fma2(x[r][1], x[r][1], mul2(x[r][0], x[r][0])))));
+        float ss = s2.x + s2.y;
+#pragma unroll
+        for (int m = LANES / 2; m >= 1; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+        root = rsqrtf(fmaf(ss, 1.f / (8 * LANES), a.spec.eps));
+      }
+      const uint64_t r2 = pack2(root, root);
+      if (rot > 0) {
+        uint64_t cu[4], su[4];
+        load_pairs(cu, bc + (row >> 3) * half, inter, i0);
+        load_pairs(su, bs + (row >> 3) * half, inter, i0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint64_t neg = su[k] ^ 0x8000000080000000ull;
+          const uint64_t c = turned ? fma2(cu[k], cv[k], mul2(neg, sv[k])) : cv[k], s = fma2(su[k], cv[k], mul2(cu[k], sv[k]));
+          uint32_t p = inter ? __byte_perm(in4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, in4[k], partner, LANES);
+          if (!turned) p = 0u;  // (an infinity times a zero sine is none)
+          x[r][k] = mul2(fma2(x[r][k], mul2(w[k], c), mul2(bf16x2_to_f32x2(p), mul2(wp[k], s))), r2);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[r][k] = mul2(mul2(x[r][k], w[k]), r2);
+      }
+      if (row >= lo && row < hi) {  // (rows that are not new are zeros under a norm of zeros)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 z = unpack2(x[r][k]);
+          amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));  // a NaN does not count
+        }
+      }
+    }
+  } else {
+    uint32_t top = 0u;  // bf16 magnitudes order as integers (rows that are not new are zeros)
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      top = __vmaxu2(__vmaxu2(top, raw[r].x & 0x7fff7fffu), __vmaxu2(raw[r].y & 0x7fff7fffu, __vmaxu2(raw[r].z & 0x7fff7fffu, raw[r].w & 0x7fff7fffu)));
+      const uint32_t in4[4] = {raw[r].x, raw[r].y, raw[r].z, raw[r].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[r][k] = bf16x2_to_f32x2(in4[k]);
+    }
+    amax = __uint_as_float(max(top << 16, top & 0xffff0000u));
+    if (amax != amax) amax = INFINITY;
   }
+  auto block_max = [&](float v) {
 #pragma unroll
-  for (int m = 16; m >= 1; m >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = amax;
-  __syncthreads();
+    for (int m = 16; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) amax = fmaxf(amax, red[w]);
+    for (int w = 0; w < THREADS / 32; ++w) v = fmaxf(v, red[w]);
+    return v;
+  };
+  amax = block_max(amax);
+  if (amax > kLargest) {  // something is not finite (the same for the whole block): the largest of the rest
+    amax = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int row = r * kRowsPerPass + sub;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 z = unpack2(x[r][k]);
+        if (row >= lo && row < hi && fabsf(z.x) <= kLargest) amax = fmaxf(amax, fabsf(z.x));
+        if (row >= lo && row < hi && fabsf(z.y) <= kLargest) amax = fmaxf(amax, fabsf(z.y));
+      }
+    }
+    __syncthreads();
+    amax = block_max(amax);
+  }
   const int e = max(need_exponent(amax), e_old);
   const float inv = exp2_int(-e);
+  const uint64_t inv2 = pack2(inv, inv);
   if (threadIdx.x == 0) *scale = (uint8_t)(e + 127);
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = r * kRowsPerPass + sub;
-    uint2* dst = reinterpret_cast<uint2*>(code + (int64_t)row * code_token + 8 * l);
+    uint2* dst = reinterpret_cast<uint2*>(code + row * code_token + 8 * l);
     if (row >= lo && row < hi) {
-      uint2 v;
-      v.x = f32x2_to_e4m3x2(x[r][0] * inv, x[r][1] * inv) | f32x2_to_e4m3x2(x[r][2] * inv, x[r][3] * inv) << 16;
-      v.y = f32x2_to_e4m3x2(x[r][4] * inv, x[r][5] * inv) | f32x2_to_e4m3x2(x[r][6] * inv, x[r][7] * inv) << 16;
-      *dst = v;
-    } else if (row < lo && e > e_old) {  // an older row: its codes move down by e - e_old exponents
-      const float f = exp2_int(max(e_old - e, -60));
-      const uint2 v = *dst;
-      const uint32_t in[4] = {e4m3x2_to_f16x2(v.x), e4m3x2_hi_to_f16x2(v.x), e4m3x2_to_f16x2(v.y), e4m3x2_hi_to_f16x2(v.y)};
       uint32_t o[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = f32x2_to_e4m3x2(f16_lo(in[i]) * f, f16_hi(in[i]) * f);
+      for (int k = 0; k < 4; ++k) {
+        const float2 z = unpack2(mul2(x[r][k], inv2));
+        o[k] = f32x2_to_e4m3x2(z.x, z.y);
+      }
       *dst = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+    } else if (row < lo && e > e_old) {  // an older row: its codes move down by e - e_old exponents
+      *dst = recode(*dst, exp2_int(max(e_old - e, -60)));
     }
   }
 }
 
 template <int SB, int THREADS>
-__global__ void __launch_bounds__(THREADS) cache8_append_kernel(const AppendArgs a) {
-  extern __shared__ __align__(16) float turns[];  // cosines, then sines: [SB][rot_dim / 2] each
+__global__ void __launch_bounds__(THREADS, 512 / THREADS) cache8_append_kernel(const __grid_constant__ AppendArgs a) {
+  extern __shared__ __align__(16) float turns[];  // cosines, then sines: [SB / 8 + 8][rot_dim / 2] each
   __shared__ float red[2][THREADS / 32];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int b = blockIdx.x / a.spans, span = blockIdx.x % a.spans;
   const int n = a.seq_len[b];
+  const int64_t start = a.block_table == nullptr ? a.seq_start[b] : 0;
   const bool reports = span == 0 && blockIdx.y == 0 && threadIdx.x == 0;
   if (n < a.T || n > a.max_seq_len) {
     if (reports) flag_status(a.status, CLSA_DEV_BAD_SEQLEN);
@@ -133,7 +233,14 @@ __global__ void __launch_bounds__(THREADS) cache8_append_kernel(const AppendArgs
   const int begin = (first / SB + span) * SB;     // first position of this scale block
   if (begin >= n) return;
   const int lo = max(first - begin, 0), hi = min(n - begin, SB);
-  if (a.block_table == nullptr && a.seq_start[b] % SB != 0) {
+  const int64_t tok0 = (int64_t)b * a.T + (begin + lo - first);  // the first new token of this block
+  const bool idx_block = (int)blockIdx.y >= a.head_groups;       // K_idx; the others K and V of heads h0 .. h1 - 1
+  const int h0 = blockIdx.y * a.heads_per_block, h1 = min(h0 + a.heads_per_block, a.heads[0]);
+  Rows<SB, THREADS, 16> next;
+  const int kind0 = idx_block ? 2 : 0;
+  if (!idx_block || a.idx_dim == 128)  // the first rows do not depend on where they go
+    next.load(a.src[kind0] + tok0 * a.src_token[kind0] + (idx_block ? 0 : h0 * a.src_head[0]), a.src_token[kind0], lo, hi);
+  if (start % SB != 0) {
     if (reports) flag_status(a.status, CLSA_DEV_BAD_SCALE_BLOCK);
     return;
   }
@@ -143,41 +250,144 @@ __global__ void __launch_bounds__(THREADS) cache8_append_kernel(const AppendArgs
     if (threadIdx.x == 0 && blockIdx.y == 0) flag_status(a.status, CLSA_DEV_BAD_INDEX);
     return;
   }
-  const int item0 = blockIdx.y * a.heads_per_block, item1 = min(item0 + a.heads_per_block, a.items);
+  const int64_t block = row0 / SB;
+  if (idx_block) {
+    uint8_t* code = a.code[2] + row0 * a.code_token[2];
+    if (a.idx_dim == 64) {
+      Rows<SB, THREADS, 8> rows;
+      rows.load(a.src[2] + tok0 * a.src_token[2], a.src_token[2], lo, hi);
+      append_head<SB, THREADS, 8, false>(rows, code, a.code_token[2], a.scale[2] + block, lo, hi, a, nullptr, nullptr, red[0]);
+    } else {
+      append_head<SB, THREADS, 16, false>(next, code, a.code_token[2], a.scale[2] + block, lo, hi, a, nullptr, nullptr, red[0]);
+    }
+    return;
+  }
   const int half = a.spec.rot_dim >> 1;
-  float* tc = turns;
-  float* ts = turns + SB * half;
-  const bool rotate = a.has_spec && a.spec.rot_dim > 0;
-  if (rotate && item0 < a.heads[0]) {
-    for (int i = threadIdx.x; i < (hi - lo) * half; i += THREADS) {
-      const int row = lo + i / half, j = i % half;
-      turn_of(begin + row, a.spec.inv_freq[j], a.spec.rot_scale, &tc[row * half + j], &ts[row * half + j]);
+  float* bc = turns;
+  float* bs = turns + (SB / 8 + 8) * half;
+  if (a.has_spec && half > 0) {
+    // positions begin + 8 u (with the scale), then 0 .. 7
+    const int j = threadIdx.x % 64;
+    if (j < half) {
+      const float freq = a.spec.inv_freq[j];
+      for (int u = threadIdx.x / 64; u < SB / 8 + 8; u += THREADS / 64)
+        turn_of(u < SB / 8 ? begin + 8 * u : u - SB / 8, freq, u < SB / 8 ? a.spec.rot_scale : 1.f, &bc[u * half + j], &bs[u * half + j]);
     }
     __syncthreads();
   }
-  const int64_t tok0 = (int64_t)b * a.T + (begin + lo - first);  // the first new token of this block
-  for (int item = item0; item < item1; ++item) {
-    const int kind = item < a.heads[0] ? 0 : (item < a.heads[0] + a.heads[1] ? 1 : 2);
-    const int h = item - (kind > 0 ? a.heads[0] : 0) - (kind > 1 ? a.heads[1] : 0);
-    const uint16_t* src = a.src[kind] + tok0 * a.src_token[kind] + h * a.src_head[kind];
+  const int count = 2 * (h1 - h0);
+#pragma unroll 1
+  for (int i = 0; i < count; ++i) {  // K of the heads, then V of them
+    const int kind = i >= h1 - h0, h = h0 + i - (kind ? h1 - h0 : 0);
+    const Rows<SB, THREADS, 16> rows = next;
+    if (i + 1 < count) {
+      const int k2 = i + 1 >= h1 - h0, h2 = h0 + i + 1 - (k2 ? h1 - h0 : 0);
+      next.load(a.src[k2] + tok0 * a.src_token[k2] + h2 * a.src_head[k2], a.src_token[k2], lo, hi);
+    }
     uint8_t* code = a.code[kind] + row0 * a.code_token[kind] + h * a.code_head[kind];
-    uint8_t* scale = a.scale[kind] + h * a.scale_head + row0 / SB;
-    float* r = red[item & 1];
-    if (kind == 2 && a.idx_dim == 64)
-      append_head<SB, THREADS, 8>(src, a.src_token[kind], code, a.code_token[kind], scale, lo, hi, false, false, a, tc, ts, r);
+    uint8_t* scale = a.scale[kind] + h * a.scale_head + block;
+    if (kind == 0 && a.has_spec)
+      append_head<SB, THREADS, 16, true>(rows, code, a.code_token[kind], scale, lo, hi, a, bc, bs, red[i & 1]);
     else
-      append_head<SB, THREADS, 16>(src, a.src_token[kind], code, a.code_token[kind], scale, lo, hi,
-                                   kind == 0 && a.has_spec && a.spec.norm, kind == 0 && rotate, a, tc, ts, r);
+      append_head<SB, THREADS, 16, false>(rows, code, a.code_token[kind], scale, lo, hi, a, nullptr, nullptr, red[i & 1]);
   }
+}
+
+// T = 1: a half warp per (sequence, item), two items of one sequence per warp.
+constexpr int kTokenThreads = 128;
+template <int SB>
+__global__ void __launch_bounds__(kTokenThreads) cache8_append_token_kernel(const AppendArgs a) {
+  __shared__ __align__(16) float turns[kTokenThreads / 32][2][64];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & 15;
+  const int pairs = (a.items + 1) / 2;
+  const uint32_t id = blockIdx.x * (kTokenThreads / 32) + warp;
+  const int b = (int)(id / (uint32_t)pairs), pair = (int)(id - (uint32_t)b * pairs);
+  if (b >= a.num_seqs) return;
+  const int item = 2 * pair + (lane >> 4);
+  const int kind = item < a.heads[0] ? 0 : (item < a.heads[0] + a.heads[1] ? 1 : 2);
+  const int h = item - (kind > 0 ? a.heads[0] : 0) - (kind > 1 ? a.heads[1] : 0);
+  const bool mine = item < a.items && (kind < 2 || 8 * l < a.idx_dim);  // this lane holds 8 elements of a row
+  const int n = a.seq_len[b];
+  const int64_t start = a.block_table == nullptr ? a.seq_start[b] : 0;
+  uint4 raw = make_uint4(0, 0, 0, 0);
+  if (mine) raw = *reinterpret_cast<const uint4*>(a.src[kind] + b * a.src_token[kind] + h * a.src_head[kind] + 8 * l);
+  const bool spec = a.has_spec && 2 * pair < a.heads[0];  // K rows among the warp's two
+  const int half = spec ? a.spec.rot_dim >> 1 : 0;
+  float w[8], freq[2] = {0.f, 0.f};
+  if (spec && a.spec.norm) load_weight8(w, a.k_weight, 8 * l);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (lane + 32 * i < half) freq[i] = a.spec.inv_freq[lane + 32 * i];
+  if (n < 1 || n > a.max_seq_len) {
+    if (pair == 0 && lane == 0) flag_status(a.status, CLSA_DEV_BAD_SEQLEN);
+    return;
+  }
+  const int pos = n - 1, begin = pos / SB * SB, lo = pos - begin;
+  if (start % SB != 0) {
+    if (pair == 0 && lane == 0) flag_status(a.status, CLSA_DEV_BAD_SCALE_BLOCK);
+    return;
+  }
+  const int64_t row0 = cache_row(a.block_table, a.block_shift, a.max_blocks, a.seq_start, a.num_rows, b, begin);
+  if (row0 < 0 || row0 + lo >= a.num_rows) {
+    if (pair == 0 && lane == 0) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+    return;
+  }
+  uint8_t* code = a.code[kind] + row0 * a.code_token[kind] + h * a.code_head[kind] + 8 * l;
+  uint8_t* scale = a.scale[kind] + h * a.scale_head + row0 / SB;
+  const int e_old = mine && lo > 0 ? scale_exponent(*scale) : kScaleExpMin;
+  float x[8];
+  unpack_bf16x8(x, raw);
+  if (spec) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[i];
+    if (a.spec.norm) head_norm<16>(y, w, a.spec.eps);
+    if (half > 0) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (lane + 32 * i < half) turn_of(pos, freq[i], a.spec.rot_scale, &turns[warp][0][lane + 32 * i], &turns[warp][1][lane + 32 * i]);
+      __syncwarp();
+      float c[8], s[8];
+      load_turns(c, s, turns[warp][0], turns[warp][1], a.spec.rot_dim, a.spec.interleaved, l);
+      head_rotate<16>(y, c, s, a.spec.rot_dim, a.spec.interleaved, l);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = kind == 0 ? y[i] : x[i];
+  }
+  float amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float m = fabsf(x[i]);
+    if (m <= 3.4028234663852886e38f) amax = fmaxf(amax, m);  // finite
+  }
+#pragma unroll
+  for (int m = 8; m >= 1; m >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
+  if (!mine) return;
+  const int e = max(need_exponent(amax), e_old);
+  const float inv = exp2_int(-e);
+  uint2 v;
+  v.x = f32x2_to_e4m3x2(x[0] * inv, x[1] * inv) | f32x2_to_e4m3x2(x[2] * inv, x[3] * inv) << 16;
+  v.y = f32x2_to_e4m3x2(x[4] * inv, x[5] * inv) | f32x2_to_e4m3x2(x[6] * inv, x[7] * inv) << 16;
+  *reinterpret_cast<uint2*>(code + lo * a.code_token[kind]) = v;
+  if (lo > 0 && e > e_old) {  // the block's older rows move down by e - e_old exponents
+    const float f = exp2_int(max(e_old - e, -60));
+    for (int r0 = 0; r0 < lo; r0 += 8) {
+      uint2 old[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + i < lo) old[i] = *reinterpret_cast<const uint2*>(code + (r0 + i) * a.code_token[kind]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + i < lo) *reinterpret_cast<uint2*>(code + (r0 + i) * a.code_token[kind]) = recode(old[i], f);
+    }
+  }
+  if (l == 0) *scale = (uint8_t)(e + 127);
 }
 
 template <int SB, int THREADS>
 cudaError_t launch(const AppendArgs& a, unsigned blocks_x, unsigned blocks_y, cudaStream_t stream) {
-  const size_t smem = a.has_spec ? (size_t)SB * a.spec.rot_dim * sizeof(float) : 0;
-  if (smem > 48 * 1024) {
-    const cudaError_t err = cudaFuncSetAttribute(cache8_append_kernel<SB, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (err != cudaSuccess) return err;
-  }
+  const size_t smem = a.has_spec ? (size_t)(SB / 8 + 8) * a.spec.rot_dim * sizeof(float) : 0;
   cache8_append_kernel<SB, THREADS><<<dim3(blocks_x, blocks_y), THREADS, smem, stream>>>(a);
   return cudaGetLastError();
 }
@@ -216,16 +426,30 @@ cudaError_t launch_cache8_append(const clsa_params& p, const clsa_cache8& c, con
   while (p.block_table != nullptr && (1 << a.block_shift) < p.block_size) ++a.block_shift;
   a.max_blocks = p.max_blocks_per_seq;
   a.num_rows = p.num_cache_rows;
+  a.num_seqs = p.num_seqs;
   a.T = p.q_per_seq;
   a.max_seq_len = p.max_seq_len;
   a.status = status;
+  if (p.q_per_seq == 1) {
+    const int64_t warps = (int64_t)p.num_seqs * ((a.items + 1) / 2);
+    const unsigned blocks = (unsigned)((warps + kTokenThreads / 32 - 1) / (kTokenThreads / 32));
+    switch (c.scale_block) {
+      case 16: cache8_append_token_kernel<16><<<blocks, kTokenThreads, 0, stream>>>(a); break;
+      case 32: cache8_append_token_kernel<32><<<blocks, kTokenThreads, 0, stream>>>(a); break;
+      case 64: cache8_append_token_kernel<64><<<blocks, kTokenThreads, 0, stream>>>(a); break;
+      default: cache8_append_token_kernel<128><<<blocks, kTokenThreads, 0, stream>>>(a); break;
+    }
+    return cudaGetLastError();
+  }
   a.spans = (p.q_per_seq - 1 + c.scale_block - 1) / c.scale_block + 1;  // scale blocks that T consecutive positions can touch
   const int64_t bx = (int64_t)p.num_seqs * a.spans;
-  // Heads per block: a block that takes several K heads forms its rows' angles once for all of them.
-  a.heads_per_block = 1;
-  while (a.heads_per_block < 8 && bx * ((a.items + 2 * a.heads_per_block - 1) / (2 * a.heads_per_block)) >= 4 * dev.sm_count)
-    a.heads_per_block *= 2;
-  const unsigned by = (unsigned)((a.items + a.heads_per_block - 1) / a.heads_per_block);
+  // Two heads per block where that still leaves about 400 threads per SM: they share the angles, and the second one's loads are
+  // hidden (4096 tokens of 8 heads, 64-row blocks: 15.4 us with one, 14.5 with two, 20.8 with four; 7 x 333 tokens of 4 heads,
+  // 16-row blocks, no rotation: 4.9 with one, 5.4 with two).
+  const int threads = c.scale_block <= 32 ? 128 : 256;
+  a.heads_per_block = bx * ((a.heads[0] + 1) / 2) * threads >= (int64_t)400 * dev.sm_count ? 2 : 1;
+  a.head_groups = (a.heads[0] + a.heads_per_block - 1) / a.heads_per_block;
+  const unsigned by = (unsigned)(a.head_groups + a.heads[2]);
   switch (c.scale_block) {
     case 16: return launch<16, 128>(a, (unsigned)bx, by, stream);
     case 32: return launch<32, 128>(a, (unsigned)bx, by, stream);

@@ -2,15 +2,19 @@
 // bound by HBM for a prefill chunk, by one launch and one memory round trip for a decode step).
 //
 // A head of D dimensions is held by D / 8 lanes of a warp, 16 bytes each; the sum of squares is a butterfly over those
-// lanes, the partner of a half-split rotation comes by one shuffle per dimension. A block takes one token: its threads
-// first issue the loads of all their heads, then compute the token's rot_dim / 2 angles once for all heads (64-bit
-// product and reduction, 32-bit functions) into shared memory, so that the angles hide behind the loads.
+// lanes, the partner of a half-split rotation comes by shuffles of the raw words. A warp takes heads of one token, 32 / (D / 8) in
+// a pass, four passes' loads and then their work together. The token's rot_dim / 2 angles (64-bit product and reduction, 32-bit
+// functions) are formed once per warp and folded with the weights into two factors per dimension, so that a dimension costs a
+// product, a multiply-add and a scaling, two dimensions per instruction. Warps are independent of one another. How many of a
+// token's heads a warp takes follows from the number of tokens: few tokens are spread over many warps (each forms the angles
+// anew), many keep a token together.
 #include "cache8.cuh"
 
 namespace clsa {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
+constexpr int kUnroll = 4;  // passes that are loaded and worked on together
 
 struct NormRopeArgs {
   HeadSpec spec;
@@ -20,61 +24,139 @@ struct NormRopeArgs {
   int64_t in_token[2], in_head[2], out_token[2], out_head[2];
   int heads[2];
   const int32_t* positions;
+  int num_tokens, parts, part_heads;  // warps per token, heads of each
 };
 
-// PASSES heads per group of lanes, loaded together.
-template <int LANES, int PASSES>
-__global__ void __launch_bounds__(kThreads) norm_rope_kernel(const NormRopeArgs a) {
-  constexpr int kGroups = kThreads / LANES;
-  __shared__ __align__(16) float tc[LANES * 4], ts[LANES * 4];
+// DENSE: heads lie head_dim apart, in and out (strides are immediates then).
+template <int LANES, bool DENSE>
+__global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
+  constexpr int kGroups = 32 / LANES;  // heads of a pass
+  __shared__ __align__(16) float turns[kThreads / 32][2][LANES * 4];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int64_t token = blockIdx.x;
-  const int l = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LANES, group = lane / LANES;
+  const uint32_t item = blockIdx.x * (kThreads / 32) + warp;
+  const uint32_t token = item / (uint32_t)a.parts;
+  if (token >= (uint32_t)a.num_tokens) return;
+  const int part0 = (int)(item - token * a.parts) * a.part_heads;
   const int pos = a.positions != nullptr ? a.positions[token] : 0;
+  // the heads of one side (0: queries, 1: keys) that this warp has, and its lanes' shares of the first pass
+  uint4 raw[kUnroll];
+  const uint16_t* in;
+  uint16_t* out;
+  int64_t in_step, out_step;
+  int left;  // heads from this batch's first one on
+  auto begin = [&](int side) {
+    const int before = side ? a.heads[0] : 0;
+    const int lo = max(part0 - before, 0);
+    left = min(part0 + a.part_heads - before, a.heads[side]) - lo;
+    in = a.in[side] + token * a.in_token[side] + (lo + group) * a.in_head[side] + 8 * l;
+    out = a.out[side] + token * a.out_token[side] + (lo + group) * a.out_head[side] + 8 * l;
+    in_step = DENSE ? 256 : kGroups * a.in_head[side];
+    out_step = DENSE ? 256 : kGroups * a.out_head[side];
+  };
+  auto load = [&]() {
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      raw[k] = make_uint4(0, 0, 0, 0);
+      if (group + k * kGroups < left) raw[k] = *reinterpret_cast<const uint4*>(in + k * in_step);
+    }
+  };
+  int side = 0;
+  begin(0);
+  if (left <= 0) begin(side = 1);
+  load();  // under way while the angles are formed
   if (pos < 0) return;  // padding
-  const int head0 = blockIdx.y * (kGroups * PASSES) + group;
-  uint4 raw[PASSES];
-#pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int h = head0 + p * kGroups, side = h >= a.heads[0], hh = side ? h - a.heads[0] : h;
-    raw[p] = make_uint4(0, 0, 0, 0);
-    if (hh < a.heads[side]) raw[p] = *reinterpret_cast<const uint4*>(a.in[side] + token * a.in_token[side] + hh * a.in_head[side] + 8 * l);
+  const int rot = a.spec.rot_dim;
+  float* tc = turns[warp][0];
+  float* ts = turns[warp][1];
+  if (rot > 0) {
+    for (int i = lane; i < rot / 2; i += 32) turn_of(pos, a.spec.inv_freq[i], a.spec.rot_scale, &tc[i], &ts[i]);
+    __syncwarp();
   }
-  float c[8], s[8];
-  if (a.spec.rot_dim > 0) {
-    for (int i = threadIdx.x; i < a.spec.rot_dim / 2; i += kThreads) turn_of(pos, a.spec.inv_freq[i], a.spec.rot_scale, &tc[i], &ts[i]);
-    __syncthreads();
-    load_turns(c, s, tc, ts, a.spec.rot_dim, a.spec.interleaved, l);
-  }
+  // The partner of this lane's dimensions in a half-split rotation sits in lane `partner` of its group.
+  const int hl = rot >> 4;
+  const bool turned = 8 * l < rot, inter = a.spec.interleaved, norm = a.spec.norm;
+  const int partner = l < hl ? l + hl : (l < 2 * hl ? l - hl : l);
+  const float sign = l < hl ? -1.f : 1.f;
+  const float eps = a.spec.eps;
+  while (true) {
+    // z_i = r (x_i A_i + x_partner B_i) with A = w cos, B = -+ w_partner sin and r the root of the mean square's inverse
+    uint64_t A[4], B[4];
+    {
+      uint4 wr = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);  // ones
+      if (norm && a.weight[side] != nullptr) wr = *reinterpret_cast<const uint4*>(a.weight[side] + 8 * l);
+      const uint32_t w4[4] = {wr.x, wr.y, wr.z, wr.w};
+      float c[8], s[8];
+      if (rot > 0) load_turns(c, s, tc, ts, rot, inter, l);
 #pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int h = head0 + p * kGroups, side = h >= a.heads[0], hh = side ? h - a.heads[0] : h;
-    float x[8];
-    unpack_bf16x8(x, raw[p]);
-    if (a.spec.norm) {
-      float w[8];
-      load_weight8(w, a.weight[side], 8 * l);
-      head_norm<LANES>(x, w, a.spec.eps);
+      for (int k = 0; k < 4; ++k) {
+        const uint64_t w = bf16x2_to_f32x2(w4[k]);
+        const uint32_t p = inter ? __byte_perm(w4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, w4[k], partner, LANES);
+        A[k] = turned ? mul2(w, pack2(c[2 * k], c[2 * k + 1])) : w;
+        B[k] = turned ? mul2(bf16x2_to_f32x2(p), inter ? pack2(-s[2 * k], s[2 * k + 1]) : pack2(sign * s[2 * k], sign * s[2 * k + 1])) : 0ull;
+      }
     }
-    if (a.spec.rot_dim > 0) head_rotate<LANES>(x, c, s, a.spec.rot_dim, a.spec.interleaved, l);
-    if (hh < a.heads[side]) {
-      const uint4 r = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-      *reinterpret_cast<uint4*>(a.out[side] + token * a.out_token[side] + hh * a.out_head[side] + 8 * l) = r;
+    auto one = [&](const uint4& raw) -> uint4 {
+      const uint32_t in4[4] = {raw.x, raw.y, raw.z, raw.w};
+      uint64_t x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = bf16x2_to_f32x2(in4[k]);
+      float r = 1.f;
+      if (norm) {
+        const float2 s2 = unpack2(fma2(x[3], x[3], fma2(x[2], x[2], fma2(x[1], x[1], mul2(x[0], x[0])))));
+        float ss = s2.x + s2.y;
+#pragma unroll
+        for (int m = LANES / 2; m >= 1; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+        r = rsqrtf(fmaf(ss, 1.f / (8 * LANES), eps));
+      }
+      const uint64_t r2 = pack2(r, r);
+      uint32_t o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t p = inter ? __byte_perm(in4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, in4[k], partner, LANES);
+        if (!turned) p = 0u;  // (an infinity times a zero sine is none)
+        const float2 z = unpack2(mul2(fma2(x[k], A[k], mul2(bf16x2_to_f32x2(p), B[k])), r2));
+        o[k] = pack_bf16x2(z.x, z.y);
+      }
+      return make_uint4(o[0], o[1], o[2], o[3]);
+    };
+#pragma unroll 1
+    while (true) {
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        if (k * kGroups >= left) break;  // the same for the whole warp
+        const uint4 z = one(raw[k]);
+        if (group + k * kGroups < left) *reinterpret_cast<uint4*>(out + k * out_step) = z;
+      }
+      left -= kUnroll * kGroups;
+      if (left <= 0) break;
+      in += kUnroll * in_step;
+      out += kUnroll * out_step;
+      load();
     }
+    if (side == 1) break;
+    begin(side = 1);
+    if (left <= 0) break;
+    load();
   }
 }
 
 template <int LANES>
-void launch(const NormRopeArgs& a, int num_tokens, const DeviceInfo& dev, cudaStream_t stream) {
-  constexpr int kGroups = kThreads / LANES;
-  const int passes = (a.heads[0] + a.heads[1] + kGroups - 1) / kGroups;
-  // few tokens: one pass per block, as many blocks as there are passes (the angles are formed in each of them)
-  int per = (int64_t)num_tokens * passes <= 4 * dev.sm_count ? 1 : (passes < 4 ? passes : 4);
-  const dim3 grid((unsigned)num_tokens, (unsigned)((passes + per - 1) / per));
-  if (per == 1) norm_rope_kernel<LANES, 1><<<grid, kThreads, 0, stream>>>(a);
-  else if (per == 2) norm_rope_kernel<LANES, 2><<<grid, kThreads, 0, stream>>>(a);
-  else if (per == 3) norm_rope_kernel<LANES, 3><<<grid, kThreads, 0, stream>>>(a);
-  else norm_rope_kernel<LANES, 4><<<grid, kThreads, 0, stream>>>(a);
+void launch(NormRopeArgs& a, const DeviceInfo& dev, cudaStream_t stream) {
+  constexpr int kGroups = 32 / LANES;
+  const int heads = a.heads[0] + a.heads[1];
+  // parts of a token: as many as give every SM about 16 warps, each a whole number of the heads that a warp holds at a time
+  int64_t parts = (16 * (int64_t)dev.sm_count + a.num_tokens - 1) / a.num_tokens;
+  const int most = (heads + kGroups - 1) / kGroups;
+  if (parts > most) parts = most;
+  a.part_heads = (int)((most + parts - 1) / parts) * kGroups;
+  a.parts = (heads + a.part_heads - 1) / a.part_heads;
+  const int64_t warps = (int64_t)a.num_tokens * a.parts;
+  const unsigned blocks = (unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32));
+  bool dense = true;
+  for (int i = 0; i < 2; ++i) dense = dense && (a.heads[i] <= 1 || (a.in_head[i] == 8 * LANES && a.out_head[i] == 8 * LANES));
+  if (dense) norm_rope_kernel<LANES, true><<<blocks, kThreads, 0, stream>>>(a);
+  else norm_rope_kernel<LANES, false><<<blocks, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -97,9 +179,10 @@ cudaError_t launch_norm_rope(const clsa_norm_rope_spec& spec, int num_tokens, co
     a.heads[i] = in[i]->num_heads;
   }
   a.positions = positions;
-  if (spec.head_dim == 64) launch<8>(a, num_tokens, dev, stream);
-  else if (spec.head_dim == 128) launch<16>(a, num_tokens, dev, stream);
-  else launch<32>(a, num_tokens, dev, stream);
+  a.num_tokens = num_tokens;
+  if (spec.head_dim == 64) launch<8>(a, dev, stream);
+  else if (spec.head_dim == 128) launch<16>(a, dev, stream);
+  else launch<32>(a, dev, stream);
   return cudaGetLastError();
 }
 
