@@ -5,18 +5,22 @@
 // convert to f16 exactly (one conversion instruction per two codes -- the arithmetic that is left beside the loads), and a
 // bf16 query row, scaled by a power of two so that its largest magnitude lies in [2^13, 2^14), is exact in f16 down to 2^-31 of it.
 // Sums are fp32; the row's and the key's powers of two are applied to the finished sum, which does not round.
-// The contraction index inside an instruction is a dummy, so the fragments are taken as the bytes lie: a lane loads 32 (16 for
-// 64-wide keys) consecutive bytes of one key row with one load, four lanes cover the row, a warp-wide load covers 8 whole rows,
-// and word w of the lane's bytes is its share of the instruction's w-th step. No shared memory, no shuffles.
+// The contraction index inside an instruction is a dummy, so the fragments are taken as the bytes lie: four lanes share a key
+// row, a lane takes the row's 16-byte chunks j and j + 4 (the one chunk j of 64-wide keys), and word w of a chunk is its share of
+// one step. Every warp streams tiles of 32 keys through a ring of its own: asynchronous 16-byte copies three tiles ahead (192 KB in
+// flight per SM), each lane reading back exactly what it copied, so there is no barrier and no shuffle. Warps take chunks of
+// four tiles round-robin (all of them read one moving window of the cache, and a sequence's query is converted once per chunk).
 // A key's sum does not depend on where the key sits, so equal keys get bit-identical scores (the top-k's tie-break).
+#include "attn_common.cuh"
 #include "cache8.cuh"
 
 namespace clsa {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarpKeys = 32;                           // keys a warp takes at a time: two 16-row tiles
-constexpr int kTile = kWarpKeys * (kThreads / 32);      // keys of a block's tile
+constexpr int kWarps = 16;
+constexpr int kTileKeys = 32;                  // keys of a tile: two 16-row instruction tiles
+constexpr int kChunkKeys = 4 * kTileKeys;      // keys a warp takes from one sequence at a time
+constexpr int kStages = 3;
 
 struct Scores8Args {
   const uint8_t* keys;
@@ -30,128 +34,178 @@ struct Scores8Args {
   int64_t num_rows;
   float* scores;
   int64_t score_stride;
-  int T, causal, max_seq_len, tiles_per_seq;
-  int64_t total_tiles;
+  int T, causal, max_seq_len;
+  uint32_t chunks_per_seq, num_chunks;
   uint32_t* status;
 };
 
-template <int WORDS>
-__device__ __forceinline__ void load_key(uint32_t (&w)[WORDS], const uint8_t* p, bool ok) {
-#pragma unroll
-  for (int i = 0; i < WORDS; ++i) w[i] = 0u;
-  if (!ok) return;
-  if constexpr (WORDS == 8) {
-    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                 : "l"(p));
-  } else {
-    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
-  }
-}
-
 // NT: n-tiles of 8 query tokens.
-template <int DIDX, int NT, int MIN_BLOCKS>
-__global__ void __launch_bounds__(kThreads, MIN_BLOCKS) index_scores8_kernel(const Scores8Args a) {
-  constexpr int W = DIDX / 16;  // instruction steps = 32-bit words of a lane's share of a key row
+template <int DIDX, int NT>
+__global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __grid_constant__ Scores8Args a) {
+  constexpr int C = DIDX / 64;  // 16-byte chunks of a key row that a lane holds
+  constexpr int kTileBytes = kTileKeys * DIDX;
+  extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, j = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const unsigned char* mine = smem + warp * (kStages * kTileBytes) + lane * 16;
+  const uint32_t mine_u32 = smem_u32(mine);
+  int4* tiles = reinterpret_cast<int4*>(smem + kWarps * kStages * kTileBytes) + warp * kStages;  // (sequence, position, length)
+
+  // The tiles of this warp in order: chunks `chunk`, + gridDim.x * kWarps, ..; empty ones are passed over.
+  uint32_t chunk = blockIdx.x + warp * gridDim.x;
+  const uint32_t step = gridDim.x * kWarps;
+  int b = -1, s = 0, n = 0, s_end = 0;
+  const int32_t* table = nullptr;
+  int64_t start = 0;
+  auto next_tile = [&]() -> bool {
+    s += kTileKeys;
+    while (s >= s_end) {
+      if (chunk >= a.num_chunks) return false;
+      b = (int)(chunk / a.chunks_per_seq);
+      s = (int)(chunk - (uint32_t)b * a.chunks_per_seq) * kChunkKeys;
+      chunk += step;
+      n = a.seq_len[b];
+      if (n < a.T || n > a.max_seq_len) {
+        if (s == 0 && lane == 0) flag_status(a.status, CLSA_DEV_BAD_SEQLEN);
+        n = 0;
+      }
+      s_end = min(n, s + kChunkKeys);
+      if (a.block_table != nullptr) table = a.block_table + (int64_t)b * a.max_blocks;
+      else start = a.seq_start[b];
+    }
+    return true;
+  };
+  // Rows of a tile's two halves (16 positions lie in one page); a row outside the row space is none.
+  auto half_row = [&](const int32_t* tab, int64_t st, int pos, int len) -> int64_t {
+    if (pos >= len) return -1;
+    return tab != nullptr ? ((int64_t)__ldg(tab + (pos >> a.block_shift)) << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : st + pos;
+  };
+  auto issue = [&](int slot) {
+    if (next_tile()) {
+      if (lane == 0) tiles[slot] = make_int4(b, s, n, 0);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const int64_t row0 = half_row(table, start, s + 16 * m, n);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int i = g + 8 * h;
+          const int64_t r = row0 + i;
+          const bool live = s + 16 * m + i < n;
+          const bool ok = live && row0 >= 0 && r < a.num_rows;
+          if (live && !ok) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+          const uint8_t* src = a.keys + (ok ? r : 0) * a.tok_stride + 16 * j;
+#pragma unroll
+          for (int c = 0; c < C; ++c)  // rows that are none become zeros
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(mine_u32 + slot * kTileBytes + ((m * 2 + h) * C + c) * 512),
+                         "l"(src + 64 * c), "r"(ok ? 16 : 0) : "memory");
+        }
+      }
+    } else if (lane == 0) {
+      tiles[slot] = make_int4(-1, 0, 0, 0);
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) issue(i);
+  __syncwarp();
+
   int cur_b = -1;
-  uint32_t qb[NT][W][2];
+  const int32_t* cur_table = nullptr;
+  int64_t cur_start = 0;
+  uint32_t qb[NT][C * 4][2];
   float qf[NT][2];  // power of two of query tokens 2j and 2j + 1 of each n-tile
-  for (int64_t tile = blockIdx.x; tile < a.total_tiles; tile += gridDim.x) {
-    const int b = (int)(tile / a.tiles_per_seq);
-    const int s0 = (int)(tile % a.tiles_per_seq) * kTile + warp * kWarpKeys;
-    const int n = a.seq_len[b];
-    if (n < a.T || n > a.max_seq_len) {
-      if (threadIdx.x == 0 && s0 == 0) flag_status(a.status, CLSA_DEV_BAD_SEQLEN);
-      continue;
-    }
-    if (s0 >= n) continue;
-    // ---- the keys' bytes and scale bytes: everything in flight at once ---------------------------------------------
-    uint32_t kw[2][2][W];
-    int sb[2][2];
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const int s = s0 + m * 16;  // 16 positions from here lie in one page
-      int64_t row = -1;
-      if (s < n) {
-        if (a.block_table != nullptr)
-          row = ((int64_t)__ldg(a.block_table + (int64_t)b * a.max_blocks + (s >> a.block_shift)) << a.block_shift) +
-                (s & ((1 << a.block_shift) - 1));
-        else
-          row = a.seq_start[b] + s;
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int i = g + 8 * h;
-        const int64_t r = row + i;
-        const bool live = s + i < n;
-        const bool ok = live && row >= 0 && r < a.num_rows;
-        if (live && !ok) flag_status(a.status, CLSA_DEV_BAD_INDEX);
-        load_key<W>(kw[m][h], a.keys + (ok ? r : 0) * a.tok_stride + j * (4 * W), ok);
-        sb[m][h] = ok ? a.scale[r >> a.scale_shift] : 127;
-      }
-    }
-    if (b != cur_b) {
-      cur_b = b;
+  for (int slot = 0;; slot = slot + 1 == kStages ? 0 : slot + 1) {
+    const int4 t = tiles[slot];
+    if (t.x < 0) break;
+    if (t.x != cur_b) {
+      cur_b = t.x;
+      if (a.block_table != nullptr) cur_table = a.block_table + (int64_t)cur_b * a.max_blocks;
+      else cur_start = a.seq_start[cur_b];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int t = nt * 8 + g;
-        const uint16_t* q = a.q + ((int64_t)b * a.T + t) * DIDX + j * (4 * W);
-        uint32_t raw[W][2];
+        const int tok = nt * 8 + g;
+        const uint16_t* q = a.q + ((int64_t)cur_b * a.T + tok) * DIDX + j * 16;
         float amax = 0.f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-          const uint2 v = t < a.T ? *reinterpret_cast<const uint2*>(q + 4 * w) : make_uint2(0u, 0u);
-          raw[w][0] = v.x; raw[w][1] = v.y;
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float lo = fabsf(bf16_lo(raw[w][i])), hi = fabsf(bf16_hi(raw[w][i]));
-            if (lo <= 3.4028234663852886e38f) amax = fmaxf(amax, lo);  // finite
-            if (hi <= 3.4028234663852886e38f) amax = fmaxf(amax, hi);
+          for (int w = 0; w < 4; ++w) {
+            const uint2 v = tok < a.T ? *reinterpret_cast<const uint2*>(q + 64 * c + 4 * w) : make_uint2(0u, 0u);
+            qb[nt][c * 4 + w][0] = v.x;
+            qb[nt][c * 4 + w][1] = v.y;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float lo = fabsf(bf16_lo(qb[nt][c * 4 + w][i])), hi = fabsf(bf16_hi(qb[nt][c * 4 + w][i]));
+              if (lo <= 3.4028234663852886e38f) amax = fmaxf(amax, lo);  // finite
+              if (hi <= 3.4028234663852886e38f) amax = fmaxf(amax, hi);
+            }
           }
-        }
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
         const int shift = min(13 + 127 - (int)(__float_as_uint(amax) >> 23), 120);
         const float up = exp2_int(shift), down = exp2_int(-shift);
 #pragma unroll
-        for (int w = 0; w < W; ++w)
+        for (int w = 0; w < C * 4; ++w)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) qb[nt][w][i] = pack_f16x2(bf16_lo(raw[w][i]) * up, bf16_hi(raw[w][i]) * up);
-        qf[nt][0] = __shfl_sync(0xffffffffu, down, 8 * j);      // lane (2j, 0) has query token 2j of the tile
+          for (int i = 0; i < 2; ++i) qb[nt][w][i] = pack_f16x2(bf16_lo(qb[nt][w][i]) * up, bf16_hi(qb[nt][w][i]) * up);
+        qf[nt][0] = __shfl_sync(0xffffffffu, down, 8 * j);  // lane (2j, 0) has query token 2j of the tile
         qf[nt][1] = __shfl_sync(0xffffffffu, down, 8 * j + 4);
       }
     }
+    // the scale bytes of the lane's four rows, on their way while the copies land
+    int sb[2][2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      float acc[NT][4];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) { acc[nt][0] = 0.f; acc[nt][1] = 0.f; acc[nt][2] = 0.f; acc[nt][3] = 0.f; }
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const uint32_t a0 = e4m3x2_to_f16x2(kw[m][0][w]), a2 = e4m3x2_hi_to_f16x2(kw[m][0][w]);
-        const uint32_t a1 = e4m3x2_to_f16x2(kw[m][1][w]), a3 = e4m3x2_hi_to_f16x2(kw[m][1][w]);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt], a0, a1, a2, a3, qb[nt][w][0], qb[nt][w][1]);
-      }
+      const int64_t row0 = half_row(cur_table, cur_start, t.y + 16 * m, t.z);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int s = s0 + m * 16 + g + 8 * h;
-        const float kf = exp2_int(scale_exponent(sb[m][h]));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int t = nt * 8 + 2 * j + i;
-            const int visible = a.causal ? n - a.T + t + 1 : n;
-            if (t < a.T && s < visible) a.scores[((int64_t)b * a.T + t) * a.score_stride + s] = acc[nt][2 * h + i] * qf[nt][i] * kf;
-          }
+        const int64_t r = row0 + g + 8 * h;
+        sb[m][h] = t.y + 16 * m + g + 8 * h < t.z && row0 >= 0 && r < a.num_rows ? a.scale[r >> a.scale_shift] : 127;
       }
     }
+    cp_async_wait<kStages - 1>();
+    const unsigned char* data = mine + slot * kTileBytes;
+    float acc[2][NT][4];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) { acc[m][nt][0] = 0.f; acc[m][nt][1] = 0.f; acc[m][nt][2] = 0.f; acc[m][nt][3] = 0.f; }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const uint4 lo = *reinterpret_cast<const uint4*>(data + ((m * 2) * C + c) * 512), hi = *reinterpret_cast<const uint4*>(data + ((m * 2 + 1) * C + c) * 512);
+        const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t a0 = e4m3x2_to_f16x2(wl[w]), a2 = e4m3x2_hi_to_f16x2(wl[w]);
+          const uint32_t a1 = e4m3x2_to_f16x2(wh[w]), a3 = e4m3x2_hi_to_f16x2(wh[w]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma_f16(acc[m][nt], a0, a1, a2, a3, qb[nt][c * 4 + w][0], qb[nt][c * 4 + w][1]);
+        }
+      }
+    __syncwarp();  // every lane has read this tile's entry
+    issue(slot);
+    __syncwarp();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int tok = nt * 8 + 2 * j + i;
+        if (tok < a.T) {
+          const int visible = a.causal ? t.z - a.T + tok + 1 : t.z;
+          float* dst = a.scores + ((int64_t)t.x * a.T + tok) * a.score_stride + t.y + g;
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (t.y + g + 16 * m + 8 * h < visible)
+                dst[16 * m + 8 * h] = acc[m][nt][2 * h + i] * qf[nt][i] * exp2_int(scale_exponent(sb[m][h]));
+        }
+      }
   }
+  cp_async_wait<0>();
 }
 
 // ---- more than 32 query tokens: the keys as bf16 rows (exact) for the tensor-core GEMM ---------------------------------
@@ -210,14 +264,14 @@ Scores8Args make_args(const clsa_params& p, const clsa_cache8& c, uint32_t* stat
 }
 
 template <int DIDX>
-void launch(const Scores8Args& a, int sm_count, cudaStream_t stream) {
-  auto grid = [&](int per_sm) {
-    const int64_t g = (int64_t)sm_count * per_sm;
-    return (unsigned)(g < a.total_tiles ? g : a.total_tiles);
-  };
-  if (a.T <= 8) index_scores8_kernel<DIDX, 1, 3><<<grid(3), kThreads, 0, stream>>>(a);
-  else if (a.T <= 16) index_scores8_kernel<DIDX, 2, 2><<<grid(2), kThreads, 0, stream>>>(a);
-  else index_scores8_kernel<DIDX, 4, 2><<<grid(2), kThreads, 0, stream>>>(a);
+cudaError_t launch(const Scores8Args& a, const DeviceInfo& dev, cudaStream_t stream) {
+  void (*kernel)(const Scores8Args) = a.T <= 8 ? index_scores8_kernel<DIDX, 1> : a.T <= 16 ? index_scores8_kernel<DIDX, 2> : index_scores8_kernel<DIDX, 4>;
+  constexpr int kSmem = kWarps * kStages * (kTileKeys * DIDX + (int)sizeof(int4));
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  if (err != cudaSuccess) return err;
+  const uint32_t blocks = a.num_chunks < (uint32_t)dev.sm_count ? a.num_chunks : (uint32_t)dev.sm_count;
+  kernel<<<blocks, kWarps * 32, kSmem, stream>>>(a);
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -228,11 +282,9 @@ cudaError_t launch_index_scores8(const clsa_params& p, const clsa_cache8& c, con
   a.q = static_cast<const uint16_t*>(q_idx);
   a.scores = scores;
   a.score_stride = score_stride;
-  a.tiles_per_seq = (p.max_seq_len + kTile - 1) / kTile;
-  a.total_tiles = (int64_t)p.num_seqs * a.tiles_per_seq;
-  if (p.idx_dim == 128) launch<128>(a, dev.sm_count, stream);
-  else launch<64>(a, dev.sm_count, stream);
-  return cudaGetLastError();
+  a.chunks_per_seq = (uint32_t)((p.max_seq_len + (int64_t)kChunkKeys - 1) / kChunkKeys);
+  a.num_chunks = (uint32_t)p.num_seqs * a.chunks_per_seq;
+  return p.idx_dim == 128 ? launch<128>(a, dev, stream) : launch<64>(a, dev, stream);
 }
 
 cudaError_t launch_index_expand8(const clsa_params& p, const clsa_cache8& c, void* keys, int64_t* starts, int64_t rows_per_seq,
