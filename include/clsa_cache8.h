@@ -26,8 +26,8 @@
 extern "C" {
 #endif
 
-#define CLSA_DEV_BAD_SCALE_BLOCK 64u /* clsa_cache8_append: seq_start[b] is not a multiple of scale_block: that sequence was
-                                        skipped */
+#define CLSA_DEV_BAD_SCALE_BLOCK 64u /* clsa_cache8_append, clsa_index_scores8: seq_start[b] is not a multiple of scale_block: that
+                                        sequence was not appended to, its scores mean nothing */
 
 /* Heads of a run of tokens: element (token, head, d) at data[token * token_stride + head * head_stride + d], bf16. Slices of
  * a projection's output rows are described as they are. data 16-byte aligned, strides (in elements) multiples of 8,
@@ -68,7 +68,8 @@ CLSA_API clsa_status clsa_norm_rope(const clsa_norm_rope_spec* spec, int32_t num
                                     const clsa_heads* q, const clsa_heads* q_out, const clsa_heads* k,
                                     const clsa_heads* k_out, clsa_stream stream);
 
-/* An 8-bit cache. Rows are those of clsa_params (seq_start / seq_len or a block table); p->num_cache_rows, the extent of the
+/* An 8-bit cache. Rows are those of clsa_params (seq_start / seq_len or a block table); a sequence begins on a scale block (in a
+ * contiguous cache every seq_start is a multiple of scale_block); p->num_cache_rows, the extent of the
  * row space, is required by every call below, and a row at or beyond it is treated like an index outside its sequence.
  * p's own bf16 cache pointers and strides are not used. */
 typedef struct {
@@ -102,8 +103,8 @@ CLSA_API clsa_status clsa_cache8_workspace_bytes(const clsa_params* p, const cls
  *             intermediate rounding); spec->head_dim must equal p->head_dim
  *   k_new, v_new  bf16 heads of the B * T new tokens in order (b, t), num_heads == num_kv_heads (both NULL: K_idx only)
  *   idx_k_new     likewise, num_heads == 1, idx_dim elements (NULL: K and V only)
- * A block that a call appends to must belong to one sequence (full blocks may be shared), and in a contiguous cache every
- * seq_start must be a multiple of scale_block (CLSA_DEV_BAD_SCALE_BLOCK otherwise). A sequence with seq_len < T or
+ * A block that a call appends to must belong to one sequence (full blocks may be shared). A sequence that does not begin on a
+ * scale block is skipped and flagged (CLSA_DEV_BAD_SCALE_BLOCK). A sequence with seq_len < T or
  * > max_seq_len is skipped and flagged (CLSA_DEV_BAD_SEQLEN), a block outside num_cache_rows too (CLSA_DEV_BAD_INDEX). */
 CLSA_API clsa_status clsa_cache8_append(const clsa_params* p, const clsa_cache8* c, const clsa_norm_rope_spec* spec,
                                         const clsa_heads* k_new, const clsa_heads* v_new, const clsa_heads* idx_k_new,

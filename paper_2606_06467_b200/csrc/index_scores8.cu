@@ -7,9 +7,11 @@
 // Sums are fp32; the row's and the key's powers of two are applied to the finished sum, which does not round.
 // The contraction index inside an instruction is a dummy, so the fragments are taken as the bytes lie: four lanes share a key
 // row, a lane takes the row's 16-byte chunks j and j + 4 (the one chunk j of 64-wide keys), and word w of a chunk is its share of
-// one step. Every warp streams tiles of 32 keys through a ring of its own: asynchronous 16-byte copies three tiles ahead (192 KB in
-// flight per SM), each lane reading back exactly what it copied, so there is no barrier and no shuffle. Warps take chunks of
-// four tiles round-robin (all of them read one moving window of the cache, and a sequence's query is converted once per chunk).
+// one step. Every warp streams tiles of 4 KB through a ring of its own: asynchronous 16-byte copies three tiles ahead (192 KB in
+// flight per SM), each lane reading back exactly what it copied, so there is no barrier and no shuffle. 16 keys share a page and a
+// scale (pages and scale blocks are multiples of 16 rows), so addresses, bounds and scales cost once per 16 keys. Warps take
+// chunks of up to four tiles round-robin: all of them read one moving window of the cache, and a sequence's query is converted
+// once per chunk.
 // A key's sum does not depend on where the key sits, so equal keys get bit-identical scores (the top-k's tie-break).
 #include "attn_common.cuh"
 #include "cache8.cuh"
@@ -18,8 +20,7 @@ namespace clsa {
 namespace {
 
 constexpr int kWarps = 16;
-constexpr int kTileKeys = 32;                  // keys of a tile: two 16-row instruction tiles
-constexpr int kChunkKeys = 4 * kTileKeys;      // keys a warp takes from one sequence at a time
+constexpr int kTileBytes = 4096;               // keys of a tile: 32 of 128 dimensions, 64 of 64
 constexpr int kStages = 3;
 
 struct Scores8Args {
@@ -31,10 +32,12 @@ struct Scores8Args {
   const int32_t* seq_len;
   const int32_t* block_table;
   int block_shift, max_blocks, scale_shift;
-  int64_t num_rows;
+  int num_rows;
+  uint32_t page_limit;  // pages of the row space (the last one may be cut short)
   float* scores;
   int64_t score_stride;
   int T, causal, max_seq_len;
+  int chunk_keys;  // keys a warp takes from one sequence at a time
   uint32_t chunks_per_seq, num_chunks;
   uint32_t* status;
 };
@@ -42,67 +45,81 @@ struct Scores8Args {
 // NT: n-tiles of 8 query tokens.
 template <int DIDX, int NT>
 __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __grid_constant__ Scores8Args a) {
-  constexpr int C = DIDX / 64;  // 16-byte chunks of a key row that a lane holds
-  constexpr int kTileBytes = kTileKeys * DIDX;
+  constexpr int C = DIDX / 64;                 // 16-byte chunks of a key row that a lane holds
+  constexpr int kTileKeys = kTileBytes / DIDX;
+  constexpr int M = kTileKeys / 16;            // 16-key groups of a tile
   extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, j = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const unsigned char* mine = smem + warp * (kStages * kTileBytes) + lane * 16;
   const uint32_t mine_u32 = smem_u32(mine);
-  int4* tiles = reinterpret_cast<int4*>(smem + kWarps * kStages * kTileBytes) + warp * kStages;  // (sequence, position, length)
+  // (sequence, position, length) of the tiles in the ring, and the cache rows of their groups (-1: none)
+  int4* tiles = reinterpret_cast<int4*>(smem + kWarps * kStages * kTileBytes) + warp * kStages * 2;
 
   // The tiles of this warp in order: chunks `chunk`, + gridDim.x * kWarps, ..; empty ones are passed over.
   uint32_t chunk = blockIdx.x + warp * gridDim.x;
   const uint32_t step = gridDim.x * kWarps;
   int b = -1, s = 0, n = 0, s_end = 0;
   const int32_t* table = nullptr;
-  int64_t start = 0;
+  int start = 0;
   auto next_tile = [&]() -> bool {
     s += kTileKeys;
     while (s >= s_end) {
       if (chunk >= a.num_chunks) return false;
       b = (int)(chunk / a.chunks_per_seq);
-      s = (int)(chunk - (uint32_t)b * a.chunks_per_seq) * kChunkKeys;
+      s = (int)(chunk - (uint32_t)b * a.chunks_per_seq) * a.chunk_keys;
       chunk += step;
       n = a.seq_len[b];
-      if (n < a.T || n > a.max_seq_len) {
-        if (s == 0 && lane == 0) flag_status(a.status, CLSA_DEV_BAD_SEQLEN);
+      const int64_t st = a.block_table == nullptr ? a.seq_start[b] : 0;
+      if (n < a.T || n > a.max_seq_len || (st & ((1 << a.scale_shift) - 1)) != 0) {
+        if (s == 0 && lane == 0) flag_status(a.status, n < a.T || n > a.max_seq_len ? CLSA_DEV_BAD_SEQLEN : CLSA_DEV_BAD_SCALE_BLOCK);
         n = 0;
       }
-      s_end = min(n, s + kChunkKeys);
-      if (a.block_table != nullptr) table = a.block_table + (int64_t)b * a.max_blocks;
-      else start = a.seq_start[b];
+      s_end = min(n, s + a.chunk_keys);
+      table = a.block_table + (int64_t)b * a.max_blocks;
+      start = (int)max((int64_t)-a.max_seq_len - 16, min(st, (int64_t)0x7fffffff - a.max_seq_len));  // rows outside stay outside
     }
     return true;
   };
-  // Rows of a tile's two halves (16 positions lie in one page); a row outside the row space is none.
-  auto half_row = [&](const int32_t* tab, int64_t st, int pos, int len) -> int64_t {
-    if (pos >= len) return -1;
-    return tab != nullptr ? ((int64_t)__ldg(tab + (pos >> a.block_shift)) << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : st + pos;
-  };
+  const uint8_t* lane_keys = a.keys + g * a.tok_stride + 16 * j;
+  const int64_t stride8 = 8 * a.tok_stride;
   auto issue = [&](int slot) {
     if (next_tile()) {
-      if (lane == 0) tiles[slot] = make_int4(b, s, n, 0);
+      int rows[4] = {-1, -1, -1, -1};
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const int64_t row0 = half_row(table, start, s + 16 * m, n);
+      for (int m = 0; m < M; ++m) {
+        const int pos = s + 16 * m;
+        int row = -1;
+        if (pos < n) {
+          if (a.block_table != nullptr) {
+            const uint32_t page = (uint32_t)__ldg(table + (pos >> a.block_shift));
+            if (page < a.page_limit) row = (int)(page << a.block_shift) + (pos & ((1 << a.block_shift) - 1));
+          } else {
+            row = start + pos;
+          }
+        }
+        const int want = min(n - pos, 16);                                       // keys of this group
+        const int have = row >= 0 && row < a.num_rows ? min(want, a.num_rows - row) : 0;  // .. that lie in the row space
+        if (have < want) {
+          if (lane == 0) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+          if (have <= 0) row = -1;
+        }
+        rows[m] = row;
+        const uint8_t* src = lane_keys + (row < 0 ? 0 : row) * a.tok_stride;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int i = g + 8 * h;
-          const int64_t r = row0 + i;
-          const bool live = s + 16 * m + i < n;
-          const bool ok = live && row0 >= 0 && r < a.num_rows;
-          if (live && !ok) flag_status(a.status, CLSA_DEV_BAD_INDEX);
-          const uint8_t* src = a.keys + (ok ? r : 0) * a.tok_stride + 16 * j;
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int c = 0; c < C; ++c)  // rows that are none become zeros
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(mine_u32 + slot * kTileBytes + ((m * 2 + h) * C + c) * 512),
-                         "l"(src + 64 * c), "r"(ok ? 16 : 0) : "memory");
-        }
+                         "l"(g + 8 * h < have ? src + h * stride8 + 64 * c : a.keys), "r"(g + 8 * h < have ? 16 : 0) : "memory");
+      }
+      if (lane == 0) {
+        tiles[2 * slot] = make_int4(b, s, n, 0);
+        tiles[2 * slot + 1] = make_int4(rows[0], rows[1], rows[2], rows[3]);
       }
     } else if (lane == 0) {
-      tiles[slot] = make_int4(-1, 0, 0, 0);
+      tiles[2 * slot] = make_int4(-1, 0, 0, 0);
     }
     cp_async_commit();
   };
@@ -111,17 +128,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
   __syncwarp();
 
   int cur_b = -1;
-  const int32_t* cur_table = nullptr;
-  int64_t cur_start = 0;
   uint32_t qb[NT][C * 4][2];
   float qf[NT][2];  // power of two of query tokens 2j and 2j + 1 of each n-tile
   for (int slot = 0;; slot = slot + 1 == kStages ? 0 : slot + 1) {
-    const int4 t = tiles[slot];
+    const int4 t = tiles[2 * slot];
     if (t.x < 0) break;
+    const int4 r4 = tiles[2 * slot + 1];
+    const int rows[4] = {r4.x, r4.y, r4.z, r4.w};
+    int sb[M];  // the groups' scale bytes, on their way while the copies land
+#pragma unroll
+    for (int m = 0; m < M; ++m) sb[m] = rows[m] >= 0 ? a.scale[rows[m] >> a.scale_shift] : 127;
     if (t.x != cur_b) {
       cur_b = t.x;
-      if (a.block_table != nullptr) cur_table = a.block_table + (int64_t)cur_b * a.max_blocks;
-      else cur_start = a.seq_start[cur_b];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int tok = nt * 8 + g;
@@ -153,26 +171,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
         qf[nt][1] = __shfl_sync(0xffffffffu, down, 8 * j + 4);
       }
     }
-    // the scale bytes of the lane's four rows, on their way while the copies land
-    int sb[2][2];
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const int64_t row0 = half_row(cur_table, cur_start, t.y + 16 * m, t.z);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int64_t r = row0 + g + 8 * h;
-        sb[m][h] = t.y + 16 * m + g + 8 * h < t.z && row0 >= 0 && r < a.num_rows ? a.scale[r >> a.scale_shift] : 127;
-      }
-    }
     cp_async_wait<kStages - 1>();
     const unsigned char* data = mine + slot * kTileBytes;
-    float acc[2][NT][4];
+    float acc[M][NT][4];
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < M; ++m)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) { acc[m][nt][0] = 0.f; acc[m][nt][1] = 0.f; acc[m][nt][2] = 0.f; acc[m][nt][3] = 0.f; }
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < M; ++m)
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const uint4 lo = *reinterpret_cast<const uint4*>(data + ((m * 2) * C + c) * 512), hi = *reinterpret_cast<const uint4*>(data + ((m * 2 + 1) * C + c) * 512);
@@ -188,20 +195,22 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
     __syncwarp();  // every lane has read this tile's entry
     issue(slot);
     __syncwarp();
+    float kf[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) kf[m] = exp2_int(scale_exponent(sb[m]));
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int tok = nt * 8 + 2 * j + i;
         if (tok < a.T) {
-          const int visible = a.causal ? t.z - a.T + tok + 1 : t.z;
+          const int left = (a.causal ? t.z - a.T + tok + 1 : t.z) - t.y - g;  // keys that it sees from this lane's first one on
           float* dst = a.scores + ((int64_t)t.x * a.T + tok) * a.score_stride + t.y + g;
 #pragma unroll
-          for (int m = 0; m < 2; ++m)
+          for (int m = 0; m < M; ++m)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              if (t.y + g + 16 * m + 8 * h < visible)
-                dst[16 * m + 8 * h] = acc[m][nt][2 * h + i] * qf[nt][i] * exp2_int(scale_exponent(sb[m][h]));
+              if (16 * m + 8 * h < left) dst[16 * m + 8 * h] = acc[m][nt][2 * h + i] * qf[nt][i] * kf[m];
         }
       }
   }
@@ -215,10 +224,10 @@ __global__ void __launch_bounds__(256) index_expand8_kernel(const Scores8Args a,
   const int b = blockIdx.x / blocks_per_seq, blk = blockIdx.x % blocks_per_seq;
   const int n = a.seq_len[b];
   if (blk == 0 && threadIdx.x == 0) starts[b] = b * rows_per_seq;
-  if (n < a.T || n > a.max_seq_len) {
-    if (blk == 0 && threadIdx.x == 0) flag_status(a.status, CLSA_DEV_BAD_SEQLEN);
-    return;
-  }
+  const bool off_block = a.block_table == nullptr && (a.seq_start[b] & ((1 << a.scale_shift) - 1)) != 0;
+  const bool bad_len = n < a.T || n > a.max_seq_len;
+  if ((bad_len || off_block) && blk == 0 && threadIdx.x == 0) flag_status(a.status, bad_len ? CLSA_DEV_BAD_SEQLEN : CLSA_DEV_BAD_SCALE_BLOCK);
+  if (bad_len) return;
   const int s = (int)(((int64_t)blk * 256 + threadIdx.x) / per_row), part = threadIdx.x % per_row;
   if (s >= n) return;
   const int64_t row = cache_row(a.block_table, a.block_shift, a.max_blocks, a.seq_start, a.num_rows, b, s);
@@ -255,7 +264,8 @@ Scores8Args make_args(const clsa_params& p, const clsa_cache8& c, uint32_t* stat
   while (p.block_table != nullptr && (1 << a.block_shift) < p.block_size) ++a.block_shift;
   a.max_blocks = p.max_blocks_per_seq;
   while ((1 << a.scale_shift) < c.scale_block) ++a.scale_shift;
-  a.num_rows = p.num_cache_rows;
+  a.num_rows = (int)p.num_cache_rows;
+  a.page_limit = (uint32_t)((p.num_cache_rows + (1 << a.block_shift) - 1) >> a.block_shift);
   a.T = p.q_per_seq;
   a.causal = p.causal;
   a.max_seq_len = p.max_seq_len;
@@ -266,7 +276,7 @@ Scores8Args make_args(const clsa_params& p, const clsa_cache8& c, uint32_t* stat
 template <int DIDX>
 cudaError_t launch(const Scores8Args& a, const DeviceInfo& dev, cudaStream_t stream) {
   void (*kernel)(const Scores8Args) = a.T <= 8 ? index_scores8_kernel<DIDX, 1> : a.T <= 16 ? index_scores8_kernel<DIDX, 2> : index_scores8_kernel<DIDX, 4>;
-  constexpr int kSmem = kWarps * kStages * (kTileKeys * DIDX + (int)sizeof(int4));
+  constexpr int kSmem = kWarps * kStages * (kTileBytes + 2 * (int)sizeof(int4));
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (err != cudaSuccess) return err;
   const uint32_t blocks = a.num_chunks < (uint32_t)dev.sm_count ? a.num_chunks : (uint32_t)dev.sm_count;
@@ -282,7 +292,11 @@ cudaError_t launch_index_scores8(const clsa_params& p, const clsa_cache8& c, con
   a.q = static_cast<const uint16_t*>(q_idx);
   a.scores = scores;
   a.score_stride = score_stride;
-  a.chunks_per_seq = (uint32_t)((p.max_seq_len + (int64_t)kChunkKeys - 1) / kChunkKeys);
+  // four tiles per chunk, fewer where that would leave a warp less than four chunks
+  const int tile = kTileBytes / p.idx_dim;
+  a.chunk_keys = 4 * tile;
+  while (a.chunk_keys > tile && (int64_t)p.num_seqs * p.max_seq_len < (int64_t)4 * kWarps * dev.sm_count * a.chunk_keys) a.chunk_keys /= 2;
+  a.chunks_per_seq = (uint32_t)((p.max_seq_len + (int64_t)a.chunk_keys - 1) / a.chunk_keys);
   a.num_chunks = (uint32_t)p.num_seqs * a.chunks_per_seq;
   return p.idx_dim == 128 ? launch<128>(a, dev, stream) : launch<64>(a, dev, stream);
 }

@@ -383,6 +383,19 @@ def test_index_scores_bad_rows_of_a_chunk():
     assert c.status() == clsa.CLSA_DEV_BAD_SEQLEN
 
 
+@pytest.mark.parametrize("T", [1, 40])
+def test_index_scores_of_a_sequence_off_the_scale_blocks_are_flagged(T):
+    c = Cache([300, 300], T, 1, 64, 32, 0, seed=2)
+    c.params(causal=1)
+    c.start[0] += 16
+    q = randn(gen(1), 2, T, 64)
+    s = run_scores(c, q, 1)
+    assert c.status() == clsa.CLSA_DEV_BAD_SCALE_BLOCK
+    code, sc = c.host()[2]
+    want, mag = ref.scores(f64(q[1]), ref.values(code, sc, 32)[c.row(1, np.arange(300)), 0])
+    assert (np.abs(s[1, 0, :301 - T].cpu().double().numpy() - want[0, :301 - T]) <= 2.0 ** -16 * mag[0, :301 - T]).all()
+
+
 # ------------------------------------------------------------------------------------------------------------ attention
 def make_index(c, top_k, causal, seed, order="ascending", counts=None):
     r = np.random.default_rng(seed)
