@@ -67,6 +67,11 @@ def _dense(t, what, dtype, device, rows=False):
     return t.data_ptr()
 
 
+def _device(torch):
+    """The current CUDA device's number, where the calls' kernels run; None before anything is on a GPU."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+
+
 def _stream8(stream, device):
     """The stream to launch on: the current one's handle without the object around it, or the caller's."""
     if stream is None and device is not None:
@@ -127,26 +132,28 @@ def make_cache8(*, k=None, v=None, k_scale=None, v_scale=None, idx_k=None, idx_k
 
 
 def _heads(t, what, device, bf16, tokens, heads, dim, flat=False):
-    """The clsa_heads bytes of a bf16 tensor [tokens, heads, dim] or [B, T, heads, dim] ([.., dim] with flat: one head) and its
-    number of tokens. tokens, heads: what they have to be, or None."""
+    """The clsa_heads bytes of a bf16 tensor [tokens, heads, dim] or [B, T, heads, dim] ([.., dim] with flat: one head), its
+    number of tokens and of heads. tokens, heads: what they have to be, or None."""
     shape, stride = t.shape, t.stride()
     if flat:
         shape, stride = (*shape[:-1], 1, shape[-1]), (*stride[:-1], dim, stride[-1])
     if len(shape) == 4:
-        T = shape[1]
-        n, token = shape[0] * T, stride[0] if T == 1 else stride[1]
-        even = T == 1 or shape[0] == 1 or stride[0] == T * stride[1]
+        B, T, h, d = shape
+        s0, s1, head, one = stride
+        n, token = B * T, s0 if T == 1 else s1
+        even = T == 1 or B == 1 or s0 == T * s1
     elif len(shape) == 3:
-        n, token, even = shape[0], stride[0], True
+        n, h, d = shape
+        token, head, one = stride
+        even = True
     else:
         even = False
-    if not even or shape[-1] != dim or stride[-1] != 1 or t.dtype != bf16 or t.get_device() != device:
+    if not even or d != dim or one != 1 or t.dtype is not bf16 or t.get_device() != device:
         raise ValueError(f"{what}: a bf16 tensor [tokens, heads, {dim}] or [B, T, heads, {dim}] on the current CUDA device, with dense heads and "
                          f"evenly spaced tokens, is wanted; got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
-    if (tokens is not None and n != tokens) or (heads is not None and shape[-2] != heads):
+    if (tokens is not None and n != tokens) or (heads is not None and h != heads):
         raise ValueError(f"{what}: {tokens} tokens of {heads} heads are wanted, got {tuple(t.shape)}")
-    h = shape[-2]
-    return _pack_heads(t.data_ptr(), h, token, stride[-2] if h > 1 else dim), n
+    return _pack_heads(t.data_ptr(), h, token, head if h > 1 else dim), n, h
 
 
 def clsa_norm_rope(spec, positions, q, q_out, k=None, k_out=None, stream=None) -> None:
@@ -156,15 +163,15 @@ def clsa_norm_rope(spec, positions, q, q_out, k=None, k_out=None, stream=None) -
 
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
         raise ValueError("q with q_out, k with k_out, or both are wanted")
-    dev, bf16, dim = torch.cuda.current_device() if torch.cuda.is_initialized() else None, torch.bfloat16, spec.head_dim
+    dev, bf16, dim = _device(torch), torch.bfloat16, spec.head_dim
     n = None if positions is None else positions.numel()
     a = b = c = d = None
     if q is not None:
-        a, n = _heads(q, "q", dev, bf16, n, None, dim)
-        b, _ = _heads(q_out, "q_out", dev, bf16, n, q.shape[-2], dim)
+        a, n, h = _heads(q, "q", dev, bf16, n, None, dim)
+        b, _, _ = _heads(q_out, "q_out", dev, bf16, n, h, dim)
     if k is not None:
-        c, n = _heads(k, "k", dev, bf16, n, None, dim)
-        d, _ = _heads(k_out, "k_out", dev, bf16, n, k.shape[-2], dim)
+        c, n, h = _heads(k, "k", dev, bf16, n, None, dim)
+        d, _, _ = _heads(k_out, "k_out", dev, bf16, n, h, dim)
     status = _lib.clsa_norm_rope(ctypes.byref(spec), n, _dense(positions, "positions", torch.int32, dev), a, b, c, d, _stream8(stream, dev))
     if status:
         _check(status, "clsa_norm_rope")
@@ -183,13 +190,13 @@ def clsa_cache8_append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace
 
     if (k_new is None) != (v_new is None) or (k_new is None and idx_k_new is None):
         raise ValueError("k_new with v_new, idx_k_new, or all three are wanted")
-    dev, bf16, n = torch.cuda.current_device() if torch.cuda.is_initialized() else None, torch.bfloat16, p.num_seqs * p.q_per_seq
+    dev, bf16, n = _device(torch), torch.bfloat16, p.num_seqs * p.q_per_seq
     k = v = i = None
     if k_new is not None:
-        k, _ = _heads(k_new, "k_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
-        v, _ = _heads(v_new, "v_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
+        k, _, _ = _heads(k_new, "k_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
+        v, _, _ = _heads(v_new, "v_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
     if idx_k_new is not None:
-        i, _ = _heads(idx_k_new, "idx_k_new", dev, bf16, n, 1, p.idx_dim, True)
+        i, _, _ = _heads(idx_k_new, "idx_k_new", dev, bf16, n, 1, p.idx_dim, True)
     status = _lib.clsa_cache8_append(ctypes.byref(p), ctypes.byref(c), None if spec is None else ctypes.byref(spec), k, v, i, _ptr(workspace),
                                      _nbytes(workspace, workspace_bytes), _stream8(stream, dev))
     if status:
@@ -200,7 +207,7 @@ def clsa_index_scores8(p, c, q_idx, scores, score_stride, workspace, workspace_b
     """clsa_index_scores over an 8-bit indexer-key cache."""
     import torch
 
-    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+    dev = _device(torch)
     status = _lib.clsa_index_scores8(ctypes.byref(p), ctypes.byref(c), _dense(q_idx, "q_idx", torch.bfloat16, dev),
                                      _dense(scores, "scores", torch.float32, dev, True), score_stride, _ptr(workspace),
                                      _nbytes(workspace, workspace_bytes), _stream8(stream, dev))
@@ -212,7 +219,7 @@ def clsa_sparse_attn8(p, c, q, idx, count, out, lse, hints, workspace, workspace
     """clsa_sparse_attn_hinted over an 8-bit K and V cache (hints: None or a clsa_attn_hints with shared_gpu 0)."""
     import torch
 
-    dev, i32 = torch.cuda.current_device() if torch.cuda.is_initialized() else None, torch.int32
+    dev, i32 = _device(torch), torch.int32
     status = _lib.clsa_sparse_attn8(ctypes.byref(p), ctypes.byref(c), _dense(q, "q", torch.bfloat16, dev), _dense(idx, "idx", i32, dev),
                                     _dense(count, "count", i32, dev), _dense(out, "out", torch.bfloat16, None),
                                     _dense(lse, "lse", torch.float32, None), None if hints is None else ctypes.byref(hints),
