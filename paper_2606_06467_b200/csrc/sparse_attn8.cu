@@ -11,7 +11,9 @@
 // K's fragments are plain matrix loads: a lane's word holds 4 dimensions of a token, its halves are the lane's two shares of a
 // step (the contraction index is a dummy, q is laid out to match). V's are the transposing 8-bit loads: a word holds 4
 // consecutive tokens of one dimension. K's rows are addressed in the order in which the weights, transposed in registers, then
-// meet those tokens.
+// meet those tokens. Groups of up to 4 query heads (FOLD) fill the columns twice: columns 4 .. 7 repeat the heads, their lanes take
+// the weights of the second 16 tokens where the others take those of the first, and the second product keeps the two halves of
+// the sum in the two column halves until the end -- half the logits and weights per lane for a few selects.
 //
 // In the log2 domain a query head keeps two running references: m near the largest x_s + ev for the numerators' weights
 // 2^(x_s + ev - m), and mx near the largest x_s for the denominators 2^(x_s - mx), so that neither underflows however far apart
@@ -95,6 +97,9 @@ __device__ __forceinline__ int k_token(int r) { return 4 * ((r >> 1) & 3) + (r &
 __device__ __forceinline__ uint32_t k_chunk(int t, int c) { return (uint32_t)(t * 128 + ((c ^ ((t & 1) | ((t >> 1) & 6))) << 4)); }
 __device__ __forceinline__ uint32_t v_chunk(int t, int c) { return (uint32_t)(t * 128 + ((c ^ (t & 7)) << 4)); }
 
+__device__ __forceinline__ void cp_async16_plain(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void ldmatrix_b8_x2_trans(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];\n"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -107,12 +112,14 @@ struct Shape {
   static constexpr size_t kSmem = (size_t)WARPS * (kRing + kScale + STAGES * 4) + WARPS * (sizeof(int2) + sizeof(int2));
 };
 
-template <int NT, int WARPS, int STAGES, bool PAGED>
+template <int NT, bool FOLD, int WARPS, int STAGES, bool PAGED>
 __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __grid_constant__ Attn8Args a) {
   using S = Shape<WARPS, STAGES>;
   extern __shared__ __align__(128) unsigned char smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rowq = lane >> 2, hcol = 2 * (lane & 3);
+  const int rowq = lane >> 2, hcol = FOLD ? 2 * (lane & 1) : 2 * (lane & 3);  // this lane's heads (of each tile): hcol, hcol + 1
+  constexpr int NX = FOLD ? 2 : 4;              // tokens of a stage whose logits this lane has
+  const bool upper = FOLD && (lane & 2) != 0;   // .. in the stage's second half
   const int G = a.group, NS = a.unit_stages, W = a.workers;
   const int w = (int)blockIdx.x * a.wpb + warp;
   const bool has_work = warp < a.wpb && w < W;
@@ -144,8 +151,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   };
   if (!a.early) wait_now();
 
-  const uint64_t pol_keep = a.keep ? l2_policy_evict_last() : l2_policy_evict_normal();
-  const uint64_t pol_last = l2_policy_evict_last(), pol_first = l2_policy_evict_first();
   // Places inside a stage, from the ring's start. This lane copies chunk lane & 7 of tokens 4 it + lane / 8: k_copy[it & 3] and
   // v_copy[it & 1] plus 512 it; it addresses row k_frag of K's fragment loads (plus 2048 for tokens 16 ..), where the chunk
   // pair 2 st is reached by an exclusive or with st << 5, and row v_frag of V's, where chunk c is with c << 4.
@@ -156,7 +161,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   for (int i = 0; i < 2; ++i) v_copy[i] = ring_u32 + kStage8Bytes / 2 + v_chunk(4 * i + (lane >> 3), lane & 7) - 512u * i;
   const uint32_t k_frag = ring_u32 + k_chunk(k_token(lane & 15), lane >> 4);
   const uint32_t v_frag = ring_u32 + kStage8Bytes / 2 + v_chunk(lane, 0);
-  const int my_tok = k_token(rowq);  // this lane's tokens of a stage: my_tok + {0, 2, 16, 18}
+  const int my_tok = k_token(rowq) + (upper ? 16 : 0);  // this lane's tokens of a stage: my_tok + {0, 2} and, unfolded, {16, 18}
 
   int cur = a.reverse ? s_end : s_begin;
   while (a.reverse ? cur > s_begin : cur < s_end) {
@@ -202,24 +207,26 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       const uint8_t* vbase = a.vc + g * a.head_stride + (lane & 7) * 16;
       const uint8_t* ksb = a.ks + g * a.scale_head;
       const uint8_t* vsb = a.vs + g * a.scale_head;
-      // stage i begins at entry t_lo + 32 i of the row's index, or, walking from the end, nstages - 1 - i in the place of i
-      const int32_t* my_idx = row_idx + t_lo + lane + (a.reverse ? (nstages - 1) * kTok : 0);
-      const int step = a.reverse ? -kTok : kTok;
-      const int full = (t_hi - t_lo) % kTok;  // tokens of the last stage if it is cut short (0: it is not)
-      auto live = [&](int i) { return i < nstages && (full == 0 || i != (a.reverse ? 0 : nstages - 1) || lane < full); };
-      auto load_raw = [&](int i) -> int { return live(i) ? my_idx[i * step] : -1; };  // position of token `lane` of step i
+      // Stage i begins at entry t_lo + 32 i of the row's index, or, walking from the end, nstages - 1 - i in the place of i.
+      const int32_t* my_idx = row_idx + t_lo;
+      const int total = t_hi - t_lo, step = a.reverse ? -kTok : kTok;
+      int tok = lane + (a.reverse ? (nstages - 1) * kTok : 0);  // entry that this lane reads next
+      auto next_raw = [&]() -> int {                            // its position (-1 past the end), one stage further each time
+        const int raw = (uint32_t)tok < (uint32_t)total ? my_idx[tok] : -1;
+        tok += step;
+        return raw;
+      };
       // Positions whose rows may be read: inside the sequence and, without pages, inside the row space too.
       const int pos_lo = PAGED || start >= 0 ? 0 : (int)min((int64_t)n, -start);
       const int pos_hi = PAGED ? n : (int)max((int64_t)pos_lo, min((int64_t)n, a.num_rows - start));
       const uint32_t pos_span = (uint32_t)(pos_hi - pos_lo);
       auto load_blk = [&](int raw) -> int { return PAGED && (uint32_t)raw < (uint32_t)n ? __ldg(table + (raw >> a.block_shift)) : -1; };
       auto settle = [&](int i, int kb, int vb) {  // the scale bytes of stage i into shared memory
-        if (i < nstages) scales[(i % STAGES) * kTok + lane] = make_float2(exp2_int(scale_exponent(kb)), (float)scale_exponent(vb));
+        scales[(i % STAGES) * kTok + lane] = make_float2(exp2_int(scale_exponent(kb)), (float)scale_exponent(vb));
       };
       auto issue = [&](int i, int raw, int blk, int& kb, int& vb) {  // the copies of stage i; its scale bytes stay in flight
         if (i < nstages) {
           const int buf = i % STAGES;
-          const uint64_t pol = a.pin < 0 ? pol_keep : (pin_rank((t_lo / kTok + (a.reverse ? nstages - 1 - i : i)) & 7) < a.pin ? pol_last : pol_first);
           uint32_t row;
           bool ok;
           if (PAGED) {
@@ -230,6 +237,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
             ok = (uint32_t)(raw - pos_lo) < pos_span;
             row = (uint32_t)start + (uint32_t)raw;
           }
+          const bool raw_live = (uint32_t)((a.reverse ? nstages - 1 - i : i) * kTok + lane) < (uint32_t)total;
           const uint32_t okmask = __ballot_sync(0xffffffffu, ok);
           if (lane == 0) stage_mask[buf] = okmask;
           kb = vb = 127;
@@ -239,15 +247,18 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
           }
           const uint32_t my16 = ok ? row * a.stride16 : 0u;  // 16-byte units: the caches span less than 2^32 of them
           const uint32_t at = (uint32_t)(buf * kStage8Bytes);
-          if (okmask == 0xffffffffu) {
+          if (okmask == 0xffffffffu && !a.keep) {  // the usual stage
 #pragma unroll
             for (int it = 0; it < 8; ++it) {
               const uint64_t off = (uint64_t)__shfl_sync(0xffffffffu, my16, 4 * it + (lane >> 3)) * 16u;
-              cp_async16_full(k_copy[it & 3] + at + 512 * it, kbase + off, pol);
-              cp_async16_full(v_copy[it & 1] + at + 512 * it, vbase + off, pol);
+              cp_async16_plain(k_copy[it & 3] + at + 512 * it, kbase + off);
+              cp_async16_plain(v_copy[it & 1] + at + 512 * it, vbase + off);
             }
-          } else {
-            if (!ok && n_ok && live(i)) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+          } else {  // some rows are none and become zeros, or rows have an L2 priority
+            if (!ok && n_ok && raw_live) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+            const uint64_t pol = !a.keep ? l2_policy_evict_normal()
+                                 : a.pin < 0 || pin_rank((t_lo / kTok + (a.reverse ? nstages - 1 - i : i)) & 7) < a.pin ? l2_policy_evict_last()
+                                                                                                                  : l2_policy_evict_first();
 #pragma unroll
             for (int it = 0; it < 8; ++it) {
               const int t = 4 * it + (lane >> 3);
@@ -264,9 +275,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       // Prologue: the ring filled, the positions of the two stages behind it and the page numbers of the first in registers.
       int raw_p[STAGES], blk_p[STAGES];
 #pragma unroll
-      for (int i = 0; i < STAGES; ++i)
-        raw_p[i] = a.reverse || i >= 2 ? load_raw(i) : (live(i) ? spec[i] : -1);
-      int rawX = load_raw(STAGES), rawY = load_raw(STAGES + 1);
+      for (int i = 0; i < STAGES; ++i) {
+        if (a.reverse || i >= 2) raw_p[i] = next_raw();
+        else { raw_p[i] = tok < total ? spec[i] : -1; tok += step; }
+      }
+      int rawX = next_raw(), rawY = next_raw();
 #pragma unroll
       for (int i = 0; i < STAGES; ++i) blk_p[i] = load_blk(raw_p[i]);
 #pragma unroll
@@ -280,11 +293,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       const uint16_t* qbase = a.q + ((int64_t)r * a.num_q_heads + h0) * 128;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int head = nt * 8 + rowq;
+        const int head = nt * 8 + (FOLD ? rowq & 3 : rowq);
         float amax = 0.f;
 #pragma unroll
         for (int st = 0; st < 8; ++st) {
-          const uint2 v = head < G ? *reinterpret_cast<const uint2*>(qbase + head * 128 + 16 * st + 2 * hcol) : make_uint2(0u, 0u);
+          const uint2 v = head < G ? *reinterpret_cast<const uint2*>(qbase + head * 128 + 16 * st + 4 * (lane & 3)) : make_uint2(0u, 0u);
           qb[nt][st][0] = v.x;
           qb[nt][st][1] = v.y;
 #pragma unroll
@@ -310,16 +323,16 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       int pend_k = raw_p[STAGES - 1], pend_v = blk_p[STAGES - 1];  // settled one iteration after their stage was issued
 #pragma unroll 1
       for (int i = 0; i < nstages; ++i) {
-        const int raw_new = load_raw(i + STAGES + 2);
+        const int raw_new = next_raw();
         const int blk_new = load_blk(rawY);
         cp_async_wait<STAGES - 1>();
         __syncwarp();
         const int buf = i % STAGES;
         const uint32_t at = (uint32_t)(buf * kStage8Bytes);
         const uint32_t okmask = stage_mask[buf];
-        float2 sc[4];  // tokens my_tok + 2 (t & 1) + 16 (t / 2)
+        float2 sc[NX];  // tokens my_tok + 2 (t & 1) + 16 (t / 2)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) sc[t] = scales[buf * kTok + my_tok + 2 * (t & 1) + 8 * (t & 2)];
+        for (int t = 0; t < NX; ++t) sc[t] = scales[buf * kTok + my_tok + 2 * (t & 1) + 8 * (t & 2)];
         float s[NT][2][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -339,25 +352,33 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
               for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt][mt], a0, a1, a2, a3, qb[nt][2 * st + k][0], qb[nt][2 * st + k][1]);
             }
           }
-        // x of the lane's four tokens and two heads per tile: x[..][2 t + head]
-        float x[NT][8], top[NT][2], tope[NT][2];
+        // x of the lane's tokens and two heads per tile: x[..][2 t + head]
+        float x[NT][2 * NX], top[NT][2], tope[NT][2];
         bool move = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[nt][i] = s[nt][i >> 2][i & 3] * sc[i >> 1].x * qf[nt][i & 1];
+          for (int i = 0; i < 2 * NX; ++i) {
+            const float dot = FOLD ? (upper ? s[nt][1][i & 3] : s[nt][0][i & 3]) : s[nt][i >> 2][i & 3];
+            x[nt][i] = dot * sc[i >> 1].x * qf[nt][i & 1];
+          }
         if (okmask != 0xffffffffu) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[nt][i] = (okmask >> (my_tok + (i & 2) + 4 * (i & 4))) & 1u ? x[nt][i] : -INFINITY;
+            for (int i = 0; i < 2 * NX; ++i) x[nt][i] = (okmask >> (my_tok + (i & 2) + 4 * (i & 4))) & 1u ? x[nt][i] : -INFINITY;
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            top[nt][h] = fmaxf(fmaxf(x[nt][h], x[nt][2 + h]), fmaxf(x[nt][4 + h], x[nt][6 + h]));
-            tope[nt][h] = fmaxf(fmaxf(x[nt][h] + sc[0].y, x[nt][2 + h] + sc[1].y), fmaxf(x[nt][4 + h] + sc[2].y, x[nt][6 + h] + sc[3].y));
+            top[nt][h] = x[nt][h];
+            tope[nt][h] = x[nt][h] + sc[0].y;
+#pragma unroll
+            for (int t = 1; t < NX; ++t) {
+              top[nt][h] = fmaxf(top[nt][h], x[nt][2 * t + h]);
+              tope[nt][h] = fmaxf(tope[nt][h], x[nt][2 * t + h] + sc[t].y);
+            }
             move = move || top[nt][h] > mx[nt][h] + kLazy || tope[nt][h] > m[nt][h] + kLazy;
           }
         if (__any_sync(0xffffffffu, move)) {  // some head's references have to move: to the largest seen so far
@@ -366,7 +387,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
-              for (int d = 4; d <= 16; d <<= 1) {
+              for (int d = FOLD ? 2 : 4; d <= 16; d <<= 1) {
                 top[nt][h] = fmaxf(top[nt][h], __shfl_xor_sync(0xffffffffu, top[nt][h], d));
                 tope[nt][h] = fmaxf(tope[nt][h], __shfl_xor_sync(0xffffffffu, tope[nt][h], d));
               }
@@ -381,9 +402,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
         }
         uint32_t pb[NT][4];  // weights as the second product's columns: tokens 4 (lane & 3) + {0, 1}, {2, 3}, then those + 16
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
+          for (int t = 0; t < NX; ++t) {
             float w[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -392,6 +413,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
             }
             pb[nt][t] = movmatrix_trans(pack_f16x2(w[0], w[1]));
           }
+          if (FOLD) {  // columns 0 .. 3 have the weights of the stage's first half, 4 .. 7 those of its second
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              pb[nt][2 + t] = rowq >= 4 ? pb[nt][t] : 0u;
+              pb[nt][t] = rowq >= 4 ? 0u : pb[nt][t];
+            }
+          }
+        }
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
           uint32_t v[4];  // tokens 0-15 of dimensions 16 c + rowq and + 8, then tokens 16-31
@@ -417,7 +446,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int d = 4; d <= 16; d <<= 1) l[nt][h] += __shfl_xor_sync(0xffffffffu, l[nt][h], d);
+          for (int d = FOLD ? 2 : 4; d <= 16; d <<= 1) l[nt][h] += __shfl_xor_sync(0xffffffffu, l[nt][h], d);
+      if (FOLD) {  // the two halves of the sums
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[0][c][i] += __shfl_xor_sync(0xffffffffu, o[0][c][i], 2);
+      }
     }
     wait_now();  // a segment without tokens has read nothing yet; what follows writes global memory
     if (!n_ok && lane == 0 && first_of_row) flag_status(a.status, CLSA_DEV_BAD_SEQLEN);
@@ -431,7 +466,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int head = nt * 8 + hcol + h;
-        if (head < G) {
+        if (head < G && !upper) {
           // a whole unit is normalised here; the references' difference is applied in two halves: its square may not be a float
           const float inv = whole ? (l[nt][h] != 0.f ? 1.f / l[nt][h] : 0.f) : 1.f;
           const float half = whole && l[nt][h] != 0.f ? fast_exp2(0.5f * (m[nt][h] - mx[nt][h])) : 1.f;
@@ -476,8 +511,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   float4* bpart = reinterpret_cast<float4*>(a.part) + (int64_t)W * rec4;  // 2 records per block: its first unit, its last
 
   // Up to 32 partials at once, lane i holding the references and sum (mx, l, m) of the i-th and fetch(i) its outputs.
-  float4 acc;
-  float L, MX, M;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float L = 0.f, MX = kNone, M = kNone;
   auto fold = [&](float4 ml, int count, auto fetch) {
     float mn = fmaxf(M, ml.z), xn = fmaxf(MX, ml.x);
 #pragma unroll
@@ -668,8 +703,9 @@ cudaError_t launch_sparse_attn8(const clsa_params& p, const clsa_cache8& c, cons
   a.scale_log2 = p.sm_scale * kLog2e;
   const bool paged = p.block_table != nullptr, wide = a.group > 8;
   void (*kernel)(const Attn8Args) =
-      wide ? (paged ? sparse_attn8_kernel<2, kWarpsWide, kStagesWide, true> : sparse_attn8_kernel<2, kWarpsWide, kStagesWide, false>)
-           : (paged ? sparse_attn8_kernel<1, kWarpsNarrow, kStagesNarrow, true> : sparse_attn8_kernel<1, kWarpsNarrow, kStagesNarrow, false>);
+      wide ? (paged ? sparse_attn8_kernel<2, false, kWarpsWide, kStagesWide, true> : sparse_attn8_kernel<2, false, kWarpsWide, kStagesWide, false>)
+      : a.group > 4 ? (paged ? sparse_attn8_kernel<1, false, kWarpsNarrow, kStagesNarrow, true> : sparse_attn8_kernel<1, false, kWarpsNarrow, kStagesNarrow, false>)
+                    : (paged ? sparse_attn8_kernel<1, true, kWarpsNarrow, kStagesNarrow, true> : sparse_attn8_kernel<1, true, kWarpsNarrow, kStagesNarrow, false>);
   cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem_bytes);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
