@@ -67,6 +67,17 @@ def _dense(t, what, dtype, device, rows=False):
     return t.data_ptr()
 
 
+_torch = None  # the torch module, from the first call on (importing this package does not import it)
+
+
+def _load_torch():
+    global _torch
+    import torch
+
+    _torch = torch
+    return torch
+
+
 def _device(torch):
     """The current CUDA device's number, where the calls' kernels run; None before anything is on a GPU."""
     return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
@@ -75,9 +86,7 @@ def _device(torch):
 def _stream8(stream, device):
     """The stream to launch on: the current one's handle without the object around it, or the caller's."""
     if stream is None and device is not None:
-        import torch
-
-        return torch._C._cuda_getCurrentRawStream(device)
+        return _torch._C._cuda_getCurrentRawStream(device)
     return _stream(stream)
 
 
@@ -137,21 +146,24 @@ def _heads(t, what, device, bf16, tokens, heads, dim, flat=False):
     shape, stride = t.shape, t.stride()
     if flat:
         shape, stride = (*shape[:-1], 1, shape[-1]), (*stride[:-1], dim, stride[-1])
-    if len(shape) == 4:
-        B, T, h, d = shape
-        s0, s1, head, one = stride
-        n, token = B * T, s0 if T == 1 else s1
-        even = T == 1 or B == 1 or s0 == T * s1
-    elif len(shape) == 3:
-        n, h, d = shape
-        token, head, one = stride
-        even = True
-    else:
+    try:
+        if len(shape) == 3:
+            n, h, d = shape
+            token, head, one = stride
+            even = True
+        else:
+            B, T, h, d = shape
+            token, s1, head, one = stride
+            n = B * T
+            even = T == 1 or B == 1 or token == T * s1
+            if T > 1:
+                token = s1
+    except ValueError:
         even = False
     if not even or d != dim or one != 1 or t.dtype is not bf16 or t.get_device() != device:
         raise ValueError(f"{what}: a bf16 tensor [tokens, heads, {dim}] or [B, T, heads, {dim}] on the current CUDA device, with dense heads and "
                          f"evenly spaced tokens, is wanted; got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
-    if (tokens is not None and n != tokens) or (heads is not None and h != heads):
+    if tokens != n and tokens is not None or heads != h and heads is not None:
         raise ValueError(f"{what}: {tokens} tokens of {heads} heads are wanted, got {tuple(t.shape)}")
     return _pack_heads(t.data_ptr(), h, token, head if h > 1 else dim), n, h
 
@@ -159,8 +171,7 @@ def _heads(t, what, device, bf16, tokens, heads, dim, flat=False):
 def clsa_norm_rope(spec, positions, q, q_out, k=None, k_out=None, stream=None) -> None:
     """Norm and rotation of the heads of q and k ([tokens, heads, D] or [B, T, heads, D], bf16, any token and head strides)
     into q_out and k_out, which may be q and k themselves. positions: int32, one per token (negative: skipped), or None."""
-    import torch
-
+    torch = _torch or _load_torch()
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
         raise ValueError("q with q_out, k with k_out, or both are wanted")
     dev, bf16, dim = _device(torch), torch.bfloat16, spec.head_dim
@@ -186,8 +197,7 @@ def clsa_cache8_workspace_bytes(p: clsa_params, c: clsa_cache8) -> int:
 def clsa_cache8_append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace_bytes=None, stream=None) -> None:
     """The newest T tokens of every sequence into the 8-bit caches: k_new, v_new [B, T, Hkv, D], idx_k_new [B, T, d_idx]
     (bf16; None leaves K and V, or K_idx, out). spec: the norm and rotation of K's rows (or None)."""
-    import torch
-
+    torch = _torch or _load_torch()
     if (k_new is None) != (v_new is None) or (k_new is None and idx_k_new is None):
         raise ValueError("k_new with v_new, idx_k_new, or all three are wanted")
     dev, bf16, n = _device(torch), torch.bfloat16, p.num_seqs * p.q_per_seq
@@ -205,8 +215,7 @@ def clsa_cache8_append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace
 
 def clsa_index_scores8(p, c, q_idx, scores, score_stride, workspace, workspace_bytes=None, stream=None) -> None:
     """clsa_index_scores over an 8-bit indexer-key cache."""
-    import torch
-
+    torch = _torch or _load_torch()
     dev = _device(torch)
     status = _lib.clsa_index_scores8(ctypes.byref(p), ctypes.byref(c), _dense(q_idx, "q_idx", torch.bfloat16, dev),
                                      _dense(scores, "scores", torch.float32, dev, True), score_stride, _ptr(workspace),
@@ -217,8 +226,7 @@ def clsa_index_scores8(p, c, q_idx, scores, score_stride, workspace, workspace_b
 
 def clsa_sparse_attn8(p, c, q, idx, count, out, lse, hints, workspace, workspace_bytes=None, stream=None) -> None:
     """clsa_sparse_attn_hinted over an 8-bit K and V cache (hints: None or a clsa_attn_hints with shared_gpu 0)."""
-    import torch
-
+    torch = _torch or _load_torch()
     dev, i32 = _device(torch), torch.int32
     status = _lib.clsa_sparse_attn8(ctypes.byref(p), ctypes.byref(c), _dense(q, "q", torch.bfloat16, dev), _dense(idx, "idx", i32, dev),
                                     _dense(count, "count", i32, dev), _dense(out, "out", torch.bfloat16, None),
