@@ -11,7 +11,7 @@
 // flight per SM), each lane reading back exactly what it copied, so there is no barrier and no shuffle. 16 keys share a page and a
 // scale (pages and scale blocks are multiples of 16 rows), so addresses, bounds and scales cost once per 16 keys. Warps take
 // chunks of up to four tiles round-robin: all of them read one moving window of the cache, and a sequence's query is converted
-// once per chunk.
+// once per chunk. The sequences' lengths wait in shared memory, and a tile's page numbers are fetched one tile before its keys.
 // A key's sum does not depend on where the key sits, so equal keys get bit-identical scores (the top-k's tie-break).
 #include "attn_common.cuh"
 #include "cache8.cuh"
@@ -22,6 +22,7 @@ namespace {
 constexpr int kWarps = 16;
 constexpr int kTileBytes = 4096;               // keys of a tile: 32 of 128 dimensions, 64 of 64
 constexpr int kStages = 3;
+constexpr int kLengths = 2048;                 // sequences whose lengths are kept in shared memory
 
 struct Scores8Args {
   const uint8_t* keys;
@@ -36,7 +37,7 @@ struct Scores8Args {
   uint32_t page_limit;  // pages of the row space (the last one may be cut short)
   float* scores;
   int64_t score_stride;
-  int T, causal, max_seq_len;
+  int num_seqs, T, causal, max_seq_len;
   int chunk_keys;  // keys a warp takes from one sequence at a time
   uint32_t chunks_per_seq, num_chunks;
   uint32_t* status;
@@ -57,72 +58,110 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
   // (sequence, position, length) of the tiles in the ring, and the cache rows of their groups (-1: none)
   int4* tiles = reinterpret_cast<int4*>(smem + kWarps * kStages * kTileBytes) + warp * kStages * 2;
 
-  // The tiles of this warp in order: chunks `chunk`, + gridDim.x * kWarps, ..; empty ones are passed over.
+  int* lengths = reinterpret_cast<int*>(smem + kWarps * kStages * (kTileBytes + 2 * (int)sizeof(int4)));
+  // A sequence's length, 0 if it is refused (flagged by the warp that has its first chunk).
+  auto length_of = [&](int b, bool report) -> int {
+    const int n = a.seq_len[b];
+    const bool bad_len = n < a.T || n > a.max_seq_len;
+    if (bad_len || (a.block_table == nullptr && (a.seq_start[b] & ((1 << a.scale_shift) - 1)) != 0)) {
+      if (report) flag_status(a.status, bad_len ? CLSA_DEV_BAD_SEQLEN : CLSA_DEV_BAD_SCALE_BLOCK);
+      return 0;
+    }
+    return n;
+  };
+  for (int i = threadIdx.x; i < min(a.num_seqs, kLengths); i += kWarps * 32) lengths[i] = length_of(i, blockIdx.x == 0);
+  __syncthreads();
+
+  // The tiles of this warp in order: chunks `chunk`, + gridDim.x * kWarps, ..; empty ones are passed over. The next tile is known
+  // one ahead of its copies, its page numbers on their way.
   uint32_t chunk = blockIdx.x + warp * gridDim.x;
   const uint32_t step = gridDim.x * kWarps;
   int b = -1, s = 0, n = 0, s_end = 0;
   const int32_t* table = nullptr;
   int start = 0;
-  auto next_tile = [&]() -> bool {
+  int page[M];
+  const bool one_run = a.block_table == nullptr || (1 << a.block_shift) >= kTileKeys;  // a tile's rows follow one another
+  auto next_tile = [&]() {  // b = -1 behind the last one
     s += kTileKeys;
     while (s >= s_end) {
-      if (chunk >= a.num_chunks) return false;
+      if (chunk >= a.num_chunks) {
+        b = -1;
+        return;
+      }
       b = (int)(chunk / a.chunks_per_seq);
       s = (int)(chunk - (uint32_t)b * a.chunks_per_seq) * a.chunk_keys;
       chunk += step;
-      n = a.seq_len[b];
-      const int64_t st = a.block_table == nullptr ? a.seq_start[b] : 0;
-      if (n < a.T || n > a.max_seq_len || (st & ((1 << a.scale_shift) - 1)) != 0) {
-        if (s == 0 && lane == 0) flag_status(a.status, n < a.T || n > a.max_seq_len ? CLSA_DEV_BAD_SEQLEN : CLSA_DEV_BAD_SCALE_BLOCK);
-        n = 0;
-      }
+      n = b < kLengths ? lengths[b] : length_of(b, s == 0 && lane == 0);
       s_end = min(n, s + a.chunk_keys);
-      table = a.block_table + (int64_t)b * a.max_blocks;
-      start = (int)max((int64_t)-a.max_seq_len - 16, min(st, (int64_t)0x7fffffff - a.max_seq_len));  // rows outside stay outside
+      if (s < s_end) {
+        if (a.block_table != nullptr) table = a.block_table + (int64_t)b * a.max_blocks;
+        else start = (int)max((int64_t)-a.max_seq_len - 16, min(a.seq_start[b], (int64_t)0x7fffffff - a.max_seq_len));  // rows outside stay outside
+      }
     }
-    return true;
+    if (table != nullptr) {
+      page[0] = __ldg(table + (s >> a.block_shift));
+      if (!one_run) {
+#pragma unroll
+        for (int m = 1; m < M; ++m) page[m] = s + 16 * m < n ? __ldg(table + ((s + 16 * m) >> a.block_shift)) : 0;
+      }
+    }
   };
   const uint8_t* lane_keys = a.keys + g * a.tok_stride + 16 * j;
   const int64_t stride8 = 8 * a.tok_stride;
-  auto issue = [&](int slot) {
-    if (next_tile()) {
+  auto issue = [&](int slot) {  // the copies of the tile found last, into the ring
+    if (b >= 0) {
       int rows[4] = {-1, -1, -1, -1};
-#pragma unroll
-      for (int m = 0; m < M; ++m) {
-        const int pos = s + 16 * m;
-        int row = -1;
-        if (pos < n) {
-          if (a.block_table != nullptr) {
-            const uint32_t page = (uint32_t)__ldg(table + (pos >> a.block_shift));
-            if (page < a.page_limit) row = (int)(page << a.block_shift) + (pos & ((1 << a.block_shift) - 1));
-          } else {
-            row = start + pos;
-          }
+      const uint32_t to = mine_u32 + slot * kTileBytes;
+      // row of position pos, and how many of `want` rows from it on lie in the row space
+      auto locate = [&](int pg, int pos, int want, int& row) -> int {
+        row = -1;
+        if (table != nullptr) {
+          if ((uint32_t)pg < a.page_limit) row = (pg << a.block_shift) + (pos & ((1 << a.block_shift) - 1));
+        } else {
+          row = start + pos;
         }
-        const int want = min(n - pos, 16);                                       // keys of this group
-        const int have = row >= 0 && row < a.num_rows ? min(want, a.num_rows - row) : 0;  // .. that lie in the row space
-        if (have < want) {
-          if (lane == 0) flag_status(a.status, CLSA_DEV_BAD_INDEX);
-          if (have <= 0) row = -1;
+        const int have = row >= 0 && row < a.num_rows ? min(want, a.num_rows - row) : 0;
+        if (have < want && lane == 0) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+        return have;
+      };
+      int row, have = 0;
+      if (one_run) have = locate(page[0], s, min(n - s, kTileKeys), row);
+      if (have == kTileKeys) {  // the usual tile
+        const uint8_t* src = lane_keys + row * a.tok_stride;
+#pragma unroll
+        for (int r = 0; r < 2 * M; ++r, src += stride8)
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(to + (r * C + c) * 512), "l"(src + 64 * c) : "memory");
+#pragma unroll
+        for (int m = 0; m < M; ++m) rows[m] = row + 16 * m;
+      } else {
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          const int pos = s + 16 * m, want = max(min(n - pos, 16), 0);
+          const int in = one_run ? max(min(have - 16 * m, want), 0) : locate(page[m], pos, want, row);
+          const int row_m = one_run ? row + 16 * m : row;
+          if (in > 0) rows[m] = row_m;
+          const uint8_t* src = lane_keys + (in > 0 ? row_m : 0) * a.tok_stride;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < C; ++c)  // rows that are none become zeros
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(to + ((m * 2 + h) * C + c) * 512),
+                           "l"(g + 8 * h < in ? src + h * stride8 + 64 * c : a.keys), "r"(g + 8 * h < in ? 16 : 0) : "memory");
         }
-        rows[m] = row;
-        const uint8_t* src = lane_keys + (row < 0 ? 0 : row) * a.tok_stride;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int c = 0; c < C; ++c)  // rows that are none become zeros
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(mine_u32 + slot * kTileBytes + ((m * 2 + h) * C + c) * 512),
-                         "l"(g + 8 * h < have ? src + h * stride8 + 64 * c : a.keys), "r"(g + 8 * h < have ? 16 : 0) : "memory");
       }
       if (lane == 0) {
         tiles[2 * slot] = make_int4(b, s, n, 0);
         tiles[2 * slot + 1] = make_int4(rows[0], rows[1], rows[2], rows[3]);
       }
+      next_tile();
     } else if (lane == 0) {
       tiles[2 * slot] = make_int4(-1, 0, 0, 0);
     }
     cp_async_commit();
   };
+  next_tile();
 #pragma unroll
   for (int i = 0; i < kStages; ++i) issue(i);
   __syncwarp();
@@ -144,24 +183,22 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
       for (int nt = 0; nt < NT; ++nt) {
         const int tok = nt * 8 + g;
         const uint16_t* q = a.q + ((int64_t)cur_b * a.T + tok) * DIDX + j * 16;
-        float amax = 0.f;
+        uint32_t top = 0u;  // bf16 magnitudes order as integers
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint2 v = tok < a.T ? *reinterpret_cast<const uint2*>(q + 64 * c + 4 * w) : make_uint2(0u, 0u);
+          for (int w = 0; w < 4; w += 2) {
+            const uint4 v = tok < a.T ? *reinterpret_cast<const uint4*>(q + 64 * c + 4 * w) : make_uint4(0u, 0u, 0u, 0u);
             qb[nt][c * 4 + w][0] = v.x;
             qb[nt][c * 4 + w][1] = v.y;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float lo = fabsf(bf16_lo(qb[nt][c * 4 + w][i])), hi = fabsf(bf16_hi(qb[nt][c * 4 + w][i]));
-              if (lo <= 3.4028234663852886e38f) amax = fmaxf(amax, lo);  // finite
-              if (hi <= 3.4028234663852886e38f) amax = fmaxf(amax, hi);
-            }
+            qb[nt][c * 4 + w + 1][0] = v.z;
+            qb[nt][c * 4 + w + 1][1] = v.w;
+            top = __vmaxu2(__vmaxu2(top, v.x & 0x7fff7fffu), __vmaxu2(v.y & 0x7fff7fffu, __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
           }
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        const int shift = min(13 + 127 - (int)(__float_as_uint(amax) >> 23), 120);
+        top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // (255 - 127: something is not finite, and neither are the scores)
+        const int shift = min(13 + 127 - (int)(max(top & 0xffffu, top >> 16) >> 7), 120);
         const float up = exp2_int(shift), down = exp2_int(-shift);
 #pragma unroll
         for (int w = 0; w < C * 4; ++w)
@@ -210,7 +247,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
           for (int m = 0; m < M; ++m)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              if (16 * m + 8 * h < left) dst[16 * m + 8 * h] = acc[m][nt][2 * h + i] * qf[nt][i] * kf[m];
+              if (16 * m + 8 * h < left) dst[16 * m + 8 * h] = acc[m][nt][2 * h + i] * qf[nt][i] * kf[m];  // (a product of the two powers may not be a float)
         }
       }
   }
@@ -266,6 +303,7 @@ Scores8Args make_args(const clsa_params& p, const clsa_cache8& c, uint32_t* stat
   while ((1 << a.scale_shift) < c.scale_block) ++a.scale_shift;
   a.num_rows = (int)p.num_cache_rows;
   a.page_limit = (uint32_t)((p.num_cache_rows + (1 << a.block_shift) - 1) >> a.block_shift);
+  a.num_seqs = p.num_seqs;
   a.T = p.q_per_seq;
   a.causal = p.causal;
   a.max_seq_len = p.max_seq_len;
@@ -276,7 +314,7 @@ Scores8Args make_args(const clsa_params& p, const clsa_cache8& c, uint32_t* stat
 template <int DIDX>
 cudaError_t launch(const Scores8Args& a, const DeviceInfo& dev, cudaStream_t stream) {
   void (*kernel)(const Scores8Args) = a.T <= 8 ? index_scores8_kernel<DIDX, 1> : a.T <= 16 ? index_scores8_kernel<DIDX, 2> : index_scores8_kernel<DIDX, 4>;
-  constexpr int kSmem = kWarps * kStages * (kTileBytes + 2 * (int)sizeof(int4));
+  constexpr int kSmem = kWarps * kStages * (kTileBytes + 2 * (int)sizeof(int4)) + kLengths * (int)sizeof(int);
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (err != cudaSuccess) return err;
   const uint32_t blocks = a.num_chunks < (uint32_t)dev.sm_count ? a.num_chunks : (uint32_t)dev.sm_count;
