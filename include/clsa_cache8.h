@@ -80,9 +80,9 @@ typedef struct {
   int64_t kv_token_stride;   /* bytes, multiple of 16; num_cache_rows * kv_token_stride < 2^36 (64 GiB) */
   int64_t kv_head_stride;    /* bytes, multiple of 16 */
   int64_t scale_head_stride; /* >= ceil(num_cache_rows / scale_block) */
-  void* idx_k;       /* e4m3 [rows][d_idx], element (r,j) at byte r*idx_token_stride + j; 32-byte aligned */
+  void* idx_k;       /* e4m3 [rows][d_idx], element (r,j) at byte r*idx_token_stride + j; 16-byte aligned */
   void* idx_k_scale; /* bytes [ceil(num_cache_rows / scale_block)] */
-  int64_t idx_token_stride; /* bytes, multiple of 32 */
+  int64_t idx_token_stride; /* bytes, multiple of 16 */
   int32_t scale_block;      /* rows per scale: 16, 32, 64 or 128. With a block table it must divide block_size */
 } clsa_cache8;
 

@@ -6,7 +6,7 @@ from __future__ import annotations
 import ctypes
 import struct
 
-from . import _H, _P, _check, _i64, _lib, _nbytes, _ptr, _stream, _sz, _vp, clsa_params
+from . import _H, _P, _check, _i64, _lib, _ptr, _stream, _sz, _vp, clsa_params
 
 CLSA_DEV_BAD_SCALE_BLOCK = 64
 
@@ -23,6 +23,8 @@ class clsa_heads(ctypes.Structure):
 class clsa_norm_rope_spec(ctypes.Structure):
     """Mirror of `clsa_norm_rope_spec` in include/clsa_cache8.h."""
 
+    _device = None  # where the tensors behind it lie, if it was made of tensors
+
     _fields_ = [("head_dim", ctypes.c_int32), ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
                 ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("rot_scale", ctypes.c_float),
                 ("inv_freq", _vp), ("q_weight", _vp), ("k_weight", _vp)]
@@ -30,6 +32,8 @@ class clsa_norm_rope_spec(ctypes.Structure):
 
 class clsa_cache8(ctypes.Structure):
     """Mirror of `clsa_cache8` in include/clsa_cache8.h."""
+
+    _device = None  # where the tensors behind it lie, if it was made of tensors
 
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("kv_token_stride", _i64),
                 ("kv_head_stride", _i64), ("scale_head_stride", _i64), ("idx_k", _vp), ("idx_k_scale", _vp),
@@ -56,15 +60,35 @@ def _want(ok, message):
         raise ValueError(message)
 
 
-def _dense(t, what, dtype, device, rows=False):
-    """Address of a buffer that is addressed as one dense array of `dtype` (None and device addresses pass). device: where it
-    has to lie, or None for anywhere the device can write (outputs may be pinned host memory). rows: its rows alone are dense."""
+def _dense(t, what, dtype, device, rows=False, output=False):
+    """Address of a buffer on the current device that is addressed as one dense array of `dtype` (None and device addresses
+    pass). rows: its rows alone are dense. output: it may also lie in pinned host memory."""
     if t is None or isinstance(t, int):
         return t
-    if t.dtype != dtype or not (t.is_contiguous() or (rows and t.stride(-1) == 1)) or (device is not None and t.get_device() != device):
-        raise ValueError(f"{what}: contiguous values of {dtype}" + (" on the current CUDA device" if device is not None else "")
-                         + f" are wanted, got {t.dtype} on {t.device}, strides {t.stride()}")
+    if t.dtype != dtype or not (t.is_contiguous() or (rows and t.stride(-1) == 1)) or (
+            t.get_device() != device and not (output and t.get_device() < 0 and t.is_pinned())):
+        raise ValueError(f"{what}: contiguous values of {dtype} on the current CUDA device are wanted, got {t.dtype} on {t.device}, "
+                         f"strides {t.stride()}")
     return t.data_ptr()
+
+
+def _workspace(ws, ws_bytes, made, device):
+    """Address and size of a workspace, behind a check that it and what the structs in `made` point to are on the device."""
+    for s in made:
+        if s is not None and s._device not in (None, device):
+            raise ValueError(f"the tensors of {type(s).__name__} are not on the current CUDA device")
+    if ws is None or isinstance(ws, int):
+        return ws, ws_bytes
+    if ws.get_device() != device:
+        raise ValueError(f"workspace: a tensor on the current CUDA device is wanted, got {ws.device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+
+
+def _device_of(*tensors):
+    """The one device of the tensors (-1: host memory), None if there are none (addresses do not count)."""
+    found = {t.get_device() for t in tensors if t is not None and not isinstance(t, int)}
+    _want(len(found) <= 1, "tensors on one device are wanted")
+    return found.pop() if found else None
 
 
 _torch = None  # the torch module, from the first call on (importing this package does not import it)
@@ -108,6 +132,7 @@ def make_norm_rope(*, head_dim=128, norm=1, eps=1e-6, rot_dim=0, interleaved=0, 
     spec = clsa_norm_rope_spec(head_dim, int(norm), eps, rot_dim, int(interleaved), rot_scale, _ptr(inv_freq), _ptr(q_weight),
                                _ptr(k_weight))
     spec._tensors = (inv_freq, q_weight, k_weight)
+    spec._device = _device_of(*spec._tensors)
     return spec
 
 
@@ -116,6 +141,7 @@ def make_cache8(*, k=None, v=None, k_scale=None, v_scale=None, idx_k=None, idx_k
     (float8_e8m0fnu or uint8), idx_k [rows, d_idx], idx_k_scale [blocks]. The struct keeps the tensors alive."""
     c = clsa_cache8()
     c._tensors = (k, v, k_scale, v_scale, idx_k, idx_k_scale)
+    c._device = _device_of(*c._tensors)
     c.scale_block = scale_block
     if k is not None or v is not None:
         for t, what in ((k, "k"), (v, "v")):
@@ -183,6 +209,8 @@ def clsa_norm_rope(spec, positions, q, q_out, k=None, k_out=None, stream=None) -
     if k is not None:
         c, n, h = _heads(k, "k", dev, bf16, n, None, dim)
         d, _, _ = _heads(k_out, "k_out", dev, bf16, n, h, dim)
+    if spec._device not in (None, dev):
+        raise ValueError("the tensors of clsa_norm_rope_spec are not on the current CUDA device")
     status = _lib.clsa_norm_rope(ctypes.byref(spec), n, _dense(positions, "positions", torch.int32, dev), a, b, c, d, _stream8(stream, dev))
     if status:
         _check(status, "clsa_norm_rope")
@@ -207,8 +235,9 @@ def clsa_cache8_append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace
         v, _, _ = _heads(v_new, "v_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
     if idx_k_new is not None:
         i, _, _ = _heads(idx_k_new, "idx_k_new", dev, bf16, n, 1, p.idx_dim, True)
-    status = _lib.clsa_cache8_append(ctypes.byref(p), ctypes.byref(c), None if spec is None else ctypes.byref(spec), k, v, i, _ptr(workspace),
-                                     _nbytes(workspace, workspace_bytes), _stream8(stream, dev))
+    ws, nbytes = _workspace(workspace, workspace_bytes, (c, spec), dev)
+    status = _lib.clsa_cache8_append(ctypes.byref(p), ctypes.byref(c), None if spec is None else ctypes.byref(spec), k, v, i, ws, nbytes,
+                                     _stream8(stream, dev))
     if status:
         _check(status, "clsa_cache8_append")
 
@@ -217,9 +246,9 @@ def clsa_index_scores8(p, c, q_idx, scores, score_stride, workspace, workspace_b
     """clsa_index_scores over an 8-bit indexer-key cache."""
     torch = _torch or _load_torch()
     dev = _device(torch)
+    ws, nbytes = _workspace(workspace, workspace_bytes, (c,), dev)
     status = _lib.clsa_index_scores8(ctypes.byref(p), ctypes.byref(c), _dense(q_idx, "q_idx", torch.bfloat16, dev),
-                                     _dense(scores, "scores", torch.float32, dev, True), score_stride, _ptr(workspace),
-                                     _nbytes(workspace, workspace_bytes), _stream8(stream, dev))
+                                     _dense(scores, "scores", torch.float32, dev, True), score_stride, ws, nbytes, _stream8(stream, dev))
     if status:
         _check(status, "clsa_index_scores8")
 
@@ -228,9 +257,10 @@ def clsa_sparse_attn8(p, c, q, idx, count, out, lse, hints, workspace, workspace
     """clsa_sparse_attn_hinted over an 8-bit K and V cache (hints: None or a clsa_attn_hints with shared_gpu 0)."""
     torch = _torch or _load_torch()
     dev, i32 = _device(torch), torch.int32
+    ws, nbytes = _workspace(workspace, workspace_bytes, (c,), dev)
     status = _lib.clsa_sparse_attn8(ctypes.byref(p), ctypes.byref(c), _dense(q, "q", torch.bfloat16, dev), _dense(idx, "idx", i32, dev),
-                                    _dense(count, "count", i32, dev), _dense(out, "out", torch.bfloat16, None),
-                                    _dense(lse, "lse", torch.float32, None), None if hints is None else ctypes.byref(hints),
-                                    _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream8(stream, dev))
+                                    _dense(count, "count", i32, dev), _dense(out, "out", torch.bfloat16, dev, output=True),
+                                    _dense(lse, "lse", torch.float32, dev, output=True), None if hints is None else ctypes.byref(hints),
+                                    ws, nbytes, _stream8(stream, dev))
     if status:
         _check(status, "clsa_sparse_attn8")

@@ -50,7 +50,11 @@ clsa_status check_params(const clsa_params* p) {
   if (!isfinite(p->sm_scale) || !(p->sm_scale > 0.f)) return CLSA_ERR_INVALID_ARG;
   if ((int64_t)p->num_seqs * p->q_per_seq > (int64_t)1 << 30) return CLSA_ERR_INVALID_ARG;
   if (p->num_cache_rows < 1 || p->num_cache_rows > 0x7fffffffLL) return CLSA_ERR_INVALID_ARG;
-  if ((double)p->num_seqs * p->q_per_seq * p->num_kv_heads * ((p->top_k + 15) / 16) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
+  // kernels number positions, 32-token stages, score tiles and appended rows with 32 bits
+  if (p->max_seq_len > 0x7fff0000) return CLSA_ERR_UNSUPPORTED;
+  if ((double)p->num_seqs * p->q_per_seq * p->num_kv_heads * ((p->top_k + 31) / 32) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
+  if ((double)p->num_seqs * ((p->max_seq_len + 31) / 32) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
+  if ((double)p->num_seqs * (2 * p->num_kv_heads + 1) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
   if (p->head_dim != 128) return CLSA_ERR_UNSUPPORTED;
   if (p->idx_dim != 64 && p->idx_dim != 128) return CLSA_ERR_UNSUPPORTED;
   if (p->num_q_heads / p->num_kv_heads > 16) return CLSA_ERR_UNSUPPORTED;
@@ -90,8 +94,8 @@ clsa_status check_kv8(const clsa_params* p, const clsa_cache8* c) {
 }
 
 clsa_status check_idx8(const clsa_params* p, const clsa_cache8* c) {
-  if (c->idx_k == nullptr || c->idx_k_scale == nullptr || !aligned(c->idx_k, 32)) return CLSA_ERR_INVALID_ARG;
-  if (c->idx_token_stride < p->idx_dim || c->idx_token_stride % 32 != 0) return CLSA_ERR_INVALID_ARG;
+  if (c->idx_k == nullptr || c->idx_k_scale == nullptr || !aligned(c->idx_k, 16)) return CLSA_ERR_INVALID_ARG;
+  if (c->idx_token_stride < p->idx_dim || c->idx_token_stride % 16 != 0) return CLSA_ERR_INVALID_ARG;
   return CLSA_OK;
 }
 

@@ -72,7 +72,7 @@ def _heads(clsa, data=0x100000, num=8, token=1024, head=128):
 BAD, UNS, WS = 1, 2, 3
 _PARAMS = [
     (dict(num_seqs=0), BAD), (dict(q_per_seq=0), BAD), (dict(num_q_heads=30), BAD), (dict(causal=2), BAD), (dict(sm_scale=0.0), BAD),
-    (dict(sm_scale=float("inf")), BAD), (dict(max_seq_len=0), BAD), (dict(num_cache_rows=0), BAD), (dict(num_cache_rows=1 << 31), BAD),
+    (dict(sm_scale=float("inf")), BAD), (dict(max_seq_len=0), BAD), (dict(max_seq_len=0x7fffffff), UNS), (dict(num_seqs=1 << 29, max_seq_len=256), UNS), (dict(num_cache_rows=0), BAD), (dict(num_cache_rows=1 << 31), BAD),
     (dict(head_dim=64), UNS), (dict(idx_dim=96), UNS), (dict(num_q_heads=34, num_kv_heads=2), UNS), (dict(seq_len=None), BAD),
     (dict(seq_start=None), BAD), (dict(seq_len=0x2002), BAD), (dict(block_table=0x3000, block_size=24, max_blocks_per_seq=64), BAD),
     (dict(block_table=0x3000, block_size=64, max_blocks_per_seq=8), BAD),
@@ -94,8 +94,8 @@ _CACHES = [
     (dict(scale_block=0), BAD, "kvi"), (dict(scale_block=48), BAD, "kvi"), (dict(scale_block=256), BAD, "kvi"),
     (dict(k=None), BAD, "kv"), (dict(v=0x20008), BAD, "kv"), (dict(k_scale=None), BAD, "kv"), (dict(v_scale=None), BAD, "kv"),
     (dict(kv_token_stride=1032), BAD, "kv"), (dict(kv_head_stride=64), BAD, "kv"), (dict(scale_head_stride=31), BAD, "kv"),
-    (dict(kv_token_stride=1 << 26), UNS, "kv"), (dict(idx_k=None), BAD, "i"), (dict(idx_k=0x50010), BAD, "i"),
-    (dict(idx_k_scale=None), BAD, "i"), (dict(idx_token_stride=64), BAD, "i"), (dict(idx_token_stride=144), BAD, "i"),
+    (dict(kv_token_stride=1 << 26), UNS, "kv"), (dict(idx_k=None), BAD, "i"), (dict(idx_k=0x50008), BAD, "i"),
+    (dict(idx_k_scale=None), BAD, "i"), (dict(idx_token_stride=64), BAD, "i"), (dict(idx_token_stride=136), BAD, "i"),
 ]
 
 
@@ -196,6 +196,16 @@ def test_binding_refuses_wrong_tensors(clsa):
         clsa.clsa_norm_rope(spec, None, q, q)
     with pytest.raises(ValueError):
         clsa.clsa_norm_rope(spec, None, q, None)
+    p = _params(clsa, num_kv_heads=2, num_q_heads=2)
+    ws = torch.zeros(256, dtype=torch.uint8)
+    b = torch.bfloat16
+    for call in (lambda: clsa.clsa_cache8_append(p, c, None, None, None, torch.zeros(2, 1, 128, dtype=b), ws),
+                 lambda: clsa.clsa_cache8_append(p, c, None, None, torch.zeros(2, 1, 2, 128, dtype=b), None, ws),
+                 lambda: clsa.clsa_index_scores8(p, c, torch.zeros(2, 1, 128, dtype=b), torch.zeros(2, 1, 1024), 1024, ws),
+                 lambda: clsa.clsa_sparse_attn8(p, c, torch.zeros(2, 1, 2, 128, dtype=b), torch.zeros(2, 1, 64, dtype=torch.int32),
+                                                torch.zeros(2, 1, dtype=torch.int32), torch.zeros(2, 1, 2, 128, dtype=b), None, None, ws)):
+        with pytest.raises(ValueError):  # host tensors, host workspaces, host caches
+            call()
 
 
 def test_reference_codes_round_to_nearest_even():
