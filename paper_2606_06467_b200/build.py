@@ -1,14 +1,16 @@
-"""Build libclsa.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Build libclsa.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and the CPython module that marshals some calls."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libclsa.so")
+MARSHAL = os.path.join(PKG, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))  # CPython module (csrc/marshal.c)
 SOURCES = ["api.cu", "index_scores.cu", "index_gemm.cu", "index_topk.cu", "topk.cu", "topk_filter.cu", "sparse_attn.cu", "sparse_attn_sk.cu", "project_append.cu",
            "api_cache8.cu", "norm_rope.cu", "cache8_append.cu", "index_scores8.cu", "sparse_attn8.cu"]
 NVCC_FLAGS = [
@@ -56,6 +58,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
         subprocess.check_call([_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", tmp] + objs
                               + ["-Xcompiler", "-fPIC"])
         os.replace(tmp, LIB)
+    src = os.path.join(CSRC, "marshal.c")
+    include = sysconfig.get_paths()["include"]
+    if os.path.exists(os.path.join(include, "Python.h")) and (force or _stale(MARSHAL, [src] + headers)):
+        tmp = MARSHAL + f".{os.getpid()}.tmp"
+        subprocess.check_call(["gcc", "-O2", "-std=c11", "-Wall", "-Wno-cast-function-type", "-fPIC", "-shared", "-I", include,
+                               "-I", os.path.join(ROOT, "include"), "-o", tmp, src])
+        os.replace(tmp, MARSHAL)
     return LIB
 
 

@@ -1,12 +1,14 @@
 """Binding of the 8-bit cache calls (`include/clsa_cache8.h`): the same names and argument orders, tensors in place of
-pointers. Checks of dtypes, shapes, strides and devices that C cannot make happen here; everything else is marshalling.
+pointers. Checks of dtypes, shapes, strides and devices that C cannot make happen here; everything else is marshalling. The
+usual call goes through the native module `_marshal` (csrc/marshal.c), which makes the same checks without the interpreter and
+hands back what it does not take as it is; without the module every call takes the way below.
 """
 from __future__ import annotations
 
 import ctypes
 import struct
 
-from . import _H, _P, _check, _i64, _lib, _ptr, _stream, _sz, _vp, clsa_params
+from . import _H, _P, _check, _i64, _lib, _ptr, _stream, _sz, _vp, clsa_attn_hints, clsa_params
 
 CLSA_DEV_BAD_SCALE_BLOCK = 64
 
@@ -92,12 +94,20 @@ def _device_of(*tensors):
 
 
 _torch = None  # the torch module, from the first call on (importing this package does not import it)
+try:
+    from . import _marshal
+except ImportError:
+    _marshal = None
 
 
 def _load_torch():
     global _torch
     import torch
 
+    if _marshal is not None:
+        where = [ctypes.cast(getattr(_lib, n), _vp).value for n in ("clsa_norm_rope", "clsa_cache8_append", "clsa_index_scores8", "clsa_sparse_attn8")]
+        _marshal.setup(*where, torch.Tensor, torch.bfloat16, torch.int32, torch.float32, torch.uint8, torch._C._cuda_getDevice,
+                       torch._C._cuda_getCurrentRawStream, clsa_params, clsa_cache8, clsa_norm_rope_spec, clsa_attn_hints)
     _torch = torch
     return torch
 
@@ -198,6 +208,9 @@ def clsa_norm_rope(spec, positions, q, q_out, k=None, k_out=None, stream=None) -
     """Norm and rotation of the heads of q and k ([tokens, heads, D] or [B, T, heads, D], bf16, any token and head strides)
     into q_out and k_out, which may be q and k themselves. positions: int32, one per token (negative: skipped), or None."""
     torch = _torch or _load_torch()
+    status = _marshal.norm_rope(spec, positions, q, q_out, k, k_out, stream) if _marshal else None
+    if status is not None:
+        return _check(status, "clsa_norm_rope") if status else None
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
         raise ValueError("q with q_out, k with k_out, or both are wanted")
     dev, bf16, dim = _device(torch), torch.bfloat16, spec.head_dim
@@ -226,6 +239,9 @@ def clsa_cache8_append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace
     """The newest T tokens of every sequence into the 8-bit caches: k_new, v_new [B, T, Hkv, D], idx_k_new [B, T, d_idx]
     (bf16; None leaves K and V, or K_idx, out). spec: the norm and rotation of K's rows (or None)."""
     torch = _torch or _load_torch()
+    status = _marshal.append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace_bytes, stream) if _marshal else None
+    if status is not None:
+        return _check(status, "clsa_cache8_append") if status else None
     if (k_new is None) != (v_new is None) or (k_new is None and idx_k_new is None):
         raise ValueError("k_new with v_new, idx_k_new, or all three are wanted")
     dev, bf16, n = _device(torch), torch.bfloat16, p.num_seqs * p.q_per_seq
@@ -245,6 +261,9 @@ def clsa_cache8_append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace
 def clsa_index_scores8(p, c, q_idx, scores, score_stride, workspace, workspace_bytes=None, stream=None) -> None:
     """clsa_index_scores over an 8-bit indexer-key cache."""
     torch = _torch or _load_torch()
+    status = _marshal.scores(p, c, q_idx, scores, score_stride, workspace, workspace_bytes, stream) if _marshal else None
+    if status is not None:
+        return _check(status, "clsa_index_scores8") if status else None
     dev = _device(torch)
     ws, nbytes = _workspace(workspace, workspace_bytes, (c,), dev)
     status = _lib.clsa_index_scores8(ctypes.byref(p), ctypes.byref(c), _dense(q_idx, "q_idx", torch.bfloat16, dev),
@@ -256,6 +275,9 @@ def clsa_index_scores8(p, c, q_idx, scores, score_stride, workspace, workspace_b
 def clsa_sparse_attn8(p, c, q, idx, count, out, lse, hints, workspace, workspace_bytes=None, stream=None) -> None:
     """clsa_sparse_attn_hinted over an 8-bit K and V cache (hints: None or a clsa_attn_hints with shared_gpu 0)."""
     torch = _torch or _load_torch()
+    status = _marshal.attn(p, c, q, idx, count, out, lse, hints, workspace, workspace_bytes, stream) if _marshal else None
+    if status is not None:
+        return _check(status, "clsa_sparse_attn8") if status else None
     dev, i32 = _device(torch), torch.int32
     ws, nbytes = _workspace(workspace, workspace_bytes, (c,), dev)
     status = _lib.clsa_sparse_attn8(ctypes.byref(p), ctypes.byref(c), _dense(q, "q", torch.bfloat16, dev), _dense(idx, "idx", i32, dev),

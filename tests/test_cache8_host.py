@@ -218,3 +218,26 @@ def test_reference_codes_round_to_nearest_even():
     assert list(ref.encode(np.array([np.inf, -np.inf, 1e9, np.nan]))) == [126, 254, 126, 127]
     for amax, e in ((448.0, 0), (448.0001, 1), (224.0, -1), (224.1, 0), (0.0, -100), (1e-40, -100), (3e38, 120), (1.75, -8), (1.0, -8)):
         assert ref.need_exponent(amax) == e, amax
+
+
+def test_native_marshalling_hands_back_what_it_does_not_take(clsa):
+    """Host tensors, addresses, wrong counts and foreign objects: the native module returns None and raises nothing."""
+    torch = pytest.importorskip("torch")
+    from paper_2606_06467_b200 import cache8
+
+    if cache8._marshal is None:
+        pytest.skip("built without Python.h")
+    cache8._load_torch()
+    m, p, c = cache8._marshal, _params(clsa), _cache(clsa)
+    spec = clsa.make_norm_rope()
+    t = torch.zeros(2, 1, 8, 128, dtype=torch.bfloat16)
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    for args in ((spec, None, t, t, None, None, None), (spec, None, None, None, None, None, None), (p, None, t, t, None, None, 0),
+                 (spec, None, 5, 5, None, None, 0), (None, None, t, t, None, None, 0), (), (object(),) * 7):
+        assert m.norm_rope(*args) is None
+    for args in ((p, c, None, t, t, None, ws, None, None), (c, p, None, t, t, None, ws, None, None), (p, c, None, None, None, None, ws, None, 0), ()):
+        assert m.append(*args) is None
+    for args in ((p, c, 0x1000, 0x2000, 1024, 0x3000, 4096, 0), (p, c, t, t, "x", ws, None, None), (p, c, t, t, 1 << 70, ws, None, None), ()):
+        assert m.scores(*args) is None
+    for args in ((p, c, 1, 2, 3, 4, None, None, 5, 6, 7), (p, c, t, t, t, t, None, 3, ws, -1, object()), ()):
+        assert m.attn(*args) is None

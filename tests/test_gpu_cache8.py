@@ -689,3 +689,61 @@ def test_outputs_in_pinned_host_memory():
     clsa.clsa_sparse_attn8(c.p, c.cache, q, idx, cnt, host, None, None, c.ws)
     torch.cuda.synchronize()
     assert torch.equal(host, want.cpu())
+
+
+def test_the_native_marshalling_and_the_python_one_agree(monkeypatch):
+    """The usual calls are taken by the native module; without it, and with layouts that only one of them takes, nothing differs."""
+    from paper_2606_06467_b200 import cache8
+
+    assert cache8._marshal is not None
+    spec = clsa.make_norm_rope(head_dim=128, norm=1, q_weight=randn(gen(1), 128), k_weight=randn(gen(2), 128))
+    taken, results = [], []
+    for native in (True, False):
+        if native:
+            class Watch:
+                def __getattr__(self, name):
+                    def call(*a):
+                        taken.append((name, getattr(real, name)(*a)))
+                        return taken[-1][1]
+                    return call
+            real = cache8._marshal
+            monkeypatch.setattr(cache8, "_marshal", Watch())
+        else:
+            monkeypatch.setattr(cache8, "_marshal", None)
+        for T, lens in ((1, [300, 70]), (3, [300, 70])):
+            c = Cache(lens, T, 2, 128, 64, 0, seed=8)
+            c.params(hq=8, top_k=64, causal=int(T > 1))
+            d = make_hidden(c, 8, 64, 9)
+            # (the first of three tokens sees 68 keys of the shorter sequence; what lies behind is not written)
+            # heads first: [B, T, H, D] as a view of [B, H, T, D], and of a fused projection
+            d["q"] = d["q"].transpose(1, 2).contiguous().transpose(1, 2) if T == 1 else d["q"]
+            fused = torch.cat([d["k"], d["v"]], 2)
+            d["k"], d["v"] = fused[:, :, :2], fused[:, :, 2:]
+            chain(c, spec, d, c.ws)
+            # the fallback's own layouts and its addresses
+            clsa.clsa_norm_rope(spec, None, d["q"].flatten(0, 1)[:1], d["qn"].flatten(0, 1)[:1])
+            out = torch.empty_like(d["out"])
+            clsa.clsa_sparse_attn8(c.p, c.cache, d["qn"], d["idx"].data_ptr(), d["cnt"], out, None, None, c.ws)
+            torch.cuda.synchronize()
+            assert c.status() == 0
+            results.append([t.clone() for t in (d["qn"], d["scores"][:, :, :68], d["idx"], d["out"], d["lse"], out, c.k, c.ks, c.idx)])
+        for wrong in (lambda: clsa.clsa_norm_rope(spec, d["pos"].long(), d["q"], d["qn"]),
+                      lambda: clsa.clsa_norm_rope(spec, d["pos"][1:], d["q"], d["qn"]),
+                      lambda: clsa.clsa_norm_rope(spec, d["pos"], d["q"].float(), d["qn"]),
+                      lambda: clsa.clsa_norm_rope(spec, d["pos"], d["q"], None),
+                      lambda: clsa.clsa_norm_rope(spec, d["pos"], d["q"], d["qn"][:, :, :4]),
+                      lambda: clsa.clsa_cache8_append(c.p, c.cache, None, d["k"][:, :, :1], d["v"], None, c.ws),
+                      lambda: clsa.clsa_cache8_append(c.p, c.cache, None, d["k"], None, None, c.ws),
+                      lambda: clsa.clsa_index_scores8(c.p, c.cache, d["qi"].half(), d["scores"], d["scores"].shape[-1], c.ws),
+                      lambda: clsa.clsa_index_scores8(c.p, c.cache, d["qi"], d["scores"], d["scores"].shape[-1], c.ws.cpu()),
+                      lambda: clsa.clsa_sparse_attn8(c.p, c.cache, d["qn"], d["idx"].transpose(0, 1), d["cnt"], d["out"], None, None, c.ws)):
+            with pytest.raises(ValueError):
+                wrong()
+        with pytest.raises(clsa.ClsaError):  # the C side's refusals
+            clsa.clsa_sparse_attn8(c.p, c.cache, d["qn"], d["idx"], d["cnt"], d["out"], None, None, c.ws, 16)
+    n = len(results) // 2
+    for a, b in zip(results[:n], results[n:]):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
+    usual = [name for name, status in taken if status == 0]
+    assert set(usual) == {"norm_rope", "append", "scores", "attn"} and len(usual) >= 10
