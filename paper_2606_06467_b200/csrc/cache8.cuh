@@ -33,11 +33,14 @@ cudaError_t launch_index_expand8(const clsa_params& p, const clsa_cache8& c, voi
                                  uint32_t* status, const DeviceInfo& dev, cudaStream_t stream);
 
 // Launch shape of the 8-bit attention kernel.
+// How the stages are dealt to the workers: one flat list cut evenly; workers of its own for every unit; or whole units per block,
+// of which its warps take some whole and share the last ones.
+enum : int { kAttn8Flat = 0, kAttn8Units = 1, kAttn8Blocks = 2 };
 struct Attn8Plan {
   int warps;            // warps per block
   int blocks, wpb;      // grid, workers per block
   int workers;          // warps that get a span of the stage list
-  int aligned;          // 1: every unit has workers of its own
+  int mode;             // kAttn8Flat, kAttn8Units or kAttn8Blocks
   int unit_stages;      // 32-token stages per (query row, KV head) unit
   int64_t units, total_stages;
   size_t smem_bytes;
@@ -175,6 +178,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
 __device__ __forceinline__ uint64_t bf16x2_to_f32x2(uint32_t w) { return pack2(bf16_lo(w), bf16_hi(w)); }

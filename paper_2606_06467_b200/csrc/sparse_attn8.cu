@@ -45,7 +45,8 @@ struct Attn8Args {
   const uint8_t* ks;
   const uint8_t* vs;
   int64_t head_stride, scale_head;
-  uint32_t stride16;  // token stride in 16-byte units
+  uint32_t unit;      // 16
+  uint32_t stride16;  // token stride in units
   int scale_shift;
   int64_t num_rows;
   const int64_t* seq_start;
@@ -61,16 +62,16 @@ struct Attn8Args {
   int rows, q_per_seq, num_q_heads, num_kv_heads, group, top_k, max_seq_len;
   int reverse, early, keep, pin;
   int unit_stages, total_stages;
-  int aligned, span_q, span_rem, workers, wpb;
+  int mode, span_q, span_rem, workers, wpb;  // Attn8Plan::mode
   float* part;       // records of [group][kPartialStride] floats: W of the workers, then 2 per block
   uint32_t* arrive;  // [blocks][group] arrival counters of the unit that leaves block b to the right, zero between launches
   float scale_log2;
 };
 
-// First stage of worker w's span (aligned: unit u has span_q workers, the first span_rem units one more, its stages cut evenly
-// over them; flat: the first span_rem workers take span_q + 1 consecutive stages, the others span_q).
+// First stage of worker w's span (kAttn8Units: unit u has span_q workers, the first span_rem units one more, its stages cut evenly
+// over them; kAttn8Flat: the first span_rem workers take span_q + 1 consecutive stages, the others span_q).
 __device__ __forceinline__ int span_begin(int w, const Attn8Args& a) {
-  if (!a.aligned) return w * a.span_q + min(w, a.span_rem);
+  if (a.mode == kAttn8Flat) return w * a.span_q + min(w, a.span_rem);
   const int big = a.span_rem * (a.span_q + 1);
   int u, j, n;
   if (w < big) { n = a.span_q + 1; u = w / n; j = w - u * n; }
@@ -78,7 +79,7 @@ __device__ __forceinline__ int span_begin(int w, const Attn8Args& a) {
   return u * a.unit_stages + (int)((int64_t)j * a.unit_stages / n);
 }
 __device__ __forceinline__ void unit_workers(int u, const Attn8Args& a, int& first, int& last) {
-  if (a.aligned) {
+  if (a.mode == kAttn8Units) {
     first = u * a.span_q + min(u, a.span_rem);
     last = first + a.span_q + (u < a.span_rem ? 1 : 0) - 1;
   } else {
@@ -97,6 +98,12 @@ __device__ __forceinline__ int k_token(int r) { return 4 * ((r >> 1) & 3) + (r &
 __device__ __forceinline__ uint32_t k_chunk(int t, int c) { return (uint32_t)(t * 128 + ((c ^ ((t & 1) | ((t >> 1) & 6))) << 4)); }
 __device__ __forceinline__ uint32_t v_chunk(int t, int c) { return (uint32_t)(t * 128 + ((c ^ (t & 7)) << 4)); }
 
+// base + units * unit: one instruction where the compiler does not know the unit (it makes four of a power of two)
+__device__ __forceinline__ const uint8_t* at_unit(const uint8_t* base, uint32_t units, uint32_t unit) {
+  const uint8_t* p;
+  asm("mad.wide.u32 %0, %1, %2, %3;" : "=l"(p) : "r"(units), "r"(unit), "l"(base));
+  return p;
+}
 __device__ __forceinline__ void cp_async16_plain(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
 }
@@ -123,8 +130,25 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   const int G = a.group, NS = a.unit_stages, W = a.workers;
   const int w = (int)blockIdx.x * a.wpb + warp;
   const bool has_work = warp < a.wpb && w < W;
-  const int s_begin = has_work ? span_begin(w, a) : 0;
-  const int s_end = has_work ? (w + 1 < W ? span_begin(w + 1, a) : a.total_stages) : 0;
+  // This worker's stages: whole units [own_lo, own_hi) (kAttn8Blocks), then the span [s_begin, s_end).
+  int own_lo = 0, own_hi = 0, s_begin = 0, s_end = 0;
+  if (a.mode == kAttn8Blocks) {
+    const int b = (int)blockIdx.x, n = a.span_q + (b < a.span_rem ? 1 : 0), each = n / a.wpb;
+    const int shared = (n - each * a.wpb) * NS, parts = min(a.wpb, shared);  // stages that the first `parts` warps share
+    const int u0 = b * a.span_q + min(b, a.span_rem), base = (u0 + each * a.wpb) * NS;
+    if (has_work) {
+      own_lo = (u0 + warp * each) * NS;
+      own_hi = own_lo + each * NS;
+    }
+    s_begin = s_end = base + shared;
+    if (warp < parts) {
+      s_begin = base + (int)((int64_t)warp * shared / parts);
+      s_end = base + (int)((int64_t)(warp + 1) * shared / parts);
+    }
+  } else if (has_work) {
+    s_begin = span_begin(w, a);
+    s_end = w + 1 < W ? span_begin(w + 1, a) : a.total_stages;
+  }
   unsigned char* ring = smem + warp * S::kRing;
   const uint32_t ring_u32 = smem_u32(ring);
   float2* scales = reinterpret_cast<float2*>(smem + WARPS * S::kRing + warp * S::kScale);
@@ -134,10 +158,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   if (lane == 0) {
     // For the merge: the units that this warp does not have whole and that no earlier warp of the block reaches into -- the
     // one its span starts in, the one it ends in -- or -1.
-    const int uf = s_begin / NS, ul = has_work ? (s_end - 1) / NS : 0;
+    const bool any = s_begin < s_end;
+    const int uf = s_begin / NS, ul = any ? (s_end - 1) / NS : 0;
     span_tab[warp] = make_int2(s_begin, s_end);
-    split_tab[warp] = make_int2(has_work && (s_begin > uf * NS || s_end < (uf + 1) * NS) && (warp == 0 || s_begin == uf * NS) ? uf : -1,
-                                has_work && ul != uf && s_end < (ul + 1) * NS ? ul : -1);
+    split_tab[warp] = make_int2(any && (s_begin > uf * NS || s_end < (uf + 1) * NS) && (warp == 0 || s_begin == uf * NS) ? uf : -1,
+                                any && ul != uf && s_end < (ul + 1) * NS ? ul : -1);
   }
 
   // Programmatic dependent launch, as in the bf16 kernels: dependents are released only behind this grid's own wait.
@@ -163,12 +188,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   const uint32_t v_frag = ring_u32 + kStage8Bytes / 2 + v_chunk(lane, 0);
   const int my_tok = k_token(rowq) + (upper ? 16 : 0);  // this lane's tokens of a stage: my_tok + {0, 2} and, unfolded, {16, 18}
 
-  int cur = a.reverse ? s_end : s_begin;
-  while (a.reverse ? cur > s_begin : cur < s_end) {
-    // ---- the next segment of this worker's span: stages [seg_lo, seg_hi) of unit u --------------------------------
-    const int u = (a.reverse ? cur - 1 : cur) / NS;
-    const int seg_lo = max(s_begin, u * NS), seg_hi = min(s_end, (u + 1) * NS);
-    cur = a.reverse ? seg_lo : seg_hi;
+  int left = own_hi - own_lo + s_end - s_begin;  // stages to go
+  while (left > 0) {
+    // ---- the next segment: stages [seg_lo, seg_hi) of unit u; the whole units first, so that what the block's warps share
+    // ---- ends the walk in either direction --------------------------------------------------------------------------
+    const bool own = left > s_end - s_begin;
+    const int lo = own ? own_lo : s_begin, hi = own ? own_hi : s_end, to_go = own ? left - (s_end - s_begin) : left;
+    const int u = (a.reverse ? lo + to_go - 1 : hi - to_go) / NS;
+    const int seg_lo = max(lo, u * NS), seg_hi = min(hi, (u + 1) * NS);
+    left -= seg_hi - seg_lo;
     const int g = u / a.rows, r = u - g * a.rows;
     const int h0 = g * G, b = r / a.q_per_seq;
     const int slot_lo = (seg_lo - u * NS) * kTok;
@@ -250,9 +278,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
           if (okmask == 0xffffffffu && !a.keep) {  // the usual stage
 #pragma unroll
             for (int it = 0; it < 8; ++it) {
-              const uint64_t off = (uint64_t)__shfl_sync(0xffffffffu, my16, 4 * it + (lane >> 3)) * 16u;
-              cp_async16_plain(k_copy[it & 3] + at + 512 * it, kbase + off);
-              cp_async16_plain(v_copy[it & 1] + at + 512 * it, vbase + off);
+              const uint32_t units = __shfl_sync(0xffffffffu, my16, 4 * it + (lane >> 3));
+              cp_async16_plain(k_copy[it & 3] + at + 512 * it, at_unit(kbase, units, a.unit));
+              cp_async16_plain(v_copy[it & 1] + at + 512 * it, at_unit(vbase, units, a.unit));
             }
           } else {  // some rows are none and become zeros, or rows have an L2 priority
             if (!ok && n_ok && raw_live) flag_status(a.status, CLSA_DEV_BAD_INDEX);
@@ -333,11 +361,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
         float2 sc[NX];  // tokens my_tok + 2 (t & 1) + 16 (t / 2)
 #pragma unroll
         for (int t = 0; t < NX; ++t) sc[t] = scales[buf * kTok + my_tok + 2 * (t & 1) + 8 * (t & 2)];
-        float s[NT][2][4];
+        float s[NT][2][4], s2[NT][2][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) { s[nt][k][0] = 0.f; s[nt][k][1] = 0.f; s[nt][k][2] = 0.f; s[nt][k][3] = 0.f; }
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][k][i] = s2[nt][k][i] = 0.f;
 #pragma unroll
         for (int st = 0; st < 4; ++st)
 #pragma unroll
@@ -349,18 +379,28 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
               const uint32_t a0 = e4m3x2_to_f16x2(kf[2 * k]), a2 = e4m3x2_hi_to_f16x2(kf[2 * k]);
               const uint32_t a1 = e4m3x2_to_f16x2(kf[2 * k + 1]), a3 = e4m3x2_hi_to_f16x2(kf[2 * k + 1]);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt][mt], a0, a1, a2, a3, qb[nt][2 * st + k][0], qb[nt][2 * st + k][1]);
+              for (int nt = 0; nt < NT; ++nt) mma_f16(k ? s2[nt][mt] : s[nt][mt], a0, a1, a2, a3, qb[nt][2 * st + k][0], qb[nt][2 * st + k][1]);
             }
           }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][k][i] += s2[nt][k][i];
         // x of the lane's tokens and two heads per tile: x[..][2 t + head]
-        float x[NT][2 * NX], top[NT][2], tope[NT][2];
+        float x[NT][2 * NX], xe[NT][2 * NX], top[NT][2], tope[NT][2];
         bool move = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 2 * NX; ++i) {
-            const float dot = FOLD ? (upper ? s[nt][1][i & 3] : s[nt][0][i & 3]) : s[nt][i >> 2][i & 3];
-            x[nt][i] = dot * sc[i >> 1].x * qf[nt][i & 1];
+          for (int t = 0; t < NX; ++t) {
+            float d[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) d[h] = FOLD ? (upper ? s[nt][1][2 * t + h] : s[nt][0][2 * t + h]) : s[nt][t >> 1][2 * (t & 1) + h];
+            const float2 y = unpack2(mul2(mul2(pack2(d[0], d[1]), pack2(sc[t].x, sc[t].x)), pack2(qf[nt][0], qf[nt][1])));
+            x[nt][2 * t] = y.x;
+            x[nt][2 * t + 1] = y.y;
           }
         if (okmask != 0xffffffffu) {
 #pragma unroll
@@ -369,18 +409,25 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
             for (int i = 0; i < 2 * NX; ++i) x[nt][i] = (okmask >> (my_tok + (i & 2) + 4 * (i & 4))) & 1u ? x[nt][i] : -INFINITY;
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int t = 0; t < NX; ++t) {  // with V's exponent
+            const float2 y = unpack2(add2(pack2(x[nt][2 * t], x[nt][2 * t + 1]), pack2(sc[t].y, sc[t].y)));
+            xe[nt][2 * t] = y.x;
+            xe[nt][2 * t + 1] = y.y;
+          }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             top[nt][h] = x[nt][h];
-            tope[nt][h] = x[nt][h] + sc[0].y;
+            tope[nt][h] = xe[nt][h];
 #pragma unroll
             for (int t = 1; t < NX; ++t) {
               top[nt][h] = fmaxf(top[nt][h], x[nt][2 * t + h]);
-              tope[nt][h] = fmaxf(tope[nt][h], x[nt][2 * t + h] + sc[t].y);
+              tope[nt][h] = fmaxf(tope[nt][h], xe[nt][2 * t + h]);
             }
             move = move || top[nt][h] > mx[nt][h] + kLazy || tope[nt][h] > m[nt][h] + kLazy;
           }
+        }
         if (__any_sync(0xffffffffu, move)) {  // some head's references have to move: to the largest seen so far
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -405,13 +452,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
           for (int t = 0; t < NX; ++t) {
-            float w[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              l[nt][h] += fast_exp2(x[nt][2 * t + h] - mx[nt][h]);
-              w[h] = fast_exp2(x[nt][2 * t + h] + sc[t].y - m[nt][h]);
-            }
-            pb[nt][t] = movmatrix_trans(pack_f16x2(w[0], w[1]));
+            const float2 d = unpack2(add2(pack2(x[nt][2 * t], x[nt][2 * t + 1]), pack2(-mx[nt][0], -mx[nt][1])));
+            const float2 w = unpack2(add2(pack2(xe[nt][2 * t], xe[nt][2 * t + 1]), pack2(-m[nt][0], -m[nt][1])));
+            const float2 y = unpack2(add2(pack2(l[nt][0], l[nt][1]), pack2(fast_exp2(d.x), fast_exp2(d.y))));
+            l[nt][0] = y.x;
+            l[nt][1] = y.y;
+            pb[nt][t] = movmatrix_trans(pack_f16x2(fast_exp2(w.x), fast_exp2(w.y)));
           }
           if (FOLD) {  // columns 0 .. 3 have the weights of the stage's first half, 4 .. 7 those of its second
 #pragma unroll
@@ -422,16 +468,19 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
           }
         }
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          uint32_t v[4];  // tokens 0-15 of dimensions 16 c + rowq and + 8, then tokens 16-31
-          ldmatrix_b8_x2_trans(v, (v_frag + at) ^ (uint32_t)(c << 4));
+        for (int c = 0; c < 8; c += 2) {
+          uint32_t v[2][4];  // tokens 0-15 of dimensions 16 c + rowq and + 8, then tokens 16-31
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint32_t a0 = e4m3x2_to_f16x2(v[2 * k]), a2 = e4m3x2_hi_to_f16x2(v[2 * k]);
-            const uint32_t a1 = e4m3x2_to_f16x2(v[2 * k + 1]), a3 = e4m3x2_hi_to_f16x2(v[2 * k + 1]);
+          for (int j = 0; j < 2; ++j) ldmatrix_b8_x2_trans(v[j], (v_frag + at) ^ (uint32_t)((c + j) << 4));
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][c], a0, a1, a2, a3, pb[nt][2 * k], pb[nt][2 * k + 1]);
-          }
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t a0 = e4m3x2_to_f16x2(v[j][2 * k]), a2 = e4m3x2_hi_to_f16x2(v[j][2 * k]);
+              const uint32_t a1 = e4m3x2_to_f16x2(v[j][2 * k + 1]), a3 = e4m3x2_hi_to_f16x2(v[j][2 * k + 1]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][c + j], a0, a1, a2, a3, pb[nt][2 * k], pb[nt][2 * k + 1]);
+            }
         }
         __syncwarp();  // everyone is done with this buffer before it is refilled
         settle(i + STAGES - 1, pend_k, pend_v);
@@ -489,7 +538,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
         if (a.lse != nullptr && lane == 0) a.lse[item] = ml.y != 0.f ? (ml.x + log2f(ml.y)) * kLn2 : -INFINITY;
       }
       __syncwarp();
-    } else if (a.reverse ? cur > s_begin : cur < s_end) {
+    } else if (left > 0) {
       // more segments follow and will reuse the ring: this partial waits in the worker's global slot
       const int rec4 = G * (kPartialStride / 4);
       float4* slot = reinterpret_cast<float4*>(a.part) + (int64_t)w * rec4;
@@ -622,18 +671,23 @@ Attn8Plan make_attn8_plan(const clsa_params& p, const DeviceInfo& dev) {
     while (per_unit * plan.wpb > plan.unit_stages) --per_unit;  // no worker without a stage
     blocks = plan.units * per_unit;
     workers = blocks * plan.wpb;
-    plan.aligned = 1;
+    plan.mode = kAttn8Units;
   } else {
     blocks = dev.sm_count;
     workers = plan.total_stages < blocks * plan.warps ? plan.total_stages : blocks * plan.warps;
     plan.wpb = (int)((workers + blocks - 1) / blocks);
     blocks = (workers + plan.wpb - 1) / plan.wpb;
-    // Unit-aligned split when every unit can have workers of its own and the longest span that results stays within 15 % of
-    // the even share.
-    plan.aligned = 0;
-    if (workers >= plan.units) {
+    // Whole units per block, where the blocks with one unit more have at most six stages per warp more than the even share: that
+    // leaves no unit to two blocks and few to two warps. Else, where every unit can have workers of its own and the longest
+    // span that results stays within 15 % of the even share, those.
+    const int64_t most = (plan.units + blocks - 1) / blocks;
+    plan.mode = kAttn8Flat;
+    if (plan.wpb == plan.warps && (most * blocks - plan.units) * plan.unit_stages <= 6 * blocks * plan.warps) {
+      plan.mode = kAttn8Blocks;
+      workers = blocks * plan.warps;
+    } else if (workers >= plan.units) {
       const int64_t longest = (plan.unit_stages + workers / plan.units - 1) / (workers / plan.units);
-      if (longest * workers * 100 <= plan.total_stages * 115) plan.aligned = 1;
+      if (longest * workers * 100 <= plan.total_stages * 115) plan.mode = kAttn8Units;
     }
   }
   plan.blocks = (int)blocks;
@@ -659,6 +713,7 @@ cudaError_t launch_sparse_attn8(const clsa_params& p, const clsa_cache8& c, cons
   a.vs = static_cast<const uint8_t*>(c.v_scale);
   a.head_stride = c.kv_head_stride;
   a.scale_head = c.scale_head_stride;
+  a.unit = 16;
   a.stride16 = (uint32_t)(c.kv_token_stride / 16);
   while ((1 << a.scale_shift) < c.scale_block) ++a.scale_shift;
   a.num_rows = p.num_cache_rows;
@@ -693,9 +748,11 @@ cudaError_t launch_sparse_attn8(const clsa_params& p, const clsa_cache8& c, cons
   }
   a.unit_stages = plan.unit_stages;
   a.total_stages = (int)plan.total_stages;  // < 2^31, checked by the entry point
-  a.aligned = plan.aligned;
-  a.span_q = plan.aligned ? (int)(plan.workers / plan.units) : (int)(plan.total_stages / plan.workers);
-  a.span_rem = plan.aligned ? (int)(plan.workers % plan.units) : (int)(plan.total_stages % plan.workers);
+  a.mode = plan.mode;
+  const int64_t split = plan.mode == kAttn8Flat ? plan.total_stages : plan.units;  // over the workers, or the blocks
+  const int64_t over = plan.mode == kAttn8Blocks ? plan.blocks : plan.workers;
+  a.span_q = plan.mode == kAttn8Units ? (int)(plan.workers / plan.units) : (int)(split / over);
+  a.span_rem = plan.mode == kAttn8Units ? (int)(plan.workers % plan.units) : (int)(split % over);
   a.workers = plan.workers;
   a.wpb = plan.wpb;
   a.arrive = arrive;
