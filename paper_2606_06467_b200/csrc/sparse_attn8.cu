@@ -45,7 +45,7 @@ struct Attn8Args {
   const uint8_t* ks;
   const uint8_t* vs;
   int64_t head_stride, scale_head;
-  uint32_t unit;      // 16
+  uint32_t unit;  // 16
   uint32_t stride16;  // token stride in units
   int scale_shift;
   int64_t num_rows;
@@ -98,7 +98,8 @@ __device__ __forceinline__ int k_token(int r) { return 4 * ((r >> 1) & 3) + (r &
 __device__ __forceinline__ uint32_t k_chunk(int t, int c) { return (uint32_t)(t * 128 + ((c ^ ((t & 1) | ((t >> 1) & 6))) << 4)); }
 __device__ __forceinline__ uint32_t v_chunk(int t, int c) { return (uint32_t)(t * 128 + ((c ^ (t & 7)) << 4)); }
 
-// base + units * unit: one instruction where the compiler does not know the unit (it makes four of a power of two)
+// base + units * unit: one instruction where the compiler does not know the unit (it makes four of a power of two, and three of a
+// product that it has already; so K and V have a unit each)
 __device__ __forceinline__ const uint8_t* at_unit(const uint8_t* base, uint32_t units, uint32_t unit) {
   const uint8_t* p;
   asm("mad.wide.u32 %0, %1, %2, %3;" : "=l"(p) : "r"(units), "r"(unit), "l"(base));
@@ -249,12 +250,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       const int pos_hi = PAGED ? n : (int)max((int64_t)pos_lo, min((int64_t)n, a.num_rows - start));
       const uint32_t pos_span = (uint32_t)(pos_hi - pos_lo);
       auto load_blk = [&](int raw) -> int { return PAGED && (uint32_t)raw < (uint32_t)n ? __ldg(table + (raw >> a.block_shift)) : -1; };
-      auto settle = [&](int i, int kb, int vb) {  // the scale bytes of stage i into shared memory
-        scales[(i % STAGES) * kTok + lane] = make_float2(exp2_int(scale_exponent(kb)), (float)scale_exponent(vb));
+      auto settle = [&](int buf, int kb, int vb) {  // the scale bytes of stage i into shared memory
+        scales[buf * kTok + lane] = make_float2(exp2_int(scale_exponent(kb)), (float)scale_exponent(vb));
       };
-      auto issue = [&](int i, int raw, int blk, int& kb, int& vb) {  // the copies of stage i; its scale bytes stay in flight
+      auto issue = [&](int i, int buf, int raw, int blk, int& kb, int& vb) {  // the copies of stage i; its scale bytes stay in flight
         if (i < nstages) {
-          const int buf = i % STAGES;
           uint32_t row;
           bool ok;
           if (PAGED) {
@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 #pragma unroll
       for (int i = 0; i < STAGES; ++i) blk_p[i] = load_blk(raw_p[i]);
 #pragma unroll
-      for (int i = 0; i < STAGES; ++i) issue(i, raw_p[i], blk_p[i], raw_p[i], blk_p[i]);  // (now the scale bytes)
+      for (int i = 0; i < STAGES; ++i) issue(i, i, raw_p[i], blk_p[i], raw_p[i], blk_p[i]);  // (now the scale bytes)
       int blkX = load_blk(rawX);
       wait_now();  // with only q pending, everything read so far was complete before this launch; q is read behind the wait
 
@@ -350,12 +350,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       for (int i = 0; i + 1 < STAGES; ++i) settle(i, raw_p[i], blk_p[i]);
       int pend_k = raw_p[STAGES - 1], pend_v = blk_p[STAGES - 1];  // settled one iteration after their stage was issued
 #pragma unroll 1
-      for (int i = 0; i < nstages; ++i) {
+      for (int i0 = 0; i0 < nstages; i0 += STAGES)
+#pragma unroll
+      for (int buf = 0; buf < STAGES; ++buf) {  // (places in the ring are constants then)
+        const int i = i0 + buf;
+        if (i >= nstages) break;
         const int raw_new = next_raw();
         const int blk_new = load_blk(rawY);
         cp_async_wait<STAGES - 1>();
         __syncwarp();
-        const int buf = i % STAGES;
         const uint32_t at = (uint32_t)(buf * kStage8Bytes);
         const uint32_t okmask = stage_mask[buf];
         float2 sc[NX];  // tokens my_tok + 2 (t & 1) + 16 (t / 2)
@@ -373,7 +376,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt) {
             uint32_t kf[4];  // chunk 2 st of rows 0-7, 8-15, chunk 2 st + 1 of them
-            ldmatrix_x4(kf, ((k_frag + at) ^ (uint32_t)(st << 5)) + 2048 * mt);
+            ldmatrix_x4(kf, (k_frag ^ (uint32_t)(st << 5)) + (at + 2048 * mt));
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               const uint32_t a0 = e4m3x2_to_f16x2(kf[2 * k]), a2 = e4m3x2_hi_to_f16x2(kf[2 * k]);
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
         for (int c = 0; c < 8; c += 2) {
           uint32_t v[2][4];  // tokens 0-15 of dimensions 16 c + rowq and + 8, then tokens 16-31
 #pragma unroll
-          for (int j = 0; j < 2; ++j) ldmatrix_b8_x2_trans(v[j], (v_frag + at) ^ (uint32_t)((c + j) << 4));
+          for (int j = 0; j < 2; ++j) ldmatrix_b8_x2_trans(v[j], (v_frag ^ (uint32_t)((c + j) << 4)) + at);
 #pragma unroll
           for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -483,8 +486,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
             }
         }
         __syncwarp();  // everyone is done with this buffer before it is refilled
-        settle(i + STAGES - 1, pend_k, pend_v);
-        issue(i + STAGES, rawX, blkX, pend_k, pend_v);
+        settle((buf + STAGES - 1) % STAGES, pend_k, pend_v);
+        issue(i + STAGES, buf, rawX, blkX, pend_k, pend_v);
         rawX = rawY;
         blkX = blk_new;
         rawY = raw_new;
