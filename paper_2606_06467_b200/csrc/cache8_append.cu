@@ -1,14 +1,19 @@
 // The newest tokens' K, V and K_idx rows into the 8-bit caches: per block of SB cache rows and head, the largest magnitude of
 // the new rows gives the block's power-of-two scale, and each element is rounded once to e4m3.
 //
-// Chunks (T > 1): a block of threads takes one scale block of one sequence and K and V of one or more heads (or K_idx), the rows of
-// the next on their way while it works on one: 16 (or, for 64-wide indexer keys, 8) lanes per row with 16 bytes each, all rows of a head in registers between the
-// pass that finds the maximum and the pass that writes the codes, so every element is read once. Bound by HBM for long prompts
-// (2 bytes in, 1 out). K's norm and rotation happen on the way in fp32. The angles of the rows are built by
-// the addition theorem: a row's position is begin + 8 u + v, and cosines and sines of SB / 8 + 8 positions, formed once for all
-// the block's K heads, give those of all SB rows at two instructions a pair of dimensions. A scale block that holds older rows is re-coded by the same threads when its exponent grows.
+// Chunks (T > 1): a block of threads takes one scale block of one sequence and K and V of one or two heads (or K_idx), the rows of
+// the next on their way while it works on one: 16 (or, for 64-wide indexer keys, 8) lanes per row with 16 bytes each, all rows of a
+// head in registers between the pass that finds the maximum and the pass that writes the codes, so every element is read once.
+// K's norm and rotation happen on the way in fp32. The angles of the rows are built by the addition theorem: a row's position is
+// begin + 8 u + v, and cosines and sines of SB / 8 + 8 positions, formed once for all the block's K heads, give those of all SB
+// rows; the part of v is folded with the weights once per head, which leaves seven packed operations per pair of dimensions.
+// A scale block that holds older rows is re-coded by the same threads when its exponent grows.
+// 4096 tokens of 8 heads, indexer keys, norm and rotation over all dimensions: 26.7 MB in 13.4 us (the bytes alone would take 4.1;
+// without rotation 8.2, without norm 6.9): bound by instruction issue at 16 warps per SM, which the rows in registers allow
+// (half of the issue slots are used; 80 registers and half as many warps again, other heads per block and K and V in
+// blocks of their own measured the same or slower).
 // Single tokens (T = 1): half a warp per row, no block barrier; what does not depend on the sequence's length (the row, the
-// weight, the frequencies) is fetched together with it. Bound by a launch and two dependent round trips.
+// weight, the frequencies) is fetched together with it. Bound by a launch and two dependent round trips: 16 sequences of 8 heads 2.8 us.
 #include "cache8.cuh"
 
 namespace clsa {
@@ -84,7 +89,7 @@ struct Rows {
 template <int SB, int THREADS, int LANES, bool SPEC>
 __device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows, uint8_t* code, int64_t code_token,
                                             uint8_t* scale, int lo, int hi, const AppendArgs& a, const float* bc, const float* bs,
-                                            float* red) {
+                                            const float* unit, float* red) {
   constexpr int kRowsPerPass = THREADS / LANES, R = Rows<SB, THREADS, LANES>::R;
   const auto& raw = rows.raw;
   const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
@@ -96,25 +101,31 @@ __device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows
     const bool turned = 8 * l < rot, inter = a.spec.interleaved;
     const int partner = l < hl ? l + hl : (l < 2 * hl ? l - hl : l);
     const int i0 = !turned ? 0 : inter ? 4 * l : (l < hl ? 8 * l : 8 * l - half);
-    // z_i = r (x_i w_i cos + x_partner w'_i sin), w' the partner's weight with the sign of its term
-    uint64_t w[4], wp[4], cv[4], sv[4];
+    // z_i = r (x_i w_i cos + x_partner w'_i sin), w' the partner's weight with the sign of its term; by the addition theorem, over the
+    // row's u and the lane's v: w cos = cu (w cv) - su (w sv), w' sin = su (w' cv) + cu (w' sv). Lanes that are not turned have
+    // cu = 1 and su = 0 of `unit`.
+    uint64_t w[4], wc[4], ws[4], pc[4], ps[4];
+    const float *cu_row = turned ? bc + i0 : unit, *su_row = turned ? bs + i0 : unit + 8;
+    const int u_step = turned ? half : 0;
     {
       uint4 wr = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);  // ones
       if (a.spec.norm && a.k_weight != nullptr) wr = *reinterpret_cast<const uint4*>(a.k_weight + 8 * l);
       const uint32_t w4[4] = {wr.x, wr.y, wr.z, wr.w};
       const float sg = l < hl ? -1.f : 1.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        w[k] = bf16x2_to_f32x2(w4[k]);
-        const uint32_t p = inter ? __byte_perm(w4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, w4[k], partner, LANES);
-        wp[k] = turned ? mul2(bf16x2_to_f32x2(p), inter ? pack2(-1.f, 1.f) : pack2(sg, sg)) : 0ull;
-      }
+      for (int k = 0; k < 4; ++k) w[k] = bf16x2_to_f32x2(w4[k]);
       if (rot > 0) {
-        load_pairs(cv, bc + (SB / 8 + (sub & 7)) * half, inter, i0);
-        load_pairs(sv, bs + (SB / 8 + (sub & 7)) * half, inter, i0);
-        if (!turned) {
+        uint64_t cv[4], sv[4];
+        load_pairs(cv, turned ? bc + (SB / 8 + (sub & 7)) * half + i0 : unit, inter, 0);
+        load_pairs(sv, turned ? bs + (SB / 8 + (sub & 7)) * half + i0 : unit + 8, inter, 0);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) { cv[k] = pack2(1.f, 1.f); sv[k] = 0ull; }
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t p = inter ? __byte_perm(w4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, w4[k], partner, LANES);
+          const uint64_t wp = turned ? mul2(bf16x2_to_f32x2(p), inter ? pack2(-1.f, 1.f) : pack2(sg, sg)) : 0ull;
+          wc[k] = mul2(w[k], cv[k]);
+          ws[k] = mul2(w[k], sv[k]) ^ 0x8000000080000000ull;
+          pc[k] = mul2(wp, cv[k]);
+          ps[k] = mul2(wp, sv[k]);
         }
       }
     }
@@ -135,15 +146,14 @@ __device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows
       const uint64_t r2 = pack2(root, root);
       if (rot > 0) {
         uint64_t cu[4], su[4];
-        load_pairs(cu, bc + (row >> 3) * half, inter, i0);
-        load_pairs(su, bs + (row >> 3) * half, inter, i0);
+        load_pairs(cu, cu_row + (row >> 3) * u_step, inter, 0);
+        load_pairs(su, su_row + (row >> 3) * u_step, inter, 0);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint64_t neg = su[k] ^ 0x8000000080000000ull;
-          const uint64_t c = turned ? fma2(cu[k], cv[k], mul2(neg, sv[k])) : cv[k], s = fma2(su[k], cv[k], mul2(cu[k], sv[k]));
           uint32_t p = inter ? __byte_perm(in4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, in4[k], partner, LANES);
           if (!turned) p = 0u;  // (an infinity times a zero sine is none)
-          x[r][k] = mul2(fma2(x[r][k], mul2(w[k], c), mul2(bf16x2_to_f32x2(p), mul2(wp[k], s))), r2);
+          const uint64_t f = fma2(cu[k], wc[k], mul2(su[k], ws[k])), fp = fma2(su[k], pc[k], mul2(cu[k], ps[k]));
+          x[r][k] = mul2(fma2(x[r][k], f, mul2(bf16x2_to_f32x2(p), fp)), r2);
         }
       } else {
 #pragma unroll
@@ -219,6 +229,7 @@ __device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows
 template <int SB, int THREADS>
 __global__ void __launch_bounds__(THREADS, 512 / THREADS) cache8_append_kernel(const __grid_constant__ AppendArgs a) {
   extern __shared__ __align__(16) float turns[];  // cosines, then sines: [SB / 8 + 8][rot_dim / 2] each
+  __shared__ __align__(16) float unit[16];  // the cosines and sines of no angle
   __shared__ float red[2][THREADS / 32];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int b = blockIdx.x / a.spans, span = blockIdx.x % a.spans;
@@ -236,6 +247,8 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) cache8_append_kernel(c
   const int64_t tok0 = (int64_t)b * a.T + (begin + lo - first);  // the first new token of this block
   const bool idx_block = (int)blockIdx.y >= a.head_groups;       // K_idx; the others K and V of heads h0 .. h1 - 1
   const int h0 = blockIdx.y * a.heads_per_block, h1 = min(h0 + a.heads_per_block, a.heads[0]);
+  const int half = a.spec.rot_dim >> 1, lanes = half > 32 ? 64 : 32;  // threads that share a position's angles
+  const float freq = !idx_block && (int)threadIdx.x % lanes < half ? a.spec.inv_freq[threadIdx.x % lanes] : 0.f;
   Rows<SB, THREADS, 16> next;
   const int kind0 = idx_block ? 2 : 0;
   if (!idx_block || a.idx_dim == 128)  // the first rows do not depend on where they go
@@ -256,23 +269,23 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) cache8_append_kernel(c
     if (a.idx_dim == 64) {
       Rows<SB, THREADS, 8> rows;
       rows.load(a.src[2] + tok0 * a.src_token[2], a.src_token[2], lo, hi);
-      append_head<SB, THREADS, 8, false>(rows, code, a.code_token[2], a.scale[2] + block, lo, hi, a, nullptr, nullptr, red[0]);
+      append_head<SB, THREADS, 8, false>(rows, code, a.code_token[2], a.scale[2] + block, lo, hi, a, nullptr, nullptr, nullptr, red[0]);
     } else {
-      append_head<SB, THREADS, 16, false>(next, code, a.code_token[2], a.scale[2] + block, lo, hi, a, nullptr, nullptr, red[0]);
+      append_head<SB, THREADS, 16, false>(next, code, a.code_token[2], a.scale[2] + block, lo, hi, a, nullptr, nullptr, nullptr, red[0]);
     }
     return;
   }
-  const int half = a.spec.rot_dim >> 1;
   float* bc = turns;
   float* bs = turns + (SB / 8 + 8) * half;
-  if (a.has_spec && half > 0) {
+  if (half > 0) {
     // positions begin + 8 u (with the scale), then 0 .. 7
-    const int j = threadIdx.x % 64;
+    const int j = threadIdx.x % lanes;
     if (j < half) {
-      const float freq = a.spec.inv_freq[j];
-      for (int u = threadIdx.x / 64; u < SB / 8 + 8; u += THREADS / 64)
+#pragma unroll 4
+      for (int u = threadIdx.x / lanes; u < SB / 8 + 8; u += THREADS / lanes)
         turn_of(u < SB / 8 ? begin + 8 * u : u - SB / 8, freq, u < SB / 8 ? a.spec.rot_scale : 1.f, &bc[u * half + j], &bs[u * half + j]);
     }
+    if (threadIdx.x < 16) unit[threadIdx.x] = threadIdx.x < 8 ? 1.f : 0.f;
     __syncthreads();
   }
   const int count = 2 * (h1 - h0);
@@ -287,9 +300,9 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) cache8_append_kernel(c
     uint8_t* code = a.code[kind] + row0 * a.code_token[kind] + h * a.code_head[kind];
     uint8_t* scale = a.scale[kind] + h * a.scale_head + block;
     if (kind == 0 && a.has_spec)
-      append_head<SB, THREADS, 16, true>(rows, code, a.code_token[kind], scale, lo, hi, a, bc, bs, red[i & 1]);
+      append_head<SB, THREADS, 16, true>(rows, code, a.code_token[kind], scale, lo, hi, a, bc, bs, unit, red[i & 1]);
     else
-      append_head<SB, THREADS, 16, false>(rows, code, a.code_token[kind], scale, lo, hi, a, nullptr, nullptr, red[i & 1]);
+      append_head<SB, THREADS, 16, false>(rows, code, a.code_token[kind], scale, lo, hi, a, nullptr, nullptr, nullptr, red[i & 1]);
   }
 }
 
@@ -444,7 +457,7 @@ cudaError_t launch_cache8_append(const clsa_params& p, const clsa_cache8& c, con
   a.spans = (p.q_per_seq - 1 + c.scale_block - 1) / c.scale_block + 1;  // scale blocks that T consecutive positions can touch
   const int64_t bx = (int64_t)p.num_seqs * a.spans;
   // Two heads per block where that still leaves about 400 threads per SM: they share the angles, and the second one's loads are
-  // hidden (4096 tokens of 8 heads, 64-row blocks: 15.4 us with one, 14.5 with two, 20.8 with four; 7 x 333 tokens of 4 heads,
+  // hidden (4096 tokens of 8 heads, 64-row blocks, first version: 15.4 us with one, 14.5 with two, 20.8 with four; 7 x 333 tokens of 4 heads,
   // 16-row blocks, no rotation: 4.9 with one, 5.4 with two).
   const int threads = c.scale_block <= 32 ? 128 : 256;
   a.heads_per_block = bx * ((a.heads[0] + 1) / 2) * threads >= (int64_t)400 * dev.sm_count ? 2 : 1;

@@ -8,6 +8,9 @@
 // product, a multiply-add and a scaling, two dimensions per instruction. Warps are independent of one another. How many of a
 // token's heads a warp takes follows from the number of tokens: few tokens are spread over many warps (each forms the angles
 // anew), many keep a token together.
+// 4096 tokens of 32 + 8 heads of 128: 84 MB in 18 us, 4.6 TB/s, 0.72 of a measured copy (14.2 us, 5.9 TB/s, with the input in L2:
+// what is missing is the ramp of one wave and the angles in front of the first product; rings of asynchronous copies took 29 to 35).
+// 16 tokens: 2.4 us, one launch.
 #include "cache8.cuh"
 
 namespace clsa {
