@@ -480,6 +480,39 @@ def test_sparse_attn_long_rows_and_hints():
     assert (counters == 0).all()
 
 
+@pytest.mark.parametrize("T,hq,hkv,top_k,lens", [
+    (223, 32, 8, 64, [700]),         # one whole unit per warp, and one that two warps share, in some blocks
+    (148, 32, 8, 300, [500]),        # eight units per block, all shared by its twelve warps
+    (190, 64, 8, 512, [800]),        # eight query heads per group
+    (111, 128, 8, 256, [400]),       # sixteen: eight warps per block, six units of a block
+    (130, 16, 8, 33, [300, 131]),    # a unit of two stages
+    (52, 40, 8, 700, [900]),         # more units than blocks, too few for whole units: units that blocks share
+    (401, 32, 8, 2048, [401]),       # short causal rows under a large budget: most stages are empty
+])
+def test_sparse_attn_ways_of_dealing_the_stages(T, hq, hkv, top_k, lens):
+    """Chunks on either side of the rules that deal units to blocks and warps, walked both ways; every row is written."""
+    c = Cache(lens, T, hkv, 64, 16, 16 if T % 2 else 0, seed=T)
+    c.params(hq=hq, top_k=top_k, causal=1)
+    q = randn(gen(T), c.B, T, hq, 128)
+    idx, cnt = make_index(c, top_k, 1, 2, counts=[top_k, 0, top_k - 1, 1, top_k])
+    out, lse = run_attn(c, q, idx, cnt)
+    assert not out.isnan().any() and not lse.isnan().any()
+    check_attn(c, hq, q, idx, cnt, out, lse, sample=40)
+    again, lse2 = run_attn(c, q, idx, cnt)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    o2, l2 = run_attn(c, q, idx, cnt, clsa.make_hints(reverse=1, keep_rows=1))
+    check_attn(c, hq, q, idx, cnt, o2, l2, sample=40)
+    # an output row depends on its own query only: one query's rows changed leave all others bit-identical
+    q2 = q.clone()
+    q2[0, T // 2] = randn(gen(5), hq, 128)
+    o3, l3 = run_attn(c, q2, idx, cnt)
+    keep = torch.ones(c.B, T, dtype=torch.bool, device=DEV)
+    keep[0, T // 2] = False
+    assert torch.equal(o3[keep], out[keep]) and torch.equal(l3[keep], lse[keep])
+    assert c.status() == 0
+    assert (c.ws[256:256 + 148 * 64].view(torch.int32) == 0).all()
+
+
 def test_sparse_attn_scales_far_apart():
     """Blocks whose V (and K) scales differ by many powers of two, a dominant logit on a block of tiny values, saturated codes."""
     c = Cache([512, 512], 1, 2, 64, 16, 0, seed=8)
