@@ -2,15 +2,15 @@
 // bound by HBM for a prefill chunk, by one launch and one memory round trip for a decode step).
 //
 // A head of D dimensions is held by D / 8 lanes of a warp, 16 bytes each; the sum of squares is a butterfly over those
-// lanes, the partner of a half-split rotation comes by shuffles of the raw words. A warp takes heads of one token, 32 / (D / 8) in
+// lanes, the partner of a half-split rotation comes by shuffles of the raw words, or, where it turns the whole head, sits in the same lane. A warp takes heads of one token, 32 / (D / 8) in
 // a pass, four passes' loads and then their work together. The token's rot_dim / 2 angles (64-bit product and reduction, 32-bit
 // functions) are formed once per warp and folded with the weights into two factors per dimension, so that a dimension costs a
 // product, a multiply-add and a scaling, two dimensions per instruction. Warps are independent of one another. How many of a
 // token's heads a warp takes follows from the number of tokens: few tokens are spread over many warps (each forms the angles
 // anew), many keep a token together.
-// 4096 tokens of 32 + 8 heads of 128: 84 MB in 18 us, 4.6 TB/s, 0.72 of a measured copy (14.2 us, 5.9 TB/s, with the input in L2:
-// what is missing is the ramp of one wave and the angles in front of the first product; rings of asynchronous copies took 29 to 35).
-// 16 tokens: 2.4 us, one launch.
+// 4096 tokens of 32 + 8 heads of 128: 84 MB in 17.2 us, 4.9 TB/s, 0.76 of a measured copy (10.8 us with the input in L2; 18.1 and
+// 14.2 before a lane had its own partners). What is missing is the launch and the ramp of one wave: two to five passes at a time
+// measure the same, rings of asynchronous copies took 29 to 35, loading ahead by a batch 19.5. 16 tokens: 2.2 us, one launch.
 #include "cache8.cuh"
 
 namespace clsa {
@@ -30,8 +30,9 @@ struct NormRopeArgs {
   int num_tokens, parts, part_heads;  // warps per token, heads of each
 };
 
-// DENSE: heads lie head_dim apart, in and out (strides are immediates then).
-template <int LANES, bool DENSE>
+// DENSE: heads lie head_dim apart, in and out (strides are immediates then). PAIR: all dimensions are turned, half apart; a lane
+// has 4 dimensions of each half then, 8 bytes apiece, and the partner of each.
+template <int LANES, bool DENSE, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
   constexpr int kGroups = 32 / LANES;  // heads of a pass
   __shared__ __align__(16) float turns[kThreads / 32][2][LANES * 4];
@@ -52,16 +53,21 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
     const int before = side ? a.heads[0] : 0;
     const int lo = max(part0 - before, 0);
     left = min(part0 + a.part_heads - before, a.heads[side]) - lo;
-    in = a.in[side] + token * a.in_token[side] + (lo + group) * a.in_head[side] + 8 * l;
-    out = a.out[side] + token * a.out_token[side] + (lo + group) * a.out_head[side] + 8 * l;
+    in = a.in[side] + token * a.in_token[side] + (lo + group) * a.in_head[side] + (PAIR ? 4 : 8) * l;
+    out = a.out[side] + token * a.out_token[side] + (lo + group) * a.out_head[side] + (PAIR ? 4 : 8) * l;
     in_step = DENSE ? 256 : kGroups * a.in_head[side];
     out_step = DENSE ? 256 : kGroups * a.out_head[side];
+  };
+  auto load8 = [](const uint16_t* at) -> uint4 {
+    if (!PAIR) return *reinterpret_cast<const uint4*>(at);
+    const uint2 lo = *reinterpret_cast<const uint2*>(at), hi = *reinterpret_cast<const uint2*>(at + 4 * LANES);
+    return make_uint4(lo.x, lo.y, hi.x, hi.y);
   };
   auto load = [&]() {
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
       raw[k] = make_uint4(0, 0, 0, 0);
-      if (group + k * kGroups < left) raw[k] = *reinterpret_cast<const uint4*>(in + k * in_step);
+      if (group + k * kGroups < left) raw[k] = load8(in + k * in_step);
     }
   };
   int side = 0;
@@ -87,12 +93,21 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
     uint64_t A[4], B[4];
     {
       uint4 wr = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);  // ones
-      if (norm && a.weight[side] != nullptr) wr = *reinterpret_cast<const uint4*>(a.weight[side] + 8 * l);
+      if (norm && a.weight[side] != nullptr) wr = load8(a.weight[side] + (PAIR ? 4 : 8) * l);
       const uint32_t w4[4] = {wr.x, wr.y, wr.z, wr.w};
-      float c[8], s[8];
-      if (rot > 0) load_turns(c, s, tc, ts, rot, inter, l);
+      if (PAIR) {
+        const float4 c = *reinterpret_cast<const float4*>(tc + 4 * l), s = *reinterpret_cast<const float4*>(ts + 4 * l);
+        const uint64_t c2[2] = {pack2(c.x, c.y), pack2(c.z, c.w)}, s2[2] = {pack2(s.x, s.y), pack2(s.z, s.w)};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 4; ++k) {
+          A[k] = mul2(bf16x2_to_f32x2(w4[k]), c2[k & 1]);
+          B[k] = mul2(bf16x2_to_f32x2(w4[k ^ 2]), s2[k & 1]) ^ (k < 2 ? 0x8000000080000000ull : 0ull);
+        }
+      }
+      float c[8], s[8];
+      if (!PAIR && rot > 0) load_turns(c, s, tc, ts, rot, inter, l);
+#pragma unroll
+      for (int k = 0; k < 4 && !PAIR; ++k) {
         const uint64_t w = bf16x2_to_f32x2(w4[k]);
         const uint32_t p = inter ? __byte_perm(w4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, w4[k], partner, LANES);
         A[k] = turned ? mul2(w, pack2(c[2 * k], c[2 * k + 1])) : w;
@@ -116,9 +131,14 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
       uint32_t o[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        uint32_t p = inter ? __byte_perm(in4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, in4[k], partner, LANES);
-        if (!turned) p = 0u;  // (an infinity times a zero sine is none)
-        const float2 z = unpack2(mul2(fma2(x[k], A[k], mul2(bf16x2_to_f32x2(p), B[k])), r2));
+        uint64_t other;
+        if (PAIR) {
+          other = x[k ^ 2];
+        } else {
+          const uint32_t p = inter ? __byte_perm(in4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, in4[k], partner, LANES);
+          other = bf16x2_to_f32x2(turned ? p : 0u);  // (an infinity times a zero sine is none)
+        }
+        const float2 z = unpack2(mul2(fma2(x[k], A[k], mul2(other, B[k])), r2));
         o[k] = pack_bf16x2(z.x, z.y);
       }
       return make_uint4(o[0], o[1], o[2], o[3]);
@@ -129,7 +149,14 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
       for (int k = 0; k < kUnroll; ++k) {
         if (k * kGroups >= left) break;  // the same for the whole warp
         const uint4 z = one(raw[k]);
-        if (group + k * kGroups < left) *reinterpret_cast<uint4*>(out + k * out_step) = z;
+        if (group + k * kGroups < left) {
+          if (PAIR) {
+            *reinterpret_cast<uint2*>(out + k * out_step) = make_uint2(z.x, z.y);
+            *reinterpret_cast<uint2*>(out + k * out_step + 4 * LANES) = make_uint2(z.z, z.w);
+          } else {
+            *reinterpret_cast<uint4*>(out + k * out_step) = z;
+          }
+        }
       }
       left -= kUnroll * kGroups;
       if (left <= 0) break;
@@ -158,8 +185,10 @@ void launch(NormRopeArgs& a, const DeviceInfo& dev, cudaStream_t stream) {
   const unsigned blocks = (unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32));
   bool dense = true;
   for (int i = 0; i < 2; ++i) dense = dense && (a.heads[i] <= 1 || (a.in_head[i] == 8 * LANES && a.out_head[i] == 8 * LANES));
-  if (dense) norm_rope_kernel<LANES, true><<<blocks, kThreads, 0, stream>>>(a);
-  else norm_rope_kernel<LANES, false><<<blocks, kThreads, 0, stream>>>(a);
+  const bool pair = a.spec.rot_dim == 8 * LANES && !a.spec.interleaved;
+  void (*kernel)(const NormRopeArgs) = dense ? (pair ? norm_rope_kernel<LANES, true, true> : norm_rope_kernel<LANES, true, false>)
+                                             : (pair ? norm_rope_kernel<LANES, false, true> : norm_rope_kernel<LANES, false, false>);
+  kernel<<<blocks, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
