@@ -56,6 +56,22 @@ __device__ __forceinline__ uint2 recode(uint2 v, float f) {
   return make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
 }
 
+// A lane's 8 codes: consecutive, or 4 of each half of the head.
+template <bool PAIR, int LANES>
+__device__ __forceinline__ uint2 get_codes(const uint8_t* at) {
+  if (!PAIR) return *reinterpret_cast<const uint2*>(at);
+  return make_uint2(*reinterpret_cast<const uint32_t*>(at), *reinterpret_cast<const uint32_t*>(at + 4 * LANES));
+}
+template <bool PAIR, int LANES>
+__device__ __forceinline__ void put_codes(uint8_t* at, uint2 v) {
+  if (!PAIR) {
+    *reinterpret_cast<uint2*>(at) = v;
+  } else {
+    *reinterpret_cast<uint32_t*>(at) = v.x;
+    *reinterpret_cast<uint32_t*>(at + 4 * LANES) = v.y;
+  }
+}
+
 constexpr float kLargest = 3.4028234663852886e38f;  // what is larger is not finite and does not count for a scale
 
 // A lane's 8 dimensions of a cosine or sine table row, as pairs.
@@ -69,6 +85,12 @@ __device__ __forceinline__ void load_pairs(uint64_t (&p)[4], const float* t, boo
   }
 }
 
+__device__ __forceinline__ void load_quad(uint64_t (&p)[2], const float* t) {
+  const float4 a = *reinterpret_cast<const float4*>(t);
+  p[0] = pack2(a.x, a.y);
+  p[1] = pack2(a.z, a.w);
+}
+
 // One head of one scale block: rows `lo` .. `hi` - 1 of the block are new, rows below `lo` older ones of the sequence. SPEC: the
 // rows go through K's norm and rotation first (LANES 16); bc, bs: cosines and sines of positions begin + 8 u, then of 0 .. 7.
 template <int SB, int THREADS, int LANES>
@@ -76,17 +98,27 @@ struct Rows {
   static constexpr int kPerPass = THREADS / LANES;  // a multiple of 8: a lane's rows share their place among 8
   static constexpr int R = SB / kPerPass;
   uint4 raw[R];
-  __device__ __forceinline__ void load(const uint16_t* src, int64_t src_token, int lo, int hi) {  // zeros for rows that are not new
+  // Zeros for rows that are not new. pair: 4 dimensions of each half of the head per lane instead of 8 consecutive ones.
+  __device__ __forceinline__ void load(const uint16_t* src, int64_t src_token, int lo, int hi, bool pair) {
     const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int row = r * kPerPass + sub;
       raw[r] = make_uint4(0, 0, 0, 0);
-      if (row >= lo && row < hi) raw[r] = *reinterpret_cast<const uint4*>(src + (row - lo) * src_token + 8 * l);
+      if (row >= lo && row < hi) {
+        const uint16_t* at = src + (row - lo) * src_token;
+        if (pair) {
+          const uint2 f = *reinterpret_cast<const uint2*>(at + 4 * l), b = *reinterpret_cast<const uint2*>(at + 4 * LANES + 4 * l);
+          raw[r] = make_uint4(f.x, f.y, b.x, b.y);
+        } else {
+          raw[r] = *reinterpret_cast<const uint4*>(at + 8 * l);
+        }
+      }
     }
   }
 };
-template <int SB, int THREADS, int LANES, bool SPEC>
+// PAIR: the rotation turns the whole head, half apart, and a lane has 4 dimensions of each half.
+template <int SB, int THREADS, int LANES, bool SPEC, bool PAIR = false>
 __device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows, uint8_t* code, int64_t code_token,
                                             uint8_t* scale, int lo, int hi, const AppendArgs& a, const float* bc, const float* bs,
                                             const float* unit, float* red) {
@@ -109,12 +141,31 @@ __device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows
     const int u_step = turned ? half : 0;
     {
       uint4 wr = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);  // ones
-      if (a.spec.norm && a.k_weight != nullptr) wr = *reinterpret_cast<const uint4*>(a.k_weight + 8 * l);
+      if (a.spec.norm && a.k_weight != nullptr) {
+        if (PAIR) {
+          const uint2 f = *reinterpret_cast<const uint2*>(a.k_weight + 4 * l), b = *reinterpret_cast<const uint2*>(a.k_weight + 4 * LANES + 4 * l);
+          wr = make_uint4(f.x, f.y, b.x, b.y);
+        } else {
+          wr = *reinterpret_cast<const uint4*>(a.k_weight + 8 * l);
+        }
+      }
       const uint32_t w4[4] = {wr.x, wr.y, wr.z, wr.w};
       const float sg = l < hl ? -1.f : 1.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = bf16x2_to_f32x2(w4[k]);
-      if (rot > 0) {
+      if (PAIR) {
+        uint64_t cv[2], sv[2];
+        load_quad(cv, bc + (SB / 8 + (sub & 7)) * half + 4 * l);
+        load_quad(sv, bs + (SB / 8 + (sub & 7)) * half + 4 * l);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {  // z = x_k w cos -+ x_(k ^ 2) w' sin, the sign of the front half negative
+          const uint64_t flip = k < 2 ? 0x8000000080000000ull : 0ull;
+          wc[k] = mul2(w[k], cv[k & 1]);
+          ws[k] = mul2(w[k], sv[k & 1]) ^ 0x8000000080000000ull;
+          pc[k] = mul2(w[k ^ 2], cv[k & 1]) ^ flip;
+          ps[k] = mul2(w[k ^ 2], sv[k & 1]) ^ flip;
+        }
+      } else if (rot > 0) {
         uint64_t cv[4], sv[4];
         load_pairs(cv, turned ? bc + (SB / 8 + (sub & 7)) * half + i0 : unit, inter, 0);
         load_pairs(sv, turned ? bs + (SB / 8 + (sub & 7)) * half + i0 : unit + 8, inter, 0);
@@ -144,7 +195,18 @@ __device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows
         root = rsqrtf(fmaf(ss, 1.f / (8 * LANES), a.spec.eps));
       }
       const uint64_t r2 = pack2(root, root);
-      if (rot > 0) {
+      if (PAIR) {
+        uint64_t cu[2], su[2], z[4];
+        load_quad(cu, bc + (row >> 3) * half + 4 * l);
+        load_quad(su, bs + (row >> 3) * half + 4 * l);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint64_t f = fma2(cu[k & 1], wc[k], mul2(su[k & 1], ws[k])), fp = fma2(su[k & 1], pc[k], mul2(cu[k & 1], ps[k]));
+          z[k] = mul2(fma2(x[r][k], f, mul2(x[r][k ^ 2], fp)), r2);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[r][k] = z[k];
+      } else if (rot > 0) {
         uint64_t cu[4], su[4];
         load_pairs(cu, cu_row + (row >> 3) * u_step, inter, 0);
         load_pairs(su, su_row + (row >> 3) * u_step, inter, 0);
@@ -211,7 +273,7 @@ __device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = r * kRowsPerPass + sub;
-    uint2* dst = reinterpret_cast<uint2*>(code + row * code_token + 8 * l);
+    uint8_t* dst = code + row * code_token + (PAIR ? 4 : 8) * l;
     if (row >= lo && row < hi) {
       uint32_t o[4];
 #pragma unroll
@@ -219,9 +281,9 @@ __device__ __forceinline__ void append_head(const Rows<SB, THREADS, LANES>& rows
         const float2 z = unpack2(mul2(x[r][k], inv2));
         o[k] = f32x2_to_e4m3x2(z.x, z.y);
       }
-      *dst = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+      put_codes<PAIR, LANES>(dst, make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16));
     } else if (row < lo && e > e_old) {  // an older row: its codes move down by e - e_old exponents
-      *dst = recode(*dst, exp2_int(max(e_old - e, -60)));
+      put_codes<PAIR, LANES>(dst, recode(get_codes<PAIR, LANES>(dst), exp2_int(max(e_old - e, -60))));
     }
   }
 }
@@ -249,10 +311,11 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) cache8_append_kernel(c
   const int h0 = blockIdx.y * a.heads_per_block, h1 = min(h0 + a.heads_per_block, a.heads[0]);
   const int half = a.spec.rot_dim >> 1, lanes = half > 32 ? 64 : 32;  // threads that share a position's angles
   const float freq = !idx_block && (int)threadIdx.x % lanes < half ? a.spec.inv_freq[threadIdx.x % lanes] : 0.f;
+  const bool pair = a.spec.rot_dim == 128 && !a.spec.interleaved;  // (K's head size is 128)
   Rows<SB, THREADS, 16> next;
   const int kind0 = idx_block ? 2 : 0;
   if (!idx_block || a.idx_dim == 128)  // the first rows do not depend on where they go
-    next.load(a.src[kind0] + tok0 * a.src_token[kind0] + (idx_block ? 0 : h0 * a.src_head[0]), a.src_token[kind0], lo, hi);
+    next.load(a.src[kind0] + tok0 * a.src_token[kind0] + (idx_block ? 0 : h0 * a.src_head[0]), a.src_token[kind0], lo, hi, pair && !idx_block);
   if (start % SB != 0) {
     if (reports) flag_status(a.status, CLSA_DEV_BAD_SCALE_BLOCK);
     return;
@@ -268,7 +331,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) cache8_append_kernel(c
     uint8_t* code = a.code[2] + row0 * a.code_token[2];
     if (a.idx_dim == 64) {
       Rows<SB, THREADS, 8> rows;
-      rows.load(a.src[2] + tok0 * a.src_token[2], a.src_token[2], lo, hi);
+      rows.load(a.src[2] + tok0 * a.src_token[2], a.src_token[2], lo, hi, false);
       append_head<SB, THREADS, 8, false>(rows, code, a.code_token[2], a.scale[2] + block, lo, hi, a, nullptr, nullptr, nullptr, red[0]);
     } else {
       append_head<SB, THREADS, 16, false>(next, code, a.code_token[2], a.scale[2] + block, lo, hi, a, nullptr, nullptr, nullptr, red[0]);
@@ -295,11 +358,13 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) cache8_append_kernel(c
     const Rows<SB, THREADS, 16> rows = next;
     if (i + 1 < count) {
       const int k2 = i + 1 >= h1 - h0, h2 = h0 + i + 1 - (k2 ? h1 - h0 : 0);
-      next.load(a.src[k2] + tok0 * a.src_token[k2] + h2 * a.src_head[k2], a.src_token[k2], lo, hi);
+      next.load(a.src[k2] + tok0 * a.src_token[k2] + h2 * a.src_head[k2], a.src_token[k2], lo, hi, pair && k2 == 0);
     }
     uint8_t* code = a.code[kind] + row0 * a.code_token[kind] + h * a.code_head[kind];
     uint8_t* scale = a.scale[kind] + h * a.scale_head + block;
-    if (kind == 0 && a.has_spec)
+    if (kind == 0 && pair)
+      append_head<SB, THREADS, 16, true, true>(rows, code, a.code_token[kind], scale, lo, hi, a, bc, bs, unit, red[i & 1]);
+    else if (kind == 0 && a.has_spec)
       append_head<SB, THREADS, 16, true>(rows, code, a.code_token[kind], scale, lo, hi, a, bc, bs, unit, red[i & 1]);
     else
       append_head<SB, THREADS, 16, false>(rows, code, a.code_token[kind], scale, lo, hi, a, nullptr, nullptr, nullptr, red[i & 1]);
