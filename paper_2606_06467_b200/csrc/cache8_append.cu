@@ -101,18 +101,23 @@ struct Rows {
   // Zeros for rows that are not new. pair: 4 dimensions of each half of the head per lane instead of 8 consecutive ones.
   __device__ __forceinline__ void load(const uint16_t* src, int64_t src_token, int lo, int hi, bool pair) {
     const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    if (pair) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int row = r * kPerPass + sub;
-      raw[r] = make_uint4(0, 0, 0, 0);
-      if (row >= lo && row < hi) {
-        const uint16_t* at = src + (row - lo) * src_token;
-        if (pair) {
-          const uint2 f = *reinterpret_cast<const uint2*>(at + 4 * l), b = *reinterpret_cast<const uint2*>(at + 4 * LANES + 4 * l);
+      for (int r = 0; r < R; ++r) {
+        const int row = r * kPerPass + sub;
+        const uint16_t* at = src + (row - lo) * src_token + 4 * l;
+        raw[r] = make_uint4(0, 0, 0, 0);
+        if (row >= lo && row < hi) {
+          const uint2 f = *reinterpret_cast<const uint2*>(at), b = *reinterpret_cast<const uint2*>(at + 4 * LANES);
           raw[r] = make_uint4(f.x, f.y, b.x, b.y);
-        } else {
-          raw[r] = *reinterpret_cast<const uint4*>(at + 8 * l);
         }
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int row = r * kPerPass + sub;
+        raw[r] = make_uint4(0, 0, 0, 0);
+        if (row >= lo && row < hi) raw[r] = *reinterpret_cast<const uint4*>(src + (row - lo) * src_token + 8 * l);
       }
     }
   }
@@ -524,7 +529,7 @@ cudaError_t launch_cache8_append(const clsa_params& p, const clsa_cache8& c, con
   // Two heads per block where that still leaves about 400 threads per SM: they share the angles, and the second one's loads are
   // hidden (4096 tokens of 8 heads, 64-row blocks, first version: 15.4 us with one, 14.5 with two, 20.8 with four; 7 x 333 tokens of 4 heads,
   // 16-row blocks, no rotation: 4.9 with one, 5.4 with two).
-  const int threads = c.scale_block <= 32 ? 128 : 256;
+  const int threads = c.scale_block <= 32 ? 128 : c.scale_block == 64 ? 256 : 512;
   a.heads_per_block = bx * ((a.heads[0] + 1) / 2) * threads >= (int64_t)400 * dev.sm_count ? 2 : 1;
   a.head_groups = (a.heads[0] + a.heads_per_block - 1) / a.heads_per_block;
   const unsigned by = (unsigned)(a.head_groups + a.heads[2]);
@@ -532,7 +537,7 @@ cudaError_t launch_cache8_append(const clsa_params& p, const clsa_cache8& c, con
     case 16: return launch<16, 128>(a, (unsigned)bx, by, stream);
     case 32: return launch<32, 128>(a, (unsigned)bx, by, stream);
     case 64: return launch<64, 256>(a, (unsigned)bx, by, stream);
-    default: return launch<128, 256>(a, (unsigned)bx, by, stream);
+    default: return launch<128, 512>(a, (unsigned)bx, by, stream);
   }
 }
 
