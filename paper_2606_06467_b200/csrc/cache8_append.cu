@@ -1,17 +1,18 @@
 // The newest tokens' K, V and K_idx rows into the 8-bit caches: per block of SB cache rows and head, the largest magnitude of
 // the new rows gives the block's power-of-two scale, and each element is rounded once to e4m3.
 //
-// Chunks (T > 1): a block of threads takes one scale block of one sequence and K and V of one or two heads (or K_idx), the rows of
+// Chunks (T > 1): a block of threads takes one scale block of one sequence and K and V of one to four heads (or K_idx), the rows of
 // the next on their way while it works on one: 16 (or, for 64-wide indexer keys, 8) lanes per row with 16 bytes each, all rows of a
 // head in registers between the pass that finds the maximum and the pass that writes the codes, so every element is read once.
 // K's norm and rotation happen on the way in fp32. The angles of the rows are built by the addition theorem: a row's position is
 // begin + 8 u + v, and cosines and sines of SB / 8 + 8 positions, formed once for all the block's K heads, give those of all SB
 // rows; the part of v is folded with the weights once per head, which leaves seven packed operations per pair of dimensions.
 // A scale block that holds older rows is re-coded by the same threads when its exponent grows.
-// 4096 tokens of 8 heads, indexer keys, norm and rotation over all dimensions: 26.7 MB in 13.4 us (the bytes alone would take 4.1;
-// without rotation 8.2, without norm 6.9): bound by instruction issue at 16 warps per SM, which the rows in registers allow
-// (half of the issue slots are used; 80 registers and half as many warps again, other heads per block and K and V in
-// blocks of their own measured the same or slower).
+// 4096 tokens of 8 heads, indexer keys, norm and rotation over all dimensions, 64-row blocks that straddle the tokens' ends:
+// 26.7 MB in 11.3 us (the bytes alone would take 4.1; aligned 10.8, without rotation 9.0, without norm 7.2): a launch, the chain
+// length - page - rows, a barrier per head, and instruction issue at 16 warps per SM, which the rows in registers allow
+// (80 registers and half as many warps again measured the same). A rotation that turns the whole head, half apart, has both
+// partners in one lane (PAIR: 13.4 -> 11.4; other rotations exchange raw words, 13.0).
 // Single tokens (T = 1): half a warp per row, no block barrier; what does not depend on the sequence's length (the row, the
 // weight, the frequencies) is fetched together with it. Bound by a launch and two dependent round trips: 16 sequences of 8 heads 2.8 us.
 #include "cache8.cuh"
@@ -526,11 +527,14 @@ cudaError_t launch_cache8_append(const clsa_params& p, const clsa_cache8& c, con
   }
   a.spans = (p.q_per_seq - 1 + c.scale_block - 1) / c.scale_block + 1;  // scale blocks that T consecutive positions can touch
   const int64_t bx = (int64_t)p.num_seqs * a.spans;
-  // Two heads per block where that still leaves about 400 threads per SM: they share the angles, and the second one's loads are
-  // hidden (4096 tokens of 8 heads, 64-row blocks, first version: 15.4 us with one, 14.5 with two, 20.8 with four; 7 x 333 tokens of 4 heads,
-  // 16-row blocks, no rotation: 4.9 with one, 5.4 with two).
+  // Two or four heads per block where that still leaves about 400 threads per SM: they share the angles, and the later ones' loads
+  // are hidden (4096 tokens of 8 heads: 16-row blocks 12.5 us with two, 11.6 with four; 64-row blocks 15.4 with one, 14.5 with two,
+  // 20.8 with four in an earlier version; 7 x 333 tokens of 4 heads, 16-row blocks, no rotation: 4.9 with one, 5.4 with two). Threads:
+  // four rows each (32-row blocks with two rows each 12.8 us instead of 10.5, 128-row blocks with eight 21.2 instead of 11.5).
   const int threads = c.scale_block <= 32 ? 128 : c.scale_block == 64 ? 256 : 512;
-  a.heads_per_block = bx * ((a.heads[0] + 1) / 2) * threads >= (int64_t)400 * dev.sm_count ? 2 : 1;
+  a.heads_per_block = 1;
+  while (a.heads_per_block < 4 && bx * ((a.heads[0] + 2 * a.heads_per_block - 1) / (2 * a.heads_per_block)) * threads >= (int64_t)400 * dev.sm_count)
+    a.heads_per_block *= 2;
   a.head_groups = (a.heads[0] + a.heads_per_block - 1) / a.heads_per_block;
   const unsigned by = (unsigned)(a.head_groups + a.heads[2]);
   switch (c.scale_block) {

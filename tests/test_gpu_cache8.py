@@ -247,6 +247,17 @@ def test_append_with_norm_and_rotation(lens, T, block, page, rot, inter, norm):
     run_append(c, 2, dict(norm=norm, interleaved=inter, inv_freq=freq), randn(gen(4), 128) if norm else None, fused=True)
 
 
+@pytest.mark.parametrize("block", [16, 64, 128])
+@pytest.mark.parametrize("rot,inter", [(128, 0), (112, 0), (128, 1)])
+def test_append_several_heads_per_block(block, rot, inter):
+    """Enough scale blocks for several heads per block of threads, a head count that they do not divide, rows on both sides of a
+    block's ends, older rows in the first blocks: whole-head rotations and others."""
+    c = Cache([1600, 1513, 2000], 1500, 7, 64, block, 0, seed=block)
+    c.params()
+    freq = (10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)).float().to(DEV)
+    run_append(c, 6, dict(norm=1, interleaved=inter, inv_freq=freq), randn(gen(4), 128), fused=True)
+
+
 def test_append_token_by_token_grows_its_blocks():
     """A sequence fed one token at a time, magnitudes rising and falling by powers of ten: every step equal to the reference
     that carries the state, re-coded rows included."""
