@@ -30,15 +30,19 @@ struct NormRopeArgs {
   int num_tokens, parts, part_heads;  // warps per token, heads of each
 };
 
-// DENSE: heads lie head_dim apart, in and out (strides are immediates then). PAIR: all dimensions are turned, half apart; a lane
-// has 4 dimensions of each half then, 8 bytes apiece, and the partner of each.
-template <int LANES, bool DENSE, bool PAIR>
+// DENSE: heads lie head_dim apart, in and out (strides are immediates then). PAIR: the pairs lie half the turned dimensions apart,
+// and a lane of those has 4 dimensions of each half, 8 bytes apiece, and so the partner of each; ALL: every dimension is turned.
+template <int LANES, bool DENSE, bool PAIR, bool ALL>
 __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
   constexpr int kGroups = 32 / LANES;  // heads of a pass
   __shared__ __align__(16) float turns[kThreads / 32][2][LANES * 4];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LANES, group = lane / LANES;
   const uint32_t item = blockIdx.x * (kThreads / 32) + warp;
+  const int rot = a.spec.rot_dim;
+  const bool turned = ALL || 8 * l < rot;
+  const int at0 = PAIR && turned ? 4 * l : 8 * l;                                // this lane's first quad of a head
+  const int apart = !PAIR || !turned ? 4 : ALL ? 4 * LANES : rot >> 1;           // and its second, behind it
   const uint32_t token = item / (uint32_t)a.parts;
   if (token >= (uint32_t)a.num_tokens) return;
   const int part0 = (int)(item - token * a.parts) * a.part_heads;
@@ -53,14 +57,14 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
     const int before = side ? a.heads[0] : 0;
     const int lo = max(part0 - before, 0);
     left = min(part0 + a.part_heads - before, a.heads[side]) - lo;
-    in = a.in[side] + token * a.in_token[side] + (lo + group) * a.in_head[side] + (PAIR ? 4 : 8) * l;
-    out = a.out[side] + token * a.out_token[side] + (lo + group) * a.out_head[side] + (PAIR ? 4 : 8) * l;
+    in = a.in[side] + token * a.in_token[side] + (lo + group) * a.in_head[side] + at0;
+    out = a.out[side] + token * a.out_token[side] + (lo + group) * a.out_head[side] + at0;
     in_step = DENSE ? 256 : kGroups * a.in_head[side];
     out_step = DENSE ? 256 : kGroups * a.out_head[side];
   };
-  auto load8 = [](const uint16_t* at) -> uint4 {
+  auto load8 = [&](const uint16_t* at) -> uint4 {
     if (!PAIR) return *reinterpret_cast<const uint4*>(at);
-    const uint2 lo = *reinterpret_cast<const uint2*>(at), hi = *reinterpret_cast<const uint2*>(at + 4 * LANES);
+    const uint2 lo = *reinterpret_cast<const uint2*>(at), hi = *reinterpret_cast<const uint2*>(at + apart);
     return make_uint4(lo.x, lo.y, hi.x, hi.y);
   };
   auto load = [&]() {
@@ -75,7 +79,6 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
   if (left <= 0) begin(side = 1);
   load();  // under way while the angles are formed
   if (pos < 0) return;  // padding
-  const int rot = a.spec.rot_dim;
   float* tc = turns[warp][0];
   float* ts = turns[warp][1];
   if (rot > 0) {
@@ -84,7 +87,7 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
   }
   // The partner of this lane's dimensions in a half-split rotation sits in lane `partner` of its group.
   const int hl = rot >> 4;
-  const bool turned = 8 * l < rot, inter = a.spec.interleaved, norm = a.spec.norm;
+  const bool inter = a.spec.interleaved, norm = a.spec.norm;
   const int partner = l < hl ? l + hl : (l < 2 * hl ? l - hl : l);
   const float sign = l < hl ? -1.f : 1.f;
   const float eps = a.spec.eps;
@@ -93,10 +96,14 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
     uint64_t A[4], B[4];
     {
       uint4 wr = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);  // ones
-      if (norm && a.weight[side] != nullptr) wr = load8(a.weight[side] + (PAIR ? 4 : 8) * l);
+      if (norm && a.weight[side] != nullptr) wr = load8(a.weight[side] + at0);
       const uint32_t w4[4] = {wr.x, wr.y, wr.z, wr.w};
       if (PAIR) {
-        const float4 c = *reinterpret_cast<const float4*>(tc + 4 * l), s = *reinterpret_cast<const float4*>(ts + 4 * l);
+        float4 c = make_float4(1.f, 1.f, 1.f, 1.f), s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (turned) {
+          c = *reinterpret_cast<const float4*>(tc + 4 * l);
+          s = *reinterpret_cast<const float4*>(ts + 4 * l);
+        }
         const uint64_t c2[2] = {pack2(c.x, c.y), pack2(c.z, c.w)}, s2[2] = {pack2(s.x, s.y), pack2(s.z, s.w)};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -133,7 +140,7 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
       for (int k = 0; k < 4; ++k) {
         uint64_t other;
         if (PAIR) {
-          other = x[k ^ 2];
+          other = turned ? x[k ^ 2] : 0ull;  // (as below)
         } else {
           const uint32_t p = inter ? __byte_perm(in4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, in4[k], partner, LANES);
           other = bf16x2_to_f32x2(turned ? p : 0u);  // (an infinity times a zero sine is none)
@@ -152,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
         if (group + k * kGroups < left) {
           if (PAIR) {
             *reinterpret_cast<uint2*>(out + k * out_step) = make_uint2(z.x, z.y);
-            *reinterpret_cast<uint2*>(out + k * out_step + 4 * LANES) = make_uint2(z.z, z.w);
+            *reinterpret_cast<uint2*>(out + k * out_step + apart) = make_uint2(z.z, z.w);
           } else {
             *reinterpret_cast<uint4*>(out + k * out_step) = z;
           }
@@ -185,9 +192,10 @@ void launch(NormRopeArgs& a, const DeviceInfo& dev, cudaStream_t stream) {
   const unsigned blocks = (unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32));
   bool dense = true;
   for (int i = 0; i < 2; ++i) dense = dense && (a.heads[i] <= 1 || (a.in_head[i] == 8 * LANES && a.out_head[i] == 8 * LANES));
-  const bool pair = a.spec.rot_dim == 8 * LANES && !a.spec.interleaved;
-  void (*kernel)(const NormRopeArgs) = dense ? (pair ? norm_rope_kernel<LANES, true, true> : norm_rope_kernel<LANES, true, false>)
-                                             : (pair ? norm_rope_kernel<LANES, false, true> : norm_rope_kernel<LANES, false, false>);
+  const bool pair = a.spec.rot_dim > 0 && !a.spec.interleaved, all = pair && a.spec.rot_dim == 8 * LANES;
+  void (*kernel)(const NormRopeArgs) =
+      dense ? (all ? norm_rope_kernel<LANES, true, true, true> : pair ? norm_rope_kernel<LANES, true, true, false> : norm_rope_kernel<LANES, true, false, false>)
+            : (all ? norm_rope_kernel<LANES, false, true, true> : pair ? norm_rope_kernel<LANES, false, true, false> : norm_rope_kernel<LANES, false, false, false>);
   kernel<<<blocks, kThreads, 0, stream>>>(a);
 }
 
