@@ -2,8 +2,8 @@
 // bound by HBM for a prefill chunk, by one launch and one memory round trip for a decode step).
 //
 // A head of D dimensions is held by D / 8 lanes of a warp, 16 bytes each; the sum of squares is a butterfly over those
-// lanes, the partner of a half-split rotation comes by shuffles of the raw words, or, where it turns the whole head, sits in the same lane. A warp takes heads of one token, 32 / (D / 8) in
-// a pass, four passes' loads and then their work together. The token's rot_dim / 2 angles (64-bit product and reduction, 32-bit
+// lanes, the partner of a half-split rotation sits in the same lane (a lane of the turned dimensions has 4 of each half). A warp
+// takes heads of one token, 32 / (D / 8) in a pass, four passes' loads and then their work together. The token's rot_dim / 2 angles (64-bit product and reduction, 32-bit
 // functions) are formed once per warp and folded with the weights into two factors per dimension, so that a dimension costs a
 // product, a multiply-add and a scaling, two dimensions per instruction. Warps are independent of one another. How many of a
 // token's heads a warp takes follows from the number of tokens: few tokens are spread over many warps (each forms the angles
@@ -32,6 +32,7 @@ struct NormRopeArgs {
 
 // DENSE: heads lie head_dim apart, in and out (strides are immediates then). PAIR: the pairs lie half the turned dimensions apart,
 // and a lane of those has 4 dimensions of each half, 8 bytes apiece, and so the partner of each; ALL: every dimension is turned.
+// Not PAIR: partners are neighbours, or nothing is turned.
 template <int LANES, bool DENSE, bool PAIR, bool ALL>
 __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
   constexpr int kGroups = 32 / LANES;  // heads of a pass
@@ -85,11 +86,7 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
     for (int i = lane; i < rot / 2; i += 32) turn_of(pos, a.spec.inv_freq[i], a.spec.rot_scale, &tc[i], &ts[i]);
     __syncwarp();
   }
-  // The partner of this lane's dimensions in a half-split rotation sits in lane `partner` of its group.
-  const int hl = rot >> 4;
-  const bool inter = a.spec.interleaved, norm = a.spec.norm;
-  const int partner = l < hl ? l + hl : (l < 2 * hl ? l - hl : l);
-  const float sign = l < hl ? -1.f : 1.f;
+  const bool norm = a.spec.norm;
   const float eps = a.spec.eps;
   while (true) {
     // z_i = r (x_i A_i + x_partner B_i) with A = w cos, B = -+ w_partner sin and r the root of the mean square's inverse
@@ -112,13 +109,13 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
         }
       }
       float c[8], s[8];
-      if (!PAIR && rot > 0) load_turns(c, s, tc, ts, rot, inter, l);
+      if (!PAIR && rot > 0) load_turns(c, s, tc, ts, rot, true, l);
 #pragma unroll
       for (int k = 0; k < 4 && !PAIR; ++k) {
         const uint64_t w = bf16x2_to_f32x2(w4[k]);
-        const uint32_t p = inter ? __byte_perm(w4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, w4[k], partner, LANES);
+        const uint32_t p = __byte_perm(w4[k], 0u, 0x1032);  // partners are neighbours
         A[k] = turned ? mul2(w, pack2(c[2 * k], c[2 * k + 1])) : w;
-        B[k] = turned ? mul2(bf16x2_to_f32x2(p), inter ? pack2(-s[2 * k], s[2 * k + 1]) : pack2(sign * s[2 * k], sign * s[2 * k + 1])) : 0ull;
+        B[k] = turned ? mul2(bf16x2_to_f32x2(p), pack2(-s[2 * k], s[2 * k + 1])) : 0ull;
       }
     }
     auto one = [&](const uint4& raw) -> uint4 {
@@ -138,13 +135,8 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
       uint32_t o[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        uint64_t other;
-        if (PAIR) {
-          other = turned ? x[k ^ 2] : 0ull;  // (as below)
-        } else {
-          const uint32_t p = inter ? __byte_perm(in4[k], 0u, 0x1032) : __shfl_sync(0xffffffffu, in4[k], partner, LANES);
-          other = bf16x2_to_f32x2(turned ? p : 0u);  // (an infinity times a zero sine is none)
-        }
+        uint64_t other = PAIR ? x[k ^ 2] : bf16x2_to_f32x2(__byte_perm(in4[k], 0u, 0x1032));
+        if (!turned) other = 0ull;  // (an infinity times a zero sine is none)
         const float2 z = unpack2(mul2(fma2(x[k], A[k], mul2(other, B[k])), r2));
         o[k] = pack_bf16x2(z.x, z.y);
       }
