@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
   const uint32_t step = gridDim.x * kWarps;
   int b = -1, s = 0, n = 0, s_end = 0;
   const int32_t* table = nullptr;
-  int start = 0;
+  int64_t start = 0;  // (start + position may pass 32 bits where max_seq_len is a loose bound)
   int page[M];
   const bool one_run = a.block_table == nullptr || (1 << a.block_shift) >= kTileKeys;  // a tile's rows follow one another
   auto next_tile = [&]() {  // b = -1 behind the last one
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
       s_end = min(n, s + a.chunk_keys);
       if (s < s_end) {
         if (a.block_table != nullptr) table = a.block_table + (int64_t)b * a.max_blocks;
-        else start = (int)max((int64_t)-a.max_seq_len - 16, min(a.seq_start[b], (int64_t)0x7fffffff - a.max_seq_len));  // rows outside stay outside
+        else start = a.seq_start[b];
       }
     }
     if (table != nullptr) {
@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
         if (table != nullptr) {
           if ((uint32_t)pg < a.page_limit) row = (pg << a.block_shift) + (pos & ((1 << a.block_shift) - 1));
         } else {
-          row = start + pos;
+          const int64_t r = start + pos;
+          if (r >= 0 && r < a.num_rows) row = (int)r;
         }
         const int have = row >= 0 && row < a.num_rows ? min(want, a.num_rows - row) : 0;
         if (have < want && lane == 0) flag_status(a.status, CLSA_DEV_BAD_INDEX);
