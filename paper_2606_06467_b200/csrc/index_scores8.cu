@@ -139,11 +139,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
 #pragma unroll
         for (int m = 0; m < M; ++m) rows[m] = row + 16 * m;
       } else {
+        const bool whole = one_run && (table != nullptr || row >= 0);  // (a tile that begins before row 0 may end behind it)
 #pragma unroll
         for (int m = 0; m < M; ++m) {
           const int pos = s + 16 * m, want = max(min(n - pos, 16), 0);
-          const int in = one_run ? max(min(have - 16 * m, want), 0) : locate(page[m], pos, want, row);
-          const int row_m = one_run ? row + 16 * m : row;
+          const int in = whole ? max(min(have - 16 * m, want), 0) : locate(page[m], pos, want, row);
+          const int row_m = whole ? row + 16 * m : row;
           if (in > 0) rows[m] = row_m;
           const uint8_t* src = lane_keys + (in > 0 ? row_m : 0) * a.tok_stride;
 #pragma unroll

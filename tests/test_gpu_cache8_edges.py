@@ -36,3 +36,43 @@ def test_index_scores_of_a_far_start_under_a_loose_length_bound():
     want, mag = ref.scores(f64(q[0]), vals)
     assert (np.abs(s[0, 0, :n].cpu().double().numpy() - want[0]) <= 2.0 ** -16 * mag[0]).all()
     assert clsa.clsa_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("T", [1, 2, 40])
+@pytest.mark.parametrize("d_idx", [64, 128])
+@pytest.mark.parametrize("first", [-16, -48, -80])
+def test_index_scores_of_rows_outside_the_row_space(T, d_idx, first):
+    """A sequence that begins before row 0 and one that ends behind the last row: the rows that exist are scored, the others are
+    rows of zeros, and both are flagged; without pages."""
+    c = Cache([150, 150, 150], T, 1, d_idx, 16, 0, seed=T + d_idx)
+    c.params()
+    c.start[0], c.start[1] = first, c.rows - 16 * 5
+    q = randn(gen(T), 3, T, d_idx)
+    s = run_scores(c, q, 0)
+    assert c.status() == clsa.CLSA_DEV_BAD_INDEX
+    code, sc = c.host()[2]
+    vals = ref.values(code, sc, 16)[:, 0]
+    for b in range(3):
+        rows = c.row(b, np.arange(150))
+        there = (rows >= 0) & (rows < c.rows)
+        want, mag = ref.scores(f64(q[b]), np.where(there[:, None], vals[np.clip(rows, 0, c.rows - 1)], 0.0))
+        assert (np.abs(s[b, :, :150].cpu().double().numpy() - want) <= 2.0 ** -16 * mag).all(), b
+
+
+def test_sparse_attn_of_rows_outside_the_row_space():
+    """The same starts for attention: entries whose rows do not exist are left out and flagged."""
+    c = Cache([150, 150, 150], 1, 2, 64, 16, 0, seed=3)
+    c.params(hq=8, top_k=60)
+    c.start[0], c.start[1] = -48, c.rows - 80
+    q = randn(gen(2), 3, 1, 8, 128)
+    idx, cnt = make_index(c, 60, 0, 1)
+    out, lse = run_attn(c, q, idx, cnt)
+    assert c.status() == clsa.CLSA_DEV_BAD_INDEX
+    i2, c2 = torch.full_like(idx, -1), cnt.clone()
+    for b in range(3):
+        mine = idx[b, 0, :int(cnt[b, 0])].cpu().numpy()
+        rows = c.row(b, mine)
+        mine = mine[(rows >= 0) & (rows < c.rows)]
+        i2[b, 0, :len(mine)], c2[b, 0] = torch.from_numpy(mine), len(mine)
+    assert int(c2[0, 0]) < 60 and int(c2[1, 0]) < 60 and int(c2[2, 0]) == 60
+    check_attn(c, 8, q, i2, c2, out, lse)
