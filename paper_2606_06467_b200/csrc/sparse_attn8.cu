@@ -15,10 +15,11 @@
 // the weights of the second 16 tokens where the others take those of the first, and the second product keeps the two halves of
 // the sum in the two column halves until the end -- half the logits and weights per lane for a few selects.
 //
-// In the log2 domain a query head keeps two running references: m near the largest x_s + ev for the numerators' weights
-// 2^(x_s + ev - m), and mx near the largest x_s for the denominators 2^(x_s - mx), so that neither underflows however far apart
-// the blocks' scales lie; the difference of the two is applied to the finished quotient. References move only when a
-// weight would leave its range (one vote per stage): a stage that moves none needs no reduction over its tokens.
+// In the log2 domain a query head keeps two running references: mx near the largest x_s for the denominators 2^(x_s - mx), and m
+// near the largest x_s - mx + ev for the numerators' weights 2^(x_s - mx + ev - m), so that neither underflows however far apart
+// the blocks' scales lie; 2^m is applied to the finished quotient. ev meets the difference x_s - mx, which is small where it counts,
+// never x_s itself, whose fp32 rounding would swallow it (logits of 1e7: V rows off by whole powers of two). References move only
+// when a weight would leave its range (one vote per stage): a stage that moves none needs no reduction over its tokens.
 //
 // The work is a flat list of 32-token stages, unit = (KV head, query row), heads outermost, so that a prefill chunk's launch
 // goes over one head's part of the cache (which fits in L2) before the next. Warp w of W takes a contiguous span of the list
@@ -398,8 +399,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
           for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[nt][k][i] += s2[nt][k][i];
-        // x of the lane's tokens and two heads per tile: x[..][2 t + head]
-        float x[NT][2 * NX], xe[NT][2 * NX], top[NT][2], tope[NT][2];
+        // x of the lane's tokens and two heads per tile: x[..][2 t + head]; y = x - mx, ye = y + V's exponent
+        float x[NT][2 * NX], y[NT][2 * NX], ye[NT][2 * NX];
         bool move = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -408,9 +409,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
             float d[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) d[h] = FOLD ? (upper ? s[nt][1][2 * t + h] : s[nt][0][2 * t + h]) : s[nt][t >> 1][2 * (t & 1) + h];
-            const float2 y = unpack2(mul2(mul2(pack2(d[0], d[1]), pack2(sc[t].x, sc[t].x)), pack2(qf[nt][0], qf[nt][1])));
-            x[nt][2 * t] = y.x;
-            x[nt][2 * t + 1] = y.y;
+            const float2 z = unpack2(mul2(mul2(pack2(d[0], d[1]), pack2(sc[t].x, sc[t].x)), pack2(qf[nt][0], qf[nt][1])));
+            x[nt][2 * t] = z.x;
+            x[nt][2 * t + 1] = z.y;
           }
         if (okmask != 0xffffffffu) {
 #pragma unroll
@@ -418,55 +419,65 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 #pragma unroll
             for (int i = 0; i < 2 * NX; ++i) x[nt][i] = (okmask >> (my_tok + (i & 2) + 4 * (i & 4))) & 1u ? x[nt][i] : -INFINITY;
         }
+        auto relate = [&](int nt) {
+#pragma unroll
+          for (int t = 0; t < NX; ++t) {
+            const uint64_t d = add2(pack2(x[nt][2 * t], x[nt][2 * t + 1]), pack2(-mx[nt][0], -mx[nt][1]));
+            const float2 z = unpack2(d), ze = unpack2(add2(d, pack2(sc[t].y, sc[t].y)));
+            y[nt][2 * t] = z.x;
+            y[nt][2 * t + 1] = z.y;
+            ye[nt][2 * t] = ze.x;
+            ye[nt][2 * t + 1] = ze.y;
+          }
+        };
+        auto largest = [&](const float (&v)[2 * NX], int h) {
+          float r = v[h];
+#pragma unroll
+          for (int t = 1; t < NX; ++t) r = fmaxf(r, v[2 * t + h]);
+          return r;
+        };
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+          relate(nt);
 #pragma unroll
-          for (int t = 0; t < NX; ++t) {  // with V's exponent
-            const float2 y = unpack2(add2(pack2(x[nt][2 * t], x[nt][2 * t + 1]), pack2(sc[t].y, sc[t].y)));
-            xe[nt][2 * t] = y.x;
-            xe[nt][2 * t + 1] = y.y;
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            top[nt][h] = x[nt][h];
-            tope[nt][h] = xe[nt][h];
-#pragma unroll
-            for (int t = 1; t < NX; ++t) {
-              top[nt][h] = fmaxf(top[nt][h], x[nt][2 * t + h]);
-              tope[nt][h] = fmaxf(tope[nt][h], xe[nt][2 * t + h]);
-            }
-            move = move || top[nt][h] > mx[nt][h] + kLazy || tope[nt][h] > m[nt][h] + kLazy;
-          }
+          for (int h = 0; h < 2; ++h) move = move || largest(y[nt], h) > kLazy || largest(ye[nt], h) > m[nt][h] + kLazy;
         }
         if (__any_sync(0xffffffffu, move)) {  // some head's references have to move: to the largest seen so far
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt) {
+            float drop[2];  // what every difference from mx loses
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+              float top = largest(x[nt], h);
 #pragma unroll
-              for (int d = FOLD ? 2 : 4; d <= 16; d <<= 1) {
-                top[nt][h] = fmaxf(top[nt][h], __shfl_xor_sync(0xffffffffu, top[nt][h], d));
-                tope[nt][h] = fmaxf(tope[nt][h], __shfl_xor_sync(0xffffffffu, tope[nt][h], d));
-              }
-              const float mxn = fmaxf(mx[nt][h], top[nt][h]), mn = fmaxf(m[nt][h], tope[nt][h]);
-              l[nt][h] *= fast_exp2(mx[nt][h] - mxn);
-              const float alpha = fast_exp2(m[nt][h] - mn);
+              for (int d = FOLD ? 2 : 4; d <= 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              const float mxn = fmaxf(mx[nt][h], top);
+              drop[h] = mx[nt][h] - mxn;
+              l[nt][h] *= fast_exp2(drop[h]);
               mx[nt][h] = mxn;
+            }
+            relate(nt);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float top = largest(ye[nt], h);
+#pragma unroll
+              for (int d = FOLD ? 2 : 4; d <= 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              const float mo = m[nt][h] + drop[h], mn = fmaxf(mo, top), alpha = fast_exp2(mo - mn);
               m[nt][h] = mn;
 #pragma unroll
               for (int c = 0; c < 8; ++c) { o[nt][c][h] *= alpha; o[nt][c][h + 2] *= alpha; }
             }
+          }
         }
         uint32_t pb[NT][4];  // weights as the second product's columns: tokens 4 (lane & 3) + {0, 1}, {2, 3}, then those + 16
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
           for (int t = 0; t < NX; ++t) {
-            const float2 d = unpack2(add2(pack2(x[nt][2 * t], x[nt][2 * t + 1]), pack2(-mx[nt][0], -mx[nt][1])));
-            const float2 w = unpack2(add2(pack2(xe[nt][2 * t], xe[nt][2 * t + 1]), pack2(-m[nt][0], -m[nt][1])));
-            const float2 y = unpack2(add2(pack2(l[nt][0], l[nt][1]), pack2(fast_exp2(d.x), fast_exp2(d.y))));
-            l[nt][0] = y.x;
-            l[nt][1] = y.y;
+            const float2 w = unpack2(add2(pack2(ye[nt][2 * t], ye[nt][2 * t + 1]), pack2(-m[nt][0], -m[nt][1])));
+            const float2 z = unpack2(add2(pack2(l[nt][0], l[nt][1]), pack2(fast_exp2(y[nt][2 * t]), fast_exp2(y[nt][2 * t + 1]))));
+            l[nt][0] = z.x;
+            l[nt][1] = z.y;
             pb[nt][t] = movmatrix_trans(pack_f16x2(fast_exp2(w.x), fast_exp2(w.y)));
           }
           if (FOLD) {  // columns 0 .. 3 have the weights of the stage's first half, 4 .. 7 those of its second
@@ -526,9 +537,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       for (int h = 0; h < 2; ++h) {
         const int head = nt * 8 + hcol + h;
         if (head < G && !upper) {
-          // a whole unit is normalised here; the references' difference is applied in two halves: its square may not be a float
+          // a whole unit is normalised here; 2^m is applied in two halves: it may not be a float
           const float inv = whole ? (l[nt][h] != 0.f ? 1.f / l[nt][h] : 0.f) : 1.f;
-          const float half = whole && l[nt][h] != 0.f ? fast_exp2(0.5f * (m[nt][h] - mx[nt][h])) : 1.f;
+          const float half = whole && l[nt][h] != 0.f ? fast_exp2(0.5f * m[nt][h]) : 1.f;
           float* dst = mypart + head * kPartialStride + rowq;
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
@@ -573,13 +584,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float L = 0.f, MX = kNone, M = kNone;
   auto fold = [&](float4 ml, int count, auto fetch) {
-    float mn = fmaxf(M, ml.z), xn = fmaxf(MX, ml.x);
+    float xn = fmaxf(MX, ml.x);
 #pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) {
-      mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
-      xn = fmaxf(xn, __shfl_xor_sync(0xffffffffu, xn, d));
-    }
-    const float sn = fast_exp2(ml.z - mn), so = fast_exp2(M - mn);
+    for (int d = 16; d >= 1; d >>= 1) xn = fmaxf(xn, __shfl_xor_sync(0xffffffffu, xn, d));
+    const float mnew = (ml.x - xn) + ml.z, mold = (MX - xn) + M;  // references to x - xn + ev
+    float mn = fmaxf(mold, mnew);
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
+    const float sn = fast_exp2(mnew - mn), so = fast_exp2(mold - mn);
     float sum = fast_exp2(ml.x - xn) * ml.y;
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -647,7 +659,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
                [&](int i) { return __ldcg(block_record(b0 + i) + lane); });
       }
       if (L != 0.f) {
-        const float inv = 1.f / L, half = fast_exp2(0.5f * (M - MX));
+        const float inv = 1.f / L, half = fast_exp2(0.5f * M);
         acc.x = acc.x * inv * half * half; acc.y = acc.y * inv * half * half;
         acc.z = acc.z * inv * half * half; acc.w = acc.w * inv * half * half;
       }

@@ -76,3 +76,38 @@ def test_sparse_attn_of_rows_outside_the_row_space():
         i2[b, 0, :len(mine)], c2[b, 0] = torch.from_numpy(mine), len(mine)
     assert int(c2[0, 0]) < 60 and int(c2[1, 0]) < 60 and int(c2[2, 0]) == 60
     check_attn(c, 8, q, i2, c2, out, lse)
+
+
+@pytest.mark.parametrize("heads,top_k", [(2, 300), (1, 2048)])
+@pytest.mark.parametrize("power", [0, 8, 16, 24, 60, 100])
+def test_sparse_attn_one_token_takes_all(power, heads, top_k):
+    """Logits of any size, one far above the rest: the output is that token's V row however large the logits are. (One weight
+    is left: it and its sum differ by the weight's f16 rounding and the exponential's and the products' fp32 ones, 2^-10 at most,
+    then one bf16 rounding.)"""
+    c = Cache([2500, 2500], 1, heads, 64, 16, 0, seed=8, exps=(100, 140))
+    c.params(hq=heads, top_k=top_k)
+    c.ks.fill_(124)
+    q = randn(gen(2), 2, 1, heads, 128) * 4
+    idx, cnt = make_index(c, top_k, 0, 1)
+    kf = c.k.view(torch.float8_e4m3fn)
+    best = []
+    for b in range(2):
+        s = int(idx[b, 0, (77, 200)[b]])
+        row = int(c.row(b, s))
+        kf[row].copy_((q[b, 0].float() * 40).clamp(-448, 448).to(torch.float8_e4m3fn))
+        best.append(row)
+    q *= 2.0 ** power
+    out, lse = run_attn(c, q, idx, cnt)
+    (kc, ks), (vc, vs), _ = c.host()
+    kv, vv = ref.values(kc, ks, 16), ref.values(vc, vs, 16)
+    for b in range(2):
+        rows = c.row(b, idx[b, 0, :top_k].cpu().numpy())
+        for h in range(heads):
+            x = kv[rows, h] @ f64(q[b, 0, h]) * 128 ** -0.5
+            mag = 2.0 ** -16 * (np.abs(kv[rows, h]) @ np.abs(f64(q[b, 0, h]))).max() * 128 ** -0.5
+            order = np.argsort(x)
+            assert rows[order[-1]] == best[b] and x[order[-1]] - x[order[-2]] > 170 + 2 * mag  # 2^40 of V's scales and 2^-40 of weight are left
+            v = vv[best[b], h]
+            got = f64(out[b, 0, h])
+            assert (np.abs(got - v) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(v) + 2.0 ** -149).all(), (b, h, float(np.nanmax(np.abs(got / np.where(v == 0, 1, v) - 1))))
+            assert abs(float(lse[b, 0, h]) - x[order[-1]]) <= mag + 2.0 ** -20 * (abs(x[order[-1]]) + 128)
