@@ -45,7 +45,7 @@ constexpr int kTok = 32;                  // tokens per stage
 constexpr int kStage8Bytes = kTok * 256;  // K rows, then V rows, 128 bytes each
 constexpr int kMaxGroup = 16;
 constexpr float kLazy = 8.f;              // a weight may exceed its reference by 2^8 before the reference moves
-constexpr float kNone = -1e30f;           // a reference before the first token: 2^(x - kNone) of a masked x = -inf is 0, not NaN
+constexpr float kNone = -3.4028234663852886e38f;  // a reference before the first token, below every logit: 2^(x - kNone) of a masked x = -inf is 0, not NaN
 
 struct Attn8Args {
   const uint16_t* q;

@@ -111,3 +111,19 @@ def test_sparse_attn_one_token_takes_all(power, heads, top_k):
             got = f64(out[b, 0, h])
             assert (np.abs(got - v) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(v) + 2.0 ** -149).all(), (b, h, float(np.nanmax(np.abs(got / np.where(v == 0, 1, v) - 1))))
             assert abs(float(lse[b, 0, h]) - x[order[-1]]) <= mag + 2.0 ** -20 * (abs(x[order[-1]]) + 128)
+
+
+def test_sparse_attn_logits_far_below_zero():
+    """A selected token whose logit lies far below -1e30 still is the one that there is."""
+    c = Cache([64], 1, 1, 64, 16, 0, seed=8)
+    c.params(hq=1, top_k=1)
+    q = randn(gen(2), 1, 1, 1, 128) * 2.0 ** 100
+    row = int(c.row(0, 9))
+    c.k.view(torch.float8_e4m3fn)[row].copy_((q[0, 0].float() * -(2.0 ** -94)).clamp(-448, 448).to(torch.float8_e4m3fn))
+    idx, cnt = torch.full((1, 1, 1), 9, dtype=torch.int32, device=DEV), torch.ones((1, 1), dtype=torch.int32, device=DEV)
+    out, lse = run_attn(c, q, idx, cnt)
+    assert float(lse) < -1e30
+    check_attn(c, 1, q, idx, cnt, out, None)
+    (kc, ks), (vc, vs), _ = c.host()
+    v = ref.values(vc, vs, 16)[row, 0]
+    assert (np.abs(f64(out[0, 0, 0]) - v) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(v)).all()
