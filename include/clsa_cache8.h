@@ -119,7 +119,8 @@ CLSA_API clsa_status clsa_index_scores8(const clsa_params* p, const clsa_cache8*
                                         int64_t score_stride, void* workspace, size_t workspace_bytes, clsa_stream stream);
 
 /* clsa_sparse_attn over an 8-bit cache: its arguments and results (bf16 outputs, optional fp32 log-sum-exp, zeros and -inf for
- * a query with count 0). T >= 1. p->sm_scale finite and > 0 as there.
+ * a query with count 0). T >= 1. p->sm_scale finite and > 0 as there. Logits may have any size that is a float, for queries of
+ * magnitudes below 2^118 / sm_scale (beyond that a query counts as less than it is).
  *   hints  NULL, or as for clsa_sparse_attn_hinted with shared_gpu == 0 (CLSA_ERR_UNSUPPORTED otherwise)
  * Results do not depend on hints beyond rounding, and are the same from call to call. */
 CLSA_API clsa_status clsa_sparse_attn8(const clsa_params* p, const clsa_cache8* c, const void* q, const int32_t* idx,

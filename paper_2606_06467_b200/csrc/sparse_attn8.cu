@@ -46,6 +46,10 @@ constexpr int kStage8Bytes = kTok * 256;  // K rows, then V rows, 128 bytes each
 constexpr int kMaxGroup = 16;
 constexpr float kLazy = 8.f;              // a weight may exceed its reference by 2^8 before the reference moves
 constexpr float kNone = -3.4028234663852886e38f;  // a reference before the first token, below every logit: 2^(x - kNone) of a masked x = -inf is 0, not NaN
+// A finished product d of codes and query is at most 128 * 448 * 2^14 < 2^30 in magnitude and meets 2^ek first: of that factor 2^22
+// is held back for the query's, so that d 2^(ek - 22) is finite for every ek (120 at most) and d's last bits stay above the smallest
+// float (ek -100, d 2^-27: 2^-149). The query's factor is a float up to |q| sm_scale < 2^118.
+constexpr int kHeldBack = 22;
 
 struct Attn8Args {
   const uint16_t* q;
@@ -124,7 +128,7 @@ __device__ __forceinline__ void ldmatrix_b8_x2_trans(uint32_t (&r)[4], uint32_t 
 template <int WARPS, int STAGES>
 struct Shape {
   static constexpr int kRing = STAGES * kStage8Bytes;
-  static constexpr int kScale = STAGES * kTok * 8;  // per token: 2^ek, ev
+  static constexpr int kScale = STAGES * kTok * 8;  // per token: 2^(ek - kHeldBack), ev
   static constexpr size_t kSmem = (size_t)WARPS * (kRing + kScale + STAGES * 4) + WARPS * (sizeof(int2) + sizeof(int2));
 };
 
@@ -259,7 +263,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
       const uint32_t pos_span = (uint32_t)(pos_hi - pos_lo);
       auto load_blk = [&](int raw) -> int { return PAGED && (uint32_t)raw < (uint32_t)n ? __ldg(table + (raw >> a.block_shift)) : -1; };
       auto settle = [&](int buf, int kb, int vb) {  // the scale bytes of stage i into shared memory
-        scales[buf * kTok + lane] = make_float2(exp2_int(scale_exponent(kb)), (float)scale_exponent(vb));
+        scales[buf * kTok + lane] = make_float2(exp2_int(scale_exponent(kb) - kHeldBack), (float)scale_exponent(vb));
       };
       auto issue = [&](int i, int buf, int raw, int blk, int& kb, int& vb) {  // the copies of stage i; its scale bytes stay in flight
         if (i < nstages) {
@@ -351,8 +355,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
         for (int st = 0; st < 8; ++st)
 #pragma unroll
           for (int k = 0; k < 2; ++k) qb[nt][st][k] = pack_f16x2(bf16_lo(qb[nt][st][k]) * up, bf16_hi(qb[nt][st][k]) * up);
-        qf[nt][0] = __shfl_sync(0xffffffffu, down, 4 * hcol) * a.scale_log2;  // lane 4 h holds head h
-        qf[nt][1] = __shfl_sync(0xffffffffu, down, 4 * hcol + 4) * a.scale_log2;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)  // lane 4 h holds head h
+          qf[nt][h] = fminf(__shfl_sync(0xffffffffu, down, 4 * (hcol + h)) * a.scale_log2 * exp2_int(kHeldBack), 3.4028234663852886e38f);
       }
 #pragma unroll
       for (int i = 0; i + 1 < STAGES; ++i) settle(i, raw_p[i], blk_p[i]);

@@ -78,6 +78,21 @@ def test_sparse_attn_of_rows_outside_the_row_space():
     check_attn(c, 8, q, i2, c2, out, lse)
 
 
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (8, 1), (16, 1)])
+@pytest.mark.parametrize("power,lo,hi", [(-116, 240, 248), (97, 27, 35), (-116, 27, 248)])
+def test_sparse_attn_at_both_ends_of_the_exponents(hq, hkv, power, lo, hi):
+    """K scales at the ends of their range under queries that make ordinary logits of them."""
+    c = Cache([300, 200], 1, hkv, 64, 16, 0, seed=hq)
+    c.params(hq=hq, top_k=128, sm_scale=2.0 ** -10)
+    c.ks.copy_(torch.randint(lo, hi, c.ks.shape, generator=gen(1), device=DEV, dtype=torch.uint8))
+    q = (torch.randn((2, 1, hq, 128), generator=gen(2), device=DEV) * 2.0 ** power).to(BF16)
+    q[1, 0, 1] = 0
+    idx, cnt = make_index(c, 128, 0, 1)
+    out, lse = run_attn(c, q, idx, cnt)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    check_attn(c, hq, q, idx, cnt, out, lse, sm_scale=2.0 ** -10)
+
+
 @pytest.mark.parametrize("heads,top_k", [(2, 300), (1, 2048)])
 @pytest.mark.parametrize("power", [0, 8, 16, 24, 60, 100])
 def test_sparse_attn_one_token_takes_all(power, heads, top_k):
