@@ -173,6 +173,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
   int cur_b = -1;
   uint32_t qb[NT][C * 4][2];
   float qf[NT][2];  // power of two of query tokens 2j and 2j + 1 of each n-tile
+  bool far = false;  // one of them lies outside 2^-60 .. 2^60
   for (int slot = 0;; slot = slot + 1 == kStages ? 0 : slot + 1) {
     const int4 t = tiles[2 * slot];
     if (t.x < 0) break;
@@ -183,6 +184,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
     for (int m = 0; m < M; ++m) sb[m] = rows[m] >= 0 ? a.scale[rows[m] >> a.scale_shift] : 127;
     if (t.x != cur_b) {
       cur_b = t.x;
+      far = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int tok = nt * 8 + g;
@@ -202,7 +204,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
         top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // (255 - 127: something is not finite, and neither are the scores)
-        const int shift = min(13 + 127 - (int)(max(top & 0xffffu, top >> 16) >> 7), 120);
+        const int shift = top == 0u ? 0 : min(13 + 127 - (int)(max(top & 0xffffu, top >> 16) >> 7), 120);
+        far = far || shift > 60 || shift < -60;
         const float up = exp2_int(shift), down = exp2_int(-shift);
 #pragma unroll
         for (int w = 0; w < C * 4; ++w)
@@ -211,6 +214,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
         qf[nt][0] = __shfl_sync(0xffffffffu, down, 8 * j);  // lane (2j, 0) has query token 2j of the tile
         qf[nt][1] = __shfl_sync(0xffffffffu, down, 8 * j + 4);
       }
+      far = __any_sync(0xffffffffu, far);
     }
     cp_async_wait<kStages - 1>();
     const unsigned char* data = mine + slot * kTileBytes;
@@ -239,21 +243,34 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
     float kf[M];
 #pragma unroll
     for (int m = 0; m < M; ++m) kf[m] = exp2_int(scale_exponent(sb[m]));
+    auto put = [&](auto score) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int tok = nt * 8 + 2 * j + i;
-        if (tok < a.T) {
-          const int left = (a.causal ? t.z - a.T + tok + 1 : t.z) - t.y - g;  // keys that it sees from this lane's first one on
-          float* dst = a.scores + ((int64_t)t.x * a.T + tok) * a.score_stride + t.y + g;
+        for (int i = 0; i < 2; ++i) {
+          const int tok = nt * 8 + 2 * j + i;
+          if (tok < a.T) {
+            const int left = (a.causal ? t.z - a.T + tok + 1 : t.z) - t.y - g;  // keys that it sees from this lane's first one on
+            float* dst = a.scores + ((int64_t)t.x * a.T + tok) * a.score_stride + t.y + g;
 #pragma unroll
-          for (int m = 0; m < M; ++m)
+            for (int m = 0; m < M; ++m)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (16 * m + 8 * h < left) dst[16 * m + 8 * h] = acc[m][nt][2 * h + i] * qf[nt][i] * kf[m];  // (a product of the two powers may not be a float)
+              for (int h = 0; h < 2; ++h)
+                if (16 * m + 8 * h < left) dst[16 * m + 8 * h] = score(acc[m][nt][2 * h + i], qf[nt][i], kf[m]);
+          }
         }
-      }
+    };
+    // Sums (2^-27 .. 2^30) stay floats under the query's power while that is ordinary. Else the two powers' product (2^-220 .. 2^235) is
+    // applied in two halves, so that what lies between is a float wherever the score is. (Halves for every query: 11.1 -> 11.4 us for
+    // 24 ragged sequences of four tokens.)
+    if (!far) {
+      put([](float sum, float q, float k) { return sum * q * k; });
+    } else {
+      put([](float sum, float q, float k) {
+        const int e = (int)(__float_as_uint(q) >> 23) + (int)(__float_as_uint(k) >> 23) - 254;
+        return sum * exp2_int(e >> 1) * exp2_int(e - (e >> 1));
+      });
+    }
   }
   cp_async_wait<0>();
 }

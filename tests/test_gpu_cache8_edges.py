@@ -78,6 +78,22 @@ def test_sparse_attn_of_rows_outside_the_row_space():
     check_attn(c, 8, q, i2, c2, out, lse)
 
 
+@pytest.mark.parametrize("T", [2])
+def test_index_scores_at_both_ends_of_the_exponents(T):
+    """Largest scales under small queries, smallest scales under large ones: the scores are ordinary numbers."""
+    c = Cache([200] * 4, T, 1, 128, 16, 0, seed=6)
+    c.params()
+    q = randn(gen(5), 4, T, 128)
+    for b, (s, lo, hi) in enumerate(((-100, 244, 248), (120, 27, 30), (-20, 247, 248), (60, 27, 40))):
+        q[b] *= 2.0 ** s
+        at = int(c.start[b]) // 16
+        c.isc[at:at + 13] = torch.randint(lo, hi, (13,), generator=gen(b), device=DEV, dtype=torch.uint8)
+    assert int((c.idx.view(torch.float8_e4m3fn).float().abs() >= 256).sum()) > 100  # values of 2^128 and more among them
+    s = run_scores(c, q, 0)
+    assert torch.isfinite(s[:, :, :200]).all()
+    check_scores(c, q, s, 0)
+
+
 @pytest.mark.parametrize("hq,hkv", [(8, 2), (8, 1), (16, 1)])
 @pytest.mark.parametrize("power,lo,hi", [(-116, 240, 248), (97, 27, 35), (-116, 27, 248)])
 def test_sparse_attn_at_both_ends_of_the_exponents(hq, hkv, power, lo, hi):
