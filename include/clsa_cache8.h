@@ -113,8 +113,8 @@ CLSA_API clsa_status clsa_cache8_append(const clsa_params* p, const clsa_cache8*
 /* scores[b][t][s] = sum_j q_idx[b][t][j] * K_idx[s][j] for every visible s: clsa_index_scores over an 8-bit cache (its
  * arguments, its results for the values that the codes stand for). Codes are exact in the 16-bit operands of the
  * matrix instructions, so are bf16 queries down to 2^-31 of their row's largest magnitude; sums are fp32. T up to 32 streams
- * the keys once; larger T expands the keys to bf16 in the workspace (exact) and runs the tensor-core GEMM of
- * clsa_index_scores over them. A row outside num_cache_rows counts as a row of zeros and flags CLSA_DEV_BAD_INDEX. */
+ * the keys once; larger T expands them to bf16 in the workspace (halved, and exact: 2^128 is no bf16) and runs the tensor-core
+ * GEMM of clsa_index_scores over them, doubling its sums. A row outside num_cache_rows counts as a row of zeros and flags CLSA_DEV_BAD_INDEX. */
 CLSA_API clsa_status clsa_index_scores8(const clsa_params* p, const clsa_cache8* c, const void* q_idx, float* scores,
                                         int64_t score_stride, void* workspace, size_t workspace_bytes, clsa_stream stream);
 

@@ -227,7 +227,7 @@ clsa_status clsa_index_scores(const clsa_params* p, const void* q_idx, float* sc
   DeviceInfo dev;
   if (!device_info(&dev)) return CLSA_ERR_CUDA;
   if (p->q_per_seq > 1)
-    return from_cuda(launch_index_scores_gemm(*p, q_idx, scores, score_stride, static_cast<uint32_t*>(workspace), dev,
+    return from_cuda(launch_index_scores_gemm(*p, q_idx, scores, score_stride, false, static_cast<uint32_t*>(workspace), dev,
                                               static_cast<cudaStream_t>(stream)));
   return from_cuda(launch_index_scores_decode(*p, q_idx, scores, score_stride, static_cast<uint32_t*>(workspace),
                                               static_cast<uint32_t*>(workspace) + kSchedWord, dev,
@@ -270,7 +270,7 @@ clsa_status clsa_index_topk(const clsa_params* p, const void* q_idx, int32_t* id
   if (p->q_per_seq > 1 && index_topk_fits(*p, dev))
     return from_cuda(launch_index_topk(*p, q_idx, idx, count, base + w.scores_off, status, dev, s));
   auto scores = reinterpret_cast<float*>(base + w.scores_off);
-  cudaError_t err = p->q_per_seq > 1 ? launch_index_scores_gemm(*p, q_idx, scores, w.score_stride, status, dev, s)
+  cudaError_t err = p->q_per_seq > 1 ? launch_index_scores_gemm(*p, q_idx, scores, w.score_stride, false, status, dev, s)
                                      : launch_index_scores_decode(*p, q_idx, scores, w.score_stride, status, status + kSchedWord, dev, s);
   if (err != cudaSuccess) return CLSA_ERR_CUDA;
   return from_cuda(launch_topk(*p, scores, w.score_stride, idx, count, status, dev, s));

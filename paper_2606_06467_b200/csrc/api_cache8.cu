@@ -219,7 +219,7 @@ clsa_status clsa_index_scores8(const clsa_params* p, const clsa_cache8* c, const
   e.seq_start = starts;
   e.block_table = nullptr;
   e.num_cache_rows = (int64_t)p->num_seqs * w.expand_rows;
-  return from_cuda(launch_index_scores_gemm(e, q_idx, scores, score_stride, status, dev, s));
+  return from_cuda(launch_index_scores_gemm(e, q_idx, scores, score_stride, true, status, dev, s));
 }
 
 clsa_status clsa_sparse_attn8(const clsa_params* p, const clsa_cache8* c, const void* q, const int32_t* idx,

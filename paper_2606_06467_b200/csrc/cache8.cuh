@@ -28,7 +28,7 @@ cudaError_t launch_cache8_append(const clsa_params& p, const clsa_cache8& c, con
                                  const DeviceInfo& dev, cudaStream_t stream);
 cudaError_t launch_index_scores8(const clsa_params& p, const clsa_cache8& c, const void* q_idx, float* scores,
                                  int64_t score_stride, uint32_t* status, const DeviceInfo& dev, cudaStream_t stream);
-// bf16 rows of the sequences' 8-bit keys, sequence b from row b * rows_per_seq, and those starts
+// Half of the sequences' 8-bit keys as bf16 rows, sequence b from row b * rows_per_seq, and those starts
 cudaError_t launch_index_expand8(const clsa_params& p, const clsa_cache8& c, void* keys, int64_t* starts, int64_t rows_per_seq,
                                  uint32_t* status, const DeviceInfo& dev, cudaStream_t stream);
 

@@ -95,8 +95,9 @@ WorkspaceLayout make_workspace_layout(const clsa_params& p, const DeviceInfo& de
 // sit kSchedWord words behind the status word)
 cudaError_t launch_index_scores_decode(const clsa_params& p, const void* q_idx, float* scores, int64_t score_stride,
                                        uint32_t* status, uint32_t* sched, const DeviceInfo& dev, cudaStream_t stream);
+// halved: the keys are half of what they stand for (so that 2^128, which an 8-bit cache can hold, is a bf16 number)
 cudaError_t launch_index_scores_gemm(const clsa_params& p, const void* q_idx, float* scores, int64_t score_stride,
-                                     uint32_t* status, const DeviceInfo& dev, cudaStream_t stream);
+                                     bool halved, uint32_t* status, const DeviceInfo& dev, cudaStream_t stream);
 // Buffers of the fused chunk routing (clsa_index_topk, T > 1) that the GEMM's filtering and hand-back modes use.
 struct GemmFused {
   const float* pivot;          // [rows] per query row: keys scoring below it cannot be among the row's k largest

@@ -198,7 +198,8 @@ __device__ __forceinline__ TileCoord tile_coord(const GemmArgs& a, int64_t id) {
 // MODE 0: the scores are stored (clsa_index_scores; also the sampling pass of clsa_index_topk).
 // MODE 1: the scores are compared with a per-row pivot in registers and only candidates leave the SM (clsa_index_topk).
 // MODE 2: MODE 0 for the few rows that clsa_index_topk hands back, into a small scratch matrix.
-template <int MODE>
+// HALVED: the keys are half of what they stand for, and so are the products; the scores are stored doubled.
+template <int MODE, bool HALVED = false>
 __global__ void __launch_bounds__(gemm_threads(MODE), 1)
 index_scores_gemm_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                          const __grid_constant__ CUtensorMap map_s, const GemmArgs a) {
@@ -486,9 +487,12 @@ index_scores_gemm_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
 #pragma unroll
-        for (int ch = 0; ch < 8; ++ch)
-          *reinterpret_cast<uint4*>(tile + lane * 128 + ((ch ^ (lane & 7)) << 4)) =
-              make_uint4(r[4 * ch], r[4 * ch + 1], r[4 * ch + 2], r[4 * ch + 3]);
+        for (int ch = 0; ch < 8; ++ch) {
+          uint32_t w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] = HALVED ? __float_as_uint(2.f * __uint_as_float(r[4 * ch + k])) : r[4 * ch + k];
+          *reinterpret_cast<uint4*>(tile + lane * 128 + ((ch ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
         if (a.vec_ok && s0 + 32 <= v_all) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the copy engine
           __syncwarp();
@@ -610,8 +614,9 @@ namespace {
 
 // One launch of the chunk GEMM. mode 0: scores are stored into `scores` (sample_gs > 0: the sampled columns only);
 // mode 1: filtered against fx.pivot into fx.cand; mode 2: rows with a slot are stored into row `slot` of `scores`.
+// halved (mode 0): see the kernel.
 cudaError_t launch_gemm(int mode, const clsa_params& p, const void* q_idx, float* scores, int64_t score_stride,
-                        int sample_gs, const GemmFused* fx, uint32_t* status, const DeviceInfo& dev, cudaStream_t stream) {
+                        int sample_gs, const GemmFused* fx, bool halved, uint32_t* status, const DeviceInfo& dev, cudaStream_t stream) {
   CUtensorMap map_q, map_k;
   const uint64_t q_rows = (uint64_t)p.num_seqs * p.q_per_seq;
   if (!make_map(&map_q, q_idx, q_rows, (uint64_t)p.idx_dim, (uint64_t)p.idx_dim, kBM)) return cudaErrorInvalidValue;
@@ -659,7 +664,7 @@ cudaError_t launch_gemm(int mode, const clsa_params& p, const void* q_idx, float
   const int64_t tiles = (int64_t)p.num_seqs * a.m_blocks * a.n_tiles;
   if (tiles < 1) return cudaSuccess;
   const int grid = (int)(tiles < dev.sm_count ? tiles : dev.sm_count);
-  auto kernel = mode == 0 ? index_scores_gemm_kernel<0> : mode == 1 ? index_scores_gemm_kernel<1> : index_scores_gemm_kernel<2>;
+  auto kernel = mode == 0 ? (halved ? index_scores_gemm_kernel<0, true> : index_scores_gemm_kernel<0>) : mode == 1 ? index_scores_gemm_kernel<1> : index_scores_gemm_kernel<2>;
   cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   if (err != cudaSuccess) return err;
   kernel<<<grid, gemm_threads(mode), kSmemBytes, stream>>>(map_q, map_k, map_s, a);
@@ -682,23 +687,23 @@ int index_gemm_filter_hole_slack(const clsa_params& p, const DeviceInfo& dev) {
 }
 
 cudaError_t launch_index_scores_gemm(const clsa_params& p, const void* q_idx, float* scores, int64_t score_stride,
-                                     uint32_t* status, const DeviceInfo& dev, cudaStream_t stream) {
-  return launch_gemm(0, p, q_idx, scores, score_stride, 0, nullptr, status, dev, stream);
+                                     bool halved, uint32_t* status, const DeviceInfo& dev, cudaStream_t stream) {
+  return launch_gemm(0, p, q_idx, scores, score_stride, 0, nullptr, halved, status, dev, stream);
 }
 
 cudaError_t launch_index_gemm_sample(const clsa_params& p, const void* q_idx, float* sample, int64_t sample_stride,
                                      int sample_gs, uint32_t* status, const DeviceInfo& dev, cudaStream_t stream) {
-  return launch_gemm(0, p, q_idx, sample, sample_stride, sample_gs, nullptr, status, dev, stream);
+  return launch_gemm(0, p, q_idx, sample, sample_stride, sample_gs, nullptr, false, status, dev, stream);
 }
 
 cudaError_t launch_index_gemm_filter(const clsa_params& p, const void* q_idx, const GemmFused& fx, uint32_t* status,
                                      const DeviceInfo& dev, cudaStream_t stream) {
-  return launch_gemm(1, p, q_idx, nullptr, 0, 0, &fx, status, dev, stream);
+  return launch_gemm(1, p, q_idx, nullptr, 0, 0, &fx, false, status, dev, stream);
 }
 
 cudaError_t launch_index_gemm_handed_back(const clsa_params& p, const void* q_idx, float* scratch, int64_t score_stride,
                                           const GemmFused& fx, uint32_t* status, const DeviceInfo& dev, cudaStream_t stream) {
-  return launch_gemm(2, p, q_idx, scratch, score_stride, 0, &fx, status, dev, stream);
+  return launch_gemm(2, p, q_idx, scratch, score_stride, 0, &fx, false, status, dev, stream);
 }
 
 }  // namespace clsa

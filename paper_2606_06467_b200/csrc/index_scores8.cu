@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) index_scores8_kernel(const __g
   cp_async_wait<0>();
 }
 
-// ---- more than 32 query tokens: the keys as bf16 rows (exact) for the tensor-core GEMM ---------------------------------
+// ---- more than 32 query tokens: half of the keys' values as bf16 rows (exact: 2^-110 .. 1.75 * 2^127) for the tensor-core GEMM ----
 __global__ void __launch_bounds__(256) index_expand8_kernel(const Scores8Args a, int idx_dim, uint4* out, int64_t* starts,
                                                             int64_t rows_per_seq, int blocks_per_seq) {
   const int per_row = idx_dim / 16;  // 16 codes per thread
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(256) index_expand8_kernel(const Scores8Args a,
   } else if (part == 0) {
     flag_status(a.status, CLSA_DEV_BAD_INDEX);
   }
-  const float f = exp2_int(e);
+  const float f = exp2_int(e - 1);
   const uint32_t in[4] = {w.x, w.y, w.z, w.w};
   uint32_t o[8];
 #pragma unroll

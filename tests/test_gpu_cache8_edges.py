@@ -78,7 +78,7 @@ def test_sparse_attn_of_rows_outside_the_row_space():
     check_attn(c, 8, q, i2, c2, out, lse)
 
 
-@pytest.mark.parametrize("T", [2])
+@pytest.mark.parametrize("T", [2, 40])
 def test_index_scores_at_both_ends_of_the_exponents(T):
     """Largest scales under small queries, smallest scales under large ones: the scores are ordinary numbers."""
     c = Cache([200] * 4, T, 1, 128, 16, 0, seed=6)
