@@ -191,7 +191,7 @@ def _heads(t, what, device, bf16, tokens, heads, dim, flat=False):
             B, T, h, d = shape
             token, s1, head, one = stride
             n = B * T
-            even = T == 1 or B == 1 or token == T * s1
+            even = T == 1 or B == 1 or n == 0 or token == T * s1
             if T > 1:
                 token = s1
     except ValueError:

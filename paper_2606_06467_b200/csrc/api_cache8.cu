@@ -130,22 +130,21 @@ clsa_status clsa_norm_rope(const clsa_norm_rope_spec* spec, int32_t num_tokens, 
                            const clsa_heads* q_out, const clsa_heads* k, const clsa_heads* k_out, clsa_stream stream) {
   CLSA_TRY(check_spec(spec));
   if (num_tokens < 0 || num_tokens > 1 << 30) return CLSA_ERR_INVALID_ARG;
-  if (!aligned(positions, 4) || (positions == nullptr && spec->rot_dim > 0)) return CLSA_ERR_INVALID_ARG;
   if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (q == nullptr && k == nullptr))
     return CLSA_ERR_INVALID_ARG;
   const clsa_heads* pairs[2][2] = {{q, q_out}, {k, k_out}};
   for (auto& pr : pairs) {
     if (pr[0] == nullptr) continue;
-    if (num_tokens > 0) {
-      CLSA_TRY(check_heads(pr[0], spec->head_dim, false));
-      CLSA_TRY(check_heads(pr[1], spec->head_dim, num_tokens > 1));
-    }
     if (pr[0]->num_heads != pr[1]->num_heads) return CLSA_ERR_INVALID_ARG;
+    if (num_tokens == 0) continue;  // nothing has an address, and no stride means anything
+    CLSA_TRY(check_heads(pr[0], spec->head_dim, false));
+    CLSA_TRY(check_heads(pr[1], spec->head_dim, num_tokens > 1));
     if (pr[0]->data == pr[1]->data && (pr[0]->token_stride != pr[1]->token_stride ||
                                        (pr[0]->num_heads > 1 && pr[0]->head_stride != pr[1]->head_stride)))
       return CLSA_ERR_INVALID_ARG;
   }
   if (num_tokens == 0) return CLSA_OK;
+  if (!aligned(positions, 4) || (positions == nullptr && spec->rot_dim > 0)) return CLSA_ERR_INVALID_ARG;
   DeviceInfo dev;
   if (!device_info(&dev)) return CLSA_ERR_CUDA;
   return from_cuda(launch_norm_rope(*spec, num_tokens, positions, q, q_out, k, k_out, dev, static_cast<cudaStream_t>(stream)));

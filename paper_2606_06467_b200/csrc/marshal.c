@@ -110,8 +110,8 @@ static int heads_of(PyObject* t, int64_t device, int64_t dim, int flat, clsa_hea
     *tokens = v.shape[0];
     token = v.stride[0];
   } else if (v.nd == 4) {
-    if (v.shape[1] != 1 && v.shape[0] != 1 && v.stride[0] != v.shape[1] * v.stride[1]) return 0;
     *tokens = v.shape[0] * v.shape[1];
+    if (v.shape[1] != 1 && v.shape[0] != 1 && *tokens != 0 && v.stride[0] != v.shape[1] * v.stride[1]) return 0;
     token = v.shape[1] == 1 ? v.stride[0] : v.stride[1];
   } else {
     return 0;

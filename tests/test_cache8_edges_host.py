@@ -1,0 +1,120 @@
+"""Host-side checks of the 8-bit cache calls without a GPU: empty batches, layouts of scales, sizes of buffers against the params,
+in the Python marshalling and in the native one (which gets stand-ins for tensors and for the library's entry points)."""
+import ctypes
+import os
+import sys
+
+import pytest
+
+torch = pytest.importorskip("torch")
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BF16, I32, F32, U8 = torch.bfloat16, torch.int32, torch.float32, torch.uint8
+
+
+@pytest.fixture(scope="module")
+def clsa():
+    sys.path.insert(0, ROOT)
+    import __graft_entry__ as entry
+
+    entry._load_build_module().build()
+    import paper_2606_06467_b200 as mod
+
+    return mod
+
+
+def test_an_empty_batch_is_a_call_that_does_nothing(clsa):
+    """No tokens, as empty tensors give them: no address of positions or heads, strides of any kind."""
+    P, raw = ctypes.byref, clsa.raw()
+    spec = clsa.clsa_norm_rope_spec(128, 1, 1e-6, 128, 0, 1.0, 0x7000, None, None)
+    a, b = clsa.clsa_heads(None, 8, 1536, 128), clsa.clsa_heads(None, 8, 1024, 128)
+    assert raw.clsa_norm_rope(P(spec), 0, None, P(a), P(b), None, None, None) == clsa.CLSA_OK
+    assert raw.clsa_norm_rope(P(spec), 0, None, None, None, P(a), P(b), None) == clsa.CLSA_OK
+    assert raw.clsa_norm_rope(P(spec), 0, None, P(a), None, None, None, None) == 1  # what is wrong without tokens is still wrong
+    assert raw.clsa_norm_rope(P(spec), 4, None, P(a), P(b), None, None, None) == 1
+
+
+class Tensor:
+    """What the marshalling asks of a tensor."""
+
+    def __init__(self, shape, dtype, stride=None, device=0):
+        self.shape, self.dtype, self.device = tuple(shape), dtype, device
+        dense = [1] * len(shape)
+        for i in reversed(range(len(shape) - 1)):
+            dense[i] = dense[i + 1] * max(shape[i + 1], 1)
+        self._dense, self._stride = tuple(dense), tuple(stride or dense)
+
+    def stride(self, i=None):
+        return self._stride if i is None else self._stride[i]
+
+    def dim(self):
+        return len(self.shape)
+
+    def size(self, i):
+        return self.shape[i]
+
+    def numel(self):
+        n = 1
+        for x in self.shape:
+            n *= x
+        return n
+
+    def element_size(self):
+        return {BF16: 2, U8: 1}.get(self.dtype, 4)
+
+    def is_contiguous(self):
+        return self._stride == self._dense
+
+    def get_device(self):
+        return self.device
+
+    def data_ptr(self):
+        return 0x100000 if self.numel() else 0
+
+
+@pytest.fixture(params=["native", "python"])
+def binding(clsa, request, monkeypatch):
+    """The package with entry points that record their calls in place of the library's, and Tensor in place of torch's."""
+    from paper_2606_06467_b200 import cache8
+
+    calls = []
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: calls.append(name) or 0
+
+    cache8._load_torch()
+    monkeypatch.setattr(cache8, "_lib", Lib())
+    monkeypatch.setattr(cache8, "_device", lambda torch: 0)
+    monkeypatch.setattr(cache8, "_stream8", lambda stream, device: 0)
+    if request.param == "python":
+        monkeypatch.setattr(cache8, "_marshal", None)
+        yield clsa, calls
+        return
+    if cache8._marshal is None:
+        pytest.skip("built without Python.h")
+    # any number of integer arguments will do: the recorder looks at none
+    kinds = {"clsa_norm_rope": 8, "clsa_cache8_append": 9, "clsa_index_scores8": 8, "clsa_sparse_attn8": 11}
+    keep = [ctypes.CFUNCTYPE(ctypes.c_int, *[ctypes.c_void_p] * n)(lambda *a, name=name: calls.append("native " + name) or 0) for name, n in kinds.items()]
+    cache8._marshal.setup(*[ctypes.cast(f, ctypes.c_void_p).value for f in keep], Tensor, BF16, I32, F32, U8, lambda: 0, lambda d: 0, clsa.clsa_params,
+                          clsa.clsa_cache8, clsa.clsa_norm_rope_spec, clsa.clsa_attn_hints)
+    yield clsa, calls
+    monkeypatch.undo()
+    cache8._load_torch()
+
+
+def _taken(calls, name):
+    """One call was made, by the native module where that is the one under test."""
+    got = list(calls)
+    calls.clear()
+    return got in ([name], ["native " + name])
+
+
+def test_empty_tensors_are_taken(binding):
+    clsa, calls = binding
+    spec = clsa.make_norm_rope(head_dim=128, norm=1, rot_dim=0)
+    for shape in ((0, 8, 128), (0, 4, 8, 128), (3, 0, 8, 128)):
+        q = Tensor(shape, BF16)
+        clsa.clsa_norm_rope(spec, Tensor((0,), I32), q, q)
+        assert _taken(calls, "clsa_norm_rope"), shape
+        clsa.clsa_norm_rope(spec, Tensor((0,), I32), None, None, q, q)
+        assert _taken(calls, "clsa_norm_rope"), shape

@@ -158,3 +158,14 @@ def test_sparse_attn_logits_far_below_zero():
     (kc, ks), (vc, vs), _ = c.host()
     v = ref.values(vc, vs, 16)[row, 0]
     assert (np.abs(f64(out[0, 0, 0]) - v) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(v)).all()
+
+
+def test_empty_batches_do_nothing():
+    freq = torch.ones(64, device=DEV)
+    spec = clsa.make_norm_rope(head_dim=128, norm=1, rot_dim=128, inv_freq=freq)
+    pos = torch.empty(0, dtype=torch.int32, device=DEV)
+    for shape in ((0, 8, 128), (0, 4, 8, 128), (3, 0, 8, 128)):
+        q = torch.empty(shape, dtype=BF16, device=DEV)
+        clsa.clsa_norm_rope(spec, pos, q, q)
+        clsa.clsa_norm_rope(spec, pos, torch.empty((*shape[:-2], 12, 128), dtype=BF16, device=DEV)[..., 2:10, :], q)  # another layout
+        clsa.clsa_norm_rope(spec, pos, None, None, q, torch.empty_like(q))
