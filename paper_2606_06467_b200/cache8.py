@@ -162,10 +162,12 @@ def make_cache8(*, k=None, v=None, k_scale=None, v_scale=None, idx_k=None, idx_k
             _want(t is not None and t.dim() == 2 and t.stride(1) == 1 and t.shape[0] == k.shape[1]
                   and t.shape[1] * scale_block >= k.shape[0], f"{what}: [heads, blocks] bytes for every row is wanted")
             _bytes_like(t, what, ("float8_e8m0fnu",))
-        _want(k_scale.stride(0) == v_scale.stride(0) or k.shape[1] == 1, "k_scale and v_scale: one layout is wanted")
+        one = k.shape[1] == 1  # nothing lies between heads then
+        _want(one or k_scale.stride(0) == v_scale.stride(0), "k_scale and v_scale: one layout is wanted")
+        _want(one or min(k_scale.stride(0), v_scale.stride(0)) >= max(k_scale.shape[1], v_scale.shape[1]), "k_scale and v_scale: every head's own bytes are wanted")
         c.k, c.v, c.k_scale, c.v_scale = _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale)
         c.kv_token_stride, c.kv_head_stride = k.stride(0), k.stride(1)
-        c.scale_head_stride = max(k_scale.stride(0), k_scale.shape[1])
+        c.scale_head_stride = k_scale.shape[1] if one else k_scale.stride(0)
     if idx_k is not None:
         _want(idx_k.dim() == 2 and idx_k.stride(1) == 1, "idx_k: [rows, d_idx] with dense rows is wanted")
         _bytes_like(idx_k, "idx_k", ("float8_e4m3fn",))

@@ -33,6 +33,21 @@ def test_an_empty_batch_is_a_call_that_does_nothing(clsa):
     assert raw.clsa_norm_rope(P(spec), 4, None, P(a), P(b), None, None, None) == 1
 
 
+def test_scale_strides_are_the_tensors_own(clsa):
+    u8 = lambda *s: torch.zeros(s, dtype=U8)  # noqa: E731
+    k = u8(128, 4, 128)
+    with pytest.raises(ValueError):  # one row of scales for all heads
+        clsa.make_cache8(k=k, v=k, k_scale=u8(1, 2).expand(4, 2), v_scale=u8(1, 2).expand(4, 2), scale_block=64)
+    with pytest.raises(ValueError):  # overlapping rows
+        s = u8(16).as_strided((4, 2), (1, 1))
+        clsa.make_cache8(k=k, v=k, k_scale=s, v_scale=s, scale_block=64)
+    wide = u8(4, 9)[:, :2]
+    assert clsa.make_cache8(k=k, v=k, k_scale=wide, v_scale=wide, scale_block=64).scale_head_stride == 9
+    one = u8(128, 1, 128)
+    for s in (u8(1, 2), u8(2).expand(1, 2), u8(2, 2)[:1]):  # one head: no distance between heads
+        assert clsa.make_cache8(k=one, v=one, k_scale=s, v_scale=s, scale_block=64).scale_head_stride >= 2
+
+
 class Tensor:
     """What the marshalling asks of a tensor."""
 
