@@ -1,5 +1,6 @@
 """Binding of the 8-bit cache calls (`include/clsa_cache8.h`): the same names and argument orders, tensors in place of
-pointers. Checks of dtypes, shapes, strides and devices that C cannot make happen here; everything else is marshalling. The
+pointers. Checks of dtypes, shapes, strides, sizes and devices that C cannot make happen here (an address in place of a tensor is
+taken as it is); everything else is marshalling. The
 usual call goes through the native module `_marshal` (csrc/marshal.c), which makes the same checks without the interpreter and
 hands back what it does not take as it is; without the module every call takes the way below.
 """
@@ -36,6 +37,7 @@ class clsa_cache8(ctypes.Structure):
     """Mirror of `clsa_cache8` in include/clsa_cache8.h."""
 
     _device = None  # where the tensors behind it lie, if it was made of tensors
+    _extent = None  # and what they hold: rows, heads and dimension of K and V, rows and dimension of K_idx (0: there are none)
 
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("kv_token_stride", _i64),
                 ("kv_head_stride", _i64), ("scale_head_stride", _i64), ("idx_k", _vp), ("idx_k_scale", _vp),
@@ -62,16 +64,30 @@ def _want(ok, message):
         raise ValueError(message)
 
 
-def _dense(t, what, dtype, device, rows=False, output=False):
-    """Address of a buffer on the current device that is addressed as one dense array of `dtype` (None and device addresses
-    pass). rows: its rows alone are dense. output: it may also lie in pinned host memory."""
+def _dense(t, what, dtype, device, need, rows=False, output=False):
+    """Address of a buffer on the current device that is addressed as one dense array of `need` or more values of `dtype` (None and
+    device addresses pass). rows: its rows alone are dense. output: it may also lie in pinned host memory."""
     if t is None or isinstance(t, int):
         return t
     if t.dtype != dtype or not (t.is_contiguous() or (rows and t.stride(-1) == 1)) or (
             t.get_device() != device and not (output and t.get_device() < 0 and t.is_pinned())):
         raise ValueError(f"{what}: contiguous values of {dtype} on the current CUDA device are wanted, got {t.dtype} on {t.device}, "
                          f"strides {t.stride()}")
+    has = 1 + sum((n - 1) * step for n, step in zip(t.shape, t.stride())) if t.numel() else 0
+    if has < need:
+        raise ValueError(f"{what}: {need} values are wanted, got {has} (shape {tuple(t.shape)})")
     return t.data_ptr()
+
+
+def _fits(p, c, kv, idx):
+    """Refuse params that name more of a cache than its tensors hold."""
+    if c._extent is None:
+        return
+    rows, heads, dim, idx_rows, idx_dim = c._extent
+    if kv and heads and (p.num_cache_rows > rows or p.num_kv_heads > heads or p.head_dim > dim):
+        raise ValueError(f"the params name {p.num_cache_rows} rows of {p.num_kv_heads} heads of {p.head_dim}, K and V hold {rows} of {heads} of {dim}")
+    if idx and idx_dim and (p.num_cache_rows > idx_rows or p.idx_dim > idx_dim):
+        raise ValueError(f"the params name {p.num_cache_rows} rows of {p.idx_dim}, K_idx holds {idx_rows} of {idx_dim}")
 
 
 def _workspace(ws, ws_bytes, made, device):
@@ -83,7 +99,10 @@ def _workspace(ws, ws_bytes, made, device):
         return ws, ws_bytes
     if ws.get_device() != device:
         raise ValueError(f"workspace: a tensor on the current CUDA device is wanted, got {ws.device}")
-    return ws.data_ptr(), ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    has = ws.numel() * ws.element_size()
+    if ws_bytes is not None and ws_bytes > has:
+        raise ValueError(f"workspace: a tensor of {ws_bytes} bytes is wanted, got {has}")
+    return ws.data_ptr(), has if ws_bytes is None else ws_bytes
 
 
 def _device_of(*tensors):
@@ -152,6 +171,7 @@ def make_cache8(*, k=None, v=None, k_scale=None, v_scale=None, idx_k=None, idx_k
     c = clsa_cache8()
     c._tensors = (k, v, k_scale, v_scale, idx_k, idx_k_scale)
     c._device = _device_of(*c._tensors)
+    c._extent = (*((0, 0, 0) if k is None else k.shape), *((0, 0) if idx_k is None else idx_k.shape))
     c.scale_block = scale_block
     if k is not None or v is not None:
         for t, what in ((k, "k"), (v, "v")):
@@ -226,7 +246,7 @@ def clsa_norm_rope(spec, positions, q, q_out, k=None, k_out=None, stream=None) -
         d, _, _ = _heads(k_out, "k_out", dev, bf16, n, h, dim)
     if spec._device not in (None, dev):
         raise ValueError("the tensors of clsa_norm_rope_spec are not on the current CUDA device")
-    status = _lib.clsa_norm_rope(ctypes.byref(spec), n, _dense(positions, "positions", torch.int32, dev), a, b, c, d, _stream8(stream, dev))
+    status = _lib.clsa_norm_rope(ctypes.byref(spec), n, _dense(positions, "positions", torch.int32, dev, n), a, b, c, d, _stream8(stream, dev))
     if status:
         _check(status, "clsa_norm_rope")
 
@@ -248,6 +268,7 @@ def clsa_cache8_append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace
         raise ValueError("k_new with v_new, idx_k_new, or all three are wanted")
     dev, bf16, n = _device(torch), torch.bfloat16, p.num_seqs * p.q_per_seq
     k = v = i = None
+    _fits(p, c, k_new is not None, idx_k_new is not None)
     if k_new is not None:
         k, _, _ = _heads(k_new, "k_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
         v, _, _ = _heads(v_new, "v_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
@@ -266,10 +287,12 @@ def clsa_index_scores8(p, c, q_idx, scores, score_stride, workspace, workspace_b
     status = _marshal.scores(p, c, q_idx, scores, score_stride, workspace, workspace_bytes, stream) if _marshal else None
     if status is not None:
         return _check(status, "clsa_index_scores8") if status else None
-    dev = _device(torch)
+    dev, n = _device(torch), p.num_seqs * p.q_per_seq
+    _fits(p, c, False, True)
     ws, nbytes = _workspace(workspace, workspace_bytes, (c,), dev)
-    status = _lib.clsa_index_scores8(ctypes.byref(p), ctypes.byref(c), _dense(q_idx, "q_idx", torch.bfloat16, dev),
-                                     _dense(scores, "scores", torch.float32, dev, True), score_stride, ws, nbytes, _stream8(stream, dev))
+    status = _lib.clsa_index_scores8(ctypes.byref(p), ctypes.byref(c), _dense(q_idx, "q_idx", torch.bfloat16, dev, n * p.idx_dim),
+                                     _dense(scores, "scores", torch.float32, dev, (n - 1) * score_stride + p.max_seq_len, rows=True), score_stride,
+                                     ws, nbytes, _stream8(stream, dev))
     if status:
         _check(status, "clsa_index_scores8")
 
@@ -280,11 +303,13 @@ def clsa_sparse_attn8(p, c, q, idx, count, out, lse, hints, workspace, workspace
     status = _marshal.attn(p, c, q, idx, count, out, lse, hints, workspace, workspace_bytes, stream) if _marshal else None
     if status is not None:
         return _check(status, "clsa_sparse_attn8") if status else None
-    dev, i32 = _device(torch), torch.int32
+    dev, i32, bf16, n = _device(torch), torch.int32, torch.bfloat16, p.num_seqs * p.q_per_seq
+    heads = n * p.num_q_heads
+    _fits(p, c, True, False)
     ws, nbytes = _workspace(workspace, workspace_bytes, (c,), dev)
-    status = _lib.clsa_sparse_attn8(ctypes.byref(p), ctypes.byref(c), _dense(q, "q", torch.bfloat16, dev), _dense(idx, "idx", i32, dev),
-                                    _dense(count, "count", i32, dev), _dense(out, "out", torch.bfloat16, dev, output=True),
-                                    _dense(lse, "lse", torch.float32, dev, output=True), None if hints is None else ctypes.byref(hints),
-                                    ws, nbytes, _stream8(stream, dev))
+    status = _lib.clsa_sparse_attn8(ctypes.byref(p), ctypes.byref(c), _dense(q, "q", bf16, dev, heads * p.head_dim),
+                                    _dense(idx, "idx", i32, dev, n * p.top_k), _dense(count, "count", i32, dev, n),
+                                    _dense(out, "out", bf16, dev, heads * p.head_dim, output=True), _dense(lse, "lse", torch.float32, dev, heads, output=True),
+                                    None if hints is None else ctypes.byref(hints), ws, nbytes, _stream8(stream, dev))
     if status:
         _check(status, "clsa_sparse_attn8")

@@ -26,7 +26,7 @@ static scores_fn f_scores;
 static attn_fn f_attn;
 static PyObject *t_tensor, *t_bf16, *t_i32, *t_f32, *t_u8, *g_device, *g_stream;  /* torch's: type, dtypes, two functions */
 static PyObject *t_params, *t_cache, *t_spec, *t_hints; /* cache8.py's structs */
-static PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_is_contiguous, *s_numel, *s__device, *s_cuda_stream;
+static PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_is_contiguous, *s_numel, *s__device, *s__extent, *s_cuda_stream;
 
 /* What a call needs of a tensor. */
 typedef struct {
@@ -80,8 +80,8 @@ static int look(PyObject* t, PyObject* dtype, int64_t device, view* v) {
   v->data = data_of(t, &bad);
   return !bad;
 }
-/* The address of a dense tensor; 0 if it is not one. None gives NULL where it is allowed. */
-static int dense(PyObject* t, PyObject* dtype, int64_t device, int none_ok, void** out) {
+/* The address of a dense tensor of `need` elements or more; 0 if it is not one. None gives NULL where it is allowed. */
+static int dense(PyObject* t, PyObject* dtype, int64_t device, int none_ok, double need, void** out) {
   *out = NULL;
   if (t == Py_None) return none_ok;
   if (!is_tensor(t, dtype, device)) return 0;
@@ -89,7 +89,7 @@ static int dense(PyObject* t, PyObject* dtype, int64_t device, int none_ok, void
   if (c == NULL) { PyErr_Clear(); return 0; }
   int bad = c != Py_True;
   Py_DECREF(c);
-  if (bad) return 0;
+  if (bad || (double)ask_int(t, s_numel, &bad) < need || bad) return 0;
   *out = data_of(t, &bad);
   return !bad;
 }
@@ -140,6 +140,21 @@ static const void* struct_of(PyObject* s, PyObject* type, Py_ssize_t bytes, int6
   PyBuffer_Release(&b);
   return p;
 }
+/* Whether a cache's tensors, if it was made of tensors, hold what the params name of K and V, and of K_idx. */
+static int fits(PyObject* cache, const clsa_params* p, int kv, int idx) {
+  int64_t e[5]; /* rows, heads, dimension; rows and dimension of K_idx */
+  PyObject* t = PyObject_GetAttr(cache, s__extent);
+  if (t == NULL) { PyErr_Clear(); return 0; }
+  int ok = t == Py_None;
+  if (!ok && PyTuple_Check(t) && PyTuple_GET_SIZE(t) == 5) {
+    for (int i = 0; i < 5; ++i) e[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+    ok = !PyErr_Occurred() && !(kv && e[1] > 0 && (p->num_cache_rows > e[0] || p->num_kv_heads > e[1] || p->head_dim > e[2])) &&
+         !(idx && e[4] > 0 && (p->num_cache_rows > e[3] || p->idx_dim > e[4]));
+    PyErr_Clear();
+  }
+  Py_DECREF(t);
+  return ok;
+}
 /* The current device, -1 if there is none. */
 static int64_t current_device(void) {
   PyObject* r = PyObject_CallNoArgs(g_device);
@@ -171,10 +186,12 @@ static int stream_of(PyObject* stream, int64_t device, clsa_stream* out) {
 static int workspace_of(PyObject* ws, PyObject* bytes, int64_t device, void** out, size_t* n) {
   int bad = 0;
   if (!is_tensor(ws, t_u8, device)) return 0;
-  if (bytes == Py_None) *n = (size_t)ask_int(ws, s_numel, &bad);
+  const size_t has = (size_t)ask_int(ws, s_numel, &bad);
+  if (bytes == Py_None) *n = has;
   else if (PyLong_Check(bytes)) *n = (size_t)PyLong_AsUnsignedLongLong(bytes);
   else return 0;
   if (PyErr_Occurred()) { PyErr_Clear(); return 0; }
+  if (*n > has) return 0;
   *out = data_of(ws, &bad);
   return !bad;
 }
@@ -207,7 +224,7 @@ static PyObject* m_norm_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     p[i] = &h[i];
   }
   void* pos;
-  if (!dense(a[1], t_i32, dev, 1, &pos) || tokens > 0x7fffffff) FALL_BACK;
+  if (!dense(a[1], t_i32, dev, 1, (double)tokens, &pos) || tokens > 0x7fffffff) FALL_BACK;
   if (pos != NULL) {
     int bad = 0;
     if (ask_int(a[1], s_numel, &bad) != tokens || bad) FALL_BACK;
@@ -225,7 +242,7 @@ static PyObject* m_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   const clsa_params* p = (const clsa_params*)struct_of(a[0], t_params, sizeof(*p), dev, 0);
   const clsa_cache8* c = (const clsa_cache8*)struct_of(a[1], t_cache, sizeof(*c), dev, 1);
   const clsa_norm_rope_spec* spec = a[2] == Py_None ? NULL : (const clsa_norm_rope_spec*)struct_of(a[2], t_spec, sizeof(*spec), dev, 1);
-  if (dev < 0 || p == NULL || c == NULL || (a[2] != Py_None && spec == NULL)) FALL_BACK;
+  if (dev < 0 || p == NULL || c == NULL || (a[2] != Py_None && spec == NULL) || !fits(a[1], p, a[3] != Py_None, a[5] != Py_None)) FALL_BACK;
   clsa_heads h[3];
   const clsa_heads* q[3] = {NULL, NULL, NULL};
   for (int i = 0; i < 3; ++i) {
@@ -252,11 +269,13 @@ static PyObject* m_scores(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   void *q, *sc, *ws;
   size_t bytes;
   clsa_stream s;
-  if (dev < 0 || p == NULL || c == NULL || !dense(a[2], t_bf16, dev, 0, &q) || !dense(a[3], t_f32, dev, 0, &sc) ||
-      !workspace_of(a[5], a[6], dev, &ws, &bytes) || !stream_of(a[7], dev, &s))
-    FALL_BACK;
   const int64_t stride = PyLong_AsLongLong(a[4]);
   if (PyErr_Occurred()) { PyErr_Clear(); FALL_BACK; }
+  if (dev < 0 || p == NULL || c == NULL || !fits(a[1], p, 0, 1)) FALL_BACK;
+  const double rows = (double)p->num_seqs * p->q_per_seq;
+  if (!dense(a[2], t_bf16, dev, 0, rows * p->idx_dim, &q) || !dense(a[3], t_f32, dev, 0, (rows - 1) * (double)stride + p->max_seq_len, &sc) ||
+      !workspace_of(a[5], a[6], dev, &ws, &bytes) || !stream_of(a[7], dev, &s))
+    FALL_BACK;
   RUN(f_scores(p, c, q, (float*)sc, stride, ws, bytes, s));
 }
 
@@ -271,9 +290,11 @@ static PyObject* m_attn(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   void *q, *idx, *count, *out, *lse, *ws;
   size_t bytes;
   clsa_stream s;
-  if (dev < 0 || p == NULL || c == NULL || (a[7] != Py_None && hints == NULL) || !dense(a[2], t_bf16, dev, 0, &q) ||
-      !dense(a[3], t_i32, dev, 0, &idx) || !dense(a[4], t_i32, dev, 0, &count) || !dense(a[5], t_bf16, dev, 0, &out) ||
-      !dense(a[6], t_f32, dev, 1, &lse) || !workspace_of(a[8], a[9], dev, &ws, &bytes) || !stream_of(a[10], dev, &s))
+  if (dev < 0 || p == NULL || c == NULL || (a[7] != Py_None && hints == NULL) || !fits(a[1], p, 1, 0)) FALL_BACK;
+  const double rows = (double)p->num_seqs * p->q_per_seq, heads = rows * p->num_q_heads;
+  if (!dense(a[2], t_bf16, dev, 0, heads * p->head_dim, &q) || !dense(a[3], t_i32, dev, 0, rows * p->top_k, &idx) ||
+      !dense(a[4], t_i32, dev, 0, rows, &count) || !dense(a[5], t_bf16, dev, 0, heads * p->head_dim, &out) ||
+      !dense(a[6], t_f32, dev, 1, heads, &lse) || !workspace_of(a[8], a[9], dev, &ws, &bytes) || !stream_of(a[10], dev, &s))
     FALL_BACK;
   RUN(f_attn(p, c, q, (const int32_t*)idx, (const int32_t*)count, out, (float*)lse, hints, ws, bytes, s));
 }
@@ -305,7 +326,7 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1,
 PyMODINIT_FUNC PyInit__marshal(void) {
   struct { PyObject** to; const char* name; } names[] = {
       {&s_dtype, "dtype"}, {&s_shape, "shape"}, {&s_stride, "stride"}, {&s_data_ptr, "data_ptr"}, {&s_get_device, "get_device"},
-      {&s_is_contiguous, "is_contiguous"}, {&s_numel, "numel"}, {&s__device, "_device"}, {&s_cuda_stream, "cuda_stream"}};
+      {&s_is_contiguous, "is_contiguous"}, {&s_numel, "numel"}, {&s__device, "_device"}, {&s__extent, "_extent"}, {&s_cuda_stream, "cuda_stream"}};
   for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
     if ((*names[i].to = PyUnicode_InternFromString(names[i].name)) == NULL) return NULL;
   return PyModule_Create(&module);

@@ -117,11 +117,87 @@ def binding(clsa, request, monkeypatch):
     cache8._load_torch()
 
 
+def _cache(clsa, rows=2048, heads=8, idx_dim=128):
+    u8 = lambda *s: torch.zeros(s, dtype=U8)  # noqa: E731
+    c = clsa.make_cache8(k=u8(rows, heads, 128), v=u8(rows, heads, 128), k_scale=u8(heads, rows // 64), v_scale=u8(heads, rows // 64),
+                         idx_k=u8(rows, idx_dim), idx_k_scale=u8(rows // 64), scale_block=64)
+    c._device = 0
+    return c
+
+
+def _params(clsa, **kw):
+    base = dict(num_seqs=2, q_per_seq=3, num_q_heads=32, num_kv_heads=8, head_dim=128, idx_dim=128, top_k=64, max_seq_len=1000, sm_scale=0.088,
+                seq_start=0x1000, seq_len=0x2000, num_cache_rows=2048)
+    base.update(kw)
+    return clsa.make_params(**base)
+
+
 def _taken(calls, name):
     """One call was made, by the native module where that is the one under test."""
     got = list(calls)
     calls.clear()
     return got in ([name], ["native " + name])
+
+
+def test_buffers_are_measured_against_the_params(binding):
+    clsa, calls = binding
+    p, c, ws = _params(clsa), _cache(clsa), Tensor((4096,), U8)
+    good = dict(q=Tensor((2, 3, 32, 128), BF16), idx=Tensor((2, 3, 64), I32), count=Tensor((2, 3), I32), out=Tensor((2, 3, 32, 128), BF16),
+                lse=Tensor((2, 3, 32), F32))
+    attn = lambda n=None, **kw: clsa.clsa_sparse_attn8(p, c, *[{**good, **kw}[x] for x in ("q", "idx", "count", "out", "lse")], None, ws, n)  # noqa: E731
+    for ok in ({}, dict(lse=None), dict(q=Tensor((7, 32, 128), BF16)), dict(n=4096), dict(n=256), dict(idx=Tensor((6 * 64,), I32))):
+        attn(**ok)
+        assert _taken(calls, "clsa_sparse_attn8"), ok
+    for bad in (dict(q=Tensor((2, 3, 31, 128), BF16)), dict(idx=Tensor((6, 63), I32)), dict(count=Tensor((5,), I32)), dict(out=Tensor((5, 32, 128), BF16)),
+                dict(lse=Tensor((6, 31), F32)), dict(n=4097)):
+        with pytest.raises(ValueError):
+            attn(**bad)
+    scores = lambda q, s, n: clsa.clsa_index_scores8(p, c, q, s, n, ws)  # noqa: E731
+    q = Tensor((2, 3, 128), BF16)
+    for s, n in ((Tensor((2, 3, 1024), F32), 1024), (Tensor((2, 3, 1000), F32, (3072 + 24, 1032, 1)), 1032), (Tensor((5 * 1024 + 1000,), F32), 1024)):
+        scores(q, s, n)
+        assert _taken(calls, "clsa_index_scores8")
+    for q_, s, n in ((Tensor((5, 128), BF16), Tensor((2, 3, 1024), F32), 1024), (q, Tensor((2, 3, 1000), F32), 1024), (q, Tensor((5 * 1024 + 999,), F32), 1024),
+                     (q, Tensor((2, 3, 999), F32, (3072 + 24, 1032, 1)), 1032), (q, Tensor((5, 1024), F32), 1024)):
+        with pytest.raises(ValueError):
+            scores(q_, s, n)
+    assert not calls
+
+
+def test_caches_are_measured_against_the_params(binding):
+    clsa, calls = binding
+    ws, p = Tensor((4096,), U8), _params(clsa)
+
+    def each(p, c):
+        q, s = Tensor((2, 3, p.num_q_heads, 128), BF16), Tensor((2, 3, 1024), F32)
+        new, idx = Tensor((2, 3, p.num_kv_heads, 128), BF16), Tensor((2, 3, p.idx_dim), BF16)
+        return dict(kv=[lambda: clsa.clsa_cache8_append(p, c, None, new, new, None, ws),
+                        lambda: clsa.clsa_sparse_attn8(p, c, q, Tensor((6, 64), I32), Tensor((6,), I32), q, None, None, ws)],
+                    idx=[lambda: clsa.clsa_cache8_append(p, c, None, None, None, idx, ws), lambda: clsa.clsa_index_scores8(p, c, idx, s, 1024, ws)])
+
+    def refused(p, c, which):
+        for call in which:
+            with pytest.raises(ValueError):
+                call()
+        assert not calls
+
+    for c in (_cache(clsa), _cache(clsa, rows=4096), _cache(clsa, heads=9)):
+        for call in sum(each(p, c).values(), []):
+            call()
+            assert len(calls) == 1
+            calls.clear()
+    for c in (_cache(clsa, rows=2048 - 64),):
+        refused(p, c, each(p, c)["kv"] + each(p, c)["idx"])
+    c = _cache(clsa, heads=7)
+    refused(p, c, each(p, c)["kv"])
+    c = _cache(clsa, idx_dim=64)
+    refused(p, c, each(p, c)["idx"])
+    # a cache described by addresses has no sizes to compare
+    c = clsa.clsa_cache8(0x10000, 0x20000, 0x30000, 0x40000, 1024, 128, 64, 0x50000, 0x60000, 128, 64)
+    for call in sum(each(p, c).values(), []):
+        call()
+        assert len(calls) == 1
+        calls.clear()
 
 
 def test_empty_tensors_are_taken(binding):

@@ -169,3 +169,41 @@ def test_empty_batches_do_nothing():
         clsa.clsa_norm_rope(spec, pos, q, q)
         clsa.clsa_norm_rope(spec, pos, torch.empty((*shape[:-2], 12, 128), dtype=BF16, device=DEV)[..., 2:10, :], q)  # another layout
         clsa.clsa_norm_rope(spec, pos, None, None, q, torch.empty_like(q))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_buffers_that_are_too_small_are_refused(native, monkeypatch):
+    from paper_2606_06467_b200 import cache8
+
+    if native:
+        assert cache8._marshal is not None
+    else:
+        monkeypatch.setattr(cache8, "_marshal", None)
+    c = Cache([100, 90], 3, 2, 64, 16, 0, seed=1)
+    c.params(hq=8, top_k=40)
+    z = lambda *s, dtype=BF16: torch.zeros(s, dtype=dtype, device=DEV)  # noqa: E731
+    i32, f32, W = torch.int32, torch.float32, 128
+    good = dict(q=z(2, 3, 8, 128), idx=z(2, 3, 40, dtype=i32), count=z(2, 3, dtype=i32), out=z(2, 3, 8, 128), lse=z(2, 3, 8, dtype=f32))
+    attn = lambda p=c.p, cache=c.cache, ws=c.ws, n=None, **kw: clsa.clsa_sparse_attn8(  # noqa: E731
+        p, cache, *[{**good, **kw}[x] for x in ("q", "idx", "count", "out", "lse")], None, ws, n)
+    attn()
+    for kw in (dict(q=z(2, 3, 7, 128)), dict(idx=z(2, 3, 39, dtype=i32)), dict(count=z(5, dtype=i32)), dict(out=z(2, 2, 8, 128)), dict(lse=z(47, dtype=f32)),
+               dict(n=c.ws.numel() + 1)):
+        with pytest.raises(ValueError):
+            attn(**kw)
+    qi, s = z(2, 3, 64), z(2, 3, W, dtype=f32)
+    clsa.clsa_index_scores8(c.p, c.cache, qi, s, W, c.ws)
+    clsa.clsa_index_scores8(c.p, c.cache, qi, s[:, :, :100], W, c.ws)  # a view of rows W apart
+    for args in ((z(2, 2, 64), s, W), (qi, s, W + 30), (qi, z(2, 3, 99, dtype=f32), 100), (qi, s[:, :2], W)):
+        with pytest.raises(ValueError):
+            clsa.clsa_index_scores8(c.p, c.cache, *args, c.ws)
+    # a cache of fewer rows, heads or dimensions than the params name
+    new, ni = z(2, 3, 2, 128), z(2, 3, 64)
+    clsa.clsa_cache8_append(c.p, c.cache, None, new, new, ni, c.ws)
+    for kw in (dict(num_cache_rows=c.rows + 1), dict(num_kv_heads=4), dict(idx_dim=128)):
+        p = c.params(hq=8, top_k=40, **kw)
+        with pytest.raises(ValueError):
+            clsa.clsa_cache8_append(p, c.cache, None, z(2, 3, p.num_kv_heads, 128), z(2, 3, p.num_kv_heads, 128), z(2, 3, p.idx_dim), c.ws)
+        with pytest.raises(ValueError):
+            attn(p=p) if "idx_dim" not in kw else clsa.clsa_index_scores8(p, c.cache, z(2, 3, 128), s, W, c.ws)
+    assert c.status() == 0
