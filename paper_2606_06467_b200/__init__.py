@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libclsa.so")
@@ -28,6 +29,8 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 class clsa_params(ctypes.Structure):
     """Mirror of `clsa_params` in include/clsa.h (same field order and types)."""
+
+    _made = None  # what seq_start, seq_len and block_table were made of: see _described
 
     _fields_ = [
         ("num_seqs", ctypes.c_int32), ("q_per_seq", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
@@ -116,6 +119,22 @@ def _nbytes(ws, ws_bytes):
     return ws.numel() * ws.element_size()
 
 
+def _described(t, dtype, step):
+    """(address, sequences that it describes, device) of a tensor with `step` elements of `dtype` for each sequence: 0 sequences
+    where it holds anything else, no device for pinned host memory, which every device reads. None for what is no tensor."""
+    torch = sys.modules.get("torch")
+    if torch is None or not isinstance(t, torch.Tensor):
+        return None
+    seqs = 0
+    if t.dtype == getattr(torch, dtype):
+        if t.is_contiguous():
+            seqs = t.numel() // max(step, 1)
+        elif t.dim() == 2 and t.stride() == (step, 1):
+            seqs = t.shape[0]
+    device = t.get_device()
+    return t.data_ptr(), seqs, None if device < 0 and t.is_pinned() else device
+
+
 def make_params(*, num_seqs, q_per_seq=1, num_q_heads, num_kv_heads, head_dim=128, idx_dim, top_k, num_layers=1,
                 causal=0, max_seq_len, sm_scale, seq_start=None, seq_len=None, k_cache=None, v_cache=None,
                 kv_token_stride=None, kv_head_stride=None, idx_k_cache=None, idx_token_stride=None,
@@ -143,6 +162,7 @@ def make_params(*, num_seqs, q_per_seq=1, num_q_heads, num_kv_heads, head_dim=12
     if max_blocks_per_seq is None and block_table is not None and not isinstance(block_table, int):
         max_blocks_per_seq = block_table.shape[1]
     p.max_blocks_per_seq = max_blocks_per_seq or 0
+    p._made = (_described(seq_start, "int64", 1), _described(seq_len, "int32", 1), _described(block_table, "int32", p.max_blocks_per_seq))
     return p
 
 

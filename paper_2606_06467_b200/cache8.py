@@ -37,7 +37,8 @@ class clsa_cache8(ctypes.Structure):
     """Mirror of `clsa_cache8` in include/clsa_cache8.h."""
 
     _device = None  # where the tensors behind it lie, if it was made of tensors
-    _extent = None  # and what they hold: rows, heads and dimension of K and V, rows and dimension of K_idx (0: there are none)
+    _extent = None  # and what they hold: rows, heads and dimension of K and V, rows and dimension of K_idx (0: there are none), and
+    # the addresses of K and K_idx that this is true of
 
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("kv_token_stride", _i64),
                 ("kv_head_stride", _i64), ("scale_head_stride", _i64), ("idx_k", _vp), ("idx_k_scale", _vp),
@@ -83,11 +84,24 @@ def _fits(p, c, kv, idx):
     """Refuse params that name more of a cache than its tensors hold."""
     if c._extent is None:
         return
-    rows, heads, dim, idx_rows, idx_dim = c._extent
-    if kv and heads and (p.num_cache_rows > rows or p.num_kv_heads > heads or p.head_dim > dim):
+    rows, heads, dim, idx_rows, idx_dim, k, idx_k = c._extent
+    if kv and heads and c.k == k and (p.num_cache_rows > rows or p.num_kv_heads > heads or p.head_dim > dim):
         raise ValueError(f"the params name {p.num_cache_rows} rows of {p.num_kv_heads} heads of {p.head_dim}, K and V hold {rows} of {heads} of {dim}")
-    if idx and idx_dim and (p.num_cache_rows > idx_rows or p.idx_dim > idx_dim):
+    if idx and idx_dim and c.idx_k == idx_k and (p.num_cache_rows > idx_rows or p.idx_dim > idx_dim):
         raise ValueError(f"the params name {p.num_cache_rows} rows of {p.idx_dim}, K_idx holds {idx_rows} of {idx_dim}")
+
+
+def _describes(p, device):
+    """Refuse params made of tensors that describe fewer sequences than they name or lie elsewhere (what has been given another address
+    since is not looked at)."""
+    if p._made is None:
+        return
+    for what, made, now in zip(("seq_start", "seq_len", "block_table"), p._made, (p.seq_start, p.seq_len, p.block_table)):
+        if made is None or made[0] != now or what == "seq_start" and p.block_table:
+            continue
+        if made[1] < p.num_seqs or made[2] not in (None, device):
+            kind = {"seq_start": "int64", "seq_len": "int32"}.get(what, f"int32 [.., {p.max_blocks_per_seq}]")
+            raise ValueError(f"{what}: contiguous {kind} values for {p.num_seqs} sequences on the current CUDA device are wanted")
 
 
 def _workspace(ws, ws_bytes, made, device):
@@ -171,7 +185,6 @@ def make_cache8(*, k=None, v=None, k_scale=None, v_scale=None, idx_k=None, idx_k
     c = clsa_cache8()
     c._tensors = (k, v, k_scale, v_scale, idx_k, idx_k_scale)
     c._device = _device_of(*c._tensors)
-    c._extent = (*((0, 0, 0) if k is None else k.shape), *((0, 0) if idx_k is None else idx_k.shape))
     c.scale_block = scale_block
     if k is not None or v is not None:
         for t, what in ((k, "k"), (v, "v")):
@@ -195,6 +208,7 @@ def make_cache8(*, k=None, v=None, k_scale=None, v_scale=None, idx_k=None, idx_k
               and idx_k_scale.numel() * scale_block >= idx_k.shape[0], "idx_k_scale: [blocks] bytes for every row is wanted")
         _bytes_like(idx_k_scale, "idx_k_scale", ("float8_e8m0fnu",))
         c.idx_k, c.idx_k_scale, c.idx_token_stride = _ptr(idx_k), _ptr(idx_k_scale), idx_k.stride(0)
+    c._extent = (*((0, 0, 0) if k is None else k.shape), *((0, 0) if idx_k is None else idx_k.shape), c.k or 0, c.idx_k or 0)
     return c
 
 
@@ -268,6 +282,7 @@ def clsa_cache8_append(p, c, spec, k_new, v_new, idx_k_new, workspace, workspace
         raise ValueError("k_new with v_new, idx_k_new, or all three are wanted")
     dev, bf16, n = _device(torch), torch.bfloat16, p.num_seqs * p.q_per_seq
     k = v = i = None
+    _describes(p, dev)
     _fits(p, c, k_new is not None, idx_k_new is not None)
     if k_new is not None:
         k, _, _ = _heads(k_new, "k_new", dev, bf16, n, p.num_kv_heads, p.head_dim)
@@ -288,6 +303,7 @@ def clsa_index_scores8(p, c, q_idx, scores, score_stride, workspace, workspace_b
     if status is not None:
         return _check(status, "clsa_index_scores8") if status else None
     dev, n = _device(torch), p.num_seqs * p.q_per_seq
+    _describes(p, dev)
     _fits(p, c, False, True)
     ws, nbytes = _workspace(workspace, workspace_bytes, (c,), dev)
     status = _lib.clsa_index_scores8(ctypes.byref(p), ctypes.byref(c), _dense(q_idx, "q_idx", torch.bfloat16, dev, n * p.idx_dim),
@@ -305,6 +321,7 @@ def clsa_sparse_attn8(p, c, q, idx, count, out, lse, hints, workspace, workspace
         return _check(status, "clsa_sparse_attn8") if status else None
     dev, i32, bf16, n = _device(torch), torch.int32, torch.bfloat16, p.num_seqs * p.q_per_seq
     heads = n * p.num_q_heads
+    _describes(p, dev)
     _fits(p, c, True, False)
     ws, nbytes = _workspace(workspace, workspace_bytes, (c,), dev)
     status = _lib.clsa_sparse_attn8(ctypes.byref(p), ctypes.byref(c), _dense(q, "q", bf16, dev, heads * p.head_dim),

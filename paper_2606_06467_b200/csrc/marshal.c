@@ -26,7 +26,7 @@ static scores_fn f_scores;
 static attn_fn f_attn;
 static PyObject *t_tensor, *t_bf16, *t_i32, *t_f32, *t_u8, *g_device, *g_stream;  /* torch's: type, dtypes, two functions */
 static PyObject *t_params, *t_cache, *t_spec, *t_hints; /* cache8.py's structs */
-static PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_is_contiguous, *s_numel, *s__device, *s__extent, *s_cuda_stream;
+static PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_is_contiguous, *s_numel, *s__device, *s__extent, *s__made, *s_cuda_stream;
 
 /* What a call needs of a tensor. */
 typedef struct {
@@ -141,17 +141,37 @@ static const void* struct_of(PyObject* s, PyObject* type, Py_ssize_t bytes, int6
   return p;
 }
 /* Whether a cache's tensors, if it was made of tensors, hold what the params name of K and V, and of K_idx. */
-static int fits(PyObject* cache, const clsa_params* p, int kv, int idx) {
-  int64_t e[5]; /* rows, heads, dimension; rows and dimension of K_idx */
+static int fits(PyObject* cache, const clsa_cache8* c, const clsa_params* p, int kv, int idx) {
+  int64_t e[7]; /* rows, heads, dimension; rows and dimension of K_idx; addresses of K and K_idx */
   PyObject* t = PyObject_GetAttr(cache, s__extent);
   if (t == NULL) { PyErr_Clear(); return 0; }
   int ok = t == Py_None;
-  if (!ok && PyTuple_Check(t) && PyTuple_GET_SIZE(t) == 5) {
-    for (int i = 0; i < 5; ++i) e[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+  if (!ok && PyTuple_Check(t) && PyTuple_GET_SIZE(t) == 7) {
+    for (int i = 0; i < 7; ++i) e[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+    kv = kv && (int64_t)(uintptr_t)c->k == e[5];
+    idx = idx && (int64_t)(uintptr_t)c->idx_k == e[6];
     ok = !PyErr_Occurred() && !(kv && e[1] > 0 && (p->num_cache_rows > e[0] || p->num_kv_heads > e[1] || p->head_dim > e[2])) &&
          !(idx && e[4] > 0 && (p->num_cache_rows > e[3] || p->idx_dim > e[4]));
     PyErr_Clear();
   }
+  Py_DECREF(t);
+  return ok;
+}
+/* Whether the tensors that the params were made of describe all their sequences and lie on the device. */
+static int describes(PyObject* params, const clsa_params* p, int64_t device) {
+  const void* now[3] = {p->block_table == NULL ? p->seq_start : NULL, p->seq_len, p->block_table};
+  PyObject* t = PyObject_GetAttr(params, s__made);
+  if (t == NULL) { PyErr_Clear(); return 0; }
+  int ok = t == Py_None || (PyTuple_Check(t) && PyTuple_GET_SIZE(t) == 3);
+  for (int i = 0; i < 3 && ok && t != Py_None; ++i) {
+    PyObject* m = PyTuple_GET_ITEM(t, i); /* address, sequences, device or None */
+    if (m == Py_None) continue;
+    ok = PyTuple_Check(m) && PyTuple_GET_SIZE(m) == 3;
+    if (!ok || now[i] == NULL || PyLong_AsLongLong(PyTuple_GET_ITEM(m, 0)) != (int64_t)(uintptr_t)now[i]) continue;
+    PyObject* d = PyTuple_GET_ITEM(m, 2);
+    ok = PyLong_AsLongLong(PyTuple_GET_ITEM(m, 1)) >= p->num_seqs && (d == Py_None || PyLong_AsLongLong(d) == device);
+  }
+  if (PyErr_Occurred()) { PyErr_Clear(); ok = 0; }
   Py_DECREF(t);
   return ok;
 }
@@ -242,7 +262,7 @@ static PyObject* m_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   const clsa_params* p = (const clsa_params*)struct_of(a[0], t_params, sizeof(*p), dev, 0);
   const clsa_cache8* c = (const clsa_cache8*)struct_of(a[1], t_cache, sizeof(*c), dev, 1);
   const clsa_norm_rope_spec* spec = a[2] == Py_None ? NULL : (const clsa_norm_rope_spec*)struct_of(a[2], t_spec, sizeof(*spec), dev, 1);
-  if (dev < 0 || p == NULL || c == NULL || (a[2] != Py_None && spec == NULL) || !fits(a[1], p, a[3] != Py_None, a[5] != Py_None)) FALL_BACK;
+  if (dev < 0 || p == NULL || c == NULL || (a[2] != Py_None && spec == NULL) || !describes(a[0], p, dev) || !fits(a[1], c, p, a[3] != Py_None, a[5] != Py_None)) FALL_BACK;
   clsa_heads h[3];
   const clsa_heads* q[3] = {NULL, NULL, NULL};
   for (int i = 0; i < 3; ++i) {
@@ -271,7 +291,7 @@ static PyObject* m_scores(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   clsa_stream s;
   const int64_t stride = PyLong_AsLongLong(a[4]);
   if (PyErr_Occurred()) { PyErr_Clear(); FALL_BACK; }
-  if (dev < 0 || p == NULL || c == NULL || !fits(a[1], p, 0, 1)) FALL_BACK;
+  if (dev < 0 || p == NULL || c == NULL || !describes(a[0], p, dev) || !fits(a[1], c, p, 0, 1)) FALL_BACK;
   const double rows = (double)p->num_seqs * p->q_per_seq;
   if (!dense(a[2], t_bf16, dev, 0, rows * p->idx_dim, &q) || !dense(a[3], t_f32, dev, 0, (rows - 1) * (double)stride + p->max_seq_len, &sc) ||
       !workspace_of(a[5], a[6], dev, &ws, &bytes) || !stream_of(a[7], dev, &s))
@@ -290,7 +310,7 @@ static PyObject* m_attn(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   void *q, *idx, *count, *out, *lse, *ws;
   size_t bytes;
   clsa_stream s;
-  if (dev < 0 || p == NULL || c == NULL || (a[7] != Py_None && hints == NULL) || !fits(a[1], p, 1, 0)) FALL_BACK;
+  if (dev < 0 || p == NULL || c == NULL || (a[7] != Py_None && hints == NULL) || !describes(a[0], p, dev) || !fits(a[1], c, p, 1, 0)) FALL_BACK;
   const double rows = (double)p->num_seqs * p->q_per_seq, heads = rows * p->num_q_heads;
   if (!dense(a[2], t_bf16, dev, 0, heads * p->head_dim, &q) || !dense(a[3], t_i32, dev, 0, rows * p->top_k, &idx) ||
       !dense(a[4], t_i32, dev, 0, rows, &count) || !dense(a[5], t_bf16, dev, 0, heads * p->head_dim, &out) ||
@@ -326,7 +346,7 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1,
 PyMODINIT_FUNC PyInit__marshal(void) {
   struct { PyObject** to; const char* name; } names[] = {
       {&s_dtype, "dtype"}, {&s_shape, "shape"}, {&s_stride, "stride"}, {&s_data_ptr, "data_ptr"}, {&s_get_device, "get_device"},
-      {&s_is_contiguous, "is_contiguous"}, {&s_numel, "numel"}, {&s__device, "_device"}, {&s__extent, "_extent"}, {&s_cuda_stream, "cuda_stream"}};
+      {&s_is_contiguous, "is_contiguous"}, {&s_numel, "numel"}, {&s__device, "_device"}, {&s__extent, "_extent"}, {&s__made, "_made"}, {&s_cuda_stream, "cuda_stream"}};
   for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
     if ((*names[i].to = PyUnicode_InternFromString(names[i].name)) == NULL) return NULL;
   return PyModule_Create(&module);

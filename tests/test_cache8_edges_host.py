@@ -192,6 +192,13 @@ def test_caches_are_measured_against_the_params(binding):
     refused(p, c, each(p, c)["kv"])
     c = _cache(clsa, idx_dim=64)
     refused(p, c, each(p, c)["idx"])
+    c = _cache(clsa, rows=64)  # another buffer's address since: nothing is known of it
+    c.k, c.idx_k = 0x10000, 0x50000
+    c.scale_head_stride = 64
+    for call in sum(each(p, c).values(), []):
+        call()
+        assert len(calls) == 1
+        calls.clear()
     # a cache described by addresses has no sizes to compare
     c = clsa.clsa_cache8(0x10000, 0x20000, 0x30000, 0x40000, 1024, 128, 64, 0x50000, 0x60000, 128, 64)
     for call in sum(each(p, c).values(), []):
@@ -209,3 +216,40 @@ def test_empty_tensors_are_taken(binding):
         assert _taken(calls, "clsa_norm_rope"), shape
         clsa.clsa_norm_rope(spec, Tensor((0,), I32), None, None, q, q)
         assert _taken(calls, "clsa_norm_rope"), shape
+
+
+def test_the_params_own_tensors_are_measured(binding):
+    """seq_start, seq_len and the block table: types, layouts, how many sequences they describe, where they lie."""
+    clsa, calls = binding
+    ws, c = Tensor((4096,), U8), clsa.clsa_cache8(0x10000, 0x20000, 0x30000, 0x40000, 1024, 128, 64, 0x50000, 0x60000, 128, 64)
+    heads, idx, s = Tensor((2, 3, 8, 128), BF16), Tensor((2, 3, 128), BF16), Tensor((2, 3, 1024), F32)
+    q = Tensor((2, 3, 32, 128), BF16)
+    each = (lambda p: clsa.clsa_cache8_append(p, c, None, heads, heads, idx, ws), lambda p: clsa.clsa_index_scores8(p, c, idx, s, 1024, ws),
+            lambda p: clsa.clsa_sparse_attn8(p, c, q, Tensor((6, 64), I32), Tensor((6,), I32), q, None, None, ws))
+    zeros = lambda *shape, dtype=I32: torch.zeros(shape, dtype=dtype)  # noqa: E731
+    here = lambda p: setattr(p, "_made", tuple(m and (*m[:2], 0) for m in p._made)) or p  # noqa: E731  (host tensors as if on device 0)
+    start, length, table = zeros(2, dtype=torch.int64), zeros(2), zeros(2, 16)
+    paged = dict(block_size=64, max_seq_len=1000)
+    good = [dict(seq_start=start, seq_len=length), dict(seq_start=zeros(9, dtype=torch.int64), seq_len=zeros(2, 1)), dict(seq_len=length, seq_start=0x1000),
+            dict(seq_start=None, seq_len=length, block_table=table, **paged),
+            dict(seq_start=None, seq_len=length, block_table=zeros(2, 20)[:, :16], max_blocks_per_seq=20, **paged),
+            dict(seq_start=zeros(1), seq_len=length, block_table=table, **paged)]  # with pages the starts are not read
+    for kw in good:
+        for call in each:
+            call(here(_params(clsa, **kw)))
+            assert len(calls) == 1, kw
+            calls.clear()
+    bad = [dict(seq_len=zeros(2, dtype=torch.int64)), dict(seq_len=zeros(1)), dict(seq_len=zeros(2, 2)[:, 0]), dict(seq_start=zeros(2)),
+           dict(seq_start=zeros(1, dtype=torch.int64)), dict(block_table=zeros(1, 16), **paged), dict(block_table=zeros(2, 16, dtype=torch.int64), **paged),
+           dict(block_table=zeros(2, 20)[:, :16], **paged)]
+    for kw in bad:
+        for call in each:
+            with pytest.raises(ValueError):
+                call(here(_params(clsa, **kw)))
+    for call in each:
+        with pytest.raises(ValueError):
+            call(_params(clsa, seq_len=length))  # host memory
+    p = _params(clsa, seq_len=zeros(1))
+    p.seq_len = 0x2000  # another buffer since
+    each[0](p)
+    assert len(calls) == 1
