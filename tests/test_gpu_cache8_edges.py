@@ -160,6 +160,127 @@ def test_sparse_attn_logits_far_below_zero():
     assert (np.abs(f64(out[0, 0, 0]) - v) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(v)).all()
 
 
+def test_queries_that_are_not_finite():
+    """An infinity or a NaN in a query row shows in that row's results and in no others."""
+    c = Cache([200, 200], 2, 2, 128, 16, 0, seed=5)
+    c.params(hq=8, top_k=64)
+    c.idx[(c.idx & 127) == 0] = 1  # no zero codes: an infinity times zero is a NaN
+    qi = randn(gen(1), 2, 2, 128)
+    clean = run_scores(c, qi, 0)
+    qi[0, 0, 5], qi[1, 1, 9] = float("inf"), float("nan")
+    s = run_scores(c, qi, 0)
+    code, _ = c.host()[2]
+    sign = np.where(code[c.row(0, np.arange(200)), 0, 5] & 128, -np.inf, np.inf)
+    np.testing.assert_array_equal(s[0, 0, :200].cpu().numpy(), sign)
+    assert torch.isnan(s[1, 1, :200]).all()
+    assert torch.equal(s[0, 1, :200], clean[0, 1, :200]) and torch.equal(s[1, 0, :200], clean[1, 0, :200])
+    q = randn(gen(2), 2, 2, 8, 128)
+    idx, cnt = make_index(c, 64, 0, 1)
+    clean, lse0 = run_attn(c, q, idx, cnt)
+    q[0, 1, 3, 7], q[1, 0, 6, 100] = float("nan"), float("inf")
+    out, lse = run_attn(c, q, idx, cnt)
+    hit = torch.zeros((2, 2, 8), dtype=torch.bool, device=DEV)
+    hit[0, 1, 3] = hit[1, 0, 6] = True
+    assert torch.isnan(out[hit]).all() and torch.isnan(lse[0, 1, 3])
+    unit = hit.view(2, 2, 2, 4).any(-1, keepdim=True).expand(2, 2, 2, 4).reshape(2, 2, 8)  # heads that share a KV head share references
+    assert torch.equal(out[~unit], clean[~unit]) and torch.equal(lse[~unit], lse0[~unit])
+    q[hit] = 0
+    out[hit], lse[hit] = run_attn(c, q, idx, cnt)[0][hit], run_attn(c, q, idx, cnt)[1][hit]
+    check_attn(c, 8, q, idx, cnt, out, lse)
+
+
+def test_index_scores_of_more_sequences_than_lengths_fit_in_shared_memory():
+    lens = [1 + (7 * b) % 40 for b in range(2100)]
+    c = Cache(lens, 1, 1, 64, 16, 0, seed=1, capacity=48)
+    c.params()
+    q = randn(gen(1), 2100, 1, 64)
+    s = run_scores(c, q, 0)
+    assert c.status() == 0
+    code, sc = c.host()[2]
+    vals = ref.values(code, sc, 16)[:, 0]
+    got, qh, start = s[:, 0].cpu().double().numpy(), f64(q[:, 0]), c.start.cpu().numpy()
+    for b in range(2100):
+        want, mag = ref.scores(qh[b:b + 1], vals[start[b]:start[b] + lens[b]])
+        assert (np.abs(got[b, :lens[b]] - want[0]) <= 2.0 ** -16 * mag[0]).all() and np.isnan(got[b, lens[b]:]).all(), b
+    for change, bit in ((lambda: c.seq_len.__setitem__(2077, 49), clsa.CLSA_DEV_BAD_SEQLEN), (lambda: c.start.__setitem__(2099, 24), clsa.CLSA_DEV_BAD_SCALE_BLOCK)):
+        change()
+        again = run_scores(c, q, 0)
+        assert c.status() == bit
+        bad = 2077 if bit == clsa.CLSA_DEV_BAD_SEQLEN else 2099
+        keep = [b for b in range(2100) if b != bad]
+        assert torch.equal(again[keep].nan_to_num(7.0), s[keep].nan_to_num(7.0)) and torch.isnan(again[bad]).all()
+        clsa.clsa_clear_status(c.ws)
+        c.seq_len[2077] = lens[2077]
+
+
+@pytest.mark.parametrize("hq", [4, 16])
+def test_sparse_attn_of_a_row_over_more_than_32_blocks(hq):
+    """One KV head's 27000 selected rows: the blocks' partials are joined in two rounds."""
+    c = Cache([30000], 1, 1, 64, 64, 64, seed=2)
+    c.params(hq=hq, top_k=27000)
+    q = randn(gen(1), 1, 1, hq, 128)
+    for counts in ([27000], [13001], [1]):
+        idx, cnt = make_index(c, 27000, 0, 3, counts=counts)
+        out, lse = run_attn(c, q, idx, cnt)
+        check_attn(c, hq, q, idx, cnt, out, lse)
+        o2, l2 = run_attn(c, q, idx, cnt, clsa.make_hints(reverse=1))
+        check_attn(c, hq, q, idx, cnt, o2, l2)
+    assert c.status() == 0
+
+
+@pytest.mark.parametrize("extra", [1, 4, 5])
+def test_index_scores_of_a_chunk_with_odd_strides(extra):
+    """More than 32 query tokens, rows of scores that are not 32-byte aligned."""
+    c = Cache([517, 300], 40, 1, 128, 64, 64, seed=4)
+    c.params(causal=1)
+    q = randn(gen(1), 2, 40, 128)
+    stride = 520 + extra
+    s = torch.full((2, 40, stride), float("nan"), device=DEV)
+    clsa.clsa_index_scores8(c.p, c.cache, q, s, stride, c.ws)
+    check_scores(c, q, s, 1)
+    assert c.status() == 0
+
+
+@pytest.mark.parametrize("T", [1, 300])
+def test_append_of_indexer_keys_alone_leaves_k_and_v(T):
+    c = Cache([300 + 7 * b for b in range(40)], T, 4, 64, 16, 16, seed=2)
+    c.params()
+    i = randn(gen(1), c.B, T, 64)
+    before = c.host()
+    clsa.clsa_cache8_append(c.p, c.cache, None, None, None, i, c.ws)
+    after = c.host()
+    for w in (0, 1):
+        assert all((x == y).all() for x, y in zip(before[w], after[w]))
+    code, sc = before[2]
+    for b in range(c.B):
+        ref.append(code, sc, lambda s, b=b: int(c.row(b, s)), c.lens[b], f64(i[b])[:, None], 16)
+    np.testing.assert_array_equal(after[2][0], code)
+    np.testing.assert_array_equal(after[2][1], sc)
+
+
+@pytest.mark.parametrize("rot,inter", [(128, 0), (64, 0), (128, 1)])
+@pytest.mark.parametrize("T,norm", [(1, 0), (1, 1), (70, 0), (70, 1)])
+def test_append_with_a_scaled_rotation(rot, inter, T, norm):
+    c = Cache([200, 131], T, 3, 64, 64, 0, seed=T)
+    c.params()
+    freq = (10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)).float().to(DEV)
+    spec = clsa.make_norm_rope(head_dim=128, norm=norm, eps=1e-6, rot_dim=rot, interleaved=inter, inv_freq=freq, rot_scale=1.375)
+    k, v = randn(gen(1), 2, T, 3, 128), randn(gen(2), 2, T, 3, 128)
+    code, sc = c.host()[0]
+    clsa.clsa_cache8_append(c.p, c.cache, spec, k, v, None, c.ws)
+    got, gsc = c.host()[0]
+    for b in range(2):
+        pos = np.arange(c.lens[b] - T, c.lens[b])
+        x, mag = ref.norm_rope(f64(k[b]), pos, None, norm, np.float32(1e-6).astype(np.float64), freq.cpu().numpy(), inter, 1.375)
+        done = ref.append(code, sc, lambda s, b=b: int(c.row(b, s)), c.lens[b], x, 64)
+        rows = c.row(b, pos)
+        for (home, h), e in done.items():
+            mine = np.array([s for s in range(T) if home <= rows[s] < home + 64])
+            err = np.abs(ref.E4M3[got[rows[mine], h]] * 2.0 ** e - x[mine, h])
+            assert (err <= ref.half_step(x[mine, h], e) + 2.0 ** -19 * mag[mine, h]).all()
+    np.testing.assert_array_equal(gsc, sc)
+
+
 def test_empty_batches_do_nothing():
     freq = torch.ones(64, device=DEV)
     spec = clsa.make_norm_rope(head_dim=128, norm=1, rot_dim=128, inv_freq=freq)
