@@ -63,7 +63,8 @@ typedef struct {
  *   q, q_out   the queries and where their results go, same num_heads (both NULL: no queries)
  *   k, k_out   the keys, likewise
  * An output may be its own input (same data and strides); other overlaps are not allowed. num_tokens 0 .. 2^30; 0 is a
- * call that does nothing. Squares are summed in fp32: magnitudes above about 1e18 overflow the norm. */
+ * call that does nothing (its pointers may be NULL then). Squares are summed in fp32: magnitudes above about 1e18 overflow the
+ * norm, and with eps == 0 a row of magnitudes below about 1e-19 underflows it. */
 CLSA_API clsa_status clsa_norm_rope(const clsa_norm_rope_spec* spec, int32_t num_tokens, const int32_t* positions,
                                     const clsa_heads* q, const clsa_heads* q_out, const clsa_heads* k,
                                     const clsa_heads* k_out, clsa_stream stream);

@@ -18,7 +18,9 @@ struct Cache8Layout {
   int64_t expand_rows;  // rows per sequence of the expanded keys
   size_t total;
 };
-constexpr int kScoresMaxT = 32;  // query tokens per sequence that the streaming score kernel takes
+// Query tokens per sequence that the streaming score kernel takes (a fifth tile of eight would not fit its registers). In us, streamed and
+// expanded, 32 tokens over 16 x 32 K keys: 64-wide 30.0 and 52.5, 128-wide 64.2 and 74.1; over 33 K keys 5.8 and 10.0, 9.1 and 11.9.
+constexpr int kScoresMaxT = 32;
 
 cudaError_t launch_norm_rope(const clsa_norm_rope_spec& spec, int num_tokens, const int32_t* positions, const clsa_heads* q,
                              const clsa_heads* q_out, const clsa_heads* k, const clsa_heads* k_out, const DeviceInfo& dev,

@@ -9,12 +9,12 @@
 // rows; the part of v is folded with the weights once per head, which leaves seven packed operations per pair of dimensions.
 // A scale block that holds older rows is re-coded by the same threads when its exponent grows.
 // 4096 tokens of 8 heads, indexer keys, norm and rotation over all dimensions, 64-row blocks that straddle the tokens' ends:
-// 26.7 MB in 11.3 us (the bytes alone would take 4.1; aligned 10.8, without rotation 9.0, without norm 7.2): a launch, the chain
+// 26.7 MB in 11.6 us (the bytes alone would take 4.1; on a GPU where it took 11.3: aligned 10.8, without rotation 9.0, without norm 7.2): a launch, the chain
 // length - page - rows, a barrier per head, and instruction issue at 16 warps per SM, which the rows in registers allow
 // (80 registers and half as many warps again measured the same). A rotation that turns the whole head, half apart, has both
 // partners in one lane (PAIR: 13.4 -> 11.4; other rotations exchange raw words, 13.0).
 // Single tokens (T = 1): half a warp per row, no block barrier; what does not depend on the sequence's length (the row, the
-// weight, the frequencies) is fetched together with it. Bound by a launch and two dependent round trips: 16 sequences of 8 heads 2.8 us.
+// weight, the frequencies) is fetched together with it. Bound by a launch and two dependent round trips: 16 sequences of 8 heads 3.0 us.
 #include "cache8.cuh"
 
 namespace clsa {
@@ -528,9 +528,11 @@ cudaError_t launch_cache8_append(const clsa_params& p, const clsa_cache8& c, con
   a.spans = (p.q_per_seq - 1 + c.scale_block - 1) / c.scale_block + 1;  // scale blocks that T consecutive positions can touch
   const int64_t bx = (int64_t)p.num_seqs * a.spans;
   // Two or four heads per block where that still leaves about 400 threads per SM: they share the angles, and the later ones' loads
-  // are hidden (4096 tokens of 8 heads: 16-row blocks 12.5 us with two, 11.6 with four; 64-row blocks 15.4 with one, 14.5 with two,
-  // 20.8 with four in an earlier version; 7 x 333 tokens of 4 heads, 16-row blocks, no rotation: 4.9 with one, 5.4 with two). Threads:
-  // four rows each (32-row blocks with two rows each 12.8 us instead of 10.5, 128-row blocks with eight 21.2 instead of 11.5).
+  // are hidden. In us with one, two and four heads (* the rule's choice): 4096 tokens of 8 heads, normed and turned, 16-row blocks
+  // 15.3, 12.9, 12.0*; 32-row 12.2, 10.7*, 15.4; 64-row 12.3, 11.7*, 16.7; 128-row 14.0, 12.4*, 20.3; 1024 tokens, 64-row 5.9*, 8.4,
+  // 13.8; 7 x 333 tokens of 4 heads, 16-row, as they are 5.0*, 5.1, 7.5, normed and turned 7.4*, 6.8, 9.9; 16 x 256 of 8 heads, 64-row
+  // 15.7, 17.3*, 19.1. (The count includes spans that hold no tokens, so many short sequences get four: 64 x 4, 64-row 12.8, 11.3, 17.3*.)
+  // Threads: four rows each (32-row blocks with two rows each took 12.8 us instead of 10.5, 128-row blocks with eight 21.2 instead of 11.5).
   const int threads = c.scale_block <= 32 ? 128 : c.scale_block == 64 ? 256 : 512;
   a.heads_per_block = 1;
   while (a.heads_per_block < 4 && bx * ((a.heads[0] + 2 * a.heads_per_block - 1) / (2 * a.heads_per_block)) * threads >= (int64_t)400 * dev.sm_count)

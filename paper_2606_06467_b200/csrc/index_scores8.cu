@@ -14,7 +14,8 @@
 // once per chunk. The sequences' lengths wait in shared memory, and a tile's page numbers are fetched one tile before its keys.
 // A key's sum does not depend on where the key sits, so equal keys get bit-identical scores (the top-k's tie-break).
 // 16 sequences of 128 K keys, one token each: 277 MB in 48.2 us, 5.75 TB/s, 0.89 of a measured copy. 24 ragged sequences of up to
-// 32 K 64-wide keys, four tokens each: 11.3 us for 32 MB, the uneven ends and the ramp of the rings.
+// 32 K 64-wide keys, four tokens each: 11.6 us for 32 MB, the uneven ends and the ramp of the rings. 16 sequences of 32 K keys with
+// 8, 16 and 32 tokens: 13.9, 18.7, 30.0 us of 64-wide keys, 21.7, 30.0, 64.2 of 128-wide ones (with 32 tokens some accumulators spill).
 #include "attn_common.cuh"
 #include "cache8.cuh"
 
@@ -351,7 +352,8 @@ cudaError_t launch_index_scores8(const clsa_params& p, const clsa_cache8& c, con
   a.q = static_cast<const uint16_t*>(q_idx);
   a.scores = scores;
   a.score_stride = score_stride;
-  // four tiles per chunk, fewer where that would leave a warp less than four chunks
+  // Four tiles per chunk, fewer where that would leave a warp less than four chunks (us with one, two, four tiles: one sequence of 4 K keys
+  // 3.3, 3.8, 5.1, four of 8 K 3.8, 4.2, 5.5, 24 ragged ones of up to 32 K 10.7, 10.6, 11.9; 64 ragged ones of up to 32 K 32.2, 29.1, 30.8).
   const int tile = kTileBytes / p.idx_dim;
   a.chunk_keys = 4 * tile;
   while (a.chunk_keys > tile && (int64_t)p.num_seqs * p.max_seq_len < (int64_t)4 * kWarps * dev.sm_count * a.chunk_keys) a.chunk_keys /= 2;

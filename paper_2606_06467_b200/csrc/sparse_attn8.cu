@@ -4,7 +4,9 @@
 // with ek, ev the exponents of the scale blocks that row s lies in.
 //
 // e4m3 codes convert to f16 exactly, a query row scaled by a power of two so that its largest magnitude lies in [2^13, 2^14) is
-// exact in f16 down to 2^-31 of it, weights are rounded to f16, sums are fp32. (There is no faster 8-bit form to be had: the
+// exact in f16 down to 2^-31 of it, sums are fp32. Weights are rounded to f16, what the matrix instruction takes: 2^-11 of each, which a
+// sum over tokens averages out below the outputs' own bf16 rounding of 2^-8 (against 64 bits both this and a form with fp32 weights are
+// off by 0.0017 in the norm); the denominators are sums of the unrounded ones. (There is no faster 8-bit form to be had: the
 // warp-level e4m3 instruction is carried out as these conversions and f16 products anyway.) A warp-level instruction has up to 8
 // query heads of the GQA group in its columns (NT tiles cover the group) and 16 tokens or 16 dimensions along M:
 //   S^T[16 tokens x 8 heads] = K[16 x 128] Q^T,   O^T[128 x 8 heads] += V^T[128 x 32 tokens] P^T
@@ -28,13 +30,13 @@
 // units that straddle blocks in global slots (two per block) with an arrival counter; the block that arrives last reads them in
 // block order, so results do not depend on timing, and puts the counter back to zero.
 //
-// 512-token chunk (32 query heads over 8 KV heads, 2048 rows each of 33 K tokens): 184.5 us. The caches come from DRAM once (98 MB) and
+// 512-token chunk (32 query heads over 8 KV heads, 2048 rows each of 33 K tokens): 185 us. The caches come from DRAM once (98 MB) and
 // 2.17 GB cross from L2 to the SMs, 11.8 TB/s; copies alone take 135 us, the arithmetic alone about 160, and what is left is
 // their overlap on 12 warps per SM (168 registers each): 59 % of issue slots and of the ALU, which converts the codes at half
 // rate, 32 % of the tensor pipe. 16 warps with 128 registers and three half-stage buffers (239 us: a third more instructions),
 // 8-row half stages, rows padded instead of permuted (218: a row then lies in two lines), fewer lanes per row (281 with four),
 // tcgen05 with two e4m3 pieces per operand (345) all lost. Decode, 16 sequences of 128 K tokens: 67 MB of gathered rows in
-// 18.9 us (3.55 TB/s; 15.6 with the rows in L2), a chain of index, page, row and merge round trips on 128 SMs.
+// 19.1 us (3.5 TB/s; 15.6 with the rows in L2), a chain of index, page, row and merge round trips on 128 SMs.
 #include "attn_common.cuh"
 #include "cache8.cuh"
 
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) sparse_attn8_kernel(const __gri
 #pragma unroll 1
       for (int i0 = 0; i0 < nstages; i0 += STAGES)
 #pragma unroll
-      for (int buf = 0; buf < STAGES; ++buf) {  // every place in the ring a constant (512-token chunk: 194 us without, 184.5 with)
+      for (int buf = 0; buf < STAGES; ++buf) {  // every place in the ring a constant (512-token chunk: 194 us without, 184.5 with, then)
         const int i = i0 + buf;
         if (i >= nstages) break;
         const int raw_new = next_raw();
@@ -706,8 +708,10 @@ Attn8Plan make_attn8_plan(const clsa_params& p, const DeviceInfo& dev) {
     plan.wpb = (int)((workers + blocks - 1) / blocks);
     blocks = (workers + plan.wpb - 1) / plan.wpb;
     // Whole units per block, where the blocks with one unit more have at most six stages per warp more than the even share: that
-    // leaves no unit to two blocks and few to two warps. Else, where every unit can have workers of its own and the longest
-    // span that results stays within 15 % of the even share, those.
+    // leaves no unit to two blocks and few to two warps (2048 rows: 192 units 26.5 us against 30.8 otherwise, 256 units 29.8 against 36.9;
+    // 152 units 25.2 against 23.7. 8192 rows, past the bound: 152 units 77.8 against 65.0, 192 units 80.3 against 77.8, but 224 units
+    // 85.6 against 92.5). Else, where every unit can have workers of its own and the longest span that results stays
+    // within 15 % of the even share, those (8192 rows: 152 units 65.0 against 68.3 for the flat list, 192 units 77.8 against 83.6).
     const int64_t most = (plan.units + blocks - 1) / blocks;
     plan.mode = kAttn8Flat;
     if (plan.wpb == plan.warps && (most * blocks - plan.units) * plan.unit_stages <= 6 * blocks * plan.warps) {
