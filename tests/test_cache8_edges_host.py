@@ -154,11 +154,11 @@ def test_buffers_are_measured_against_the_params(binding):
             attn(**bad)
     scores = lambda q, s, n: clsa.clsa_index_scores8(p, c, q, s, n, ws)  # noqa: E731
     q = Tensor((2, 3, 128), BF16)
-    for s, n in ((Tensor((2, 3, 1024), F32), 1024), (Tensor((2, 3, 1000), F32, (3072 + 24, 1032, 1)), 1032), (Tensor((5 * 1024 + 1000,), F32), 1024)):
+    for s, n in ((Tensor((2, 3, 1040), F32), 1040), (Tensor((2, 3, 1000), F32, (3096, 1032, 1)), 1032), (Tensor((5 * 1040 + 1000,), F32), 1040)):
         scores(q, s, n)
         assert _taken(calls, "clsa_index_scores8")
-    for q_, s, n in ((Tensor((5, 128), BF16), Tensor((2, 3, 1024), F32), 1024), (q, Tensor((2, 3, 1000), F32), 1024), (q, Tensor((5 * 1024 + 999,), F32), 1024),
-                     (q, Tensor((2, 3, 999), F32, (3072 + 24, 1032, 1)), 1032), (q, Tensor((5, 1024), F32), 1024)):
+    for q_, s, n in ((Tensor((5, 128), BF16), Tensor((2, 3, 1040), F32), 1040), (q, Tensor((2, 3, 1000), F32), 1040), (q, Tensor((5 * 1040 + 999,), F32), 1040),
+                     (q, Tensor((2, 3, 999), F32, (3096, 1032, 1)), 1032), (q, Tensor((5, 1040), F32), 1040)):
         with pytest.raises(ValueError):
             scores(q_, s, n)
     assert not calls
@@ -169,11 +169,11 @@ def test_caches_are_measured_against_the_params(binding):
     ws, p = Tensor((4096,), U8), _params(clsa)
 
     def each(p, c):
-        q, s = Tensor((2, 3, p.num_q_heads, 128), BF16), Tensor((2, 3, 1024), F32)
+        q, s = Tensor((2, 3, p.num_q_heads, 128), BF16), Tensor((2, 3, 1040), F32)
         new, idx = Tensor((2, 3, p.num_kv_heads, 128), BF16), Tensor((2, 3, p.idx_dim), BF16)
         return dict(kv=[lambda: clsa.clsa_cache8_append(p, c, None, new, new, None, ws),
                         lambda: clsa.clsa_sparse_attn8(p, c, q, Tensor((6, 64), I32), Tensor((6,), I32), q, None, None, ws)],
-                    idx=[lambda: clsa.clsa_cache8_append(p, c, None, None, None, idx, ws), lambda: clsa.clsa_index_scores8(p, c, idx, s, 1024, ws)])
+                    idx=[lambda: clsa.clsa_cache8_append(p, c, None, None, None, idx, ws), lambda: clsa.clsa_index_scores8(p, c, idx, s, 1040, ws)])
 
     def refused(p, c, which):
         for call in which:
@@ -222,9 +222,9 @@ def test_the_params_own_tensors_are_measured(binding):
     """seq_start, seq_len and the block table: types, layouts, how many sequences they describe, where they lie."""
     clsa, calls = binding
     ws, c = Tensor((4096,), U8), clsa.clsa_cache8(0x10000, 0x20000, 0x30000, 0x40000, 1024, 128, 64, 0x50000, 0x60000, 128, 64)
-    heads, idx, s = Tensor((2, 3, 8, 128), BF16), Tensor((2, 3, 128), BF16), Tensor((2, 3, 1024), F32)
+    heads, idx, s = Tensor((2, 3, 8, 128), BF16), Tensor((2, 3, 128), BF16), Tensor((2, 3, 1040), F32)
     q = Tensor((2, 3, 32, 128), BF16)
-    each = (lambda p: clsa.clsa_cache8_append(p, c, None, heads, heads, idx, ws), lambda p: clsa.clsa_index_scores8(p, c, idx, s, 1024, ws),
+    each = (lambda p: clsa.clsa_cache8_append(p, c, None, heads, heads, idx, ws), lambda p: clsa.clsa_index_scores8(p, c, idx, s, 1040, ws),
             lambda p: clsa.clsa_sparse_attn8(p, c, q, Tensor((6, 64), I32), Tensor((6,), I32), q, None, None, ws))
     zeros = lambda *shape, dtype=I32: torch.zeros(shape, dtype=dtype)  # noqa: E731
     here = lambda p: setattr(p, "_made", tuple(m and (*m[:2], 0) for m in p._made)) or p  # noqa: E731  (host tensors as if on device 0)
