@@ -31,6 +31,7 @@ class clsa_params(ctypes.Structure):
     """Mirror of `clsa_params` in include/clsa.h (same field order and types)."""
 
     _made = None  # what seq_start, seq_len and block_table were made of: see _described
+    _kv = None  # and k_cache and v_cache: see _cached
 
     _fields_ = [
         ("num_seqs", ctypes.c_int32), ("q_per_seq", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
@@ -135,6 +136,15 @@ def _described(t, dtype, step):
     return t.data_ptr(), seqs, None if device < 0 and t.is_pinned() else device
 
 
+def _cached(t):
+    """(address, dtype, elements from the first to behind the last, device) of a cache's tensor. None for what is no tensor."""
+    torch = sys.modules.get("torch")
+    if torch is None or not isinstance(t, torch.Tensor):
+        return None
+    reach = 1 + sum((n - 1) * step for n, step in zip(t.shape, t.stride())) if t.numel() else 0
+    return t.data_ptr(), str(t.dtype), reach, t.get_device()
+
+
 def make_params(*, num_seqs, q_per_seq=1, num_q_heads, num_kv_heads, head_dim=128, idx_dim, top_k, num_layers=1,
                 causal=0, max_seq_len, sm_scale, seq_start=None, seq_len=None, k_cache=None, v_cache=None,
                 kv_token_stride=None, kv_head_stride=None, idx_k_cache=None, idx_token_stride=None,
@@ -163,6 +173,7 @@ def make_params(*, num_seqs, q_per_seq=1, num_q_heads, num_kv_heads, head_dim=12
         max_blocks_per_seq = block_table.shape[1]
     p.max_blocks_per_seq = max_blocks_per_seq or 0
     p._made = (_described(seq_start, "int64", 1), _described(seq_len, "int32", 1), _described(block_table, "int32", p.max_blocks_per_seq))
+    p._kv = (_cached(k_cache), _cached(v_cache))
     return p
 
 
@@ -294,3 +305,6 @@ def raw():
 from .cache8 import (CLSA_DEV_BAD_SCALE_BLOCK, EXPORTS_CACHE8, clsa_cache8, clsa_cache8_append,  # noqa: E402
                      clsa_cache8_workspace_bytes, clsa_heads, clsa_index_scores8, clsa_norm_rope, clsa_norm_rope_spec,
                      clsa_sparse_attn8, make_cache8, make_norm_rope)
+# The calls around a layer's cache (include/clsa_layer.h).
+from .layer import (CLSA_MAX_AXES, EXPORTS_LAYER, clsa_add_norm, clsa_add_norm_spec, clsa_dense_attn, clsa_dense_attn8,  # noqa: E402
+                    clsa_dense_workspace_bytes, clsa_norm_rope_axes, clsa_rope_axes, clsa_rows, make_add_norm, make_rope_axes)

@@ -12,7 +12,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libclsa.so")
 MARSHAL = os.path.join(PKG, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))  # CPython module (csrc/marshal.c)
 SOURCES = ["api.cu", "index_scores.cu", "index_gemm.cu", "index_topk.cu", "topk.cu", "topk_filter.cu", "sparse_attn.cu", "sparse_attn_sk.cu", "project_append.cu",
-           "api_cache8.cu", "norm_rope.cu", "cache8_append.cu", "index_scores8.cu", "sparse_attn8.cu"]
+           "api_cache8.cu", "norm_rope.cu", "cache8_append.cu", "index_scores8.cu", "sparse_attn8.cu",
+           "api_layer.cu", "dense_attn.cu", "add_norm.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
@@ -36,7 +37,7 @@ def _stale(target: str, deps) -> bool:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
-    headers += [os.path.join(ROOT, "include", f) for f in ("clsa.h", "clsa_cache8.h")]
+    headers += [os.path.join(ROOT, "include", f) for f in ("clsa.h", "clsa_cache8.h", "clsa_layer.h")]
     objdir = os.path.join(PKG, "build")
     os.makedirs(objdir, exist_ok=True)
     objs, procs = [], []

@@ -3,19 +3,9 @@
 #include <math.h>
 
 #include "cache8.cuh"
+#include "checks.cuh"
 
 namespace clsa {
-namespace {
-
-bool aligned(const void* ptr, size_t a) { return (reinterpret_cast<uintptr_t>(ptr) % a) == 0; }
-
-#define CLSA_TRY(expr)                     \
-  do {                                     \
-    const clsa_status st__ = (expr);       \
-    if (st__ != CLSA_OK) return st__;      \
-  } while (0)
-
-clsa_status from_cuda(cudaError_t e) { return e == cudaSuccess ? CLSA_OK : CLSA_ERR_CUDA; }
 
 clsa_status check_heads(const clsa_heads* h, int dim, bool output) {
   if (h->data == nullptr || !aligned(h->data, 16)) return CLSA_ERR_INVALID_ARG;
@@ -35,29 +25,6 @@ clsa_status check_spec(const clsa_norm_rope_spec* s) {
   if (!aligned(s->q_weight, 16) || !aligned(s->k_weight, 16)) return CLSA_ERR_INVALID_ARG;
   if (s->head_dim != 64 && s->head_dim != 128 && s->head_dim != 256) return CLSA_ERR_UNSUPPORTED;
   if (s->rot_dim % 16 != 0) return CLSA_ERR_UNSUPPORTED;
-  return CLSA_OK;
-}
-
-// The params fields that these calls use.
-clsa_status check_params(const clsa_params* p) {
-  if (p == nullptr) return CLSA_ERR_INVALID_ARG;
-  if (p->num_seqs < 1 || p->q_per_seq < 1 || p->num_q_heads < 1 || p->num_kv_heads < 1 || p->head_dim < 1 || p->idx_dim < 1 ||
-      p->top_k < 1)
-    return CLSA_ERR_INVALID_ARG;
-  if (p->num_q_heads % p->num_kv_heads != 0 || p->num_kv_heads > 1024) return CLSA_ERR_INVALID_ARG;
-  if (p->causal != 0 && p->causal != 1) return CLSA_ERR_INVALID_ARG;
-  if (p->max_seq_len < p->q_per_seq) return CLSA_ERR_INVALID_ARG;
-  if (!isfinite(p->sm_scale) || !(p->sm_scale > 0.f)) return CLSA_ERR_INVALID_ARG;
-  if ((int64_t)p->num_seqs * p->q_per_seq > (int64_t)1 << 30) return CLSA_ERR_INVALID_ARG;
-  if (p->num_cache_rows < 1 || p->num_cache_rows > 0x7fffffffLL) return CLSA_ERR_INVALID_ARG;
-  // kernels number positions, 32-token stages, score tiles and appended rows with 32 bits
-  if (p->max_seq_len > 0x7fff0000) return CLSA_ERR_UNSUPPORTED;
-  if ((double)p->num_seqs * p->q_per_seq * p->num_kv_heads * ((p->top_k + 31) / 32) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
-  if ((double)p->num_seqs * ((p->max_seq_len + 31) / 32) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
-  if ((double)p->num_seqs * (2 * p->num_kv_heads + 1) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
-  if (p->head_dim != 128) return CLSA_ERR_UNSUPPORTED;
-  if (p->idx_dim != 64 && p->idx_dim != 128) return CLSA_ERR_UNSUPPORTED;
-  if (p->num_q_heads / p->num_kv_heads > 16) return CLSA_ERR_UNSUPPORTED;
   return CLSA_OK;
 }
 
@@ -90,6 +57,51 @@ clsa_status check_kv8(const clsa_params* p, const clsa_cache8* c) {
   if (c->scale_head_stride < (p->num_cache_rows + c->scale_block - 1) / c->scale_block) return CLSA_ERR_INVALID_ARG;
   // row offsets are 32-bit counts of 16 bytes
   if ((double)p->num_cache_rows * (double)(c->kv_token_stride / 16) >= 4294967296.0) return CLSA_ERR_UNSUPPORTED;
+  return CLSA_OK;
+}
+
+clsa_status check_norm_rope(const clsa_norm_rope_spec* spec, int32_t num_tokens, const clsa_heads* q, const clsa_heads* q_out,
+                            const clsa_heads* k, const clsa_heads* k_out) {
+  CLSA_TRY(check_spec(spec));
+  if (num_tokens < 0 || num_tokens > 1 << 30) return CLSA_ERR_INVALID_ARG;
+  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (q == nullptr && k == nullptr))
+    return CLSA_ERR_INVALID_ARG;
+  const clsa_heads* pairs[2][2] = {{q, q_out}, {k, k_out}};
+  for (auto& pr : pairs) {
+    if (pr[0] == nullptr) continue;
+    if (pr[0]->num_heads != pr[1]->num_heads) return CLSA_ERR_INVALID_ARG;
+    if (num_tokens == 0) continue;  // nothing has an address, and no stride means anything
+    CLSA_TRY(check_heads(pr[0], spec->head_dim, false));
+    CLSA_TRY(check_heads(pr[1], spec->head_dim, num_tokens > 1));
+    if (pr[0]->data == pr[1]->data && (pr[0]->token_stride != pr[1]->token_stride ||
+                                       (pr[0]->num_heads > 1 && pr[0]->head_stride != pr[1]->head_stride)))
+      return CLSA_ERR_INVALID_ARG;
+  }
+  return CLSA_OK;
+}
+
+namespace {
+
+// The params fields that these calls use.
+clsa_status check_params(const clsa_params* p) {
+  if (p == nullptr) return CLSA_ERR_INVALID_ARG;
+  if (p->num_seqs < 1 || p->q_per_seq < 1 || p->num_q_heads < 1 || p->num_kv_heads < 1 || p->head_dim < 1 || p->idx_dim < 1 ||
+      p->top_k < 1)
+    return CLSA_ERR_INVALID_ARG;
+  if (p->num_q_heads % p->num_kv_heads != 0 || p->num_kv_heads > 1024) return CLSA_ERR_INVALID_ARG;
+  if (p->causal != 0 && p->causal != 1) return CLSA_ERR_INVALID_ARG;
+  if (p->max_seq_len < p->q_per_seq) return CLSA_ERR_INVALID_ARG;
+  if (!isfinite(p->sm_scale) || !(p->sm_scale > 0.f)) return CLSA_ERR_INVALID_ARG;
+  if ((int64_t)p->num_seqs * p->q_per_seq > (int64_t)1 << 30) return CLSA_ERR_INVALID_ARG;
+  if (p->num_cache_rows < 1 || p->num_cache_rows > 0x7fffffffLL) return CLSA_ERR_INVALID_ARG;
+  // kernels number positions, 32-token stages, score tiles and appended rows with 32 bits
+  if (p->max_seq_len > 0x7fff0000) return CLSA_ERR_UNSUPPORTED;
+  if ((double)p->num_seqs * p->q_per_seq * p->num_kv_heads * ((p->top_k + 31) / 32) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
+  if ((double)p->num_seqs * ((p->max_seq_len + 31) / 32) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
+  if ((double)p->num_seqs * (2 * p->num_kv_heads + 1) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
+  if (p->head_dim != 128) return CLSA_ERR_UNSUPPORTED;
+  if (p->idx_dim != 64 && p->idx_dim != 128) return CLSA_ERR_UNSUPPORTED;
+  if (p->num_q_heads / p->num_kv_heads > 16) return CLSA_ERR_UNSUPPORTED;
   return CLSA_OK;
 }
 
@@ -128,21 +140,7 @@ extern "C" {
 
 clsa_status clsa_norm_rope(const clsa_norm_rope_spec* spec, int32_t num_tokens, const int32_t* positions, const clsa_heads* q,
                            const clsa_heads* q_out, const clsa_heads* k, const clsa_heads* k_out, clsa_stream stream) {
-  CLSA_TRY(check_spec(spec));
-  if (num_tokens < 0 || num_tokens > 1 << 30) return CLSA_ERR_INVALID_ARG;
-  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (q == nullptr && k == nullptr))
-    return CLSA_ERR_INVALID_ARG;
-  const clsa_heads* pairs[2][2] = {{q, q_out}, {k, k_out}};
-  for (auto& pr : pairs) {
-    if (pr[0] == nullptr) continue;
-    if (pr[0]->num_heads != pr[1]->num_heads) return CLSA_ERR_INVALID_ARG;
-    if (num_tokens == 0) continue;  // nothing has an address, and no stride means anything
-    CLSA_TRY(check_heads(pr[0], spec->head_dim, false));
-    CLSA_TRY(check_heads(pr[1], spec->head_dim, num_tokens > 1));
-    if (pr[0]->data == pr[1]->data && (pr[0]->token_stride != pr[1]->token_stride ||
-                                       (pr[0]->num_heads > 1 && pr[0]->head_stride != pr[1]->head_stride)))
-      return CLSA_ERR_INVALID_ARG;
-  }
+  CLSA_TRY(check_norm_rope(spec, num_tokens, q, q_out, k, k_out));
   if (num_tokens == 0) return CLSA_OK;
   if (!aligned(positions, 4) || (positions == nullptr && spec->rot_dim > 0)) return CLSA_ERR_INVALID_ARG;
   DeviceInfo dev;

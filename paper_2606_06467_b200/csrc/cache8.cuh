@@ -57,6 +57,12 @@ cudaError_t launch_sparse_attn8(const clsa_params& p, const clsa_cache8& c, cons
 #ifdef __CUDACC__
 // Scale byte -> its exponent, brought into the range that the format allows.
 __device__ __forceinline__ int scale_exponent(int byte) { return min(max(byte, kScaleExpMin + 127), kScaleExpMax + 127) - 127; }
+// Smallest exponent e with amax <= 448 * 2^e = 1.75 * 2^(e + 8), within the allowed range.
+__device__ __forceinline__ int need_exponent(float amax) {
+  const uint32_t bits = __float_as_uint(amax);
+  const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return min(max(e, kScaleExpMin), kScaleExpMax);
+}
 // 2^e for -126 <= e <= 127.
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 

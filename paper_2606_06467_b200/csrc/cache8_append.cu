@@ -41,13 +41,6 @@ struct AppendArgs {
   uint32_t* status;
 };
 
-// Smallest exponent e with amax <= 448 * 2^e = 1.75 * 2^(e + 8), within the allowed range.
-__device__ __forceinline__ int need_exponent(float amax) {
-  const uint32_t bits = __float_as_uint(amax);
-  const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return min(max(e, kScaleExpMin), kScaleExpMax);
-}
-
 // Eight codes times a power of two, rounded again.
 __device__ __forceinline__ uint2 recode(uint2 v, float f) {
   const uint32_t in[4] = {e4m3x2_to_f16x2(v.x), e4m3x2_hi_to_f16x2(v.x), e4m3x2_to_f16x2(v.y), e4m3x2_hi_to_f16x2(v.y)};

@@ -1,0 +1,927 @@
+// Attention of the newest T tokens of every sequence over all of its cached rows, or those of a window.
+//
+//   x_s = sm_scale q . K_s,   O = sum_s exp(x_s) V_s / sum_s exp(x_s)   over the positions that a query sees
+//
+// The T queries of a sequence and the query heads of a KV head's group are columns of one product, so that a row of the cache
+// is read once for all of them: with up to about 64 columns the launch is bound by HBM.
+//
+// Work. A granule is 16 consecutive positions (starting on a multiple of 16, so that it lies in one page and one scale block) of
+// `heads` KV heads. The granules of all (sequence, head group) units form one list, sequence after sequence; its length is known on the
+// device only, where every block adds up the lengths and takes an even stretch of the list, whatever the sequences' lengths are. One
+// producer warp fetches granules into a ring by tiled bulk copies (one for K, one for V: 16 rows of every head, 128-byte swizzle); eight
+// warps consume them, each with one head's rows: `lanes` warps take a head's granules in turn, `col_warps` share a head's query columns.
+// Products are formed transposed, tokens along M of warp-level instructions:
+//   S^T[16 tokens x 8 columns] = K Q^T,   O^T[128 x 8 columns] += V^T P^T
+// A block that holds several heads reads whole token rows, 16 at a time: what DRAM likes best.
+//
+// Softmax. One pass, in the log2 domain, relative to a reference per column that moves only when a weight would exceed 2^8 (one
+// vote per granule, no reduction over its tokens otherwise). Weights are rounded to what the matrix instruction takes beside V. bf16: two
+// parts of 8 bits each (p and what its rounding left) where that costs nothing, with up to 32 columns: the error of a single part is as
+// large as the output's own rounding; up to 4 columns are held twice and the second copy takes the second parts. 8-bit caches: f16,
+// 2^-11 of each weight. Denominators are sums of the unrounded weights in fp32.
+//
+// 8-bit caches. Codes convert to f16 exactly; the scale exponents ek, ev are the same for all of a granule, so that they are one number
+// per warp: x = (d 2^(ek - 22)) qf with qf = 2^22 sm_scale / (the power of two that q was scaled by). As in the sparse attention,
+// numerators have a reference of their own, m near the largest x - mx + ev, and 2^m meets the finished quotient.
+//
+// Joining. A unit that lies in one stretch is finished by its block. Of the others every block leaves one record per column (128
+// unnormalised outputs, reference, sum, in fp32), and a second kernel, whose launch overlaps the first one's end, joins a row's records in
+// the order of the stretches: results do not depend on timing.
+#include <cuda.h>
+
+#include "attn_common.cuh"
+#include "layer.cuh"
+
+namespace clsa {
+namespace {
+
+constexpr int kGran = 16;                 // positions per granule
+constexpr int kConsumers = 8;             // consuming warps
+constexpr int kThreads = (kConsumers + 1) * 32;
+constexpr int kJoinThreads = 256;
+constexpr int kMaxSlots = 40;
+constexpr int kMergeBytes = kConsumers * 8 * kPartialStride * 4;  // a column tile of every consuming warp
+constexpr int kCtrlBytes = 1024;
+constexpr uint32_t kSpinLimit = 1u << 22;  // polls of a barrier, each of which sleeps for a while: seconds
+constexpr float kLazy = 8.f;
+constexpr float kNone = -3.4028234663852886e38f;  // a reference before the first token
+constexpr int kHeldBack = 22;                     // of K's exponent, kept for the query's factor: d 2^(ek - 22) is finite and keeps its last bits
+
+struct DenseArgs {
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  uint32_t* status;
+  float* part;
+  const int64_t* seq_start;
+  const int32_t* seq_len;
+  const int32_t* block_table;
+  const uint8_t* ks;
+  const uint8_t* vs;
+  int64_t scale_head, num_rows;
+  int scale_shift, block_shift, max_blocks, pages;
+  int num_seqs, T, num_q_heads, group, columns_used;  // columns_used: T * group
+  int window, causal, max_seq_len;
+  int columns, col_tiles, heads, lanes, col_warps, head_groups, slots, spans, min_granules;
+  float scale_log2;
+};
+
+// ---- barriers and copies --------------------------------------------------------------------------------------------
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Bounded wait; false once the limit ran out here or in another role (nothing waits any more then, and the results mean nothing).
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
+  if (mbar_try_wait(bar, parity)) return true;
+  for (uint32_t it = 0; it < kSpinLimit; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((it & 63u) == 63u) {
+      if (*abort_flag != 0u) return false;
+      __nanosleep(64);
+    }
+  }
+  *abort_flag = 1u;
+  return false;
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_b8_x2_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// ---- which positions and granules a sequence has ----------------------------------------------------------------------
+struct Seq {
+  int n;      // its length, 0 if it counts as empty
+  int first;  // first position that some query sees
+  int base;   // .. rounded down to a granule
+  int gran;   // granules (one for an empty sequence, whose outputs have to be written too)
+  bool bad;
+};
+__device__ __forceinline__ Seq look_at(const DenseArgs& a, int len) {
+  Seq s;
+  s.bad = len < (a.causal || a.window ? a.T : 0) || len > a.max_seq_len;
+  s.n = s.bad ? 0 : len;
+  s.first = a.window ? max(0, s.n - a.T + 1 - a.window) : 0;
+  s.base = s.first & ~(kGran - 1);
+  s.gran = max(1, (s.n - s.base + kGran - 1) / kGran);
+  return s;
+}
+// How the list of `total` granules is cut: the first total % spans stretches have one more than total / spans.
+struct Cut {
+  int spans, each, more;
+  __device__ __forceinline__ Cut(const DenseArgs& a, int total) {
+    spans = min(a.spans, max(1, (total + a.min_granules - 1) / a.min_granules));
+    each = total / spans;
+    more = total - each * spans;
+  }
+  __device__ __forceinline__ int begin(int s) const { return s * each + min(s, more); }
+  __device__ __forceinline__ int owner(int g) const {
+    const int big = more * (each + 1);
+    return g < big ? g / (each + 1) : more + (g - big) / each;
+  }
+};
+// Sum over the block, and of the threads before this one. `sums`: a word for each warp and one more.
+template <int THREADS>
+__device__ __forceinline__ int block_scan(int v, int* sums, int& before) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int incl = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int o = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 31) sums[warp] = incl;
+  __syncthreads();
+  int total = 0;
+  before = incl - v;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    const int x = sums[w];
+    if (w < warp) before += x;
+    total += x;
+  }
+  __syncthreads();
+  return total;
+}
+
+// Row r of K's 16 as the first product sees them holds token r for bf16. For codes it is k_token(r), chosen so that a lane's word of the
+// transposing 8-bit loads, four consecutive V rows (v_token), holds the tokens whose weights the transposed first product gives
+// it, and so that the eight rows that either load reads together lie in different banks of the 128-byte swizzle.
+__device__ __forceinline__ int k_token(int r) { return r < 4 ? r : r < 8 ? r + 8 : r - 4; }
+__device__ __forceinline__ int v_token(int i) { return k_token(2 * (i >> 2) + (i & 1) + ((i & 2) << 2)); }
+
+// Records of partial results (kPartialStride floats: 128 outputs, then mx, l, m) folded into a running one, lane i of a warp having the
+// i-th one's (mx, l, m) and fetch(i) its outputs.
+struct Folded {
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float mx = kNone, l = 0.f, m = kNone;
+  template <class F>
+  __device__ __forceinline__ void fold(float4 head, int count, F fetch) {
+    float xn = fmaxf(mx, head.x);
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) xn = fmaxf(xn, __shfl_xor_sync(0xffffffffu, xn, d));
+    const float mnew = (head.x - xn) + head.z, mold = (mx - xn) + m;  // references to x - xn + ev
+    float mn = fmaxf(mold, mnew);
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
+    const float sn = fast_exp2(mnew - mn), so = fast_exp2(mold - mn);
+    float sum = fast_exp2(head.x - xn) * head.y;
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    l = l * fast_exp2(mx - xn) + sum;
+    acc.x *= so; acc.y *= so; acc.z *= so; acc.w *= so;
+#pragma unroll 8
+    for (int i = 0; i < count; ++i) {
+      const float4 v = fetch(i);
+      const float f = __shfl_sync(0xffffffffu, sn, i);
+      acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+    }
+    mx = xn;
+    m = mn;
+  }
+  __device__ __forceinline__ void write(const DenseArgs& a, int64_t item, int lane) const {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (l != 0.f) {  // 2^m in two halves: it may not be a float
+      const float inv = 1.f / l, half = fast_exp2(0.5f * m);
+      v = make_float4(acc.x * inv * half * half, acc.y * inv * half * half, acc.z * inv * half * half, acc.w * inv * half * half);
+    }
+    *reinterpret_cast<uint2*>(a.out + item * 128 + lane * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    if (a.lse != nullptr && lane == 0) a.lse[item] = l != 0.f ? (mx + log2f(l)) * kLn2 : -INFINITY;
+  }
+};
+__device__ __forceinline__ float4 no_head() { return make_float4(kNone, 0.f, kNone, 0.f); }
+
+// The record of column cc of head hh that block `block` leaves of the unit that its stretch begins (which = 0) or ends in (1).
+__device__ __forceinline__ float4* record_at(const DenseArgs& a, int block, int which, int hh, int cc) {
+  return reinterpret_cast<float4*>(a.part) + ((((int64_t)block * 2 + which) * a.heads + hh) * a.columns + cc) * (kPartialStride / 4);
+}
+
+// ---- the kernel --------------------------------------------------------------------------------------------------------
+// EIGHT: an 8-bit cache. NT: column tiles per warp. PARTS (bf16): 1, the weights' rounding is all there is; 2, a second product takes
+// what it left; 3 (NT = 1, up to 4 columns), columns 4 .. 7 repeat the first four and take it.
+template <bool EIGHT, int NT, int PARTS>
+__global__ void __launch_bounds__(kThreads, 1)
+dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ DenseArgs a) {
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t raw = smem_u32(smem_dyn), base = (raw + 1023u) & ~1023u;
+  unsigned char* base_ptr = smem_dyn + (base - raw);
+  const int row_bytes = EIGHT ? 128 : 256;
+  const uint32_t half_bytes = (uint32_t)(a.heads * kGran * row_bytes);  // a slot's K rows, then its V rows
+  const uint32_t ring_bytes = (uint32_t)a.slots * 2u * half_bytes;
+  float* merge = reinterpret_cast<float*>(base_ptr + ring_bytes);
+  unsigned char* ctrl = base_ptr + ring_bytes + kMergeBytes;
+  const uint32_t bars = base + ring_bytes + kMergeBytes;
+  auto full_bar = [&](int s) { return bars + 16u * s; };
+  auto empty_bar = [&](int s) { return bars + 16u * s + 8u; };
+  uint32_t* slot_mask = reinterpret_cast<uint32_t*>(ctrl + 16 * kMaxSlots);  // rows of the slot that exist
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 20 * kMaxSlots);
+  int* found = reinterpret_cast<int*>(ctrl + 20 * kMaxSlots + 16);  // first sequence of this block's stretch, granules before it
+  int* sums = found + 4;
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) {
+    for (int s = 0; s < a.slots; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), a.heads * a.col_warps); }
+    *abort_flag = 0u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind this grid's own wait, as in every kernel of the library
+
+  // this block's stretch of the list
+  const int HG = a.head_groups;
+  const int span = (int)blockIdx.x / a.col_tiles, ct = (int)blockIdx.x - span * a.col_tiles;
+  int total = 0;
+  for (int b0 = 0; b0 < a.num_seqs; b0 += kThreads) {
+    int before;
+    total += block_scan<kThreads>(b0 + tid < a.num_seqs ? look_at(a, a.seq_len[b0 + tid]).gran : 0, sums, before);
+  }
+  const Cut cut(a, total * HG);
+  if (span >= cut.spans) return;
+  const int span_lo = cut.begin(span), span_hi = cut.begin(span + 1);
+  for (int b0 = 0, run = 0; b0 < a.num_seqs; b0 += kThreads) {
+    const int g = b0 + tid < a.num_seqs ? look_at(a, a.seq_len[b0 + tid]).gran : 0;
+    int before;
+    const int sum = block_scan<kThreads>(g, sums, before);
+    const int lo = (run + before) * HG;
+    if (lo <= span_lo && span_lo < lo + g * HG) { found[0] = b0 + tid; found[1] = lo; }
+    run += sum;
+    if (run * HG > span_lo) break;
+  }
+  __syncthreads();
+
+  int b = found[0], seq_base = found[1], cur = span_lo, seq = 0;  // seq: granules of this block before the segment
+  const bool paged = a.block_table != nullptr;
+
+  if (warp == kConsumers) {
+    // ---------------- producer ----------------
+    uint32_t issued = 0;
+    bool alive = true;
+    while (cur < span_hi) {
+      const Seq s = look_at(a, a.seq_len[b]);
+      int64_t start = paged ? 0 : a.seq_start[b];
+      bool bad = s.bad;
+      uint32_t bad_bit = CLSA_DEV_BAD_SEQLEN;
+      if (EIGHT && !paged && (start & (kGran - 1)) != 0) { bad = true; bad_bit = CLSA_DEV_BAD_SCALE_BLOCK; }
+      if (bad && lane == 0) flag_status(a.status, bad_bit);
+      for (int hg = (cur - seq_base) / s.gran; hg < HG && cur < span_hi; ++hg) {
+        const int unit = seq_base + hg * s.gran;
+        const int lo = cur - unit, hi = min(span_hi - unit, s.gran);
+        int entry = 0;
+        for (int i = lo; i < hi; ++i) {
+          const int k = (i - lo) & 31;
+          const int pos = s.base + kGran * i;
+          if (paged && k == 0) {  // the pages of the next 32 granules, a lane each
+            const int mine = pos + kGran * lane;
+            entry = mine < s.n ? a.block_table[(int64_t)b * a.max_blocks + (mine >> a.block_shift)] : -1;
+          }
+          int64_t row = start + pos;
+          if (paged) {
+            const int blk = __shfl_sync(0xffffffffu, entry, k);
+            row = blk >= 0 && blk < a.pages ? ((int64_t)blk << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : -kGran;
+          }
+          uint32_t mask = 0xffffu;
+          if (row < 0 || row + kGran > a.num_rows) {
+            if (row <= -kGran || row >= a.num_rows) { mask = 0u; row = -kGran; }  // nothing of it exists: a copy of zeros
+            if (mask != 0u && row < 0) mask &= 0xffffu << (int)-row;
+            if (mask != 0u && row + kGran > a.num_rows) mask &= 0xffffu >> (int)(row + kGran - a.num_rows);
+            const int from = max(0, s.first - pos), to = min(kGran, s.n - pos);
+            const uint32_t wanted = to > from ? ((1u << to) - 1u) & ~((1u << from) - 1u) : 0u;
+            if (lane == 0 && !bad && (wanted & ~mask) != 0u) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+          }
+          if (bad) mask = 0u;
+          const int slot = (int)(issued % (uint32_t)a.slots);
+          if (alive) alive = mbar_wait(empty_bar(slot), ((issued / (uint32_t)a.slots) & 1u) ^ 1u, abort_flag);
+          if (alive && lane == 0) {
+            slot_mask[slot] = mask;
+            mbar_expect_tx(full_bar(slot), 2u * half_bytes);
+            const uint32_t dst = base + (uint32_t)slot * 2u * half_bytes;
+            if (EIGHT) {
+              tma_load_3d(dst, &map_k, 0, (int)row, hg * a.heads, full_bar(slot));
+              tma_load_3d(dst + half_bytes, &map_v, 0, (int)row, hg * a.heads, full_bar(slot));
+            } else {
+              tma_load_4d(dst, &map_k, 0, (int)row, hg * a.heads, 0, full_bar(slot));
+              tma_load_4d(dst + half_bytes, &map_v, 0, (int)row, hg * a.heads, 0, full_bar(slot));
+            }
+          }
+          alive = __shfl_sync(0xffffffffu, (int)alive, 0) != 0;
+          if (alive) ++issued;
+        }
+        cur = unit + hi;
+      }
+      seq_base += s.gran * HG;
+      ++b;
+    }
+    if (!alive && lane == 0) {  // given up: the copies under way still land in this block's memory
+      flag_status(a.status, CLSA_DEV_TIMEOUT);
+      for (uint32_t i = issued > (uint32_t)a.slots ? issued - a.slots : 0u; i < issued; ++i)
+        for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(full_bar((int)(i % a.slots)), (i / a.slots) & 1u); ++it) __nanosleep(64);
+    }
+    return;
+  }
+
+  // ---------------- consumers ----------------
+  const int my_cw = warp % a.col_warps, my_head = (warp / a.col_warps) % a.heads, my_lane = warp / (a.col_warps * a.heads);
+  const int rowq = lane >> 2, hcol = (lane & 3) * 2, t7 = lane & 7;
+  const bool second = PARTS == 3 && (lane & 2) != 0;  // this lane's columns take what the rounding left
+  const int G = a.group, T = a.T;
+  const int col0 = ct * a.columns + my_cw * NT * 8;
+  // the query token of this lane's two columns of each tile (columns past the last one count as the last token's)
+  int tok_of[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) tok_of[nt][h] = min(T - 1, (col0 + nt * 8 + (PARTS == 3 ? (hcol + h) & 3 : hcol + h)) / G);
+  // this lane's places in a slot's K and V rows
+  uint32_t k_at, v_at;
+  int row_lo, row_hi;  // tokens of rows rowq and rowq + 8 of the first product
+  if (EIGHT) {
+    const int kt = k_token(t7 + 8 * ((lane >> 3) & 1)), vt = v_token(lane & 15);
+    k_at = (uint32_t)(my_head * 2048 + kt * 128 + (((lane >> 4) ^ (kt & 7)) << 4));
+    v_at = (uint32_t)(my_head * 2048 + vt * 128 + (((lane >> 4) ^ (vt & 7)) << 4)) + half_bytes;
+    row_lo = k_token(rowq);
+    row_hi = k_token(rowq + 8);
+  } else {
+    const int kt = t7 + 8 * ((lane >> 3) & 1), vt = t7 + 8 * (lane >> 4);
+    k_at = (uint32_t)(my_head * 2048 + kt * 128 + (((lane >> 4) ^ t7) << 4));
+    v_at = (uint32_t)(my_head * 2048 + vt * 128 + ((((lane >> 3) & 1) ^ t7) << 4)) + half_bytes;
+    row_lo = rowq;
+    row_hi = rowq + 8;
+  }
+  const uint32_t upper = half_bytes / 2;  // from dimensions 0 .. 63 of the bf16 rows to 64 .. 127
+  int slot = 0;             // of this block's granule `at`, and the parity of its round
+  uint32_t round = 0;
+  int at = 0;
+
+  while (cur < span_hi) {
+    const Seq s = look_at(a, a.seq_len[b]);
+    const int64_t start = EIGHT && !paged ? a.seq_start[b] : 0;
+    for (int hg = (cur - seq_base) / s.gran; hg < HG && cur < span_hi; ++hg) {
+      const int unit = seq_base + hg * s.gran;
+      const int lo = cur - unit, hi = min(span_hi - unit, s.gran);
+      const int g = hg * a.heads + my_head;  // KV head
+      // queries, as B operands: column rowq of a tile
+      uint32_t qb[NT][8][2];
+      float qf[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int col = col0 + nt * 8 + (PARTS == 3 ? rowq & 3 : rowq);
+        const bool used = col < a.columns_used && (PARTS != 3 || (rowq & 3) < a.columns);
+        const int t = col / G, j = col - t * G;
+        const uint16_t* src = a.q + (((int64_t)b * T + t) * a.num_q_heads + g * G + j) * 128;
+        if (EIGHT) {
+          float amax = 0.f;
+#pragma unroll
+          for (int st = 0; st < 8; ++st) {  // dimensions 16 st + 4 (lane & 3) .. + 3
+            const uint2 v = used ? *reinterpret_cast<const uint2*>(src + 16 * st + 2 * hcol) : make_uint2(0u, 0u);
+            qb[nt][st][0] = v.x;
+            qb[nt][st][1] = v.y;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float x = fabsf(bf16_lo(qb[nt][st][k])), y = fabsf(bf16_hi(qb[nt][st][k]));
+              if (x <= 3.4028234663852886e38f) amax = fmaxf(amax, x);  // finite
+              if (y <= 3.4028234663852886e38f) amax = fmaxf(amax, y);
+            }
+          }
+          amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+          amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+          const int shift = min(13 + 127 - (int)(__float_as_uint(amax) >> 23), 120);  // largest magnitude into [2^13, 2^14)
+          const float up = exp2_int(shift), down = exp2_int(-shift);
+#pragma unroll
+          for (int st = 0; st < 8; ++st)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) qb[nt][st][k] = pack_f16x2(bf16_lo(qb[nt][st][k]) * up, bf16_hi(qb[nt][st][k]) * up);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            qf[nt][h] = fminf(__shfl_sync(0xffffffffu, down, 4 * (hcol + h)) * a.scale_log2 * exp2_int(kHeldBack), 3.4028234663852886e38f);
+        } else {
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks) {  // dimensions 16 ks + hcol, + 1, and those + 8
+            qb[nt][ks][0] = used ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + hcol) : 0u;
+            qb[nt][ks][1] = used ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + hcol + 8) : 0u;
+          }
+        }
+      }
+      float o[NT][8][4], mx[NT][2], m[NT][2], l[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) { mx[nt][h] = kNone; m[nt][h] = EIGHT ? kNone : 0.f; l[nt][h] = 0.f; }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[nt][j][i] = 0.f;
+      }
+      // every query sees [all_from, all_to)
+      const int all_from = a.window ? max(0, s.n - a.window) : 0, all_to = a.causal ? s.n - T + 1 : s.n;
+      uint32_t codes = 0;  // 8-bit: scale bytes of this lane's granules, 32 at a time, one per lane of the warp
+      int batch = 0;
+
+      int i = lo + ((my_lane - seq) % a.lanes + a.lanes) % a.lanes;  // this warp's granules: those whose number in the block is my_lane mod lanes
+      for (; i < hi; i += a.lanes, ++batch) {
+        if (EIGHT && (batch & 31) == 0) {
+          const int mine = i + a.lanes * lane;
+          codes = 127u | 127u << 8;
+          if (mine < hi) {
+            const int pos = s.base + kGran * mine;
+            int64_t row = start + pos;
+            if (paged) {
+              const int blk = pos < s.n ? a.block_table[(int64_t)b * a.max_blocks + (pos >> a.block_shift)] : -1;
+              row = blk >= 0 && blk < a.pages ? ((int64_t)blk << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : -1;
+            }
+            if (row >= 0 && row < a.num_rows) {
+              const int64_t from = g * a.scale_head + (row >> a.scale_shift);
+              codes = (uint32_t)a.ks[from] | (uint32_t)a.vs[from] << 8;
+            }
+          }
+        }
+        // on to granule number seq + i - lo of the block
+        slot += seq + i - lo - at;
+        at = seq + i - lo;
+        while (slot >= a.slots) { slot -= a.slots; round ^= 1u; }
+        if (!mbar_wait(full_bar(slot), round, abort_flag) && lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
+        const uint32_t kb = base + (uint32_t)slot * 2u * half_bytes + k_at, vb = base + (uint32_t)slot * 2u * half_bytes + v_at;
+        const uint32_t rows_ok = slot_mask[slot];
+        const int pos = s.base + kGran * i;
+        const bool whole = rows_ok == 0xffffu && pos >= all_from && pos + kGran <= all_to;  // every query sees all of it
+
+        float x[NT][4];  // rows rowq (columns hcol, hcol + 1), rowq + 8
+        {
+          float odd[NT][4];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[nt][k] = odd[nt][k] = 0.f;
+          if (EIGHT) {
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+              uint32_t kf[4];
+              ldmatrix_x4(kf, kb ^ (uint32_t)(st << 5));
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const uint32_t a0 = e4m3x2_to_f16x2(kf[2 * k]), a2 = e4m3x2_hi_to_f16x2(kf[2 * k]);
+                const uint32_t a1 = e4m3x2_to_f16x2(kf[2 * k + 1]), a3 = e4m3x2_hi_to_f16x2(kf[2 * k + 1]);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_f16(k ? odd[nt] : x[nt], a0, a1, a2, a3, qb[nt][2 * st + k][0], qb[nt][2 * st + k][1]);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) {
+              uint32_t kf[4];
+              ldmatrix_x4(kf, (kb ^ (uint32_t)((ks & 3) << 5)) + (ks & 4 ? upper : 0u));
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_bf16((ks & 1) ? odd[nt] : x[nt], kf, qb[nt][ks][0], qb[nt][ks][1]);
+            }
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[nt][k] += odd[nt][k];
+        }
+        // logits in the log2 domain
+        float ev = 0.f;
+        if (EIGHT) {
+          const uint32_t c = __shfl_sync(0xffffffffu, codes, batch & 31);
+          const float kf = exp2_int(scale_exponent(c & 255u) - kHeldBack);
+          ev = (float)scale_exponent(c >> 8);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[nt][k] = x[nt][k] * kf * qf[nt][k & 1];
+        } else {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[nt][k] *= a.scale_log2;
+        }
+        auto sees = [&](int t, int p, int row) {  // whether query token t sees position p, row `row` of the granule
+          const int here = s.n - T + t;
+          return ((rows_ok >> row) & 1u) && p < (a.causal ? here + 1 : s.n) && (a.window == 0 || p > here - a.window);
+        };
+        if (!whole) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int row = k < 2 ? row_lo : row_hi;
+              if (!sees(tok_of[nt][k & 1], pos + row, row)) x[nt][k] = -INFINITY;
+            }
+        }
+        // references: moved only where a weight would leave its range
+        bool move = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float y = fmaxf(x[nt][h], x[nt][h + 2]) - mx[nt][h];
+            move = move || y > kLazy || (EIGHT && y + ev > m[nt][h] + kLazy);
+          }
+        if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float top = fmaxf(x[nt][h], x[nt][h + 2]);
+#pragma unroll
+              for (int d = 4; d <= 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              const float mxn = fmaxf(mx[nt][h], top), drop = mx[nt][h] - mxn;
+              float alpha = fast_exp2(drop);
+              l[nt][h] *= alpha;
+              mx[nt][h] = mxn;
+              if (EIGHT) {
+                const float mo = m[nt][h] + drop, mn = fmaxf(mo, (top - mxn) + ev);
+                alpha = fast_exp2(mo - mn);
+                m[nt][h] = mn;
+              }
+#pragma unroll
+              for (int c = 0; c < 8; ++c) { o[nt][c][h] *= alpha; o[nt][c][h + 2] *= alpha; }
+            }
+        }
+        // weights, as the second product's B operand: column rowq of a tile
+        uint32_t pb[NT][2], pc[NT][2];  // (pc: what the rounding of pb left)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float y0 = x[nt][2 * r] - mx[nt][0], y1 = x[nt][2 * r + 1] - mx[nt][1];
+            const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
+            l[nt][0] += p0;
+            l[nt][1] += p1;
+            if (EIGHT) {
+              pb[nt][r] = movmatrix_trans(pack_f16x2(fast_exp2(y0 + (ev - m[nt][0])), fast_exp2(y1 + (ev - m[nt][1]))));
+            } else {
+              uint32_t first = pack_bf16x2(p0, p1);
+              if (PARTS > 1) {
+                const uint32_t rest = pack_bf16x2(p0 - bf16_lo(first), p1 - bf16_hi(first));
+                if (PARTS == 3) first = second ? rest : first;
+                else pc[nt][r] = movmatrix_trans(rest);
+              }
+              pb[nt][r] = movmatrix_trans(first);
+            }
+          }
+        auto add_to = [&](float (&d)[4], int nt, const uint32_t (&v)[4]) {
+          if (EIGHT) {
+            mma_f16(d, v[0], v[1], v[2], v[3], pb[nt][0], pb[nt][1]);
+          } else {
+            mma_bf16(d, v, pb[nt][0], pb[nt][1]);
+            if (PARTS == 2) mma_bf16(d, v, pc[nt][0], pc[nt][1]);
+          }
+        };
+        auto all_columns = [&](int c, const uint32_t (&v)[4]) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) add_to(o[nt][c], nt, v);
+        };
+        // O^T += V^T P^T
+        auto second_product = [&](uint32_t keep_lo, uint32_t keep_hi, auto multiply) {
+          if (EIGHT) {
+#pragma unroll
+            for (int c = 0; c < 8; c += 2) {
+              uint32_t v[4];
+              ldmatrix_b8_x2_trans(v, vb ^ (uint32_t)(c << 4));
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const uint32_t v0 = v[2 * j] & keep_lo, v1 = v[2 * j + 1] & keep_lo;
+                const uint32_t a0 = e4m3x2_to_f16x2(v0), a2 = e4m3x2_hi_to_f16x2(v0);
+                const uint32_t a1 = e4m3x2_to_f16x2(v1), a3 = e4m3x2_hi_to_f16x2(v1);
+                const uint32_t a4[4] = {a0, a1, a2, a3};
+                multiply(c + j, a4);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              uint32_t v[4];
+              ldmatrix_x4_trans(v, (vb ^ (uint32_t)((c & 3) << 5)) + (c & 4 ? upper : 0u));
+              v[0] &= keep_lo; v[1] &= keep_lo; v[2] &= keep_hi; v[3] &= keep_hi;
+              multiply(c, v);
+            }
+          }
+        };
+        if (whole) {
+          second_product(0xffffffffu, 0xffffffffu, all_columns);
+        } else {
+          // Rows that a query does not see have weight 0 there, and 0 times a NaN or an infinity is none: rows that nobody sees count
+          // as zeros. V rows of this lane's words: bf16 tokens hcol, + 1 (low and high half), those + 8; codes v_token(4 (lane & 3)) ..
+          auto keep = [&](auto visible, uint32_t& k_lo, uint32_t& k_hi) {
+            k_lo = k_hi = 0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int row = EIGHT ? v_token(2 * hcol + k) : hcol + (k & 1) + 8 * (k >> 1);
+              if (!visible(row)) continue;
+              if (EIGHT) k_lo |= 0xffu << (8 * k);
+              else if (k < 2) k_lo |= 0xffffu << (16 * k);
+              else k_hi |= 0xffffu << (16 * (k - 2));
+            }
+          };
+          uint32_t any_lo, any_hi, all_lo, all_hi;
+          keep([&](int row) { return ((rows_ok >> row) & 1u) && pos + row >= s.first && pos + row < s.n; }, any_lo, any_hi);
+          keep([&](int row) { return ((rows_ok >> row) & 1u) && pos + row >= all_from && pos + row < all_to; }, all_lo, all_hi);
+          bool odd_one = false;  // a number that is not finite in a row that some queries see and others do not
+          if (__any_sync(0xffffffffu, any_lo != all_lo || any_hi != all_hi)) {
+            const uint32_t part_lo = any_lo & ~all_lo, part_hi = any_hi & ~all_hi;
+            auto strange = [&](uint32_t w) {
+              if (EIGHT) return ((w & 0x7fu) == 0x7fu) | ((w & 0x7f00u) == 0x7f00u) | ((w & 0x7f0000u) == 0x7f0000u) | ((w & 0x7f000000u) == 0x7f000000u);
+              return ((w & 0x7f80u) == 0x7f80u) | ((w & 0x7f800000u) == 0x7f800000u);
+            };
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+              uint32_t v[4];
+              if (EIGHT) {
+                if (c & 1) continue;
+                ldmatrix_b8_x2_trans(v, vb ^ (uint32_t)(c << 4));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) odd_one = odd_one || strange(v[k] & part_lo);
+              } else {
+                ldmatrix_x4_trans(v, (vb ^ (uint32_t)((c & 3) << 5)) + (c & 4 ? upper : 0u));
+                odd_one = odd_one || strange(v[0] & part_lo) || strange(v[1] & part_lo) || strange(v[2] & part_hi) || strange(v[3] & part_hi);
+              }
+            }
+          }
+          if (!__any_sync(0xffffffffu, odd_one)) {
+            second_product(any_lo, any_hi, all_columns);
+          } else {  // one query token at a time, with the rows that it sees; the other columns' sums are dropped
+#pragma unroll 1
+            for (int t = 0; t < T; ++t) {
+              uint32_t one_lo, one_hi;
+              keep([&](int row) { return sees(t, pos + row, row); }, one_lo, one_hi);
+              second_product(one_lo, one_hi, [&](int c, const uint32_t (&v)[4]) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  float d[4] = {o[nt][c][0], o[nt][c][1], o[nt][c][2], o[nt][c][3]};
+                  add_to(d, nt, v);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) o[nt][c][k] = tok_of[nt][k & 1] == t ? d[k] : o[nt][c][k];
+                }
+              });
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty_bar(slot));
+      }
+      seq += hi - lo;
+      cur = unit + hi;
+
+      // ---- what becomes of the segment: the lanes' parts meet in shared memory, a column tile at a time ----------------
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int d = 4; d <= 16; d <<= 1) l[nt][h] += __shfl_xor_sync(0xffffffffu, l[nt][h], d);
+        }
+      if (PARTS == 3) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[0][c][k] += __shfl_xor_sync(0xffffffffu, o[0][c][k], 2);
+      }
+      const bool whole_unit = lo == 0 && hi == s.gran;
+      const int which = lo > 0 || unit == span_lo ? 0 : 1;
+      auto together = [&]() {
+        if (a.lanes > 1) named_barrier(1 + my_head * a.col_warps + my_cw, a.lanes * 32);
+        else __syncwarp();
+      };
+      float* mine = merge + warp * 8 * kPartialStride;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (PARTS == 3 && second) continue;
+          float* dst = mine + (hcol + h) * kPartialStride + rowq;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) { dst[16 * c] = o[nt][c][h]; dst[16 * c + 8] = o[nt][c][h + 2]; }
+          if (rowq == 0) *reinterpret_cast<float4*>(mine + (hcol + h) * kPartialStride + 128) = make_float4(mx[nt][h], l[nt][h], m[nt][h], 0.f);
+        }
+        together();
+        const int cols = min(PARTS == 3 ? 4 : 8, a.columns_used - col0 - nt * 8);
+        for (int c = my_lane; c < cols; c += a.lanes) {
+          auto part_of = [&](int i) {  // lane i's part of the column
+            return reinterpret_cast<const float4*>(merge + (((i * a.heads + my_head) * a.col_warps + my_cw) * 8 + c) * kPartialStride);
+          };
+          Folded f;
+          f.fold(lane < a.lanes ? part_of(lane)[32] : no_head(), a.lanes, [&](int i) { return part_of(i)[lane]; });
+          const int col = col0 + nt * 8 + c, t = col / G;
+          if (whole_unit) {
+            f.write(a, ((int64_t)b * T + t) * a.num_q_heads + g * G + (col - t * G), lane);
+          } else {
+            float4* rec = record_at(a, (int)blockIdx.x, which, my_head, my_cw * NT * 8 + nt * 8 + c);
+            __stcg(rec + lane, f.acc);
+            if (lane == 0) __stcg(rec + 32, make_float4(f.mx, f.l, f.m, 0.f));
+          }
+        }
+        together();
+      }
+    }
+    seq_base += s.gran * HG;
+    ++b;
+  }
+}
+
+// Joins the records of the rows whose unit several stretches share. ROWS rows per block, kJoinThreads / 32 / ROWS warps for each.
+template <int ROWS>
+__global__ void __launch_bounds__(kJoinThreads) dense_join_kernel(const __grid_constant__ DenseArgs a) {
+  constexpr int kWarps = kJoinThreads / 32, kShare = kWarps / ROWS;
+  __shared__ int sums[kWarps];
+  __shared__ __align__(16) float parts[kShare > 1 ? kWarps * kPartialStride : 4];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rows = a.T * a.num_q_heads, blocks_per_seq = (rows + ROWS - 1) / ROWS;
+  const int b = (int)blockIdx.x / blocks_per_seq, r = ((int)blockIdx.x - b * blocks_per_seq) * ROWS + warp / kShare;
+  // The lengths may be read before the wait: the kernel in front of this one released it behind its own wait.
+  int all = 0, prior = 0;
+  for (int i = tid; i < a.num_seqs; i += kJoinThreads) {
+    const int g = look_at(a, a.seq_len[i]).gran;
+    all += g;
+    if (i < b) prior += g;
+  }
+  int unused;
+  all = block_scan<kJoinThreads>(all, sums, unused);
+  prior = block_scan<kJoinThreads>(prior, sums, unused);
+  const Cut cut(a, all * a.head_groups);
+  const int gran = look_at(a, a.seq_len[b]).gran;
+  const int t = r / a.num_q_heads, h = r - t * a.num_q_heads, g = h / a.group;
+  const int hg = g / a.heads, hh = g - hg * a.heads, col = t * a.group + (h - g * a.group), ct = col / a.columns, cc = col - ct * a.columns;
+  const int unit = prior * a.head_groups + hg * gran;
+  const int first = cut.owner(unit), last = cut.owner(unit + gran - 1);
+  const bool mine = r < rows && last > first;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (kShare == 1) {
+    if (!mine) return;
+  } else if (!mine) {
+    return;  // the same for the whole block: it has one row
+  }
+  const int own = warp % kShare;
+  auto record = [&](int s) { return record_at(a, s * a.col_tiles + ct, s == first && cut.begin(s) < unit ? 1 : 0, hh, cc); };
+  Folded f;
+  const int count = (last - first - own + kShare) / kShare;  // stretches first + own, + kShare, ..
+  for (int k = 0; k < count; k += 32) {
+    const int s0 = first + own + k * kShare;
+    f.fold(k + lane < count ? __ldcg(record(s0 + lane * kShare) + 32) : no_head(), min(32, count - k),
+           [&](int i) { return __ldcg(record(s0 + i * kShare) + lane); });
+  }
+  if (kShare > 1) {
+    float4* p = reinterpret_cast<float4*>(parts + warp * kPartialStride);
+    p[lane] = f.acc;
+    if (lane == 0) p[32] = make_float4(f.mx, f.l, f.m, 0.f);
+    __syncthreads();
+    if (own != 0) return;
+    f = Folded();
+    f.fold(lane < kShare ? reinterpret_cast<const float4*>(parts + (warp + lane) * kPartialStride)[32] : no_head(), kShare,
+           [&](int i) { return reinterpret_cast<const float4*>(parts + (warp + i) * kPartialStride)[lane]; });
+  }
+  f.write(a, ((int64_t)b * a.T + t) * a.num_q_heads + h, lane);
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------------
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() {
+  static EncodeTiledFn fn = nullptr;
+  if (fn == nullptr) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess)
+      return nullptr;
+    fn = reinterpret_cast<EncodeTiledFn>(p);
+  }
+  return fn;
+}
+
+// K or V rows as boxes of 16 rows of `heads` heads. bf16: [half][head][row][64 elements], codes: [head][row][128].
+bool make_map(CUtensorMap* map, const void* ptr, bool eight, const clsa_params& p, int64_t token_stride, int64_t head_stride, int heads) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t size = eight ? 1 : 2;
+  if (p.num_kv_heads == 1) head_stride = 128;  // of one head it means nothing
+  const cuuint64_t dims[4] = {eight ? 128u : 64u, (cuuint64_t)p.num_cache_rows, (cuuint64_t)p.num_kv_heads, 2};
+  const cuuint64_t strides[3] = {(cuuint64_t)token_stride * size, (cuuint64_t)head_stride * size, 128};
+  const cuuint32_t box[4] = {eight ? 128u : 64u, kGran, (cuuint32_t)heads, 2};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, eight ? 3 : 4, const_cast<void*>(ptr), dims,
+            strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+DensePlan make_dense_plan(const clsa_params& p, bool eight, const DeviceInfo& dev) {
+  DensePlan d = {};
+  const int cols = p.q_per_seq * (p.num_q_heads / p.num_kv_heads);
+  d.fold = !eight && cols <= 4;
+  d.tiles = cols <= 8 ? 1 : 2;
+  d.col_warps = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
+  d.columns = d.fold ? 4 : d.tiles * d.col_warps * 8;
+  d.col_tiles = (cols + d.columns - 1) / d.columns;
+  d.heads = kConsumers / d.col_warps;
+  while (p.num_kv_heads % d.heads != 0) d.heads /= 2;
+  d.lanes = kConsumers / (d.col_warps * d.heads);
+  d.head_groups = p.num_kv_heads / d.heads;
+  d.slot_bytes = d.heads * kGran * (eight ? 256 : 512);
+  const int room = dev.max_smem_optin - kMergeBytes - kCtrlBytes - 1024;
+  d.slots = room / d.slot_bytes;
+  if (d.slots > kMaxSlots) d.slots = kMaxSlots;
+  d.smem_bytes = (size_t)d.slots * d.slot_bytes + kMergeBytes + kCtrlBytes + 1024;
+  d.spans = dev.sm_count / d.col_tiles;
+  return d;
+}
+
+size_t dense_partial_bytes(const DensePlan& d) {
+  return (size_t)d.spans * d.col_tiles * 2 * d.heads * d.columns * kPartialStride * sizeof(float);
+}
+
+cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int window, const DensePlan& plan, const void* q, void* out,
+                              float* lse, uint32_t* status, float* part, cudaStream_t stream) {
+  CUtensorMap map_k, map_v;
+  const bool eight = c != nullptr;
+  const int64_t token = eight ? c->kv_token_stride : p.kv_token_stride, head = eight ? c->kv_head_stride : p.kv_head_stride;
+  if (!make_map(&map_k, eight ? c->k : p.k_cache, eight, p, token, head, plan.heads) ||
+      !make_map(&map_v, eight ? c->v : p.v_cache, eight, p, token, head, plan.heads))
+    return cudaErrorInvalidValue;
+  DenseArgs a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.status = status;
+  a.part = part;
+  a.seq_start = p.seq_start;
+  a.seq_len = p.seq_len;
+  a.block_table = p.block_table;
+  if (eight) {
+    a.ks = static_cast<const uint8_t*>(c->k_scale);
+    a.vs = static_cast<const uint8_t*>(c->v_scale);
+    a.scale_head = c->scale_head_stride;
+    while ((1 << a.scale_shift) < c->scale_block) ++a.scale_shift;
+  }
+  a.num_rows = p.num_cache_rows;
+  while (p.block_table != nullptr && (1 << a.block_shift) < p.block_size) ++a.block_shift;
+  a.max_blocks = p.max_blocks_per_seq;
+  a.pages = (int)((p.num_cache_rows + (1 << a.block_shift) - 1) >> a.block_shift);
+  a.num_seqs = p.num_seqs;
+  a.T = p.q_per_seq;
+  a.num_q_heads = p.num_q_heads;
+  a.group = p.num_q_heads / p.num_kv_heads;
+  a.columns_used = a.T * a.group;
+  a.window = window < p.max_seq_len ? window : p.max_seq_len;  // (as far as a window reaches)
+  a.causal = p.causal;
+  a.max_seq_len = p.max_seq_len;
+  a.columns = plan.columns;
+  a.col_tiles = plan.col_tiles;
+  a.heads = plan.heads;
+  a.lanes = plan.lanes;
+  a.col_warps = plan.col_warps;
+  a.head_groups = plan.head_groups;
+  a.slots = plan.slots;
+  a.spans = plan.spans;
+  a.min_granules = plan.lanes > 2 ? plan.lanes : 2;
+  a.scale_log2 = p.sm_scale * kLog2e;
+  void (*kernel)(const CUtensorMap, const CUtensorMap, const DenseArgs) =
+      eight ? (plan.tiles == 1 ? dense_attn_kernel<true, 1, 1> : dense_attn_kernel<true, 2, 1>)
+            : (plan.fold ? dense_attn_kernel<false, 1, 3>
+               : plan.tiles == 1 ? dense_attn_kernel<false, 1, 2>
+               : plan.col_warps <= 2 ? dense_attn_kernel<false, 2, 2> : dense_attn_kernel<false, 2, 1>);
+  cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem_bytes);
+  if (err != cudaSuccess) return err;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(plan.spans * plan.col_tiles), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = plan.smem_bytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  err = cudaLaunchKernelEx(&cfg, kernel, map_k, map_v, a);
+  if (err != cudaSuccess) return err;
+  const int rows = a.T * a.num_q_heads;
+  const bool few = (int64_t)rows * a.num_seqs <= 1024;
+  cfg.gridDim = dim3((unsigned)(a.num_seqs * (few ? rows : (rows + 7) / 8)), 1, 1);
+  cfg.blockDim = dim3(kJoinThreads, 1, 1);
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, few ? dense_join_kernel<1> : dense_join_kernel<8>, a);
+}
+
+}  // namespace clsa

@@ -11,7 +11,9 @@
 // 4096 tokens of 32 + 8 heads of 128: 84 MB in 17.1 us, 4.9 TB/s, 0.76 of a measured copy (10.8 us with the input in L2; 18.1 and
 // 14.2 before a lane had its own partners). What is missing is the launch and the ramp of one wave: two to five passes at a time
 // measure the same, rings of asynchronous copies took 29 to 35, loading ahead by a batch 19.5. 16 tokens: 2.2 us, one launch.
-#include "cache8.cuh"
+#include <type_traits>
+
+#include "layer.cuh"
 
 namespace clsa {
 namespace {
@@ -29,12 +31,18 @@ struct NormRopeArgs {
   const int32_t* positions;
   int num_tokens, parts, part_heads;  // warps per token, heads of each
 };
+// With several positions per token: how far apart the axes lie, and the axis of each pair.
+struct NormRopeAxesArgs : NormRopeArgs {
+  int64_t axis_stride;
+  clsa_rope_axes axes;
+};
 
 // DENSE: heads lie head_dim apart, in and out (strides are immediates then). PAIR: the pairs lie half the turned dimensions apart,
 // and a lane of those has 4 dimensions of each half, 8 bytes apiece, and so the partner of each; ALL: every dimension is turned.
-// Not PAIR: partners are neighbours, or nothing is turned.
-template <int LANES, bool DENSE, bool PAIR, bool ALL>
-__global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
+// Not PAIR: partners are neighbours, or nothing is turned. Args: NormRopeArgs, or NormRopeAxesArgs.
+template <int LANES, bool DENSE, bool PAIR, bool ALL, class Args>
+__global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_constant__ Args a) {
+  constexpr bool kAxes = std::is_same<Args, NormRopeAxesArgs>::value;
   constexpr int kGroups = 32 / LANES;  // heads of a pass
   __shared__ __align__(16) float turns[kThreads / 32][2][LANES * 4];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -48,6 +56,11 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
   if (token >= (uint32_t)a.num_tokens) return;
   const int part0 = (int)(item - token * a.parts) * a.part_heads;
   const int pos = a.positions != nullptr ? a.positions[token] : 0;
+  int on_axis[CLSA_MAX_AXES - 1];  // the positions on the axes behind the first
+  if constexpr (kAxes) {
+#pragma unroll
+    for (int k = 1; k < CLSA_MAX_AXES; ++k) on_axis[k - 1] = k < a.axes.num_axes ? a.positions[k * a.axis_stride + token] : 0;
+  }
   // the heads of one side (0: queries, 1: keys) that this warp has, and its lanes' shares of the first pass
   uint4 raw[kUnroll];
   const uint16_t* in;
@@ -83,7 +96,15 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
   float* tc = turns[warp][0];
   float* ts = turns[warp][1];
   if (rot > 0) {
-    for (int i = lane; i < rot / 2; i += 32) turn_of(pos, a.spec.inv_freq[i], a.spec.rot_scale, &tc[i], &ts[i]);
+    for (int i = lane; i < rot / 2; i += 32) {
+      int at = pos;
+      if constexpr (kAxes) {
+        const int axis = a.axes.axis_of_pair[i];
+#pragma unroll
+        for (int k = 1; k < CLSA_MAX_AXES; ++k) at = axis == k ? on_axis[k - 1] : at;
+      }
+      turn_of(at, a.spec.inv_freq[i], a.spec.rot_scale, &tc[i], &ts[i]);
+    }
     __syncwarp();
   }
   const bool norm = a.spec.norm;
@@ -170,8 +191,8 @@ __global__ void __launch_bounds__(kThreads, 7) norm_rope_kernel(const __grid_con
   }
 }
 
-template <int LANES>
-void launch(NormRopeArgs& a, const DeviceInfo& dev, cudaStream_t stream) {
+template <int LANES, class Args>
+void launch(Args& a, const DeviceInfo& dev, cudaStream_t stream) {
   constexpr int kGroups = 32 / LANES;
   const int heads = a.heads[0] + a.heads[1];
   // parts of a token: as many as give every SM about 16 warps, each a whole number of the heads that a warp holds at a time (us with 8, 16
@@ -186,18 +207,15 @@ void launch(NormRopeArgs& a, const DeviceInfo& dev, cudaStream_t stream) {
   bool dense = true;
   for (int i = 0; i < 2; ++i) dense = dense && (a.heads[i] <= 1 || (a.in_head[i] == 8 * LANES && a.out_head[i] == 8 * LANES));
   const bool pair = a.spec.rot_dim > 0 && !a.spec.interleaved, all = pair && a.spec.rot_dim == 8 * LANES;
-  void (*kernel)(const NormRopeArgs) =
-      dense ? (all ? norm_rope_kernel<LANES, true, true, true> : pair ? norm_rope_kernel<LANES, true, true, false> : norm_rope_kernel<LANES, true, false, false>)
-            : (all ? norm_rope_kernel<LANES, false, true, true> : pair ? norm_rope_kernel<LANES, false, true, false> : norm_rope_kernel<LANES, false, false, false>);
+  void (*kernel)(const Args) =
+      dense ? (all ? norm_rope_kernel<LANES, true, true, true, Args> : pair ? norm_rope_kernel<LANES, true, true, false, Args> : norm_rope_kernel<LANES, true, false, false, Args>)
+            : (all ? norm_rope_kernel<LANES, false, true, true, Args> : pair ? norm_rope_kernel<LANES, false, true, false, Args> : norm_rope_kernel<LANES, false, false, false, Args>);
   kernel<<<blocks, kThreads, 0, stream>>>(a);
 }
 
-}  // namespace
-
-cudaError_t launch_norm_rope(const clsa_norm_rope_spec& spec, int num_tokens, const int32_t* positions, const clsa_heads* q,
-                             const clsa_heads* q_out, const clsa_heads* k, const clsa_heads* k_out, const DeviceInfo& dev,
-                             cudaStream_t stream) {
-  NormRopeArgs a = {};
+template <class Args>
+cudaError_t launch_any(Args& a, const clsa_norm_rope_spec& spec, int num_tokens, const int32_t* positions, const clsa_heads* q,
+                       const clsa_heads* q_out, const clsa_heads* k, const clsa_heads* k_out, const DeviceInfo& dev, cudaStream_t stream) {
   a.spec = {spec.norm, spec.rot_dim, spec.interleaved, spec.eps, spec.rot_scale, spec.inv_freq};
   a.weight[0] = static_cast<const uint16_t*>(spec.q_weight);
   a.weight[1] = static_cast<const uint16_t*>(spec.k_weight);
@@ -217,6 +235,24 @@ cudaError_t launch_norm_rope(const clsa_norm_rope_spec& spec, int num_tokens, co
   else if (spec.head_dim == 128) launch<16>(a, dev, stream);
   else launch<32>(a, dev, stream);
   return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_norm_rope(const clsa_norm_rope_spec& spec, int num_tokens, const int32_t* positions, const clsa_heads* q,
+                             const clsa_heads* q_out, const clsa_heads* k, const clsa_heads* k_out, const DeviceInfo& dev,
+                             cudaStream_t stream) {
+  NormRopeArgs a = {};
+  return launch_any(a, spec, num_tokens, positions, q, q_out, k, k_out, dev, stream);
+}
+
+cudaError_t launch_norm_rope_axes(const clsa_norm_rope_spec& spec, const clsa_rope_axes& axes, int num_tokens, const int32_t* positions,
+                                  int64_t axis_stride, const clsa_heads* q, const clsa_heads* q_out, const clsa_heads* k,
+                                  const clsa_heads* k_out, const DeviceInfo& dev, cudaStream_t stream) {
+  NormRopeAxesArgs a = {};
+  a.axis_stride = axis_stride;
+  a.axes = axes;
+  return launch_any(a, spec, num_tokens, positions, q, q_out, k, k_out, dev, stream);
 }
 
 }  // namespace clsa
