@@ -46,12 +46,12 @@ clsa_status dense(const clsa_params* p, const clsa_cache8* c, int32_t window, co
   if (workspace == nullptr || !aligned(workspace, 256)) return CLSA_ERR_WORKSPACE;
   DeviceInfo dev;
   if (!device_info(&dev)) return CLSA_ERR_CUDA;
-  const DensePlan plan = make_dense_plan(*p, c != nullptr, dev);
+  const DensePlan plan = make_dense_plan(*p, c != nullptr, window, dev);
   const size_t at = dense_scratch_offset(dev);
-  if (workspace_bytes < at + dense_partial_bytes(plan)) return CLSA_ERR_WORKSPACE;
+  if (workspace_bytes < at + plan.scratch_bytes) return CLSA_ERR_WORKSPACE;
   auto base = static_cast<unsigned char*>(workspace);
-  return from_cuda(launch_dense_attn(*p, c, window, plan, q, out, lse, reinterpret_cast<uint32_t*>(base),
-                                     reinterpret_cast<float*>(base + at), static_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_dense_attn(*p, c, window, plan, q, out, lse, reinterpret_cast<uint32_t*>(base), base + at,
+                                     static_cast<cudaStream_t>(stream)));
 }
 
 // A matrix of rows of `elements` elements, 16 bytes being `per16` of them (1: bytes without an alignment).
@@ -75,7 +75,7 @@ clsa_status clsa_dense_workspace_bytes(const clsa_params* p, size_t* bytes) {
   CLSA_TRY(check_dense(p, 0));
   DeviceInfo dev;
   if (!device_info(&dev)) return CLSA_ERR_CUDA;
-  const size_t a = dense_partial_bytes(make_dense_plan(*p, false, dev)), b = dense_partial_bytes(make_dense_plan(*p, true, dev));
+  const size_t a = make_dense_plan(*p, false, 0, dev).scratch_bytes, b = make_dense_plan(*p, true, 0, dev).scratch_bytes;
   *bytes = (dense_scratch_offset(dev) + (a > b ? a : b) + 255) / 256 * 256;
   return CLSA_OK;
 }

@@ -29,6 +29,9 @@
 // the order of the stretches: results do not depend on timing.
 #include <cuda.h>
 
+#include <atomic>
+#include <type_traits>
+
 #include "attn_common.cuh"
 #include "layer.cuh"
 
@@ -37,12 +40,13 @@ namespace {
 
 constexpr int kGran = 16;                 // positions per granule
 constexpr int kConsumers = 8;             // consuming warps
-constexpr int kThreads = (kConsumers + 1) * 32;
+constexpr int kThreads = (kConsumers + 4) * 32;  // .. and a warpgroup of which one warp fetches
+constexpr int kConsumerRegs = 224, kProducerRegs = 56;  // 8 x 32 x 224 + 4 x 32 x 56 = 64512 = kThreads x 168, what a launch gets
 constexpr int kJoinThreads = 256;
-constexpr int kMaxSlots = 40;
+constexpr int kMaxSlots = 32;                     // a lane of the producer for each
 constexpr int kMergeBytes = kConsumers * 8 * kPartialStride * 4;  // a column tile of every consuming warp
 constexpr int kCtrlBytes = 1024;
-constexpr uint32_t kSpinLimit = 1u << 22;  // polls of a barrier, each of which sleeps for a while: seconds
+constexpr uint32_t kSpinLimit = 1u << 22;  // polls of a barrier: seconds
 constexpr float kLazy = 8.f;
 constexpr float kNone = -3.4028234663852886e38f;  // a reference before the first token
 constexpr int kHeldBack = 22;                     // of K's exponent, kept for the query's factor: d 2^(ek - 22) is finite and keeps its last bits
@@ -53,6 +57,7 @@ struct DenseArgs {
   float* lse;
   uint32_t* status;
   float* part;
+  int2* units;  // per (sequence, head group): 2 x the first stretch it lies in + whether another unit is in front of it there, the last one
   const int64_t* seq_start;
   const int32_t* seq_len;
   const int32_t* block_table;
@@ -62,7 +67,7 @@ struct DenseArgs {
   int scale_shift, block_shift, max_blocks, pages;
   int num_seqs, T, num_q_heads, group, columns_used;  // columns_used: T * group
   int window, causal, max_seq_len;
-  int columns, col_tiles, heads, lanes, col_warps, head_groups, slots, spans, min_granules;
+  int columns, col_tiles, heads, lanes, col_warps, head_groups, slots, lane_slots, spans, min_granules, whole_units;
   float scale_log2;
 };
 
@@ -94,6 +99,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   }
   *abort_flag = 1u;
   return false;
+}
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {  // without waiting
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
 }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -170,13 +181,12 @@ __device__ __forceinline__ int block_scan(int v, int* sums, int& before) {
 __device__ __forceinline__ int k_token(int r) { return r < 4 ? r : r < 8 ? r + 8 : r - 4; }
 __device__ __forceinline__ int v_token(int i) { return k_token(2 * (i >> 2) + (i & 1) + ((i & 2) << 2)); }
 
-// Records of partial results (kPartialStride floats: 128 outputs, then mx, l, m) folded into a running one, lane i of a warp having the
-// i-th one's (mx, l, m) and fetch(i) its outputs.
+// Records of partial results (kPartialStride floats: 128 outputs, then mx, l, m) folded into a running one; a lane has four outputs.
 struct Folded {
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float mx = kNone, l = 0.f, m = kNone;
-  template <class F>
-  __device__ __forceinline__ void fold(float4 head, int count, F fetch) {
+  // What the running sums (returned) and the records' (into `share`, the lane's record's) are to be multiplied by; updates the references.
+  __device__ __forceinline__ float refer(float4 head, float& share) {
     float xn = fmaxf(mx, head.x);
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) xn = fmaxf(xn, __shfl_xor_sync(0xffffffffu, xn, d));
@@ -184,20 +194,47 @@ struct Folded {
     float mn = fmaxf(mold, mnew);
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
-    const float sn = fast_exp2(mnew - mn), so = fast_exp2(mold - mn);
+    share = fast_exp2(mnew - mn);
     float sum = fast_exp2(head.x - xn) * head.y;
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     l = l * fast_exp2(mx - xn) + sum;
-    acc.x *= so; acc.y *= so; acc.z *= so; acc.w *= so;
-#pragma unroll 8
-    for (int i = 0; i < count; ++i) {
-      const float4 v = fetch(i);
-      const float f = __shfl_sync(0xffffffffu, sn, i);
-      acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+    const float old = fast_exp2(mold - mn);
+    mx = xn;
+    m = mn;
+    return old;
+  }
+  __device__ __forceinline__ void scale(float f) { acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f; }
+  __device__ __forceinline__ void add(float f, float4 v) {
+    acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+  }
+  // A few records whose heads every lane of the warp has.
+  template <int N>
+  __device__ __forceinline__ void fold_few(const float4 (&head)[N], const float4 (&v)[N]) {
+    float xn = mx;
+#pragma unroll
+    for (int i = 0; i < N; ++i) xn = fmaxf(xn, head[i].x);
+    const float mold = (mx - xn) + m;
+    float mn = mold;
+#pragma unroll
+    for (int i = 0; i < N; ++i) mn = fmaxf(mn, (head[i].x - xn) + head[i].z);
+    l *= fast_exp2(mx - xn);
+    scale(fast_exp2(mold - mn));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      l = fmaf(fast_exp2(head[i].x - xn), head[i].y, l);
+      add(fast_exp2(((head[i].x - xn) + head[i].z) - mn), v[i]);
     }
     mx = xn;
     m = mn;
+  }
+  // N records, lane i having the i-th one's head (no_head and zeros where there is none).
+  template <int N>
+  __device__ __forceinline__ void fold_batch(float4 head, const float4 (&v)[N]) {
+    float share;
+    scale(refer(head, share));
+#pragma unroll
+    for (int i = 0; i < N; ++i) add(__shfl_sync(0xffffffffu, share, i), v[i]);
   }
   __device__ __forceinline__ void write(const DenseArgs& a, int64_t item, int lane) const {
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -218,8 +255,8 @@ __device__ __forceinline__ float4* record_at(const DenseArgs& a, int block, int 
 
 // ---- the kernel --------------------------------------------------------------------------------------------------------
 // EIGHT: an 8-bit cache. NT: column tiles per warp. PARTS (bf16): 1, the weights' rounding is all there is; 2, a second product takes
-// what it left; 3 (NT = 1, up to 4 columns), columns 4 .. 7 repeat the first four and take it.
-template <bool EIGHT, int NT, int PARTS>
+// what it left; 3 (NT = 1, up to 4 columns), columns 4 .. 7 repeat the first four and take it. STEP: granules that a warp works on together.
+template <bool EIGHT, int NT, int PARTS, int STEP>
 __global__ void __launch_bounds__(kThreads, 1)
 dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ DenseArgs a) {
   extern __shared__ unsigned char smem_dyn[];
@@ -235,14 +272,17 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   auto empty_bar = [&](int s) { return bars + 16u * s + 8u; };
   uint32_t* slot_mask = reinterpret_cast<uint32_t*>(ctrl + 16 * kMaxSlots);  // rows of the slot that exist
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 20 * kMaxSlots);
-  int* found = reinterpret_cast<int*>(ctrl + 20 * kMaxSlots + 16);  // first sequence of this block's stretch, granules before it
-  int* sums = found + 4;
+  int* found = reinterpret_cast<int*>(ctrl + 20 * kMaxSlots + 16);  // first sequence of this block's stretch, granules before it, its length
+  int64_t* found_start = reinterpret_cast<int64_t*>(found + 4);  // .. and its first row
+  int* sums = found + 6;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) {
-    for (int s = 0; s < a.slots; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), a.heads * a.col_warps); }
-    *abort_flag = 0u;
+  if (tid < a.slots) {
+    mbar_init(full_bar(tid), 1);
+    mbar_init(empty_bar(tid), a.heads * a.col_warps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  } else if (tid == kMaxSlots) {
+    *abort_flag = 0u;
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
   }
@@ -252,96 +292,150 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   // this block's stretch of the list
   const int HG = a.head_groups;
   const int span = (int)blockIdx.x / a.col_tiles, ct = (int)blockIdx.x - span * a.col_tiles;
-  int total = 0;
+  const bool one_pass = a.num_seqs <= kThreads, paged = a.block_table != nullptr;
+  int total = 0, len = 0, gran = 0, before = 0;
+  int64_t begin = 0;
+  auto read = [&](int i) {
+    gran = 0;
+    if (i >= a.num_seqs) return;
+    len = a.seq_len[i];
+    if (!paged) begin = a.seq_start[i];
+    gran = look_at(a, len).gran;
+  };
   for (int b0 = 0; b0 < a.num_seqs; b0 += kThreads) {
-    int before;
-    total += block_scan<kThreads>(b0 + tid < a.num_seqs ? look_at(a, a.seq_len[b0 + tid]).gran : 0, sums, before);
+    read(b0 + tid);
+    total += block_scan<kThreads>(gran, sums, before);
   }
   const Cut cut(a, total * HG);
   if (span >= cut.spans) return;
-  const int span_lo = cut.begin(span), span_hi = cut.begin(span + 1);
+  int span_lo = cut.begin(span), span_hi = cut.begin(span + 1);
   for (int b0 = 0, run = 0; b0 < a.num_seqs; b0 += kThreads) {
-    const int g = b0 + tid < a.num_seqs ? look_at(a, a.seq_len[b0 + tid]).gran : 0;
-    int before;
-    const int sum = block_scan<kThreads>(g, sums, before);
+    if (!one_pass) read(b0 + tid);
+    const int sum = one_pass ? total : block_scan<kThreads>(gran, sums, before);
     const int lo = (run + before) * HG;
-    if (lo <= span_lo && span_lo < lo + g * HG) { found[0] = b0 + tid; found[1] = lo; }
+    if (lo <= span_lo && span_lo < lo + gran * HG) {
+      found[0] = b0 + tid;
+      found[1] = lo;
+      found[2] = len;
+      *found_start = begin;
+    }
     run += sum;
     if (run * HG > span_lo) break;
   }
   __syncthreads();
+  const int b_first = found[0], base_first = found[1], len_first = found[2];
+  const int64_t start_first = *found_start;
+  if (a.whole_units) {  // the units that begin in the stretch, whole
+    const int g = look_at(a, len_first).gran;
+    span_lo = base_first + (span_lo - base_first + g - 1) / g * g;  // (within the sequence, or the next one's beginning)
+  }
 
-  int b = found[0], seq_base = found[1], cur = span_lo, seq = 0;  // seq: granules of this block before the segment
-  const bool paged = a.block_table != nullptr;
-
-  if (warp == kConsumers) {
-    // ---------------- producer ----------------
-    uint32_t issued = 0;
-    bool alive = true;
-    while (cur < span_hi) {
-      const Seq s = look_at(a, a.seq_len[b]);
-      int64_t start = paged ? 0 : a.seq_start[b];
-      bool bad = s.bad;
-      uint32_t bad_bit = CLSA_DEV_BAD_SEQLEN;
-      if (EIGHT && !paged && (start & (kGran - 1)) != 0) { bad = true; bad_bit = CLSA_DEV_BAD_SCALE_BLOCK; }
-      if (bad && lane == 0) flag_status(a.status, bad_bit);
-      for (int hg = (cur - seq_base) / s.gran; hg < HG && cur < span_hi; ++hg) {
-        const int unit = seq_base + hg * s.gran;
-        const int lo = cur - unit, hi = min(span_hi - unit, s.gran);
-        int entry = 0;
-        for (int i = lo; i < hi; ++i) {
-          const int k = (i - lo) & 31;
-          const int pos = s.base + kGran * i;
-          if (paged && k == 0) {  // the pages of the next 32 granules, a lane each
-            const int mine = pos + kGran * lane;
-            entry = mine < s.n ? a.block_table[(int64_t)b * a.max_blocks + (mine >> a.block_shift)] : -1;
-          }
-          int64_t row = start + pos;
-          if (paged) {
-            const int blk = __shfl_sync(0xffffffffu, entry, k);
-            row = blk >= 0 && blk < a.pages ? ((int64_t)blk << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : -kGran;
-          }
-          uint32_t mask = 0xffffu;
-          if (row < 0 || row + kGran > a.num_rows) {
-            if (row <= -kGran || row >= a.num_rows) { mask = 0u; row = -kGran; }  // nothing of it exists: a copy of zeros
-            if (mask != 0u && row < 0) mask &= 0xffffu << (int)-row;
-            if (mask != 0u && row + kGran > a.num_rows) mask &= 0xffffu >> (int)(row + kGran - a.num_rows);
-            const int from = max(0, s.first - pos), to = min(kGran, s.n - pos);
-            const uint32_t wanted = to > from ? ((1u << to) - 1u) & ~((1u << from) - 1u) : 0u;
-            if (lane == 0 && !bad && (wanted & ~mask) != 0u) flag_status(a.status, CLSA_DEV_BAD_INDEX);
-          }
-          if (bad) mask = 0u;
-          const int slot = (int)(issued % (uint32_t)a.slots);
-          if (alive) alive = mbar_wait(empty_bar(slot), ((issued / (uint32_t)a.slots) & 1u) ^ 1u, abort_flag);
-          if (alive && lane == 0) {
-            slot_mask[slot] = mask;
-            mbar_expect_tx(full_bar(slot), 2u * half_bytes);
-            const uint32_t dst = base + (uint32_t)slot * 2u * half_bytes;
-            if (EIGHT) {
-              tma_load_3d(dst, &map_k, 0, (int)row, hg * a.heads, full_bar(slot));
-              tma_load_3d(dst + half_bytes, &map_v, 0, (int)row, hg * a.heads, full_bar(slot));
-            } else {
-              tma_load_4d(dst, &map_k, 0, (int)row, hg * a.heads, 0, full_bar(slot));
-              tma_load_4d(dst + half_bytes, &map_v, 0, (int)row, hg * a.heads, 0, full_bar(slot));
-            }
-          }
-          alive = __shfl_sync(0xffffffffu, (int)alive, 0) != 0;
-          if (alive) ++issued;
-        }
-        cur = unit + hi;
+  if (warp >= kConsumers) {
+    // ---------------- producer: lane s of the warp has slot s ----------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
+    if (warp > kConsumers) return;
+    int b = b_first, seq_base = base_first;
+    Seq s = look_at(a, len_first);
+    int64_t start = start_first;
+    // The ring is one of lane_slots slots for each consuming lane, so that a slot's granules are waited for by the same warps in every round
+    // (a warp that waited for a round while the one before had not landed yet would take the parity of the one before that). Steps of STEP
+    // granules go to the lanes in turn: slot s holds granules number k = s % lane_slots, + lane_slots, .. of its lane.
+    const int ring = lane / a.lane_slots;
+    int k = lane - ring * a.lane_slots;
+    auto list_at = [&]() { return span_lo + (k / STEP * a.lanes + ring) * STEP + k % STEP; };
+    int at = list_at();  // the place of this lane's next granule in the list
+    // its place: position, head group, page table entry
+    bool valid;
+    int pos, hg, entry;
+    auto place = [&]() {
+      valid = lane < a.slots && at < span_hi;
+      if (!valid && !(a.whole_units && lane < a.slots)) return;
+      while (b < a.num_seqs && at >= seq_base + s.gran * HG) {
+        seq_base += s.gran * HG;
+        if (++b == a.num_seqs) break;
+        s = look_at(a, a.seq_len[b]);
+        start = paged ? 0 : a.seq_start[b];
       }
-      seq_base += s.gran * HG;
-      ++b;
-    }
-    if (!alive && lane == 0) {  // given up: the copies under way still land in this block's memory
-      flag_status(a.status, CLSA_DEV_TIMEOUT);
-      for (uint32_t i = issued > (uint32_t)a.slots ? issued - a.slots : 0u; i < issued; ++i)
-        for (uint32_t it = 0; it < kSpinLimit && !mbar_try_wait(full_bar((int)(i % a.slots)), (i / a.slots) & 1u); ++it) __nanosleep(64);
+      if (b == a.num_seqs) { valid = false; return; }
+      hg = (at - seq_base) / s.gran;
+      const int unit = seq_base + hg * s.gran, i = at - unit;
+      if (a.whole_units) {
+        valid = unit < span_hi;
+      } else if (i == 0 && ct == 0) {
+        a.units[(int64_t)b * HG + hg] = make_int2(2 * span + (unit == span_lo ? 0 : 1), cut.owner(unit + s.gran - 1));
+      }
+      pos = s.base + kGran * i;
+      entry = paged && valid && pos < s.n ? a.block_table[(int64_t)b * a.max_blocks + (pos >> a.block_shift)] : -1;
+    };
+    place();
+    uint32_t round = 0;
+    int rounds = 0;  // that this lane has issued
+    bool alive = true;
+    while (__any_sync(0xffffffffu, valid)) {
+      // the row, and what of the granule exists
+      int row32 = -kGran, z = 0;
+      uint32_t mask = 0u;
+      if (valid) {
+        bool bad = s.bad;
+        uint32_t bad_bit = CLSA_DEV_BAD_SEQLEN;
+        if (EIGHT && !paged && (start & (kGran - 1)) != 0) { bad = true; bad_bit = CLSA_DEV_BAD_SCALE_BLOCK; }
+        int64_t row = start + pos;
+        if (paged) row = entry >= 0 && entry < a.pages ? ((int64_t)entry << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : -kGran;
+        if (row > -kGran && row < a.num_rows) {
+          row32 = (int)row;
+          mask = 0xffffu;
+          if (row < 0) mask &= 0xffffu << (int)-row;
+          if (row + kGran > a.num_rows) mask &= 0xffffu >> (int)(row + kGran - a.num_rows);
+        }
+        if (bad) {
+          flag_status(a.status, bad_bit);
+          mask = 0u;
+        } else if (mask != 0xffffu) {
+          const int from = max(0, s.first - pos), to = min(kGran, s.n - pos);
+          const uint32_t wanted = to > from ? ((1u << to) - 1u) & ~((1u << from) - 1u) : 0u;
+          if ((wanted & ~mask) != 0u) flag_status(a.status, CLSA_DEV_BAD_INDEX);
+        }
+        z = hg * a.heads;
+      }
+      const bool mine = valid;
+      k += a.lane_slots;
+      at = list_at();
+      place();  // the next one's, whose lookups are under way while this one waits for its slot
+      bool pending = mine;
+      for (uint32_t it = 0; alive && __any_sync(0xffffffffu, pending); ++it) {
+        if (pending && mbar_test(empty_bar(lane), (round & 1u) ^ 1u)) {
+          slot_mask[lane] = mask;
+          const uint32_t bar = full_bar(lane), dst = base + (uint32_t)lane * 2u * half_bytes;
+          mbar_expect_tx(bar, 2u * half_bytes);
+          if (EIGHT) {
+            tma_load_3d(dst, &map_k, 0, row32, z, bar);
+            tma_load_3d(dst + half_bytes, &map_v, 0, row32, z, bar);
+          } else {
+            tma_load_4d(dst, &map_k, 0, row32, z, 0, bar);
+            tma_load_4d(dst + half_bytes, &map_v, 0, row32, z, 0, bar);
+          }
+          pending = false;
+          ++rounds;
+        }
+        if (it >= kSpinLimit) *abort_flag = 1u;
+        if ((it & 63u) == 63u) {
+          __nanosleep(64);
+          alive = !__any_sync(0xffffffffu, *abort_flag != 0u);
+        }
+      }
+      if (!alive) {  // given up: the copies under way still land in this block's memory
+        if (lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
+        if (rounds > 0)
+          for (uint32_t it = 0; it < kSpinLimit && !mbar_test(full_bar(lane), (uint32_t)(rounds - 1) & 1u); ++it) __nanosleep(64);
+        return;
+      }
+      ++round;
     }
     return;
   }
 
   // ---------------- consumers ----------------
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs));
   const int my_cw = warp % a.col_warps, my_head = (warp / a.col_warps) % a.heads, my_lane = warp / (a.col_warps * a.heads);
   const int rowq = lane >> 2, hcol = (lane & 3) * 2, t7 = lane & 7;
   const bool second = PARTS == 3 && (lane & 2) != 0;  // this lane's columns take what the rounding left
@@ -358,28 +452,32 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   int row_lo, row_hi;  // tokens of rows rowq and rowq + 8 of the first product
   if (EIGHT) {
     const int kt = k_token(t7 + 8 * ((lane >> 3) & 1)), vt = v_token(lane & 15);
-    k_at = (uint32_t)(my_head * 2048 + kt * 128 + (((lane >> 4) ^ (kt & 7)) << 4));
-    v_at = (uint32_t)(my_head * 2048 + vt * 128 + (((lane >> 4) ^ (vt & 7)) << 4)) + half_bytes;
+    k_at = base + (uint32_t)(my_head * 2048 + kt * 128 + (((lane >> 4) ^ (kt & 7)) << 4));
+    v_at = base + (uint32_t)(my_head * 2048 + vt * 128 + (((lane >> 4) ^ (vt & 7)) << 4)) + half_bytes;
     row_lo = k_token(rowq);
     row_hi = k_token(rowq + 8);
   } else {
     const int kt = t7 + 8 * ((lane >> 3) & 1), vt = t7 + 8 * (lane >> 4);
-    k_at = (uint32_t)(my_head * 2048 + kt * 128 + (((lane >> 4) ^ t7) << 4));
-    v_at = (uint32_t)(my_head * 2048 + vt * 128 + ((((lane >> 3) & 1) ^ t7) << 4)) + half_bytes;
+    k_at = base + (uint32_t)(my_head * 2048 + kt * 128 + (((lane >> 4) ^ t7) << 4));
+    v_at = base + (uint32_t)(my_head * 2048 + vt * 128 + ((((lane >> 3) & 1) ^ t7) << 4)) + half_bytes;
     row_lo = rowq;
     row_hi = rowq + 8;
   }
   const uint32_t upper = half_bytes / 2;  // from dimensions 0 .. 63 of the bf16 rows to 64 .. 127
-  int slot = 0;             // of this block's granule `at`, and the parity of its round
+  int b = b_first, seq_base = base_first, cur = span_lo, len_b = len_first;
+  int64_t start = start_first;
+  int seq = 0;                           // granules of this block before the segment
+  const int ring0 = my_lane * a.lane_slots;
+  int slot = 0;                          // of this lane's ring: its next granule's, and the parity of that round
   uint32_t round = 0;
-  int at = 0;
 
-  while (cur < span_hi) {
-    const Seq s = look_at(a, a.seq_len[b]);
-    const int64_t start = EIGHT && !paged ? a.seq_start[b] : 0;
+  while (cur < span_hi && b < a.num_seqs) {
+    const Seq s = look_at(a, len_b);
+    const int len_next = b + 1 < a.num_seqs ? a.seq_len[b + 1] : 0;
+    const int64_t start_next = EIGHT && !paged && b + 1 < a.num_seqs ? a.seq_start[b + 1] : 0;
     for (int hg = (cur - seq_base) / s.gran; hg < HG && cur < span_hi; ++hg) {
       const int unit = seq_base + hg * s.gran;
-      const int lo = cur - unit, hi = min(span_hi - unit, s.gran);
+      const int lo = cur - unit, hi = a.whole_units ? s.gran : min(span_hi - unit, s.gran);
       const int g = hg * a.heads + my_head;  // KV head
       // queries, as B operands: column rowq of a tile
       uint32_t qb[NT][8][2];
@@ -387,7 +485,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int col = col0 + nt * 8 + (PARTS == 3 ? rowq & 3 : rowq);
-        const bool used = col < a.columns_used && (PARTS != 3 || (rowq & 3) < a.columns);
+        const bool used = col < a.columns_used;
         const int t = col / G, j = col - t * G;
         const uint16_t* src = a.q + (((int64_t)b * T + t) * a.num_q_heads + g * G + j) * 128;
         if (EIGHT) {
@@ -397,13 +495,15 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const uint2 v = used ? *reinterpret_cast<const uint2*>(src + 16 * st + 2 * hcol) : make_uint2(0u, 0u);
             qb[nt][st][0] = v.x;
             qb[nt][st][1] = v.y;
+          }
+#pragma unroll
+          for (int st = 0; st < 8; ++st)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               const float x = fabsf(bf16_lo(qb[nt][st][k])), y = fabsf(bf16_hi(qb[nt][st][k]));
               if (x <= 3.4028234663852886e38f) amax = fmaxf(amax, x);  // finite
               if (y <= 3.4028234663852886e38f) amax = fmaxf(amax, y);
             }
-          }
           amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
           amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
           const int shift = min(13 + 127 - (int)(__float_as_uint(amax) >> 23), 120);  // largest magnitude into [2^13, 2^14)
@@ -435,99 +535,72 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       }
       // every query sees [all_from, all_to)
       const int all_from = a.window ? max(0, s.n - a.window) : 0, all_to = a.causal ? s.n - T + 1 : s.n;
-      uint32_t codes = 0;  // 8-bit: scale bytes of this lane's granules, 32 at a time, one per lane of the warp
-      int batch = 0;
 
-      int i = lo + ((my_lane - seq) % a.lanes + a.lanes) % a.lanes;  // this warp's granules: those whose number in the block is my_lane mod lanes
-      for (; i < hi; i += a.lanes, ++batch) {
-        if (EIGHT && (batch & 31) == 0) {
-          const int mine = i + a.lanes * lane;
-          codes = 127u | 127u << 8;
-          if (mine < hi) {
-            const int pos = s.base + kGran * mine;
-            int64_t row = start + pos;
-            if (paged) {
-              const int blk = pos < s.n ? a.block_table[(int64_t)b * a.max_blocks + (pos >> a.block_shift)] : -1;
-              row = blk >= 0 && blk < a.pages ? ((int64_t)blk << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : -1;
-            }
-            if (row >= 0 && row < a.num_rows) {
-              const int64_t from = g * a.scale_head + (row >> a.scale_shift);
-              codes = (uint32_t)a.ks[from] | (uint32_t)a.vs[from] << 8;
-            }
+      // One step: U granules from position pos0 on, in the slots whose K and V rows are at kb[] and vb[]. MASKED (U = 1): some query does not
+      // see all of it, rows_ok has its rows that exist. codes: the scale bytes (8-bit caches).
+      auto step = [&](auto u_const, auto masked_const, int pos0, const uint32_t* kb, const uint32_t* vb, uint32_t rows_ok, const uint32_t* codes) {
+        constexpr int U = decltype(u_const)::value;
+        constexpr bool MASKED = decltype(masked_const)::value;
+        float x[U][NT][4], ev[U];  // rows rowq (columns hcol, hcol + 1), rowq + 8
+        constexpr bool kOdd = U * NT == 1;  // two chains of dependent products where there would be one
+        float odd[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            odd[nt][k] = 0.f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u][nt][k] = 0.f;
           }
-        }
-        // on to granule number seq + i - lo of the block
-        slot += seq + i - lo - at;
-        at = seq + i - lo;
-        while (slot >= a.slots) { slot -= a.slots; round ^= 1u; }
-        if (!mbar_wait(full_bar(slot), round, abort_flag) && lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
-        const uint32_t kb = base + (uint32_t)slot * 2u * half_bytes + k_at, vb = base + (uint32_t)slot * 2u * half_bytes + v_at;
-        const uint32_t rows_ok = slot_mask[slot];
-        const int pos = s.base + kGran * i;
-        const bool whole = rows_ok == 0xffffu && pos >= all_from && pos + kGran <= all_to;  // every query sees all of it
-
-        float x[NT][4];  // rows rowq (columns hcol, hcol + 1), rowq + 8
-        {
-          float odd[NT][4];
+        if (EIGHT) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int st = 0; st < 4; ++st)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[nt][k] = odd[nt][k] = 0.f;
-          if (EIGHT) {
-#pragma unroll
-            for (int st = 0; st < 4; ++st) {
+            for (int u = 0; u < U; ++u) {
               uint32_t kf[4];
-              ldmatrix_x4(kf, kb ^ (uint32_t)(st << 5));
+              ldmatrix_x4(kf, kb[u] ^ (uint32_t)(st << 5));
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
                 const uint32_t a0 = e4m3x2_to_f16x2(kf[2 * k]), a2 = e4m3x2_hi_to_f16x2(kf[2 * k]);
                 const uint32_t a1 = e4m3x2_to_f16x2(kf[2 * k + 1]), a3 = e4m3x2_hi_to_f16x2(kf[2 * k + 1]);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma_f16(k ? odd[nt] : x[nt], a0, a1, a2, a3, qb[nt][2 * st + k][0], qb[nt][2 * st + k][1]);
+                for (int nt = 0; nt < NT; ++nt) mma_f16(kOdd && k ? odd[nt] : x[u][nt], a0, a1, a2, a3, qb[nt][2 * st + k][0], qb[nt][2 * st + k][1]);
               }
             }
-          } else {
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-              uint32_t kf[4];
-              ldmatrix_x4(kf, (kb ^ (uint32_t)((ks & 3) << 5)) + (ks & 4 ? upper : 0u));
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_bf16((ks & 1) ? odd[nt] : x[nt], kf, qb[nt][ks][0], qb[nt][ks][1]);
-            }
-          }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[nt][k] += odd[nt][k];
-        }
-        // logits in the log2 domain
-        float ev = 0.f;
-        if (EIGHT) {
-          const uint32_t c = __shfl_sync(0xffffffffu, codes, batch & 31);
-          const float kf = exp2_int(scale_exponent(c & 255u) - kHeldBack);
-          ev = (float)scale_exponent(c >> 8);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[nt][k] = x[nt][k] * kf * qf[nt][k & 1];
         } else {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[nt][k] *= a.scale_log2;
+            for (int u = 0; u < U; ++u) {
+              uint32_t kf[4];
+              ldmatrix_x4(kf, (kb[u] ^ (uint32_t)((ks & 3) << 5)) + (ks & 4 ? upper : 0u));
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_bf16(kOdd && (ks & 1) ? odd[nt] : x[u][nt], kf, qb[nt][ks][0], qb[nt][ks][1]);
+            }
         }
-        auto sees = [&](int t, int p, int row) {  // whether query token t sees position p, row `row` of the granule
-          const int here = s.n - T + t;
-          return ((rows_ok >> row) & 1u) && p < (a.causal ? here + 1 : s.n) && (a.window == 0 || p > here - a.window);
-        };
-        if (!whole) {
+        // logits in the log2 domain
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float kf = EIGHT ? exp2_int(scale_exponent(codes[u] & 255u) - kHeldBack) : a.scale_log2;
+          ev[u] = EIGHT ? (float)scale_exponent(codes[u] >> 8) : 0.f;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const int row = k < 2 ? row_lo : row_hi;
-              if (!sees(tok_of[nt][k & 1], pos + row, row)) x[nt][k] = -INFINITY;
+              const float d = kOdd ? x[u][nt][k] + odd[nt][k] : x[u][nt][k];
+              x[u][nt][k] = EIGHT ? d * kf * qf[nt][k & 1] : d * kf;
             }
+        }
+        auto sees = [&](int t, int row) {  // whether query token t sees row `row` of the granule
+          const int here = s.n - T + t, p = pos0 + row;
+          return ((rows_ok >> row) & 1u) && p < (a.causal ? here + 1 : s.n) && (a.window == 0 || p > here - a.window);
+        };
+        if constexpr (MASKED) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (!sees(tok_of[nt][k & 1], k < 2 ? row_lo : row_hi)) x[0][nt][k] = -INFINITY;
         }
         // references: moved only where a weight would leave its range
         bool move = false;
@@ -535,23 +608,37 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float y = fmaxf(x[nt][h], x[nt][h + 2]) - mx[nt][h];
-            move = move || y > kLazy || (EIGHT && y + ev > m[nt][h] + kLazy);
+            float top = -INFINITY, top_e = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const float y = fmaxf(x[u][nt][h], x[u][nt][h + 2]) - mx[nt][h];
+              top = fmaxf(top, y);
+              if (EIGHT) top_e = fmaxf(top_e, y + ev[u]);
+            }
+            move = move || top > kLazy || (EIGHT && top_e > m[nt][h] + kLazy);
           }
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              float top = fmaxf(x[nt][h], x[nt][h + 2]);
+              float tops[U], top = -INFINITY;
 #pragma unroll
-              for (int d = 4; d <= 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              for (int u = 0; u < U; ++u) {
+                tops[u] = fmaxf(x[u][nt][h], x[u][nt][h + 2]);
+#pragma unroll
+                for (int d = 4; d <= 16; d <<= 1) tops[u] = fmaxf(tops[u], __shfl_xor_sync(0xffffffffu, tops[u], d));
+                top = fmaxf(top, tops[u]);
+              }
               const float mxn = fmaxf(mx[nt][h], top), drop = mx[nt][h] - mxn;
               float alpha = fast_exp2(drop);
               l[nt][h] *= alpha;
               mx[nt][h] = mxn;
               if (EIGHT) {
-                const float mo = m[nt][h] + drop, mn = fmaxf(mo, (top - mxn) + ev);
+                const float mo = m[nt][h] + drop;
+                float mn = mo;
+#pragma unroll
+                for (int u = 0; u < U; ++u) mn = fmaxf(mn, (tops[u] - mxn) + ev[u]);
                 alpha = fast_exp2(mo - mn);
                 m[nt][h] = mn;
               }
@@ -560,67 +647,71 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
         }
         // weights, as the second product's B operand: column rowq of a tile
-        uint32_t pb[NT][2], pc[NT][2];  // (pc: what the rounding of pb left)
+        uint32_t pb[U][NT][2], pc[U][NT][2];  // (pc: what the rounding of pb left)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const float y0 = x[nt][2 * r] - mx[nt][0], y1 = x[nt][2 * r + 1] - mx[nt][1];
-            const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
-            l[nt][0] += p0;
-            l[nt][1] += p1;
-            if (EIGHT) {
-              pb[nt][r] = movmatrix_trans(pack_f16x2(fast_exp2(y0 + (ev - m[nt][0])), fast_exp2(y1 + (ev - m[nt][1]))));
-            } else {
-              uint32_t first = pack_bf16x2(p0, p1);
-              if (PARTS > 1) {
-                const uint32_t rest = pack_bf16x2(p0 - bf16_lo(first), p1 - bf16_hi(first));
-                if (PARTS == 3) first = second ? rest : first;
-                else pc[nt][r] = movmatrix_trans(rest);
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const float y0 = x[u][nt][2 * r] - mx[nt][0], y1 = x[u][nt][2 * r + 1] - mx[nt][1];
+              const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
+              l[nt][0] += p0;
+              l[nt][1] += p1;
+              if (EIGHT) {
+                pb[u][nt][r] = movmatrix_trans(pack_f16x2(fast_exp2(y0 + (ev[u] - m[nt][0])), fast_exp2(y1 + (ev[u] - m[nt][1]))));
+              } else {
+                uint32_t first = pack_bf16x2(p0, p1);
+                if (PARTS > 1) {
+                  const uint32_t rest = pack_bf16x2(p0 - bf16_lo(first), p1 - bf16_hi(first));
+                  if (PARTS == 3) first = second ? rest : first;
+                  else pc[u][nt][r] = movmatrix_trans(rest);
+                }
+                pb[u][nt][r] = movmatrix_trans(first);
               }
-              pb[nt][r] = movmatrix_trans(first);
             }
-          }
-        auto add_to = [&](float (&d)[4], int nt, const uint32_t (&v)[4]) {
+        auto add_to = [&](float (&d)[4], int u, int nt, const uint32_t (&v)[4]) {
           if (EIGHT) {
-            mma_f16(d, v[0], v[1], v[2], v[3], pb[nt][0], pb[nt][1]);
+            mma_f16(d, v[0], v[1], v[2], v[3], pb[u][nt][0], pb[u][nt][1]);
           } else {
-            mma_bf16(d, v, pb[nt][0], pb[nt][1]);
-            if (PARTS == 2) mma_bf16(d, v, pc[nt][0], pc[nt][1]);
+            mma_bf16(d, v, pb[u][nt][0], pb[u][nt][1]);
+            if (PARTS == 2) mma_bf16(d, v, pc[u][nt][0], pc[u][nt][1]);
           }
         };
-        auto all_columns = [&](int c, const uint32_t (&v)[4]) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) add_to(o[nt][c], nt, v);
-        };
-        // O^T += V^T P^T
+        // O^T += V^T P^T, with the V rows that keep_lo and keep_hi let through
         auto second_product = [&](uint32_t keep_lo, uint32_t keep_hi, auto multiply) {
           if (EIGHT) {
 #pragma unroll
-            for (int c = 0; c < 8; c += 2) {
-              uint32_t v[4];
-              ldmatrix_b8_x2_trans(v, vb ^ (uint32_t)(c << 4));
+            for (int c = 0; c < 8; c += 2)
 #pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const uint32_t v0 = v[2 * j] & keep_lo, v1 = v[2 * j + 1] & keep_lo;
-                const uint32_t a0 = e4m3x2_to_f16x2(v0), a2 = e4m3x2_hi_to_f16x2(v0);
-                const uint32_t a1 = e4m3x2_to_f16x2(v1), a3 = e4m3x2_hi_to_f16x2(v1);
-                const uint32_t a4[4] = {a0, a1, a2, a3};
-                multiply(c + j, a4);
+              for (int u = 0; u < U; ++u) {
+                uint32_t v[4];
+                ldmatrix_b8_x2_trans(v, vb[u] ^ (uint32_t)(c << 4));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                  const uint32_t v0 = MASKED ? v[2 * j] & keep_lo : v[2 * j], v1 = MASKED ? v[2 * j + 1] & keep_lo : v[2 * j + 1];
+                  const uint32_t a4[4] = {e4m3x2_to_f16x2(v0), e4m3x2_to_f16x2(v1), e4m3x2_hi_to_f16x2(v0), e4m3x2_hi_to_f16x2(v1)};
+                  multiply(u, c + j, a4);
+                }
               }
-            }
           } else {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              uint32_t v[4];
-              ldmatrix_x4_trans(v, (vb ^ (uint32_t)((c & 3) << 5)) + (c & 4 ? upper : 0u));
-              v[0] &= keep_lo; v[1] &= keep_lo; v[2] &= keep_hi; v[3] &= keep_hi;
-              multiply(c, v);
-            }
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+              for (int u = 0; u < U; ++u) {
+                uint32_t v[4];
+                ldmatrix_x4_trans(v, (vb[u] ^ (uint32_t)((c & 3) << 5)) + (c & 4 ? upper : 0u));
+                if (MASKED) { v[0] &= keep_lo; v[1] &= keep_lo; v[2] &= keep_hi; v[3] &= keep_hi; }
+                multiply(u, c, v);
+              }
           }
         };
-        if (whole) {
-          second_product(0xffffffffu, 0xffffffffu, all_columns);
+        auto all_columns = [&](int u, int c, const uint32_t (&v)[4]) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) add_to(o[nt][c], u, nt, v);
+        };
+        if constexpr (!MASKED) {
+          second_product(0u, 0u, all_columns);
         } else {
           // Rows that a query does not see have weight 0 there, and 0 times a NaN or an infinity is none: rows that nobody sees count
           // as zeros. V rows of this lane's words: bf16 tokens hcol, + 1 (low and high half), those + 8; codes v_token(4 (lane & 3)) ..
@@ -636,41 +727,36 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
           };
           uint32_t any_lo, any_hi, all_lo, all_hi;
-          keep([&](int row) { return ((rows_ok >> row) & 1u) && pos + row >= s.first && pos + row < s.n; }, any_lo, any_hi);
-          keep([&](int row) { return ((rows_ok >> row) & 1u) && pos + row >= all_from && pos + row < all_to; }, all_lo, all_hi);
-          bool odd_one = false;  // a number that is not finite in a row that some queries see and others do not
+          keep([&](int row) { return ((rows_ok >> row) & 1u) && pos0 + row >= s.first && pos0 + row < s.n; }, any_lo, any_hi);
+          keep([&](int row) { return ((rows_ok >> row) & 1u) && pos0 + row >= all_from && pos0 + row < all_to; }, all_lo, all_hi);
+          bool strange = false;  // a number that is not finite in a row that some queries see and others do not
           if (__any_sync(0xffffffffu, any_lo != all_lo || any_hi != all_hi)) {
             const uint32_t part_lo = any_lo & ~all_lo, part_hi = any_hi & ~all_hi;
-            auto strange = [&](uint32_t w) {
+            auto look = [&](uint32_t w) {
               if (EIGHT) return ((w & 0x7fu) == 0x7fu) | ((w & 0x7f00u) == 0x7f00u) | ((w & 0x7f0000u) == 0x7f0000u) | ((w & 0x7f000000u) == 0x7f000000u);
               return ((w & 0x7f80u) == 0x7f80u) | ((w & 0x7f800000u) == 0x7f800000u);
             };
 #pragma unroll 1
-            for (int c = 0; c < 8; ++c) {
+            for (int c = 0; c < 8; c += EIGHT ? 2 : 1) {
               uint32_t v[4];
-              if (EIGHT) {
-                if (c & 1) continue;
-                ldmatrix_b8_x2_trans(v, vb ^ (uint32_t)(c << 4));
+              if (EIGHT) ldmatrix_b8_x2_trans(v, vb[0] ^ (uint32_t)(c << 4));
+              else ldmatrix_x4_trans(v, (vb[0] ^ (uint32_t)((c & 3) << 5)) + (c & 4 ? upper : 0u));
 #pragma unroll
-                for (int k = 0; k < 4; ++k) odd_one = odd_one || strange(v[k] & part_lo);
-              } else {
-                ldmatrix_x4_trans(v, (vb ^ (uint32_t)((c & 3) << 5)) + (c & 4 ? upper : 0u));
-                odd_one = odd_one || strange(v[0] & part_lo) || strange(v[1] & part_lo) || strange(v[2] & part_hi) || strange(v[3] & part_hi);
-              }
+              for (int k = 0; k < 4; ++k) strange = strange || look(v[k] & (EIGHT || k < 2 ? part_lo : part_hi));
             }
           }
-          if (!__any_sync(0xffffffffu, odd_one)) {
+          if (!__any_sync(0xffffffffu, strange)) {
             second_product(any_lo, any_hi, all_columns);
           } else {  // one query token at a time, with the rows that it sees; the other columns' sums are dropped
 #pragma unroll 1
             for (int t = 0; t < T; ++t) {
               uint32_t one_lo, one_hi;
-              keep([&](int row) { return sees(t, pos + row, row); }, one_lo, one_hi);
-              second_product(one_lo, one_hi, [&](int c, const uint32_t (&v)[4]) {
+              keep([&](int row) { return sees(t, row); }, one_lo, one_hi);
+              second_product(one_lo, one_hi, [&](int u, int c, const uint32_t (&v)[4]) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                   float d[4] = {o[nt][c][0], o[nt][c][1], o[nt][c][2], o[nt][c][3]};
-                  add_to(d, nt, v);
+                  add_to(d, u, nt, v);
 #pragma unroll
                   for (int k = 0; k < 4; ++k) o[nt][c][k] = tok_of[nt][k & 1] == t ? d[k] : o[nt][c][k];
                 }
@@ -678,10 +764,62 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
           }
         }
+      };
+
+      // This lane's steps of the block are those with number my_lane mod lanes; a segment that ends inside one has its part of it.
+      const int end = seq + hi - lo, step0 = seq / STEP;
+      int n_step = step0 + (my_lane - step0 % a.lanes + a.lanes) % a.lanes;
+      uint32_t held = 0;  // 8-bit: scale bytes of this warp's granules, 32 at a time, one per lane
+      int have = 0;       // .. of which granules this step's are
+      for (; n_step * STEP < end; n_step += a.lanes, have += STEP) {
+        if (EIGHT && (have & 31) == 0) {
+          const int n = (n_step + lane / STEP * a.lanes) * STEP + lane % STEP;
+          held = 127u | 127u << 8;
+          if (n >= seq && n < end) {
+            const int pos = s.base + kGran * (lo + n - seq);
+            int64_t row = start + pos;
+            if (paged) {
+              const int blk = pos < s.n ? a.block_table[(int64_t)b * a.max_blocks + (pos >> a.block_shift)] : -1;
+              row = blk >= 0 && blk < a.pages ? ((int64_t)blk << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : -1;
+            }
+            if (row >= 0 && row < a.num_rows) {
+              const int64_t from = g * a.scale_head + (row >> a.scale_shift);
+              held = (uint32_t)a.ks[from] | (uint32_t)a.vs[from] << 8;
+            }
+          }
+        }
+        const int n0 = max(n_step * STEP, seq), count = min(n_step * STEP + STEP, end) - n0, skip = n0 - n_step * STEP;
+        const int pos0 = s.base + kGran * (lo + n0 - seq);
+        uint32_t kb[STEP], vb[STEP], codes[STEP];
+        uint32_t rows_ok = 0xffffu;
+        const int slot_before = slot;
+#pragma unroll
+        for (int u = 0; u < STEP; ++u) {
+          const uint32_t off = (uint32_t)(ring0 + slot) * 2u * half_bytes;
+          kb[u] = k_at + off;
+          vb[u] = v_at + off;
+          codes[u] = EIGHT ? __shfl_sync(0xffffffffu, held, (have + skip + u) & 31) : 0u;
+          if (u < count) {
+            if (!mbar_wait(full_bar(ring0 + slot), round, abort_flag) && lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
+            rows_ok &= slot_mask[ring0 + slot];
+            if (++slot == a.lane_slots) { slot = 0; round ^= 1u; }
+          }
+        }
+        if (count == STEP && rows_ok == 0xffffu && pos0 >= all_from && pos0 + STEP * kGran <= all_to) {  // every query sees all of it
+          step(std::integral_constant<int, STEP>(), std::false_type(), pos0, kb, vb, 0xffffu, codes);
+        } else {
+#pragma unroll 1
+          for (int u = 0; u < count; ++u) {
+            const int here = ring0 + (slot_before + u >= a.lane_slots ? slot_before + u - a.lane_slots : slot_before + u);
+            const uint32_t kb1 = k_at + (uint32_t)here * 2u * half_bytes, vb1 = v_at + (uint32_t)here * 2u * half_bytes;
+            const uint32_t code1 = EIGHT ? __shfl_sync(0xffffffffu, held, (have + skip + u) & 31) : 0u;
+            step(std::integral_constant<int, 1>(), std::true_type(), pos0 + u * kGran, &kb1, &vb1, slot_mask[here], &code1);
+          }
+        }
         __syncwarp();
-        if (lane == 0) mbar_arrive(empty_bar(slot));
+        if (lane < count) mbar_arrive(empty_bar(ring0 + (slot_before + lane >= a.lane_slots ? slot_before + lane - a.lane_slots : slot_before + lane)));
       }
-      seq += hi - lo;
+      seq = end;
       cur = unit + hi;
 
       // ---- what becomes of the segment: the lanes' parts meet in shared memory, a column tile at a time ----------------
@@ -717,13 +855,18 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
         together();
         const int cols = min(PARTS == 3 ? 4 : 8, a.columns_used - col0 - nt * 8);
+#pragma unroll 1
         for (int c = my_lane; c < cols; c += a.lanes) {
-          auto part_of = [&](int i) {  // lane i's part of the column
-            return reinterpret_cast<const float4*>(merge + (((i * a.heads + my_head) * a.col_warps + my_cw) * 8 + c) * kPartialStride);
-          };
-          Folded f;
-          f.fold(lane < a.lanes ? part_of(lane)[32] : no_head(), a.lanes, [&](int i) { return part_of(i)[lane]; });
           const int col = col0 + nt * 8 + c, t = col / G;
+          Folded f;
+          float4 head[kConsumers], v[kConsumers];  // the lanes' parts of the column
+#pragma unroll
+          for (int i = 0; i < kConsumers; ++i) {
+            const float4* part = reinterpret_cast<const float4*>(merge + (((i * a.heads + my_head) * a.col_warps + my_cw) * 8 + c) * kPartialStride);
+            head[i] = i < a.lanes ? part[32] : no_head();
+            v[i] = i < a.lanes ? part[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+          f.fold_few(head, v);
           if (whole_unit) {
             f.write(a, ((int64_t)b * T + t) * a.num_q_heads + g * G + (col - t * G), lane);
           } else {
@@ -737,61 +880,55 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
     seq_base += s.gran * HG;
     ++b;
+    len_b = len_next;
+    start = start_next;
   }
 }
 
-// Joins the records of the rows whose unit several stretches share. ROWS rows per block, kJoinThreads / 32 / ROWS warps for each.
-template <int ROWS>
+// Joins the records of the rows whose unit several stretches share. A row has SHARE warps, which take its records in turn, BATCH at a time.
+template <int SHARE, int BATCH>
 __global__ void __launch_bounds__(kJoinThreads) dense_join_kernel(const __grid_constant__ DenseArgs a) {
-  constexpr int kWarps = kJoinThreads / 32, kShare = kWarps / ROWS;
-  __shared__ int sums[kWarps];
-  __shared__ __align__(16) float parts[kShare > 1 ? kWarps * kPartialStride : 4];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rows = a.T * a.num_q_heads, blocks_per_seq = (rows + ROWS - 1) / ROWS;
-  const int b = (int)blockIdx.x / blocks_per_seq, r = ((int)blockIdx.x - b * blocks_per_seq) * ROWS + warp / kShare;
-  // The lengths may be read before the wait: the kernel in front of this one released it behind its own wait.
-  int all = 0, prior = 0;
-  for (int i = tid; i < a.num_seqs; i += kJoinThreads) {
-    const int g = look_at(a, a.seq_len[i]).gran;
-    all += g;
-    if (i < b) prior += g;
-  }
-  int unused;
-  all = block_scan<kJoinThreads>(all, sums, unused);
-  prior = block_scan<kJoinThreads>(prior, sums, unused);
-  const Cut cut(a, all * a.head_groups);
-  const int gran = look_at(a, a.seq_len[b]).gran;
-  const int t = r / a.num_q_heads, h = r - t * a.num_q_heads, g = h / a.group;
-  const int hg = g / a.heads, hh = g - hg * a.heads, col = t * a.group + (h - g * a.group), ct = col / a.columns, cc = col - ct * a.columns;
-  const int unit = prior * a.head_groups + hg * gran;
-  const int first = cut.owner(unit), last = cut.owner(unit + gran - 1);
-  const bool mine = r < rows && last > first;
+  constexpr int kWarps = kJoinThreads / 32, kRows = kWarps / SHARE;
+  __shared__ __align__(16) float parts[SHARE > 1 ? kWarps * kPartialStride : 4];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, own = warp % SHARE;
+  const int64_t row = (int64_t)blockIdx.x * kRows + warp / SHARE;  // (sequence, token, head)
+  const int h = (int)(row % a.num_q_heads), t = (int)(row / a.num_q_heads % a.T), b = (int)(row / a.num_q_heads / a.T);
+  const int g = h / a.group, hg = g / a.heads, hh = g - hg * a.heads, col = t * a.group + (h - g * a.group), ct = col / a.columns, cc = col - ct * a.columns;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (kShare == 1) {
-    if (!mine) return;
-  } else if (!mine) {
-    return;  // the same for the whole block: it has one row
-  }
-  const int own = warp % kShare;
-  auto record = [&](int s) { return record_at(a, s * a.col_tiles + ct, s == first && cut.begin(s) < unit ? 1 : 0, hh, cc); };
+  int2 unit = make_int2(0, 0);
+  if (b < a.num_seqs) unit = __ldcg(&a.units[(int64_t)b * a.head_groups + hg]);
+  const int first = unit.x >> 1, last = unit.y;
+  const bool joined = last > first;
+  if (SHARE == 1 ? !joined : !__syncthreads_or(joined)) return;
   Folded f;
-  const int count = (last - first - own + kShare) / kShare;  // stretches first + own, + kShare, ..
-  for (int k = 0; k < count; k += 32) {
-    const int s0 = first + own + k * kShare;
-    f.fold(k + lane < count ? __ldcg(record(s0 + lane * kShare) + 32) : no_head(), min(32, count - k),
-           [&](int i) { return __ldcg(record(s0 + i * kShare) + lane); });
+  if (joined) {
+    auto record = [&](int s) { return record_at(a, s * a.col_tiles + ct, s == first ? unit.x & 1 : 0, hh, cc); };
+    const int count = (last - first - own + SHARE) / SHARE;  // stretches first + own, + SHARE, ..
+    for (int k = 0; k < count; k += BATCH) {
+      const int s0 = first + own + k * SHARE, n = min(BATCH, count - k);
+      float4 v[BATCH];
+      const float4 head = lane < n ? __ldcg(record(s0 + lane * SHARE) + 32) : no_head();
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) v[i] = i < n ? __ldcg(record(s0 + i * SHARE) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+      f.fold_batch(head, v);
+    }
   }
-  if (kShare > 1) {
+  if (SHARE > 1) {
     float4* p = reinterpret_cast<float4*>(parts + warp * kPartialStride);
     p[lane] = f.acc;
     if (lane == 0) p[32] = make_float4(f.mx, f.l, f.m, 0.f);
     __syncthreads();
-    if (own != 0) return;
+    if (own != 0 || !joined) return;
     f = Folded();
-    f.fold(lane < kShare ? reinterpret_cast<const float4*>(parts + (warp + lane) * kPartialStride)[32] : no_head(), kShare,
-           [&](int i) { return reinterpret_cast<const float4*>(parts + (warp + i) * kPartialStride)[lane]; });
+    float4 head[SHARE], v[SHARE];
+#pragma unroll
+    for (int i = 0; i < SHARE; ++i) {
+      head[i] = reinterpret_cast<const float4*>(parts + (warp + i) * kPartialStride)[32];
+      v[i] = reinterpret_cast<const float4*>(parts + (warp + i) * kPartialStride)[lane];
+    }
+    f.fold_few(head, v);
   }
-  f.write(a, ((int64_t)b * a.T + t) * a.num_q_heads + h, lane);
+  f.write(a, row, lane);
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------------
@@ -827,33 +964,69 @@ bool make_map(CUtensorMap* map, const void* ptr, bool eight, const clsa_params& 
 
 }  // namespace
 
-DensePlan make_dense_plan(const clsa_params& p, bool eight, const DeviceInfo& dev) {
+// A launch that cuts the list anywhere pays a second kernel for the joining; one that gives each block whole units does not, but waits
+// for its longest block. Estimated from the longest sequence: bytes per block at an SM's share of the HBM bandwidth, 3 us for the joining, and
+// 0.7 for lengths below the longest, which only the first kind profits from.
+DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const DeviceInfo& dev) {
   DensePlan d = {};
   const int cols = p.q_per_seq * (p.num_q_heads / p.num_kv_heads);
   d.fold = !eight && cols <= 4;
   d.tiles = cols <= 8 ? 1 : 2;
+  d.step = d.tiles == 1 && !eight ? 1 : 2;
   d.col_warps = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
   d.columns = d.fold ? 4 : d.tiles * d.col_warps * 8;
   d.col_tiles = (cols + d.columns - 1) / d.columns;
-  d.heads = kConsumers / d.col_warps;
-  while (p.num_kv_heads % d.heads != 0) d.heads /= 2;
+  d.spans = dev.sm_count / d.col_tiles;
+  const int head_bytes = kGran * (eight ? 256 : 512);  // of a granule
+  const int room = dev.max_smem_optin - kMergeBytes - kCtrlBytes - 1024;
+  int most = kConsumers / d.col_warps;
+  while (p.num_kv_heads % most != 0 || room / (most * head_bytes) < 3) most /= 2;
+  d.heads = most;
+  const int64_t reach = window > 0 && window < p.max_seq_len - p.q_per_seq ? window + p.q_per_seq + kGran : p.max_seq_len;
+  const double granules = (double)((reach + kGran - 1) / kGran), us_per_head = head_bytes / 44e3;
+  double best = 0.7 * granules * us_per_head * p.num_seqs * p.num_kv_heads / d.spans + 3.0;
+  for (int h = most; h >= 1; h /= 2) {
+    const int64_t units = (int64_t)p.num_seqs * (p.num_kv_heads / h);
+    const double whole = (double)((units + d.spans - 1) / d.spans) * granules * h * us_per_head;
+    if (whole < best) { best = whole; d.heads = h; d.whole_units = 1; }
+  }
   d.lanes = kConsumers / (d.col_warps * d.heads);
   d.head_groups = p.num_kv_heads / d.heads;
-  d.slot_bytes = d.heads * kGran * (eight ? 256 : 512);
-  const int room = dev.max_smem_optin - kMergeBytes - kCtrlBytes - 1024;
-  d.slots = room / d.slot_bytes;
-  if (d.slots > kMaxSlots) d.slots = kMaxSlots;
+  d.slot_bytes = d.heads * head_bytes;
+  d.lane_slots = room / d.slot_bytes;
+  if (d.lane_slots > kMaxSlots) d.lane_slots = kMaxSlots;
+  d.lane_slots /= d.lanes;  // (three at least)
+  d.slots = d.lane_slots * d.lanes;
   d.smem_bytes = (size_t)d.slots * d.slot_bytes + kMergeBytes + kCtrlBytes + 1024;
-  d.spans = dev.sm_count / d.col_tiles;
+  auto align = [](size_t x) { return (x + 255) / 256 * 256; };
+  d.unit_bytes = align((size_t)p.num_seqs * p.num_kv_heads * sizeof(int2));
+  // (of the heads that a block has at most: the size does not go by the window)
+  d.scratch_bytes = d.unit_bytes + align((size_t)d.spans * d.col_tiles * 2 * most * d.columns * kPartialStride * sizeof(float));
   return d;
 }
 
-size_t dense_partial_bytes(const DensePlan& d) {
-  return (size_t)d.spans * d.col_tiles * 2 * d.heads * d.columns * kPartialStride * sizeof(float);
+template <bool EIGHT, int NT, int PARTS, int STEP>
+cudaError_t launch_kernel(const cudaLaunchConfig_t& cfg, const CUtensorMap& map_k, const CUtensorMap& map_v, const DenseArgs& a) {
+  auto kernel = dense_attn_kernel<EIGHT, NT, PARTS, STEP>;
+  // The kernel's warpgroups redistribute the registers that it was launched with: it may not have been built with fewer.
+  static std::atomic<uint64_t> known{0};  // devices on which it has been looked at, and allowed its shared memory
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  if (dev >= 64 || !(known.load(std::memory_order_relaxed) >> dev & 1)) {
+    cudaFuncAttributes f;
+    int room = 0;
+    if ((err = cudaFuncGetAttributes(&f, kernel)) != cudaSuccess) return err;
+    if (f.numRegs * kThreads < kConsumers * 32 * kConsumerRegs + (kThreads - kConsumers * 32) * kProducerRegs) return cudaErrorInvalidConfiguration;
+    if ((err = cudaDeviceGetAttribute(&room, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev)) != cudaSuccess) return err;
+    if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room)) != cudaSuccess) return err;
+    if (dev < 64) known.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, map_k, map_v, a);
 }
 
 cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int window, const DensePlan& plan, const void* q, void* out,
-                              float* lse, uint32_t* status, float* part, cudaStream_t stream) {
+                              float* lse, uint32_t* status, unsigned char* scratch, cudaStream_t stream) {
   CUtensorMap map_k, map_v;
   const bool eight = c != nullptr;
   const int64_t token = eight ? c->kv_token_stride : p.kv_token_stride, head = eight ? c->kv_head_stride : p.kv_head_stride;
@@ -865,7 +1038,8 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
   a.status = status;
-  a.part = part;
+  a.units = reinterpret_cast<int2*>(scratch);
+  a.part = reinterpret_cast<float*>(scratch + plan.unit_bytes);
   a.seq_start = p.seq_start;
   a.seq_len = p.seq_len;
   a.block_table = p.block_table;
@@ -894,16 +1068,11 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   a.col_warps = plan.col_warps;
   a.head_groups = plan.head_groups;
   a.slots = plan.slots;
+  a.lane_slots = plan.lane_slots;
   a.spans = plan.spans;
-  a.min_granules = plan.lanes > 2 ? plan.lanes : 2;
+  a.min_granules = plan.lanes * plan.step;
+  a.whole_units = plan.whole_units;
   a.scale_log2 = p.sm_scale * kLog2e;
-  void (*kernel)(const CUtensorMap, const CUtensorMap, const DenseArgs) =
-      eight ? (plan.tiles == 1 ? dense_attn_kernel<true, 1, 1> : dense_attn_kernel<true, 2, 1>)
-            : (plan.fold ? dense_attn_kernel<false, 1, 3>
-               : plan.tiles == 1 ? dense_attn_kernel<false, 1, 2>
-               : plan.col_warps <= 2 ? dense_attn_kernel<false, 2, 2> : dense_attn_kernel<false, 2, 1>);
-  cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem_bytes);
-  if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(plan.spans * plan.col_tiles), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
@@ -914,14 +1083,19 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  err = cudaLaunchKernelEx(&cfg, kernel, map_k, map_v, a);
-  if (err != cudaSuccess) return err;
-  const int rows = a.T * a.num_q_heads;
-  const bool few = (int64_t)rows * a.num_seqs <= 1024;
-  cfg.gridDim = dim3((unsigned)(a.num_seqs * (few ? rows : (rows + 7) / 8)), 1, 1);
+  const cudaError_t err = eight ? (plan.tiles == 1 ? launch_kernel<true, 1, 1, 2>(cfg, map_k, map_v, a) : launch_kernel<true, 2, 1, 2>(cfg, map_k, map_v, a))
+                          : plan.fold           ? launch_kernel<false, 1, 3, 1>(cfg, map_k, map_v, a)
+                          : plan.tiles == 1     ? launch_kernel<false, 1, 2, 1>(cfg, map_k, map_v, a)
+                          : plan.col_warps <= 2 ? launch_kernel<false, 2, 2, 2>(cfg, map_k, map_v, a)
+                                                : launch_kernel<false, 2, 1, 2>(cfg, map_k, map_v, a);
+  if (err != cudaSuccess || plan.whole_units) return err;
+  const int64_t rows = (int64_t)a.num_seqs * a.T * a.num_q_heads;
+  // Few rows have a block and all of their records in flight at once (148 stretches are 19 per warp of 8), which takes an SM's registers.
+  const int share = rows <= 1024 ? 8 : 2;
+  cfg.gridDim = dim3((unsigned)((rows * share + 7) / 8), 1, 1);
   cfg.blockDim = dim3(kJoinThreads, 1, 1);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, few ? dense_join_kernel<1> : dense_join_kernel<8>, a);
+  return cudaLaunchKernelEx(&cfg, rows <= 296 ? dense_join_kernel<8, 20> : share == 8 ? dense_join_kernel<8, 8> : dense_join_kernel<2, 8>, a);
 }
 
 }  // namespace clsa

@@ -12,15 +12,17 @@ struct DensePlan {
   int col_tiles;               // blocks that share one stretch of the cache, each with its own query columns
   int heads, lanes;            // KV heads of a block; warps that take 16-token granules of one head (and column share) in turn
   int head_groups;             // Hkv / heads
-  int slots, slot_bytes;       // the ring: one granule's K and V rows of the block's heads in each slot
+  int slots, lane_slots, slot_bytes;  // the rings, one per lane: a granule's K and V rows of the block's heads in each slot
+  int step;                    // granules that a warp works on together
   int spans;                   // stretches that the list of granules is cut into, at most
+  int whole_units;             // 1: a stretch has the units that begin in it, whole (nothing to join)
   size_t smem_bytes;
+  size_t unit_bytes, scratch_bytes;  // scratch: where each unit lies, then records of partial results (the same for every window)
 };
-DensePlan make_dense_plan(const clsa_params& p, bool eight, const DeviceInfo& dev);
-size_t dense_partial_bytes(const DensePlan& plan);
-// c: an 8-bit cache, or nullptr (p's own caches). part: dense_partial_bytes of scratch.
+DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const DeviceInfo& dev);
+// c: an 8-bit cache, or nullptr (p's own caches). scratch: 256-byte aligned.
 cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int window, const DensePlan& plan, const void* q, void* out,
-                              float* lse, uint32_t* status, float* part, cudaStream_t stream);
+                              float* lse, uint32_t* status, unsigned char* scratch, cudaStream_t stream);
 
 cudaError_t launch_norm_rope_axes(const clsa_norm_rope_spec& spec, const clsa_rope_axes& axes, int num_tokens, const int32_t* positions,
                                   int64_t axis_stride, const clsa_heads* q, const clsa_heads* q_out, const clsa_heads* k,

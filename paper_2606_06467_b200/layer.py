@@ -1,6 +1,6 @@
 """Binding of the calls around a layer's cache (`include/clsa_layer.h`): the same names and argument orders, tensors in place of
 pointers. Checks of dtypes, shapes, strides, sizes and devices that C cannot make happen here (an address in place of a tensor is
-taken as it is); everything else is marshalling.
+taken as it is); everything else is marshalling. As in cache8.py, the usual call goes through the native module `_marshal`.
 """
 from __future__ import annotations
 
@@ -10,6 +10,9 @@ from . import _P, _check, _i64, _lib, _ptr, _sz, _vp, cache8, clsa_params
 from .cache8 import _C, _D, _N, _dense, _describes, _device, _device_of, _fits, _heads, _stream8, _want, _workspace
 
 CLSA_MAX_AXES = 4
+
+_torch = None  # the torch module, from the first call on
+_marshal = cache8._marshal  # the native module, or None
 
 EXPORTS_LAYER = ("clsa_dense_workspace_bytes", "clsa_dense_attn", "clsa_dense_attn8", "clsa_add_norm", "clsa_norm_rope_axes")
 
@@ -31,6 +34,8 @@ class clsa_add_norm_spec(ctypes.Structure):
 class clsa_rope_axes(ctypes.Structure):
     """Mirror of `clsa_rope_axes` in include/clsa_layer.h."""
 
+    _pairs = None  # pairs that it was made for
+
     _fields_ = [("num_axes", ctypes.c_int32), ("axis_of_pair", ctypes.c_uint8 * 128)]
 
 
@@ -44,8 +49,14 @@ for _name in EXPORTS_LAYER:
     getattr(_lib, _name).restype = ctypes.c_int
 
 
-def _torch():
-    return cache8._torch or cache8._load_torch()
+def _load_torch():
+    torch = cache8._torch or cache8._load_torch()
+    if _marshal is not None:
+        where = [ctypes.cast(getattr(_lib, n), _vp).value for n in ("clsa_dense_attn", "clsa_dense_attn8", "clsa_add_norm", "clsa_norm_rope_axes")]
+        _marshal.setup_layer(*where, torch.float8_e4m3fn, torch.float8_e8m0fnu, clsa_add_norm_spec, clsa_rope_axes)
+    global _torch
+    _torch = torch
+    return torch
 
 
 def clsa_dense_workspace_bytes(p: clsa_params) -> int:
@@ -67,7 +78,7 @@ def _holds(p, device):
 
 
 def _dense_call(name, call, p, window, q, out, lse, workspace, workspace_bytes, stream, made):
-    torch = _torch()
+    torch = _torch
     dev, bf16, heads = _device(torch), torch.bfloat16, p.num_seqs * p.q_per_seq * p.num_q_heads
     _describes(p, dev)
     ws, nbytes = _workspace(workspace, workspace_bytes, made, dev)
@@ -80,14 +91,21 @@ def _dense_call(name, call, p, window, q, out, lse, workspace, workspace_bytes, 
 def clsa_dense_attn(p, window, q, out, lse, workspace, workspace_bytes=None, stream=None) -> None:
     """Attention of the T newest tokens of every sequence over all of its rows of p's bf16 caches (window 0) or the last `window` of each
     token. q, out [B, T, Hq, D] bf16, lse [B, T, Hq] fp32 or None."""
-    _holds(p, _device(_torch()))
+    torch = _torch or _load_torch()
+    status = _marshal.dense(p, window, q, out, lse, workspace, workspace_bytes, stream) if _marshal else None
+    if status is not None:
+        return _check(status, "clsa_dense_attn") if status else None
+    _holds(p, _device(torch))
     _dense_call("clsa_dense_attn", lambda *a: _lib.clsa_dense_attn(ctypes.byref(p), *a), p, window, q, out, lse, workspace, workspace_bytes,
                 stream, ())
 
 
 def clsa_dense_attn8(p, c, window, q, out, lse, workspace, workspace_bytes=None, stream=None) -> None:
     """clsa_dense_attn over an 8-bit K and V cache."""
-    _torch()
+    _torch or _load_torch()
+    status = _marshal.dense8(p, c, window, q, out, lse, workspace, workspace_bytes, stream) if _marshal else None
+    if status is not None:
+        return _check(status, "clsa_dense_attn8") if status else None
     _fits(p, c, True, False)
     _dense_call("clsa_dense_attn8", lambda *a: _lib.clsa_dense_attn8(ctypes.byref(p), ctypes.byref(c), *a), p, window, q, out, lse, workspace,
                 workspace_bytes, stream, (c,))
@@ -131,7 +149,10 @@ def _matrix(t, what, dtypes, device, rows, length):
 def clsa_add_norm(spec, x, residual, sum_out, y_out, codes_out=None, scales_out=None, stream=None) -> None:
     """s = x + residual and its RMS norm: x, residual, sum_out, y_out [.., dim] bf16, codes_out [.., dim] (float8_e4m3fn or uint8),
     scales_out [.., dim / scale_group] (float8_e8m0fnu or uint8). residual, sum_out, and y_out or both of the last may be None."""
-    torch = _torch()
+    torch = _torch or _load_torch()
+    status = _marshal.add_norm(spec, x, residual, sum_out, y_out, codes_out, scales_out, stream) if _marshal else None
+    if status is not None:
+        return _check(status, "clsa_add_norm") if status else None
     dev, bf16 = _device(torch), (torch.bfloat16,)
     if spec._device not in (None, dev):
         raise ValueError("the tensors of clsa_add_norm_spec are not on the current CUDA device")
@@ -162,7 +183,10 @@ def make_rope_axes(axis_of_pair, num_axes=None) -> clsa_rope_axes:
 
 def clsa_norm_rope_axes(spec, axes, positions, q, q_out, k=None, k_out=None, stream=None) -> None:
     """clsa_norm_rope with positions [num_axes, tokens] (int32, dense rows; or [tokens], one position for every axis)."""
-    torch = _torch()
+    torch = _torch or _load_torch()
+    status = _marshal.norm_rope_axes(spec, axes, positions, q, q_out, k, k_out, stream) if _marshal else None
+    if status is not None:
+        return _check(status, "clsa_norm_rope_axes") if status else None
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
         raise ValueError("q with q_out, k with k_out, or both are wanted")
     dev, bf16, dim = _device(torch), torch.bfloat16, spec.head_dim
@@ -173,7 +197,7 @@ def clsa_norm_rope_axes(spec, axes, positions, q, q_out, k=None, k_out=None, str
     if k is not None:
         c, n, h = _heads(k, "k", dev, bf16, n, None, dim)
         d, _, _ = _heads(k_out, "k_out", dev, bf16, n, h, dim)
-    if getattr(axes, "_pairs", spec.rot_dim // 2) * 2 != spec.rot_dim:
+    if axes._pairs is not None and axes._pairs * 2 != spec.rot_dim:
         raise ValueError(f"axes: {spec.rot_dim // 2} pairs are wanted, got {axes._pairs}")
     if positions.dtype != torch.int32 or positions.get_device() != dev or positions.shape[-1:] != (n,) or positions.dim() > 2 or (
             positions.stride(-1) != 1 and n > 1) or (positions.dim() == 2 and (positions.shape[0] != axes.num_axes or 0 < positions.stride(0) < n)):
