@@ -23,7 +23,7 @@ clsa_status check_dense(const clsa_params* p, int32_t window) {
   if (p->head_dim != 128 || p->q_per_seq > kDenseMaxT || p->num_q_heads / p->num_kv_heads > 16) return CLSA_ERR_UNSUPPORTED;
   // positions, granules of all units and output rows are numbered with 32 bits
   if (p->max_seq_len > 0x7fff0000) return CLSA_ERR_UNSUPPORTED;
-  if ((double)p->num_seqs * p->num_kv_heads * ((double)p->max_seq_len / 16 + 2) >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
+  if ((double)p->num_seqs * p->num_kv_heads * ((double)p->max_seq_len / 16 + 2) >= 1073741824.0) return CLSA_ERR_UNSUPPORTED;
   if ((double)p->num_seqs * p->q_per_seq * p->num_q_heads >= 2147483648.0) return CLSA_ERR_UNSUPPORTED;
   return CLSA_OK;
 }

@@ -7,8 +7,8 @@
 //
 // Work. A granule is 16 consecutive positions (starting on a multiple of 16, so that it lies in one page and one scale block) of
 // `heads` KV heads. The granules of all (sequence, head group) units form one list, sequence after sequence; its length is known on the
-// device only, where every block adds up the lengths and takes an even stretch of the list, whatever the sequences' lengths are. One
-// producer warp fetches granules into a ring by tiled bulk copies (one for K, one for V: 16 rows of every head, 128-byte swizzle); eight
+// device only, where every block adds up the lengths and takes an even stretch of the list, whatever the sequences' lengths are. Four
+// warps fetch granules into rings by tiled bulk copies (one for K, one for V: 16 rows of every head, 128-byte swizzle); eight
 // warps consume them, each with one head's rows: `lanes` warps take a head's granules in turn, `col_warps` share a head's query columns.
 // Products are formed transposed, tokens along M of warp-level instructions:
 //   S^T[16 tokens x 8 columns] = K Q^T,   O^T[128 x 8 columns] += V^T P^T
@@ -40,10 +40,12 @@ namespace {
 
 constexpr int kGran = 16;                 // positions per granule
 constexpr int kConsumers = 8;             // consuming warps
-constexpr int kThreads = (kConsumers + 4) * 32;  // .. and a warpgroup of which one warp fetches
+constexpr int kProducers = 4;             // .. and fetching ones
+constexpr int kThreads = (kConsumers + kProducers) * 32;
 constexpr int kConsumerRegs = 224, kProducerRegs = 56;  // 8 x 32 x 224 + 4 x 32 x 56 = 64512 = kThreads x 168, what a launch gets
 constexpr int kJoinThreads = 256;
-constexpr int kMaxSlots = 32;                     // a lane of the producer for each
+constexpr int kPerLane = 4;                       // sequences to a lane where every warp adds up the lengths by itself
+constexpr int kMaxSlots = 32;
 constexpr int kMergeBytes = kConsumers * 8 * kPartialStride * 4;  // a column tile of every consuming warp
 constexpr int kCtrlBytes = 1024;
 constexpr uint32_t kSpinLimit = 1u << 22;  // polls of a barrier: seconds
@@ -67,7 +69,9 @@ struct DenseArgs {
   int scale_shift, block_shift, max_blocks, pages;
   int num_seqs, T, num_q_heads, group, columns_used;  // columns_used: T * group
   int window, causal, max_seq_len;
-  int columns, col_tiles, heads, lanes, col_warps, head_groups, slots, lane_slots, spans, min_granules, whole_units;
+  int columns, col_tiles, heads, lanes, col_warps, head_groups, slots, lane_slots, spans, min_granules;
+  int whole_units;  // 1: a stretch has the units that begin in it, whole
+  int cluster;      // > 0: each cluster of so many blocks has one unit, cut evenly; 0: stretches of the list
   float scale_log2;
 };
 
@@ -119,6 +123,18 @@ __device__ __forceinline__ void ldmatrix_b8_x2_trans(uint32_t (&r)[4], uint32_t 
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+constexpr int kMaxCluster = 8;
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float4 peer_float4(uint32_t at, int block) {  // from the shared memory of a block of the cluster
+  uint32_t there;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(block));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
+  return v;
+}
 
 // ---- which positions and granules a sequence has ----------------------------------------------------------------------
 struct Seq {
@@ -185,25 +201,6 @@ __device__ __forceinline__ int v_token(int i) { return k_token(2 * (i >> 2) + (i
 struct Folded {
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float mx = kNone, l = 0.f, m = kNone;
-  // What the running sums (returned) and the records' (into `share`, the lane's record's) are to be multiplied by; updates the references.
-  __device__ __forceinline__ float refer(float4 head, float& share) {
-    float xn = fmaxf(mx, head.x);
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) xn = fmaxf(xn, __shfl_xor_sync(0xffffffffu, xn, d));
-    const float mnew = (head.x - xn) + head.z, mold = (mx - xn) + m;  // references to x - xn + ev
-    float mn = fmaxf(mold, mnew);
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
-    share = fast_exp2(mnew - mn);
-    float sum = fast_exp2(head.x - xn) * head.y;
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    l = l * fast_exp2(mx - xn) + sum;
-    const float old = fast_exp2(mold - mn);
-    mx = xn;
-    m = mn;
-    return old;
-  }
   __device__ __forceinline__ void scale(float f) { acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f; }
   __device__ __forceinline__ void add(float f, float4 v) {
     acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
@@ -228,22 +225,14 @@ struct Folded {
     mx = xn;
     m = mn;
   }
-  // N records, lane i having the i-th one's head (no_head and zeros where there is none).
-  template <int N>
-  __device__ __forceinline__ void fold_batch(float4 head, const float4 (&v)[N]) {
-    float share;
-    scale(refer(head, share));
-#pragma unroll
-    for (int i = 0; i < N; ++i) add(__shfl_sync(0xffffffffu, share, i), v[i]);
-  }
-  __device__ __forceinline__ void write(const DenseArgs& a, int64_t item, int lane) const {
+  __device__ __forceinline__ void write(const DenseArgs& a, int64_t item, int quad) const {
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (l != 0.f) {  // 2^m in two halves: it may not be a float
       const float inv = 1.f / l, half = fast_exp2(0.5f * m);
       v = make_float4(acc.x * inv * half * half, acc.y * inv * half * half, acc.z * inv * half * half, acc.w * inv * half * half);
     }
-    *reinterpret_cast<uint2*>(a.out + item * 128 + lane * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-    if (a.lse != nullptr && lane == 0) a.lse[item] = l != 0.f ? (mx + log2f(l)) * kLn2 : -INFINITY;
+    *reinterpret_cast<uint2*>(a.out + item * 128 + quad * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    if (a.lse != nullptr && quad == 0) a.lse[item] = l != 0.f ? (mx + log2f(l)) * kLn2 : -INFINITY;
   }
 };
 __device__ __forceinline__ float4 no_head() { return make_float4(kNone, 0.f, kNone, 0.f); }
@@ -286,70 +275,135 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
   }
+  __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind this grid's own wait, as in every kernel of the library
 
-  // this block's stretch of the list
+  // This block's stretch of the list: the first sequence that it reaches into (its number, the granules before it, length and first row).
   const int HG = a.head_groups;
-  const int span = (int)blockIdx.x / a.col_tiles, ct = (int)blockIdx.x - span * a.col_tiles;
-  const bool one_pass = a.num_seqs <= kThreads, paged = a.block_table != nullptr;
-  int total = 0, len = 0, gran = 0, before = 0;
-  int64_t begin = 0;
-  auto read = [&](int i) {
-    gran = 0;
-    if (i >= a.num_seqs) return;
-    len = a.seq_len[i];
-    if (!paged) begin = a.seq_start[i];
-    gran = look_at(a, len).gran;
-  };
-  for (int b0 = 0; b0 < a.num_seqs; b0 += kThreads) {
-    read(b0 + tid);
-    total += block_scan<kThreads>(gran, sums, before);
+  const int rank = a.cluster > 0 ? (int)blockIdx.x % a.cluster : 0;
+  const int span = (int)blockIdx.x / a.col_tiles;  // (of the list)
+  const int ct = a.cluster > 0 ? (int)blockIdx.x / a.cluster % a.col_tiles : (int)blockIdx.x % a.col_tiles;
+  const bool paged = a.block_table != nullptr;
+  int total = 0, b_first, base_first, len_first;
+  int64_t start_first;
+  int span_lo, span_hi, hg_first = 0;
+  if (a.cluster > 0) {  // no list: the unit's granules count from 0, those of its sequence's head groups before it below
+    const int unit = (int)blockIdx.x / (a.cluster * a.col_tiles);
+    b_first = unit / HG;
+    hg_first = unit - b_first * HG;
+    len_first = a.seq_len[b_first];
+    start_first = paged ? 0 : a.seq_start[b_first];
+  } else if (a.num_seqs <= 32 * kPerLane) {  // every warp by itself, kPerLane sequences to a lane
+    int len[kPerLane], gran[kPerLane], mine = 0;
+    int64_t begin[kPerLane];
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+      const int i = lane * kPerLane + k;
+      len[k] = i < a.num_seqs ? a.seq_len[i] : 0;
+      begin[k] = i < a.num_seqs && !paged ? a.seq_start[i] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+      gran[k] = lane * kPerLane + k < a.num_seqs ? look_at(a, len[k]).gran : 0;
+      mine += gran[k];
+    }
+    int incl = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += o;
+    }
+    total = __shfl_sync(0xffffffffu, incl, 31);
+    const int from = Cut(a, total * HG).begin(span);
+    int lo = (incl - mine) * HG;
+    b_first = lane * kPerLane;
+    base_first = lo;
+    len_first = len[0];
+    start_first = begin[0];
+#pragma unroll
+    for (int k = 1; k < kPerLane; ++k) {
+      lo += gran[k - 1] * HG;
+      if (gran[k] > 0 && lo <= from) { b_first = lane * kPerLane + k; base_first = lo; len_first = len[k]; start_first = begin[k]; }
+    }
+    const uint32_t here = __ballot_sync(0xffffffffu, (incl - mine) * HG <= from && from < incl * HG);
+    const int who = here != 0u ? __ffs(here) - 1 : 0;  // (none: a stretch beyond the last one)
+    b_first = __shfl_sync(0xffffffffu, b_first, who);
+    base_first = __shfl_sync(0xffffffffu, base_first, who);
+    len_first = __shfl_sync(0xffffffffu, len_first, who);
+    start_first = __shfl_sync(0xffffffffu, start_first, who);
+  } else {
+    int len = 0, gran = 0, before = 0;
+    int64_t begin = 0;
+    auto read = [&](int i) {
+      gran = 0;
+      if (i >= a.num_seqs) return;
+      len = a.seq_len[i];
+      if (!paged) begin = a.seq_start[i];
+      gran = look_at(a, len).gran;
+    };
+    total = 0;
+    for (int b0 = 0; b0 < a.num_seqs; b0 += kThreads) {
+      read(b0 + tid);
+      total += block_scan<kThreads>(gran, sums, before);
+    }
+    const int from = Cut(a, total * HG).begin(span);
+    for (int b0 = 0, run = 0; b0 < a.num_seqs; b0 += kThreads) {
+      read(b0 + tid);
+      const int sum = block_scan<kThreads>(gran, sums, before);
+      const int lo = (run + before) * HG;
+      if (lo <= from && from < lo + gran * HG) {
+        found[0] = b0 + tid;
+        found[1] = lo;
+        found[2] = len;
+        *found_start = begin;
+      }
+      run += sum;
+      if (run * HG > from) break;
+    }
+    __syncthreads();
+    b_first = found[0];
+    base_first = found[1];
+    len_first = found[2];
+    start_first = *found_start;
   }
   const Cut cut(a, total * HG);
-  if (span >= cut.spans) return;
-  int span_lo = cut.begin(span), span_hi = cut.begin(span + 1);
-  for (int b0 = 0, run = 0; b0 < a.num_seqs; b0 += kThreads) {
-    if (!one_pass) read(b0 + tid);
-    const int sum = one_pass ? total : block_scan<kThreads>(gran, sums, before);
-    const int lo = (run + before) * HG;
-    if (lo <= span_lo && span_lo < lo + gran * HG) {
-      found[0] = b0 + tid;
-      found[1] = lo;
-      found[2] = len;
-      *found_start = begin;
-    }
-    run += sum;
-    if (run * HG > span_lo) break;
+  if (a.cluster > 0) {
+    const int g = look_at(a, len_first).gran;
+    base_first = -hg_first * g;
+    span_lo = g * rank / a.cluster;
+    span_hi = g * (rank + 1) / a.cluster;
+  } else {
+    if (span >= cut.spans) return;
+    span_lo = cut.begin(span);
+    span_hi = cut.begin(span + 1);
   }
-  __syncthreads();
-  const int b_first = found[0], base_first = found[1], len_first = found[2];
-  const int64_t start_first = *found_start;
   if (a.whole_units) {  // the units that begin in the stretch, whole
     const int g = look_at(a, len_first).gran;
     span_lo = base_first + (span_lo - base_first + g - 1) / g * g;  // (within the sequence, or the next one's beginning)
   }
 
   if (warp >= kConsumers) {
-    // ---------------- producer: lane s of the warp has slot s ----------------
+    // ---------------- producers: lane i of warp w has slot w + 4 i ----------------
+    // (Copies are issued lane by lane: with all slots' in one warp 64 sequences of 4096 tokens of one 8-bit KV head took 34 us.)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
-    if (warp > kConsumers) return;
+    const int slot = warp - kConsumers + kProducers * lane;
     int b = b_first, seq_base = base_first;
     Seq s = look_at(a, len_first);
     int64_t start = start_first;
     // The ring is one of lane_slots slots for each consuming lane, so that a slot's granules are waited for by the same warps in every round
     // (a warp that waited for a round while the one before had not landed yet would take the parity of the one before that). Steps of STEP
     // granules go to the lanes in turn: slot s holds granules number k = s % lane_slots, + lane_slots, .. of its lane.
-    const int ring = lane / a.lane_slots;
-    int k = lane - ring * a.lane_slots;
+    const int ring = slot / a.lane_slots;
+    int k = slot - ring * a.lane_slots;
     auto list_at = [&]() { return span_lo + (k / STEP * a.lanes + ring) * STEP + k % STEP; };
     int at = list_at();  // the place of this lane's next granule in the list
     // its place: position, head group, page table entry
     bool valid;
     int pos, hg, entry;
     auto place = [&]() {
-      valid = lane < a.slots && at < span_hi;
-      if (!valid && !(a.whole_units && lane < a.slots)) return;
+      valid = slot < a.slots && at < span_hi;
+      if (!valid && !(a.whole_units && slot < a.slots)) return;
       while (b < a.num_seqs && at >= seq_base + s.gran * HG) {
         seq_base += s.gran * HG;
         if (++b == a.num_seqs) break;
@@ -361,7 +415,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       const int unit = seq_base + hg * s.gran, i = at - unit;
       if (a.whole_units) {
         valid = unit < span_hi;
-      } else if (i == 0 && ct == 0) {
+      } else if (a.cluster == 0 && i == 0 && ct == 0) {
         a.units[(int64_t)b * HG + hg] = make_int2(2 * span + (unit == span_lo ? 0 : 1), cut.owner(unit + s.gran - 1));
       }
       pos = s.base + kGran * i;
@@ -397,15 +451,11 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
         z = hg * a.heads;
       }
-      const bool mine = valid;
-      k += a.lane_slots;
-      at = list_at();
-      place();  // the next one's, whose lookups are under way while this one waits for its slot
-      bool pending = mine;
-      for (uint32_t it = 0; alive && __any_sync(0xffffffffu, pending); ++it) {
-        if (pending && mbar_test(empty_bar(lane), (round & 1u) ^ 1u)) {
-          slot_mask[lane] = mask;
-          const uint32_t bar = full_bar(lane), dst = base + (uint32_t)lane * 2u * half_bytes;
+      bool pending = valid;
+      auto issue = [&]() {
+        if (pending && mbar_test(empty_bar(slot), (round & 1u) ^ 1u)) {
+          slot_mask[slot] = mask;
+          const uint32_t bar = full_bar(slot), dst = base + (uint32_t)slot * 2u * half_bytes;
           mbar_expect_tx(bar, 2u * half_bytes);
           if (EIGHT) {
             tma_load_3d(dst, &map_k, 0, row32, z, bar);
@@ -417,6 +467,13 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           pending = false;
           ++rounds;
         }
+      };
+      issue();
+      k += a.lane_slots;
+      at = list_at();
+      place();  // the next one's, whose lookups are under way while this one waits for its slot
+      for (uint32_t it = 0; alive && __any_sync(0xffffffffu, pending); ++it) {
+        issue();
         if (it >= kSpinLimit) *abort_flag = 1u;
         if ((it & 63u) == 63u) {
           __nanosleep(64);
@@ -426,7 +483,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       if (!alive) {  // given up: the copies under way still land in this block's memory
         if (lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
         if (rounds > 0)
-          for (uint32_t it = 0; it < kSpinLimit && !mbar_test(full_bar(lane), (uint32_t)(rounds - 1) & 1u); ++it) __nanosleep(64);
+          for (uint32_t it = 0; it < kSpinLimit && !mbar_test(full_bar(slot), (uint32_t)(rounds - 1) & 1u); ++it) __nanosleep(64);
         return;
       }
       ++round;
@@ -471,11 +528,12 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   int slot = 0;                          // of this lane's ring: its next granule's, and the parity of that round
   uint32_t round = 0;
 
-  while (cur < span_hi && b < a.num_seqs) {
+  bool more = a.cluster > 0 || cur < span_hi;  // (a cluster's block without granules takes part in the joining)
+  while (more && b < a.num_seqs) {
     const Seq s = look_at(a, len_b);
     const int len_next = b + 1 < a.num_seqs ? a.seq_len[b + 1] : 0;
     const int64_t start_next = EIGHT && !paged && b + 1 < a.num_seqs ? a.seq_start[b + 1] : 0;
-    for (int hg = (cur - seq_base) / s.gran; hg < HG && cur < span_hi; ++hg) {
+    for (int hg = (cur - seq_base) / s.gran; hg < HG && more; ++hg) {
       const int unit = seq_base + hg * s.gran;
       const int lo = cur - unit, hi = a.whole_units ? s.gran : min(span_hi - unit, s.gran);
       const int g = hg * a.heads + my_head;  // KV head
@@ -821,6 +879,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       }
       seq = end;
       cur = unit + hi;
+      more = cur < span_hi;
 
       // ---- what becomes of the segment: the lanes' parts meet in shared memory, a column tile at a time ----------------
 #pragma unroll
@@ -859,15 +918,30 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         for (int c = my_lane; c < cols; c += a.lanes) {
           const int col = col0 + nt * 8 + c, t = col / G;
           Folded f;
-          float4 head[kConsumers], v[kConsumers];  // the lanes' parts of the column
+          const float4* part = reinterpret_cast<const float4*>(merge + ((my_head * a.col_warps + my_cw) * 8 + c) * kPartialStride);
+          if (a.lanes == 1) {
+            const float4 head = part[32];
+            f.acc = part[lane];
+            f.mx = head.x; f.l = head.y; f.m = head.z;
+          } else {
+            float4 head[kConsumers], v[kConsumers];  // the lanes' parts of the column
 #pragma unroll
-          for (int i = 0; i < kConsumers; ++i) {
-            const float4* part = reinterpret_cast<const float4*>(merge + (((i * a.heads + my_head) * a.col_warps + my_cw) * 8 + c) * kPartialStride);
-            head[i] = i < a.lanes ? part[32] : no_head();
-            v[i] = i < a.lanes ? part[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int i = 0; i < kConsumers; ++i) {
+              head[i] = no_head();
+              v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (i < a.lanes) {
+                head[i] = part[32];
+                v[i] = part[lane];
+              }
+              part += a.heads * a.col_warps * 8 * (kPartialStride / 4);
+            }
+            f.fold_few(head, v);
           }
-          f.fold_few(head, v);
-          if (whole_unit) {
+          if (a.cluster > 1) {  // left for the cluster's blocks to join
+            float4* rec = reinterpret_cast<float4*>(merge + ((my_head * a.col_warps + my_cw) * 8 + c) * kPartialStride);
+            rec[lane] = f.acc;
+            if (lane == 0) rec[32] = make_float4(f.mx, f.l, f.m, 0.f);
+          } else if (whole_unit) {
             f.write(a, ((int64_t)b * T + t) * a.num_q_heads + g * G + (col - t * G), lane);
           } else {
             float4* rec = record_at(a, (int)blockIdx.x, which, my_head, my_cw * NT * 8 + nt * 8 + c);
@@ -876,6 +950,30 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           }
         }
         together();
+        if (a.cluster > 1) {  // the columns of this tile, of every head and column share, are dealt to the cluster's warps
+          cluster_barrier();
+          for (int k = rank + a.cluster * warp; k < a.heads * a.col_warps * 8; k += a.cluster * kConsumers) {
+            const int hc = k >> 3, c = k & 7, head_of = hc / a.col_warps;
+            const int col = ct * a.columns + (hc - head_of * a.col_warps) * NT * 8 + nt * 8 + c;
+            if (col >= a.columns_used || (PARTS == 3 && c >= 4)) continue;
+            const uint32_t rec = smem_u32(merge + k * kPartialStride);
+            float4 head[kMaxCluster], v[kMaxCluster];
+#pragma unroll
+            for (int i = 0; i < kMaxCluster; ++i) {
+              head[i] = no_head();
+              v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (i < a.cluster) {
+                head[i] = peer_float4(rec + 512u, i);
+                v[i] = peer_float4(rec + 16u * lane, i);
+              }
+            }
+            Folded f;
+            f.fold_few(head, v);
+            const int t = col / G;
+            f.write(a, ((int64_t)b * T + t) * a.num_q_heads + (hg * a.heads + head_of) * G + (col - t * G), lane);
+          }
+          cluster_barrier();  // before the records are written over, or gone with their block
+        }
       }
     }
     seq_base += s.gran * HG;
@@ -885,50 +983,70 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   }
 }
 
-// Joins the records of the rows whose unit several stretches share. A row has SHARE warps, which take its records in turn, BATCH at a time.
-template <int SHARE, int BATCH>
+// Joins the records of the rows whose unit several stretches share. A row's part (all 128 outputs, or SPLIT of them 32 each, with a block
+// of its own then) has SHARE warps, a warp's lanes 4 outputs each of SPLIT records at a time; a lane has BATCH records in flight.
+template <int SHARE, int SPLIT, int BATCH>
 __global__ void __launch_bounds__(kJoinThreads) dense_join_kernel(const __grid_constant__ DenseArgs a) {
-  constexpr int kWarps = kJoinThreads / 32, kRows = kWarps / SHARE;
-  __shared__ __align__(16) float parts[SHARE > 1 ? kWarps * kPartialStride : 4];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, own = warp % SHARE;
-  const int64_t row = (int64_t)blockIdx.x * kRows + warp / SHARE;  // (sequence, token, head)
+  constexpr int kWarps = kJoinThreads / 32, kParts = kWarps / SHARE, kWide = 32 / SPLIT;  // lanes of a record
+  __shared__ float4 heads[SHARE * SPLIT > 1 ? kWarps * SPLIT : 1], sums[SHARE * SPLIT > 1 ? kWarps * 32 : 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / kWide;
+  const int64_t part = (int64_t)blockIdx.x * kParts + warp / SHARE, row = part / SPLIT;  // (sequence, token, head)
+  const int quad = (int)(part % SPLIT) * kWide + lane % kWide;                              // of the row's outputs
+  const int own = warp % SHARE * SPLIT + sub;
   const int h = (int)(row % a.num_q_heads), t = (int)(row / a.num_q_heads % a.T), b = (int)(row / a.num_q_heads / a.T);
   const int g = h / a.group, hg = g / a.heads, hh = g - hg * a.heads, col = t * a.group + (h - g * a.group), ct = col / a.columns, cc = col - ct * a.columns;
+  // a stretch's records lie `step` apart, the first one's perhaps among those of the units that it ends in
+  const float4* from = record_at(a, ct, 0, hh, cc);
+  const int64_t step = (int64_t)a.col_tiles * 2 * a.heads * a.columns * (kPartialStride / 4);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   int2 unit = make_int2(0, 0);
   if (b < a.num_seqs) unit = __ldcg(&a.units[(int64_t)b * a.head_groups + hg]);
   const int first = unit.x >> 1, last = unit.y;
   const bool joined = last > first;
   if (SHARE == 1 ? !joined : !__syncthreads_or(joined)) return;
+  const int aside = unit.x & 1 ? a.heads * a.columns * (kPartialStride / 4) : 0;
   Folded f;
   if (joined) {
-    auto record = [&](int s) { return record_at(a, s * a.col_tiles + ct, s == first ? unit.x & 1 : 0, hh, cc); };
-    const int count = (last - first - own + SHARE) / SHARE;  // stretches first + own, + SHARE, ..
-    for (int k = 0; k < count; k += BATCH) {
-      const int s0 = first + own + k * SHARE, n = min(BATCH, count - k);
-      float4 v[BATCH];
-      const float4 head = lane < n ? __ldcg(record(s0 + lane * SHARE) + 32) : no_head();
+    for (int s0 = first + own; s0 <= last; s0 += BATCH * SHARE * SPLIT) {
+      float4 head[BATCH], v[BATCH];
+      const float4* at = from + s0 * step;
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) v[i] = i < n ? __ldcg(record(s0 + i * SHARE) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
-      f.fold_batch(head, v);
+      for (int i = 0; i < BATCH; ++i) {
+        head[i] = no_head();
+        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s0 + i * SHARE * SPLIT <= last) {
+          const float4* rec = at + (i == 0 && s0 == first ? aside : 0);
+          head[i] = __ldcg(rec + 32);
+          v[i] = __ldcg(rec + quad);
+        }
+        at += SHARE * SPLIT * step;
+      }
+      f.fold_few(head, v);
     }
   }
-  if (SHARE > 1) {
-    float4* p = reinterpret_cast<float4*>(parts + warp * kPartialStride);
-    p[lane] = f.acc;
-    if (lane == 0) p[32] = make_float4(f.mx, f.l, f.m, 0.f);
+  if (SHARE * SPLIT > 1) {
+    sums[warp * 32 + lane] = f.acc;
+    if (lane % kWide == 0) heads[warp * SPLIT + sub] = make_float4(f.mx, f.l, f.m, 0.f);
     __syncthreads();
-    if (own != 0 || !joined) return;
+    if (warp % SHARE != 0 || sub != 0 || !joined) return;
     f = Folded();
-    float4 head[SHARE], v[SHARE];
 #pragma unroll
-    for (int i = 0; i < SHARE; ++i) {
-      head[i] = reinterpret_cast<const float4*>(parts + (warp + i) * kPartialStride)[32];
-      v[i] = reinterpret_cast<const float4*>(parts + (warp + i) * kPartialStride)[lane];
+    for (int w = 0; w < SHARE; w += 4 / SPLIT) {  // four partial sums at a time
+      float4 head[4], v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int from_warp = warp + w + i / SPLIT, k = i % SPLIT;
+        head[i] = no_head();
+        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (w + i / SPLIT < SHARE) {
+          head[i] = heads[from_warp * SPLIT + k];
+          v[i] = sums[from_warp * 32 + k * kWide + lane];
+        }
+      }
+      f.fold_few(head, v);
     }
-    f.fold_few(head, v);
   }
-  f.write(a, row, lane);
+  f.write(a, row, quad);
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------------
@@ -964,9 +1082,13 @@ bool make_map(CUtensorMap* map, const void* ptr, bool eight, const clsa_params& 
 
 }  // namespace
 
-// A launch that cuts the list anywhere pays a second kernel for the joining; one that gives each block whole units does not, but waits
-// for its longest block. Estimated from the longest sequence: bytes per block at an SM's share of the HBM bandwidth, 3 us for the joining, and
-// 0.7 for lengths below the longest, which only the first kind profits from.
+// Three ways of dealing the work. Stretches of the list, cut anywhere: even whatever the lengths are, but a second kernel joins them.
+// A cluster of blocks per unit, where all fit on the GPU at once: joined in shared memory, but the longest sequence decides. Whole units:
+// nothing to join, the longest stretch of them decides. Chosen by an estimate from the longest sequence that the call allows: a block gets its
+// share of HBM, but no more than kBlockRate; the second kernel costs 3.5 us, a cluster's joining 0.8; and the lengths are taken to be 0.7
+// of the longest one on average, which only the first way profits from.
+constexpr double kRate = 6500e3, kBlockRate = 100e3;  // bytes per us
+
 DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const DeviceInfo& dev) {
   DensePlan d = {};
   const int cols = p.q_per_seq * (p.num_q_heads / p.num_kv_heads);
@@ -983,12 +1105,18 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   while (p.num_kv_heads % most != 0 || room / (most * head_bytes) < 3) most /= 2;
   d.heads = most;
   const int64_t reach = window > 0 && window < p.max_seq_len - p.q_per_seq ? window + p.q_per_seq + kGran : p.max_seq_len;
-  const double granules = (double)((reach + kGran - 1) / kGran), us_per_head = head_bytes / 44e3;
-  double best = 0.7 * granules * us_per_head * p.num_seqs * p.num_kv_heads / d.spans + 3.0;
+  const double granules = (double)((reach + kGran - 1) / kGran);
+  double best = 0.7 * granules * head_bytes * p.num_seqs * p.num_kv_heads / kRate + 3.5;
   for (int h = most; h >= 1; h /= 2) {
-    const int64_t units = (int64_t)p.num_seqs * (p.num_kv_heads / h);
-    const double whole = (double)((units + d.spans - 1) / d.spans) * granules * h * us_per_head;
-    if (whole < best) { best = whole; d.heads = h; d.whole_units = 1; }
+    const int64_t units = (int64_t)p.num_seqs * (p.num_kv_heads / h) * d.col_tiles;
+    for (int c = kMaxCluster; c >= 1; c /= 2) {
+      if (units * c > (c == 8 ? 128 : c == 4 ? 136 : dev.sm_count) || (c > 1 && c * 2 > granules)) continue;  // (clusters of 8 and 4 find place for so many blocks)
+      const double rate = kRate / (double)(units * c) < kBlockRate ? kRate / (double)(units * c) : kBlockRate;
+      const double cost = granules * h * head_bytes / c / rate + (c > 1 ? 0.8 : 0.0);
+      if (cost < best) { best = cost; d.heads = h; d.cluster = c; d.whole_units = 0; }
+    }
+    const double cost = (double)((units + dev.sm_count - 1) / dev.sm_count) * granules * h * head_bytes * dev.sm_count / kRate;
+    if (units > dev.sm_count && cost < best) { best = cost; d.heads = h; d.cluster = 0; d.whole_units = 1; }
   }
   d.lanes = kConsumers / (d.col_warps * d.heads);
   d.head_groups = p.num_kv_heads / d.heads;
@@ -1074,28 +1202,33 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   a.whole_units = plan.whole_units;
   a.scale_log2 = p.sm_scale * kLog2e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(plan.spans * plan.col_tiles), 1, 1);
+  a.cluster = plan.cluster;
+  cfg.gridDim = dim3((unsigned)(plan.cluster > 0 ? p.num_seqs * plan.head_groups * plan.col_tiles * plan.cluster : plan.spans * plan.col_tiles), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = plan.smem_bytes;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = plan.cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = plan.cluster > 1 ? 2 : 1;
   const cudaError_t err = eight ? (plan.tiles == 1 ? launch_kernel<true, 1, 1, 2>(cfg, map_k, map_v, a) : launch_kernel<true, 2, 1, 2>(cfg, map_k, map_v, a))
                           : plan.fold           ? launch_kernel<false, 1, 3, 1>(cfg, map_k, map_v, a)
                           : plan.tiles == 1     ? launch_kernel<false, 1, 2, 1>(cfg, map_k, map_v, a)
                           : plan.col_warps <= 2 ? launch_kernel<false, 2, 2, 2>(cfg, map_k, map_v, a)
                                                 : launch_kernel<false, 2, 1, 2>(cfg, map_k, map_v, a);
-  if (err != cudaSuccess || plan.whole_units) return err;
+  if (err != cudaSuccess || plan.whole_units || plan.cluster > 0) return err;
   const int64_t rows = (int64_t)a.num_seqs * a.T * a.num_q_heads;
-  // Few rows have a block and all of their records in flight at once (148 stretches are 19 per warp of 8), which takes an SM's registers.
+  // Few rows are cut into parts of 32 outputs, so that all SMs take part and everything is in flight at once (148 stretches are 5 per lane).
+  const bool few = rows <= 64;
   const int share = rows <= 1024 ? 8 : 2;
-  cfg.gridDim = dim3((unsigned)((rows * share + 7) / 8), 1, 1);
+  cfg.gridDim = dim3((unsigned)(few ? rows * 4 : (rows * share + 7) / 8), 1, 1);
   cfg.blockDim = dim3(kJoinThreads, 1, 1);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, rows <= 296 ? dense_join_kernel<8, 20> : share == 8 ? dense_join_kernel<8, 8> : dense_join_kernel<2, 8>, a);
+  return cudaLaunchKernelEx(&cfg, few ? dense_join_kernel<8, 4, 5> : share == 8 ? dense_join_kernel<8, 1, 5> : dense_join_kernel<2, 1, 5>, a);
 }
 
 }  // namespace clsa
