@@ -69,9 +69,11 @@ struct DenseArgs {
   int scale_shift, block_shift, max_blocks, pages;
   int num_seqs, T, num_q_heads, group, columns_used;  // columns_used: T * group
   int window, causal, max_seq_len;
-  int columns, col_tiles, heads, lanes, col_warps, head_groups, slots, lane_slots, spans, min_granules;
+  int columns, col_tiles, heads, lanes, col_warps, head_groups, slots, lane_slots, spans, min_shift;
   int whole_units;  // 1: a stretch has the units that begin in it, whole
-  int cluster;      // > 0: each cluster of so many blocks has one unit, cut evenly; 0: stretches of the list
+  int cluster;      // > 0: each cluster of so many blocks (2^cluster_shift) has one unit, cut evenly; 0: stretches of the list
+  int cluster_shift;
+  uint32_t group_inv;  // ceil(2^16 / group): c / group = c * group_inv >> 16 for the columns, of which there are at most 512
   float scale_log2;
 };
 
@@ -157,14 +159,14 @@ __device__ __forceinline__ Seq look_at(const DenseArgs& a, int len) {
 struct Cut {
   int spans, each, more;
   __device__ __forceinline__ Cut(const DenseArgs& a, int total) {
-    spans = min(a.spans, max(1, (total + a.min_granules - 1) / a.min_granules));
-    each = total / spans;
+    spans = min(a.spans, max(1, (total + (1 << a.min_shift) - 1) >> a.min_shift));
+    each = (int)((uint32_t)total / (uint32_t)spans);
     more = total - each * spans;
   }
   __device__ __forceinline__ int begin(int s) const { return s * each + min(s, more); }
   __device__ __forceinline__ int owner(int g) const {
     const int big = more * (each + 1);
-    return g < big ? g / (each + 1) : more + (g - big) / each;
+    return g < big ? (int)((uint32_t)g / (uint32_t)(each + 1)) : more + (int)((uint32_t)(g - big) / (uint32_t)each);
   }
 };
 // Sum over the block, and of the threads before this one. `sums`: a word for each warp and one more.
@@ -197,6 +199,8 @@ __device__ __forceinline__ int block_scan(int v, int* sums, int& before) {
 __device__ __forceinline__ int k_token(int r) { return r < 4 ? r : r < 8 ? r + 8 : r - 4; }
 __device__ __forceinline__ int v_token(int i) { return k_token(2 * (i >> 2) + (i & 1) + ((i & 2) << 2)); }
 
+__device__ __forceinline__ int token_of(const DenseArgs& a, int col) { return (int)((uint32_t)col * a.group_inv >> 16); }
+
 // Records of partial results (kPartialStride floats: 128 outputs, then mx, l, m) folded into a running one; a lane has four outputs.
 struct Folded {
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -204,6 +208,29 @@ struct Folded {
   __device__ __forceinline__ void scale(float f) { acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f; }
   __device__ __forceinline__ void add(float f, float4 v) {
     acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+  }
+  // Up to 8 records, lane i (mod 8) having the i-th one's head (no_head where there is none) and fetch(i) its outputs.
+  template <class F>
+  __device__ __forceinline__ void fold8(float4 head, int count, F fetch) {
+    float4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i < count) v[i] = fetch(i);
+    }
+    mx = head.x;
+#pragma unroll
+    for (int d = 4; d >= 1; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    const float own = (head.x - mx) + head.z;
+    m = own;
+#pragma unroll
+    for (int d = 4; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    l = fast_exp2(head.x - mx) * head.y;
+#pragma unroll
+    for (int d = 4; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    const float share = fast_exp2(own - m);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) add(__shfl_sync(0xffffffffu, share, i), v[i]);
   }
   // A few records whose heads every lane of the warp has.
   template <int N>
@@ -281,17 +308,16 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
   // This block's stretch of the list: the first sequence that it reaches into (its number, the granules before it, length and first row).
   const int HG = a.head_groups;
-  const int rank = a.cluster > 0 ? (int)blockIdx.x % a.cluster : 0;
-  const int span = (int)blockIdx.x / a.col_tiles;  // (of the list)
-  const int ct = a.cluster > 0 ? (int)blockIdx.x / a.cluster % a.col_tiles : (int)blockIdx.x % a.col_tiles;
+  // Blocks of clusters are (rank, head group, sequence and column tile), of stretches (stretch and column tile).
+  const int rank = (int)blockIdx.x, tiled = a.cluster > 0 ? (int)blockIdx.z : (int)blockIdx.x;
+  const int span = a.col_tiles > 1 ? tiled / a.col_tiles : tiled, ct = tiled - span * a.col_tiles;
   const bool paged = a.block_table != nullptr;
   int total = 0, b_first, base_first, len_first;
   int64_t start_first;
   int span_lo, span_hi, hg_first = 0;
   if (a.cluster > 0) {  // no list: the unit's granules count from 0, those of its sequence's head groups before it below
-    const int unit = (int)blockIdx.x / (a.cluster * a.col_tiles);
-    b_first = unit / HG;
-    hg_first = unit - b_first * HG;
+    b_first = span;
+    hg_first = (int)blockIdx.y;
     len_first = a.seq_len[b_first];
     start_first = paged ? 0 : a.seq_start[b_first];
   } else if (a.num_seqs <= 32 * kPerLane) {  // every warp by itself, kPerLane sequences to a lane
@@ -367,13 +393,13 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     len_first = found[2];
     start_first = *found_start;
   }
-  const Cut cut(a, total * HG);
   if (a.cluster > 0) {
     const int g = look_at(a, len_first).gran;
     base_first = -hg_first * g;
-    span_lo = g * rank / a.cluster;
-    span_hi = g * (rank + 1) / a.cluster;
+    span_lo = g * rank >> a.cluster_shift;
+    span_hi = g * (rank + 1) >> a.cluster_shift;
   } else {
+    const Cut cut(a, total * HG);
     if (span >= cut.spans) return;
     span_lo = cut.begin(span);
     span_hi = cut.begin(span + 1);
@@ -394,8 +420,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     // The ring is one of lane_slots slots for each consuming lane, so that a slot's granules are waited for by the same warps in every round
     // (a warp that waited for a round while the one before had not landed yet would take the parity of the one before that). Steps of STEP
     // granules go to the lanes in turn: slot s holds granules number k = s % lane_slots, + lane_slots, .. of its lane.
-    const int ring = slot / a.lane_slots;
-    int k = slot - ring * a.lane_slots;
+    int ring = 0, k = slot;
+    while (k >= a.lane_slots) { k -= a.lane_slots; ++ring; }
     auto list_at = [&]() { return span_lo + (k / STEP * a.lanes + ring) * STEP + k % STEP; };
     int at = list_at();  // the place of this lane's next granule in the list
     // its place: position, head group, page table entry
@@ -411,25 +437,61 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         start = paged ? 0 : a.seq_start[b];
       }
       if (b == a.num_seqs) { valid = false; return; }
-      hg = (at - seq_base) / s.gran;
+      hg = a.cluster > 0 ? hg_first : (int)((uint32_t)(at - seq_base) / (uint32_t)s.gran);
       const int unit = seq_base + hg * s.gran, i = at - unit;
       if (a.whole_units) {
         valid = unit < span_hi;
       } else if (a.cluster == 0 && i == 0 && ct == 0) {
-        a.units[(int64_t)b * HG + hg] = make_int2(2 * span + (unit == span_lo ? 0 : 1), cut.owner(unit + s.gran - 1));
+        a.units[(int64_t)b * HG + hg] = make_int2(2 * span + (unit == span_lo ? 0 : 1), Cut(a, total * HG).owner(unit + s.gran - 1));
       }
       pos = s.base + kGran * i;
       entry = paged && valid && pos < s.n ? a.block_table[(int64_t)b * a.max_blocks + (pos >> a.block_shift)] : -1;
     };
-    place();
-    uint32_t round = 0;
-    int rounds = 0;  // that this lane has issued
-    bool alive = true;
-    while (__any_sync(0xffffffffu, valid)) {
-      // the row, and what of the granule exists
-      int row32 = -kGran, z = 0;
-      uint32_t mask = 0u;
+    uint32_t parity = 0;                      // of the round that is waited for
+    int row32 = 0, z = 0, rounds = -1;        // row and head of the granule that waits for its slot; rounds before this lane's last one
+    uint32_t mask = 0u;                       // .. and what of it exists
+    bool pending = false, alive = true;
+    while (true) {
+      // Issue what waits for its slot, and find the next granules' places once that has been tried: their lookups are under way meanwhile.
+#pragma unroll 1
+      for (uint32_t it = 0;; ++it) {
+        const bool ready = pending && mbar_test(empty_bar(slot), parity);
+        if (ready) {
+          slot_mask[slot] = mask;
+          const uint32_t bar = full_bar(slot), dst = base + (uint32_t)slot * 2u * half_bytes;
+          mbar_expect_tx(bar, 2u * half_bytes);
+          if (EIGHT) {
+            tma_load_3d(dst, &map_k, 0, row32, z, bar);
+            tma_load_3d(dst + half_bytes, &map_v, 0, row32, z, bar);
+          } else {
+            tma_load_4d(dst, &map_k, 0, row32, z, 0, bar);
+            tma_load_4d(dst + half_bytes, &map_v, 0, row32, z, 0, bar);
+          }
+          pending = false;
+          ++rounds;
+        }
+        if (it == 0) {
+          place();
+          k += a.lane_slots;
+          at = list_at();
+        }
+        if (!__any_sync(0xffffffffu, pending)) break;
+        if (it >= kSpinLimit) *abort_flag = 1u;
+        if ((it & 63u) == 63u) {
+          __nanosleep(64);
+          if (__any_sync(0xffffffffu, *abort_flag != 0u)) {
+            alive = false;
+            break;
+          }
+        }
+      }
+      if (!alive || !__any_sync(0xffffffffu, valid)) break;
+      // the next granule's row, and what of it exists
+      pending = valid;
+      parity ^= 1u;
       if (valid) {
+        row32 = -kGran;
+        mask = 0u;
         bool bad = s.bad;
         uint32_t bad_bit = CLSA_DEV_BAD_SEQLEN;
         if (EIGHT && !paged && (start & (kGran - 1)) != 0) { bad = true; bad_bit = CLSA_DEV_BAD_SCALE_BLOCK; }
@@ -451,42 +513,11 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
         z = hg * a.heads;
       }
-      bool pending = valid;
-      auto issue = [&]() {
-        if (pending && mbar_test(empty_bar(slot), (round & 1u) ^ 1u)) {
-          slot_mask[slot] = mask;
-          const uint32_t bar = full_bar(slot), dst = base + (uint32_t)slot * 2u * half_bytes;
-          mbar_expect_tx(bar, 2u * half_bytes);
-          if (EIGHT) {
-            tma_load_3d(dst, &map_k, 0, row32, z, bar);
-            tma_load_3d(dst + half_bytes, &map_v, 0, row32, z, bar);
-          } else {
-            tma_load_4d(dst, &map_k, 0, row32, z, 0, bar);
-            tma_load_4d(dst + half_bytes, &map_v, 0, row32, z, 0, bar);
-          }
-          pending = false;
-          ++rounds;
-        }
-      };
-      issue();
-      k += a.lane_slots;
-      at = list_at();
-      place();  // the next one's, whose lookups are under way while this one waits for its slot
-      for (uint32_t it = 0; alive && __any_sync(0xffffffffu, pending); ++it) {
-        issue();
-        if (it >= kSpinLimit) *abort_flag = 1u;
-        if ((it & 63u) == 63u) {
-          __nanosleep(64);
-          alive = !__any_sync(0xffffffffu, *abort_flag != 0u);
-        }
-      }
-      if (!alive) {  // given up: the copies under way still land in this block's memory
-        if (lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
-        if (rounds > 0)
-          for (uint32_t it = 0; it < kSpinLimit && !mbar_test(full_bar(slot), (uint32_t)(rounds - 1) & 1u); ++it) __nanosleep(64);
-        return;
-      }
-      ++round;
+    }
+    if (!alive) {  // given up: the copies under way still land in this block's memory
+      if (lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
+      if (rounds >= 0)
+        for (uint32_t it = 0; it < kSpinLimit && !mbar_test(full_bar(slot), (uint32_t)rounds & 1u); ++it) __nanosleep(64);
     }
     return;
   }
@@ -503,7 +534,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) tok_of[nt][h] = min(T - 1, (col0 + nt * 8 + (PARTS == 3 ? (hcol + h) & 3 : hcol + h)) / G);
+    for (int h = 0; h < 2; ++h) tok_of[nt][h] = min(T - 1, token_of(a, col0 + nt * 8 + (PARTS == 3 ? (hcol + h) & 3 : hcol + h)));
   // this lane's places in a slot's K and V rows
   uint32_t k_at, v_at;
   int row_lo, row_hi;  // tokens of rows rowq and rowq + 8 of the first product
@@ -533,7 +564,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const Seq s = look_at(a, len_b);
     const int len_next = b + 1 < a.num_seqs ? a.seq_len[b + 1] : 0;
     const int64_t start_next = EIGHT && !paged && b + 1 < a.num_seqs ? a.seq_start[b + 1] : 0;
-    for (int hg = (cur - seq_base) / s.gran; hg < HG && more; ++hg) {
+    for (int hg = a.cluster > 0 ? hg_first : (int)((uint32_t)(cur - seq_base) / (uint32_t)s.gran); hg < HG && more; ++hg) {
       const int unit = seq_base + hg * s.gran;
       const int lo = cur - unit, hi = a.whole_units ? s.gran : min(span_hi - unit, s.gran);
       const int g = hg * a.heads + my_head;  // KV head
@@ -544,7 +575,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       for (int nt = 0; nt < NT; ++nt) {
         const int col = col0 + nt * 8 + (PARTS == 3 ? rowq & 3 : rowq);
         const bool used = col < a.columns_used;
-        const int t = col / G, j = col - t * G;
+        const int t = token_of(a, col), j = col - t * G;
         const uint16_t* src = a.q + (((int64_t)b * T + t) * a.num_q_heads + g * G + j) * 128;
         if (EIGHT) {
           float amax = 0.f;
@@ -826,7 +857,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
       // This lane's steps of the block are those with number my_lane mod lanes; a segment that ends inside one has its part of it.
       const int end = seq + hi - lo, step0 = seq / STEP;
-      int n_step = step0 + (my_lane - step0 % a.lanes + a.lanes) % a.lanes;
+      int n_step = step0 + ((my_lane - step0) & (a.lanes - 1));  // (a power of two)
       uint32_t held = 0;  // 8-bit: scale bytes of this warp's granules, 32 at a time, one per lane
       int have = 0;       // .. of which granules this step's are
       for (; n_step * STEP < end; n_step += a.lanes, have += STEP) {
@@ -916,7 +947,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         const int cols = min(PARTS == 3 ? 4 : 8, a.columns_used - col0 - nt * 8);
 #pragma unroll 1
         for (int c = my_lane; c < cols; c += a.lanes) {
-          const int col = col0 + nt * 8 + c, t = col / G;
+          const int col = col0 + nt * 8 + c, t = token_of(a, col);
           Folded f;
           const float4* part = reinterpret_cast<const float4*>(merge + ((my_head * a.col_warps + my_cw) * 8 + c) * kPartialStride);
           if (a.lanes == 1) {
@@ -924,18 +955,9 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             f.acc = part[lane];
             f.mx = head.x; f.l = head.y; f.m = head.z;
           } else {
-            float4 head[kConsumers], v[kConsumers];  // the lanes' parts of the column
-#pragma unroll
-            for (int i = 0; i < kConsumers; ++i) {
-              head[i] = no_head();
-              v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (i < a.lanes) {
-                head[i] = part[32];
-                v[i] = part[lane];
-              }
-              part += a.heads * a.col_warps * 8 * (kPartialStride / 4);
-            }
-            f.fold_few(head, v);
+            // the lanes' parts of the column
+            const int stride = a.heads * a.col_warps * 8 * (kPartialStride / 4), who = lane & 7;
+            f.fold8(who < a.lanes ? part[who * stride + 32] : no_head(), a.lanes, [&](int i) { return part[i * stride + lane]; });
           }
           if (a.cluster > 1) {  // left for the cluster's blocks to join
             float4* rec = reinterpret_cast<float4*>(merge + ((my_head * a.col_warps + my_cw) * 8 + c) * kPartialStride);
@@ -957,19 +979,10 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const int col = ct * a.columns + (hc - head_of * a.col_warps) * NT * 8 + nt * 8 + c;
             if (col >= a.columns_used || (PARTS == 3 && c >= 4)) continue;
             const uint32_t rec = smem_u32(merge + k * kPartialStride);
-            float4 head[kMaxCluster], v[kMaxCluster];
-#pragma unroll
-            for (int i = 0; i < kMaxCluster; ++i) {
-              head[i] = no_head();
-              v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (i < a.cluster) {
-                head[i] = peer_float4(rec + 512u, i);
-                v[i] = peer_float4(rec + 16u * lane, i);
-              }
-            }
             Folded f;
-            f.fold_few(head, v);
-            const int t = col / G;
+            const int who = lane & 7;
+            f.fold8(who < a.cluster ? peer_float4(rec + 512u, who) : no_head(), a.cluster, [&](int i) { return peer_float4(rec + 16u * lane, i); });
+            const int t = token_of(a, col);
             f.write(a, ((int64_t)b * T + t) * a.num_q_heads + (hg * a.heads + head_of) * G + (col - t * G), lane);
           }
           cluster_barrier();  // before the records are written over, or gone with their block
@@ -1198,12 +1211,15 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   a.slots = plan.slots;
   a.lane_slots = plan.lane_slots;
   a.spans = plan.spans;
-  a.min_granules = plan.lanes * plan.step;
+  while ((1 << a.min_shift) < plan.lanes * plan.step) ++a.min_shift;
   a.whole_units = plan.whole_units;
+  a.cluster = plan.cluster;
+  while ((1 << a.cluster_shift) < plan.cluster) ++a.cluster_shift;
+  a.group_inv = (65536u + (uint32_t)a.group - 1u) / (uint32_t)a.group;
   a.scale_log2 = p.sm_scale * kLog2e;
   cudaLaunchConfig_t cfg = {};
-  a.cluster = plan.cluster;
-  cfg.gridDim = dim3((unsigned)(plan.cluster > 0 ? p.num_seqs * plan.head_groups * plan.col_tiles * plan.cluster : plan.spans * plan.col_tiles), 1, 1);
+  cfg.gridDim = plan.cluster > 0 ? dim3((unsigned)plan.cluster, (unsigned)plan.head_groups, (unsigned)(p.num_seqs * plan.col_tiles))
+                                 : dim3((unsigned)(plan.spans * plan.col_tiles), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = plan.smem_bytes;
   cfg.stream = stream;
