@@ -60,7 +60,7 @@ __device__ __forceinline__ int scale_exponent(int byte) { return min(max(byte, k
 // Smallest exponent e with amax <= 448 * 2^e = 1.75 * 2^(e + 8), within the allowed range.
 __device__ __forceinline__ int need_exponent(float amax) {
   const uint32_t bits = __float_as_uint(amax);
-  const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  const int e = (int)((bits + 0x1fffffu) >> 23) - 127 - 8;  // (a mantissa above 0x600000 carries)
   return min(max(e, kScaleExpMin), kScaleExpMax);
 }
 // 2^e for -126 <= e <= 127.
