@@ -38,7 +38,6 @@
 namespace clsa {
 namespace {
 
-constexpr int kGran = 16;                 // positions per granule
 constexpr int kConsumers = 8;             // consuming warps
 constexpr int kProducers = 4;             // .. and fetching ones
 constexpr int kThreads = (kConsumers + kProducers) * 32;
@@ -69,6 +68,8 @@ struct DenseArgs {
   int scale_shift, block_shift, max_blocks, pages;
   int num_seqs, T, num_q_heads, group, columns_used;  // columns_used: T * group
   int window, causal, max_seq_len;
+  int gran_shift;   // a granule is 16 positions, or 32 of an 8-bit cache
+  int two_boxes;    // 1: its two halves are fetched apart (pages of 16 rows)
   int columns, col_tiles, heads, lanes, col_warps, head_groups, slots, lane_slots, spans, min_shift;
   int whole_units;  // 1: a stretch has the units that begin in it, whole
   int cluster;      // > 0: each cluster of so many blocks (2^cluster_shift) has one unit, cut evenly; 0: stretches of the list
@@ -151,8 +152,8 @@ __device__ __forceinline__ Seq look_at(const DenseArgs& a, int len) {
   s.bad = len < (a.causal || a.window ? a.T : 0) || len > a.max_seq_len;
   s.n = s.bad ? 0 : len;
   s.first = a.window ? max(0, s.n - a.T + 1 - a.window) : 0;
-  s.base = s.first & ~(kGran - 1);
-  s.gran = max(1, (s.n - s.base + kGran - 1) / kGran);
+  s.base = s.first >> a.gran_shift << a.gran_shift;
+  s.gran = max(1, (s.n - s.base + (1 << a.gran_shift) - 1) >> a.gran_shift);
   return s;
 }
 // How the list of `total` granules is cut: the first total % spans stretches have one more than total / spans.
@@ -271,13 +272,15 @@ __device__ __forceinline__ float4* record_at(const DenseArgs& a, int block, int 
 
 // ---- the kernel --------------------------------------------------------------------------------------------------------
 // EIGHT: an 8-bit cache. NT: column tiles per warp. PARTS (bf16): 1, the weights' rounding is all there is; 2, a second product takes
-// what it left; 3 (NT = 1, up to 4 columns), columns 4 .. 7 repeat the first four and take it. STEP: granules that a warp works on together.
-template <bool EIGHT, int NT, int PARTS, int STEP>
+// what it left; 3 (NT = 1, up to 4 columns), columns 4 .. 7 repeat the first four and take it. PIPED: a granule's first product is formed while the one
+// before it is finished.
+template <bool EIGHT, int NT, int PARTS, bool PIPED>
 __global__ void __launch_bounds__(kThreads, 1)
 dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ DenseArgs a) {
   extern __shared__ unsigned char smem_dyn[];
   const uint32_t raw = smem_u32(smem_dyn), base = (raw + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_dyn + (base - raw);
+  constexpr int kSub = EIGHT ? 2 : 1, kGran = 16 * kSub;  // 16-row parts of a granule
   const int row_bytes = EIGHT ? 128 : 256;
   const uint32_t half_bytes = (uint32_t)(a.heads * kGran * row_bytes);  // a slot's K rows, then its V rows
   const uint32_t ring_bytes = (uint32_t)a.slots * 2u * half_bytes;
@@ -418,15 +421,15 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     Seq s = look_at(a, len_first);
     int64_t start = start_first;
     // The ring is one of lane_slots slots for each consuming lane, so that a slot's granules are waited for by the same warps in every round
-    // (a warp that waited for a round while the one before had not landed yet would take the parity of the one before that). Steps of STEP
-    // granules go to the lanes in turn: slot s holds granules number k = s % lane_slots, + lane_slots, .. of its lane.
+    // (a warp that waited for a round while the one before had not landed yet would take the parity of the one before that). Granules
+    // go to the lanes in turn: slot s holds granules number k = s % lane_slots, + lane_slots, .. of its lane.
     int ring = 0, k = slot;
     while (k >= a.lane_slots) { k -= a.lane_slots; ++ring; }
-    auto list_at = [&]() { return span_lo + (k / STEP * a.lanes + ring) * STEP + k % STEP; };
+    auto list_at = [&]() { return span_lo + k * a.lanes + ring; };
     int at = list_at();  // the place of this lane's next granule in the list
     // its place: position, head group, page table entry
     bool valid;
-    int pos, hg, entry;
+    int pos, hg, entry, entry2 = -1;
     auto place = [&]() {
       valid = slot < a.slots && at < span_hi;
       if (!valid && !(a.whole_units && slot < a.slots)) return;
@@ -445,10 +448,15 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         a.units[(int64_t)b * HG + hg] = make_int2(2 * span + (unit == span_lo ? 0 : 1), Cut(a, total * HG).owner(unit + s.gran - 1));
       }
       pos = s.base + kGran * i;
-      entry = paged && valid && pos < s.n ? a.block_table[(int64_t)b * a.max_blocks + (pos >> a.block_shift)] : -1;
+      entry = entry2 = -1;
+      if (paged && valid) {
+        const int32_t* row_of_table = a.block_table + (int64_t)b * a.max_blocks;
+        if (pos < s.n) entry = row_of_table[pos >> a.block_shift];
+        if (kSub == 2 && a.two_boxes && pos + 16 < s.n) entry2 = row_of_table[(pos >> a.block_shift) + 1];
+      }
     };
     uint32_t parity = 0;                      // of the round that is waited for
-    int row32 = 0, z = 0, rounds = -1;        // row and head of the granule that waits for its slot; rounds before this lane's last one
+    int row32 = 0, row32b = 0, z = 0, rounds = -1;  // row (of its second half, where that is apart) and head of the granule that waits for its slot; rounds before this lane's last one
     uint32_t mask = 0u;                       // .. and what of it exists
     bool pending = false, alive = true;
     while (true) {
@@ -463,6 +471,10 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           if (EIGHT) {
             tma_load_3d(dst, &map_k, 0, row32, z, bar);
             tma_load_3d(dst + half_bytes, &map_v, 0, row32, z, bar);
+            if (a.two_boxes) {
+              tma_load_3d(dst + half_bytes / 2, &map_k, 0, row32b, z, bar);
+              tma_load_3d(dst + half_bytes + half_bytes / 2, &map_v, 0, row32b, z, bar);
+            }
           } else {
             tma_load_4d(dst, &map_k, 0, row32, z, 0, bar);
             tma_load_4d(dst + half_bytes, &map_v, 0, row32, z, 0, bar);
@@ -490,25 +502,35 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       pending = valid;
       parity ^= 1u;
       if (valid) {
-        row32 = -kGran;
-        mask = 0u;
         bool bad = s.bad;
         uint32_t bad_bit = CLSA_DEV_BAD_SEQLEN;
-        if (EIGHT && !paged && (start & (kGran - 1)) != 0) { bad = true; bad_bit = CLSA_DEV_BAD_SCALE_BLOCK; }
-        int64_t row = start + pos;
-        if (paged) row = entry >= 0 && entry < a.pages ? ((int64_t)entry << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : -kGran;
-        if (row > -kGran && row < a.num_rows) {
-          row32 = (int)row;
-          mask = 0xffffu;
-          if (row < 0) mask &= 0xffffu << (int)-row;
-          if (row + kGran > a.num_rows) mask &= 0xffffu >> (int)(row + kGran - a.num_rows);
+        if (EIGHT && !paged && (start & 15) != 0) { bad = true; bad_bit = CLSA_DEV_BAD_SCALE_BLOCK; }
+        // a box of `rows` rows from cache row `row` on: where to fetch it from (somewhere outside for one of zeros), its rows that exist
+        auto box = [&](int64_t row, int rows, int& from) {
+          from = -kGran;
+          if (row <= -rows || row >= a.num_rows) return 0u;
+          from = (int)row;
+          uint32_t m = 0xffffffffu >> (32 - rows);
+          if (row < 0) m &= 0xffffffffu << (int)-row;
+          if (row + rows > a.num_rows) m &= 0xffffffffu >> (int)(32 - (a.num_rows - row));
+          return m;
+        };
+        auto row_of = [&](int of_entry) {
+          if (!paged) return start + pos;
+          return of_entry >= 0 && of_entry < a.pages ? ((int64_t)of_entry << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : (int64_t)-kGran;
+        };
+        if (kSub == 2 && a.two_boxes) {  // (16-row pages: both halves are whole pages)
+          mask = box(row_of(entry), 16, row32);
+          mask |= box(entry2 >= 0 && entry2 < a.pages ? (int64_t)entry2 << 4 : (int64_t)-kGran, 16, row32b) << 16;
+        } else {
+          mask = box(row_of(entry), kGran, row32);
         }
         if (bad) {
           flag_status(a.status, bad_bit);
           mask = 0u;
-        } else if (mask != 0xffffu) {
+        } else if (mask != 0xffffffffu >> (32 - kGran)) {
           const int from = max(0, s.first - pos), to = min(kGran, s.n - pos);
-          const uint32_t wanted = to > from ? ((1u << to) - 1u) & ~((1u << from) - 1u) : 0u;
+          const uint32_t wanted = to > from ? (0xffffffffu >> (32 - to)) & (0xffffffffu << from) : 0u;
           if ((wanted & ~mask) != 0u) flag_status(a.status, CLSA_DEV_BAD_INDEX);
         }
         z = hg * a.heads;
@@ -535,19 +557,20 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int h = 0; h < 2; ++h) tok_of[nt][h] = min(T - 1, token_of(a, col0 + nt * 8 + (PARTS == 3 ? (hcol + h) & 3 : hcol + h)));
-  // this lane's places in a slot's K and V rows
+  // this lane's places in a slot's K and V rows (its 16-row parts lie part_step apart)
+  const uint32_t part_step = a.two_boxes ? half_bytes / 2 : 2048u, head_at = (uint32_t)my_head * (kSub == 2 && !a.two_boxes ? 4096u : 2048u);
   uint32_t k_at, v_at;
   int row_lo, row_hi;  // tokens of rows rowq and rowq + 8 of the first product
   if (EIGHT) {
     const int kt = k_token(t7 + 8 * ((lane >> 3) & 1)), vt = v_token(lane & 15);
-    k_at = base + (uint32_t)(my_head * 2048 + kt * 128 + (((lane >> 4) ^ (kt & 7)) << 4));
-    v_at = base + (uint32_t)(my_head * 2048 + vt * 128 + (((lane >> 4) ^ (vt & 7)) << 4)) + half_bytes;
+    k_at = base + head_at + (uint32_t)(kt * 128 + (((lane >> 4) ^ (kt & 7)) << 4));
+    v_at = base + head_at + (uint32_t)(vt * 128 + (((lane >> 4) ^ (vt & 7)) << 4)) + half_bytes;
     row_lo = k_token(rowq);
     row_hi = k_token(rowq + 8);
   } else {
     const int kt = t7 + 8 * ((lane >> 3) & 1), vt = t7 + 8 * (lane >> 4);
-    k_at = base + (uint32_t)(my_head * 2048 + kt * 128 + (((lane >> 4) ^ t7) << 4));
-    v_at = base + (uint32_t)(my_head * 2048 + vt * 128 + ((((lane >> 3) & 1) ^ t7) << 4)) + half_bytes;
+    k_at = base + head_at + (uint32_t)(kt * 128 + (((lane >> 4) ^ t7) << 4));
+    v_at = base + head_at + (uint32_t)(vt * 128 + ((((lane >> 3) & 1) ^ t7) << 4)) + half_bytes;
     row_lo = rowq;
     row_hi = rowq + 8;
   }
@@ -625,12 +648,10 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       // every query sees [all_from, all_to)
       const int all_from = a.window ? max(0, s.n - a.window) : 0, all_to = a.causal ? s.n - T + 1 : s.n;
 
-      // One step: U granules from position pos0 on, in the slots whose K and V rows are at kb[] and vb[]. MASKED (U = 1): some query does not
-      // see all of it, rows_ok has its rows that exist. codes: the scale bytes (8-bit caches).
-      auto step = [&](auto u_const, auto masked_const, int pos0, const uint32_t* kb, const uint32_t* vb, uint32_t rows_ok, const uint32_t* codes) {
+      // U parts of 16 rows, whose K and V rows are at kb[] and vb[], in two steps. The first product: x, rows rowq (columns hcol, hcol + 1) and
+      // rowq + 8.
+      auto first_product = [&](auto u_const, const uint32_t* kb, float (*x)[NT][4]) {
         constexpr int U = decltype(u_const)::value;
-        constexpr bool MASKED = decltype(masked_const)::value;
-        float x[U][NT][4], ev[U];  // rows rowq (columns hcol, hcol + 1), rowq + 8
         constexpr bool kOdd = U * NT == 1;  // two chains of dependent products where there would be one
         float odd[NT][4];
 #pragma unroll
@@ -667,6 +688,17 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
               for (int nt = 0; nt < NT; ++nt) mma_bf16(kOdd && (ks & 1) ? odd[nt] : x[u][nt], kf, qb[nt][ks][0], qb[nt][ks][1]);
             }
         }
+        if (kOdd) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[0][0][k] += odd[0][k];
+        }
+      };
+      // Everything behind it. pos0: the (first) part's first position. MASKED (U = 1): some query does not see all of it, rows_ok has its rows
+      // that exist. codes: the scale bytes (8-bit caches): K's, V's.
+      auto finish = [&](auto u_const, auto masked_const, int pos0, float (*x)[NT][4], const uint32_t* vb, uint32_t rows_ok, const uint32_t* codes) {
+        constexpr int U = decltype(u_const)::value;
+        constexpr bool MASKED = decltype(masked_const)::value;
+        float ev[U];
         // logits in the log2 domain
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -676,8 +708,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float d = kOdd ? x[u][nt][k] + odd[nt][k] : x[u][nt][k];
-              x[u][nt][k] = EIGHT ? d * kf * qf[nt][k & 1] : d * kf;
+              x[u][nt][k] = EIGHT ? x[u][nt][k] * kf * qf[nt][k & 1] : x[u][nt][k] * kf;
             }
         }
         auto sees = [&](int t, int row) {  // whether query token t sees row `row` of the granule
@@ -855,58 +886,109 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
       };
 
-      // This lane's steps of the block are those with number my_lane mod lanes; a segment that ends inside one has its part of it.
-      const int end = seq + hi - lo, step0 = seq / STEP;
-      int n_step = step0 + ((my_lane - step0) & (a.lanes - 1));  // (a power of two)
-      uint32_t held = 0;  // 8-bit: scale bytes of this warp's granules, 32 at a time, one per lane
-      int have = 0;       // .. of which granules this step's are
-      for (; n_step * STEP < end; n_step += a.lanes, have += STEP) {
-        if (EIGHT && (have & 31) == 0) {
-          const int n = (n_step + lane / STEP * a.lanes) * STEP + lane % STEP;
-          held = 127u | 127u << 8;
-          if (n >= seq && n < end) {
-            const int pos = s.base + kGran * (lo + n - seq);
-            int64_t row = start + pos;
-            if (paged) {
-              const int blk = pos < s.n ? a.block_table[(int64_t)b * a.max_blocks + (pos >> a.block_shift)] : -1;
-              row = blk >= 0 && blk < a.pages ? ((int64_t)blk << a.block_shift) + (pos & ((1 << a.block_shift) - 1)) : -1;
-            }
-            if (row >= 0 && row < a.num_rows) {
-              const int64_t from = g * a.scale_head + (row >> a.scale_shift);
-              held = (uint32_t)a.ks[from] | (uint32_t)a.vs[from] << 8;
-            }
-          }
-        }
-        const int n0 = max(n_step * STEP, seq), count = min(n_step * STEP + STEP, end) - n0, skip = n0 - n_step * STEP;
-        const int pos0 = s.base + kGran * (lo + n0 - seq);
-        uint32_t kb[STEP], vb[STEP], codes[STEP];
-        uint32_t rows_ok = 0xffffu;
-        const int slot_before = slot;
-#pragma unroll
-        for (int u = 0; u < STEP; ++u) {
-          const uint32_t off = (uint32_t)(ring0 + slot) * 2u * half_bytes;
-          kb[u] = k_at + off;
-          vb[u] = v_at + off;
-          codes[u] = EIGHT ? __shfl_sync(0xffffffffu, held, (have + skip + u) & 31) : 0u;
-          if (u < count) {
-            if (!mbar_wait(full_bar(ring0 + slot), round, abort_flag) && lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
-            rows_ok &= slot_mask[ring0 + slot];
-            if (++slot == a.lane_slots) { slot = 0; round ^= 1u; }
-          }
-        }
-        if (count == STEP && rows_ok == 0xffffu && pos0 >= all_from && pos0 + STEP * kGran <= all_to) {  // every query sees all of it
-          step(std::integral_constant<int, STEP>(), std::false_type(), pos0, kb, vb, 0xffffu, codes);
-        } else {
-#pragma unroll 1
-          for (int u = 0; u < count; ++u) {
-            const int here = ring0 + (slot_before + u >= a.lane_slots ? slot_before + u - a.lane_slots : slot_before + u);
-            const uint32_t kb1 = k_at + (uint32_t)here * 2u * half_bytes, vb1 = v_at + (uint32_t)here * 2u * half_bytes;
-            const uint32_t code1 = EIGHT ? __shfl_sync(0xffffffffu, held, (have + skip + u) & 31) : 0u;
-            step(std::integral_constant<int, 1>(), std::true_type(), pos0 + u * kGran, &kb1, &vb1, slot_mask[here], &code1);
-          }
-        }
+      // This lane's granules of the block are those with number my_lane mod lanes.
+      const int end = seq + hi - lo;
+      int n = seq + ((my_lane - seq) & (a.lanes - 1));  // (a power of two)
+      const auto all_parts = std::integral_constant<int, kSub>();
+      const int pos_step = kGran * a.lanes;
+      int pos = s.base + kGran * (lo + n - seq);
+      const int last_whole = all_to - kGran;  // every query sees all of a granule from all_from to here
+      uint32_t held = 0;  // 8-bit: the scale bytes (K's, V's of either part) of 32 granules of this warp, one per lane
+      int have = 0;       // .. of which this one is
+      // With PIPED a granule that every query sees whole has its first product formed while the one before it is finished: `held_x` is that
+      // product of the granule whose V rows are at held_vb, in slot held_slot.
+      float held_x[kSub][NT][4];
+      uint32_t held_vb = 0u;
+      int held_slot = -1;
+      auto release = [&](int which) {
         __syncwarp();
-        if (lane < count) mbar_arrive(empty_bar(ring0 + (slot_before + lane >= a.lane_slots ? slot_before + lane - a.lane_slots : slot_before + lane)));
+        if (lane == 0) mbar_arrive(empty_bar(which));
+      };
+      for (; PIPED || n < end; n += a.lanes, pos += pos_step) {
+        const bool any = !PIPED || n < end;
+        uint32_t codes[kSub] = {};
+        if (EIGHT) {
+          if ((have & 31) == 0) {
+            held = 0x7f7f7f7fu;
+            const int at = pos + pos_step * lane;
+            if (n + a.lanes * lane < end) {
+#pragma unroll
+              for (int u = 0; u < kSub; ++u) {
+                const int p = at + 16 * u;
+                int64_t row = start + p;
+                if (paged) {
+                  const int blk = p < s.n ? a.block_table[(int64_t)b * a.max_blocks + (p >> a.block_shift)] : -1;
+                  row = blk >= 0 && blk < a.pages ? ((int64_t)blk << a.block_shift) + (p & ((1 << a.block_shift) - 1)) : -1;
+                }
+                if (p < s.n && row >= 0 && row < a.num_rows) {
+                  const int64_t from = g * a.scale_head + (row >> a.scale_shift);
+                  held = (held & ~(0xffffu << (16 * u))) | ((uint32_t)a.ks[from] | (uint32_t)a.vs[from] << 8) << (16 * u);
+                }
+              }
+            }
+          }
+          const uint32_t both = __shfl_sync(0xffffffffu, held, have & 31);
+          ++have;
+#pragma unroll
+          for (int u = 0; u < kSub; ++u) codes[u] = both >> (16 * u) & 0xffffu;
+        }
+        const int here = ring0 + slot;
+        const uint32_t off = (uint32_t)here * 2u * half_bytes;
+        uint32_t kb[kSub], vb[kSub];
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) {
+          kb[u] = k_at + off + (uint32_t)u * part_step;
+          vb[u] = v_at + off + (uint32_t)u * part_step;
+        }
+        uint32_t rows_ok = 0u;
+        if (any) {
+          if (!mbar_wait(full_bar(here), round, abort_flag) && lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
+          rows_ok = slot_mask[here];
+          if (++slot == a.lane_slots) { slot = 0; round ^= 1u; }
+        }
+        const bool whole = rows_ok == 0xffffffffu >> (32 - kGran) && pos >= all_from && pos <= last_whole;
+        if constexpr (PIPED) {
+          static_assert(!PIPED || kSub == 1, "one part");
+          if (whole && held_slot >= 0) {
+            float x[kSub][NT][4];
+            first_product(all_parts, kb, x);
+            finish(all_parts, std::false_type(), 0, held_x, &held_vb, 0xffffu, codes);
+            release(held_slot);
+            held_slot = here;
+            held_vb = vb[0];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) held_x[0][nt][k] = x[0][nt][k];
+            continue;
+          }
+          if (held_slot >= 0) {
+            finish(all_parts, std::false_type(), 0, held_x, &held_vb, 0xffffu, codes);
+            release(held_slot);
+            held_slot = -1;
+          }
+          if (!any) break;
+          if (whole) {
+            first_product(all_parts, kb, held_x);
+            held_slot = here;
+            held_vb = vb[0];
+            continue;
+          }
+        } else if (whole) {
+          first_product(all_parts, kb, held_x);
+          finish(all_parts, std::false_type(), 0, held_x, vb, 0xffffu, codes);
+          release(here);
+          continue;
+        }
+#pragma unroll 1
+        for (int u = 0; u < kSub; ++u) {
+          const uint32_t kb1 = kb[0] + (uint32_t)u * part_step, vb1 = vb[0] + (uint32_t)u * part_step;
+          const uint32_t code1 = u == 0 ? codes[0] : codes[kSub - 1];
+          float x[1][NT][4];
+          first_product(std::integral_constant<int, 1>(), &kb1, x);
+          finish(std::integral_constant<int, 1>(), std::true_type(), pos + 16 * u, x, &vb1, rows_ok >> (16 * u), &code1);
+        }
+        release(here);
       }
       seq = end;
       cur = unit + hi;
@@ -1078,15 +1160,15 @@ EncodeTiledFn encode_tiled_fn() {
   return fn;
 }
 
-// K or V rows as boxes of 16 rows of `heads` heads. bf16: [half][head][row][64 elements], codes: [head][row][128].
-bool make_map(CUtensorMap* map, const void* ptr, bool eight, const clsa_params& p, int64_t token_stride, int64_t head_stride, int heads) {
+// K or V rows as boxes of `rows` rows of `heads` heads. bf16: [half][head][row][64 elements], codes: [head][row][128].
+bool make_map(CUtensorMap* map, const void* ptr, bool eight, const clsa_params& p, int64_t token_stride, int64_t head_stride, int heads, int rows) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
   const cuuint64_t size = eight ? 1 : 2;
   if (p.num_kv_heads == 1) head_stride = 128;  // of one head it means nothing
   const cuuint64_t dims[4] = {eight ? 128u : 64u, (cuuint64_t)p.num_cache_rows, (cuuint64_t)p.num_kv_heads, 2};
   const cuuint64_t strides[3] = {(cuuint64_t)token_stride * size, (cuuint64_t)head_stride * size, 128};
-  const cuuint32_t box[4] = {eight ? 128u : 64u, kGran, (cuuint32_t)heads, 2};
+  const cuuint32_t box[4] = {eight ? 128u : 64u, (cuuint32_t)rows, (cuuint32_t)heads, 2};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
   return fn(map, eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, eight ? 3 : 4, const_cast<void*>(ptr), dims,
             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -1107,18 +1189,17 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   const int cols = p.q_per_seq * (p.num_q_heads / p.num_kv_heads);
   d.fold = !eight && cols <= 4;
   d.tiles = cols <= 8 ? 1 : 2;
-  d.step = d.tiles == 1 && !eight ? 1 : 2;
   d.col_warps = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
   d.columns = d.fold ? 4 : d.tiles * d.col_warps * 8;
   d.col_tiles = (cols + d.columns - 1) / d.columns;
   d.spans = dev.sm_count / d.col_tiles;
-  const int head_bytes = kGran * (eight ? 256 : 512);  // of a granule
+  const int gran = eight ? 32 : 16, head_bytes = gran * (eight ? 256 : 512);  // positions of a granule, bytes of a head's part of it
   const int room = dev.max_smem_optin - kMergeBytes - kCtrlBytes - 1024;
   int most = kConsumers / d.col_warps;
   while (p.num_kv_heads % most != 0 || room / (most * head_bytes) < 3) most /= 2;
   d.heads = most;
-  const int64_t reach = window > 0 && window < p.max_seq_len - p.q_per_seq ? window + p.q_per_seq + kGran : p.max_seq_len;
-  const double granules = (double)((reach + kGran - 1) / kGran);
+  const int64_t reach = window > 0 && window < p.max_seq_len - p.q_per_seq ? window + p.q_per_seq + gran : p.max_seq_len;
+  const double granules = (double)((reach + gran - 1) / gran);
   double best = 0.7 * granules * head_bytes * p.num_seqs * p.num_kv_heads / kRate + 3.5;
   for (int h = most; h >= 1; h /= 2) {
     const int64_t units = (int64_t)p.num_seqs * (p.num_kv_heads / h) * d.col_tiles;
@@ -1146,9 +1227,9 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   return d;
 }
 
-template <bool EIGHT, int NT, int PARTS, int STEP>
+template <bool EIGHT, int NT, int PARTS, bool PIPED>
 cudaError_t launch_kernel(const cudaLaunchConfig_t& cfg, const CUtensorMap& map_k, const CUtensorMap& map_v, const DenseArgs& a) {
-  auto kernel = dense_attn_kernel<EIGHT, NT, PARTS, STEP>;
+  auto kernel = dense_attn_kernel<EIGHT, NT, PARTS, PIPED>;
   // The kernel's warpgroups redistribute the registers that it was launched with: it may not have been built with fewer.
   static std::atomic<uint64_t> known{0};  // devices on which it has been looked at, and allowed its shared memory
   int dev = 0;
@@ -1170,9 +1251,11 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
                               float* lse, uint32_t* status, unsigned char* scratch, cudaStream_t stream) {
   CUtensorMap map_k, map_v;
   const bool eight = c != nullptr;
+  const bool two_boxes = eight && p.block_table != nullptr && p.block_size == 16;
+  const int box_rows = eight && !two_boxes ? 32 : 16;
   const int64_t token = eight ? c->kv_token_stride : p.kv_token_stride, head = eight ? c->kv_head_stride : p.kv_head_stride;
-  if (!make_map(&map_k, eight ? c->k : p.k_cache, eight, p, token, head, plan.heads) ||
-      !make_map(&map_v, eight ? c->v : p.v_cache, eight, p, token, head, plan.heads))
+  if (!make_map(&map_k, eight ? c->k : p.k_cache, eight, p, token, head, plan.heads, box_rows) ||
+      !make_map(&map_v, eight ? c->v : p.v_cache, eight, p, token, head, plan.heads, box_rows))
     return cudaErrorInvalidValue;
   DenseArgs a = {};
   a.q = static_cast<const uint16_t*>(q);
@@ -1211,7 +1294,9 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   a.slots = plan.slots;
   a.lane_slots = plan.lane_slots;
   a.spans = plan.spans;
-  while ((1 << a.min_shift) < plan.lanes * plan.step) ++a.min_shift;
+  while ((1 << a.min_shift) < plan.lanes) ++a.min_shift;
+  a.gran_shift = eight ? 5 : 4;
+  a.two_boxes = two_boxes;
   a.whole_units = plan.whole_units;
   a.cluster = plan.cluster;
   while ((1 << a.cluster_shift) < plan.cluster) ++a.cluster_shift;
@@ -1231,11 +1316,11 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = plan.cluster > 1 ? 2 : 1;
-  const cudaError_t err = eight ? (plan.tiles == 1 ? launch_kernel<true, 1, 1, 2>(cfg, map_k, map_v, a) : launch_kernel<true, 2, 1, 2>(cfg, map_k, map_v, a))
-                          : plan.fold           ? launch_kernel<false, 1, 3, 1>(cfg, map_k, map_v, a)
-                          : plan.tiles == 1     ? launch_kernel<false, 1, 2, 1>(cfg, map_k, map_v, a)
-                          : plan.col_warps <= 2 ? launch_kernel<false, 2, 2, 2>(cfg, map_k, map_v, a)
-                                                : launch_kernel<false, 2, 1, 2>(cfg, map_k, map_v, a);
+  const cudaError_t err = eight ? (plan.tiles == 1 ? launch_kernel<true, 1, 1, false>(cfg, map_k, map_v, a) : launch_kernel<true, 2, 1, false>(cfg, map_k, map_v, a))
+                          : plan.fold           ? launch_kernel<false, 1, 3, false>(cfg, map_k, map_v, a)
+                          : plan.tiles == 1     ? launch_kernel<false, 1, 2, false>(cfg, map_k, map_v, a)
+                          : plan.col_warps <= 2 ? launch_kernel<false, 2, 2, true>(cfg, map_k, map_v, a)
+                                                : launch_kernel<false, 2, 1, true>(cfg, map_k, map_v, a);
   if (err != cudaSuccess || plan.whole_units || plan.cluster > 0) return err;
   const int64_t rows = (int64_t)a.num_seqs * a.T * a.num_q_heads;
   // Few rows are cut into parts of 32 outputs, so that all SMs take part and everything is in flight at once (148 stretches are 5 per lane).

@@ -10,10 +10,9 @@ struct DensePlan {
   int fold, tiles, col_warps;  // query columns of a block: 4 (held twice), or col_warps * tiles * 8
   int columns;                 // .. their number
   int col_tiles;               // blocks that share one stretch of the cache, each with its own query columns
-  int heads, lanes;            // KV heads of a block; warps that take 16-token granules of one head (and column share) in turn
+  int heads, lanes;            // KV heads of a block; warps that take granules of one head (and column share) in turn
   int head_groups;             // Hkv / heads
   int slots, lane_slots, slot_bytes;  // the rings, one per lane: a granule's K and V rows of the block's heads in each slot
-  int step;                    // granules that a warp works on together
   int spans;                   // stretches that the list of granules is cut into, at most
   int whole_units;             // 1: a stretch has the units that begin in it, whole (nothing to join)
   int cluster;                 // > 0: each cluster of so many blocks has one unit instead (joined in shared memory)
