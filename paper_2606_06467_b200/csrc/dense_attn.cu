@@ -68,7 +68,7 @@ struct DenseArgs {
   int scale_shift, block_shift, max_blocks, pages;
   int num_seqs, T, num_q_heads, group, columns_used;  // columns_used: T * group
   int window, causal, max_seq_len;
-  int gran_shift;   // a granule is 16 positions, or 32 of an 8-bit cache
+  int gran_shift;   // a granule is 16 or 32 positions
   int two_boxes;    // 1: its two halves are fetched apart (pages of 16 rows)
   int columns, col_tiles, heads, lanes, col_warps, head_groups, slots, lane_slots, spans, min_shift;
   int whole_units;  // 1: a stretch has the units that begin in it, whole
@@ -272,15 +272,15 @@ __device__ __forceinline__ float4* record_at(const DenseArgs& a, int block, int 
 
 // ---- the kernel --------------------------------------------------------------------------------------------------------
 // EIGHT: an 8-bit cache. NT: column tiles per warp. PARTS (bf16): 1, the weights' rounding is all there is; 2, a second product takes
-// what it left; 3 (NT = 1, up to 4 columns), columns 4 .. 7 repeat the first four and take it. PIPED: a granule's first product is formed while the one
-// before it is finished.
-template <bool EIGHT, int NT, int PARTS, bool PIPED>
+// what it left; 3 (NT = 1, up to 4 columns), columns 4 .. 7 repeat the first four and take it. SUB: 16-row parts of a granule. PIPED (SUB = 1): a
+// granule's first product is formed while the one before it is finished.
+template <bool EIGHT, int NT, int PARTS, int SUB, bool PIPED>
 __global__ void __launch_bounds__(kThreads, 1)
 dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ DenseArgs a) {
   extern __shared__ unsigned char smem_dyn[];
   const uint32_t raw = smem_u32(smem_dyn), base = (raw + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_dyn + (base - raw);
-  constexpr int kSub = EIGHT ? 2 : 1, kGran = 16 * kSub;  // 16-row parts of a granule
+  constexpr int kSub = SUB, kGran = 16 * SUB;
   const int row_bytes = EIGHT ? 128 : 256;
   const uint32_t half_bytes = (uint32_t)(a.heads * kGran * row_bytes);  // a slot's K rows, then its V rows
   const uint32_t ring_bytes = (uint32_t)a.slots * 2u * half_bytes;
@@ -478,6 +478,10 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           } else {
             tma_load_4d(dst, &map_k, 0, row32, z, 0, bar);
             tma_load_4d(dst + half_bytes, &map_v, 0, row32, z, 0, bar);
+            if (kSub == 2 && a.two_boxes) {
+              tma_load_4d(dst + half_bytes / 2, &map_k, 0, row32b, z, 0, bar);
+              tma_load_4d(dst + half_bytes + half_bytes / 2, &map_v, 0, row32b, z, 0, bar);
+            }
           }
           pending = false;
           ++rounds;
@@ -574,7 +578,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     row_lo = rowq;
     row_hi = rowq + 8;
   }
-  const uint32_t upper = half_bytes / 2;  // from dimensions 0 .. 63 of the bf16 rows to 64 .. 127
+  const uint32_t upper = half_bytes / (kSub == 2 && a.two_boxes ? 4 : 2);  // from dimensions 0 .. 63 of the bf16 rows to 64 .. 127
   int b = b_first, seq_base = base_first, cur = span_lo, len_b = len_first;
   int64_t start = start_first;
   int seq = 0;                           // granules of this block before the segment
@@ -1193,7 +1197,8 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   d.columns = d.fold ? 4 : d.tiles * d.col_warps * 8;
   d.col_tiles = (cols + d.columns - 1) / d.columns;
   d.spans = dev.sm_count / d.col_tiles;
-  const int gran = eight ? 32 : 16, head_bytes = gran * (eight ? 256 : 512);  // positions of a granule, bytes of a head's part of it
+  d.sub = eight || d.col_warps > 1 ? 2 : 1;
+  const int gran = 16 * d.sub, head_bytes = gran * (eight ? 256 : 512);  // positions of a granule, bytes of a head's part of it
   const int room = dev.max_smem_optin - kMergeBytes - kCtrlBytes - 1024;
   int most = kConsumers / d.col_warps;
   while (p.num_kv_heads % most != 0 || room / (most * head_bytes) < 3) most /= 2;
@@ -1227,9 +1232,9 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   return d;
 }
 
-template <bool EIGHT, int NT, int PARTS, bool PIPED>
+template <bool EIGHT, int NT, int PARTS, int SUB, bool PIPED>
 cudaError_t launch_kernel(const cudaLaunchConfig_t& cfg, const CUtensorMap& map_k, const CUtensorMap& map_v, const DenseArgs& a) {
-  auto kernel = dense_attn_kernel<EIGHT, NT, PARTS, PIPED>;
+  auto kernel = dense_attn_kernel<EIGHT, NT, PARTS, SUB, PIPED>;
   // The kernel's warpgroups redistribute the registers that it was launched with: it may not have been built with fewer.
   static std::atomic<uint64_t> known{0};  // devices on which it has been looked at, and allowed its shared memory
   int dev = 0;
@@ -1251,8 +1256,8 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
                               float* lse, uint32_t* status, unsigned char* scratch, cudaStream_t stream) {
   CUtensorMap map_k, map_v;
   const bool eight = c != nullptr;
-  const bool two_boxes = eight && p.block_table != nullptr && p.block_size == 16;
-  const int box_rows = eight && !two_boxes ? 32 : 16;
+  const bool two_boxes = plan.sub == 2 && p.block_table != nullptr && p.block_size == 16;
+  const int box_rows = two_boxes ? 16 : 16 * plan.sub;
   const int64_t token = eight ? c->kv_token_stride : p.kv_token_stride, head = eight ? c->kv_head_stride : p.kv_head_stride;
   if (!make_map(&map_k, eight ? c->k : p.k_cache, eight, p, token, head, plan.heads, box_rows) ||
       !make_map(&map_v, eight ? c->v : p.v_cache, eight, p, token, head, plan.heads, box_rows))
@@ -1295,7 +1300,7 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   a.lane_slots = plan.lane_slots;
   a.spans = plan.spans;
   while ((1 << a.min_shift) < plan.lanes) ++a.min_shift;
-  a.gran_shift = eight ? 5 : 4;
+  a.gran_shift = plan.sub == 2 ? 5 : 4;
   a.two_boxes = two_boxes;
   a.whole_units = plan.whole_units;
   a.cluster = plan.cluster;
@@ -1316,11 +1321,12 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = plan.cluster > 1 ? 2 : 1;
-  const cudaError_t err = eight ? (plan.tiles == 1 ? launch_kernel<true, 1, 1, false>(cfg, map_k, map_v, a) : launch_kernel<true, 2, 1, false>(cfg, map_k, map_v, a))
-                          : plan.fold           ? launch_kernel<false, 1, 3, false>(cfg, map_k, map_v, a)
-                          : plan.tiles == 1     ? launch_kernel<false, 1, 2, false>(cfg, map_k, map_v, a)
-                          : plan.col_warps <= 2 ? launch_kernel<false, 2, 2, true>(cfg, map_k, map_v, a)
-                                                : launch_kernel<false, 2, 1, true>(cfg, map_k, map_v, a);
+  const cudaError_t err = eight ? (plan.tiles == 1 ? launch_kernel<true, 1, 1, 2, false>(cfg, map_k, map_v, a) : launch_kernel<true, 2, 1, 2, false>(cfg, map_k, map_v, a))
+                          : plan.fold           ? launch_kernel<false, 1, 3, 1, false>(cfg, map_k, map_v, a)
+                          : plan.tiles == 1     ? launch_kernel<false, 1, 2, 1, false>(cfg, map_k, map_v, a)
+                          : plan.col_warps == 1 ? launch_kernel<false, 2, 2, 1, true>(cfg, map_k, map_v, a)
+                          : plan.col_warps == 2 ? launch_kernel<false, 2, 2, 2, false>(cfg, map_k, map_v, a)
+                                                : launch_kernel<false, 2, 1, 2, false>(cfg, map_k, map_v, a);
   if (err != cudaSuccess || plan.whole_units || plan.cluster > 0) return err;
   const int64_t rows = (int64_t)a.num_seqs * a.T * a.num_q_heads;
   // Few rows are cut into parts of 32 outputs, so that all SMs take part and everything is in flight at once (148 stretches are 5 per lane).

@@ -13,6 +13,7 @@ struct DensePlan {
   int heads, lanes;            // KV heads of a block; warps that take granules of one head (and column share) in turn
   int head_groups;             // Hkv / heads
   int slots, lane_slots, slot_bytes;  // the rings, one per lane: a granule's K and V rows of the block's heads in each slot
+  int sub;                     // a granule is so many parts of 16 positions
   int spans;                   // stretches that the list of granules is cut into, at most
   int whole_units;             // 1: a stretch has the units that begin in it, whole (nothing to join)
   int cluster;                 // > 0: each cluster of so many blocks has one unit instead (joined in shared memory)
