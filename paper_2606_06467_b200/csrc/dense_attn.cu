@@ -702,19 +702,6 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       auto finish = [&](auto u_const, auto masked_const, int pos0, float (*x)[NT][4], const uint32_t* vb, uint32_t rows_ok, const uint32_t* codes) {
         constexpr int U = decltype(u_const)::value;
         constexpr bool MASKED = decltype(masked_const)::value;
-        float ev[U];
-        // logits in the log2 domain
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const float kf = EIGHT ? exp2_int(scale_exponent(codes[u] & 255u) - kHeldBack) : a.scale_log2;
-          ev[u] = EIGHT ? (float)scale_exponent(codes[u] >> 8) : 0.f;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              x[u][nt][k] = EIGHT ? x[u][nt][k] * kf * qf[nt][k & 1] : x[u][nt][k] * kf;
-            }
-        }
         auto sees = [&](int t, int row) {  // whether query token t sees row `row` of the granule
           const int here = s.n - T + t, p = pos0 + row;
           return ((rows_ok >> row) & 1u) && p < (a.causal ? here + 1 : s.n) && (a.window == 0 || p > here - a.window);
@@ -726,30 +713,53 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             for (int k = 0; k < 4; ++k)
               if (!sees(tok_of[nt][k & 1], k < 2 ? row_lo : row_hi)) x[0][nt][k] = -INFINITY;
         }
+        // y: logits in the log2 domain (two columns to a register pair) less their columns' references
+        uint64_t y[U][NT][2], kf2[U];
+        float ev[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float kf = EIGHT ? exp2_int(scale_exponent(codes[u] & 255u) - kHeldBack) : a.scale_log2;
+          kf2[u] = pack2(kf, kf);
+          ev[u] = EIGHT ? (float)scale_exponent(codes[u] >> 8) : 0.f;
+        }
+        auto relate = [&](int nt) {
+          const uint64_t less = pack2(-mx[nt][0], -mx[nt][1]);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const uint64_t d = pack2(x[u][nt][2 * r], x[u][nt][2 * r + 1]);
+              y[u][nt][r] = EIGHT ? add2(mul2(mul2(d, kf2[u]), pack2(qf[nt][0], qf[nt][1])), less) : fma2(d, kf2[u], less);
+            }
+        };
         // references: moved only where a weight would leave its range
         bool move = false;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+          relate(nt);
+          float top[2] = {-INFINITY, -INFINITY}, top_e[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float top = -INFINITY, top_e = -INFINITY;
+          for (int u = 0; u < U; ++u) {
+            const float2 lo2 = unpack2(y[u][nt][0]), hi2 = unpack2(y[u][nt][1]);
+            const float most[2] = {fmaxf(lo2.x, hi2.x), fmaxf(lo2.y, hi2.y)};
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-              const float y = fmaxf(x[u][nt][h], x[u][nt][h + 2]) - mx[nt][h];
-              top = fmaxf(top, y);
-              if (EIGHT) top_e = fmaxf(top_e, y + ev[u]);
+            for (int h = 0; h < 2; ++h) {
+              top[h] = fmaxf(top[h], most[h]);
+              if (EIGHT) top_e[h] = fmaxf(top_e[h], most[h] + ev[u]);
             }
-            move = move || top > kLazy || (EIGHT && top_e > m[nt][h] + kLazy);
           }
+          move = move || fmaxf(top[0], top[1]) > kLazy || (EIGHT && (top_e[0] > m[nt][0] + kLazy || top_e[1] > m[nt][1] + kLazy));
+        }
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float tops[U], top = -INFINITY;
 #pragma unroll
               for (int u = 0; u < U; ++u) {
-                tops[u] = fmaxf(x[u][nt][h], x[u][nt][h + 2]);
+                const float kf = unpack2(kf2[u]).x, d = fmaxf(x[u][nt][h], x[u][nt][h + 2]);  // (the factors are positive)
+                tops[u] = EIGHT ? d * kf * qf[nt][h] : d * kf;
 #pragma unroll
                 for (int d = 4; d <= 16; d <<= 1) tops[u] = fmaxf(tops[u], __shfl_xor_sync(0xffffffffu, tops[u], d));
                 top = fmaxf(top, tops[u]);
@@ -769,6 +779,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
               for (int c = 0; c < 8; ++c) { o[nt][c][h] *= alpha; o[nt][c][h + 2] *= alpha; }
             }
+            relate(nt);
+          }
         }
         // weights, as the second product's B operand: column rowq of a tile
         uint32_t pb[U][NT][2], pc[U][NT][2];  // (pc: what the rounding of pb left)
@@ -778,12 +790,14 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              const float y0 = x[u][nt][2 * r] - mx[nt][0], y1 = x[u][nt][2 * r + 1] - mx[nt][1];
-              const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
-              l[nt][0] += p0;
-              l[nt][1] += p1;
+              const float2 e = unpack2(y[u][nt][r]);
+              const float p0 = fast_exp2(e.x), p1 = fast_exp2(e.y);
+              const float2 sum = unpack2(add2(pack2(l[nt][0], l[nt][1]), pack2(p0, p1)));
+              l[nt][0] = sum.x;
+              l[nt][1] = sum.y;
               if (EIGHT) {
-                pb[u][nt][r] = movmatrix_trans(pack_f16x2(fast_exp2(y0 + (ev[u] - m[nt][0])), fast_exp2(y1 + (ev[u] - m[nt][1]))));
+                const float2 w = unpack2(add2(y[u][nt][r], pack2(ev[u] - m[nt][0], ev[u] - m[nt][1])));
+                pb[u][nt][r] = movmatrix_trans(pack_f16x2(fast_exp2(w.x), fast_exp2(w.y)));
               } else {
                 uint32_t first = pack_bf16x2(p0, p1);
                 if (PARTS > 1) {
