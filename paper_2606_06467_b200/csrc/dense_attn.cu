@@ -492,9 +492,9 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           at = list_at();
         }
         if (!__any_sync(0xffffffffu, pending)) break;
+        if (it > 0) __nanosleep(64);  // (the consumers want the issue slots)
         if (it >= kSpinLimit) *abort_flag = 1u;
         if ((it & 63u) == 63u) {
-          __nanosleep(64);
           if (__any_sync(0xffffffffu, *abort_flag != 0u)) {
             alive = false;
             break;
