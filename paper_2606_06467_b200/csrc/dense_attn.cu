@@ -44,7 +44,7 @@ constexpr int kThreads = (kConsumers + kProducers) * 32;
 constexpr int kConsumerRegs = 224, kProducerRegs = 56;  // 8 x 32 x 224 + 4 x 32 x 56 = 64512 = kThreads x 168, what a launch gets
 constexpr int kJoinThreads = 256;
 constexpr int kPerLane = 4;                       // sequences to a lane where every warp adds up the lengths by itself
-constexpr int kMaxSlots = 32;
+constexpr int kMaxSlots = 24;                     // 24 granules of one head are what shared memory holds
 constexpr int kMergeBytes = kConsumers * 8 * kPartialStride * 4;  // a column tile of every consuming warp
 constexpr int kCtrlBytes = 1024;
 constexpr uint32_t kSpinLimit = 1u << 22;  // polls of a barrier: seconds
@@ -64,7 +64,8 @@ struct DenseArgs {
   const int32_t* block_table;
   const uint8_t* ks;
   const uint8_t* vs;
-  int64_t scale_head, num_rows;
+  int64_t scale_head, scale_bytes, num_rows;  // scale_bytes: from the first head's first scale byte to behind the last one's last
+  int head_shift;                             // of the heads of a block
   int scale_shift, block_shift, max_blocks, pages;
   int num_seqs, T, num_q_heads, group, columns_used;  // columns_used: T * group
   int window, causal, max_seq_len;
@@ -210,6 +211,18 @@ struct Folded {
   __device__ __forceinline__ void add(float f, float4 v) {
     acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
   }
+  // One record more, this one's outputs shared with another that has the same head.
+  __device__ __forceinline__ void fold_pair(float4 head, float4 v0, float4 v1, Folded& other) {
+    const float xn = fmaxf(mx, head.x), mold = (mx - xn) + m, mnew = (head.x - xn) + head.z, mn = fmaxf(mold, mnew);
+    const float so = fast_exp2(mold - mn), sn = fast_exp2(mnew - mn);
+    l = fmaf(fast_exp2(head.x - xn), head.y, l * fast_exp2(mx - xn));
+    mx = xn;
+    m = mn;
+    scale(so);
+    other.scale(so);
+    add(sn, v0);
+    other.add(sn, v1);
+  }
   // Up to 8 records, lane i (mod 8) having the i-th one's head (no_head where there is none) and fetch(i) its outputs.
   template <class F>
   __device__ __forceinline__ void fold8(float4 head, int count, F fetch) {
@@ -289,15 +302,19 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   const uint32_t bars = base + ring_bytes + kMergeBytes;
   auto full_bar = [&](int s) { return bars + 16u * s; };
   auto empty_bar = [&](int s) { return bars + 16u * s + 8u; };
-  uint32_t* slot_mask = reinterpret_cast<uint32_t*>(ctrl + 16 * kMaxSlots);  // rows of the slot that exist
-  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 20 * kMaxSlots);
-  int* found = reinterpret_cast<int*>(ctrl + 20 * kMaxSlots + 16);  // first sequence of this block's stretch, granules before it, its length
+  uint32_t* slot_mask = reinterpret_cast<uint32_t*>(ctrl + 16 * kMaxSlots);   // rows of the slot that exist
+  uint32_t* slot_blocks = reinterpret_cast<uint32_t*>(ctrl + 20 * kMaxSlots);  // 8-bit: the low two bits of its parts' scale blocks
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 24 * kMaxSlots);
+  // 8-bit: the words that the parts' scale bytes lie in, [slot][part][K, V][head]: 24 x 16 bytes in all. Before that, of use while the
+  // block looks for its work:
+  uint32_t* slot_scales = reinterpret_cast<uint32_t*>(ctrl + 24 * kMaxSlots + 16);
+  int* found = reinterpret_cast<int*>(ctrl + 24 * kMaxSlots + 16);  // first sequence of this block's stretch, granules before it, its length
   int64_t* found_start = reinterpret_cast<int64_t*>(found + 4);  // .. and its first row
   int* sums = found + 6;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid < a.slots) {
-    mbar_init(full_bar(tid), 1);
+    mbar_init(full_bar(tid), EIGHT ? 1 + 4 * a.heads : 1);  // the rows; lanes' copies of scale bytes
     mbar_init(empty_bar(tid), a.heads * a.col_warps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   } else if (tid == kMaxSlots) {
@@ -395,6 +412,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     base_first = found[1];
     len_first = found[2];
     start_first = *found_start;
+    __syncthreads();  // (the place is free now)
   }
   if (a.cluster > 0) {
     const int g = look_at(a, len_first).gran;
@@ -428,7 +446,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     auto list_at = [&]() { return span_lo + k * a.lanes + ring; };
     int at = list_at();  // the place of this lane's next granule in the list
     // its place: position, head group, page table entry
-    bool valid;
+    bool valid, fresh = false;  // fresh: the first granule of its unit
     int pos, hg, entry, entry2 = -1;
     auto place = [&]() {
       valid = slot < a.slots && at < span_hi;
@@ -447,6 +465,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       } else if (a.cluster == 0 && i == 0 && ct == 0) {
         a.units[(int64_t)b * HG + hg] = make_int2(2 * span + (unit == span_lo ? 0 : 1), Cut(a, total * HG).owner(unit + s.gran - 1));
       }
+      fresh = i == 0;
       pos = s.base + kGran * i;
       entry = entry2 = -1;
       if (paged && valid) {
@@ -466,6 +485,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         const bool ready = pending && mbar_test(empty_bar(slot), parity);
         if (ready) {
           slot_mask[slot] = mask;
+          if (EIGHT) slot_blocks[slot] = (uint32_t)(row32 >> a.scale_shift & 3) | (uint32_t)((a.two_boxes ? row32b : row32 + 16) >> a.scale_shift & 3) << 2;
           const uint32_t bar = full_bar(slot), dst = base + (uint32_t)slot * 2u * half_bytes;
           mbar_expect_tx(bar, 2u * half_bytes);
           if (EIGHT) {
@@ -486,10 +506,48 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           pending = false;
           ++rounds;
         }
+        if (EIGHT) {  // the scale bytes of the granules just issued: 4 lanes each and head, (part, K or V, head)
+          __syncwarp();
+          uint32_t todo = __ballot_sync(0xffffffffu, ready);
+          while (todo != 0u) {
+            uint32_t mine = todo;
+#pragma unroll
+            for (int k = 1; k < 8; ++k) {
+              if (k << (a.head_shift + 2) >= 32) break;
+              todo &= todo - 1u;
+              if (lane >> (a.head_shift + 2) >= k) mine = todo;
+            }
+            todo &= todo - 1u;
+            const int j = max(__ffs(mine) - 1, 0), its = warp - kConsumers + kProducers * j;
+            const int part = lane >> (a.head_shift + 1) & 1, side = lane >> a.head_shift & 1, head = lane & (a.heads - 1);
+            const uint32_t there = __shfl_sync(0xffffffffu, mask, j) >> (16 * part) & 0xffffu;
+            const int first_row = __shfl_sync(0xffffffffu, row32, j), second_row = __shfl_sync(0xffffffffu, row32b, j);
+            const int first_head = __shfl_sync(0xffffffffu, z, j);
+            if (mine != 0u) {
+              if (there != 0u) {
+                const int row = part == 0 ? first_row : a.two_boxes ? second_row : first_row + 16;
+                const int64_t at_byte = (int64_t)(first_head + head) * a.scale_head + (row >> a.scale_shift);
+                const uint8_t* from = side ? a.vs : a.ks;
+                const uint32_t skip = (uint32_t)(reinterpret_cast<uintptr_t>(from + at_byte) & 3u);  // words are copied; not beyond the last byte
+                const int64_t left = a.scale_bytes - at_byte + skip;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(smem_u32(slot_scales + (its << (a.head_shift + 2)) + (lane & (4 * a.heads - 1)))),
+                             "l"(from + at_byte - skip), "r"(left < 4 ? (int)left : 4) : "memory");
+              }
+              asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full_bar(its)) : "memory");
+            }
+          }
+        }
         if (it == 0) {
           place();
           k += a.lane_slots;
           at = list_at();
+          // A unit comes up: its queries on their way to L2 (behind all the rows that are asked for they would take as long as those).
+          for (uint32_t todo = __ballot_sync(0xffffffffu, valid && fresh && rounds >= 0); todo != 0u; todo &= todo - 1u) {
+            const int j = __ffs(todo) - 1;
+            const uint16_t* src = a.q + ((int64_t)__shfl_sync(0xffffffffu, b, j) * a.T * a.num_q_heads + __shfl_sync(0xffffffffu, hg, j) * a.heads * a.group) * 128;
+            for (int t = 0; t < a.T; ++t, src += (int64_t)a.num_q_heads * 128)
+              for (int k64 = lane; k64 < a.heads * a.group * 2; k64 += 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + k64 * 64));
+          }
         }
         if (!__any_sync(0xffffffffu, pending)) break;
         if (it > 0) __nanosleep(64);  // (the consumers want the issue slots)
@@ -544,6 +602,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       if (lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
       if (rounds >= 0)
         for (uint32_t it = 0; it < kSpinLimit && !mbar_test(full_bar(slot), (uint32_t)rounds & 1u); ++it) __nanosleep(64);
+      if (EIGHT) asm volatile("cp.async.wait_all;" ::: "memory");
     }
     return;
   }
@@ -580,7 +639,6 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   }
   const uint32_t upper = half_bytes / (kSub == 2 && a.two_boxes ? 4 : 2);  // from dimensions 0 .. 63 of the bf16 rows to 64 .. 127
   int b = b_first, seq_base = base_first, cur = span_lo, len_b = len_first;
-  int64_t start = start_first;
   int seq = 0;                           // granules of this block before the segment
   const int ring0 = my_lane * a.lane_slots;
   int slot = 0;                          // of this lane's ring: its next granule's, and the parity of that round
@@ -589,8 +647,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   bool more = a.cluster > 0 || cur < span_hi;  // (a cluster's block without granules takes part in the joining)
   while (more && b < a.num_seqs) {
     const Seq s = look_at(a, len_b);
-    const int len_next = b + 1 < a.num_seqs ? a.seq_len[b + 1] : 0;
-    const int64_t start_next = EIGHT && !paged && b + 1 < a.num_seqs ? a.seq_start[b + 1] : 0;
+    int len_next = 0;  // asked for here and not where it is used
+    if (b + 1 < a.num_seqs) asm volatile("ld.global.b32 %0, [%1];" : "=r"(len_next) : "l"(a.seq_len + b + 1));
     for (int hg = a.cluster > 0 ? hg_first : (int)((uint32_t)(cur - seq_base) / (uint32_t)s.gran); hg < HG && more; ++hg) {
       const int unit = seq_base + hg * s.gran;
       const int lo = cur - unit, hi = a.whole_units ? s.gran : min(span_hi - unit, s.gran);
@@ -702,16 +760,16 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       auto finish = [&](auto u_const, auto masked_const, int pos0, float (*x)[NT][4], const uint32_t* vb, uint32_t rows_ok, const uint32_t* codes) {
         constexpr int U = decltype(u_const)::value;
         constexpr bool MASKED = decltype(masked_const)::value;
-        auto sees = [&](int t, int row) {  // whether query token t sees row `row` of the granule
-          const int here = s.n - T + t, p = pos0 + row;
-          return ((rows_ok >> row) & 1u) && p < (a.causal ? here + 1 : s.n) && (a.window == 0 || p > here - a.window);
-        };
         if constexpr (MASKED) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (!sees(tok_of[nt][k & 1], k < 2 ? row_lo : row_hi)) x[0][nt][k] = -INFINITY;
+            for (int h = 0; h < 2; ++h) {  // the column's query token sees `seen` positions from `from` on
+              const int here = s.n - T + tok_of[nt][h], from = a.window ? max(0, here - a.window + 1) : 0;
+              const unsigned seen = (unsigned)max(0, (a.causal ? here + 1 : s.n) - from);
+              if ((unsigned)(pos0 + row_lo - from) >= seen || !(rows_ok >> row_lo & 1u)) x[0][nt][h] = -INFINITY;
+              if ((unsigned)(pos0 + row_hi - from) >= seen || !(rows_ok >> row_hi & 1u)) x[0][nt][2 + h] = -INFINITY;
+            }
         }
         // y: logits in the log2 domain (two columns to a register pair) less their columns' references
         uint64_t y[U][NT][2], kf2[U];
@@ -889,7 +947,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll 1
             for (int t = 0; t < T; ++t) {
               uint32_t one_lo, one_hi;
-              keep([&](int row) { return sees(t, row); }, one_lo, one_hi);
+              const int here = s.n - T + t, to = a.causal ? here + 1 : s.n;
+              keep([&](int row) { return ((rows_ok >> row) & 1u) && pos0 + row < to && (a.window == 0 || pos0 + row > here - a.window); }, one_lo, one_hi);
               second_product(one_lo, one_hi, [&](int u, int c, const uint32_t (&v)[4]) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
@@ -911,8 +970,9 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       const int pos_step = kGran * a.lanes;
       int pos = s.base + kGran * (lo + n - seq);
       const int last_whole = all_to - kGran;  // every query sees all of a granule from all_from to here
-      uint32_t held = 0;  // 8-bit: the scale bytes (K's, V's of either part) of 32 granules of this warp, one per lane
-      int have = 0;       // .. of which this one is
+      // 8-bit: where in their words this head's scale bytes lie, but for the block's number
+      const uint32_t skip_k = EIGHT ? (uint32_t)(reinterpret_cast<uintptr_t>(a.ks) + g * a.scale_head) & 3u : 0u;
+      const uint32_t skip_v = EIGHT ? (uint32_t)(reinterpret_cast<uintptr_t>(a.vs) + g * a.scale_head) & 3u : 0u;
       // With PIPED a granule that every query sees whole has its first product formed while the one before it is finished: `held_x` is that
       // product of the granule whose V rows are at held_vb, in slot held_slot.
       float held_x[kSub][NT][4];
@@ -925,31 +985,6 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       for (; PIPED || n < end; n += a.lanes, pos += pos_step) {
         const bool any = !PIPED || n < end;
         uint32_t codes[kSub] = {};
-        if (EIGHT) {
-          if ((have & 31) == 0) {
-            held = 0x7f7f7f7fu;
-            const int at = pos + pos_step * lane;
-            if (n + a.lanes * lane < end) {
-#pragma unroll
-              for (int u = 0; u < kSub; ++u) {
-                const int p = at + 16 * u;
-                int64_t row = start + p;
-                if (paged) {
-                  const int blk = p < s.n ? a.block_table[(int64_t)b * a.max_blocks + (p >> a.block_shift)] : -1;
-                  row = blk >= 0 && blk < a.pages ? ((int64_t)blk << a.block_shift) + (p & ((1 << a.block_shift) - 1)) : -1;
-                }
-                if (p < s.n && row >= 0 && row < a.num_rows) {
-                  const int64_t from = g * a.scale_head + (row >> a.scale_shift);
-                  held = (held & ~(0xffffu << (16 * u))) | ((uint32_t)a.ks[from] | (uint32_t)a.vs[from] << 8) << (16 * u);
-                }
-              }
-            }
-          }
-          const uint32_t both = __shfl_sync(0xffffffffu, held, have & 31);
-          ++have;
-#pragma unroll
-          for (int u = 0; u < kSub; ++u) codes[u] = both >> (16 * u) & 0xffffu;
-        }
         const int here = ring0 + slot;
         const uint32_t off = (uint32_t)here * 2u * half_bytes;
         uint32_t kb[kSub], vb[kSub];
@@ -963,6 +998,15 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           if (!mbar_wait(full_bar(here), round, abort_flag) && lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
           rows_ok = slot_mask[here];
           if (++slot == a.lane_slots) { slot = 0; round ^= 1u; }
+          if (EIGHT) {
+            const uint32_t blocks = slot_blocks[here];
+            const uint32_t* words = slot_scales + (here << (a.head_shift + 2)) + my_head;
+#pragma unroll
+            for (int u = 0; u < kSub; ++u) {
+              const uint32_t block = blocks >> (2 * u);
+              codes[u] = (words[2 * u * a.heads] >> ((skip_k + block & 3u) * 8u) & 255u) | (words[(2 * u + 1) * a.heads] >> ((skip_v + block & 3u) * 8u) & 255u) << 8;
+            }
+          }
         }
         const bool whole = rows_ok == 0xffffffffu >> (32 - kGran) && pos >= all_from && pos <= last_whole;
         if constexpr (PIPED) {
@@ -1044,31 +1088,44 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           if (rowq == 0) *reinterpret_cast<float4*>(mine + (hcol + h) * kPartialStride + 128) = make_float4(mx[nt][h], l[nt][h], m[nt][h], 0.f);
         }
         together();
+        // the lanes' parts of a column become one: a half warp per column, 8 outputs a lane
         const int cols = min(PARTS == 3 ? 4 : 8, a.columns_used - col0 - nt * 8);
+        const int lane_step = a.heads * a.col_warps * 8 * (kPartialStride / 4);
 #pragma unroll 1
-        for (int c = my_lane; c < cols; c += a.lanes) {
-          const int col = col0 + nt * 8 + c, t = token_of(a, col);
-          Folded f;
-          const float4* part = reinterpret_cast<const float4*>(merge + ((my_head * a.col_warps + my_cw) * 8 + c) * kPartialStride);
-          if (a.lanes == 1) {
-            const float4 head = part[32];
-            f.acc = part[lane];
-            f.mx = head.x; f.l = head.y; f.m = head.z;
-          } else {
-            // the lanes' parts of the column
-            const int stride = a.heads * a.col_warps * 8 * (kPartialStride / 4), who = lane & 7;
-            f.fold8(who < a.lanes ? part[who * stride + 32] : no_head(), a.lanes, [&](int i) { return part[i * stride + lane]; });
+        for (int c = 2 * my_lane + (lane >> 4); c - (lane >> 4) < cols; c += 2 * a.lanes) {
+          if (c >= cols) continue;
+          const int mine_at = ((my_head * a.col_warps + my_cw) * 8 + c) * kPartialStride, quad = 2 * (lane & 15);
+          const float4* part = reinterpret_cast<const float4*>(merge + mine_at);
+          Folded f0, f1;
+          float4 head = part[32], v0 = part[quad], v1 = part[quad + 1];
+          f0.acc = v0;
+          f1.acc = v1;
+          f0.mx = head.x; f0.l = head.y; f0.m = head.z;
+          if (a.lanes > 1) {
+            part += lane_step;
+            head = part[32]; v0 = part[quad]; v1 = part[quad + 1];
           }
-          if (a.cluster > 1) {  // left for the cluster's blocks to join
-            float4* rec = reinterpret_cast<float4*>(merge + ((my_head * a.col_warps + my_cw) * 8 + c) * kPartialStride);
-            rec[lane] = f.acc;
-            if (lane == 0) rec[32] = make_float4(f.mx, f.l, f.m, 0.f);
-          } else if (whole_unit) {
-            f.write(a, ((int64_t)b * T + t) * a.num_q_heads + g * G + (col - t * G), lane);
+#pragma unroll 1
+          for (int i = a.lanes - 1; i > 0; --i) {  // (one part ahead)
+            const float4 of = head, w0 = v0, w1 = v1;
+            if (i > 1) {
+              part += lane_step;
+              head = part[32]; v0 = part[quad]; v1 = part[quad + 1];
+            }
+            f0.fold_pair(of, w0, w1, f1);
+          }
+          f1.mx = f0.mx; f1.l = f0.l; f1.m = f0.m;
+          const int col = col0 + nt * 8 + c, t = token_of(a, col);
+          __syncwarp(0xffffu << (lane & 16));  // (the record may take the first part's place)
+          if (a.cluster > 1 || !whole_unit) {  // left for the cluster's blocks, or the second kernel, to join
+            float4* rec = a.cluster > 1 ? reinterpret_cast<float4*>(merge + mine_at) : record_at(a, (int)blockIdx.x, which, my_head, my_cw * NT * 8 + nt * 8 + c);
+            rec[quad] = f0.acc;
+            rec[quad + 1] = f1.acc;
+            if (quad == 0) rec[32] = make_float4(f0.mx, f0.l, f0.m, 0.f);
           } else {
-            float4* rec = record_at(a, (int)blockIdx.x, which, my_head, my_cw * NT * 8 + nt * 8 + c);
-            __stcg(rec + lane, f.acc);
-            if (lane == 0) __stcg(rec + 32, make_float4(f.mx, f.l, f.m, 0.f));
+            const int64_t item = ((int64_t)b * T + t) * a.num_q_heads + g * G + (col - t * G);
+            f0.write(a, item, quad);
+            f1.write(a, item, quad + 1);
           }
         }
         together();
@@ -1092,7 +1149,6 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     seq_base += s.gran * HG;
     ++b;
     len_b = len_next;
-    start = start_next;
   }
 }
 
@@ -1235,7 +1291,7 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   d.head_groups = p.num_kv_heads / d.heads;
   d.slot_bytes = d.heads * head_bytes;
   d.lane_slots = room / d.slot_bytes;
-  if (d.lane_slots > kMaxSlots) d.lane_slots = kMaxSlots;
+  if (d.lane_slots > kMaxSlots / d.heads) d.lane_slots = kMaxSlots / d.heads;
   d.lane_slots /= d.lanes;  // (three at least)
   d.slots = d.lane_slots * d.lanes;
   d.smem_bytes = (size_t)d.slots * d.slot_bytes + kMergeBytes + kCtrlBytes + 1024;
@@ -1291,6 +1347,7 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
     a.vs = static_cast<const uint8_t*>(c->v_scale);
     a.scale_head = c->scale_head_stride;
     while ((1 << a.scale_shift) < c->scale_block) ++a.scale_shift;
+    a.scale_bytes = (p.num_kv_heads - 1) * c->scale_head_stride + ((p.num_cache_rows - 1) >> a.scale_shift) + 1;
   }
   a.num_rows = p.num_cache_rows;
   while (p.block_table != nullptr && (1 << a.block_shift) < p.block_size) ++a.block_shift;
@@ -1307,6 +1364,7 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   a.columns = plan.columns;
   a.col_tiles = plan.col_tiles;
   a.heads = plan.heads;
+  while ((1 << a.head_shift) < plan.heads) ++a.head_shift;
   a.lanes = plan.lanes;
   a.col_warps = plan.col_warps;
   a.head_groups = plan.head_groups;
