@@ -3,30 +3,47 @@
 //   x_s = sm_scale q . K_s,   O = sum_s exp(x_s) V_s / sum_s exp(x_s)   over the positions that a query sees
 //
 // The T queries of a sequence and the query heads of a KV head's group are columns of one product, so that a row of the cache
-// is read once for all of them: with up to about 64 columns the launch is bound by HBM.
+// is read once for all of them: with up to about 16 columns the launch is bound by HBM.
 //
-// Work. A granule is 16 consecutive positions (starting on a multiple of 16, so that it lies in one page and one scale block) of
-// `heads` KV heads. The granules of all (sequence, head group) units form one list, sequence after sequence; its length is known on the
-// device only, where every block adds up the lengths and takes an even stretch of the list, whatever the sequences' lengths are. Four
-// warps fetch granules into rings by tiled bulk copies (one for K, one for V: 16 rows of every head, 128-byte swizzle); eight
-// warps consume them, each with one head's rows: `lanes` warps take a head's granules in turn, `col_warps` share a head's query columns.
+// Work. A granule is 16 or 32 consecutive positions, starting on a multiple of that, of `heads` KV heads; its 16-row parts lie in one
+// page and one scale block each. The granules of all (sequence, head group) units form one list, sequence after sequence; its length is
+// known on the device only, where every block adds up the lengths and takes an even stretch of the list, whatever the sequences' lengths
+// are (or a unit's even share, with the cluster that has the unit, or whole units: make_dense_plan). Four warps fetch granules into rings by tiled bulk
+// copies (one for K, one for V: the rows of every head, 128-byte swizzle); eight warps consume them, each with one head's rows: `lanes`
+// warps take a head's granules in turn, `col_warps` share a head's query columns. A block that holds several heads reads whole token rows,
+// 16 or 32 at a time: what DRAM likes best. Every consuming lane has a ring of its own, so that a slot's rounds are waited for by the same
+// warps; a fetching warp's lane has one slot, and waits for it, looks up its next page and issues its copies beside the others.
 // Products are formed transposed, tokens along M of warp-level instructions:
 //   S^T[16 tokens x 8 columns] = K Q^T,   O^T[128 x 8 columns] += V^T P^T
-// A block that holds several heads reads whole token rows, 16 at a time: what DRAM likes best.
+// Up to 16 columns that is enough to keep up with HBM. Beyond, a block's warps divide the columns, and the instruction rate decides: 64 columns run
+// at 0.23 PFLOP/s over bf16 rows, 0.20 over codes, which every column share converts for itself.
 //
 // Softmax. One pass, in the log2 domain, relative to a reference per column that moves only when a weight would exceed 2^8 (one
 // vote per granule, no reduction over its tokens otherwise). Weights are rounded to what the matrix instruction takes beside V. bf16: two
 // parts of 8 bits each (p and what its rounding left) where that costs nothing, with up to 32 columns: the error of a single part is as
 // large as the output's own rounding; up to 4 columns are held twice and the second copy takes the second parts. 8-bit caches: f16,
 // 2^-11 of each weight. Denominators are sums of the unrounded weights in fp32.
+// Granules that some query sees in part only run a second instance of the step: positions out of sight get logits of -inf, and V rows that nobody sees
+// are taken as zeros (a weight of 0 times a NaN is none). Blocks in which a sequence ends pay for it, and for an epilogue and
+// queries in the middle of their stretch, with code that comes from memory: about 8 us over 8-bit caches, of which the next queries' way to L2 ahead of
+// time and two columns of the epilogue at a time took off 4.
 //
-// 8-bit caches. Codes convert to f16 exactly; the scale exponents ek, ev are the same for all of a granule, so that they are one number
+// 8-bit caches. Codes convert to f16 exactly; the scale exponents ek, ev are the same for all of a 16-row part, so that they are one number
 // per warp: x = (d 2^(ek - 22)) qf with qf = 2^22 sm_scale / (the power of two that q was scaled by). As in the sparse attention,
-// numerators have a reference of their own, m near the largest x - mx + ev, and 2^m meets the finished quotient.
+// numerators have a reference of their own, m near the largest x - mx + ev, and 2^m meets the finished quotient. Scale bytes come with their rows:
+// the fetching warp copies the words that they lie in, and the slot's barrier counts those copies (fetched by the consumers, 32 granules at a
+// time, they held up whoever began a sequence: 24 ragged sequences of up to 32768 tokens, 15 columns, 103 us, now 85).
 //
 // Joining. A unit that lies in one stretch is finished by its block. Of the others every block leaves one record per column (128
 // unnormalised outputs, reference, sum, in fp32), and a second kernel, whose launch overlaps the first one's end, joins a row's records in
-// the order of the stretches: results do not depend on timing.
+// the order of the stretches; a cluster's blocks join theirs in shared memory, in the order of their ranks. Results do not depend on timing.
+//
+// Measured (HBM's measured rate 6.55 TB/s). 16 sequences of 32768 tokens, 32 / 8 heads: bf16 315 us, 6.8 TB/s; 8-bit 168 us, 6.4 TB/s. 24 ragged ones up to
+// 32768 tokens in pages of 16 rows: 4 tokens of 32 / 8 heads, bf16, 260 us, 6.4 TB/s; 3 tokens of 20 / 4, 8-bit, 85 us, 4.9 TB/s. The last 512 tokens of
+// 64 sequences, 20 / 4 heads: 17.0 us, 3.9 TB/s (a launch's start, 4 us of one-off code, and its joining do not overlap the reading). One
+// sequence of 777 tokens and one KV head: 6.8 us, of one of 131072 tokens and 8 heads: 88 us, 6.1 TB/s.
+// Slower: granules of 16 rows fetched as 16-byte copies by the fetching warps (one KV head, 64 x 4096 tokens, 8-bit: 43 us for 22.7; bf16 45 for
+// 38.5); sixteen consuming warps of one column tile each instead of eight of two (8-bit draft 151 us for 110 at that time).
 #include <cuda.h>
 
 #include <atomic>
@@ -284,9 +301,10 @@ __device__ __forceinline__ float4* record_at(const DenseArgs& a, int block, int 
 }
 
 // ---- the kernel --------------------------------------------------------------------------------------------------------
-// EIGHT: an 8-bit cache. NT: column tiles per warp. PARTS (bf16): 1, the weights' rounding is all there is; 2, a second product takes
-// what it left; 3 (NT = 1, up to 4 columns), columns 4 .. 7 repeat the first four and take it. SUB: 16-row parts of a granule. PIPED (SUB = 1): a
-// granule's first product is formed while the one before it is finished.
+// EIGHT: an 8-bit cache. NT: column tiles per warp (two where there are more than 8 columns: a fragment of the cache feeds both).
+// PARTS (bf16): 1, the weights' rounding is all there is; 2, a second product takes what it left; 3 (NT = 1, up to 4 columns), columns 4 .. 7
+// repeat the first four and take it. SUB: 16-row parts of a granule. PIPED (SUB = 1): a granule's first product is formed while the one before it is
+// finished.
 template <bool EIGHT, int NT, int PARTS, int SUB, bool PIPED>
 __global__ void __launch_bounds__(kThreads, 1)
 dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ DenseArgs a) {
@@ -475,7 +493,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       }
     };
     uint32_t parity = 0;                      // of the round that is waited for
-    int row32 = 0, row32b = 0, z = 0, rounds = -1;  // row (of its second half, where that is apart) and head of the granule that waits for its slot; rounds before this lane's last one
+    int row32 = 0, row32b = 0, z = 0;         // row (of its second half, where that is apart) and head of the granule that waits for its slot
+    int rounds = -1;                          // .. and the number of this lane's last round
     uint32_t mask = 0u;                       // .. and what of it exists
     bool pending = false, alive = true;
     while (true) {
@@ -530,8 +549,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 const uint8_t* from = side ? a.vs : a.ks;
                 const uint32_t skip = (uint32_t)(reinterpret_cast<uintptr_t>(from + at_byte) & 3u);  // words are copied; not beyond the last byte
                 const int64_t left = a.scale_bytes - at_byte + skip;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(smem_u32(slot_scales + (its << (a.head_shift + 2)) + (lane & (4 * a.heads - 1)))),
-                             "l"(from + at_byte - skip), "r"(left < 4 ? (int)left : 4) : "memory");
+                const uint32_t dst = smem_u32(slot_scales + (its << (a.head_shift + 2)) + (lane & (4 * a.heads - 1)));
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(from + at_byte - skip), "r"(left < 4 ? (int)left : 4) : "memory");
               }
               asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full_bar(its)) : "memory");
             }
@@ -1004,7 +1023,9 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
             for (int u = 0; u < kSub; ++u) {
               const uint32_t block = blocks >> (2 * u);
-              codes[u] = (words[2 * u * a.heads] >> ((skip_k + block & 3u) * 8u) & 255u) | (words[(2 * u + 1) * a.heads] >> ((skip_v + block & 3u) * 8u) & 255u) << 8;
+              const uint32_t k_byte = words[2 * u * a.heads] >> (((skip_k + block) & 3u) * 8u) & 255u;
+              const uint32_t v_byte = words[(2 * u + 1) * a.heads] >> (((skip_v + block) & 3u) * 8u) & 255u;
+              codes[u] = k_byte | v_byte << 8;
             }
           }
         }
@@ -1255,7 +1276,8 @@ bool make_map(CUtensorMap* map, const void* ptr, bool eight, const clsa_params& 
 // A cluster of blocks per unit, where all fit on the GPU at once: joined in shared memory, but the longest sequence decides. Whole units:
 // nothing to join, the longest stretch of them decides. Chosen by an estimate from the longest sequence that the call allows: a block gets its
 // share of HBM, but no more than kBlockRate; the second kernel costs 3.5 us, a cluster's joining 0.8; and the lengths are taken to be 0.7
-// of the longest one on average, which only the first way profits from.
+// of the longest one on average, which only the first way profits from. Stretches against a cluster per unit: one sequence of 777 tokens 8.5 and
+// 6.5 us, one of 8192 19.3 and 13.8, the last 512 tokens of 64 sequences 23.8 and 17.5; they win from about 16 MB on (16 x 32768 tokens).
 constexpr double kRate = 6500e3, kBlockRate = 100e3;  // bytes per us
 
 DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const DeviceInfo& dev) {
@@ -1267,6 +1289,9 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   d.columns = d.fold ? 4 : d.tiles * d.col_warps * 8;
   d.col_tiles = (cols + d.columns - 1) / d.columns;
   d.spans = dev.sm_count / d.col_tiles;
+  // Granules of 32 positions where the step's instructions bound it: half the votes, waits and barriers (bf16, 16 sequences of 8192 tokens, 32 and 64
+  // columns: 122 and 178 us with 16, 103 and 146 with 32; the 8-bit draft case 110 and 105). With fewer columns bf16 rows keep to 16, in half the time
+  // from the first row to the last one's end; 9 to 16 columns form a granule's first product beside the one before it instead (284 us, now 260).
   d.sub = eight || d.col_warps > 1 ? 2 : 1;
   const int gran = 16 * d.sub, head_bytes = gran * (eight ? 256 : 512);  // positions of a granule, bytes of a head's part of it
   const int room = dev.max_smem_optin - kMergeBytes - kCtrlBytes - 1024;

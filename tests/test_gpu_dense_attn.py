@@ -246,6 +246,22 @@ def test_scales_far_apart():
     p.check()
 
 
+@pytest.mark.parametrize("heads", [(8, 1), (20, 4), (8, 8)], ids=str)
+@pytest.mark.parametrize("offset,gap,page", [(0, 0, 0), (1, 2, 0), (2, 1, 16), (3, 4, 16), (3, 0, 64), (1, 3, 32)])
+def test_scale_bytes_at_any_address(offset, gap, page, heads):
+    """Heads' scale bytes at every place of a 4-byte word, the last head's last one at the end of its memory."""
+    w = Problem([1, 17, 333, 2049, 640], *heads, T=2, eight=True, page=page, block=16, seed=offset + 5)
+    for name in ("ks", "vs"):
+        of = getattr(w, name)
+        stride = of.shape[1] + gap
+        room = torch.full((offset + (heads[1] - 1) * stride + of.shape[1],), 255, dtype=torch.uint8, device=DEV)
+        there = room.as_strided(of.shape, (stride, 1), offset)
+        there.copy_(of)
+        setattr(w, name, there)
+    w.make()
+    w.check()
+
+
 @pytest.mark.parametrize("eight", [False, True], ids=["bf16", "e4m3"])
 def test_bad_pages_and_rows(eight):
     p = Problem([200, 90, 33], 8, 2, T=2, causal=1, eight=eight, page=16, seed=13)
