@@ -7,8 +7,8 @@
 //
 // Work. A granule is 16 or 32 consecutive positions, starting on a multiple of that, of `heads` KV heads; its 16-row parts lie in one
 // page and one scale block each. The granules of all (sequence, head group) units form one list, sequence after sequence; its length is
-// known on the device only, where every block adds up the lengths and takes an even stretch of the list, whatever the sequences' lengths
-// are (or a unit's even share, with the cluster that has the unit, or whole units: make_dense_plan). Four warps fetch granules into rings by tiled bulk
+// known on the device only, where every block adds up the lengths and takes an even stretch of the list (to which a unit's beginning and end
+// count, too), whatever the sequences' lengths are (or a unit's even share, with the cluster that has the unit, or whole units: make_dense_plan). Four warps fetch granules into rings by tiled bulk
 // copies (one for K, one for V: the rows of every head, 128-byte swizzle); eight warps consume them, each with one head's rows: `lanes`
 // warps take a head's granules in turn, `col_warps` share a head's query columns. A block that holds several heads reads whole token rows,
 // 16 or 32 at a time: what DRAM likes best. Every consuming lane has a ring of its own, so that a slot's rounds are waited for by the same
@@ -25,21 +25,20 @@
 // 2^-11 of each weight. Denominators are sums of the unrounded weights in fp32.
 // Granules that some query sees in part only run a second instance of the step: positions out of sight get logits of -inf, and V rows that nobody sees
 // are taken as zeros (a weight of 0 times a NaN is none). Blocks in which a sequence ends pay for it, and for an epilogue and
-// queries in the middle of their stretch, with code that comes from memory: about 8 us over 8-bit caches, of which the next queries' way to L2 ahead of
-// time and two columns of the epilogue at a time took off 4.
+// queries in the middle of their stretch, with code that comes from memory: about 10 us, which the cut of the list makes up for.
 //
 // 8-bit caches. Codes convert to f16 exactly; the scale exponents ek, ev are the same for all of a 16-row part, so that they are one number
 // per warp: x = (d 2^(ek - 22)) qf with qf = 2^22 sm_scale / (the power of two that q was scaled by). As in the sparse attention,
 // numerators have a reference of their own, m near the largest x - mx + ev, and 2^m meets the finished quotient. Scale bytes come with their rows:
 // the fetching warp copies the words that they lie in, and the slot's barrier counts those copies (fetched by the consumers, 32 granules at a
-// time, they held up whoever began a sequence: 24 ragged sequences of up to 32768 tokens, 15 columns, 103 us, now 85).
+// time, they held up whoever began a sequence: 24 ragged sequences of up to 32768 tokens, 15 columns, 103 us then, 85 since).
 //
 // Joining. A unit that lies in one stretch is finished by its block. Of the others every block leaves one record per column (128
 // unnormalised outputs, reference, sum, in fp32), and a second kernel, whose launch overlaps the first one's end, joins a row's records in
 // the order of the stretches; a cluster's blocks join theirs in shared memory, in the order of their ranks. Results do not depend on timing.
 //
 // Measured (HBM's measured rate 6.55 TB/s). 16 sequences of 32768 tokens, 32 / 8 heads: bf16 315 us, 6.8 TB/s; 8-bit 168 us, 6.4 TB/s. 24 ragged ones up to
-// 32768 tokens in pages of 16 rows: 4 tokens of 32 / 8 heads, bf16, 260 us, 6.4 TB/s; 3 tokens of 20 / 4, 8-bit, 85 us, 4.9 TB/s. The last 512 tokens of
+// 32768 tokens in pages of 16 rows: 4 tokens of 32 / 8 heads, bf16, 260 us, 6.4 TB/s; 3 tokens of 20 / 4, 8-bit, 79 us, 5.3 TB/s. The last 512 tokens of
 // 64 sequences, 20 / 4 heads: 17.0 us, 3.9 TB/s (a launch's start, 4 us of one-off code, and its joining do not overlap the reading). One
 // sequence of 777 tokens and one KV head: 6.8 us, of one of 131072 tokens and 8 heads: 88 us, 6.1 TB/s.
 // Slower: granules of 16 rows fetched as 16-byte copies by the fetching warps (one KV head, 64 x 4096 tokens, 8-bit: 43 us for 22.7; bf16 45 for
@@ -92,6 +91,7 @@ struct DenseArgs {
   int whole_units;  // 1: a stretch has the units that begin in it, whole
   int cluster;      // > 0: each cluster of so many blocks (2^cluster_shift) has one unit, cut evenly; 0: stretches of the list
   int cluster_shift;
+  int pad;          // granules that a unit's beginning and end count for, where the list is cut
   uint32_t group_inv;  // ceil(2^16 / group): c / group = c * group_inv >> 16 for the columns, of which there are at most 512
   float scale_log2;
 };
@@ -327,8 +327,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   // block looks for its work:
   uint32_t* slot_scales = reinterpret_cast<uint32_t*>(ctrl + 24 * kMaxSlots + 16);
   int* found = reinterpret_cast<int*>(ctrl + 24 * kMaxSlots + 16);  // first sequence of this block's stretch, granules before it, its length
-  int64_t* found_start = reinterpret_cast<int64_t*>(found + 4);  // .. and its first row
-  int* sums = found + 6;
+  int64_t* found_start = reinterpret_cast<int64_t*>(found + 6);  // .. and its first row
+  int* sums = found + 8;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid < a.slots) {
@@ -344,7 +344,13 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind this grid's own wait, as in every kernel of the library
 
-  // This block's stretch of the list: the first sequence that it reaches into (its number, the granules before it, length and first row).
+  // This block's stretch of the list: the first sequence that it reaches into (its number, the granules before it, length and first row), and
+  // its granules, span_lo .. span_hi - 1. The list is cut with a.pad places more behind every unit; `place_of` takes a place of that list to the
+  // granule there, or the next one.
+  auto place_of = [&](int at, int list_base, int granule_base, int gran) {
+    const int off = at - list_base, unit = (int)((uint32_t)off / (uint32_t)(gran + a.pad));
+    return granule_base + unit * gran + min(off - unit * (gran + a.pad), gran);
+  };
   const int HG = a.head_groups;
   // Blocks of clusters are (rank, head group, sequence and column tile), of stretches (stretch and column tile).
   const int rank = (int)blockIdx.x, tiled = a.cluster > 0 ? (int)blockIdx.z : (int)blockIdx.x;
@@ -358,77 +364,88 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     hg_first = (int)blockIdx.y;
     len_first = a.seq_len[b_first];
     start_first = paged ? 0 : a.seq_start[b_first];
-  } else if (a.num_seqs <= 32 * kPerLane) {  // every warp by itself, kPerLane sequences to a lane
-    int len[kPerLane], gran[kPerLane], mine = 0;
-    int64_t begin[kPerLane];
-#pragma unroll
-    for (int k = 0; k < kPerLane; ++k) {
-      const int i = lane * kPerLane + k;
-      len[k] = i < a.num_seqs ? a.seq_len[i] : 0;
-      begin[k] = i < a.num_seqs && !paged ? a.seq_start[i] : 0;
-    }
-#pragma unroll
-    for (int k = 0; k < kPerLane; ++k) {
-      gran[k] = lane * kPerLane + k < a.num_seqs ? look_at(a, len[k]).gran : 0;
-      mine += gran[k];
-    }
-    int incl = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += o;
-    }
-    total = __shfl_sync(0xffffffffu, incl, 31);
-    const int from = Cut(a, total * HG).begin(span);
-    int lo = (incl - mine) * HG;
-    b_first = lane * kPerLane;
-    base_first = lo;
-    len_first = len[0];
-    start_first = begin[0];
-#pragma unroll
-    for (int k = 1; k < kPerLane; ++k) {
-      lo += gran[k - 1] * HG;
-      if (gran[k] > 0 && lo <= from) { b_first = lane * kPerLane + k; base_first = lo; len_first = len[k]; start_first = begin[k]; }
-    }
-    const uint32_t here = __ballot_sync(0xffffffffu, (incl - mine) * HG <= from && from < incl * HG);
-    const int who = here != 0u ? __ffs(here) - 1 : 0;  // (none: a stretch beyond the last one)
-    b_first = __shfl_sync(0xffffffffu, b_first, who);
-    base_first = __shfl_sync(0xffffffffu, base_first, who);
-    len_first = __shfl_sync(0xffffffffu, len_first, who);
-    start_first = __shfl_sync(0xffffffffu, start_first, who);
   } else {
-    int len = 0, gran = 0, before = 0;
-    int64_t begin = 0;
-    auto read = [&](int i) {
-      gran = 0;
-      if (i >= a.num_seqs) return;
-      len = a.seq_len[i];
-      if (!paged) begin = a.seq_start[i];
-      gran = look_at(a, len).gran;
-    };
-    total = 0;
-    for (int b0 = 0; b0 < a.num_seqs; b0 += kThreads) {
-      read(b0 + tid);
-      total += block_scan<kThreads>(gran, sums, before);
-    }
-    const int from = Cut(a, total * HG).begin(span);
-    for (int b0 = 0, run = 0; b0 < a.num_seqs; b0 += kThreads) {
-      read(b0 + tid);
-      const int sum = block_scan<kThreads>(gran, sums, before);
-      const int lo = (run + before) * HG;
-      if (lo <= from && from < lo + gran * HG) {
-        found[0] = b0 + tid;
-        found[1] = lo;
-        found[2] = len;
-        *found_start = begin;
+    if (a.num_seqs > 32 * kPerLane) {
+      int len = 0, gran = 0, before = 0;
+      int64_t begin = 0;
+      auto read = [&](int i) {
+        gran = 0;
+        if (i >= a.num_seqs) return;
+        len = a.seq_len[i];
+        if (!paged) begin = a.seq_start[i];
+        gran = look_at(a, len).gran;
+      };
+      for (int b0 = 0; b0 < a.num_seqs; b0 += kThreads) {
+        read(b0 + tid);
+        total += block_scan<kThreads>(gran, sums, before);
       }
-      run += sum;
-      if (run * HG > from) break;
+      total = total * HG + (a.num_seqs * HG - 1) * a.pad;  // (nothing behind the last one)
+      const Cut cut(a, total);
+      const int from = cut.begin(span), to = cut.begin(span + 1), pad = a.pad * HG;
+      if (tid == 0) { found[3] = total; found[5] = total; }
+      for (int b0 = 0, run = 0; b0 < a.num_seqs; b0 += kThreads) {
+        read(b0 + tid);
+        const int sum = block_scan<kThreads>(gran, sums, before);
+        const int lo = (run + before) * HG, list = lo + (b0 + tid) * pad, list_end = list + gran * HG + pad;
+        if (gran > 0 && list <= from && from < list_end) {
+          found[0] = b0 + tid;
+          found[1] = lo;
+          found[2] = len;
+          found[4] = place_of(from, list, lo, gran);
+          *found_start = begin;
+        }
+        if (gran > 0 && list <= to && to < list_end) found[3] = place_of(to, list, lo, gran);
+        run += sum;
+        if (run * HG + min(a.num_seqs, b0 + kThreads) * pad > to) break;
+      }
+    } else if (warp == 0) {  // kPerLane sequences to a lane
+      int len[kPerLane], gran[kPerLane], mine = 0;
+      int64_t begin[kPerLane];
+#pragma unroll
+      for (int k = 0; k < kPerLane; ++k) {
+        const int i = lane * kPerLane + k;
+        len[k] = i < a.num_seqs ? a.seq_len[i] : 0;
+        begin[k] = i < a.num_seqs && !paged ? a.seq_start[i] : 0;
+      }
+#pragma unroll
+      for (int k = 0; k < kPerLane; ++k) {
+        gran[k] = lane * kPerLane + k < a.num_seqs ? look_at(a, len[k]).gran : 0;
+        mine += gran[k];
+      }
+      int incl = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+      }
+      const int all = __shfl_sync(0xffffffffu, incl, 31) * HG + (a.num_seqs * HG - 1) * a.pad;  // (nothing behind the last one)
+      const Cut cut(a, all);
+      const int from = cut.begin(span), to = cut.begin(span + 1), pad = a.pad * HG;
+      if (lane == 0) { found[3] = all; found[5] = all; }
+      __syncwarp();
+      int lo = (incl - mine) * HG, list = lo + lane * kPerLane * pad;
+#pragma unroll
+      for (int k = 0; k < kPerLane; ++k) {
+        const int list_end = list + gran[k] * HG + pad;
+        if (gran[k] > 0 && list <= from && from < list_end) {
+          found[0] = lane * kPerLane + k;
+          found[1] = lo;
+          found[2] = len[k];
+          found[4] = place_of(from, list, lo, gran[k]);
+          *found_start = begin[k];
+        }
+        if (gran[k] > 0 && list <= to && to < list_end) found[3] = place_of(to, list, lo, gran[k]);
+        lo += gran[k] * HG;
+        list = list_end;
+      }
     }
     __syncthreads();
+    total = found[5];
     b_first = found[0];
     base_first = found[1];
     len_first = found[2];
+    span_hi = found[3];  // (all of it, unless another stretch begins somewhere)
+    span_lo = found[4];
     start_first = *found_start;
     __syncthreads();  // (the place is free now)
   }
@@ -437,11 +454,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     base_first = -hg_first * g;
     span_lo = g * rank >> a.cluster_shift;
     span_hi = g * (rank + 1) >> a.cluster_shift;
-  } else {
-    const Cut cut(a, total * HG);
-    if (span >= cut.spans) return;
-    span_lo = cut.begin(span);
-    span_hi = cut.begin(span + 1);
+  } else if (span >= Cut(a, total).spans) {
+    return;
   }
   if (a.whole_units) {  // the units that begin in the stretch, whole
     const int g = look_at(a, len_first).gran;
@@ -481,7 +495,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       if (a.whole_units) {
         valid = unit < span_hi;
       } else if (a.cluster == 0 && i == 0 && ct == 0) {
-        a.units[(int64_t)b * HG + hg] = make_int2(2 * span + (unit == span_lo ? 0 : 1), Cut(a, total * HG).owner(unit + s.gran - 1));
+        a.units[(int64_t)b * HG + hg] = make_int2(2 * span + (unit == span_lo ? 0 : 1), Cut(a, total).owner(unit + s.gran - 1 + (b * HG + hg) * a.pad));
       }
       fresh = i == 0;
       pos = s.base + kGran * i;
@@ -1279,6 +1293,10 @@ bool make_map(CUtensorMap* map, const void* ptr, bool eight, const clsa_params& 
 // of the longest one on average, which only the first way profits from. Stretches against a cluster per unit: one sequence of 777 tokens 8.5 and
 // 6.5 us, one of 8192 19.3 and 13.8, the last 512 tokens of 64 sequences 23.8 and 17.5; they win from about 16 MB on (16 x 32768 tokens).
 constexpr double kRate = 6500e3, kBlockRate = 100e3;  // bytes per us
+// Where the list is cut, a unit's beginning and end count for what they take a block (other queries, a granule that some queries see in part, an
+// epilogue: kUnitCost), in granules at the rate of HBM or of the products. Nothing for them, 10 us for them: the 8-bit draft case 85 and 79 us, 8 drafted
+// tokens over bf16 103 and 100, 16 sequences of 16 heads' one 38.6 and 37.
+constexpr double kUnitCost = 10.0;
 
 DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const DeviceInfo& dev) {
   DensePlan d = {};
@@ -1313,6 +1331,12 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
     if (units > dev.sm_count && cost < best) { best = cost; d.heads = h; d.cluster = 0; d.whole_units = 1; }
   }
   d.lanes = kConsumers / (d.col_warps * d.heads);
+  if (d.cluster == 0 && !d.whole_units) {
+    const double products = (eight ? 100e6 : 240e6) / d.columns;  // bytes per us that they keep up with, as measured with 32 and 64 columns
+    d.pad = (int)(kUnitCost * (kRate < products ? kRate : products) / dev.sm_count / (d.heads * head_bytes));
+    const int64_t units = (int64_t)p.num_seqs * (p.num_kv_heads / d.heads);
+    while (units * d.pad > 1 << 28) d.pad /= 2;  // (places are numbered with 32 bits)
+  }
   d.head_groups = p.num_kv_heads / d.heads;
   d.slot_bytes = d.heads * head_bytes;
   d.lane_slots = room / d.slot_bytes;
@@ -1401,6 +1425,7 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   a.two_boxes = two_boxes;
   a.whole_units = plan.whole_units;
   a.cluster = plan.cluster;
+  a.pad = plan.pad;
   while ((1 << a.cluster_shift) < plan.cluster) ++a.cluster_shift;
   a.group_inv = (65536u + (uint32_t)a.group - 1u) / (uint32_t)a.group;
   a.scale_log2 = p.sm_scale * kLog2e;
