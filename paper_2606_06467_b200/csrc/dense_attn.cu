@@ -92,6 +92,7 @@ struct DenseArgs {
   int cluster;      // > 0: each cluster of so many blocks (2^cluster_shift) has one unit, cut evenly; 0: stretches of the list
   int cluster_shift;
   int pad;          // granules that a unit's beginning and end count for, where the list is cut
+  uint32_t ring_inv;   // ceil(2^16 / lane_slots): slot / lane_slots = slot * ring_inv >> 16 for slots below 128
   uint32_t group_inv;  // ceil(2^16 / group): c / group = c * group_inv >> 16 for the columns, of which there are at most 512
   float scale_log2;
 };
@@ -473,8 +474,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     // The ring is one of lane_slots slots for each consuming lane, so that a slot's granules are waited for by the same warps in every round
     // (a warp that waited for a round while the one before had not landed yet would take the parity of the one before that). Granules
     // go to the lanes in turn: slot s holds granules number k = s % lane_slots, + lane_slots, .. of its lane.
-    int ring = 0, k = slot;
-    while (k >= a.lane_slots) { k -= a.lane_slots; ++ring; }
+    const int ring = (int)((uint32_t)slot * a.ring_inv >> 16);
+    int k = slot - ring * a.lane_slots;
     auto list_at = [&]() { return span_lo + k * a.lanes + ring; };
     int at = list_at();  // the place of this lane's next granule in the list
     // its place: position, head group, page table entry
@@ -1419,6 +1420,7 @@ cudaError_t launch_dense_attn(const clsa_params& p, const clsa_cache8* c, int wi
   a.head_groups = plan.head_groups;
   a.slots = plan.slots;
   a.lane_slots = plan.lane_slots;
+  a.ring_inv = (65536u + (uint32_t)plan.lane_slots - 1u) / (uint32_t)plan.lane_slots;
   a.spans = plan.spans;
   while ((1 << a.min_shift) < plan.lanes) ++a.min_shift;
   a.gran_shift = plan.sub == 2 ? 5 : 4;
