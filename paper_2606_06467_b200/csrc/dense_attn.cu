@@ -35,14 +35,15 @@
 //
 // Joining. A unit that lies in one stretch is finished by its block. Of the others every block leaves one record per column (128
 // unnormalised outputs, reference, sum, in fp32), and a second kernel, whose launch overlaps the first one's end, joins a row's records in
-// the order of the stretches; a cluster's blocks join theirs in shared memory, in the order of their ranks. Results do not depend on timing.
+// the order of the stretches. A cluster's blocks send each column's record to the block that finishes it, which joins them in the order of
+// their ranks. Results do not depend on timing.
 //
 // Measured (HBM's measured rate 6.55 TB/s). 16 sequences of 32768 tokens, 32 / 8 heads: bf16 315 us, 6.8 TB/s; 8-bit 168 us, 6.4 TB/s. 24 ragged ones up to
 // 32768 tokens in pages of 16 rows: 4 tokens of 32 / 8 heads, bf16, 260 us, 6.4 TB/s; 3 tokens of 20 / 4, 8-bit, 79 us, 5.3 TB/s. The last 512 tokens of
-// 64 sequences, 20 / 4 heads: 17.0 us, 3.9 TB/s (a launch's start, 4 us of one-off code, and its joining do not overlap the reading). One
-// sequence of 777 tokens and one KV head: 6.8 us, of one of 131072 tokens and 8 heads: 88 us, 6.1 TB/s.
-// Slower: granules of 16 rows fetched as 16-byte copies by the fetching warps (one KV head, 64 x 4096 tokens, 8-bit: 43 us for 22.7; bf16 45 for
-// 38.5); sixteen consuming warps of one column tile each instead of eight of two (8-bit draft 151 us for 110 at that time).
+// 64 sequences, 20 / 4 heads: 15.8 us, 4.2 TB/s (a launch's start, one-off code and the joining do not overlap the reading). One sequence
+// of 777 tokens and one KV head: 4.9 us, of 8192 tokens and 8 heads 11.4 us, of 131072 tokens 88 us, 6.1 TB/s.
+// Slower: granules of 16 rows fetched as 16-byte copies by the fetching warps (one KV head, 64 x 4096 tokens, 8-bit: 43 us for 25 at that time; bf16 45 for
+// 41); sixteen consuming warps of one column tile each instead of eight of two (8-bit draft 151 us for 110 at that time).
 #include <cuda.h>
 
 #include <atomic>
@@ -147,15 +148,16 @@ __device__ __forceinline__ void ldmatrix_b8_x2_trans(uint32_t (&r)[4], uint32_t 
 __device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 constexpr int kMaxCluster = 8;
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float4 peer_float4(uint32_t at, int block) {  // from the shared memory of a block of the cluster
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ uint32_t peer_address(uint32_t at, int block) {  // of a place in the shared memory of a block of the cluster
   uint32_t there;
-  float4 v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(block));
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
-  return v;
+  return there;
+}
+__device__ __forceinline__ void peer_store(uint32_t at, float4 v, uint32_t bar) {  // 16 bytes that a barrier there counts
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+               ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(bar) : "memory");
 }
 
 // ---- which positions and granules a sequence has ----------------------------------------------------------------------
@@ -287,13 +289,34 @@ struct Folded {
   __device__ __forceinline__ void write(const DenseArgs& a, int64_t item, int quad) const {
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (l != 0.f) {  // 2^m in two halves: it may not be a float
-      const float inv = 1.f / l, half = fast_exp2(0.5f * m);
+      const float inv = __fdividef(1.f, l), half = fast_exp2(0.5f * m);
       v = make_float4(acc.x * inv * half * half, acc.y * inv * half * half, acc.z * inv * half * half, acc.w * inv * half * half);
     }
     *reinterpret_cast<uint2*>(a.out + item * 128 + quad * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
     if (a.lse != nullptr && quad == 0) a.lse[item] = l != 0.f ? (mx + log2f(l)) * kLn2 : -INFINITY;
   }
 };
+// `count` records that lie `step` apart, outputs 4 quad .. + 7 of each: two running ones that have the same head.
+__device__ __forceinline__ void fold_parts(const float4* part, int step, int count, int quad, Folded& f0, Folded& f1) {
+  float4 head = part[32], v0 = part[quad], v1 = part[quad + 1];
+  f0.acc = v0;
+  f1.acc = v1;
+  f0.mx = head.x; f0.l = head.y; f0.m = head.z;
+  if (count > 1) {
+    part += step;
+    head = part[32]; v0 = part[quad]; v1 = part[quad + 1];
+  }
+#pragma unroll 1
+  for (int i = count - 1; i > 0; --i) {  // (one ahead)
+    const float4 of = head, w0 = v0, w1 = v1;
+    if (i > 1) {
+      part += step;
+      head = part[32]; v0 = part[quad]; v1 = part[quad + 1];
+    }
+    f0.fold_pair(of, w0, w1, f1);
+  }
+  f1.mx = f0.mx; f1.l = f0.l; f1.m = f0.m;
+}
 __device__ __forceinline__ float4 no_head() { return make_float4(kNone, 0.f, kNone, 0.f); }
 
 // The record of column cc of head hh that block `block` leaves of the unit that its stretch begins (which = 0) or ends in (1).
@@ -319,6 +342,12 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   float* merge = reinterpret_cast<float*>(base_ptr + ring_bytes);
   unsigned char* ctrl = base_ptr + ring_bytes + kMergeBytes;
   const uint32_t bars = base + ring_bytes + kMergeBytes;
+  // Of a cluster: the records of the columns that this block finishes, [column tile][column][block], and barriers that count their bytes. The
+  // columns of a tile, of every head and column share, are dealt to the cluster's blocks: column k to block k mod cluster.
+  auto inbox_at = [&](int nt, int k) {
+    return reinterpret_cast<float*>(ctrl + kCtrlBytes) + (nt * a.heads * a.col_warps * 8 + (k >> a.cluster_shift << a.cluster_shift)) * kPartialStride;
+  };
+  auto inbox_bar = [&](int nt) { return bars + (uint32_t)kCtrlBytes - 16u + 8u * nt; };
   auto full_bar = [&](int s) { return bars + 16u * s; };
   auto empty_bar = [&](int s) { return bars + 16u * s + 8u; };
   uint32_t* slot_mask = reinterpret_cast<uint32_t*>(ctrl + 16 * kMaxSlots);   // rows of the slot that exist
@@ -341,7 +370,27 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
   }
+  // (Blocks of clusters are (rank, head group, sequence and column tile), of stretches (stretch and column tile).)
+  const int HG = a.head_groups;
+  const int rank = (int)blockIdx.x, tiled = a.cluster > 0 ? (int)blockIdx.z : (int)blockIdx.x;
+  const int span = a.col_tiles > 1 ? tiled / a.col_tiles : tiled, ct = tiled - span * a.col_tiles;
+  auto column_of = [&](int k, int nt) {  // the query column; -1 if there is none
+    const int col = ct * a.columns + ((k >> 3) & (a.col_warps - 1)) * NT * 8 + nt * 8 + (k & 7);
+    return col < a.columns_used && !(PARTS == 3 && (k & 4)) ? col : -1;
+  };
+  if (a.cluster > 1 && warp > 0 && warp <= NT) {
+    const uint32_t bar = inbox_bar(warp - 1);
+    int mine = 0;
+    for (int k = rank + a.cluster * lane; k < a.heads * a.col_warps * 8; k += a.cluster * 32) mine += column_of(k, warp - 1) >= 0;
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    if (lane == 0) {
+      mbar_init(bar, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      mbar_expect_tx(bar, (uint32_t)(mine * a.cluster * kPartialStride * 4));
+    }
+  }
   __syncthreads();
+  if (a.cluster > 1) cluster_arrive();  // (whoever has seen all of the cluster arrive may write to its inboxes)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind this grid's own wait, as in every kernel of the library
 
@@ -352,10 +401,6 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int off = at - list_base, unit = (int)((uint32_t)off / (uint32_t)(gran + a.pad));
     return granule_base + unit * gran + min(off - unit * (gran + a.pad), gran);
   };
-  const int HG = a.head_groups;
-  // Blocks of clusters are (rank, head group, sequence and column tile), of stretches (stretch and column tile).
-  const int rank = (int)blockIdx.x, tiled = a.cluster > 0 ? (int)blockIdx.z : (int)blockIdx.x;
-  const int span = a.col_tiles > 1 ? tiled / a.col_tiles : tiled, ct = tiled - span * a.col_tiles;
   const bool paged = a.block_table != nullptr;
   int total = 0, b_first, base_first, len_first;
   int64_t start_first;
@@ -649,11 +694,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   const int G = a.group, T = a.T;
   const int col0 = ct * a.columns + my_cw * NT * 8;
   // the query token of this lane's two columns of each tile (columns past the last one count as the last token's)
-  int tok_of[NT][2];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) tok_of[nt][h] = min(T - 1, token_of(a, col0 + nt * 8 + (PARTS == 3 ? (hcol + h) & 3 : hcol + h)));
+  auto tok_of = [&](int nt, int h) { return min(T - 1, token_of(a, col0 + nt * 8 + (PARTS == 3 ? (hcol + h) & 3 : hcol + h))); };
   // this lane's places in a slot's K and V rows (its 16-row parts lie part_step apart)
   const uint32_t part_step = a.two_boxes ? half_bytes / 2 : 2048u, head_at = (uint32_t)my_head * (kSub == 2 && !a.two_boxes ? 4096u : 2048u);
   uint32_t k_at, v_at;
@@ -799,7 +840,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // the column's query token sees `seen` positions from `from` on
-              const int here = s.n - T + tok_of[nt][h], from = a.window ? max(0, here - a.window + 1) : 0;
+              const int here = s.n - T + tok_of(nt, h), from = a.window ? max(0, here - a.window + 1) : 0;
               const unsigned seen = (unsigned)max(0, (a.causal ? here + 1 : s.n) - from);
               if ((unsigned)(pos0 + row_lo - from) >= seen || !(rows_ok >> row_lo & 1u)) x[0][nt][h] = -INFINITY;
               if ((unsigned)(pos0 + row_hi - from) >= seen || !(rows_ok >> row_hi & 1u)) x[0][nt][2 + h] = -INFINITY;
@@ -989,7 +1030,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                   float d[4] = {o[nt][c][0], o[nt][c][1], o[nt][c][2], o[nt][c][3]};
                   add_to(d, u, nt, v);
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) o[nt][c][k] = tok_of[nt][k & 1] == t ? d[k] : o[nt][c][k];
+                  for (int k = 0; k < 4; ++k) o[nt][c][k] = tok_of(nt, k & 1) == t ? d[k] : o[nt][c][k];
                 }
               });
             }
@@ -1078,7 +1119,8 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           release(here);
           continue;
         }
-#pragma unroll 1
+        // (8-bit: unrolled, because the compiler spills around the loop: the 8-bit draft case 81.5 us and 79. bf16: not, 64 columns 135 and 126.)
+#pragma unroll (EIGHT ? kSub : 1)
         for (int u = 0; u < kSub; ++u) {
           const uint32_t kb1 = kb[0] + (uint32_t)u * part_step, vb1 = vb[0] + (uint32_t)u * part_step;
           const uint32_t code1 = u == 0 ? codes[0] : codes[kSub - 1];
@@ -1112,49 +1154,41 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         if (a.lanes > 1) named_barrier(1 + my_head * a.col_warps + my_cw, a.lanes * 32);
         else __syncwarp();
       };
-      float* mine = merge + warp * 8 * kPartialStride;
+      // (What follows is formed anew for every segment: the compiler would rather form it ahead, and spill over the work.)
+      int this_lane = lane, this_warp = warp;
+      asm volatile("" : "+r"(this_lane), "+r"(this_warp));
+      const int share = this_warp & (a.heads * a.col_warps - 1), half = this_lane >> 4, quad = 2 * (this_lane & 15);  // (head, column share)
+      float* mine = merge + this_warp * 8 * kPartialStride + (this_lane & 3) * 2 * kPartialStride;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (PARTS == 3 && second) continue;
-          float* dst = mine + (hcol + h) * kPartialStride + rowq;
+          float* dst = mine + h * kPartialStride + (this_lane >> 2);
 #pragma unroll
           for (int c = 0; c < 8; ++c) { dst[16 * c] = o[nt][c][h]; dst[16 * c + 8] = o[nt][c][h + 2]; }
-          if (rowq == 0) *reinterpret_cast<float4*>(mine + (hcol + h) * kPartialStride + 128) = make_float4(mx[nt][h], l[nt][h], m[nt][h], 0.f);
+          if (this_lane < 4) *reinterpret_cast<float4*>(mine + h * kPartialStride + 128) = make_float4(mx[nt][h], l[nt][h], m[nt][h], 0.f);
         }
         together();
+        if (nt == 0 && a.cluster > 1) cluster_wait();  // the inboxes are there
         // the lanes' parts of a column become one: a half warp per column, 8 outputs a lane
         const int cols = min(PARTS == 3 ? 4 : 8, a.columns_used - col0 - nt * 8);
         const int lane_step = a.heads * a.col_warps * 8 * (kPartialStride / 4);
 #pragma unroll 1
-        for (int c = 2 * my_lane + (lane >> 4); c - (lane >> 4) < cols; c += 2 * a.lanes) {
+        for (int c = 2 * my_lane + half; c - half < cols; c += 2 * a.lanes) {
           if (c >= cols) continue;
-          const int mine_at = ((my_head * a.col_warps + my_cw) * 8 + c) * kPartialStride, quad = 2 * (lane & 15);
-          const float4* part = reinterpret_cast<const float4*>(merge + mine_at);
+          const float4* part = reinterpret_cast<const float4*>(merge + (share * 8 + c) * kPartialStride);
           Folded f0, f1;
-          float4 head = part[32], v0 = part[quad], v1 = part[quad + 1];
-          f0.acc = v0;
-          f1.acc = v1;
-          f0.mx = head.x; f0.l = head.y; f0.m = head.z;
-          if (a.lanes > 1) {
-            part += lane_step;
-            head = part[32]; v0 = part[quad]; v1 = part[quad + 1];
-          }
-#pragma unroll 1
-          for (int i = a.lanes - 1; i > 0; --i) {  // (one part ahead)
-            const float4 of = head, w0 = v0, w1 = v1;
-            if (i > 1) {
-              part += lane_step;
-              head = part[32]; v0 = part[quad]; v1 = part[quad + 1];
-            }
-            f0.fold_pair(of, w0, w1, f1);
-          }
-          f1.mx = f0.mx; f1.l = f0.l; f1.m = f0.m;
+          fold_parts(part, lane_step, a.lanes, quad, f0, f1);
           const int col = col0 + nt * 8 + c, t = token_of(a, col);
-          __syncwarp(0xffffu << (lane & 16));  // (the record may take the first part's place)
-          if (a.cluster > 1 || !whole_unit) {  // left for the cluster's blocks, or the second kernel, to join
-            float4* rec = a.cluster > 1 ? reinterpret_cast<float4*>(merge + mine_at) : record_at(a, (int)blockIdx.x, which, my_head, my_cw * NT * 8 + nt * 8 + c);
+          if (a.cluster > 1) {  // to the block that finishes the column
+            const int k = share * 8 + c, owner = k & (a.cluster - 1);
+            const uint32_t rec = peer_address(smem_u32(inbox_at(nt, k) + rank * kPartialStride), owner), bar = peer_address(inbox_bar(nt), owner);
+            peer_store(rec + 16u * quad, f0.acc, bar);
+            peer_store(rec + 16u * quad + 16u, f1.acc, bar);
+            if (quad == 0) peer_store(rec + 512u, make_float4(f0.mx, f0.l, f0.m, 0.f), bar);
+          } else if (!whole_unit) {  // left for the second kernel to join
+            float4* rec = record_at(a, (int)blockIdx.x, which, share / a.col_warps, (share & (a.col_warps - 1)) * NT * 8 + nt * 8 + c);
             rec[quad] = f0.acc;
             rec[quad + 1] = f1.acc;
             if (quad == 0) rec[32] = make_float4(f0.mx, f0.l, f0.m, 0.f);
@@ -1165,26 +1199,33 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           }
         }
         together();
-        if (a.cluster > 1) {  // the columns of this tile, of every head and column share, are dealt to the cluster's warps
-          cluster_barrier();
-          for (int k = rank + a.cluster * warp; k < a.heads * a.col_warps * 8; k += a.cluster * kConsumers) {
-            const int hc = k >> 3, c = k & 7, head_of = hc / a.col_warps;
-            const int col = ct * a.columns + (hc - head_of * a.col_warps) * NT * 8 + nt * 8 + c;
-            if (col >= a.columns_used || (PARTS == 3 && c >= 4)) continue;
-            const uint32_t rec = smem_u32(merge + k * kPartialStride);
-            Folded f;
-            const int who = lane & 7;
-            f.fold8(who < a.cluster ? peer_float4(rec + 512u, who) : no_head(), a.cluster, [&](int i) { return peer_float4(rec + 16u * lane, i); });
-            const int t = token_of(a, col);
-            f.write(a, ((int64_t)b * T + t) * a.num_q_heads + (hg * a.heads + head_of) * G + (col - t * G), lane);
-          }
-          cluster_barrier();  // before the records are written over, or gone with their block
-        }
       }
     }
     seq_base += s.gran * HG;
     ++b;
     len_b = len_next;
+  }
+  if (a.cluster > 1) {  // the columns that this block finishes, once every block's records of them are there
+#pragma unroll 1
+    for (int nt = 0; nt < NT; ++nt) {
+      // (Waits beyond the other blocks' own limits: nobody writes here once this block has given up.)
+      for (uint32_t it = 0; !mbar_try_wait(inbox_bar(nt), 0u); ++it) {
+        if ((it & 63u) == 63u) __nanosleep(64);
+        if (it < 4 * kSpinLimit) continue;
+        if (lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
+        break;
+      }
+#pragma unroll 1
+      for (int k = rank + a.cluster * warp; k < a.heads * a.col_warps * 8; k += a.cluster * kConsumers) {
+        const int col = column_of(k, nt), head_of = (k >> 3) / a.col_warps, who = lane & 7;
+        if (col < 0) continue;
+        const float4* rec = reinterpret_cast<const float4*>(inbox_at(nt, k));
+        Folded f;
+        f.fold8(who < a.cluster ? rec[who * (kPartialStride / 4) + 32] : no_head(), a.cluster, [&](int i) { return rec[i * (kPartialStride / 4) + lane]; });
+        const int t = token_of(a, col);
+        f.write(a, ((int64_t)b_first * T + t) * a.num_q_heads + (hg_first * a.heads + head_of) * G + (col - t * G), lane);
+      }
+    }
   }
 }
 
@@ -1292,7 +1333,8 @@ bool make_map(CUtensorMap* map, const void* ptr, bool eight, const clsa_params& 
 // nothing to join, the longest stretch of them decides. Chosen by an estimate from the longest sequence that the call allows: a block gets its
 // share of HBM, but no more than kBlockRate; the second kernel costs 3.5 us, a cluster's joining 0.8; and the lengths are taken to be 0.7
 // of the longest one on average, which only the first way profits from. Stretches against a cluster per unit: one sequence of 777 tokens 8.5 and
-// 6.5 us, one of 8192 19.3 and 13.8, the last 512 tokens of 64 sequences 23.8 and 17.5; they win from about 16 MB on (16 x 32768 tokens).
+// 6.5 us, one of 8192 19.3 and 13.8, the last 512 tokens of 64 sequences 23.8 and 17.5 (records sent instead of fetched have taken off 0.9, 1.9 and 0.2
+// since); they win from about 16 MB on (16 x 32768 tokens).
 constexpr double kRate = 6500e3, kBlockRate = 100e3;  // bytes per us
 // Where the list is cut, a unit's beginning and end count for what they take a block (other queries, a granule that some queries see in part, an
 // epilogue: kUnitCost), in granules at the rate of HBM or of the products. Nothing for them, 10 us for them: the 8-bit draft case 85 and 79 us, 8 drafted
@@ -1312,8 +1354,9 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   // columns: 122 and 178 us with 16, 103 and 146 with 32; the 8-bit draft case 110 and 105). With fewer columns bf16 rows keep to 16, in half the time
   // from the first row to the last one's end; 9 to 16 columns form a granule's first product beside the one before it instead (284 us, now 260).
   d.sub = eight || d.col_warps > 1 ? 2 : 1;
+  const int records = d.tiles * d.col_warps * 8 * kPartialStride * 4;  // of a head in a cluster
   const int gran = 16 * d.sub, head_bytes = gran * (eight ? 256 : 512);  // positions of a granule, bytes of a head's part of it
-  const int room = dev.max_smem_optin - kMergeBytes - kCtrlBytes - 1024;
+  int room = dev.max_smem_optin - kMergeBytes - kCtrlBytes - 1024;
   int most = kConsumers / d.col_warps;
   while (p.num_kv_heads % most != 0 || room / (most * head_bytes) < 3) most /= 2;
   d.heads = most;
@@ -1323,7 +1366,8 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   for (int h = most; h >= 1; h /= 2) {
     const int64_t units = (int64_t)p.num_seqs * (p.num_kv_heads / h) * d.col_tiles;
     for (int c = kMaxCluster; c >= 1; c /= 2) {
-      if (units * c > (c == 8 ? 128 : c == 4 ? 136 : dev.sm_count) || (c > 1 && c * 2 > granules)) continue;  // (clusters of 8 and 4 find place for so many blocks)
+      if (units * c > (c == 8 ? 128 : c == 4 ? 136 : dev.sm_count) || (c > 1 && c * 2 > granules)) continue;
+      if (c > 1 && (room - h * records) / (h * head_bytes) < 2 * kConsumers / (d.col_warps * h)) continue;  // (two slots per lane, as below)  // (clusters of 8 and 4 find place for so many blocks)
       const double rate = kRate / (double)(units * c) < kBlockRate ? kRate / (double)(units * c) : kBlockRate;
       const double cost = granules * h * head_bytes / c / rate + (c > 1 ? 0.8 : 0.0);
       if (cost < best) { best = cost; d.heads = h; d.cluster = c; d.whole_units = 0; }
@@ -1340,11 +1384,12 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   }
   d.head_groups = p.num_kv_heads / d.heads;
   d.slot_bytes = d.heads * head_bytes;
+  if (d.cluster > 1) room -= d.inbox_bytes = d.heads * records;
   d.lane_slots = room / d.slot_bytes;
   if (d.lane_slots > kMaxSlots / d.heads) d.lane_slots = kMaxSlots / d.heads;
-  d.lane_slots /= d.lanes;  // (three at least)
+  d.lane_slots /= d.lanes;  // (two at least)
   d.slots = d.lane_slots * d.lanes;
-  d.smem_bytes = (size_t)d.slots * d.slot_bytes + kMergeBytes + kCtrlBytes + 1024;
+  d.smem_bytes = (size_t)d.slots * d.slot_bytes + kMergeBytes + kCtrlBytes + d.inbox_bytes + 1024;
   auto align = [](size_t x) { return (x + 255) / 256 * 256; };
   d.unit_bytes = align((size_t)p.num_seqs * p.num_kv_heads * sizeof(int2));
   // (of the heads that a block has at most: the size does not go by the window)

@@ -18,6 +18,7 @@ struct DensePlan {
   int whole_units;             // 1: a stretch has the units that begin in it, whole (nothing to join)
   int cluster;                 // > 0: each cluster of so many blocks has one unit instead (joined in shared memory)
   int pad;                     // .. else: granules that a unit counts for beyond its own, where the list is cut
+  int inbox_bytes;             // a cluster's block: records that it joins
   size_t smem_bytes;
   size_t unit_bytes, scratch_bytes;  // scratch: where each unit lies, then records of partial results (the same for every window)
 };
