@@ -82,6 +82,8 @@ def _dense_call(name, call, p, window, q, out, lse, workspace, workspace_bytes, 
     dev, bf16, heads = _device(torch), torch.bfloat16, p.num_seqs * p.q_per_seq * p.num_q_heads
     _describes(p, dev)
     ws, nbytes = _workspace(workspace, workspace_bytes, made, dev)
+    if not -(1 << 31) <= window < 1 << 31:
+        raise ValueError(f"window: a 32-bit number is wanted, got {window}")
     status = call(int(window), _dense(q, "q", bf16, dev, heads * p.head_dim), _dense(out, "out", bf16, dev, heads * p.head_dim, output=True),
                   _dense(lse, "lse", torch.float32, dev, heads, output=True), ws, nbytes, _stream8(stream, dev))
     if status:

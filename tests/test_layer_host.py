@@ -246,6 +246,19 @@ def test_the_binding_compares_dense_calls_with_the_params(binding):
         clsa.clsa_dense_attn(p, 0, q, out, lse, ws)
 
 
+def test_the_binding_refuses_windows_beyond_32_bits(binding):
+    clsa, calls = binding
+    p = _params(clsa)
+    p._kv = None
+    q, out, ws = Tensor((2, 1, 32, 128), BF16), Tensor((2, 1, 32, 128), BF16), Tensor((1 << 20,), U8)
+    clsa.clsa_dense_attn(p, 0x7fffffff, q, out, None, ws)
+    assert _taken(calls, "clsa_dense_attn")
+    for window in (1 << 31, (1 << 32) + 5, -(1 << 32) + 5, -(1 << 31) - 1):  # as 32 bits some of these would be other windows
+        with pytest.raises(ValueError):
+            clsa.clsa_dense_attn(p, window, q, out, None, ws)
+        assert not calls, window
+
+
 def test_the_binding_takes_rows_of_any_even_spacing(binding):
     clsa, calls = binding
     spec = clsa.make_add_norm(dim=256, scale_group=32)
