@@ -1331,11 +1331,13 @@ bool make_map(CUtensorMap* map, const void* ptr, bool eight, const clsa_params& 
 // Three ways of dealing the work. Stretches of the list, cut anywhere: even whatever the lengths are, but a second kernel joins them.
 // A cluster of blocks per unit, where all fit on the GPU at once: joined in shared memory, but the longest sequence decides. Whole units:
 // nothing to join, the longest stretch of them decides. Chosen by an estimate from the longest sequence that the call allows: a block gets its
-// share of HBM, but no more than kBlockRate; the second kernel costs 3.5 us, a cluster's joining 0.8; and the lengths are taken to be 0.7
-// of the longest one on average, which only the first way profits from. Stretches against a cluster per unit: one sequence of 777 tokens 8.5 and
-// 6.5 us, one of 8192 19.3 and 13.8, the last 512 tokens of 64 sequences 23.8 and 17.5 (records sent instead of fetched have taken off 0.9, 1.9 and 0.2
-// since); they win from about 16 MB on (16 x 32768 tokens).
-constexpr double kRate = 6500e3, kBlockRate = 100e3;  // bytes per us
+// share of HBM, but no more than kBlockRate (or what its products keep up with); a cluster's joining costs 0.8 us. Stretches count as 14 us and 0.7 of
+// the bytes, between even lengths (measured as 9 us and all of them) and ragged ones. 32 / 8 heads, bf16, us, stretches and clusters (of one block where
+// units are enough): 1 x 8192 tokens 19.3 and 11.6, 4 x 4096 21.2 and 15.6 (lengths from 205 to 4096: 16.7 and 12.0), 16 x 4096 50.4 and 44.3 (32.6 and
+// 29.4), 4 x 16384 49.9 and 43.2 (33.2 and 33.0); 20 x 8192 107.7 and 103 (54.5 and 64.4), which goes to stretches. 8-bit: 17.7 and 11.1 (14.1 and
+// 9.5), 33.1 and 27.0 (24.3 and 22.8), 33.0 and 28.1 (25.5 and 25.3); 62.5 and 65.1 (35.5 and 51.7).
+// Fourteen clusters of 8 find place at once, 34 of 4: sixteen of 8 take 24.4 us for 4 x 4096, 32 of 4 take 15.6.
+constexpr double kRate = 6500e3, kBlockRate = 85e3, kBlockRate8 = 65e3;  // bytes per us
 // Where the list is cut, a unit's beginning and end count for what they take a block (other queries, a granule that some queries see in part, an
 // epilogue: kUnitCost), in granules at the rate of HBM or of the products. Nothing for them, 10 us for them: the 8-bit draft case 85 and 79 us, 8 drafted
 // tokens over bf16 103 and 100, 16 sequences of 16 heads' one 38.6 and 37.
@@ -1362,13 +1364,16 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   d.heads = most;
   const int64_t reach = window > 0 && window < p.max_seq_len - p.q_per_seq ? window + p.q_per_seq + gran : p.max_seq_len;
   const double granules = (double)((reach + gran - 1) / gran);
-  double best = 0.7 * granules * head_bytes * p.num_seqs * p.num_kv_heads / kRate + 3.5;
+  double best = 0.7 * granules * head_bytes * p.num_seqs * p.num_kv_heads / kRate + 14.0;
+  const double products = (eight ? 100e6 : 240e6) / d.columns;  // bytes per us that the GPU's products keep up with, as measured with 32 and 64 columns
+  double block_rate = eight ? kBlockRate8 : kBlockRate;
+  if (products / dev.sm_count < block_rate) block_rate = products / dev.sm_count;
   for (int h = most; h >= 1; h /= 2) {
     const int64_t units = (int64_t)p.num_seqs * (p.num_kv_heads / h) * d.col_tiles;
     for (int c = kMaxCluster; c >= 1; c /= 2) {
-      if (units * c > (c == 8 ? 128 : c == 4 ? 136 : dev.sm_count) || (c > 1 && c * 2 > granules)) continue;
-      if (c > 1 && (room - h * records) / (h * head_bytes) < 2 * kConsumers / (d.col_warps * h)) continue;  // (two slots per lane, as below)  // (clusters of 8 and 4 find place for so many blocks)
-      const double rate = kRate / (double)(units * c) < kBlockRate ? kRate / (double)(units * c) : kBlockRate;
+      if (units * c > (c == 8 ? 112 : c == 4 ? 136 : dev.sm_count) || (c > 1 && c * 2 > granules)) continue;
+      if (c > 1 && (room - h * records) / (h * head_bytes) < 2 * kConsumers / (d.col_warps * h)) continue;  // (two slots per lane, as below)
+      const double rate = kRate / (double)(units * c) < block_rate ? kRate / (double)(units * c) : block_rate;
       const double cost = granules * h * head_bytes / c / rate + (c > 1 ? 0.8 : 0.0);
       if (cost < best) { best = cost; d.heads = h; d.cluster = c; d.whole_units = 0; }
     }
@@ -1377,7 +1382,6 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   }
   d.lanes = kConsumers / (d.col_warps * d.heads);
   if (d.cluster == 0 && !d.whole_units) {
-    const double products = (eight ? 100e6 : 240e6) / d.columns;  // bytes per us that they keep up with, as measured with 32 and 64 columns
     d.pad = (int)(kUnitCost * (kRate < products ? kRate : products) / dev.sm_count / (d.heads * head_bytes));
     const int64_t units = (int64_t)p.num_seqs * (p.num_kv_heads / d.heads);
     while (units * d.pad > 1 << 28) d.pad /= 2;  // (places are numbered with 32 bits)
