@@ -214,11 +214,13 @@ cudaError_t launch_add_norm(const clsa_add_norm_spec& spec, int num_rows, const 
   a.num_rows = num_rows;
   const int vecs = spec.dim / 8;
   // Many rows: blocks that stay and fetch ahead, as many as the registers allow; else a block, of as many threads as fit, for each row.
-  // Two vectors per thread where two such blocks fit on an SM, else four (4096 rows of 8192, a scale per row: 47 us and 39.6; of 7168, where they
-  // fit: 34.9 and 35.8).
+  // Up to 256 vectors a row: two per thread where that leaves no more lanes idle (8192 rows of 512, 896, 1536, 8-bit output: 6.8, 12.4, 17.9 us with
+  // one, 5.9, 11.0, 16.8 with two; of 768, where a quarter would be: 10.0 and 10.4). Beyond: two where two such blocks fit on an SM, else
+  // four (4096 rows of 8192, a scale per row: 47 us and 39.6; of 7168, where they fit: 34.9 and 35.8).
   const bool loop = num_rows > kLoopRows * dev.sm_count;
-  const int per = loop ? (vecs <= 256 ? 1 : vecs <= 896 ? 2 : 4) : vecs <= 1024 ? 1 : 2;
-  const int threads = ((vecs + per - 1) / per + 31) / 32 * 32;
+  auto lanes = [&](int per) { return ((vecs + per - 1) / per + 31) / 32 * 32; };
+  const int per = loop ? (vecs <= 256 && 2 * lanes(2) > lanes(1) ? 1 : vecs <= 896 ? 2 : 4) : vecs <= 1024 ? 1 : 2;
+  const int threads = lanes(per);
   void (*kernel)(const AddNormArgs) = loop ? (per == 1 ? add_norm_kernel<1, 3> : per == 2 ? add_norm_kernel<2, 1> : add_norm_kernel<4, 1>)
                                            : (per == 1 ? add_norm_kernel<1, 0> : add_norm_kernel<2, 0>);
   int64_t blocks = num_rows;
