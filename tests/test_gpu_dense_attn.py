@@ -178,6 +178,30 @@ def test_long_sequences_split_over_blocks(lens, eight):
 
 
 @pytest.mark.parametrize("eight", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("T,heads", [(1, (32, 8)), (1, (8, 1)), (3, (20, 4)), (8, (32, 8)), (16, (16, 2)), (32, (16, 1))], ids=str)
+@pytest.mark.parametrize("lens", [[1], [600, 0, 17], [0, 0, 0, 5000], [33] * 24, "24", "129", "300"], ids=str)
+def test_stretches_of_the_list(lens, T, heads, eight):
+    """Where sequences may be long (and are not) the work is cut into stretches, a unit's ends counted: of single granules, of units' ends only."""
+    if isinstance(lens, str):
+        g = torch.Generator()
+        g.manual_seed(int(lens))
+        lens = [0 if n < 60 else n for n in torch.randint(0, 700, (int(lens),), generator=g).tolist()]
+    Problem(lens, *heads, T=T, eight=eight, max_len=1 << 20, seed=len(lens)).check()
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("page", [16, 32, 256])
+@pytest.mark.parametrize("T,heads", [(1, (32, 8)), (4, (20, 4)), (8, (16, 2))], ids=str)
+def test_stretches_of_paged_sequences(page, T, heads, eight):
+    w = Problem([900, 8, 1300, 77, 513, 16, 31], *heads, T=T, eight=eight, page=page, causal=1)
+    pad = torch.full((7, (1 << 20) // page - w.table.shape[1]), -1, dtype=torch.int32, device=DEV)  # pages that no length reaches
+    w.table_ = torch.cat([w.table, pad], 1).contiguous()
+    w.max_len = 1 << 20
+    w.make()
+    w.check()
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["bf16", "e4m3"])
 def test_numbers_that_are_not_finite_stay_where_they_are_seen(eight):
     """V (and K) of the newest tokens not finite: the queries in front of them do not see them."""
     for T, heads, window in ((4, (8, 2), 0), (8, (32, 8), 0), (3, (5, 1), 6), (8, (8, 8), 4)):

@@ -67,6 +67,20 @@ def test_add_norm(rows, dim, group):
             assert (codes[:, dim:] == 0x55).all() and (scales[:, dim // group:] == 0x55).all()
 
 
+@pytest.mark.parametrize("dim,group", [(64, 64), (128, 32), (512, 64), (768, 0), (768, 128), (896, 896), (1536, 64), (2304, 32)])
+def test_blocks_that_take_many_short_rows(dim, group):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(dim + group)
+    rows = 19003
+    x, r, weight = _rows(g, rows, dim), _rows(g, rows, dim, 3.0), (1 + 0.2 * torch.randn(dim, generator=g, device=DEV)).to(torch.bfloat16)
+    s, y = torch.empty_like(x), torch.empty_like(x)
+    codes = torch.empty((rows, dim), dtype=torch.uint8, device=DEV) if group else None
+    scales = torch.empty((rows, dim // group), dtype=torch.uint8, device=DEV) if group else None
+    spec = clsa.make_add_norm(dim=dim, eps=1e-5, weight=weight, scale_group=group)
+    clsa.clsa_add_norm(spec, x, r, s, y, codes, scales)
+    check_add_norm(spec, x, r, weight, 1e-5, s, y, codes, scales, group)
+
+
 def test_add_norm_in_place_and_shared_rows():
     g = torch.Generator(device=DEV)
     g.manual_seed(1)
