@@ -47,7 +47,8 @@ CLSA_API clsa_status clsa_dense_attn(const clsa_params* p, int32_t window, const
 
 /* clsa_dense_attn over an 8-bit cache (its K and V; a sequence begins on a multiple of 16 rows, as every scale block makes it: flagged
  * CLSA_DEV_BAD_SCALE_BLOCK and counted as empty otherwise). Logits may have any size that is a float, for queries of magnitudes below
- * 2^118 / sm_scale; a query's elements below 2^-31 of its head's largest round to f16's last place. */
+ * 2^118 / sm_scale; a query's elements below 2^-31 of its head's largest round to f16's last place. Weights meet V in f16: off by up to 2^-11
+ * of each, and by up to 2^-36 of the largest weight times its V's scale. */
 CLSA_API clsa_status clsa_dense_attn8(const clsa_params* p, const clsa_cache8* c, int32_t window, const void* q, void* out, float* lse,
                                       void* workspace, size_t workspace_bytes, clsa_stream stream);
 

@@ -22,7 +22,7 @@
 // vote per granule, no reduction over its tokens otherwise). Weights are rounded to what the matrix instruction takes beside V. bf16: two
 // parts of 8 bits each (p and what its rounding left) where that costs nothing, with up to 32 columns: the error of a single part is as
 // large as the output's own rounding; up to 4 columns are held twice and the second copy takes the second parts. 8-bit caches: f16,
-// 2^-11 of each weight. Denominators are sums of the unrounded weights in fp32.
+// 2^-11 of each weight, and 2^-36 of the largest one with its V's scale. Denominators are sums of the unrounded weights in fp32.
 // Granules that some query sees in part only run a second instance of the step: positions out of sight get logits of -inf, and V rows that nobody sees
 // are taken as zeros (a weight of 0 times a NaN is none). Blocks in which a sequence ends pay for it, and for an epilogue and
 // queries in the middle of their stretch, with code that comes from memory: about 10 us, which the cut of the list makes up for.
@@ -66,6 +66,10 @@ constexpr int kMergeBytes = kConsumers * 8 * kPartialStride * 4;  // a column ti
 constexpr int kCtrlBytes = 1024;
 constexpr uint32_t kSpinLimit = 1u << 22;  // polls of a barrier: seconds
 constexpr float kLazy = 8.f;
+// 8-bit: the numerators' reference lies 2^11 below the largest weight that it was set by and moves when one would exceed 2^15 (f16 ends at 2^16), so that
+// f16's smallest steps are 2^-35 of the largest weight and not 2^-24: weights of a long flat tail behind one large weight would be rounded to such steps or to
+// nothing, while the denominators count them.
+constexpr float kAbove8 = 11.f, kLazy8 = 15.f;
 constexpr float kNone = -3.4028234663852886e38f;  // a reference before the first token
 constexpr int kHeldBack = 22;                     // of K's exponent, kept for the query's factor: d 2^(ek - 22) is finite and keeps its last bits
 
@@ -881,7 +885,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
               if (EIGHT) top_e[h] = fmaxf(top_e[h], most[h] + ev[u]);
             }
           }
-          move = move || fmaxf(top[0], top[1]) > kLazy || (EIGHT && (top_e[0] > m[nt][0] + kLazy || top_e[1] > m[nt][1] + kLazy));
+          move = move || fmaxf(top[0], top[1]) > kLazy || (EIGHT && (top_e[0] > m[nt][0] + kLazy8 || top_e[1] > m[nt][1] + kLazy8));
         }
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
@@ -905,7 +909,7 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 const float mo = m[nt][h] + drop;
                 float mn = mo;
 #pragma unroll
-                for (int u = 0; u < U; ++u) mn = fmaxf(mn, (tops[u] - mxn) + ev[u]);
+                for (int u = 0; u < U; ++u) mn = fmaxf(mn, (tops[u] - mxn) + ev[u] - kAbove8);
                 alpha = fast_exp2(mo - mn);
                 m[nt][h] = mn;
               }
