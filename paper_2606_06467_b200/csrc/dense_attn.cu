@@ -50,6 +50,7 @@
 #include <type_traits>
 
 #include "attn_common.cuh"
+#include "dense_units.h"
 #include "layer.cuh"
 
 namespace clsa {
@@ -1252,7 +1253,9 @@ __global__ void __launch_bounds__(kJoinThreads) dense_join_kernel(const __grid_c
   int2 unit = make_int2(0, 0);
   if (b < a.num_seqs) unit = __ldcg(&a.units[(int64_t)b * a.head_groups + hg]);
   const int first = unit.x >> 1, last = unit.y;
-  const bool joined = last > first;
+  const Noted noted = noted_unit(unit.x, unit.y, a.spans);
+  const bool joined = noted == Noted::kCut;
+  if (noted == Noted::kNever && lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);  // (a fetching warp gave up before this unit)
   if (SHARE == 1 ? !joined : !__syncthreads_or(joined)) return;
   const int aside = unit.x & 1 ? a.heads * a.columns * (kPartialStride / 4) : 0;
   Folded f;
