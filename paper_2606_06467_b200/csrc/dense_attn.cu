@@ -138,6 +138,17 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {  // w
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
+// Bounded wait for the records that other blocks of the cluster send, which the barrier counts; false once the limit ran out.
+__device__ __forceinline__ bool records_wait(uint32_t bar) {
+  for (uint32_t it = 0; it < 4 * kSpinLimit; ++it) {
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], 0;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(bar) : "memory");
+    if (ok != 0) return true;
+    if ((it & 63u) == 63u) __nanosleep(64);
+  }
+  return false;
+}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
@@ -1211,14 +1222,17 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     len_b = len_next;
   }
   if (a.cluster > 1) {  // the columns that this block finishes, once every block's records of them are there
+    asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");  // (its records are on their way; waited for below only)
+    bool all_sent = false;
 #pragma unroll 1
     for (int nt = 0; nt < NT; ++nt) {
-      // (Waits beyond the other blocks' own limits: nobody writes here once this block has given up.)
-      for (uint32_t it = 0; !mbar_try_wait(inbox_bar(nt), 0u); ++it) {
-        if ((it & 63u) == 63u) __nanosleep(64);
-        if (it < 4 * kSpinLimit) continue;
+      if (!__all_sync(0xffffffffu, records_wait(inbox_bar(nt)))) {
+        // Given up. Records that are still to come would be written to memory that this block has left: it stays until every thread has sent its
+        // own (each wait in front of that is bounded, and a block that gave up sends as well), and those on their way have landed.
         if (lane == 0) flag_status(a.status, CLSA_DEV_TIMEOUT);
-        break;
+        if (!all_sent) cluster_wait();
+        all_sent = true;
+        records_wait(inbox_bar(nt));
       }
 #pragma unroll 1
       for (int k = rank + a.cluster * warp; k < a.heads * a.col_warps * 8; k += a.cluster * kConsumers) {
