@@ -80,6 +80,8 @@ typedef struct {
  *   sum_out      bf16, s rounded to nearest even; NULL: not wanted. May be x or residual itself (same data and stride)
  *   y_out        bf16, y rounded to nearest even; NULL: not wanted. May be x or residual itself, where sum_out is not
  *   codes_out    e4m3 [num_rows][dim], scales_out  bytes [num_rows][dim / scale_group]: both, with scale_group > 0, or neither
+ * Beyond that no output shares memory with another argument: such calls are refused (rows of different distances in bytes count as all that lies
+ * between the first and the last of them).
  * At least one of y_out and codes_out is given. num_rows 0 .. 2^30; 0 does nothing. Squares are summed in fp32: magnitudes above about
  * 1e17 overflow the norm. */
 CLSA_API clsa_status clsa_add_norm(const clsa_add_norm_spec* spec, int32_t num_rows, const clsa_rows* x, const clsa_rows* residual,

@@ -61,7 +61,23 @@ clsa_status check_matrix(const clsa_rows* m, int64_t elements, int per16, int nu
   if (m->stride < elements && num_rows > 1 && (output || m->stride != 0)) return CLSA_ERR_INVALID_ARG;
   return CLSA_OK;
 }
-bool same_rows(const clsa_rows* a, const clsa_rows* b) { return a != nullptr && b != nullptr && a->data == b->data; }
+// The bytes of a matrix' rows: runs of `length`, `step` apart.
+struct Runs {
+  __int128 at, length, step, rows;
+  __int128 end() const { return at + (rows - 1) * step + length; }
+};
+Runs runs_of(const clsa_rows* m, int64_t elements, int size, int num_rows) {
+  if (m == nullptr || m->data == nullptr) return {0, 0, 0, 0};
+  return {(__int128)reinterpret_cast<uintptr_t>(m->data), (__int128)elements * size, (__int128)m->stride * size, m->stride == 0 ? 1 : num_rows};
+}
+// Whether two matrices share a byte. Rows of different distances count by the memory from the first to the last of them.
+bool overlap(const Runs& a, const Runs& b) {
+  if (a.rows == 0 || b.rows == 0 || a.at >= b.end() || b.at >= a.end()) return false;
+  if (a.rows == 1 && b.rows == 1) return true;
+  if (a.rows > 1 && b.rows > 1 && a.step != b.step) return true;
+  const __int128 step = a.rows > 1 ? a.step : b.step, behind = ((b.at - a.at) % step + step) % step;  // of a's next row in front of it
+  return behind < a.length || behind + b.length > step;
+}
 
 }  // namespace
 }  // namespace clsa
@@ -117,13 +133,20 @@ clsa_status clsa_add_norm(const clsa_add_norm_spec* spec, int32_t num_rows, cons
     CLSA_TRY(check_matrix(codes_out, spec->dim, 16, num_rows, true));
     CLSA_TRY(check_matrix(scales_out, spec->dim / g, 1, num_rows, true));
   }
-  // an output may be an input's own rows, not another output's
-  if (same_rows(sum_out, y_out)) return CLSA_ERR_INVALID_ARG;
-  const clsa_rows* outs[2] = {sum_out, y_out};
-  const clsa_rows* ins[2] = {x, residual};
-  for (const clsa_rows* o : outs)
-    for (const clsa_rows* i : ins)
-      if (same_rows(o, i) && num_rows > 1 && o->stride != i->stride) return CLSA_ERR_INVALID_ARG;
+  // Blocks write some rows while others read theirs: an output shares no byte with another argument, but for sum_out and y_out, which may be an
+  // input's own rows (whose elements the thread that writes them has read).
+  const clsa_rows weight = {const_cast<void*>(spec->weight), 0};
+  const Runs outs[4] = {runs_of(sum_out, spec->dim, 2, num_rows), runs_of(y_out, spec->dim, 2, num_rows), runs_of(codes_out, spec->dim, 1, num_rows),
+                        runs_of(scales_out, g > 0 ? spec->dim / g : 0, 1, num_rows)};
+  const Runs ins[3] = {runs_of(x, spec->dim, 2, num_rows), runs_of(residual, spec->dim, 2, num_rows), runs_of(&weight, spec->dim, 2, 1)};
+  for (int o = 0; o < 4; ++o) {
+    for (int i = 0; i < o; ++i)
+      if (overlap(outs[o], outs[i])) return CLSA_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i) {
+      const bool own = o < 2 && i < 2 && outs[o].at == ins[i].at && outs[o].rows == ins[i].rows && (num_rows == 1 || outs[o].step == ins[i].step);
+      if (!own && overlap(outs[o], ins[i])) return CLSA_ERR_INVALID_ARG;
+    }
+  }
   DeviceInfo dev;
   if (!device_info(&dev)) return CLSA_ERR_CUDA;
   return from_cuda(launch_add_norm(*spec, num_rows, x, residual, sum_out, y_out, codes_out, scales_out, dev, static_cast<cudaStream_t>(stream)));

@@ -14,6 +14,7 @@ entry._load_build_module().build()
 import _layer_ref as ref
 import paper_2606_06467_b200 as clsa
 from test_gpu_dense_attn import SM, Problem
+from test_gpu_layer_norms import check_add_norm
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -48,3 +49,50 @@ def test_a_flat_tail_behind_large_weights(T, heads, gap, exponent):
         largest = 2.0 ** exponent / len(range(5, n, 32))
         tol[b] = (2.0 ** -8 + 2.0 ** -11 + 4 * eps + 2 * steps) * out[b].abs() + 2.0 ** -36 * largest * n
     ref.check_close(p.out, out, tol, "out")
+
+
+@pytest.mark.parametrize("dim,group", [(256, 32), (512, 512), (2560, 0), (2560, 2560), (8192, 128)])
+def test_add_norm_in_place_over_many_rows(dim, group):
+    """Blocks that stay and fetch rows ahead of those that they overwrite; a row that all share; arguments side by side in one buffer."""
+    rows = 4099
+    g = torch.Generator(device=DEV)
+    g.manual_seed(dim + group)
+    new = lambda: torch.randn((rows, dim), generator=g, device=DEV).to(torch.bfloat16)  # noqa: E731
+    x, r, weight = new(), new() * 3, (1 + 0.2 * torch.randn(dim, generator=g, device=DEV)).to(torch.bfloat16)
+    spec = clsa.make_add_norm(dim=dim, eps=1e-5, weight=weight, scale_group=group)
+    outs = lambda: (torch.full((rows, dim), 0x55, dtype=torch.uint8, device=DEV), torch.full((rows, dim // group), 0x55, dtype=torch.uint8, device=DEV)) if group else (None, None)  # noqa: E731
+    s, y = torch.empty_like(x), torch.empty_like(x)
+    codes, scales = outs()
+    clsa.clsa_add_norm(spec, x, r, s, y, codes, scales)
+    check_add_norm(spec, x, r, weight, 1e-5, s, y, codes, scales, group)
+
+    def same(a, b):
+        assert (a is None and b is None) or torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+    for into_s, into_y in (("x", "r"), ("r", "x"), ("x", None), (None, "r"), ("r", "own")):
+        t = dict(x=x.clone(), r=r.clone(), own=torch.empty_like(x))
+        c2, e2 = outs()
+        if into_y is None and not group:
+            into_y = "own"
+        clsa.clsa_add_norm(spec, t["x"], t["r"], t.get(into_s), t.get(into_y), c2, e2)
+        if into_s:
+            same(t[into_s], s)
+        if into_y:
+            same(t[into_y], y)
+        same(c2, codes), same(e2, scales)
+    t = x.clone()
+    clsa.clsa_add_norm(spec, t, t, t, y, None, None) if not group else clsa.clsa_add_norm(spec, t, t, t, y, *outs())
+    check_add_norm(spec, x, x, weight, 1e-5, t, y, None, None, group)
+    shared, t = r[17:18].clone().expand(rows, dim), x.clone()
+    clsa.clsa_add_norm(spec, t, shared, t, y, *outs())
+    check_add_norm(spec, x, shared, weight, 1e-5, t, y, None, None, group)
+    wide = torch.zeros((rows, 5 * dim), dtype=torch.bfloat16, device=DEV)
+    part = [wide[:, k * dim:(k + 1) * dim] for k in range(5)]
+    part[0].copy_(x), part[2].copy_(r)
+    tail = part[4].view(torch.uint8)
+    clsa.clsa_add_norm(spec, part[0], part[2], part[1], part[3], *((tail[:, :dim], tail[:, dim:dim + dim // group]) if group else (None, None)))
+    want = dict(zip(range(4), (x, s, r, None)))
+    for k in (0, 1, 2):
+        same(part[k], want[k])
+    check_add_norm(spec, x, r, weight, 1e-5, part[1], part[3], *((tail[:, :dim], tail[:, dim:dim + dim // group]) if group else (None, None)), group)
+    assert group == 0 or (tail[:, dim + dim // group:] == 0).all()
