@@ -1,5 +1,6 @@
 """Calls around a layer's cache at the edges of what their header allows, on a GPU against the definitions in 64 bits."""
 import math
+import os
 
 import pytest
 
@@ -96,3 +97,30 @@ def test_add_norm_in_place_over_many_rows(dim, group):
         same(part[k], want[k])
     check_add_norm(spec, x, r, weight, 1e-5, part[1], part[3], *((tail[:, :dim], tail[:, dim:dim + dim // group]) if group else (None, None)), group)
     assert group == 0 or (tail[:, dim + dim // group:] == 0).all()
+
+
+def test_the_readme_runs():
+    """README.md's calls around a layer as they stand there, and their attention's results."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    block = text[text.index("### Around a layer"):].split("```python\n")[1].split("```")[0]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(31)
+    n16 = lambda *s: torch.randn(s, generator=g, device=DEV).to(torch.bfloat16)  # noqa: E731
+    w = Problem([700, 33], 32, 8, causal=1, window=512, seed=31)
+    w8 = Problem([700, 33], 32, 8, causal=1, eight=True, block=64, seed=32)
+    assert w.rows <= w8.rows
+    names = dict(clsa=clsa, torch=torch, B=2, T=1, n=700, rows=w.rows, seq_start=w.start, seq_len=w.seq_len, k_cache=w.k, v_cache=w.v, q=w.q, out=w.out,
+                 lse=w.lse, cache=w8.cache, inv_freq=torch.rand(64, generator=g, device=DEV), w_norm=n16(2560), wq=n16(128), wk=n16(128), x=n16(2, 1, 2560),
+                 residual=n16(2, 1, 2560), x_sum=n16(2, 1, 2560), codes=torch.zeros(2, 1, 2560, dtype=torch.uint8, device=DEV),
+                 scales=torch.zeros(2, 1, 80, dtype=torch.uint8, device=DEV), positions=torch.tensor([[699, 32], [5, 6], [7, 8]], dtype=torch.int32, device=DEV),
+                 k=n16(2, 1, 8, 128))
+    first = block.index("clsa.clsa_dense_attn8(")
+    exec(block[:first], names)
+    torch.cuda.synchronize()
+    out, lse, tol, ltol = w.want()
+    ref.check_close(w.lse, lse, ltol, "lse")
+    ref.check_close(w.out, out, tol, "out")
+    w8.start, w8.q = w.start, w.q  # (the other cache's rows are where this one's are)
+    exec(block[first:], names)
+    out, lse, tol, ltol = w8.want()
+    ref.check_close(w.out, out, tol, "out over codes")

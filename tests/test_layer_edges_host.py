@@ -66,3 +66,29 @@ def test_add_norm_refuses_outputs_that_share_memory(clsa):
     ]
     for kw in bad:
         assert call(**kw) == 1, kw
+
+
+def test_the_readme_makes_params_that_the_dense_calls_take(clsa):
+    """README.md's calls around a layer, with stand-ins for what they launch: the params are complete (found on a GPU machine: nothing missing; here: no
+    device)."""
+    text = open(os.path.join(ROOT, "README.md")).read()
+    block = text[text.index("### Around a layer"):].split("```python\n")[1].split("```")[0]
+    made = []
+
+    class Stand:
+        def __getattr__(self, name):
+            if name.startswith("make_"):
+                return getattr(clsa, name)
+            if name == "clsa_dense_workspace_bytes":
+                return lambda p: made.append(p) or 1024
+            return lambda *a: made.extend(x for x in a if isinstance(x, clsa.clsa_params)) or 0
+
+    kv = lambda: torch.zeros(256, 8, 128, dtype=torch.bfloat16)  # noqa: E731
+    names = dict(clsa=Stand(), torch=torch, B=2, T=1, n=100, rows=256, seq_start=torch.tensor([0, 128]), seq_len=torch.tensor([100, 7], dtype=torch.int32),
+                 k_cache=kv(), v_cache=kv(), inv_freq=torch.zeros(64), w_norm=torch.zeros(2560, dtype=torch.bfloat16), wq=torch.zeros(128, dtype=torch.bfloat16),
+                 wk=torch.zeros(128, dtype=torch.bfloat16), **{k: None for k in "x residual x_sum codes scales positions q k out lse cache".split()})
+    exec(block.replace('device="cuda"', 'device="cpu"'), names)
+    assert len(made) == 3
+    n = ctypes.c_size_t(0)
+    for p in made:
+        assert clsa.raw().clsa_dense_workspace_bytes(ctypes.byref(p), ctypes.byref(n)) in (0, 4)
