@@ -772,14 +772,16 @@ dense_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
           amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
           const int shift = min(13 + 127 - (int)(__float_as_uint(amax) >> 23), 120);  // largest magnitude into [2^13, 2^14)
-          const float up = exp2_int(shift), down = exp2_int(-shift);
+          const float up = exp2_int(shift);
 #pragma unroll
           for (int st = 0; st < 8; ++st)
 #pragma unroll
             for (int k = 0; k < 2; ++k) qb[nt][st][k] = pack_f16x2(bf16_lo(qb[nt][st][k]) * up, bf16_hi(qb[nt][st][k]) * up);
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            qf[nt][h] = fminf(__shfl_sync(0xffffffffu, down, 4 * (hcol + h)) * a.scale_log2 * exp2_int(kHeldBack), 3.4028234663852886e38f);
+          for (int h = 0; h < 2; ++h) {  // scale_log2 2^(kHeldBack - shift), in halves; never 0, so that it leaves a logit of -inf one
+            const int e = kHeldBack - __shfl_sync(0xffffffffu, shift, 4 * (hcol + h));
+            qf[nt][h] = fminf(fmaxf(a.scale_log2 * exp2_int(e >> 1) * exp2_int(e - (e >> 1)), 1.4012984643e-45f), 3.4028234663852886e38f);
+          }
         } else {
 #pragma unroll
           for (int ks = 0; ks < 8; ++ks) {  // dimensions 16 ks + hcol, + 1, and those + 8

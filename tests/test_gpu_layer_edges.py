@@ -124,3 +124,35 @@ def test_the_readme_runs():
     exec(block[first:], names)
     out, lse, tol, ltol = w8.want()
     ref.check_close(w.out, out, tol, "out over codes")
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("scale", [1e-9, 1e-20, 1e-44])
+def test_tiny_scales_and_queries(eight, scale):
+    """Logits of next to nothing: the mean of what is seen. (A factor that falls to 0 would make NaN of the logits, -inf, of what is not seen.)"""
+    p = Problem([100, 17, 1], 8, 2, T=2, causal=0, eight=eight, seed=33)
+    p.q.zero_()
+    p.p.sm_scale = scale
+    p.check()
+    p.q.fill_(2.0 ** -100)
+    p.run()
+    p.q.zero_()  # (the reference's: its scale is another)
+    out, lse, tol, ltol = p.want()
+    ref.check_close(p.lse, lse, ltol, "lse")
+    ref.check_close(p.out, out, tol, "out")
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("power", [-100, -30, 30, 100])
+def test_scales_and_queries_that_make_up_for_one_another(eight, power):
+    p = Problem([300, 77], 16, 4, eight=eight, seed=34)
+    if eight:
+        p.check()
+    q = p.q.clone()
+    p.q.copy_((q.float() * 2.0 ** power).to(torch.bfloat16))
+    p.p.sm_scale = SM * 2.0 ** -power
+    p.run()
+    p.q.copy_(q)
+    out, lse, tol, ltol = p.want()
+    ref.check_close(p.lse, lse, ltol, "lse")
+    ref.check_close(p.out, out, tol, "out")
