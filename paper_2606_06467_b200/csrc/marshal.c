@@ -254,10 +254,12 @@ static int matrix_of(PyObject* t, PyObject* dtype, PyObject* other, int64_t devi
   if (!look(t, dtype, device, &v) && (other == NULL || !look(t, other, device, &v))) return 0;
   if (v.shape[v.nd - 1] != length || (v.stride[v.nd - 1] != 1 && length != 1)) return 0;
   int64_t n = 1, step = -1;
+  int none = 0; /* no rows at all: nothing is spaced */
+  for (int i = v.nd - 2; i >= 0; --i) none |= v.shape[i] == 0;
   for (int i = v.nd - 2; i >= 0; --i) {
     if (v.shape[i] == 1) continue;
     if (step < 0) step = v.stride[i];
-    else if (v.stride[i] != n * step) return 0;
+    else if (v.stride[i] != n * step && !none) return 0;
     n *= v.shape[i];
   }
   if ((*rows >= 0 && n != *rows) || n > 0x7fffffff) return 0;

@@ -137,7 +137,7 @@ def _matrix(t, what, dtypes, device, rows, length):
             continue
         if step is None:
             step = s
-        elif s != n * step:
+        elif s != n * step and 0 not in shape:  # (of no rows at all nothing is spaced)
             even = False
         n *= size
     if not even or t.dtype not in dtypes or t.get_device() != device:

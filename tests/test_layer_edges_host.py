@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 torch = pytest.importorskip("torch")
+from test_cache8_edges_host import BF16, U8, Tensor
 from test_layer_host import binding, clsa  # noqa: F401 (fixtures)
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -92,3 +93,14 @@ def test_the_readme_makes_params_that_the_dense_calls_take(clsa):
     n = ctypes.c_size_t(0)
     for p in made:
         assert clsa.raw().clsa_dense_workspace_bytes(ctypes.byref(p), ctypes.byref(n)) in (0, 4)
+
+
+@pytest.mark.parametrize("shape", [(0, 256), (2, 0, 256), (0, 5, 256), (3, 0, 2, 256), (2, 2, 0, 256)])
+def test_the_binding_takes_batches_without_rows(binding, shape):  # noqa: F811
+    clsa, calls = binding
+    spec = clsa.make_add_norm(dim=256, scale_group=32)
+    t, c, e = Tensor(shape, BF16), Tensor(shape, U8), Tensor((*shape[:-1], 8), U8)
+    for args in ((t, None, None, t, None, None), (t, t, t, None, c, e)):
+        clsa.clsa_add_norm(spec, *args)
+        assert calls in (["clsa_add_norm"], ["native clsa_add_norm"])
+        calls.clear()
