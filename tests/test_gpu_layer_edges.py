@@ -156,3 +156,29 @@ def test_scales_and_queries_that_make_up_for_one_another(eight, power):
     out, lse, tol, ltol = p.want()
     ref.check_close(p.lse, lse, ltol, "lse")
     ref.check_close(p.out, out, tol, "out")
+
+
+@pytest.mark.parametrize("rows,dim,group", [(15, 512, 32), (3000, 1536, 128), (700, 4096, 4096)])
+def test_norm_codes_captured_and_replayed(rows, dim, group):
+    """Every output of the eager call, and of replays with other inputs."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(rows)
+    new = lambda: torch.randn((rows, dim), generator=g, device=DEV).to(torch.bfloat16)  # noqa: E731
+    x, r, s, y = new(), new(), new(), new()
+    weight = (1 + 0.2 * torch.randn(dim, generator=g, device=DEV)).to(torch.bfloat16)
+    codes, scales = torch.zeros((rows, dim), dtype=torch.uint8, device=DEV), torch.zeros((rows, dim // group), dtype=torch.uint8, device=DEV)
+    spec = clsa.make_add_norm(dim=dim, eps=1e-5, weight=weight, scale_group=group)
+    call = lambda: clsa.clsa_add_norm(spec, x, r, s, y, codes.view(torch.float8_e4m3fn), scales.view(torch.float8_e8m0fnu))  # noqa: E731
+    call()
+    check_add_norm(spec, x, r, weight, 1e-5, s, y, codes, scales, group)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for size in (1.0, 100.0):
+        x.copy_(new() * size)
+        r.copy_(new())
+        for t in (s, y, codes, scales):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        check_add_norm(spec, x, r, weight, 1e-5, s, y, codes, scales, group)
