@@ -16,12 +16,12 @@
 // Products are formed transposed, tokens along M of warp-level instructions:
 //   S^T[16 tokens x 8 columns] = K Q^T,   O^T[128 x 8 columns] += V^T P^T
 // Up to 16 columns that is enough to keep up with HBM. Beyond, a block's warps divide the columns, and the instruction rate decides: 64 columns run
-// at 0.23 PFLOP/s over bf16 rows, 0.20 over codes, which every column share converts for itself.
+// at 0.24 to 0.27 PFLOP/s over bf16 rows, 0.21 over codes, which every column share converts for itself.
 //
 // Softmax. One pass, in the log2 domain, relative to a reference per column that moves only when a weight would exceed 2^8 (one
 // vote per granule, no reduction over its tokens otherwise). Weights are rounded to what the matrix instruction takes beside V. bf16: two
 // parts of 8 bits each (p and what its rounding left) where that costs nothing, with up to 32 columns: the error of a single part is as
-// large as the output's own rounding; up to 4 columns are held twice and the second copy takes the second parts. 8-bit caches: f16,
+// large as the output's own rounding (beyond, it is taken: the products are the bound there, and a second part is half as many again); up to 4 columns are held twice and the second copy takes the second parts. 8-bit caches: f16,
 // 2^-11 of each weight, and 2^-36 of the largest one with its V's scale. Denominators are sums of the unrounded weights in fp32.
 // Granules that some query sees in part only run a second instance of the step: positions out of sight get logits of -inf, and V rows that nobody sees
 // are taken as zeros (a weight of 0 times a NaN is none). Blocks in which a sequence ends pay for it, and for an epilogue and
@@ -31,7 +31,7 @@
 // per warp: x = (d 2^(ek - 22)) qf with qf = 2^22 sm_scale / (the power of two that q was scaled by). As in the sparse attention,
 // numerators have a reference of their own, m near the largest x - mx + ev, and 2^m meets the finished quotient. Scale bytes come with their rows:
 // the fetching warp copies the words that they lie in, and the slot's barrier counts those copies (fetched by the consumers, 32 granules at a
-// time, they held up whoever began a sequence: 24 ragged sequences of up to 32768 tokens, 15 columns, 103 us then, 85 since).
+// time, they held up whoever began a sequence: 24 ragged sequences of up to 32768 tokens, 15 columns, 103 us, 85 with the words).
 //
 // Joining. A unit that lies in one stretch is finished by its block. Of the others every block leaves one record per column (128
 // unnormalised outputs, reference, sum, in fp32), and a second kernel, whose launch overlaps the first one's end, joins a row's records in
@@ -1388,7 +1388,7 @@ DensePlan make_dense_plan(const clsa_params& p, bool eight, int window, const De
   const int64_t reach = window > 0 && window < p.max_seq_len - p.q_per_seq ? window + p.q_per_seq + gran : p.max_seq_len;
   const double granules = (double)((reach + gran - 1) / gran);
   double best = 0.7 * granules * head_bytes * p.num_seqs * p.num_kv_heads / kRate + 14.0;
-  const double products = (eight ? 100e6 : 240e6) / d.columns;  // bytes per us that the GPU's products keep up with, as measured with 32 and 64 columns
+  const double products = (eight ? 100e6 : 265e6) / d.columns;  // bytes per us that the GPU's products keep up with (measured: 64 columns over bf16 241 to 271e6 / columns, 32 and 64 over codes 94e6 and 106e6)
   double block_rate = eight ? kBlockRate8 : kBlockRate;
   if (products / dev.sm_count < block_rate) block_rate = products / dev.sm_count;
   for (int h = most; h >= 1; h /= 2) {
