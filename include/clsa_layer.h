@@ -32,11 +32,13 @@ CLSA_API clsa_status clsa_dense_workspace_bytes(const clsa_params* p, size_t* by
  *                                (cross attention to states of another length, empty places of a batch)
  *     causal == 1                s <= seq_len[b] - T + t
  *     window  > 0                s >  seq_len[b] - T + t - window  as well: the query's own position and the window - 1 before it
- *   q   bf16 [B][T][Hq][D], 16-byte aligned;  out  bf16 [B][T][Hq][D], 16-byte aligned, rounded once from fp32
+ *   q   bf16 [B][T][Hq][D], 16-byte aligned;  out  bf16 [B][T][Hq][D], 16-byte aligned, rounded from fp32. Weights meet V in 16 bits (two
+ *       bf16) for up to 32 query columns (T * Hq/Hkv) of a KV head, in one bf16 for more: off by up to 2^-16 and 2^-8 of each
  *   lse fp32 [B][T][Hq] or NULL: log-sum-exp of the scaled logits (natural log); with it, results over two parts of a context join
  * A query that sees nothing yields zeros and lse = -inf. What lies in cache rows that a query does not see (rows behind the sequence,
  * in front of its window, other pages' rows) never reaches its result, NaN and infinities included. A NaN or an infinite logit among
  * the visible ones gives NaN, a logit of -inf has weight 0; an element of V that is not finite makes those outputs that see it not finite.
+ * Sums over V are divided by the weights' sum at their end: V's magnitudes times the rows seen stay below 2^119.
  * T <= 32 and T * Hq/Hkv <= 512; groups up to 16; D == 128. p->num_cache_rows, the extent of the row space, is required: a row
  * outside it, or of a page outside it, counts as not visible and flags CLSA_DEV_BAD_INDEX. A sequence with seq_len > max_seq_len or < T
  * (< 0 where window == 0 and causal == 0) counts as empty and flags CLSA_DEV_BAD_SEQLEN. idx_dim, top_k and the indexer's cache are not
@@ -48,7 +50,8 @@ CLSA_API clsa_status clsa_dense_attn(const clsa_params* p, int32_t window, const
 /* clsa_dense_attn over an 8-bit cache (its K and V; a sequence begins on a multiple of 16 rows, as every scale block makes it: flagged
  * CLSA_DEV_BAD_SCALE_BLOCK and counted as empty otherwise). Logits may have any size that is a float, for queries of magnitudes below
  * 2^118 / sm_scale; a query's elements below 2^-31 of its head's largest round to f16's last place. Weights meet V in f16: off by up to 2^-11
- * of each, and by up to 2^-36 of the largest weight times its V's scale. */
+ * of each, and by up to 2^-36 of the largest weight times its V's scale. Scale bytes are fetched by the aligned words of 4 that they lie in: up to
+ * 3 bytes in front of the first one are read (and not used), none behind the last. */
 CLSA_API clsa_status clsa_dense_attn8(const clsa_params* p, const clsa_cache8* c, int32_t window, const void* q, void* out, float* lse,
                                       void* workspace, size_t workspace_bytes, clsa_stream stream);
 

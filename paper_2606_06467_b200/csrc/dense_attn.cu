@@ -21,7 +21,7 @@
 // Softmax. One pass, in the log2 domain, relative to a reference per column that moves only when a weight would exceed 2^8 (one
 // vote per granule, no reduction over its tokens otherwise). Weights are rounded to what the matrix instruction takes beside V. bf16: two
 // parts of 8 bits each (p and what its rounding left) where that costs nothing, with up to 32 columns: the error of a single part is as
-// large as the output's own rounding (beyond, it is taken: the products are the bound there, and a second part is half as many again); up to 4 columns are held twice and the second copy takes the second parts. 8-bit caches: f16,
+// large as the output's own rounding (beyond, one: 16 sequences of 8192 tokens, 64 columns, 127 us with it and 157 with two); up to 4 columns are held twice and the second copy takes the second parts. 8-bit caches: f16,
 // 2^-11 of each weight, and 2^-36 of the largest one with its V's scale. Denominators are sums of the unrounded weights in fp32.
 // Granules that some query sees in part only run a second instance of the step: positions out of sight get logits of -inf, and V rows that nobody sees
 // are taken as zeros (a weight of 0 times a NaN is none). Blocks in which a sequence ends pay for it, and for an epilogue and
