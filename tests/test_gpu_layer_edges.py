@@ -100,7 +100,7 @@ def test_add_norm_in_place_over_many_rows(dim, group):
 
 
 def test_the_readme_runs():
-    """README.md's calls around a layer as they stand there, and their attention's results."""
+    """The documented calls around a layer as they stand there, and their attention's results."""
     text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
     block = text[text.index("### Around a layer"):].split("```python\n")[1].split("```")[0]
     g = torch.Generator(device=DEV)

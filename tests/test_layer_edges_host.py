@@ -70,8 +70,7 @@ def test_add_norm_refuses_outputs_that_share_memory(clsa):
 
 
 def test_the_readme_makes_params_that_the_dense_calls_take(clsa):
-    """README.md's calls around a layer, with stand-ins for what they launch: the params are complete (found on a GPU machine: nothing missing; here: no
-    device)."""
+    """The documented calls around a layer, with stand-ins for what they launch: the params are complete (0; 4 where there is no device)."""
     text = open(os.path.join(ROOT, "README.md")).read()
     block = text[text.index("### Around a layer"):].split("```python\n")[1].split("```")[0]
     made = []
